@@ -230,6 +230,51 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
                               int32_t n_split, void* d_q_scratch, float* d_out, size_t out_layer_stride,
                               int32_t advance, void* stream);
 
+/* ---- the cache held in 4 bits ---------------------------------------------------------------
+ * The same composition at half the width.  A cached row x of W numbers keeps codes c_i in 0..15, a step s and a middle
+ * z (both bf16), decided in fp32 with round-half-even from the row's largest and smallest number hi and lo:
+ *     z = bf16(hi / 2 + lo / 2),   s = bf16(max(hi - z, z - lo) / 7.5),   c_i = rint((x_i - z) (1 / s) + 7.5),
+ *     x_i ~ z + s (c_i - 7.5),     |x_i - (z + s (c_i - 7.5))| <= s / 2 up to fp32 rounding.
+ * The middle follows rows that are not centred (a K bias), which costs 2 bytes a row.  A step below 2^-126 counts as 0
+ * (the codes are 8 and the row reads back as z); a row that holds a NaN or an infinity, or whose range leaves fp32,
+ * reads back as NaN everywhere.  A row occupies rap_q4_row_bytes(W) = an odd number of 32-bit words >= (W + 1) / 2 + 4
+ * bytes: byte i holds code 2i in its low half and code 2i + 1 in its high half, then zeros (a spare half byte included),
+ * and the last word holds s (low half) and z (high half).  W <= 256.  Quantised caches are [B][H_kv][S_cap][row bytes],
+ * dense; q~ is not quantised.
+ *   rap_quantize_rows_q4    d_rows [n_rows][W] (dtype_in = RAP_F32 or RAP_BF16) -> d_q4 [n_rows][row bytes]; also the way
+ *                           to convert a layer's cache (n_rows = B * H_kv * S_cap).  RAP_ESHAPE if W > 256.
+ *   rap_dequantize_rows_q4  the way back: d_q4 -> d_rows [n_rows][W], rounded once to dtype_out.
+ *   rap_read_cache_q4       rows [0, d_seq_len[b]) of every sequence of a layer's K and V cache -> compact caches in the
+ *                           storage dtype (d_k_cache, d_v_cache as in rap_decode_attn, same S_cap), for calls that take
+ *                           those (rap_prefill_attn over a quantised prefix).  Rows from d_seq_len[b] on are neither read
+ *                           nor written.  h_seq_len_max: the caller's bound on d_seq_len (<= S_cap).
+ *   rap_qkv_rope_append_q4  rap_qkv_rope_append with the new K and V rows quantised straight from their fp32 values; q~
+ *                           as in rap_qkv_rope_append.  The rows of one call name distinct (sequence, slot) pairs.
+ *   rap_decode_attn_q4      rap_decode_attn over quantised caches (Eq. 2 on the values above; a row's weight stays fp32
+ *                           to about 2^-22).  Rows past a sequence's length may hold anything.
+ *   rap_decode_step_q4      rap_decode_step over quantised caches (h_k4 / h_v4: HOST arrays of L device pointers).
+ * Arguments, errors and stream behaviour as for the unquantised calls; RAP_EINVAL when the current device is not the
+ * one the context was created on. */
+size_t rap_q4_row_bytes(int32_t W);
+rap_status rap_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, int64_t n_rows, int32_t W, const void* d_rows, void* d_q4,
+                                void* stream);
+rap_status rap_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, int64_t n_rows, int32_t W, const void* d_q4, void* d_rows,
+                                  void* stream);
+rap_status rap_read_cache_q4(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_k4, const void* d_v4, int32_t S_cap,
+                             const int32_t* d_seq_len, int32_t h_seq_len_max, void* d_k_cache, void* d_v_cache, void* stream);
+rap_status rap_qkv_rope_append_q4(rap_ctx* ctx, int32_t layer, int32_t T, const void* d_x, const void* d_w_qkv,
+                                  const void* d_bias, const int32_t* d_seq_id, const int32_t* d_pos,
+                                  const int32_t* d_slot, int32_t h_slot_max, const double* d_inv_freq, void* d_q_out,
+                                  void* d_k4, void* d_v4, int32_t B_cache, int32_t S_cap, void* stream);
+rap_status rap_decode_attn_q4(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_q, const void* d_k4, const void* d_v4,
+                              int32_t S_cap, const int32_t* d_seq_len, int32_t h_seq_len_max, int32_t n_split,
+                              float* d_out, void* stream);
+rap_status rap_decode_step_q4(rap_ctx* ctx, int32_t B, const void* d_x, const void* const* h_w_qkv,
+                              const void* const* h_bias, const double* d_inv_freq, void* const* h_k4,
+                              void* const* h_v4, int32_t S_cap, int32_t* d_seq_len, int32_t h_seq_len_max,
+                              int32_t n_split, void* d_q_scratch, float* d_out, size_t out_layer_stride,
+                              int32_t advance, void* stream);
+
 /* ---- decode attention without any allocation (the paper has no counterpart) --------------
  * Same result as rap_decode_attn, for callers that cannot allocate device memory: code running
  * inside someone else's memory budget (a serving engine that hands out every byte of HBM up

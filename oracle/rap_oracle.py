@@ -659,6 +659,53 @@ def kv_bytes_per_token_q8(n_layers, n_kv_heads, k_width, v_width):
 
 
 # --------------------------------------------------------------------------------------
+# the same composition at 4 bits
+# --------------------------------------------------------------------------------------
+def quantize_rows_q4(x):
+    """4-bit round-to-nearest quantisation of cache rows around a middle, one step and one middle per row.
+
+    Reading (the paper fixes no cache format; a row keeps 16 levels, spread evenly around its middle): with hi, lo the
+    largest and smallest of the row,
+        z  = bf16( hi / 2 + lo / 2 ),    s = bf16( max(hi - z, z - lo) / 7.5 ),
+        c_i = rint( (x_i - z) (1 / s) + 7.5 )  in 0..15,    x_i ~ z + s (c_i - 7.5),
+    each operation in fp32, half to even.  s below 2^-126 counts as 0 (c = 8); a row that is not finite, or whose range
+    is not, has s = z = NaN (c = 8).
+    x [..., W] -> (codes uint8 [..., W], steps fp64 [...], middles fp64 [...]; both hold bf16 values)."""
+    f = np.float32
+    x32 = np.asarray(x, dtype=f)
+    with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
+        hi, lo = x32.max(axis=-1), x32.min(axis=-1)
+        z = round_bf16(hi * f(0.5) + lo * f(0.5)).astype(f)
+        s = round_bf16(np.maximum(hi - z, z - lo) / f(7.5)).astype(f)
+        bad = ~(s < np.inf)
+        s = np.where(s < f(2.0 ** -126), f(0), s)
+        r = np.where(s > 0, f(1) / s, f(0)).astype(f)
+        t = ((x32 - z[..., None]) * r[..., None] + f(7.5)).astype(f)
+        c = np.where(bad[..., None], 8.0, np.rint(t))
+    nan = np.where(bad, np.nan, 0.0)
+    return c.astype(np.uint8), s.astype(np.float64) + nan, z.astype(np.float64) + nan
+
+
+def dequantize_rows_q4(codes, steps, middles):
+    """x_i = z + s (c_i - 7.5), fp64."""
+    c = np.asarray(codes, dtype=np.float64) - 7.5
+    return np.asarray(middles, dtype=np.float64)[..., None] + np.asarray(steps, dtype=np.float64)[..., None] * c
+
+
+def decode_attn_q4(q, k_held, v_held, seq_len, head_dim):
+    """Eq. 2 on the reduced dims over a cache held in 4 bits: decode_attn on the values the rows stand for; k_held and
+    v_held are (codes, steps, middles) triples, q is not quantised."""
+    return decode_attn(q, dequantize_rows_q4(*k_held), dequantize_rows_q4(*v_held), seq_len, head_dim)
+
+
+def kv_bytes_per_token_q4(n_layers, n_kv_heads, k_width, v_width):
+    """Resident bytes per token of the 4-bit cache as the library lays it out: per row two codes a byte, then a word of
+    step and middle, in an odd number of 32-bit words."""
+    row = lambda w: 4 * ((((w + 1) // 2 + 4 + 3) // 4) | 1)
+    return n_layers * n_kv_heads * (row(k_width) + row(v_width))
+
+
+# --------------------------------------------------------------------------------------
 # closed-form accounting (Table 3 cost model; Table 15 bytes per token)
 # --------------------------------------------------------------------------------------
 def kv_bytes_per_token(n_layers, n_kv_heads, k_width, v_width, elem_bytes):

@@ -29,6 +29,8 @@ EXPORTS = [
     "rap_pack_wo", "rap_out_proj", "rap_budget_alloc", "rap_prefill_attn", "rap_build_tables_hybrid",
     "rap_build_tables_partial", "rap_build_tables_freq", "rap_set_proj_variant", "rap_debug_arm_wait_timeout", "rap_debug_claim_scan_workspace", "rap_debug_set_scan_pieces",
     "rap_q8_row_bytes", "rap_quantize_rows", "rap_qkv_rope_append_q8", "rap_decode_attn_q8", "rap_decode_step_q8",
+    "rap_q4_row_bytes", "rap_quantize_rows_q4", "rap_dequantize_rows_q4", "rap_read_cache_q4", "rap_qkv_rope_append_q4",
+    "rap_decode_attn_q4", "rap_decode_step_q4",
 ]
 
 
@@ -93,6 +95,14 @@ def _lib():
     lib.rap_qkv_rope_append_q8.argtypes = lib.rap_qkv_rope_append.argtypes
     lib.rap_decode_attn_q8.argtypes = lib.rap_decode_attn.argtypes
     lib.rap_decode_step_q8.argtypes = lib.rap_decode_step.argtypes
+    lib.rap_q4_row_bytes.argtypes = [c_int32]
+    lib.rap_q4_row_bytes.restype = c_size_t
+    lib.rap_quantize_rows_q4.argtypes = lib.rap_quantize_rows.argtypes
+    lib.rap_dequantize_rows_q4.argtypes = lib.rap_quantize_rows.argtypes
+    lib.rap_read_cache_q4.argtypes = [P, c_int32, c_int32, P, P, c_int32, P, c_int32, P, P, P]
+    lib.rap_qkv_rope_append_q4.argtypes = lib.rap_qkv_rope_append.argtypes
+    lib.rap_decode_attn_q4.argtypes = lib.rap_decode_attn.argtypes
+    lib.rap_decode_step_q4.argtypes = lib.rap_decode_step.argtypes
     lib.rap_budget_alloc.argtypes = [c_int32, c_int32, c_int32, P, c_double, P, P]
     lib.rap_prefill_attn.argtypes = [P, c_int32, c_int32, c_int32, P, P, P, c_int32, P, c_int32, P, P]
     lib.rap_pack_wo.argtypes = [P, c_int32, P, P, P, P]
@@ -152,6 +162,10 @@ def rap_budget_alloc(k_pair_scores, rho, head_dim):
 
 def rap_q8_row_bytes(W):
     return int(_lib().rap_q8_row_bytes(W))
+
+
+def rap_q4_row_bytes(W):
+    return int(_lib().rap_q4_row_bytes(W))
 
 
 def rap_cache_elem_offset(n_kv_heads, S_cap, W, b, h, pos, c):
@@ -285,6 +299,30 @@ class RapContext:
                                               _ptr(d_seq_len), h_seq_len_max, n_split, _ptr(d_out), _stream()),
                     "rap_decode_attn_q8")
 
+    def rap_quantize_rows_q4(self, dtype_in, n_rows, W, d_rows, d_q4):
+        self._check(_lib().rap_quantize_rows_q4(self._ctx, dtype_in, n_rows, W, _ptr(d_rows), _ptr(d_q4), _stream()),
+                    "rap_quantize_rows_q4")
+
+    def rap_dequantize_rows_q4(self, dtype_out, n_rows, W, d_q4, d_rows):
+        self._check(_lib().rap_dequantize_rows_q4(self._ctx, dtype_out, n_rows, W, _ptr(d_q4), _ptr(d_rows), _stream()),
+                    "rap_dequantize_rows_q4")
+
+    def rap_read_cache_q4(self, layer, B, d_k4, d_v4, S_cap, d_seq_len, h_seq_len_max, d_k_cache, d_v_cache):
+        self._check(_lib().rap_read_cache_q4(self._ctx, layer, B, _ptr(d_k4), _ptr(d_v4), S_cap, _ptr(d_seq_len), h_seq_len_max,
+                                             _ptr(d_k_cache), _ptr(d_v_cache), _stream()), "rap_read_cache_q4")
+
+    def rap_qkv_rope_append_q4(self, layer, T, d_x, d_w_qkv, d_bias, d_seq_id, d_pos, d_slot, h_slot_max, d_inv_freq,
+                               d_q_out, d_k4, d_v4, B_cache, S_cap):
+        self._check(_lib().rap_qkv_rope_append_q4(self._ctx, layer, T, _ptr(d_x), _ptr(d_w_qkv), _ptr(d_bias),
+                                                  _ptr(d_seq_id), _ptr(d_pos), _ptr(d_slot), h_slot_max,
+                                                  _ptr(d_inv_freq), _ptr(d_q_out), _ptr(d_k4), _ptr(d_v4), B_cache,
+                                                  S_cap, _stream()), "rap_qkv_rope_append_q4")
+
+    def rap_decode_attn_q4(self, layer, B, d_q, d_k4, d_v4, S_cap, d_seq_len, h_seq_len_max, n_split, d_out):
+        self._check(_lib().rap_decode_attn_q4(self._ctx, layer, B, _ptr(d_q), _ptr(d_k4), _ptr(d_v4), S_cap,
+                                              _ptr(d_seq_len), h_seq_len_max, n_split, _ptr(d_out), _stream()),
+                    "rap_decode_attn_q4")
+
     def rap_decode_step(self, B, d_x, w_qkv, bias, d_inv_freq, k_cache, v_cache, S_cap, d_seq_len,
                         h_seq_len_max, n_split, d_q_scratch, d_out, out_layer_stride, advance):
         """w_qkv / bias / k_cache / v_cache: per-layer lists of tensors, or prebuilt pointer arrays."""
@@ -300,6 +338,13 @@ class RapContext:
         self._check(_lib().rap_decode_step_q8(self._ctx, B, _ptr(d_x), args[0], args[1], _ptr(d_inv_freq), args[2], args[3],
                                               S_cap, _ptr(d_seq_len), h_seq_len_max, n_split, _ptr(d_q_scratch),
                                               _ptr(d_out), out_layer_stride, advance, _stream()), "rap_decode_step_q8")
+
+    def rap_decode_step_q4(self, B, d_x, w_qkv, bias, d_inv_freq, k4, v4, S_cap, d_seq_len, h_seq_len_max, n_split,
+                           d_q_scratch, d_out, out_layer_stride, advance):
+        args = [a if isinstance(a, ctypes.Array) or a is None else _ptr_array(a) for a in (w_qkv, bias, k4, v4)]
+        self._check(_lib().rap_decode_step_q4(self._ctx, B, _ptr(d_x), args[0], args[1], _ptr(d_inv_freq), args[2], args[3],
+                                              S_cap, _ptr(d_seq_len), h_seq_len_max, n_split, _ptr(d_q_scratch),
+                                              _ptr(d_out), out_layer_stride, advance, _stream()), "rap_decode_step_q4")
 
     def rap_decode_step_host(self, B, h_x, w_qkv, bias, d_inv_freq, k_cache, v_cache, S_cap, d_seq_len,
                              h_seq_len_max, n_split, h_out, out_layer_stride, advance):

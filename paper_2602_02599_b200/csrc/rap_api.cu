@@ -580,6 +580,148 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
   return RAP_OK;
 }
 
+// ---- the cache held in 4 bits -------------------------------------------------------------------------------------------
+// the context's buffers and streams belong to the device it was created on
+static rap_status on_own_device(rap_ctx* ctx) {
+  int dev = -1;
+  RAP_CUDA_TRY(ctx, cudaGetDevice(&dev));
+  return dev == ctx->device ? RAP_OK : RAP_EINVAL;
+}
+
+size_t rap_q4_row_bytes(int32_t W) { return W < 1 ? 0 : 4 * (((((size_t)W + 1) / 2 + 4 + 3) / 4) | 1); }
+
+// shared by the two directions; an empty call is not checked further by the callers
+static rap_status rows_q4_check(rap_ctx* ctx, int32_t dtype, int64_t n_rows, int32_t W, const void* from, const void* to) {
+  if (!ctx || !from || !to) return RAP_EINVAL;
+  if ((dtype != RAP_F32 && dtype != RAP_BF16) || n_rows < 0 || W < 1) return RAP_EINVAL;
+  if (!rap_aligned16(from) || !rap_aligned16(to)) return RAP_EALIGN;
+  if (W > 256 || (n_rows + 7) / 8 > 0x7fffffffLL) return RAP_ESHAPE;
+  return on_own_device(ctx);
+}
+
+rap_status rap_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, int64_t n_rows, int32_t W, const void* d_rows, void* d_q4,
+                                void* stream) {
+  const rap_status s = rows_q4_check(ctx, dtype_in, n_rows, W, d_rows, d_q4);
+  if (s != RAP_OK || n_rows == 0) return s;
+  return rap_launch_quantize_rows_q4(ctx, dtype_in, n_rows, W, d_rows, d_q4, (cudaStream_t)stream);
+}
+
+rap_status rap_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, int64_t n_rows, int32_t W, const void* d_q4, void* d_rows,
+                                  void* stream) {
+  const rap_status s = rows_q4_check(ctx, dtype_out, n_rows, W, d_q4, d_rows);
+  if (s != RAP_OK || n_rows == 0) return s;
+  return rap_launch_dequantize_rows_q4(ctx, dtype_out, n_rows, W, d_q4, d_rows, (cudaStream_t)stream);
+}
+
+rap_status rap_read_cache_q4(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_k4, const void* d_v4, int32_t S_cap,
+                             const int32_t* d_seq_len, int32_t h_seq_len_max, void* d_k_cache, void* d_v_cache, void* stream) {
+  if (!ctx || !d_k4 || !d_v4 || !d_seq_len || !d_k_cache || !d_v_cache) return RAP_EINVAL;
+  if (!ctx->tables_built) return RAP_ESTATE;
+  const rap_model_desc& d = ctx->desc;
+  if (layer < 0 || layer >= d.n_layers || B < 0 || S_cap < 1 || h_seq_len_max < 0) return RAP_EINVAL;
+  if (B > d.max_batch) return RAP_ESHAPE;
+  if (S_cap % 8) return RAP_EALIGN;
+  if (h_seq_len_max > S_cap) return RAP_ECAPACITY;
+  if (!rap_aligned16(d_k4) || !rap_aligned16(d_v4) || !rap_aligned16(d_seq_len) || !rap_aligned16(d_k_cache) ||
+      !rap_aligned16(d_v_cache))
+    return RAP_EALIGN;
+  const rap_status s = on_own_device(ctx);
+  if (s != RAP_OK || B == 0 || h_seq_len_max == 0) return s;
+  return rap_launch_read_cache_q4(ctx, d.dtype, B, d.n_kv_heads, S_cap, 2 * ctx->n_pairs[layer], ctx->n_vch[layer], d_k4, d_v4,
+                                  d_seq_len, h_seq_len_max, d_k_cache, d_v_cache, (cudaStream_t)stream);
+}
+
+rap_status rap_qkv_rope_append_q4(rap_ctx* ctx, int32_t layer, int32_t T, const void* d_x, const void* d_w_qkv,
+                                  const void* d_bias, const int32_t* d_seq_id, const int32_t* d_pos, const int32_t* d_slot,
+                                  int32_t h_slot_max, const double* d_inv_freq, void* d_q_out, void* d_k4, void* d_v4,
+                                  int32_t B_cache, int32_t S_cap, void* stream) {
+  if (!ctx || !d_x || !d_w_qkv || !d_seq_id || !d_pos || !d_slot || !d_inv_freq || !d_q_out || !d_k4 || !d_v4)
+    return RAP_EINVAL;
+  if (!ctx->tables_built) return RAP_ESTATE;
+  const rap_model_desc& d = ctx->desc;
+  if (layer < 0 || layer >= d.n_layers || T < 0 || B_cache < 1 || S_cap < 1) return RAP_EINVAL;
+  if (T > d.max_rows) return RAP_ESHAPE;
+  if (S_cap % 8) return RAP_EALIGN;
+  if (h_slot_max < 0) return RAP_EINVAL;
+  if (h_slot_max >= S_cap) return RAP_ECAPACITY;
+  if (!rap_aligned16(d_x) || !rap_aligned16(d_w_qkv) || !rap_aligned16(d_q_out) || !rap_aligned16(d_k4) ||
+      !rap_aligned16(d_v4) || !rap_aligned16(d_inv_freq) || (d_bias && !rap_aligned16(d_bias)))
+    return RAP_EALIGN;
+  const rap_status s = on_own_device(ctx);
+  if (s != RAP_OK || T == 0) return s;
+  rap_proj_args a;
+  a.x = d_x; a.w = d_w_qkv; a.bias = d_bias;
+  a.seq_id = d_seq_id; a.pos = d_pos; a.slot = d_slot;
+  a.inv_freq = d_inv_freq + (size_t)layer * d.n_kv_heads * (d.head_dim / 2);
+  a.q_out = d_q_out; a.k_cache = d_k4; a.v_cache = d_v4;
+  a.T = T; a.hidden = d.hidden; a.Hq = d.n_q_heads; a.Hkv = d.n_kv_heads;
+  a.P2 = 2 * ctx->n_pairs[layer]; a.dv = ctx->n_vch[layer]; a.half_dim = d.head_dim / 2;
+  a.B_cache = B_cache; a.S_cap = S_cap; a.dtype = d.dtype;
+  return rap_launch_qkv_rope_append_q4(ctx, a, (cudaStream_t)stream);
+}
+
+rap_status rap_decode_attn_q4(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_q, const void* d_k4, const void* d_v4,
+                              int32_t S_cap, const int32_t* d_seq_len, int32_t h_seq_len_max, int32_t n_split, float* d_out,
+                              void* stream) {
+  if (!ctx || !d_q || !d_k4 || !d_v4 || !d_seq_len || !d_out) return RAP_EINVAL;
+  if (!ctx->tables_built) return RAP_ESTATE;
+  const rap_model_desc& d = ctx->desc;
+  if (layer < 0 || layer >= d.n_layers || B < 0 || S_cap < 1 || n_split < 0 || h_seq_len_max < 0) return RAP_EINVAL;
+  if (B > d.max_batch || n_split > RAP_MAX_SPLIT) return RAP_ESHAPE;
+  if (S_cap % 8) return RAP_EALIGN;
+  if (h_seq_len_max > S_cap) return RAP_ECAPACITY;
+  if (!rap_aligned16(d_q) || !rap_aligned16(d_k4) || !rap_aligned16(d_v4) || !rap_aligned16(d_out) || !rap_aligned16(d_seq_len))
+    return RAP_EALIGN;
+  const rap_status s = on_own_device(ctx);
+  if (s != RAP_OK || B == 0) return s;
+  rap_attn_args a;
+  a.q = d_q; a.k = d_k4; a.v = d_v4; a.seq_len = d_seq_len; a.len_add = 0;
+  a.B = B; a.Hq = d.n_q_heads; a.Hkv = d.n_kv_heads; a.P2 = 2 * ctx->n_pairs[layer]; a.dv = ctx->n_vch[layer];
+  a.S_cap = S_cap; a.head_dim = d.head_dim; a.dtype = d.dtype; a.n_split = n_split; a.h_len_max = h_seq_len_max;
+  a.out = d_out;
+  return rap_launch_attn_q4(ctx, a, (cudaStream_t)stream);
+}
+
+static rap_status decode_step_check(rap_ctx* ctx, int32_t B, const void* d_x, const void* const* h_w_qkv,
+                                    const void* const* h_bias, const double* d_inv_freq, void* const* h_k_cache,
+                                    void* const* h_v_cache, int32_t S_cap, int32_t* d_seq_len, int32_t h_seq_len_max,
+                                    int32_t n_split, void* d_q_scratch, float* d_out, size_t out_layer_stride);
+
+rap_status rap_decode_step_q4(rap_ctx* ctx, int32_t B, const void* d_x, const void* const* h_w_qkv, const void* const* h_bias,
+                              const double* d_inv_freq, void* const* h_k4, void* const* h_v4, int32_t S_cap,
+                              int32_t* d_seq_len, int32_t h_seq_len_max, int32_t n_split, void* d_q_scratch, float* d_out,
+                              size_t out_layer_stride, int32_t advance, void* stream) {
+  rap_status s = decode_step_check(ctx, B, d_x, h_w_qkv, h_bias, d_inv_freq, h_k4, h_v4, S_cap, d_seq_len, h_seq_len_max, n_split,
+                                   d_q_scratch, d_out, out_layer_stride);
+  if (s != RAP_OK) return s;
+  if ((s = on_own_device(ctx)) != RAP_OK || B == 0) return s;
+  const rap_model_desc& d = ctx->desc;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t e = rap_elem_bytes(d.dtype);
+  for (int l = 0; l < d.n_layers; ++l) {
+    rap_proj_args p;
+    p.x = (const char*)d_x + (size_t)l * B * d.hidden * e;
+    p.w = h_w_qkv[l]; p.bias = h_bias ? h_bias[l] : nullptr;
+    p.seq_id = nullptr; p.pos = d_seq_len; p.slot = nullptr;   // decode mode: row r = sequence r at pos = slot = len
+    p.inv_freq = d_inv_freq + (size_t)l * d.n_kv_heads * (d.head_dim / 2);
+    p.q_out = d_q_scratch; p.k_cache = h_k4[l]; p.v_cache = h_v4[l];
+    p.T = B; p.hidden = d.hidden; p.Hq = d.n_q_heads; p.Hkv = d.n_kv_heads;
+    p.P2 = 2 * ctx->n_pairs[l]; p.dv = ctx->n_vch[l]; p.half_dim = d.head_dim / 2;
+    p.B_cache = B; p.S_cap = S_cap; p.dtype = d.dtype;
+    p.pdl = l > 0 ? 1 : 0;     // the GEMM of layer l may stream its weights while the scan of layer l - 1 drains
+    if ((s = rap_launch_qkv_rope_append_q4(ctx, p, st)) != RAP_OK) return s;
+    rap_attn_args a;
+    a.q = d_q_scratch; a.k = h_k4[l]; a.v = h_v4[l]; a.seq_len = d_seq_len; a.len_add = 1;
+    a.B = B; a.Hq = d.n_q_heads; a.Hkv = d.n_kv_heads; a.P2 = p.P2; a.dv = p.dv; a.S_cap = S_cap;
+    a.head_dim = d.head_dim; a.dtype = d.dtype; a.n_split = n_split; a.h_len_max = h_seq_len_max + 1;
+    a.out = d_out + (size_t)l * out_layer_stride;
+    a.pdl = 1;
+    if ((s = rap_launch_attn_q4(ctx, a, st)) != RAP_OK) return s;
+  }
+  if (advance) return rap_launch_advance(ctx, d_seq_len, B, st);
+  return RAP_OK;
+}
+
 rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, const void* d_q, const void* d_k_cache,
                             const void* d_v_cache, int32_t S_cap, const int32_t* d_start, int32_t h_start_max,
                             float* d_out, void* stream) {

@@ -194,3 +194,13 @@ rap_status rap_launch_quantize_rows(rap_ctx* ctx, int32_t dtype_in, long long n_
                                     cudaStream_t st);
 rap_status rap_launch_qkv_rope_append_q8(rap_ctx* ctx, const rap_proj_args& a, cudaStream_t st);
 rap_status rap_launch_attn_q8(rap_ctx* ctx, const rap_attn_args& a, cudaStream_t st);
+
+// cache held in 4 bits (rap_q4.cu)
+rap_status rap_launch_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, long long n_rows, int W, const void* src, void* dst,
+                                       cudaStream_t st);
+rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long long n_rows, int W, const void* src, void* dst,
+                                         cudaStream_t st);
+rap_status rap_launch_read_cache_q4(rap_ctx* ctx, int dtype, int B, int Hkv, int S_cap, int P2, int dv, const void* k4, const void* v4,
+                                    const int32_t* seq_len, int len_max, void* k, void* v, cudaStream_t st);
+rap_status rap_launch_qkv_rope_append_q4(rap_ctx* ctx, const rap_proj_args& a, cudaStream_t st);
+rap_status rap_launch_attn_q4(rap_ctx* ctx, const rap_attn_args& a, cudaStream_t st);

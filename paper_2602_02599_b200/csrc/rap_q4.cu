@@ -1,0 +1,427 @@
+// The cache held in 4 bits (format: rap_q4_common.cuh): conversion of rows and of a layer's cache in both directions, the
+// RoPE / append epilogue that quantises new K and V rows straight from their fp32 values, and the shape-generic split-KV
+// attention over a 4-bit cache.
+#include "rap_q4_common.cuh"
+
+rap_status rap_launch_proj_tc(rap_ctx* ctx, const rap_proj_args& a, int* ksplit_out, cudaStream_t st);
+rap_status rap_launch_proj_generic(rap_ctx* ctx, const rap_proj_args& a, cudaStream_t st);
+
+namespace {
+
+__device__ __forceinline__ float warp_max_nan(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = q4_max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_min_nan(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = q4_min(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+// One warp per row, one lane per word of eight codes.
+template <typename T>
+__global__ void __launch_bounds__(256) quantize_rows_q4_kernel(const T* __restrict__ src, uint32_t* __restrict__ dst,
+                                                               long long n_rows, int W) {
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (row >= n_rows) return;
+  const T* x = src + row * W;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = q4_ld(x + min(8 * lane + i, W - 1));      // past the end: the last element again
+  float hi = v[0], lo = v[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    hi = q4_max(hi, v[i]);
+    lo = q4_min(lo, v[i]);
+  }
+  const Q4Row q = q4_decide(warp_max_nan(hi), warp_min_nan(lo));
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (8 * lane + i < W) word |= q4_code(v[i], q) << (4 * i);
+  const int nw = q4_row_words(W);
+  uint32_t* d = dst + row * nw;
+  if (lane < nw - 1) d[lane] = word;
+  if (lane == 0) d[nw - 1] = q.sz;
+}
+
+template <typename T>
+__device__ __forceinline__ void dequantize_row(const uint32_t* __restrict__ src, T* __restrict__ dst, int W, int lane) {
+  const int nw = q4_row_words(W);
+  const uint32_t sz = src[nw - 1];
+  if (8 * lane >= W) return;
+  const uint32_t word = src[lane];
+  const float s = q4_step(sz), z = q4_middle(sz);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (8 * lane + i < W) q4_st(dst + 8 * lane + i, fmaf(s, (float)((word >> (4 * i)) & 15u) - 7.5f, z));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) dequantize_rows_q4_kernel(const uint32_t* __restrict__ src, T* __restrict__ dst,
+                                                                 long long n_rows, int W) {
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= n_rows) return;
+  dequantize_row(src + row * q4_row_words(W), dst + row * W, W, threadIdx.x & 31);
+}
+
+// A layer's K rows (blockIdx.z = 0) and V rows (1), up to every sequence's length: grid (rows of a unit / 8, units, 2)
+template <typename T>
+__global__ void __launch_bounds__(256)
+read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict__ v4, T* __restrict__ k, T* __restrict__ v,
+                     const int32_t* __restrict__ seq_len, int Hkv, int S_cap, int P2, int dv) {
+  const int pos = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int unit = blockIdx.y;
+  const int len = min(seq_len[unit / Hkv], S_cap);
+  if (pos >= len) return;
+  const size_t row = (size_t)unit * S_cap + pos;
+  if (blockIdx.z == 0) dequantize_row(k4 + row * q4_row_words(P2), k + row * P2, P2, threadIdx.x & 31);
+  else dequantize_row(v4 + row * q4_row_words(dv), v + row * dv, dv, threadIdx.x & 31);
+}
+
+// RoPE / append epilogue with quantisation.  One warp per (row t, item): items are the H_q query heads (rotated, rounded
+// to the storage dtype, written to q_out as in the unquantised path), then the H_kv key heads (rotated in fp32, quantised,
+// appended), then the H_kv value heads (quantised, appended).  A lane owns pairs of neighbouring numbers, that is whole
+// bytes of a quantised row: P <= 128, d_v' <= 256, so at most four.  y holds `ksplit` partial results, each [T][n_out].
+template <typename T>
+__global__ void __launch_bounds__(256)
+rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restrict__ bias, const int32_t* __restrict__ seq_id,
+                      const int32_t* __restrict__ pos, const int32_t* __restrict__ slot, const double* __restrict__ inv_freq,
+                      T* __restrict__ q_out, uint32_t* __restrict__ k4, uint32_t* __restrict__ v4, int Trows, int Hq, int Hkv,
+                      int P2, int dv, int half_dim, int B_cache, int S_cap, int32_t* __restrict__ status) {
+  // launched behind the GEMM with programmatic serialization inside a decode step: nothing above this line touches
+  // memory; the GEMM's results (and, through the GEMM, the end of the scan before it) are awaited here
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int items = Hq + 2 * Hkv;
+  const long long wid = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (wid >= (long long)Trows * items) return;
+  const int t = (int)(wid / items), item = (int)(wid - (long long)t * items);
+  const int P = P2 >> 1, G = Hq / Hkv;
+  const int n_out = (Hq + Hkv) * P2 + Hkv * dv;
+  const int p = pos[t];
+  const int sq = seq_id ? seq_id[t] : t;
+  const int sl = slot ? slot[t] : p;
+  const bool row_ok = (sq >= 0 && sq < B_cache && sl >= 0 && sl < S_cap);
+  if (!row_ok && item == 0 && lane == 0) {
+    atomicCAS(&status[0], 0, (int)RAP_ECAPACITY);
+    status[1] = t;
+  }
+  const bool is_v = item >= Hq + Hkv, is_q = item < Hq;
+  if (!is_q && !row_ok) return;
+  const int h = is_q ? item / G : is_v ? item - Hq - Hkv : item - Hq;
+  const int col0 = is_v ? (Hq + Hkv) * P2 + h * dv : item * P2;      // q heads, then k heads: item * 2P either way
+  const int W = is_v ? dv : P2;
+  const size_t split_stride = (size_t)Trows * n_out;
+  const float* yr = y + (size_t)t * n_out + col0;
+  // every partial of this lane's numbers first (independent loads), then the sums in split order and the bias
+  float pa[4][RAP_MAX_KSPLIT], pb[4][RAP_MAX_KSPLIT];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int s = 0; s < RAP_MAX_KSPLIT; ++s) {
+      const int c = 2 * (lane + 32 * k);
+      pa[k][s] = (c < W && s < ksplit) ? yr[s * split_stride + c] : 0.f;
+      pb[k][s] = (c + 1 < W && s < ksplit) ? yr[s * split_stride + c + 1] : 0.f;
+    }
+  float a[4], b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int c = 2 * (lane + 32 * k);
+    a[k] = b[k] = 0.f;
+#pragma unroll
+    for (int s = 0; s < RAP_MAX_KSPLIT; ++s)
+      if (s < ksplit) { a[k] += pa[k][s]; b[k] += pb[k][s]; }
+    if (bias && c < W) a[k] += q4_ld(bias + col0 + c);
+    if (bias && c + 1 < W) b[k] += q4_ld(bias + col0 + c + 1);
+    if (!is_v && c < W) {
+      // fp64 angle and reduction to [-pi, pi], fp32 sine and cosine of the reduced angle (as in the unquantised path)
+      const double ang = (double)p * inv_freq[h * half_dim + (c >> 1)];
+      const double turns = rint(ang * 0.15915494309189535);
+      const double red = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, ang));
+      float sf, cf;
+      sincosf((float)red, &sf, &cf);
+      const float x0 = a[k], x1 = b[k];
+      a[k] = fmaf(-x1, sf, __fmul_rn(x0, cf));          // the same roundings as the unquantised kernels
+      b[k] = fmaf(x0, sf, __fmul_rn(x1, cf));
+    }
+  }
+  if (is_q) {
+    T* dst = q_out + ((size_t)t * Hq + item) * P2;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = 2 * (lane + 32 * k);
+      if (c < W) {
+        q4_st(dst + c, a[k]);
+        q4_st(dst + c + 1, b[k]);
+      }
+    }
+    return;
+  }
+  float hi = -INFINITY, lo = INFINITY;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int c = 2 * (lane + 32 * k);
+    if (c < W) { hi = q4_max(hi, a[k]); lo = q4_min(lo, a[k]); }
+    if (c + 1 < W) { hi = q4_max(hi, b[k]); lo = q4_min(lo, b[k]); }
+  }
+  const Q4Row q = q4_decide(warp_max_nan(hi), warp_min_nan(lo));
+  const int nw = q4_row_words(W);
+  uint32_t* row = (is_v ? v4 : k4) + (((size_t)sq * Hkv + h) * S_cap + sl) * (size_t)nw;
+  unsigned char* bytes = reinterpret_cast<unsigned char*>(row);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = lane + 32 * k, c = 2 * i;
+    if (c < W) bytes[i] = (unsigned char)(q4_code(a[k], q) | (c + 1 < W ? q4_code(b[k], q) << 4 : 0u));
+    else if (i < 4 * (nw - 1)) bytes[i] = 0;
+  }
+  if (lane == 0) row[nw - 1] = q.sz;
+}
+
+// ---- shape-generic split-KV attention over a 4-bit cache: fp32 q~, rows wider than 128, and the cross-check ----------
+constexpr int Q4G_TILE = 64;
+constexpr int Q4G_THREADS = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(Q4G_THREADS)
+attn_q4_generic_kernel(const T* __restrict__ q, const unsigned char* __restrict__ k4, const unsigned char* __restrict__ v4,
+                       const int32_t* __restrict__ seq_len, int len_add, int Hq, int Hkv, int P2, int dv, int S_cap,
+                       float qscale, int n_split, float* __restrict__ ws) {
+  extern __shared__ float smem[];
+  const int G = Hq / Hkv;
+  const int kb_row = 4 * q4_row_words(P2), vb_row = 4 * q4_row_words(dv);
+  float* q_s = smem;                      // [G][P2] scaled by log2(e) / sqrt(D)
+  float* s_s = q_s + G * P2;              // [G][TILE] logits, then weights
+  float* qsum_s = s_s + G * Q4G_TILE;     // [G] sums of the scaled q
+  float* alpha_s = qsum_s + G;            // [G]
+  const int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int len = min(max(seq_len[b] + len_add, 0), S_cap);
+  const int n_tiles = (len + Q4G_TILE - 1) / Q4G_TILE;
+  const int tps = (n_tiles + n_split - 1) / n_split;
+  const int tile_begin = split * tps, tile_end = min(n_tiles, tile_begin + tps);
+  for (int i = tid; i < G * P2; i += Q4G_THREADS) q_s[i] = q4_ld(q + ((size_t)b * Hq + h * G) * P2 + i) * qscale;
+  __syncthreads();
+  if (warp < G) {
+    float sum = 0.f;
+    for (int d = lane; d < P2; d += 32) sum += q_s[warp * P2 + d];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) qsum_s[warp] = sum;
+  }
+  const unsigned char* kb = k4 + ((size_t)b * Hkv + h) * (size_t)S_cap * kb_row;
+  const unsigned char* vb = v4 + ((size_t)b * Hkv + h) * (size_t)S_cap * vb_row;
+  float m_run = -INFINITY, l_run = 0.f;
+  float acc[RAP_MAX_GROUP];
+#pragma unroll
+  for (int g = 0; g < RAP_MAX_GROUP; ++g) acc[g] = 0.f;
+  __syncthreads();
+  for (int tile = tile_begin; tile < tile_end; ++tile) {
+    const int j0 = tile * Q4G_TILE;
+    const int nj = min(Q4G_TILE, len - j0);
+    for (int j = warp; j < nj; j += Q4G_THREADS / 32) {
+      const unsigned char* kr = kb + (size_t)(j0 + j) * kb_row;
+      float part[RAP_MAX_GROUP];
+#pragma unroll
+      for (int g = 0; g < RAP_MAX_GROUP; ++g) part[g] = 0.f;
+      for (int c = lane; c < P2 / 2; c += 32) {
+        const uint32_t byte = kr[c];
+        const float c0 = (float)(byte & 15u) - 7.5f, c1 = (float)(byte >> 4) - 7.5f;
+#pragma unroll
+        for (int g = 0; g < RAP_MAX_GROUP; ++g)
+          if (g < G) part[g] = fmaf(c1, q_s[g * P2 + 2 * c + 1], fmaf(c0, q_s[g * P2 + 2 * c], part[g]));
+      }
+      const uint32_t sz = *reinterpret_cast<const uint32_t*>(kr + kb_row - 4);
+#pragma unroll
+      for (int g = 0; g < RAP_MAX_GROUP; ++g) {
+        if (g < G) {
+          float v = part[g];
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+          if (lane == 0) s_s[g * Q4G_TILE + j] = fmaf(q4_step(sz), v, q4_middle(sz) * qsum_s[g]);
+        }
+      }
+    }
+    __syncthreads();
+    if (warp < G) {
+      const int g = warp;
+      float mx = -INFINITY;
+      for (int j = lane; j < nj; j += 32) mx = fmaxf(mx, s_s[g * Q4G_TILE + j]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float m_new = fmaxf(m_run, mx);
+      float sum = 0.f;
+      for (int j = lane; j < nj; j += 32) {
+        const float pw = exp2f(s_s[g * Q4G_TILE + j] - m_new);
+        s_s[g * Q4G_TILE + j] = pw;
+        sum += pw;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const float alpha = exp2f(m_run - m_new);
+      l_run = l_run * alpha + sum;
+      m_run = m_new;
+      if (lane == 0) alpha_s[g] = alpha;
+    }
+    __syncthreads();
+    if (tid < dv) {
+#pragma unroll
+      for (int g = 0; g < RAP_MAX_GROUP; ++g)
+        if (g < G) acc[g] *= alpha_s[g];
+      for (int j = 0; j < nj; ++j) {
+        const unsigned char* vr = vb + (size_t)(j0 + j) * vb_row;
+        const uint32_t sz = *reinterpret_cast<const uint32_t*>(vr + vb_row - 4);
+        const float vv = fmaf(q4_step(sz), (float)((vr[tid >> 1] >> (4 * (tid & 1))) & 15u) - 7.5f, q4_middle(sz));
+#pragma unroll
+        for (int g = 0; g < RAP_MAX_GROUP; ++g)
+          if (g < G) acc[g] = fmaf(s_s[g * Q4G_TILE + j], vv, acc[g]);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int g = 0; g < RAP_MAX_GROUP; ++g) {
+    if (g < G) {
+      float* dst = ws + (((size_t)b * Hq + h * G + g) * n_split + split) * (size_t)(dv + 2);
+      if (tid < dv) dst[tid] = acc[g];
+      if (warp == g && lane == 0) {
+        dst[dv] = m_run;
+        dst[dv + 1] = l_run;
+      }
+    }
+  }
+}
+
+// out[b][g][c] = sum_s 2^(m_s - M) acc_s[c] / sum_s 2^(m_s - M) l_s; an empty split has l = 0 (a NaN in l is kept)
+__global__ void attn_q4_combine_kernel(const float* __restrict__ ws, int n_split, int dv, float* __restrict__ out) {
+  const size_t bg = blockIdx.x;
+  const float* base = ws + bg * n_split * (size_t)(dv + 2);
+  float M = -INFINITY;
+  for (int s = 0; s < n_split; ++s)
+    if (base[(size_t)s * (dv + 2) + dv + 1] != 0.f) M = fmaxf(M, base[(size_t)s * (dv + 2) + dv]);
+  float den = 0.f;
+  for (int s = 0; s < n_split; ++s) {
+    const float l = base[(size_t)s * (dv + 2) + dv + 1];
+    if (l != 0.f) den += exp2f(base[(size_t)s * (dv + 2) + dv] - M) * l;
+  }
+  for (int c = threadIdx.x; c < dv; c += blockDim.x) {
+    float num = 0.f;
+    for (int s = 0; s < n_split; ++s) {
+      const float l = base[(size_t)s * (dv + 2) + dv + 1];
+      if (l != 0.f) num += exp2f(base[(size_t)s * (dv + 2) + dv] - M) * base[(size_t)s * (dv + 2) + c];
+    }
+    out[bg * dv + c] = den != 0.f ? num / den : 0.f;
+  }
+}
+
+}  // namespace
+
+rap_status rap_launch_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, long long n_rows, int W, const void* src, void* dst,
+                                       cudaStream_t st) {
+  const unsigned blocks = (unsigned)((n_rows + 7) / 8);
+  if (dtype_in == RAP_F32)
+    quantize_rows_q4_kernel<float><<<blocks, 256, 0, st>>>((const float*)src, (uint32_t*)dst, n_rows, W);
+  else
+    quantize_rows_q4_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>((const __nv_bfloat16*)src, (uint32_t*)dst, n_rows, W);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}
+
+rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long long n_rows, int W, const void* src, void* dst,
+                                         cudaStream_t st) {
+  const unsigned blocks = (unsigned)((n_rows + 7) / 8);
+  if (dtype_out == RAP_F32)
+    dequantize_rows_q4_kernel<float><<<blocks, 256, 0, st>>>((const uint32_t*)src, (float*)dst, n_rows, W);
+  else
+    dequantize_rows_q4_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>((const uint32_t*)src, (__nv_bfloat16*)dst, n_rows, W);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}
+
+rap_status rap_launch_read_cache_q4(rap_ctx* ctx, int dtype, int B, int Hkv, int S_cap, int P2, int dv, const void* k4, const void* v4,
+                                    const int32_t* seq_len, int len_max, void* k, void* v, cudaStream_t st) {
+  if ((long long)B * Hkv > 65535) return RAP_ESHAPE;
+  const dim3 grid((len_max + 7) / 8, B * Hkv, 2);
+  if (dtype == RAP_F32)
+    read_cache_q4_kernel<float><<<grid, 256, 0, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (float*)k, (float*)v, seq_len, Hkv,
+                                                      S_cap, P2, dv);
+  else
+    read_cache_q4_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (__nv_bfloat16*)k,
+                                                              (__nv_bfloat16*)v, seq_len, Hkv, S_cap, P2, dv);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}
+
+// a.k_cache / a.v_cache are the quantised caches of this layer
+rap_status rap_launch_qkv_rope_append_q4(rap_ctx* ctx, const rap_proj_args& a, cudaStream_t st) {
+  int ksplit = 1;
+  rap_status s = RAP_EUNSUPPORTED;
+  if (a.dtype == RAP_BF16) s = rap_launch_proj_tc(ctx, a, &ksplit, st);
+  if (s == RAP_EUNSUPPORTED) {
+    ksplit = 1;
+    s = rap_launch_proj_generic(ctx, a, st);
+  }
+  if (s != RAP_OK) return s;
+  const long long warps = (long long)a.T * (a.Hq + 2 * a.Hkv);
+  // inside a decode step (a.pdl): launched behind the tcgen05 GEMM with programmatic serialization, so that its launch
+  // overlaps the GEMM's tail (the CUDA-core GEMM never triggers early, which makes the attribute a no-op there)
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((warps + 7) / 8), 1, 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.pdl ? 1 : 0;
+  const float* y = ctx->d_proj_ws;
+  uint32_t* k4 = (uint32_t*)a.k_cache;
+  uint32_t* v4 = (uint32_t*)a.v_cache;
+  if (a.dtype == RAP_F32)
+    RAP_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, rope_append_q4_kernel<float>, y, ksplit, (const float*)a.bias, a.seq_id, a.pos,
+                                         a.slot, a.inv_freq, (float*)a.q_out, k4, v4, a.T, a.Hq, a.Hkv, a.P2, a.dv, a.half_dim,
+                                         a.B_cache, a.S_cap, ctx->d_status));
+  else
+    RAP_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, rope_append_q4_kernel<__nv_bfloat16>, y, ksplit, (const __nv_bfloat16*)a.bias,
+                                         a.seq_id, a.pos, a.slot, a.inv_freq, (__nv_bfloat16*)a.q_out, k4, v4, a.T, a.Hq, a.Hkv,
+                                         a.P2, a.dv, a.half_dim, a.B_cache, a.S_cap, ctx->d_status));
+  ctx->launches++;
+  return RAP_OK;
+}
+
+// a.k / a.v are the quantised caches; a.q has the storage dtype
+rap_status rap_launch_attn_q4(rap_ctx* ctx, const rap_attn_args& a, cudaStream_t st) {
+  if (a.B > 65535 || a.Hkv > 65535) return RAP_ESHAPE;
+  const int G = a.Hq / a.Hkv;
+  int n_split = a.n_split;
+  if (n_split <= 0) {      // a few CTAs per SM, splits of at least four tiles
+    const int n_tiles = (a.h_len_max + Q4G_TILE - 1) / Q4G_TILE;
+    n_split = (8 * ctx->sm_count + a.B * a.Hkv - 1) / (a.B * a.Hkv);
+    if (n_split > n_tiles / 4) n_split = n_tiles / 4;
+    if (n_split > RAP_MAX_SPLIT) n_split = RAP_MAX_SPLIT;
+    if (n_split < 1) n_split = 1;
+  }
+  const float qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
+  const size_t smem = (size_t)(G * a.P2 + G * Q4G_TILE + 2 * G) * sizeof(float);
+  dim3 grid(n_split, a.Hkv, a.B);
+  if (a.dtype == RAP_F32)
+    attn_q4_generic_kernel<float><<<grid, Q4G_THREADS, smem, st>>>((const float*)a.q, (const unsigned char*)a.k,
+                                                                   (const unsigned char*)a.v, a.seq_len, a.len_add, a.Hq, a.Hkv,
+                                                                   a.P2, a.dv, a.S_cap, qscale, n_split, ctx->d_attn_ws);
+  else
+    attn_q4_generic_kernel<__nv_bfloat16><<<grid, Q4G_THREADS, smem, st>>>(
+        (const __nv_bfloat16*)a.q, (const unsigned char*)a.k, (const unsigned char*)a.v, a.seq_len, a.len_add, a.Hq, a.Hkv, a.P2,
+        a.dv, a.S_cap, qscale, n_split, ctx->d_attn_ws);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  attn_q4_combine_kernel<<<a.B * a.Hq, 128, 0, st>>>(ctx->d_attn_ws, n_split, a.dv, a.out);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}

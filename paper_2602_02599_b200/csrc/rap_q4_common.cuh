@@ -1,0 +1,63 @@
+// The 4-bit row format, shared by everything that writes or reads it.  A row x of W numbers keeps codes c_i in 0..15, a
+// step s and a middle z (both bf16):
+//     z = bf16(hi / 2 + lo / 2),   s = bf16(max(hi - z, z - lo) / 7.5),   c_i = rint((x_i - z) (1 / s) + 7.5),
+//     x_i ~ z + s (c_i - 7.5),
+// hi and lo being the row's extremes, every step decided in fp32 (round half to even, no contraction).  The middle is
+// rounded first and the step taken from it, so the codes stay inside 0..15 without clipping: |x - z| <= 7.5 s (1 + 2^-8).
+// A step below the smallest normal number counts as zero (codes 8, the row reads back as z); a row with a NaN, an
+// infinity or a range beyond fp32 has no such form and is held as NaN (step and middle NaN, codes 8).
+// Layout: an odd number of 32-bit words, so that rows staged back to back in shared memory start on different banks; byte
+// i holds code 2i (low half) and 2i + 1 (high half), then zeros, and the last word is s (low half) and z (high half).
+#pragma once
+#include <math.h>
+
+#include "rap_internal.h"
+
+namespace {
+
+constexpr int Q4_MAX_WIDTH = 256;      // one lane of a warp per word of eight codes
+
+__host__ __device__ constexpr int q4_row_words(int W) { return (((W + 1) / 2 + 4 + 3) / 4) | 1; }
+
+__device__ __forceinline__ float q4_ld(const float* p) { return *p; }
+__device__ __forceinline__ float q4_ld(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void q4_st(float* p, float v) { *p = v; }
+__device__ __forceinline__ void q4_st(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// maximum and minimum that keep a NaN (fmaxf drops it)
+__device__ __forceinline__ float q4_max(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float q4_min(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+struct Q4Row {
+  float z, r;            // middle; 1 / step (0 where the step is)
+  uint32_t sz;           // the row's last word
+  bool bad;              // not representable
+};
+__device__ __forceinline__ Q4Row q4_decide(float hi, float lo) {
+  Q4Row q;
+  q.z = __bfloat162float(__float2bfloat16_rn(__fadd_rn(__fmul_rn(hi, 0.5f), __fmul_rn(lo, 0.5f))));
+  const float reach = q4_max(__fsub_rn(hi, q.z), __fsub_rn(q.z, lo));
+  float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(reach, 7.5f)));
+  q.bad = !(s < INFINITY);
+  if (s < 1.17549435e-38f) s = 0.f;
+  q.r = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
+  q.sz = q.bad ? 0x7fff7fffu : (__float_as_uint(q.z) & 0xffff0000u) | (__float_as_uint(s) >> 16);      // bf16 numbers: exact
+  return q;
+}
+// code of x: adding 1.5 * 2^23 rounds to an integer (half to even) and leaves it in the low mantissa bits
+__device__ __forceinline__ uint32_t q4_code(float x, const Q4Row& q) {
+  const float t = __fadd_rn(__fmul_rn(__fsub_rn(x, q.z), q.r), 7.5f);
+  return q.bad ? 8u : __float_as_uint(__fadd_rn(t, 12582912.0f)) & 15u;
+}
+__device__ __forceinline__ float q4_step(uint32_t sz) { return __uint_as_float(sz << 16); }
+__device__ __forceinline__ float q4_middle(uint32_t sz) { return __uint_as_float(sz & 0xffff0000u); }
+
+}  // namespace

@@ -1,0 +1,553 @@
+"""The cache held in 4 bits on the GPU: conversion both ways, the quantising append, the attention and whole decode steps,
+against the fp64 oracle through the C ABI."""
+from dataclasses import replace
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import rap_oracle as O
+from paper_2602_02599_b200 import binding, synth
+from paper_2602_02599_b200.stack import DecodeStack
+
+import q4_util
+import util
+
+pytestmark = pytest.mark.gpu
+
+
+def _bare_stack(w=None, **kw):
+    w = w or synth.scaled_down(synth.LLAMA_8B, n_layers=1, batch=1, seq=8, hidden=256)
+    return DecodeStack(w, s_cap=kw.pop("s_cap", 8), alloc_cache=False, **kw)
+
+
+def _ok(st):
+    torch.cuda.synchronize()
+    assert st.ctx.rap_get_last_device_status() == (0, 0)
+
+
+def _kind(dtype):
+    return binding.RAP_F32 if dtype == "f32" else binding.RAP_BF16
+
+
+# ---- rows ----------------------------------------------------------------------------------------------------------------
+
+
+def _rows(n, W, dtype, seed):
+    rng = np.random.default_rng(seed)
+    x = (rng.normal(0, 1, (n, W)) * rng.lognormal(0, 3, (n, 1)) + rng.normal(0, 2, (n, 1))).astype(np.float32)
+    x[0] = 0.0
+    if n > 8:
+        x[1] = -0.3                                       # one value (not a bf16 number when fp32)
+        x[2, : min(W, 4)] = np.array([7.5, -7.5, 1.0, -2.0], dtype=np.float32)[: min(W, 4)]     # s = 1, z = 0: ties to even
+        x[2, 4:] = 0.0
+        x[3, W // 2] = np.nan
+        x[4, 0] = np.inf
+        x[5, W - 1] = -np.inf
+        x[6] = 1e-40
+        x[7] = np.where(np.arange(W) % 2, 3e38, -3e38)
+        x[8] = 3.4e38
+    return O.round_bf16(x).astype(np.float32) if dtype == "bf16" else x
+
+
+@pytest.mark.parametrize("W", [1, 2, 3, 7, 8, 9, 31, 32, 33, 48, 64, 90, 115, 116, 128, 129, 255, 256])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 9, 1003])
+def test_rows_both_ways_bit_exact(W, dtype, n):
+    """Bytes of rap_quantize_rows_q4 and values of rap_dequantize_rows_q4 equal the oracle's: rows of very different
+    magnitudes, special rows, ties; what lies behind the last row stays as it was."""
+    st = _bare_stack()
+    x = _rows(n, W, dtype, W + n)
+    tdt = torch.float32 if dtype == "f32" else torch.bfloat16
+    dx = torch.from_numpy(x).to(st.device).to(tdt)
+    rb = binding.rap_q4_row_bytes(W)
+    packed = torch.full((n + 3, rb), 0xAB, dtype=torch.uint8, device=st.device)
+    st.ctx.rap_quantize_rows_q4(_kind(dtype), n, W, dx, packed)
+    back = torch.full((n + 3, W), 77.0, dtype=tdt, device=st.device)
+    st.ctx.rap_dequantize_rows_q4(_kind(dtype), n, W, packed, back)
+    wide = torch.full((n + 3, W), 77.0, dtype=torch.float32, device=st.device)
+    st.ctx.rap_dequantize_rows_q4(binding.RAP_F32, n, W, packed, wide)
+    _ok(st)
+    held = O.quantize_rows_q4(x)
+    got = packed.cpu().numpy()
+    assert np.array_equal(got[:n], q4_util.pack(*held))
+    assert np.all(got[n:] == 0xAB) and torch.all(back[n:] == 77.0) and torch.all(wide[n:] == 77.0)
+    with np.errstate(over="ignore"):
+        want = O.dequantize_rows_q4(*held).astype(np.float32)          # exact in 64 bits, one rounding
+    assert np.array_equal(wide[:n].cpu().numpy(), want, equal_nan=True)
+    if dtype == "bf16":
+        assert np.array_equal(util.to_np64(back[:n]), O.round_bf16(want), equal_nan=True)
+    st.close()
+
+
+def test_rows_on_another_stream_and_an_empty_call():
+    st = _bare_stack()
+    x = torch.randn((4096, 90), device=st.device)
+    packed = torch.zeros((4096, 52), dtype=torch.uint8, device=st.device)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        st.ctx.rap_quantize_rows_q4(binding.RAP_F32, 4096, 90, x, packed)
+        st.ctx.rap_quantize_rows_q4(binding.RAP_F32, 0, 90, x, packed)
+        st.ctx.rap_dequantize_rows_q4(binding.RAP_F32, 0, 90, packed, x)
+    side.synchronize()
+    assert np.array_equal(packed.cpu().numpy(), q4_util.pack(*O.quantize_rows_q4(x.cpu().numpy())))
+    st.close()
+
+
+@pytest.mark.parametrize("name", ["8b", "3b", "sweep0.5", "tiny"])
+@pytest.mark.parametrize("lens", [[40], [0, 1, 7, 39, 40, 17, 0, 8]])
+def test_read_cache_up_to_every_length(name, lens):
+    base = synth.CONFIGS[name]
+    w = replace(base, batch=len(lens), seq=40, n_layers=1)
+    st = DecodeStack(w, s_cap=48)
+    st.build_tables(*synth.draw_scores(w))
+    k4, v4 = q4_util.caches(st, 0)
+    g = torch.Generator(device=st.device).manual_seed(1)
+    want = []
+    for packed, W in ((k4, 2 * w.n_pairs), (v4, w.n_vch)):
+        x = torch.empty(packed.shape[:3] + (W,), device=st.device).normal_(0.2, 1, generator=g)
+        st.ctx.rap_quantize_rows_q4(binding.RAP_F32, x.shape[0] * x.shape[1] * x.shape[2], W, x, packed)
+        back = torch.empty(x.shape, dtype=st.dt, device=st.device)
+        st.ctx.rap_dequantize_rows_q4(_kind(w.dtype), x.shape[0] * x.shape[1] * x.shape[2], W, packed, back)
+        for b, n in enumerate(lens):
+            back[b, :, n:] = 5.0
+            packed[b, :, n:] = 0xFF                  # not to be read as numbers
+        want.append(back)
+    st.k_cache[0].fill_(5.0)
+    st.v_cache[0].fill_(5.0)
+    dl = torch.tensor(lens, dtype=torch.int32, device=st.device)
+    st.ctx.rap_read_cache_q4(0, len(lens), k4, v4, 48, dl, max(lens), st.k_cache[0], st.v_cache[0])
+    _ok(st)
+    assert torch.equal(st.k_cache[0], want[0]) and torch.equal(st.v_cache[0], want[1])
+    st.ctx.rap_read_cache_q4(0, len(lens), k4, v4, 48, torch.zeros_like(dl), 0, st.k_cache[0], st.v_cache[0])
+    _ok(st)
+    assert torch.equal(st.k_cache[0], want[0])
+    st.close()
+
+
+# ---- append ----------------------------------------------------------------------------------------------------------------
+
+
+def _append_case(st, w, T, seed, with_bias=False):
+    rng = np.random.default_rng(seed)
+    seq_id = rng.integers(0, st.B, size=T).astype(np.int32)
+    slot = np.zeros(T, np.int32)
+    for b in range(st.B):                                # distinct slots per sequence
+        m = seq_id == b
+        slot[m] = rng.permutation(st.s_cap)[: m.sum()]
+    pos = rng.integers(0, 100000, size=T).astype(np.int32)
+    up = lambda a: torch.from_numpy(a).to(st.device)
+    bias = None
+    if with_bias:
+        bias = rng.normal(0, 2, st.n_out(0)).astype(np.float32)
+    return seq_id, slot, pos, up(seq_id), up(slot), up(pos), bias
+
+
+@pytest.mark.parametrize("T", [1, 5, 70])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_append_fp32_equals_the_plain_append_then_the_row_quantiser(T, with_bias):
+    """An fp32 stack's plain append writes the unrounded K and V rows, so the quantising append has to write exactly what
+    rap_quantize_rows_q4 makes of them, and nothing else; q~ is the same bit for bit."""
+    w = replace(synth.TINY, batch=3, seq=96)
+    ks, vs = synth.draw_scores(w)
+    st, tabs, w_host = util.build_small_stack(w, ks, vs, s_cap=96, max_rows=128)
+    seq_id, slot, pos, dsid, dslot, dpos, bias = _append_case(st, w, T, T, with_bias)
+    dbias = None if bias is None else torch.from_numpy(bias).to(st.device)
+    dx = torch.from_numpy(synth.draw_hidden(w, 0, 1, T)).to(st.device)
+    st.k_cache[0].zero_()
+    st.v_cache[0].zero_()
+    q1, q2 = (torch.full((T, w.n_q_heads, 2 * w.n_pairs), float("nan"), device=st.device) for _ in range(2))
+    st.ctx.rap_qkv_rope_append(0, T, dx, st.w_qkv[0], dbias, dsid, dpos, dslot, int(slot.max()), st.inv_freq, q1, st.k_cache[0],
+                               st.v_cache[0], st.B, st.s_cap)
+    k4, v4 = q4_util.caches(st, 0)
+    st.ctx.rap_qkv_rope_append_q4(0, T, dx, st.w_qkv[0], dbias, dsid, dpos, dslot, int(slot.max()), st.inv_freq, q2, k4, v4, st.B,
+                                  st.s_cap)
+    _ok(st)
+    assert torch.equal(q1, q2)
+    written = np.zeros((st.B, w.n_kv_heads, st.s_cap), bool)
+    written[seq_id, :, slot] = True
+    for packed, plain in ((k4, st.k_cache[0]), (v4, st.v_cache[0])):
+        got = packed.cpu().numpy()
+        assert not got[~written].any()
+        want = q4_util.pack(*O.quantize_rows_q4(plain.cpu().numpy()))
+        assert np.array_equal(got[written], want[written])
+    st.close()
+
+
+@pytest.mark.parametrize("name,T", [("8b", 1), ("8b", 32), ("3b", 17), ("sweep1.0", 5), ("8b", 100), ("sweep0.5", 300)])
+def test_append_bf16_holds_the_oracle_rows(name, T):
+    """Decode-sized and prompt-sized calls: q~ as the plain append writes it, and every appended row within half a step of
+    the oracle's own fp64 projection and rotation (plus the fp32 sum's error, 1e-3 of the row's largest entry), its step
+    within a bf16 step and a bit of the oracle's."""
+    w = synth.scaled_down(synth.CONFIGS[name], n_layers=1, batch=4, seq=64, hidden=512)
+    ks, vs = synth.draw_scores(w)
+    st, tabs, w_host = util.build_small_stack(w, ks, vs, s_cap=160, max_rows=512)
+    seq_id, slot, pos, dsid, dslot, dpos, _ = _append_case(st, w, T, T)
+    P, dv = w.n_pairs, w.n_vch
+    X = synth.draw_hidden(w, 0, 2, T)
+    dx = torch.from_numpy(X).to(st.device).to(st.dt)
+    q1, q2 = (torch.full((T, w.n_q_heads, 2 * P), float("nan"), dtype=st.dt, device=st.device) for _ in range(2))
+    k4, v4 = q4_util.caches(st, 0)
+    st.ctx.rap_qkv_rope_append_q4(0, T, dx, st.w_qkv[0], None, dsid, dpos, dslot, int(slot.max()), st.inv_freq, q1, k4, v4, st.B,
+                                  st.s_cap)
+    st.qkv_rope_append(0, dx, dsid, dpos, dslot, int(slot.max()), q_out=q2)
+    _ok(st)
+    assert torch.equal(q1, q2)
+    _, k, v = O.qkv_rope(O.round_storage(X, w.dtype), w_host[0], None, pos, tabs["inv_freq"][0], w.n_q_heads, w.n_kv_heads, P, dv)
+    written = np.zeros((st.B, w.n_kv_heads, st.s_cap), bool)
+    written[seq_id, :, slot] = True
+    for packed, rows, W in ((k4, k, 2 * P), (v4, v, dv)):
+        got = packed.cpu().numpy()
+        assert not got[~written].any()
+        c, s, z = (a[seq_id, :, slot] for a in q4_util.unpack(got, W))
+        off = 1e-3 * np.abs(rows).max(-1)
+        assert np.all(np.abs(O.dequantize_rows_q4(c, s, z) - rows) <= (0.5 * s * (1 + 2.0 ** -16) + off)[..., None])
+        want_s = O.quantize_rows_q4(rows)[1]
+        assert np.all(np.abs(s - want_s) <= want_s * 2.0 ** -7 + off / 3)      # z may sit a bf16 step apart: /7.5 of it
+    st.close()
+
+
+def test_append_skips_rows_out_of_range_and_reports_them():
+    w = synth.scaled_down(synth.LLAMA_8B, n_layers=1, batch=2, seq=16, hidden=256)
+    ks, vs = synth.draw_scores(w)
+    st, _, _ = util.build_small_stack(w, ks, vs, s_cap=16, max_rows=8)
+    k4, v4 = q4_util.caches(st, 0)
+    dx = torch.from_numpy(synth.draw_hidden(w, 0, 1, 4)).to(st.device).to(st.dt)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device=st.device)
+    q = torch.empty((4, w.n_q_heads, 2 * w.n_pairs), dtype=st.dt, device=st.device)
+    st.ctx.rap_qkv_rope_append_q4(0, 4, dx, st.w_qkv[0], None, i32(0, 2, -1, 1), i32(1, 2, 3, 4), i32(3, 3, 3, 16), 15, st.inv_freq, q,
+                                  k4, v4, 2, 16)
+    torch.cuda.synchronize()
+    code, detail = st.ctx.rap_get_last_device_status()
+    assert code == binding.RAP_ECAPACITY and detail in (1, 2, 3)
+    touched = k4.cpu().numpy().any(axis=(-1)) | v4.cpu().numpy().any(axis=-1)
+    want = np.zeros_like(touched)
+    want[0, :, 3] = True
+    assert np.array_equal(touched, want)
+    st.close()
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------------
+
+
+def _attn_stack(w, lens, seed=0, gain=1.0, s_cap=None, shift=0.0):
+    """(stack, q, k4, v4, lengths): caches quantised from random rows of unlike magnitudes; rows past the end are 0xFF."""
+    st = DecodeStack(w, s_cap=s_cap or ((max(lens) + 8 + 7) // 8) * 8, alloc_cache=False)
+    st.build_tables(*synth.draw_scores(w))
+    g = torch.Generator(device=st.device).manual_seed(seed)
+    packed = []
+    for cache, W in zip(q4_util.caches(st, 0), (2 * w.n_pairs, w.n_vch)):
+        ramp = (1.0 + 0.02 * torch.arange(st.s_cap, device=st.device) % 3.0).view(1, 1, -1, 1)
+        x = torch.empty(cache.shape[:3] + (W,), device=st.device).normal_(shift, 1.28, generator=g) * ramp
+        st.ctx.rap_quantize_rows_q4(binding.RAP_F32, x.numel() // W, W, x, cache)
+        for b, n in enumerate(lens):
+            cache[b, :, n:] = 0xFF
+        packed.append(cache)
+    q = torch.empty((len(lens), w.n_q_heads, 2 * w.n_pairs), dtype=st.dt, device=st.device).normal_(0, 1.28 * gain, generator=g)
+    return st, q, packed[0], packed[1], torch.tensor(lens, dtype=torch.int32, device=st.device)
+
+
+def _run_attn(st, w, q, k4, v4, dl, n_split=0, bound=None):
+    out = torch.full((q.shape[0], w.n_q_heads, w.n_vch), float("nan"), dtype=torch.float32, device=st.device)
+    st.ctx.rap_decode_attn_q4(0, q.shape[0], q, k4, v4, st.s_cap, dl, int(dl.max()) if bound is None else bound, n_split, out)
+    return out
+
+
+def _attn_case(w, lens, n_split=0, variant=0, **kw):
+    st, q, k4, v4, dl = _attn_stack(w, lens, **kw)
+    st.ctx.rap_set_attn_variant(variant)
+    out = _run_attn(st, w, q, k4, v4, dl, n_split)
+    _ok(st)
+    held = [q4_util.unpack(c, W) for c, W in ((k4, 2 * w.n_pairs), (v4, w.n_vch))]
+    generic = variant == 1 or w.dtype == "f32" or max(2 * w.n_pairs, w.n_vch) > 128
+    q4_util.check_attn(util.to_np64(out), util.to_np64(q), held[0], held[1], lens, w.head_dim, 1 if generic else 16)
+    st.close()
+
+
+def _small(name="8b", **kw):
+    return replace(synth.scaled_down(synth.CONFIGS[name], n_layers=1, batch=1, seq=64), **kw)
+
+
+EDGES = [[1], [2, 31, 32, 33, 63], [0, 300, 0, 1, 129, 0], [0, 0], [255, 256, 257, 511, 512, 513], [1] * 9]
+
+
+@pytest.mark.parametrize("lens", EDGES)
+@pytest.mark.parametrize("n_split", [0, 1, 4])
+@pytest.mark.parametrize("variant", [0, 1])
+def test_attention_lengths_at_every_border(lens, n_split, variant):
+    _attn_case(_small(batch=len(lens)), lens, n_split, variant, seed=len(lens))
+
+
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 6, 7, 8])
+@pytest.mark.parametrize("P,dv", [(45, 90), (58, 115), (32, 64), (64, 128), (51, 102)])
+def test_attention_head_shapes(G, P, dv):
+    w = _small(batch=2, n_pairs=P, n_vch=dv, n_q_heads=2 * G, n_kv_heads=2)
+    _attn_case(w, [777, 130], seed=G)
+
+
+@pytest.mark.parametrize("P", [1, 2, 4, 5, 11, 16, 17, 23, 31, 33, 48, 49, 63])
+def test_attention_odd_widths(P):
+    """Any retained counts, K and V apart: fewer numbers than a word of codes, one more than a group of 32."""
+    for dv in (1, 2 * P, 129 - 2 * P, 33, 97):
+        _attn_case(_small(batch=2, n_pairs=P, n_vch=dv, n_q_heads=6, n_kv_heads=2), [300, 45], seed=P + dv)
+
+
+@pytest.mark.parametrize("n_split", [0, 7])
+@pytest.mark.parametrize("name", ["3b", "8b", "14b"])
+def test_attention_longer_sequences(name, n_split):
+    _attn_case(replace(_small(name), batch=3), [6000, 2500, 33], n_split, seed=5)
+
+
+@pytest.mark.parametrize("gain", [0.0, 1e-30, 0.05, 12.0, 1e6])
+def test_attention_flat_and_peaked(gain):
+    """q of any size: all weights equal, one weight left, a q far outside fp16's range."""
+    _attn_case(_small(batch=2), [1500, 40], seed=7, gain=gain)
+
+
+@pytest.mark.parametrize("shift", [50.0, -3.0])
+def test_attention_rows_off_centre(shift):
+    _attn_case(_small(batch=2), [1100, 200], seed=8, shift=shift)
+
+
+@pytest.mark.parametrize("scale", [1e-20, 1e-6, 3e4, 1e20])
+def test_attention_v_of_any_magnitude(scale):
+    """Steps of V far outside fp16's range, and unlike ones side by side: the weights carry them."""
+    lens = [700, 350]
+    w = _small(batch=2)
+    st, q, k4, v4, dl = _attn_stack(w, lens, seed=9)
+    g = torch.Generator(device=st.device).manual_seed(3)
+    spread = torch.exp(3 * torch.randn((2, w.n_kv_heads, st.s_cap, 1), generator=g, device=st.device))
+    x = torch.randn((2, w.n_kv_heads, st.s_cap, w.n_vch), generator=g, device=st.device) * spread * scale
+    st.ctx.rap_quantize_rows_q4(binding.RAP_F32, x.numel() // w.n_vch, w.n_vch, x, v4)
+    out = _run_attn(st, w, q, k4, v4, dl)
+    _ok(st)
+    q4_util.check_attn(util.to_np64(out), util.to_np64(q), q4_util.unpack(k4, 2 * w.n_pairs), q4_util.unpack(v4, w.n_vch), lens, w.head_dim)
+    st.close()
+
+
+def test_attention_fp32_and_wide_heads():
+    _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], seed=2)
+    _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], 3, seed=3)
+    w = _small(batch=2, head_dim=256, n_pairs=90, n_vch=179, n_q_heads=4, n_kv_heads=2)
+    _attn_case(w, [500, 65], seed=4)
+
+
+@pytest.mark.parametrize("variant", [0, 1])
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_a_nan_row_reaches_its_own_heads_only(variant, where):
+    lens = [900, 400]
+    w = _small(batch=2)
+    st, q, k4, v4, dl = _attn_stack(w, lens, seed=6)
+    st.ctx.rap_set_attn_variant(variant)
+    clean = _run_attn(st, w, q, k4, v4, dl)
+    (k4 if where == "k" else v4)[1, 3, 222] = 0xFF
+    out = _run_attn(st, w, q, k4, v4, dl)
+    _ok(st)
+    hit = torch.zeros((2, w.n_q_heads), dtype=torch.bool, device=st.device)
+    hit[1, 3 * w.group: 4 * w.group] = True
+    assert torch.isnan(out[hit]).all()
+    assert torch.equal(out[~hit], clean[~hit])
+    st.close()
+
+
+def test_attention_offsets_past_32_bits():
+    """A cache of more than 2^32 bytes whose last sequence alone is in use."""
+    w = _small(batch=32)
+    st = DecodeStack(w, s_cap=330000, alloc_cache=False)
+    st.build_tables(*synth.draw_scores(w))
+    k4, v4 = q4_util.caches(st, 0)
+    assert k4.numel() > 2 ** 32
+    n = 1500
+    g = torch.Generator(device=st.device).manual_seed(2)
+    for cache, W in ((k4, 2 * w.n_pairs), (v4, w.n_vch)):
+        x = torch.randn((w.n_kv_heads, n, W), generator=g, device=st.device)
+        packed = torch.empty((w.n_kv_heads, n, cache.shape[-1]), dtype=torch.uint8, device=st.device)
+        st.ctx.rap_quantize_rows_q4(binding.RAP_F32, w.n_kv_heads * n, W, x, packed)
+        cache[31, :, :n] = packed
+    q = torch.randn((32, w.n_q_heads, 2 * w.n_pairs), generator=g, device=st.device).to(st.dt)
+    lens = [0] * 31 + [n]
+    dl = torch.tensor(lens, dtype=torch.int32, device=st.device)
+    out = _run_attn(st, w, q, k4, v4, dl)
+    _ok(st)
+    assert not out[:31].any()
+    one = lambda c, W: q4_util.unpack(c[31:, :, :n].contiguous(), W)
+    q4_util.check_attn(util.to_np64(out[31:]), util.to_np64(q[31:]), one(k4, 2 * w.n_pairs), one(v4, w.n_vch), [n], w.head_dim)
+    st.close()
+
+
+def test_attention_repeats_bit_for_bit_on_one_split_and_on_a_side_stream():
+    w = _small(batch=5)
+    st, q, k4, v4, dl = _attn_stack(w, [3000, 5, 0, 911, 64], seed=3)
+    first = _run_attn(st, w, q, k4, v4, dl)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = [_run_attn(st, w, q, k4, v4, dl) for _ in range(5)]
+    torch.cuda.current_stream().wait_stream(side)
+    _ok(st)
+    assert all(torch.equal(first, a) for a in again)
+    st.close()
+
+
+def test_attention_captured_and_replayed():
+    """Two graphs on one context, replayed in turns, with lengths that change between replays (within the bound)."""
+    w = _small(batch=3)
+    lens = [2000, 700, 0]
+    st, q, k4, v4, dl = _attn_stack(w, [2000, 2000, 2000], seed=4)
+    dl.copy_(torch.tensor(lens, dtype=torch.int32))
+    outs = [torch.zeros((3, w.n_q_heads, w.n_vch), dtype=torch.float32, device=st.device) for _ in range(2)]
+    _run_attn(st, w, q, k4, v4, dl, bound=2000)
+    torch.cuda.synchronize()
+    graphs = []
+    for o in outs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            st.ctx.rap_decode_attn_q4(0, 3, q, k4, v4, st.s_cap, dl, 2000, 0, o)
+        graphs.append(g)
+    held = [q4_util.unpack(c, W) for c, W in ((k4, 2 * w.n_pairs), (v4, w.n_vch))]
+    for lens in ([2000, 700, 0], [1, 0, 1999], [64, 64, 64]):
+        dl.copy_(torch.tensor(lens, dtype=torch.int32))
+        for i in (0, 1, 0, 0):
+            outs[i].fill_(float("nan"))
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            q4_util.check_attn(util.to_np64(outs[i]), util.to_np64(q), held[0], held[1], lens, w.head_dim)
+    assert st.ctx.rap_get_last_device_status() == (0, 0)
+    del graphs
+    st.close()
+
+
+# ---- together ------------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("name", ["8b", "3b", "tiny"])
+def test_decode_step_equals_the_separate_calls(name):
+    """rap_decode_step_q4 against rap_qkv_rope_append_q4 + rap_decode_attn_q4 per layer, bit for bit, caches and outputs;
+    the lengths advance; the attention against the oracle on the device's own rows."""
+    base = synth.CONFIGS[name]
+    w = replace(base, batch=2, seq=300) if name == "tiny" else synth.scaled_down(base, n_layers=3, batch=2, seq=300, hidden=512)
+    lens = np.array([300, 211], dtype=np.int32)
+    ks, vs = synth.draw_scores(w)
+    st, _, _ = util.build_small_stack(w, ks, vs, full_weights=False, max_rows=256)
+    B, L = w.batch, w.n_layers
+    g = torch.Generator(device=st.device).manual_seed(11)
+    k4, v4 = [], []
+    for l in range(L):
+        pair = q4_util.caches(st, l)
+        for packed, W in zip(pair, (2 * st.n_pairs[l], st.n_vch[l])):
+            x = torch.empty(packed.shape[:3] + (W,), device=st.device).normal_(0, 1, generator=g)
+            st.ctx.rap_quantize_rows_q4(binding.RAP_F32, x.numel() // W, W, x, packed)
+        k4.append(pair[0])
+        v4.append(pair[1])
+    k4_ref, v4_ref = [t.clone() for t in k4], [t.clone() for t in v4]
+    x = torch.empty((L, B, w.hidden), device=st.device).normal_(0, 1, generator=g).to(st.dt)
+    st.seq_len.copy_(torch.from_numpy(lens))
+    for step in range(2):
+        dl = torch.from_numpy(lens + step).to(st.device)
+        sid = torch.arange(B, dtype=torch.int32, device=st.device)
+        want = []
+        for l in range(L):
+            q = torch.empty((B, w.n_q_heads, 2 * st.n_pairs[l]), dtype=st.dt, device=st.device)
+            st.ctx.rap_qkv_rope_append_q4(l, B, x[l], st.w_qkv[l], None, sid, dl, dl, int(lens.max()) + step, st.inv_freq, q, k4_ref[l],
+                                          v4_ref[l], B, st.s_cap)
+            o = torch.empty((B, w.n_q_heads, st.n_vch[l]), dtype=torch.float32, device=st.device)
+            st.ctx.rap_decode_attn_q4(l, B, q, k4_ref[l], v4_ref[l], st.s_cap, dl + 1, int(lens.max()) + step + 1, 0, o)
+            want.append((q, o))
+        st.out.fill_(float("nan"))
+        st.ctx.rap_decode_step_q4(B, x, st.w_qkv, None, st.inv_freq, k4, v4, st.s_cap, st.seq_len, int(lens.max()) + step, 0,
+                                  st.q_scratch, st.out, st.out_stride, 1)
+        _ok(st)
+        assert np.array_equal(st.seq_len.cpu().numpy(), lens + step + 1)
+        for l in range(L):
+            assert torch.equal(k4[l], k4_ref[l]) and torch.equal(v4[l], v4_ref[l])
+            assert torch.equal(st.out[l][: want[l][1].numel()].view_as(want[l][1]), want[l][1])
+    l = L - 1
+    held = [q4_util.unpack(c, W) for c, W in ((k4[l], 2 * st.n_pairs[l]), (v4[l], st.n_vch[l]))]
+    q4_util.check_attn(util.to_np64(want[l][1]), util.to_np64(want[l][0]), held[0], held[1], lens + 2, w.head_dim,
+                       1 if w.dtype == "f32" else 16)
+    st.close()
+
+
+def test_prompt_chunk_behind_a_quantised_prefix_then_decode():
+    """As a server uses them: a prompt's first part appended in 4 bits, the rows read back, the second part attended over
+    them by rap_prefill_attn, appended in 4 bits too, then a decode step of the attention over everything."""
+    w = synth.scaled_down(synth.LLAMA_8B, n_layers=1, batch=2, seq=400, hidden=512)
+    ks, vs = synth.draw_scores(w)
+    st, tabs, w_host = util.build_small_stack(w, ks, vs, s_cap=448, max_rows=512)
+    B, T1, T2, P, dv = 2, 250, 128, w.n_pairs, w.n_vch
+    k4, v4 = q4_util.caches(st, 0)
+
+    def append(first, count, seed):
+        sid = torch.arange(B, dtype=torch.int32, device=st.device).repeat_interleave(count)
+        pos = torch.arange(first, first + count, dtype=torch.int32, device=st.device).repeat(B)
+        x = torch.from_numpy(synth.draw_hidden(w, 0, seed, B * count)).to(st.device).to(st.dt)
+        q = torch.empty((B * count, w.n_q_heads, 2 * P), dtype=st.dt, device=st.device)
+        st.ctx.rap_qkv_rope_append_q4(0, B * count, x, st.w_qkv[0], None, sid, pos, pos, first + count - 1, st.inv_freq, q, k4, v4, B,
+                                      st.s_cap)
+        return q
+
+    append(0, T1, 1)
+    q = append(T1, T2, 2)
+    dl = torch.full((B,), T1 + T2, dtype=torch.int32, device=st.device)
+    start = torch.full((B,), T1, dtype=torch.int32, device=st.device)
+    st.ctx.rap_read_cache_q4(0, B, k4, v4, st.s_cap, dl, T1 + T2, st.k_cache[0], st.v_cache[0])
+    out = torch.empty((B, T2, w.n_q_heads, dv), dtype=torch.float32, device=st.device)
+    st.ctx.rap_prefill_attn(0, B, T2, q, st.k_cache[0], st.v_cache[0], st.s_cap, start, T1, out)
+    _ok(st)
+    held = [q4_util.unpack(c, W) for c, W in ((k4, 2 * P), (v4, dv))]
+    K, V = (O.round_bf16(O.dequantize_rows_q4(*h)) for h in held)
+    want = O.prefill_attn(util.to_np64(q).reshape(B, T2, w.n_q_heads, 2 * P), K, V, np.full(B, T1), w.head_dim)
+    util.check_attn(util.to_np64(out), want, "bf16")
+    q1 = append(T1 + T2, 1, 3)
+    o1 = _run_attn(st, w, q1, k4, v4, dl + 1)
+    _ok(st)
+    held = [q4_util.unpack(c, W) for c, W in ((k4, 2 * P), (v4, dv))]
+    q4_util.check_attn(util.to_np64(o1), util.to_np64(q1), held[0], held[1], [T1 + T2 + 1] * B, w.head_dim)
+    st.close()
+
+
+def test_refusals():
+    w = synth.scaled_down(synth.LLAMA_8B, n_layers=1, batch=2, seq=16, hidden=256)
+    ks, vs = synth.draw_scores(w)
+    st, _, _ = util.build_small_stack(w, ks, vs, s_cap=16, max_rows=8)
+    k4, v4 = q4_util.caches(st, 0)
+    dl = torch.tensor([3, 4], dtype=torch.int32, device=st.device)
+    q = torch.zeros((2, w.n_q_heads, 2 * w.n_pairs), dtype=st.dt, device=st.device)
+    out = torch.zeros((2, w.n_q_heads, w.n_vch), dtype=torch.float32, device=st.device)
+    x = torch.zeros((2, w.hidden), dtype=st.dt, device=st.device)
+
+    def refused(status, f, *a):
+        with pytest.raises(binding.RapError) as e:
+            f(*a)
+        assert e.value.status == status
+
+    A = st.ctx.rap_decode_attn_q4
+    refused(binding.RAP_EINVAL, A, 1, 2, q, k4, v4, 16, dl, 4, 0, out)
+    refused(binding.RAP_EINVAL, A, 0, 2, None, k4, v4, 16, dl, 4, 0, out)
+    refused(binding.RAP_EINVAL, A, 0, 2, q, k4, v4, 16, dl, 4, -1, out)
+    refused(binding.RAP_ESHAPE, A, 0, 3, q, k4, v4, 16, dl, 4, 0, out)
+    refused(binding.RAP_ESHAPE, A, 0, 2, q, k4, v4, 16, dl, 4, 65, out)
+    refused(binding.RAP_EALIGN, A, 0, 2, q, k4, v4, 12, dl, 4, 0, out)
+    refused(binding.RAP_EALIGN, A, 0, 2, q, k4.data_ptr() + 4, v4, 16, dl, 4, 0, out)
+    refused(binding.RAP_ECAPACITY, A, 0, 2, q, k4, v4, 16, dl, 17, 0, out)
+    A(0, 0, q, k4, v4, 16, dl, 4, 0, out)
+    R = st.ctx.rap_read_cache_q4
+    refused(binding.RAP_EINVAL, R, 0, 2, k4, v4, 16, None, 4, st.k_cache[0], st.v_cache[0])
+    refused(binding.RAP_EINVAL, R, -1, 2, k4, v4, 16, dl, 4, st.k_cache[0], st.v_cache[0])
+    refused(binding.RAP_ESHAPE, R, 0, 3, k4, v4, 16, dl, 4, st.k_cache[0], st.v_cache[0])
+    refused(binding.RAP_EALIGN, R, 0, 2, k4, v4, 12, dl, 4, st.k_cache[0], st.v_cache[0])
+    refused(binding.RAP_ECAPACITY, R, 0, 2, k4, v4, 16, dl, 17, st.k_cache[0], st.v_cache[0])
+    P = st.ctx.rap_qkv_rope_append_q4
+    refused(binding.RAP_ESHAPE, P, 0, 9, x, st.w_qkv[0], None, dl, dl, dl, 4, st.inv_freq, q, k4, v4, 2, 16)
+    refused(binding.RAP_ECAPACITY, P, 0, 2, x, st.w_qkv[0], None, dl, dl, dl, 16, st.inv_freq, q, k4, v4, 2, 16)
+    refused(binding.RAP_EINVAL, P, 0, 2, x, st.w_qkv[0], None, None, dl, dl, 4, st.inv_freq, q, k4, v4, 2, 16)
+    refused(binding.RAP_EALIGN, P, 0, 2, x, st.w_qkv[0], None, dl, dl, dl, 4, st.inv_freq, q, k4.data_ptr() + 8, v4, 2, 16)
+    S = st.ctx.rap_decode_step_q4
+    refused(binding.RAP_ECAPACITY, S, 2, x, st.w_qkv, None, st.inv_freq, [k4], [v4], 16, dl, 16, 0, st.q_scratch, st.out, st.out_stride, 0)
+    refused(binding.RAP_EINVAL, S, 2, x, st.w_qkv, None, st.inv_freq, [None], [v4], 16, dl, 4, 0, st.q_scratch, st.out, st.out_stride, 0)
+    refused(binding.RAP_ESHAPE, S, 2, x, st.w_qkv, None, st.inv_freq, [k4], [v4], 16, dl, 4, 0, st.q_scratch, st.out, 4, 0)
+    refused(binding.RAP_ESHAPE, st.ctx.rap_quantize_rows_q4, binding.RAP_F32, 1, 257, x, k4)
+    _ok(st)
+    assert not k4.any() and not v4.any()
+    st.close()
