@@ -85,6 +85,16 @@ def q8_shapes():
     return shapes
 
 
+Q4_PARTS = 16
+
+
+def q4_shapes():
+    """(words per K row, words per V row, heads per lane) of the tensor-core scan over a 4-bit cache: every odd number of
+    words up to 17 on both sides, so it covers every head of up to 128 dims and every group size up to 8."""
+    words = range(3, 18, 2)
+    return [(k, v, c) for c in (1, 2) for k in words for v in words]
+
+
 def write_scan_sources():
     """Generated translation units: SCAN_PARTS files of instantiations and the lookup over them."""
     os.makedirs(OBJ, exist_ok=True)
@@ -134,7 +144,25 @@ def write_scan_sources():
         body += ["    entry<%d, %d, %d>()," % sh for sh in mine]
         body += ["  };", "  *n = (int)(sizeof(table) / sizeof(table[0]));", "  return table;", "}", ""]
         names.append(_write_if_changed(os.path.join(OBJ, "q8_inst_%d.cu" % k), "\n".join(body)))
+    for k in range(Q4_PARTS):
+        mine = q4_shapes()[k::Q4_PARTS]
+        body = ['// generated by build.py: instantiations of the tensor-core scan over a 4-bit cache, part %d' % k,
+                '#include "rap_attn_q4_kernel.cuh"', "namespace {",
+                "template <int K, int V, int C> rap_q4_entry entry() {",
+                "  return rap_q4_entry{K, V, C, Q4Cfg<K, V, C>::SMEM, (const void*)attn_q4_kernel<K, V, C>};", "}", "}  // namespace",
+                "const rap_q4_entry* rap_q4_table_%d(int* n) {" % k, "  static const rap_q4_entry table[] = {"]
+        body += ["    entry<%d, %d, %d>()," % sh for sh in mine]
+        body += ["  };", "  *n = (int)(sizeof(table) / sizeof(table[0]));", "  return table;", "}", ""]
+        names.append(_write_if_changed(os.path.join(OBJ, "q4_inst_%d.cu" % k), "\n".join(body)))
     look = ['// generated by build.py: lookup over the instantiation tables', '#include "rap_internal.h"']
+    look += ["const rap_q4_entry* rap_q4_table_%d(int* n);" % k for k in range(Q4_PARTS)]
+    look += ["const rap_q4_entry* rap_q4_find(int k_words, int v_words, int heads_per_lane) {",
+             "  typedef const rap_q4_entry* (*table_fn)(int*);",
+             "  static const table_fn parts[] = {" + ", ".join("rap_q4_table_%d" % k for k in range(Q4_PARTS)) + "};",
+             "  for (table_fn f : parts) {", "    int n = 0;", "    const rap_q4_entry* t = f(&n);",
+             "    for (int i = 0; i < n; ++i)",
+             "      if (t[i].k_words == k_words && t[i].v_words == v_words && t[i].heads_per_lane == heads_per_lane) return &t[i];",
+             "  }", "  return nullptr;", "}"]
     look += ["const rap_scan_entry* rap_q8_table_%d(int* n);" % k for k in range(Q8_PARTS)]
     look += ["const rap_scan_entry* rap_q8_find(int G, int WK, int DV) {",
              "  typedef const rap_scan_entry* (*table_fn)(int*);",

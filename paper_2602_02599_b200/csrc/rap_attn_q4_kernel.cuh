@@ -1,0 +1,676 @@
+// Split-KV decode scan over a cache held in 4 bits (rap_decode_attn_q4).  Same work plan, per-warp copy pipelines, lazy
+// online softmax and fused merge as the other tensor-core scans; rows are 52 bytes where bf16 rows are 180, so the issue
+// slots per row -- above all those of the integer pipe, which unpacks -- are what the design is about (mma.sync m16n8k16,
+// fp16 in, fp32 accumulate):
+//   * The cache is the A operand (16 rows, or 16 channels, on M), the query heads the B operand (8 columns): half the
+//     padding of the other way round.
+//   * A nibble under no exponent bits is an fp16 subnormal (c 2^-22 in bits 2..5, c 2^-18 in bits 6..9), so an operand
+//     register of two codes is ONE mask of a shifted word: no exponent constant, no conversion, no offset to subtract.
+//     Which code sits on which k-slot is free as long as both operands agree; on the K side the factor of 16 between the
+//     two positions goes into q (exactly).  Row strides are compile-time constants, so every fragment load is one
+//     instruction.
+//   * S = K q: q enters in fp16, scaled per head by a power of two into fp16's range (a bf16 number keeps all its bits
+//     down to 2^-28 of the head's largest).  A logit is s_K (sum q c - 7.5 sum q) + z_K sum q; the 7.5 sum q is the
+//     initial value of the accumulator, the row's step and middle are applied to the accumulators in fp32.  Up to four
+//     heads sit on the even columns, so that every lane ends up with one head of four rows and no logit twice.
+//   * O += V p: the row's step goes into its weight, which enters as two fp16 numbers: its upper 8 bits and the rest
+//     (19 bits together).  Up to four heads they are two columns of one MMA, beyond that two MMAs.  The tensor core aligns
+//     the 16 products of a step by their exponents and cuts them off below, and a subnormal operand brings its leading
+//     zeros along: hence the short first part, and all V codes in the highest position (output off by 7e-6 from bits 0..3,
+//     9e-7 from bits 4..7).  Weights are scaled by a power of two per warp that follows the largest seen, so that steps
+//     of any magnitude stay inside fp16.  The middles are summed apart, in fp32.
+//   * The codes 0..15 are 7.5 off centre, and a tensor core's running sum, which is cut off rather than rounded, must not
+//     carry an offset that grows with the row: of every two rows that share an operand register the second enters with its
+//     codes complemented (15 - c, the same mask operation) and its weight negated, so the offsets alternate in sign (output
+//     off by 3e-4 at 32K rows without it).  What is left of them is 7.5 times the sum of the signed weights, which one MMA
+//     against ones keeps along.  Every Q4_FLUSH blocks the accumulators move into fp32 sums in shared memory, which keeps
+//     the cut-off of a long row's running sum below 1e-6 as well.
+//   * Weights leave the first MMA with rows on M and enter the second with rows on K: one 8x8 transpose per 8 rows.
+//   * Block row of tile row i (0..7) of half-tile t is 4 i + t: rows of an odd number of words then start on eight
+//     banks, four apart, and all fragment and scale loads are free of conflicts.
+//   * A unit that one CTA scans alone is written out directly, and the first copies of a CTA's next unit are issued before
+//     the merge of the last: batches of short sequences are chains of such units.
+// Rows past the end of a sequence get weight, step and middle zero by selection; their bytes may be anything.
+// Every mbarrier wait is bounded: on timeout the CTA records RAP_ETIMEOUT and leaves.
+#pragma once
+#include <type_traits>
+
+#include "rap_attn_common.cuh"
+#include "rap_q4_common.cuh"
+
+namespace {
+
+constexpr float Q4_WEIGHT_MAX = 32768.f; // a scaled weight above this raises the reference maximum and the steps' scale
+constexpr int Q4_BR = 32;                // rows per warp block
+constexpr int Q4_NW = 8;                 // warps per CTA
+constexpr int Q4_TILE = Q4_NW * Q4_BR;   // rows per CTA tile
+constexpr int Q4_MAX_STG = 8;
+constexpr int Q4_FLUSH = 16;             // blocks between two moves of the accumulators into shared memory
+constexpr int Q4_OFF_MAIN = 1024 + 128;  // barriers, merge scalars and flags below
+constexpr int Q4_PAD = 64;               // the last row's fragment loads may reach one word past it
+
+// KSW, VSW: words per K / V row (odd); GC: heads per lane (1: up to four heads, the two parts of a weight on neighbouring
+// columns; 2: up to eight heads)
+template <int KSW, int VSW, int GC>
+struct Q4Cfg {
+  static_assert(KSW % 2 == 1 && VSW % 2 == 1 && KSW <= 17 && VSW <= 17, "rows of up to 128 codes");
+  static constexpr int NGK = (KSW + 2) / 4, NGV = (VSW + 2) / 4;      // groups of 4 words: 32 dims / channels
+  static constexpr int NT = 2 * NGV;                                  // tiles of 16 channels
+  static constexpr int CW = 32 * NGV;                                 // channel slots of the reduction buffer
+  static constexpr int MAIN_F = 4 * GC * CW;                          // floats per warp: fp32 sums, then [4 GC][CW] for the merge
+  static constexpr int STAGE_W = Q4_BR * (KSW + VSW);                 // words per stage
+  static constexpr int OFF_RING = Q4_OFF_MAIN + Q4_NW * MAIN_F * 4;
+  static constexpr int FIT = (SMEM_BUDGET - OFF_RING - Q4_PAD) / (Q4_NW * STAGE_W * 4);
+  static constexpr int NSTG = FIT < Q4_MAX_STG ? FIT : Q4_MAX_STG;    // stages per warp: 3 for rows of 90, 2 for rows of 128
+  static constexpr int SMEM = OFF_RING + Q4_NW * NSTG * STAGE_W * 4 + Q4_PAD;
+  static_assert(NSTG >= 2 && SMEM <= SMEM_BUDGET, "ring does not fit");
+  static_assert(OFF_RING % 128 == 0 && Q4_NW * MAIN_F >= RAP_MAX_GROUP * (RAP_MAX_SPLIT + 1), "merge weights fit");
+};
+
+struct Q4ScanParams {
+  ScanParams s;
+  int P, dv, G;
+};
+
+__device__ __forceinline__ void q4_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same with accumulators that start from (c0, c1) in both halves
+__device__ __forceinline__ void q4_mma_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                            uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ float q4_ex2(float x) {      // 2^x, one instruction; 2^(-inf) = 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t q4_pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float q4_low(uint32_t h2) {
+  float r;
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, l;}" : "=f"(r) : "r"(h2));
+  return r;
+}
+__device__ __forceinline__ float q4_high(uint32_t h2) {
+  float r;
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, h;}" : "=f"(r) : "r"(h2));
+  return r;
+}
+__device__ __forceinline__ uint32_t q4_transpose(uint32_t x) {      // an 8x8 tile of 16-bit numbers across the warp
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ float q4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
+__device__ __forceinline__ int q4_exponent(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
+constexpr uint32_t Q4_LO = 0x003c003cu, Q4_HI = 0x03c003c0u;
+// the codes in the high position with the second row's complemented, (y ^ flip) & Q4_HI with flip = 0x03c00000 in a register:
+// one instruction, where two immediates would make two
+__device__ __forceinline__ uint32_t q4_pair(uint32_t y, uint32_t flip) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(y), "r"(flip), "r"(Q4_HI));
+  return r;
+}
+
+template <int KSW, int VSW, int GC>
+__global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanParams pp) {
+  using C = Q4Cfg<KSW, VSW, GC>;
+  const ScanParams& p = pp.s;
+  constexpr int NW = Q4_NW, THREADS = NW * 32, ST = Q4_TILE, NSTG = C::NSTG;
+  constexpr int NGK = C::NGK, NGV = C::NGV, NT = C::NT, CW = C::CW, MV = 2 * GC;      // MV: sums per lane and tile
+  extern __shared__ __align__(128) unsigned char q4_smem[];
+  unsigned char* const smem = q4_smem;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                        // [NW][Q4_MAX_STG]
+  float* m_s = reinterpret_cast<float*>(smem + NW * Q4_MAX_STG * 8);         // [NW][8] reference maxima of the warps
+  float* l_s = m_s + NW * 8;                                                 // [NW][8] scaled row sums
+  int* s_flag = reinterpret_cast<int*>(l_s + NW * 8);                        // time-out seen by any warp
+  int* s_last = s_flag + 1;
+  float* red = reinterpret_cast<float*>(smem + Q4_OFF_MAIN);                 // [NW][MAIN_F]: sums, merge buffer, merge weights
+  static_assert(NW * Q4_MAX_STG * 8 + NW * 64 + 8 <= Q4_OFF_MAIN, "barriers and merge scalars sit below");
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int gid = lane >> 2, tq = lane & 3;
+  const int G = pp.G, DV = pp.dv;
+  int b = 0, h = 0;
+  SkPlan plan;
+  plan.T = 0; plan.nc = 0;
+  int cur = 0, hi = 0, unit_start = 0;
+  if (p.balanced) {
+    // the plan (reads the lengths only): computed by the first warp where the ring will be
+    int* pref = reinterpret_cast<int*>(smem + C::OFF_RING);
+    const bool shared_plan = sk_plan_shared(p.seq_len, p.B, p.Hkv, p.len_add, p.S_cap, ST, (int)gridDim.x, pref,
+                                            NW * NSTG * C::STAGE_W, &plan);
+    if (!shared_plan) plan = sk_plan(p.seq_len, p.B, p.Hkv, p.len_add, p.S_cap, ST, (int)gridDim.x);
+    // everything below reads what the previous kernel in the stream wrote, and writes what the next one may depend on
+    pdl_wait();
+    pdl_launch_dependents();
+    if (blockIdx.x == 0) {   // sequences without any row are scanned by nobody: their output is zero
+      for (int i = tid; i < p.B * p.Hkv; i += THREADS) p.unit_cnt_other[i] = 0;   // counters a launch that gave up left behind
+      if (tid == 0) *p.dyn_next_other = 0;          // and the piece counter a bf16 tensor-core launch before this one used
+      for (int bb = 0; bb < p.B; ++bb) {
+        const bool empty = shared_plan ? pref[bb] == (bb > 0 ? pref[bb - 1] : 0)
+                                       : sk_tiles_of(p.seq_len, bb, p.len_add, p.S_cap, ST) == 0;
+        if (empty)
+          for (int i = tid; i < p.Hq * DV; i += THREADS) p.out[(size_t)bb * p.Hq * DV + i] = 0.f;
+      }
+    }
+    if ((int)blockIdx.x >= plan.nc) return;
+    cur = (int)((long long)blockIdx.x * plan.T / plan.nc);
+    hi = (int)((long long)(blockIdx.x + 1) * plan.T / plan.nc);
+    if (cur >= hi) return;
+    int pb = 0;
+    if (shared_plan) {       // the unit that holds tile `cur`
+      b = sk_seq_of(pref, p.B, cur);
+      pb = b > 0 ? pref[b - 1] : 0;
+    } else {
+      for (b = 0; b < p.B; ++b) {
+        const int nb = sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST) * p.Hkv;
+        if (cur < pb + nb) break;
+        pb += nb;
+      }
+    }
+    const int ntb = sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST);
+    h = (cur - pb) / ntb;
+    unit_start = pb + h * ntb;
+  } else {
+    pdl_wait();
+    pdl_launch_dependents();
+    b = blockIdx.z;
+    h = blockIdx.y;
+  }
+  const uint32_t bar0 = smem_u32(bars) + warp * Q4_MAX_STG * 8;               // this warp's barriers
+  const uint32_t* ring = reinterpret_cast<const uint32_t*>(smem + C::OFF_RING) + warp * NSTG * C::STAGE_W;   // and stages
+  const uint32_t ring_u = smem_u32(ring);
+  float* const my_main = red + warp * C::MAIN_F;                              // and sums: [tile][lane][MV] while scanning
+  if (tid == 0) {
+    *s_flag = 0;
+    for (int i = 0; i < NW * Q4_MAX_STG; ++i) mbar_init(smem_u32(bars) + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the plan's stores, before copies land on them
+  __syncthreads();
+
+  // Fragment addressing inside a stage (words).  K: half-tile t, tile row gid: block row 4 gid + t, word 4 j + tq of group
+  // j.  V: k-slots 2 tq, 2 tq + 1 of half-tile t: block rows 8 tq + t and 8 tq + 4 + t.
+  const int k_at = 4 * gid * KSW + tq;
+  const int v_at = Q4_BR * KSW + 8 * tq * VSW + gid;
+  const int vh_at = 2 * (Q4_BR * KSW + 8 * tq * VSW) + 8 * (NGV - 1) + gid;     // half words: the last, odd group of 32
+  const int ksz_at = 4 * gid * KSW + KSW - 1, vsz_at = Q4_BR * KSW + 4 * gid * VSW + VSW - 1;
+  const float row_sign = (gid & 1) ? -1.f : 1.f;      // rows 4 gid + t of odd gid are the second of their pair
+  uint32_t flip;
+  asm volatile("mov.b32 %0, 0x03c00000;" : "=r"(flip));
+  int st = 0, st_issue = 0;    // ring positions of the next block to use and to copy, running on across units
+  uint32_t parity = 0;
+  bool timed_out = false;
+
+  // the segment being scanned: tiles [t_begin, t_begin + n_my) of unit (b, h), seg_tiles in all; this warp's blocks are the
+  // rows [(t_begin + i) ST + 32 warp, + 32) for i < n_blk, those that hold a valid row
+  int len = 0, seg_tiles = 0, t_begin = 0, n_my = 0, row_w = 0, n_blk = 0;
+  auto issue_block = [&](int i) {                     // all lanes converged; lane 0 issues
+    const int j0 = row_w + i * ST;
+    const int rows = min(Q4_BR, ((len + 7) & ~7) - j0);      // rows a copy may touch: S_cap is a multiple of 8
+    const uint32_t kb = (uint32_t)rows * 4 * KSW, vb = (uint32_t)rows * 4 * VSW;     // multiples of 16: rows is a multiple of 8
+    if (lane == 0 && RAP_BOUNDS(j0 + rows - 1, p.S_cap, p.status, 0x402) && RAP_BOUNDS(rows - 1, Q4_BR, p.status, 0x404) &&
+        RAP_BOUNDS(st_issue, NSTG, p.status, 0x403)) {
+      const uint32_t bar = bar0 + 8 * st_issue, dst = ring_u + 4 * st_issue * C::STAGE_W;
+      const size_t row0 = ((size_t)b * p.Hkv + h) * (size_t)p.S_cap + j0;
+      mbar_expect_tx(bar, kb + vb);
+      if (!(p.dbg_skip_copy && blockIdx.x == 0 && warp == 0 && i == 0)) {
+        bulk_g2s(dst, p.k + row0 * (4 * KSW), kb, bar);
+        bulk_g2s(dst + 4 * Q4_BR * KSW, p.v + row0 * (4 * VSW), vb, bar);
+      }
+    }
+    if (++st_issue == NSTG) st_issue = 0;
+  };
+  auto start_segment = [&]() {                        // lengths and first copies of unit (b, h) from tile t_begin on
+    len = min(max(p.seq_len[b] + p.len_add, 0), p.S_cap);
+    seg_tiles = (len + ST - 1) / ST;
+    if (p.balanced) {
+      t_begin = cur - unit_start;
+      n_my = min(seg_tiles - t_begin, hi - cur);
+    } else {
+      const int tps = (seg_tiles + p.n_split - 1) / p.n_split;
+      t_begin = min(seg_tiles, (int)blockIdx.x * tps);
+      n_my = min(seg_tiles, t_begin + tps) - t_begin;
+    }
+    row_w = t_begin * ST + Q4_BR * warp;
+    n_blk = len > row_w ? min(n_my, (len - row_w + ST - 1) / ST) : 0;
+    const int pre = min(n_blk, NSTG - 1);
+    for (int i = 0; i < pre; ++i) issue_block(i);
+  };
+  start_segment();
+  if (n_my <= 0) {             // (equal ranges only) nothing to scan: neutral partials
+    float* base = p.ws + (((size_t)b * p.Hq + (size_t)h * G) * p.n_split + blockIdx.x) * (size_t)(DV + 2);
+    for (int i = tid; i < G * (DV + 2); i += THREADS) {
+      const int g = i / (DV + 2), c = i - g * (DV + 2);
+      base[(size_t)g * p.n_split * (DV + 2) + c] = (c == DV) ? -INFINITY : 0.f;
+    }
+    return;
+  }
+
+  for (;;) {   // one pass per segment (a single one unless the mode is balanced)
+    // ---- q as the B operand: column gid is head gid / 2 on even columns (GC = 1) or head gid (GC = 2), else zeros.  Of
+    // word w = 4 j + tq of a row: k-slots 2 tq, 2 tq + 1 and 2 tq + 8, 2 tq + 9 hold dims 8 w + (0, 4) and (2, 6) in the
+    // step of the low position (with 16 q: its codes count 2^-22), (1, 5) and (3, 7) in that of the high one (2^-18). ----
+    uint32_t qa[NGK][2], qb[NGK][2];
+    float off[2], f_q[GC], zq[GC], m_ref[GC], l_thr[GC], z_thr[GC];
+    {
+      const int col_head = GC == 1 ? gid >> 1 : gid;
+      const bool on = col_head < G && (GC == 2 || (gid & 1) == 0);
+      const uint32_t* qrow = p.q + ((size_t)b * p.Hq + (size_t)h * G + (on ? col_head : 0)) * pp.P;
+      uint32_t w[NGK][4];
+      float top = 0.f, sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < NGK; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = 4 * (4 * j + tq) + i;
+          w[j][i] = (on && at < pp.P) ? qrow[at] : 0u;
+        }
+#pragma unroll
+      for (int j = 0; j < NGK; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x0 = __uint_as_float(w[j][i] << 16), x1 = __uint_as_float(w[j][i] & 0xffff0000u);
+          top = fmaxf(top, fmaxf(fabsf(x0), fabsf(x1)));
+          sum += x0 + x1;
+        }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = min(max(10 - q4_exponent(top), -100), 120);       // the largest |q| 2^e lies in [2^10, 2^11)
+      const float sc = q4_pow2(e);
+      float seen = 0.f;            // sum of q 2^e as the MMAs see it
+#pragma unroll
+      for (int j = 0; j < NGK; ++j) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[2 * i] = __uint_as_float(w[j][i] << 16) * sc;
+          x[2 * i + 1] = __uint_as_float(w[j][i] & 0xffff0000u) * sc;
+        }
+        qa[j][0] = q4_pack(16.f * x[0], 16.f * x[4]);
+        qa[j][1] = q4_pack(16.f * x[2], 16.f * x[6]);
+        qb[j][0] = q4_pack(x[1], x[5]);
+        qb[j][1] = q4_pack(x[3], x[7]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          seen += 0.0625f * (q4_low(qa[j][i]) + q4_high(qa[j][i])) + (q4_low(qb[j][i]) + q4_high(qb[j][i]));
+      }
+      seen += __shfl_xor_sync(0xffffffffu, seen, 1);
+      seen += __shfl_xor_sync(0xffffffffu, seen, 2);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      // what the accumulator columns 2 tq, 2 tq + 1 need, from the lanes that hold those columns of q
+      const float cs = p.qscale;   // log2(e) / sqrt(D)
+      const float off_c = -7.5f * 0x1p-18f * seen, f_c = cs * q4_pow2(18 - e), z_c = cs * sum;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) off[i] = __shfl_sync(0xffffffffu, off_c, 4 * (2 * tq + i));
+#pragma unroll
+      for (int i = 0; i < GC; ++i) {
+        f_q[i] = __shfl_sync(0xffffffffu, f_c, 4 * (2 * tq + i));
+        zq[i] = __shfl_sync(0xffffffffu, z_c, 4 * (2 * tq + i));
+        m_ref[i] = -INFINITY;
+        l_thr[i] = z_thr[i] = 0.f;
+      }
+    }
+    float o[NT][4], dsum[4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
+    dsum[0] = dsum[1] = dsum[2] = dsum[3] = 0.f;
+    float vn = 1.f;              // power of two the steps of V are scaled by
+    bool have_main = false;      // the sums in shared memory hold something
+    // the accumulators, less 7.5 per summed (signed) weight, plus what shared memory holds of them; channel rows gid (r = 0)
+    // and gid + 8 (1) of tile t, in units of 2^-18.  GC = 1: both columns belong to one head.
+    auto total = [&](int t, int r, int g) {
+      constexpr float unit = -7.5f * 0x1p-18f;
+      float v = GC == 1 ? fmaf(unit, dsum[0], o[t][2 * r]) + fmaf(unit, dsum[1], o[t][2 * r + 1]) : fmaf(unit, dsum[g], o[t][2 * r + g]);
+      if (have_main) v += my_main[(t * 32 + lane) * MV + r * GC + g];
+      return v;
+    };
+
+    // one block of 32 rows; TAIL: some of them (4 gid + t >= nrows) lie past the end
+    auto block = [&](auto tail, const uint32_t* __restrict__ sw, int nrows, bool first) {
+      constexpr bool TAIL = decltype(tail)::value;
+      // ---- S = K q: two tiles of 16 rows, two steps of 16 dims per group ----
+      float s[2][4];
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+        for (int j = 0; j < NGK; ++j) {
+          const uint32_t x0 = sw[k_at + 2 * mt * KSW + 4 * j], x1 = sw[k_at + (2 * mt + 1) * KSW + 4 * j];
+          const uint32_t l0 = x0 << 2, l1 = x1 << 2, h0 = x0 >> 6, h1 = x1 >> 6;
+          if (j == 0) q4_mma_from(s[mt], off[0], off[1], l0 & Q4_LO, l1 & Q4_LO, h0 & Q4_LO, h1 & Q4_LO, qa[j][0], qa[j][1]);
+          else q4_mma(s[mt], l0 & Q4_LO, l1 & Q4_LO, h0 & Q4_LO, h1 & Q4_LO, qa[j][0], qa[j][1]);
+          q4_mma(s[mt], l0 & Q4_HI, l1 & Q4_HI, h0 & Q4_HI, h1 & Q4_HI, qb[j][0], qb[j][1]);
+        }
+      }
+      // ---- logits in base 2 less the reference maximum; weights times the (scaled, signed) V steps ----
+      uint32_t ksz[4], vsz[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        ksz[t] = sw[ksz_at + t * KSW];
+        vsz[t] = sw[vsz_at + t * VSW];
+        if (TAIL && 4 * gid + t >= nrows) ksz[t] = vsz[t] = 0u;
+      }
+      float e[4][GC], w[4][GC];
+      float big = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float ks = q4_step(ksz[t]), kz = q4_middle(ksz[t]), vs = q4_step(vsz[t]) * (vn * row_sign);
+#pragma unroll
+        for (int g = 0; g < GC; ++g) {
+          float x = fmaf(ks * f_q[g], s[t >> 1][2 * (t & 1) + g], fmaf(kz, zq[g], -m_ref[g]));
+          if (TAIL && 4 * gid + t >= nrows) x = -INFINITY;
+          e[t][g] = q4_ex2(x);
+          w[t][g] = e[t][g] * vs;
+          big = q4_max(big, fabsf(w[t][g]));
+        }
+      }
+      if (__any_sync(0xffffffffu, first || !(big <= Q4_WEIGHT_MAX))) {
+        // raise the reference maxima to the block's, and set the scale of the steps so that the largest weight is 4 .. 8
+        float a[2], most = 0.f, ratio = 1.f;
+#pragma unroll
+        for (int g = 0; g < GC; ++g) {
+          float x[4], mx = -3e38f;
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            x[t] = fmaf(q4_step(ksz[t]) * f_q[g], s[t >> 1][2 * (t & 1) + g], q4_middle(ksz[t]) * zq[g]);
+            if (TAIL && 4 * gid + t >= nrows) x[t] = -INFINITY;
+            mx = fmaxf(mx, x[t]);
+          }
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+          const float m_new = fmaxf(m_ref[g], mx);
+          a[g] = a[1] = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
+          m_ref[g] = m_new;
+          l_thr[g] *= a[g];
+          z_thr[g] *= a[g];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            e[t][g] = q4_ex2(x[t] - m_new);
+            most = fmaxf(most, e[t][g] * q4_step(vsz[t]));
+          }
+        }
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        if (first || most * vn > 8.f) {
+          const float to = q4_pow2(min(max(2 - q4_exponent(most), -120), 120));
+          if (!first) ratio = to / vn;
+          vn = to;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int g = 0; g < GC; ++g) w[t][g] = e[t][g] * (q4_step(vsz[t]) * (vn * row_sign));
+        a[0] *= ratio;
+        a[1] *= ratio;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          o[t][0] *= a[0]; o[t][1] *= a[1];
+          o[t][2] *= a[0]; o[t][3] *= a[1];
+          if (have_main) {
+#pragma unroll
+            for (int r = 0; r < MV; ++r) my_main[(t * 32 + lane) * MV + r] *= a[r % GC];
+          }
+        }
+        dsum[0] *= a[0]; dsum[1] *= a[1];
+      }
+      // ---- row sums; the weights as fp16 pairs, turned into the B operand ----
+      uint32_t pb[4], pl[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float vz = q4_middle(vsz[t]);
+        float top[GC], rest[GC];
+#pragma unroll
+        for (int g = 0; g < GC; ++g) {
+          l_thr[g] += e[t][g];
+          z_thr[g] = fmaf(e[t][g], vz, z_thr[g]);
+          top[g] = __uint_as_float(__float_as_uint(w[t][g]) & 0xffff0000u);
+          rest[g] = w[t][g] - top[g];
+        }
+        if constexpr (GC == 1) {
+          pb[t] = q4_transpose(q4_pack(top[0], rest[0]));
+          pl[t] = 0u;
+        } else {
+          pb[t] = q4_transpose(q4_pack(top[0], top[GC - 1]));
+          pl[t] = q4_transpose(q4_pack(rest[0], rest[GC - 1]));
+        }
+      }
+      // ---- O += V p: two steps of 16 rows, tiles of 16 channels ----
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        const uint32_t b0 = pb[2 * mt], b1 = pb[2 * mt + 1];
+        [[maybe_unused]] const uint32_t c0 = pl[2 * mt], c1 = pl[2 * mt + 1];
+        // four channels of 16 rows: y holds k-slots 2 tq, 2 tq + 1, z those + 8; codes 0 .. 3 go to rows gid and
+        // gid + 8 of two tiles
+        auto tiles = [&](float (&acc0)[4], float (&acc1)[4], uint32_t y, uint32_t z) {
+          const uint32_t a0 = q4_pair(y << 6, flip), a1 = q4_pair(y << 2, flip), a2 = q4_pair(z << 6, flip), a3 = q4_pair(z << 2, flip);
+          q4_mma(acc0, a0, a1, a2, a3, b0, b1);
+          if constexpr (GC == 2) q4_mma(acc0, a0, a1, a2, a3, c0, c1);
+          const uint32_t d0 = q4_pair(y >> 2, flip), d1 = q4_pair(y >> 6, flip), d2 = q4_pair(z >> 2, flip), d3 = q4_pair(z >> 6, flip);
+          q4_mma(acc1, d0, d1, d2, d3, b0, b1);
+          if constexpr (GC == 2) q4_mma(acc1, d0, d1, d2, d3, c0, c1);
+        };
+        constexpr uint32_t ones = 0x3c003c00u;
+        q4_mma(dsum, ones, ones, ones, ones, b0, b1);
+        if constexpr (GC == 2) q4_mma(dsum, ones, ones, ones, ones, c0, c1);
+        const uint32_t* v0 = sw + v_at + 2 * mt * VSW;
+#pragma unroll
+        for (int u = 0; u < NGV / 2; ++u) {      // 64 channels: word 8 u + gid holds channels 64 u + 8 gid ..
+          const uint32_t xa = v0[8 * u], xb = v0[8 * u + 4 * VSW], xc = v0[8 * u + VSW], xd = v0[8 * u + 5 * VSW];
+          const uint32_t ya = __byte_perm(xa, xb, 0x5410), yb = __byte_perm(xa, xb, 0x7632);
+          const uint32_t za = __byte_perm(xc, xd, 0x5410), zb = __byte_perm(xc, xd, 0x7632);
+          tiles(o[4 * u], o[4 * u + 1], ya, za);
+          tiles(o[4 * u + 2], o[4 * u + 3], yb, zb);
+        }
+        if constexpr (NGV % 2 == 1) {            // the last 32 channels: half word 8 (NGV - 1) + gid holds channels + 4 gid ..
+          const uint16_t* vh = reinterpret_cast<const uint16_t*>(sw) + vh_at + 4 * mt * VSW;
+          const uint32_t y = __byte_perm(vh[0], vh[8 * VSW], 0x5410), z = __byte_perm(vh[2 * VSW], vh[10 * VSW], 0x5410);
+          tiles(o[NT - 2], o[NT - 1], y, z);
+        }
+      }
+    };
+
+    for (int i = 0; i < n_blk; ++i) {
+      if (i + NSTG - 1 < n_blk) issue_block(i + NSTG - 1);
+      if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar0 + 8 * st, parity, p.wait_limit))) {   // warp-uniform verdict
+        timed_out = true;
+        break;
+      }
+      const uint32_t* sw = ring + st * C::STAGE_W;
+      const int nrows = len - (row_w + i * ST);      // valid rows of this block (>= 1)
+      bool in_ok = true;
+#ifdef RAP_DEBUG_BOUNDS
+      const int at = (int)(sw - reinterpret_cast<const uint32_t*>(smem));      // the largest offsets this lane reads
+      in_ok = __all_sync(0xffffffffu, RAP_BOUNDS(at + k_at + 3 * KSW + 4 * NGK - 4, C::SMEM / 4, p.status, 0x406) &&
+                                          RAP_BOUNDS(at + v_at + 7 * VSW + (NGV > 1 ? 8 * (NGV / 2 - 1) : 0), C::SMEM / 4, p.status, 0x405) &&
+                                          RAP_BOUNDS(2 * at + vh_at + 14 * VSW, C::SMEM / 2, p.status, 0x407) &&
+                                          RAP_BOUNDS(at + vsz_at + 3 * VSW, C::SMEM / 4, p.status, 0x408));
+#endif
+      if (in_ok) {
+        if (nrows >= Q4_BR) block(std::false_type{}, sw, nrows, i == 0);
+        else block(std::true_type{}, sw, nrows, i == 0);
+      }
+      if ((i & (Q4_FLUSH - 1)) == Q4_FLUSH - 1) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+          for (int r = 0; r < MV; ++r) my_main[(t * 32 + lane) * MV + r] = total(t, r / GC, r % GC);
+          o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
+        }
+        dsum[0] = dsum[1] = dsum[2] = dsum[3] = 0.f;
+        have_main = true;
+      }
+      __syncwarp();            // every lane is done with this stage before lane 0 refills it
+      if (++st == NSTG) { st = 0; parity ^= 1u; }
+    }
+
+    // ---- merge the warps: common maximum per head, scaled sums ----
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float v[MV];
+#pragma unroll
+      for (int r = 0; r < MV; ++r) v[r] = total(t, r / GC, r % GC);
+#pragma unroll
+      for (int r = 0; r < MV; ++r) o[t][r] = v[r];
+    }
+#pragma unroll
+    for (int g = 0; g < GC; ++g)
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        l_thr[g] += __shfl_xor_sync(0xffffffffu, l_thr[g], d);
+        z_thr[g] += __shfl_xor_sync(0xffffffffu, z_thr[g], d);
+      }
+    if (timed_out && lane == 0) *s_flag = 1;
+    if (gid == 0) {
+#pragma unroll
+      for (int g = 0; g < GC; ++g) m_s[warp * 8 + GC * tq + g] = m_ref[g];
+    }
+    __syncthreads();
+    if (*s_flag) {
+      if (tid == 0) {
+        atomicCAS(&p.status[0], 0, (int)RAP_ETIMEOUT);
+        p.status[1] = (b * p.Hkv + h) * RAP_MAX_SPLIT + (int)(blockIdx.x % RAP_MAX_SPLIT);
+      }
+      // give copies still in flight a bounded chance to land before the shared memory is released
+      if (lane == 0)
+        for (int sg = 0; sg < NSTG; ++sg) {
+          mbar_wait_bounded(bar0 + 8 * sg, 0, p.wait_limit);
+          mbar_wait_bounded(bar0 + 8 * sg, 1, p.wait_limit);
+        }
+      __syncthreads();
+      return;
+    }
+    const float unscale = 1.f / vn;
+#pragma unroll
+    for (int g = 0; g < GC; ++g) {
+      const int head = GC * tq + g;
+      float m_all = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, m_s[w * 8 + head]);
+      const float f = m_ref[g] == -INFINITY ? 0.f : q4_ex2(m_ref[g] - m_all);   // a warp without a block contributes nothing
+      if (gid == 0) l_s[warp * 8 + head] = l_thr[g] * f;
+      if (head < G) {
+        float* rr = my_main + head * CW;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const bool wide = t < 4 * (NGV / 2);
+          const int c = wide ? 64 * (t / 4) + 8 * gid + 2 * (t % 4) : 32 * (NGV - 1) + 4 * gid + 2 * (t % 2);
+          rr[c] = fmaf(o[t][g] * 0x1p18f, unscale, z_thr[g]) * f;
+          rr[c + 1] = fmaf(o[t][GC + g] * 0x1p18f, unscale, z_thr[g]) * f;
+        }
+      }
+    }
+    // this segment's place; then the next one's first copies, under the merge
+    const int b0 = b, h0 = h, start0 = unit_start, tiles0 = seg_tiles;
+    bool more = false;
+    if (p.balanced) {
+      cur += n_my;
+      if (cur < hi) {
+        unit_start += seg_tiles;
+        if (++h == p.Hkv) {
+          h = 0;
+          do { ++b; } while (b < p.B && sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST) == 0);
+        }
+        more = b < p.B;
+        if (more) start_segment();
+      }
+    }
+    __syncthreads();
+    const int first = p.balanced ? sk_cta_of(start0, plan) : 0;
+    const int nseg = p.balanced ? sk_cta_of(start0 + tiles0 - 1, plan) - first + 1 : 0;
+    if (nseg == 1) {
+      // the whole unit was scanned here: straight to the output
+      const bool o_ok = RAP_BOUNDS(((size_t)b0 * p.Hq + (size_t)h0 * G + G) * DV - 1, (size_t)p.B * p.Hq * DV, p.status, 0x40c);
+      for (int i = tid; i < G * DV && o_ok; i += THREADS) {
+        const int g = i / DV, c = i - g * DV;
+        float sum = 0.f, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          sum += red[w * C::MAIN_F + g * CW + c];
+          l += l_s[w * 8 + g];
+        }
+        p.out[((size_t)b0 * p.Hq + (size_t)h0 * G) * DV + i] = l != 0.f ? sum / l : 0.f;
+      }
+    } else {
+      const size_t ws_head = (size_t)(p.balanced ? RAP_MAX_SPLIT : p.n_split) * (DV + 2);
+      float* unit_ws = p.ws + ((size_t)b0 * p.Hq + (size_t)h0 * G) * ws_head;
+      float* ws_base = unit_ws + (size_t)((int)blockIdx.x - first) * (DV + 2);
+      const bool ws_ok = RAP_BOUNDS((ws_base - p.ws) + (long long)(G - 1) * ws_head + DV + 1, p.ws_floats, p.status, 0x409);
+      for (int i = tid; i < G * DV && ws_ok; i += THREADS) {
+        const int g = i / DV, c = i - g * DV;
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += red[w * C::MAIN_F + g * CW + c];
+        ws_base[g * ws_head + c] = sum;
+      }
+      if (tid < G && ws_ok) {
+        float l = 0.f, mm = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          l += l_s[w * 8 + tid];
+          mm = fmaxf(mm, m_s[w * 8 + tid]);
+        }
+        ws_base[tid * ws_head + DV] = mm;
+        ws_base[tid * ws_head + DV + 1] = l;
+      }
+      if (!p.balanced) return;
+      // ---- the CTA that delivers a unit's last partial merges them (no separate combine launch) ----
+      __threadfence();           // this CTA's partials are visible before its arrival is counted
+      __syncthreads();
+      const int u = b0 * p.Hkv + h0;
+      if (tid == 0) *s_last = RAP_BOUNDS(u, p.B * p.Hkv, p.status, 0x40a) && atomicAdd(&p.unit_cnt[u], 1) == nseg - 1;
+      __syncthreads();
+      if (*s_last) {
+        __threadfence();
+        const bool m_ok = RAP_BOUNDS((unit_ws - p.ws) + (long long)(G - 1) * ws_head + (long long)(nseg - 1) * (DV + 2) + DV + 1,
+                                     p.ws_floats, p.status, 0x40b);
+        float* wgt = red;        // [G][RAP_MAX_SPLIT] segment weights, then G reciprocals of the denominators
+        for (int g = warp; g < G && m_ok; g += NW) {
+          const float* gb = unit_ws + (size_t)g * ws_head;
+          float mv[2], lv[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int sg = lane + 32 * k;
+            lv[k] = sg < nseg ? __ldcg(gb + (size_t)sg * (DV + 2) + DV + 1) : 0.f;
+            mv[k] = sg < nseg ? __ldcg(gb + (size_t)sg * (DV + 2) + DV) : -INFINITY;
+          }
+          float M = fmaxf(lv[0] != 0.f ? mv[0] : -INFINITY, lv[1] != 0.f ? mv[1] : -INFINITY);
+#pragma unroll
+          for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+          float den = 0.f;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float wk = lv[k] != 0.f ? exp2f(mv[k] - M) : 0.f;      // (a NaN in a row sum is kept)
+            wgt[g * RAP_MAX_SPLIT + lane + 32 * k] = wk;
+            den += wk * lv[k];
+          }
+#pragma unroll
+          for (int d = 16; d > 0; d >>= 1) den += __shfl_xor_sync(0xffffffffu, den, d);
+          if (lane == 0) wgt[G * RAP_MAX_SPLIT + g] = den != 0.f ? 1.f / den : 0.f;
+        }
+        __syncthreads();
+        for (int i = tid; i < G * DV && m_ok; i += THREADS) {
+          const int g = i / DV, c = i - g * DV;
+          const float* gb = unit_ws + (size_t)g * ws_head + c;
+          float num = 0.f;
+          for (int sg = 0; sg < nseg; ++sg) num += wgt[g * RAP_MAX_SPLIT + sg] * __ldcg(gb + (size_t)sg * (DV + 2));
+          p.out[((size_t)b0 * p.Hq + (size_t)h0 * G) * DV + i] = num * wgt[G * RAP_MAX_SPLIT + g];
+        }
+        if (tid == 0) p.unit_cnt[u] = 0;   // ready for the next call on this context
+      }
+    }
+    if (!more) break;
+    __syncthreads();   // the reduction buffer and the merge scalars are reused by the next segment
+  }   // segment loop
+}
+
+}  // namespace

@@ -60,8 +60,9 @@ __global__ void __launch_bounds__(128) attn_scan_combine_kernel(const float* __r
 
 }  // namespace
 
-static rap_status launch_split_kv(rap_ctx* ctx, const rap_attn_args& a, int n_split_req, cudaStream_t st,
-                                  const rap_scan_entry* e, bool is_mma) {
+// Parameters common to the split-KV scans: n_split_req = 0 asks for the balanced mode (p.balanced), whose launch has
+// 2 * SMs CTAs; otherwise p.n_split equal ranges per unit.  A balanced launch takes the next of the two counter sets.
+rap_scan_params rap_fill_scan_params(rap_ctx* ctx, const rap_attn_args& a, int n_split_req) {
   // n_split = 0: balanced mode, one CTA per resident slot; an explicit n_split keeps equal ranges per split
   const bool balanced = n_split_req <= 0 && (long long)a.B * a.Hkv * ((a.S_cap + 63) / 64) < (1LL << 31);
   int n_split = balanced ? RAP_MAX_SPLIT : n_split_req;
@@ -88,15 +89,26 @@ static rap_status launch_split_kv(rap_ctx* ctx, const rap_attn_args& a, int n_sp
     p.dyn_next = ctx->d_unit_cnt + 2 * n_units + set;
     p.dyn_next_other = ctx->d_unit_cnt + 2 * n_units + (set ^ 1u);
   }
+  p.dyn_piece = 0;
+  p.dyn_frac_x256 = 0;
+  p.dyn_guard = 0;
+  p.out = a.out;
+  p.wait_limit = WAIT_LIMIT;
+  p.dbg_skip_copy = 0;
+  return p;
+}
+
+static rap_status launch_split_kv(rap_ctx* ctx, const rap_attn_args& a, int n_split_req, cudaStream_t st,
+                                  const rap_scan_entry* e, bool is_mma) {
+  ScanParams p = rap_fill_scan_params(ctx, a, n_split_req);
+  const bool balanced = p.balanced != 0;
+  const int n_split = p.n_split;
   // Long launches of the tensor-core form: the CTAs do not stream at the same pace (the memory system shares its
   // bandwidth unevenly), so the last tenth of the tiles is not assigned up front but claimed piece by piece by
   // whoever is done.  A piece costs a pipeline refill and a partial, so short launches (under ~100 tiles per CTA)
   // keep the fixed split -- and the kernel without that logic, which starts and ends a microsecond or two sooner; a
   // piece is long enough that no unit gets more than ~24 of them.  (Measured on the quantised cache: no gain, a
   // piece's overhead weighs twice as much there.)
-  p.dyn_piece = 0;
-  p.dyn_frac_x256 = 0;
-  p.dyn_guard = 0;
   const void* fn = e->fn;
   if (balanced && is_mma && e->fn_dyn) {
     const long long unit_tiles = (a.h_len_max + e->tile - 1) / e->tile;
@@ -111,9 +123,6 @@ static rap_status launch_split_kv(rap_ctx* ctx, const rap_attn_args& a, int n_sp
     }
     if (p.dyn_piece > 0 && p.dyn_frac_x256 > 0) fn = e->fn_dyn;
   }
-  p.out = a.out;
-  p.wait_limit = WAIT_LIMIT;
-  p.dbg_skip_copy = 0;
   if (ctx->dbg_arm_timeout && !e->tma && is_mma) {
     // test hook (rap_debug_arm_wait_timeout): one stage of this launch is armed without a copy and polled a few
     // thousand times only, so the launch reports RAP_ETIMEOUT and leaves its units unfinished

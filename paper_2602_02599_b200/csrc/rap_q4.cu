@@ -1,7 +1,8 @@
 // The cache held in 4 bits (format: rap_q4_common.cuh): conversion of rows and of a layer's cache in both directions, the
-// RoPE / append epilogue that quantises new K and V rows straight from their fp32 values, and the shape-generic split-KV
-// attention over a 4-bit cache.
-#include "rap_q4_common.cuh"
+// RoPE / append epilogue that quantises new K and V rows straight from their fp32 values, and the launch side of the split-KV
+// attention over a 4-bit cache: the tensor-core scan (rap_attn_q4_kernel.cuh) for bf16 q~ and rows of up to 128 numbers,
+// a shape-generic kernel behind it.
+#include "rap_attn_q4_kernel.cuh"
 
 rap_status rap_launch_proj_tc(rap_ctx* ctx, const rap_proj_args& a, int* ksplit_out, cudaStream_t st);
 rap_status rap_launch_proj_generic(rap_ctx* ctx, const rap_proj_args& a, cudaStream_t st);
@@ -395,8 +396,44 @@ rap_status rap_launch_qkv_rope_append_q4(rap_ctx* ctx, const rap_proj_args& a, c
   return RAP_OK;
 }
 
+// bf16 q~, rows of up to 128 numbers, any group size: one launch (balanced split) or scan and combine (explicit n_split)
+static rap_status launch_attn_q4_scan(rap_ctx* ctx, const rap_attn_args& a, cudaStream_t st) {
+  const int G = a.Hq / a.Hkv;
+  const rap_q4_entry* e = rap_q4_find(q4_row_words(a.P2), q4_row_words(a.dv), G <= 4 ? 1 : 2);
+  if (!e) return RAP_EUNSUPPORTED;
+  Q4ScanParams p;
+  p.s = rap_fill_scan_params(ctx, a, a.n_split);
+  p.P = a.P2 / 2; p.dv = a.dv; p.G = G;
+  if (!p.s.balanced && (a.B > 65535 || a.Hkv > 65535)) return RAP_ESHAPE;
+  if (ctx->dbg_arm_timeout) {     // test hook: one stage is armed without a copy and polled a few thousand times only
+    p.s.wait_limit = 4096;
+    p.s.dbg_skip_copy = 1;
+    ctx->dbg_arm_timeout = 0;
+  }
+  RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, e->fn, e->smem));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = p.s.balanced ? dim3(2 * ctx->sm_count) : dim3(p.s.n_split, a.Hkv, a.B);
+  cfg.blockDim = dim3(Q4_NW * 32);
+  cfg.dynamicSmemBytes = (size_t)e->smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.pdl ? 1 : 0;      // the kernel waits for its predecessor before it reads q~ or a cache row
+  void* args[] = {&p};
+  RAP_CUDA_TRY(ctx, cudaLaunchKernelExC(&cfg, e->fn, args));
+  ctx->launches++;
+  if (p.s.balanced) return RAP_OK;
+  attn_q4_combine_kernel<<<a.B * a.Hq, 128, 0, st>>>(ctx->d_attn_ws, p.s.n_split, a.dv, a.out);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}
+
 // a.k / a.v are the quantised caches; a.q has the storage dtype
 rap_status rap_launch_attn_q4(rap_ctx* ctx, const rap_attn_args& a, cudaStream_t st) {
+  if (a.dtype == RAP_BF16 && a.P2 <= 128 && a.dv <= 128 && ctx->attn_variant != 1) return launch_attn_q4_scan(ctx, a, st);
   if (a.B > 65535 || a.Hkv > 65535) return RAP_ESHAPE;
   const int G = a.Hq / a.Hkv;
   int n_split = a.n_split;
