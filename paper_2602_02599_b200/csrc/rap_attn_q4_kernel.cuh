@@ -28,8 +28,10 @@
 //   * Weights leave the first MMA with rows on M and enter the second with rows on K: one 8x8 transpose per 8 rows.
 //   * Block row of tile row i (0..7) of half-tile t is 4 i + t: rows of an odd number of words then start on eight
 //     banks, four apart, and all fragment and scale loads are free of conflicts.
-//   * A unit that one CTA scans alone is written out directly, and the first copies of a CTA's next unit are issued before
-//     the merge of the last: batches of short sequences are chains of such units.
+//   * A tile (256 rows of K and of V, two bulk copies) is shared by the CTA's eight warps, 32 rows each; the warp that is
+//     the last to finish with a stage refills it, so no warp waits for another and none is spent on copying (a ring per warp
+//     cost a quarter of all instructions).  Copies run on across units: batches of short sequences are chains of units, and
+//     a unit that one CTA scans alone is written out directly.
 // Rows past the end of a sequence get weight, step and middle zero by selection; their bytes may be anything.
 // Every mbarrier wait is bounded: on timeout the CTA records RAP_ETIMEOUT and leaves.
 #pragma once
@@ -44,9 +46,9 @@ constexpr float Q4_WEIGHT_MAX = 32768.f; // a scaled weight above this raises th
 constexpr int Q4_BR = 32;                // rows per warp block
 constexpr int Q4_NW = 8;                 // warps per CTA
 constexpr int Q4_TILE = Q4_NW * Q4_BR;   // rows per CTA tile
-constexpr int Q4_MAX_STG = 8;
+constexpr int Q4_MAX_STG = 8;            // stages of one tile each
 constexpr int Q4_FLUSH = 16;             // blocks between two moves of the accumulators into shared memory
-constexpr int Q4_OFF_MAIN = 1024 + 128;  // barriers, merge scalars and flags below
+constexpr int Q4_OFF_MAIN = 768;         // barriers, counters, merge scalars and flags below
 constexpr int Q4_PAD = 64;               // the last row's fragment loads may reach one word past it
 
 // KSW, VSW: words per K / V row (odd); GC: heads per lane (1: up to four heads, the two parts of a weight on neighbouring
@@ -58,13 +60,13 @@ struct Q4Cfg {
   static constexpr int NT = 2 * NGV;                                  // tiles of 16 channels
   static constexpr int CW = 32 * NGV;                                 // channel slots of the reduction buffer
   static constexpr int MAIN_F = 4 * GC * CW;                          // floats per warp: fp32 sums, then [4 GC][CW] for the merge
-  static constexpr int STAGE_W = Q4_BR * (KSW + VSW);                 // words per stage
+  static constexpr int STAGE_W = Q4_TILE * (KSW + VSW);               // words per stage
   static constexpr int OFF_RING = Q4_OFF_MAIN + Q4_NW * MAIN_F * 4;
-  static constexpr int FIT = (SMEM_BUDGET - OFF_RING - Q4_PAD) / (Q4_NW * STAGE_W * 4);
-  static constexpr int NSTG = FIT < Q4_MAX_STG ? FIT : Q4_MAX_STG;    // stages per warp: 3 for rows of 90, 2 for rows of 128
-  static constexpr int SMEM = OFF_RING + Q4_NW * NSTG * STAGE_W * 4 + Q4_PAD;
+  static constexpr int FIT = (SMEM_BUDGET - OFF_RING - Q4_PAD) / (STAGE_W * 4);
+  static constexpr int NSTG = FIT < Q4_MAX_STG ? FIT : Q4_MAX_STG;    // 3 for rows of 90, 2 for rows of 128
+  static constexpr int SMEM = OFF_RING + NSTG * STAGE_W * 4 + Q4_PAD;
   static_assert(NSTG >= 2 && SMEM <= SMEM_BUDGET, "ring does not fit");
-  static_assert(OFF_RING % 128 == 0 && Q4_NW * MAIN_F >= RAP_MAX_GROUP * (RAP_MAX_SPLIT + 1), "merge weights fit");
+  static_assert(OFF_RING % 128 == 0 && STAGE_W % 32 == 0 && Q4_NW * MAIN_F >= RAP_MAX_GROUP * (RAP_MAX_SPLIT + 1), "merge weights fit");
 };
 
 struct Q4ScanParams {
@@ -73,14 +75,14 @@ struct Q4ScanParams {
 };
 
 __device__ __forceinline__ void q4_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // the same with accumulators that start from (c0, c1) in both halves
 __device__ __forceinline__ void q4_mma_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                             uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
 }
@@ -106,17 +108,22 @@ __device__ __forceinline__ float q4_high(uint32_t h2) {
 }
 __device__ __forceinline__ uint32_t q4_transpose(uint32_t x) {      // an 8x8 tile of 16-bit numbers across the warp
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
 __device__ __forceinline__ float q4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
 __device__ __forceinline__ int q4_exponent(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
-constexpr uint32_t Q4_LO = 0x003c003cu, Q4_HI = 0x03c003c0u;
-// the codes in the high position with the second row's complemented, (y ^ flip) & Q4_HI with flip = 0x03c00000 in a register:
-// one instruction, where two immediates would make two
+// two codes with the second row's complemented, (y ^ flip) & MASK with flip in a register: one instruction, where two
+// immediates would make two
+template <uint32_t MASK>
 __device__ __forceinline__ uint32_t q4_pair(uint32_t y, uint32_t flip) {
   uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(y), "r"(flip), "r"(Q4_HI));
+  asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(y), "r"(flip), "n"(MASK));
+  return r;
+}
+__device__ __forceinline__ uint32_t q4_mul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 
@@ -128,13 +135,14 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
   constexpr int NGK = C::NGK, NGV = C::NGV, NT = C::NT, CW = C::CW, MV = 2 * GC;      // MV: sums per lane and tile
   extern __shared__ __align__(128) unsigned char q4_smem[];
   unsigned char* const smem = q4_smem;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                        // [NW][Q4_MAX_STG]
-  float* m_s = reinterpret_cast<float*>(smem + NW * Q4_MAX_STG * 8);         // [NW][8] reference maxima of the warps
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                        // [Q4_MAX_STG] a stage's copies have landed
+  int* used = reinterpret_cast<int*>(smem + Q4_MAX_STG * 8);                 // [Q4_MAX_STG] warps that are done with a stage
+  float* m_s = reinterpret_cast<float*>(smem + Q4_MAX_STG * 12);             // [NW][8] reference maxima of the warps
   float* l_s = m_s + NW * 8;                                                 // [NW][8] scaled row sums
   int* s_flag = reinterpret_cast<int*>(l_s + NW * 8);                        // time-out seen by any warp
   int* s_last = s_flag + 1;
   float* red = reinterpret_cast<float*>(smem + Q4_OFF_MAIN);                 // [NW][MAIN_F]: sums, merge buffer, merge weights
-  static_assert(NW * Q4_MAX_STG * 8 + NW * 64 + 8 <= Q4_OFF_MAIN, "barriers and merge scalars sit below");
+  static_assert(Q4_MAX_STG * 12 + NW * 64 + 8 <= Q4_OFF_MAIN, "barriers and merge scalars sit below");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gid = lane >> 2, tq = lane & 3;
@@ -147,7 +155,7 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
     // the plan (reads the lengths only): computed by the first warp where the ring will be
     int* pref = reinterpret_cast<int*>(smem + C::OFF_RING);
     const bool shared_plan = sk_plan_shared(p.seq_len, p.B, p.Hkv, p.len_add, p.S_cap, ST, (int)gridDim.x, pref,
-                                            NW * NSTG * C::STAGE_W, &plan);
+                                            NSTG * C::STAGE_W, &plan);
     if (!shared_plan) plan = sk_plan(p.seq_len, p.B, p.Hkv, p.len_add, p.S_cap, ST, (int)gridDim.x);
     // everything below reads what the previous kernel in the stream wrote, and writes what the next one may depend on
     pdl_wait();
@@ -186,13 +194,16 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
     b = blockIdx.z;
     h = blockIdx.y;
   }
-  const uint32_t bar0 = smem_u32(bars) + warp * Q4_MAX_STG * 8;               // this warp's barriers
-  const uint32_t* ring = reinterpret_cast<const uint32_t*>(smem + C::OFF_RING) + warp * NSTG * C::STAGE_W;   // and stages
+  const uint32_t bar0 = smem_u32(bars);
+  const uint32_t* ring = reinterpret_cast<const uint32_t*>(smem + C::OFF_RING);
   const uint32_t ring_u = smem_u32(ring);
-  float* const my_main = red + warp * C::MAIN_F;                              // and sums: [tile][lane][MV] while scanning
+  float* const my_main = red + warp * C::MAIN_F;                              // this warp's sums: [tile][lane][MV] while scanning
   if (tid == 0) {
     *s_flag = 0;
-    for (int i = 0; i < NW * Q4_MAX_STG; ++i) mbar_init(smem_u32(bars) + 8 * i, 1);
+    for (int i = 0; i < Q4_MAX_STG; ++i) {
+      mbar_init(bar0 + 8 * i, 1);
+      used[i] = 0;
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the plan's stores, before copies land on them
@@ -200,37 +211,23 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
 
   // Fragment addressing inside a stage (words).  K: half-tile t, tile row gid: block row 4 gid + t, word 4 j + tq of group
   // j.  V: k-slots 2 tq, 2 tq + 1 of half-tile t: block rows 8 tq + t and 8 tq + 4 + t.
-  const int k_at = 4 * gid * KSW + tq;
-  const int v_at = Q4_BR * KSW + 8 * tq * VSW + gid;
-  const int vh_at = 2 * (Q4_BR * KSW + 8 * tq * VSW) + 8 * (NGV - 1) + gid;     // half words: the last, odd group of 32
-  const int ksz_at = 4 * gid * KSW + KSW - 1, vsz_at = Q4_BR * KSW + 4 * gid * VSW + VSW - 1;
+  const int k_blk = Q4_BR * warp * KSW, v_blk = Q4_TILE * KSW + Q4_BR * warp * VSW;      // this warp's block of a tile
+  const int k_at = k_blk + 4 * gid * KSW + tq;
+  const int v_at = v_blk + 8 * tq * VSW + gid;
+  const int vh_at = 2 * (v_blk + 8 * tq * VSW) + 8 * (NGV - 1) + gid;     // half words: the last, odd group of 32
+  const int ksz_at = k_blk + 4 * gid * KSW + KSW - 1, vsz_at = v_blk + 4 * gid * VSW + VSW - 1;
   const float row_sign = (gid & 1) ? -1.f : 1.f;      // rows 4 gid + t of odd gid are the second of their pair
-  uint32_t flip;
-  asm volatile("mov.b32 %0, 0x03c00000;" : "=r"(flip));
-  int st = 0, st_issue = 0;    // ring positions of the next block to use and to copy, running on across units
+  constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, up = 0x64006400u;      // up: 2^10 twice
+  uint32_t flip0, flip4;
+  asm volatile("mov.b32 %0, 0x000f0000;" : "=r"(flip0));
+  asm volatile("mov.b32 %0, 0x00f00000;" : "=r"(flip4));
+  int st = 0;                  // ring position of the next tile, running on across units
   uint32_t parity = 0;
   bool timed_out = false;
 
-  // the segment being scanned: tiles [t_begin, t_begin + n_my) of unit (b, h), seg_tiles in all; this warp's blocks are the
-  // rows [(t_begin + i) ST + 32 warp, + 32) for i < n_blk, those that hold a valid row
-  int len = 0, seg_tiles = 0, t_begin = 0, n_my = 0, row_w = 0, n_blk = 0;
-  auto issue_block = [&](int i) {                     // all lanes converged; lane 0 issues
-    const int j0 = row_w + i * ST;
-    const int rows = min(Q4_BR, ((len + 7) & ~7) - j0);      // rows a copy may touch: S_cap is a multiple of 8
-    const uint32_t kb = (uint32_t)rows * 4 * KSW, vb = (uint32_t)rows * 4 * VSW;     // multiples of 16: rows is a multiple of 8
-    if (lane == 0 && RAP_BOUNDS(j0 + rows - 1, p.S_cap, p.status, 0x402) && RAP_BOUNDS(rows - 1, Q4_BR, p.status, 0x404) &&
-        RAP_BOUNDS(st_issue, NSTG, p.status, 0x403)) {
-      const uint32_t bar = bar0 + 8 * st_issue, dst = ring_u + 4 * st_issue * C::STAGE_W;
-      const size_t row0 = ((size_t)b * p.Hkv + h) * (size_t)p.S_cap + j0;
-      mbar_expect_tx(bar, kb + vb);
-      if (!(p.dbg_skip_copy && blockIdx.x == 0 && warp == 0 && i == 0)) {
-        bulk_g2s(dst, p.k + row0 * (4 * KSW), kb, bar);
-        bulk_g2s(dst + 4 * Q4_BR * KSW, p.v + row0 * (4 * VSW), vb, bar);
-      }
-    }
-    if (++st_issue == NSTG) st_issue = 0;
-  };
-  auto start_segment = [&]() {                        // lengths and first copies of unit (b, h) from tile t_begin on
+  // the segment being scanned: tiles [t_begin, t_begin + n_my) of unit (b, h), seg_tiles in all
+  int len = 0, seg_tiles = 0, t_begin = 0, n_my = 0;
+  auto segment = [&]() {
     len = min(max(p.seq_len[b] + p.len_add, 0), p.S_cap);
     seg_tiles = (len + ST - 1) / ST;
     if (p.balanced) {
@@ -241,12 +238,8 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
       t_begin = min(seg_tiles, (int)blockIdx.x * tps);
       n_my = min(seg_tiles, t_begin + tps) - t_begin;
     }
-    row_w = t_begin * ST + Q4_BR * warp;
-    n_blk = len > row_w ? min(n_my, (len - row_w + ST - 1) / ST) : 0;
-    const int pre = min(n_blk, NSTG - 1);
-    for (int i = 0; i < pre; ++i) issue_block(i);
   };
-  start_segment();
+  segment();
   if (n_my <= 0) {             // (equal ranges only) nothing to scan: neutral partials
     float* base = p.ws + (((size_t)b * p.Hq + (size_t)h * G) * p.n_split + blockIdx.x) * (size_t)(DV + 2);
     for (int i = tid; i < G * (DV + 2); i += THREADS) {
@@ -255,11 +248,43 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
     }
     return;
   }
+  // Copies run ahead of the scan over the CTA's whole tile sequence, unit borders included: copy_ahead brings the tile that
+  // lies k >= 0 places behind the current segment's first one (by one lane), if the CTA has it.
+  const int seq_tiles = p.balanced ? hi - cur : n_my;
+  int done = 0;                // tiles of the segments before this one
+  auto copy_ahead = [&](int k, int stg) {
+    if (done + k >= seq_tiles) return;
+    int ib = b, ih = h, ilen = len, it = t_begin + k;
+    for (int n = seg_tiles; it >= n;) {               // a later unit (only in balanced mode)
+      it -= n;
+      if (++ih == p.Hkv) {
+        ih = 0;
+        do { ++ib; } while (ib < p.B - 1 && sk_tiles_of(p.seq_len, ib, p.len_add, p.S_cap, ST) == 0);
+        ilen = min(max(p.seq_len[ib] + p.len_add, 0), p.S_cap);
+        n = (ilen + ST - 1) / ST;
+      }
+    }
+    const int j0 = it * ST;
+    const int rows = min(ST, ((ilen + 7) & ~7) - j0);        // rows a copy may touch: S_cap is a multiple of 8
+    if (RAP_BOUNDS(j0 + rows - 1, p.S_cap, p.status, 0x402) && RAP_BOUNDS(rows - 1, ST, p.status, 0x404) &&
+        RAP_BOUNDS(stg, NSTG, p.status, 0x403) && RAP_BOUNDS(ib, p.B, p.status, 0x401)) {
+      const uint32_t kb = (uint32_t)rows * 4 * KSW, vb = (uint32_t)rows * 4 * VSW;     // multiples of 16: rows is a multiple of 8
+      const uint32_t bar = bar0 + 8 * stg, dst = ring_u + 4 * stg * C::STAGE_W;
+      const size_t row0 = ((size_t)ib * p.Hkv + ih) * (size_t)p.S_cap + j0;
+      mbar_expect_tx(bar, kb + vb);
+      if (!(p.dbg_skip_copy && blockIdx.x == 0 && done + k == 0)) {
+        bulk_g2s(dst, p.k + row0 * (4 * KSW), kb, bar);
+        bulk_g2s(dst + 4 * ST * KSW, p.v + row0 * (4 * VSW), vb, bar);
+      }
+    }
+  };
+  if (tid == 0)
+    for (int i = 0; i < NSTG; ++i) copy_ahead(i, i);
 
   for (;;) {   // one pass per segment (a single one unless the mode is balanced)
     // ---- q as the B operand: column gid is head gid / 2 on even columns (GC = 1) or head gid (GC = 2), else zeros.  Of
-    // word w = 4 j + tq of a row: k-slots 2 tq, 2 tq + 1 and 2 tq + 8, 2 tq + 9 hold dims 8 w + (0, 4) and (2, 6) in the
-    // step of the low position (with 16 q: its codes count 2^-22), (1, 5) and (3, 7) in that of the high one (2^-18). ----
+    // word w = 4 j + tq of a row: k-slots 2 tq, 2 tq + 1 and 2 tq + 8, 2 tq + 9 hold dims 8 w + (0, 4) and (2, 6) in one
+    // step, (1, 5) and (3, 7) in the next; a code counts 2^-24, 2^-22 and 2^-20, 2^-18 there, which q makes up for. ----
     uint32_t qa[NGK][2], qb[NGK][2];
     float off[2], f_q[GC], zq[GC], m_ref[GC], l_thr[GC], z_thr[GC];
     {
@@ -285,7 +310,7 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int e = min(max(10 - q4_exponent(top), -100), 120);       // the largest |q| 2^e lies in [2^10, 2^11)
+      const int e = min(max(8 - q4_exponent(top), -100), 120);        // the largest |q| 2^e lies in [2^8, 2^9)
       const float sc = q4_pow2(e);
       float seen = 0.f;            // sum of q 2^e as the MMAs see it
 #pragma unroll
@@ -296,13 +321,12 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
           x[2 * i] = __uint_as_float(w[j][i] << 16) * sc;
           x[2 * i + 1] = __uint_as_float(w[j][i] & 0xffff0000u) * sc;
         }
-        qa[j][0] = q4_pack(16.f * x[0], 16.f * x[4]);
+        qa[j][0] = q4_pack(64.f * x[0], 64.f * x[4]);
         qa[j][1] = q4_pack(16.f * x[2], 16.f * x[6]);
-        qb[j][0] = q4_pack(x[1], x[5]);
+        qb[j][0] = q4_pack(4.f * x[1], 4.f * x[5]);
         qb[j][1] = q4_pack(x[3], x[7]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          seen += 0.0625f * (q4_low(qa[j][i]) + q4_high(qa[j][i])) + (q4_low(qb[j][i]) + q4_high(qb[j][i]));
+        seen += 0.015625f * (q4_low(qa[j][0]) + q4_high(qa[j][0])) + 0.0625f * (q4_low(qa[j][1]) + q4_high(qa[j][1])) +
+                0.25f * (q4_low(qb[j][0]) + q4_high(qb[j][0])) + (q4_low(qb[j][1]) + q4_high(qb[j][1]));
       }
       seen += __shfl_xor_sync(0xffffffffu, seen, 1);
       seen += __shfl_xor_sync(0xffffffffu, seen, 2);
@@ -328,9 +352,9 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
     float vn = 1.f;              // power of two the steps of V are scaled by
     bool have_main = false;      // the sums in shared memory hold something
     // the accumulators, less 7.5 per summed (signed) weight, plus what shared memory holds of them; channel rows gid (r = 0)
-    // and gid + 8 (1) of tile t, in units of 2^-18.  GC = 1: both columns belong to one head.
+    // and gid + 8 (1) of tile t, in units of 2^-14 and 2^-20.  GC = 1: both columns belong to one head.
     auto total = [&](int t, int r, int g) {
-      constexpr float unit = -7.5f * 0x1p-18f;
+      const float unit = r ? -7.5f * 0x1p-20f : -7.5f * 0x1p-14f;
       float v = GC == 1 ? fmaf(unit, dsum[0], o[t][2 * r]) + fmaf(unit, dsum[1], o[t][2 * r + 1]) : fmaf(unit, dsum[g], o[t][2 * r + g]);
       if (have_main) v += my_main[(t * 32 + lane) * MV + r * GC + g];
       return v;
@@ -346,10 +370,11 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
 #pragma unroll
         for (int j = 0; j < NGK; ++j) {
           const uint32_t x0 = sw[k_at + 2 * mt * KSW + 4 * j], x1 = sw[k_at + (2 * mt + 1) * KSW + 4 * j];
-          const uint32_t l0 = x0 << 2, l1 = x1 << 2, h0 = x0 >> 6, h1 = x1 >> 6;
-          if (j == 0) q4_mma_from(s[mt], off[0], off[1], l0 & Q4_LO, l1 & Q4_LO, h0 & Q4_LO, h1 & Q4_LO, qa[j][0], qa[j][1]);
-          else q4_mma(s[mt], l0 & Q4_LO, l1 & Q4_LO, h0 & Q4_LO, h1 & Q4_LO, qa[j][0], qa[j][1]);
-          q4_mma(s[mt], l0 & Q4_HI, l1 & Q4_HI, h0 & Q4_HI, h1 & Q4_HI, qb[j][0], qb[j][1]);
+          const uint32_t h0 = x0 >> 6, h1 = x1 >> 6;
+          const uint32_t a0 = x0 & 0x000f000fu, a1 = x1 & 0x000f000fu, a2 = h0 & 0x003c003cu, a3 = h1 & 0x003c003cu;
+          if (j == 0) q4_mma_from(s[mt], off[0], off[1], a0, a1, a2, a3, qa[j][0], qa[j][1]);
+          else q4_mma(s[mt], a0, a1, a2, a3, qa[j][0], qa[j][1]);
+          q4_mma(s[mt], x0 & 0x00f000f0u, x1 & 0x00f000f0u, h0 & 0x03c003c0u, h1 & 0x03c003c0u, qb[j][0], qb[j][1]);
         }
       }
       // ---- logits in base 2 less the reference maximum; weights times the (scaled, signed) V steps ----
@@ -452,10 +477,14 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         // four channels of 16 rows: y holds k-slots 2 tq, 2 tq + 1, z those + 8; codes 0 .. 3 go to rows gid and
         // gid + 8 of two tiles
         auto tiles = [&](float (&acc0)[4], float (&acc1)[4], uint32_t y, uint32_t z) {
-          const uint32_t a0 = q4_pair(y << 6, flip), a1 = q4_pair(y << 2, flip), a2 = q4_pair(z << 6, flip), a3 = q4_pair(z << 2, flip);
+          const uint32_t a0 = q4_mul2(q4_pair<LO>(y, flip0), up), a1 = q4_pair<HI>(y, flip4);
+          const uint32_t a2 = q4_mul2(q4_pair<LO>(z, flip0), up), a3 = q4_pair<HI>(z, flip4);
           q4_mma(acc0, a0, a1, a2, a3, b0, b1);
           if constexpr (GC == 2) q4_mma(acc0, a0, a1, a2, a3, c0, c1);
-          const uint32_t d0 = q4_pair(y >> 2, flip), d1 = q4_pair(y >> 6, flip), d2 = q4_pair(z >> 2, flip), d3 = q4_pair(z >> 6, flip);
+          y >>= 8;
+          z >>= 8;
+          const uint32_t d0 = q4_mul2(q4_pair<LO>(y, flip0), up), d1 = q4_pair<HI>(y, flip4);
+          const uint32_t d2 = q4_mul2(q4_pair<LO>(z, flip0), up), d3 = q4_pair<HI>(z, flip4);
           q4_mma(acc1, d0, d1, d2, d3, b0, b1);
           if constexpr (GC == 2) q4_mma(acc1, d0, d1, d2, d3, c0, c1);
         };
@@ -479,14 +508,15 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
       }
     };
 
-    for (int i = 0; i < n_blk; ++i) {
-      if (i + NSTG - 1 < n_blk) issue_block(i + NSTG - 1);
-      if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar0 + 8 * st, parity, p.wait_limit))) {   // warp-uniform verdict
+    bool fresh = true;           // no row of this segment so far
+    int nrows = len - t_begin * ST - Q4_BR * warp;      // valid rows from this warp's block on
+    for (int i = 0; i < n_my; ++i, nrows -= ST) {
+      if (__any_sync(0xffffffffu, !mbar_test_wait(bar0 + 8 * st, parity)) &&
+          !__all_sync(0xffffffffu, mbar_wait_slow(bar0 + 8 * st, parity, p.wait_limit))) {   // warp-uniform verdict
         timed_out = true;
         break;
       }
       const uint32_t* sw = ring + st * C::STAGE_W;
-      const int nrows = len - (row_w + i * ST);      // valid rows of this block (>= 1)
       bool in_ok = true;
 #ifdef RAP_DEBUG_BOUNDS
       const int at = (int)(sw - reinterpret_cast<const uint32_t*>(smem));      // the largest offsets this lane reads
@@ -495,9 +525,10 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
                                           RAP_BOUNDS(2 * at + vh_at + 14 * VSW, C::SMEM / 2, p.status, 0x407) &&
                                           RAP_BOUNDS(at + vsz_at + 3 * VSW, C::SMEM / 4, p.status, 0x408));
 #endif
-      if (in_ok) {
-        if (nrows >= Q4_BR) block(std::false_type{}, sw, nrows, i == 0);
-        else block(std::true_type{}, sw, nrows, i == 0);
+      if (in_ok && nrows > 0) {
+        if (nrows >= Q4_BR) block(std::false_type{}, sw, nrows, fresh);
+        else block(std::true_type{}, sw, nrows, fresh);
+        fresh = false;
       }
       if ((i & (Q4_FLUSH - 1)) == Q4_FLUSH - 1) {
 #pragma unroll
@@ -509,7 +540,16 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         dsum[0] = dsum[1] = dsum[2] = dsum[3] = 0.f;
         have_main = true;
       }
-      __syncwarp();            // every lane is done with this stage before lane 0 refills it
+      // this warp is done with the stage (its loads have been used); the last one of the CTA refills it
+      __syncwarp();
+      if (lane == 0) {
+        __threadfence_block();
+        if (atomicAdd(&used[st], 1) == NW - 1) {
+          used[st] = 0;
+          __threadfence_block();
+          copy_ahead(i + NSTG, st);
+        }
+      }
       if (++st == NSTG) { st = 0; parity ^= 1u; }
     }
 
@@ -541,7 +581,7 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         p.status[1] = (b * p.Hkv + h) * RAP_MAX_SPLIT + (int)(blockIdx.x % RAP_MAX_SPLIT);
       }
       // give copies still in flight a bounded chance to land before the shared memory is released
-      if (lane == 0)
+      if (tid == 0)
         for (int sg = 0; sg < NSTG; ++sg) {
           mbar_wait_bounded(bar0 + 8 * sg, 0, p.wait_limit);
           mbar_wait_bounded(bar0 + 8 * sg, 1, p.wait_limit);
@@ -564,24 +604,24 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         for (int t = 0; t < NT; ++t) {
           const bool wide = t < 4 * (NGV / 2);
           const int c = wide ? 64 * (t / 4) + 8 * gid + 2 * (t % 4) : 32 * (NGV - 1) + 4 * gid + 2 * (t % 2);
-          rr[c] = fmaf(o[t][g] * 0x1p18f, unscale, z_thr[g]) * f;
-          rr[c + 1] = fmaf(o[t][GC + g] * 0x1p18f, unscale, z_thr[g]) * f;
+          rr[c] = fmaf(o[t][g] * 0x1p14f, unscale, z_thr[g]) * f;
+          rr[c + 1] = fmaf(o[t][GC + g] * 0x1p20f, unscale, z_thr[g]) * f;
         }
       }
     }
-    // this segment's place; then the next one's first copies, under the merge
-    const int b0 = b, h0 = h, start0 = unit_start, tiles0 = seg_tiles;
+    const int b0 = b, h0 = h, start0 = unit_start, tiles0 = seg_tiles;      // this segment's place
     bool more = false;
     if (p.balanced) {
       cur += n_my;
-      if (cur < hi) {
+      done += n_my;
+      more = cur < hi;
+      if (more) {              // the following unit, from its first tile
         unit_start += seg_tiles;
         if (++h == p.Hkv) {
           h = 0;
-          do { ++b; } while (b < p.B && sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST) == 0);
+          do { ++b; } while (b < p.B - 1 && sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST) == 0);
         }
-        more = b < p.B;
-        if (more) start_segment();
+        segment();
       }
     }
     __syncthreads();
