@@ -149,7 +149,7 @@ def write_scan_sources():
         body = ['// generated by build.py: instantiations of the tensor-core scan over a 4-bit cache, part %d' % k,
                 '#include "rap_attn_q4_kernel.cuh"', "namespace {",
                 "template <int K, int V, int C> rap_q4_entry entry() {",
-                "  return rap_q4_entry{K, V, C, Q4Cfg<K, V, C>::SMEM, (const void*)attn_q4_kernel<K, V, C>};", "}", "}  // namespace",
+                "  return rap_q4_entry{K, V, C, Q4Cfg<K, V, C>::SMEM, Q4Cfg<K, V, C>::NW * 32, (const void*)attn_q4_kernel<K, V, C>};", "}", "}  // namespace",
                 "const rap_q4_entry* rap_q4_table_%d(int* n) {" % k, "  static const rap_q4_entry table[] = {"]
         body += ["    entry<%d, %d, %d>()," % sh for sh in mine]
         body += ["  };", "  *n = (int)(sizeof(table) / sizeof(table[0]));", "  return table;", "}", ""]

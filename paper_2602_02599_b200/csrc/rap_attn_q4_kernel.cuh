@@ -17,8 +17,9 @@
 //     (19 bits together).  Up to four heads they are two columns of one MMA, beyond that two MMAs.  The tensor core aligns
 //     the 16 products of a step by their exponents and cuts them off below, and a subnormal operand brings its leading
 //     zeros along: hence the short first part, and all V codes in the highest position (output off by 7e-6 from bits 0..3,
-//     9e-7 from bits 4..7).  Weights are scaled by a power of two per warp that follows the largest seen, so that steps
-//     of any magnitude stay inside fp16.  The middles are summed apart, in fp32.
+//     9e-7 from bits 4..7).  The softmax reference is not the largest logit but the one that makes the largest weight,
+//     its step included, 4 .. 8 (raised when one passes 2^15), so that steps of any magnitude stay inside fp16; a power of
+//     two in every weight drops out of the quotient.  The middles are summed apart, in fp32.
 //   * The codes 0..15 are 7.5 off centre, and a tensor core's running sum, which is cut off rather than rounded, must not
 //     carry an offset that grows with the row: of every two rows that share an operand register the second enters with its
 //     codes complemented (15 - c, the same mask operation) and its weight negated, so the offsets alternate in sign (output
@@ -28,10 +29,10 @@
 //   * Weights leave the first MMA with rows on M and enter the second with rows on K: one 8x8 transpose per 8 rows.
 //   * Block row of tile row i (0..7) of half-tile t is 4 i + t: rows of an odd number of words then start on eight
 //     banks, four apart, and all fragment and scale loads are free of conflicts.
-//   * A tile (256 rows of K and of V, two bulk copies) is shared by the CTA's eight warps, 32 rows each; the warp that is
-//     the last to finish with a stage refills it, so no warp waits for another and none is spent on copying (a ring per warp
-//     cost a quarter of all instructions).  Copies run on across units: batches of short sequences are chains of units, and
-//     a unit that one CTA scans alone is written out directly.
+//   * A tile (256 rows of K and of V, two bulk copies) is shared by the CTA's eight warps, 32 rows each; they take turns to
+//     refill the stage of the tile before, once all are done with it (a ring per warp cost a quarter of all instructions).
+//     Copies run on across units: batches of short sequences are chains of units, and a unit that one CTA scans alone is
+//     written out directly.
 // Rows past the end of a sequence get weight, step and middle zero by selection; their bytes may be anything.
 // Every mbarrier wait is bounded: on timeout the CTA records RAP_ETIMEOUT and leaves.
 #pragma once
@@ -42,13 +43,11 @@
 
 namespace {
 
-constexpr float Q4_WEIGHT_MAX = 32768.f; // a scaled weight above this raises the reference maximum and the steps' scale
+constexpr float Q4_WEIGHT_MAX = 32768.f; // a weight (step included) above this raises the reference of its head
 constexpr int Q4_BR = 32;                // rows per warp block
-constexpr int Q4_NW = 8;                 // warps per CTA
-constexpr int Q4_TILE = Q4_NW * Q4_BR;   // rows per CTA tile
 constexpr int Q4_MAX_STG = 8;            // stages of one tile each
 constexpr int Q4_FLUSH = 16;             // blocks between two moves of the accumulators into shared memory
-constexpr int Q4_OFF_MAIN = 768;         // barriers, counters, merge scalars and flags below
+constexpr int Q4_OFF_MAIN = 896;         // barriers, merge scalars and flags below
 constexpr int Q4_PAD = 64;               // the last row's fragment loads may reach one word past it
 
 // KSW, VSW: words per K / V row (odd); GC: heads per lane (1: up to four heads, the two parts of a weight on neighbouring
@@ -57,16 +56,18 @@ template <int KSW, int VSW, int GC>
 struct Q4Cfg {
   static_assert(KSW % 2 == 1 && VSW % 2 == 1 && KSW <= 17 && VSW <= 17, "rows of up to 128 codes");
   static constexpr int NGK = (KSW + 2) / 4, NGV = (VSW + 2) / 4;      // groups of 4 words: 32 dims / channels
+  static constexpr int NW = 8;                                    // warps per CTA (ten, at 96 registers, measured 8% slower)
+  static constexpr int TILE = NW * Q4_BR;                             // rows per CTA tile
   static constexpr int NT = 2 * NGV;                                  // tiles of 16 channels
   static constexpr int CW = 32 * NGV;                                 // channel slots of the reduction buffer
   static constexpr int MAIN_F = 4 * GC * CW;                          // floats per warp: fp32 sums, then [4 GC][CW] for the merge
-  static constexpr int STAGE_W = Q4_TILE * (KSW + VSW);               // words per stage
-  static constexpr int OFF_RING = Q4_OFF_MAIN + Q4_NW * MAIN_F * 4;
+  static constexpr int STAGE_W = TILE * (KSW + VSW);               // words per stage
+  static constexpr int OFF_RING = Q4_OFF_MAIN + NW * MAIN_F * 4;
   static constexpr int FIT = (SMEM_BUDGET - OFF_RING - Q4_PAD) / (STAGE_W * 4);
   static constexpr int NSTG = FIT < Q4_MAX_STG ? FIT : Q4_MAX_STG;    // 3 for rows of 90, 2 for rows of 128
   static constexpr int SMEM = OFF_RING + NSTG * STAGE_W * 4 + Q4_PAD;
   static_assert(NSTG >= 2 && SMEM <= SMEM_BUDGET, "ring does not fit");
-  static_assert(OFF_RING % 128 == 0 && STAGE_W % 32 == 0 && Q4_NW * MAIN_F >= RAP_MAX_GROUP * (RAP_MAX_SPLIT + 1), "merge weights fit");
+  static_assert(OFF_RING % 128 == 0 && STAGE_W % 32 == 0 && NW * MAIN_F >= RAP_MAX_GROUP * (RAP_MAX_SPLIT + 1), "merge weights fit");
 };
 
 struct Q4ScanParams {
@@ -79,12 +80,20 @@ __device__ __forceinline__ void q4_mma(float (&c)[4], uint32_t a0, uint32_t a1, 
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// the same with accumulators that start from (c0, c1) in both halves
-__device__ __forceinline__ void q4_mma_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+// the same with other accumulators to start from
+__device__ __forceinline__ void q4_mma_from(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                             uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
-               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+// a value the compiler takes for unknown, so that it stays in its register instead of being made anew at every use
+template <bool KEEP>
+__device__ __forceinline__ uint32_t q4_keep(uint32_t x) {
+  if constexpr (!KEEP) return x;
+  uint32_t r;
+  asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 __device__ __forceinline__ float q4_ex2(float x) {      // 2^x, one instruction; 2^(-inf) = 0
   float y;
@@ -128,21 +137,20 @@ __device__ __forceinline__ uint32_t q4_mul2(uint32_t a, uint32_t b) {
 }
 
 template <int KSW, int VSW, int GC>
-__global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanParams pp) {
+__global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kernel(const Q4ScanParams pp) {
   using C = Q4Cfg<KSW, VSW, GC>;
   const ScanParams& p = pp.s;
-  constexpr int NW = Q4_NW, THREADS = NW * 32, ST = Q4_TILE, NSTG = C::NSTG;
+  constexpr int NW = C::NW, THREADS = NW * 32, ST = C::TILE, NSTG = C::NSTG;
   constexpr int NGK = C::NGK, NGV = C::NGV, NT = C::NT, CW = C::CW, MV = 2 * GC;      // MV: sums per lane and tile
   extern __shared__ __align__(128) unsigned char q4_smem[];
   unsigned char* const smem = q4_smem;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                        // [Q4_MAX_STG] a stage's copies have landed
-  int* used = reinterpret_cast<int*>(smem + Q4_MAX_STG * 8);                 // [Q4_MAX_STG] warps that are done with a stage
-  float* m_s = reinterpret_cast<float*>(smem + Q4_MAX_STG * 12);             // [NW][8] reference maxima of the warps
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                        // [Q4_MAX_STG] a stage's copies have landed; [Q4_MAX_STG] its warps are done with it
+  float* m_s = reinterpret_cast<float*>(smem + Q4_MAX_STG * 16);             // [NW][8] references of the warps
   float* l_s = m_s + NW * 8;                                                 // [NW][8] scaled row sums
   int* s_flag = reinterpret_cast<int*>(l_s + NW * 8);                        // time-out seen by any warp
   int* s_last = s_flag + 1;
   float* red = reinterpret_cast<float*>(smem + Q4_OFF_MAIN);                 // [NW][MAIN_F]: sums, merge buffer, merge weights
-  static_assert(Q4_MAX_STG * 12 + NW * 64 + 8 <= Q4_OFF_MAIN, "barriers and merge scalars sit below");
+  static_assert(Q4_MAX_STG * 16 + NW * 64 + 8 <= Q4_OFF_MAIN, "barriers and merge scalars sit below");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gid = lane >> 2, tq = lane & 3;
@@ -202,7 +210,7 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
     *s_flag = 0;
     for (int i = 0; i < Q4_MAX_STG; ++i) {
       mbar_init(bar0 + 8 * i, 1);
-      used[i] = 0;
+      mbar_init(bar0 + 8 * (Q4_MAX_STG + i), NW);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -211,18 +219,23 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
 
   // Fragment addressing inside a stage (words).  K: half-tile t, tile row gid: block row 4 gid + t, word 4 j + tq of group
   // j.  V: k-slots 2 tq, 2 tq + 1 of half-tile t: block rows 8 tq + t and 8 tq + 4 + t.
-  const int k_blk = Q4_BR * warp * KSW, v_blk = Q4_TILE * KSW + Q4_BR * warp * VSW;      // this warp's block of a tile
+  const int k_blk = Q4_BR * warp * KSW, v_blk = C::TILE * KSW + Q4_BR * warp * VSW;      // this warp's block of a tile
   const int k_at = k_blk + 4 * gid * KSW + tq;
   const int v_at = v_blk + 8 * tq * VSW + gid;
   const int vh_at = 2 * (v_blk + 8 * tq * VSW) + 8 * (NGV - 1) + gid;     // half words: the last, odd group of 32
   const int ksz_at = k_blk + 4 * gid * KSW + KSW - 1, vsz_at = v_blk + 4 * gid * VSW + VSW - 1;
-  const float row_sign = (gid & 1) ? -1.f : 1.f;      // rows 4 gid + t of odd gid are the second of their pair
+  const uint32_t row_sign = (gid & 1) ? 0x80000000u : 0u;      // rows 4 gid + t of odd gid are the second of their pair
   constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, up = 0x64006400u;      // up: 2^10 twice
-  uint32_t flip0, flip4;
-  asm volatile("mov.b32 %0, 0x000f0000;" : "=r"(flip0));
-  asm volatile("mov.b32 %0, 0x00f00000;" : "=r"(flip4));
+  const uint32_t flip0 = q4_keep<true>(0x000f0000u), flip4 = q4_keep<true>(0x00f00000u);
+  constexpr bool KEEP = false;
+  const uint32_t one0 = q4_keep<KEEP>(0x3c003c00u), one1 = q4_keep<KEEP>(0x3c003c00u), one2 = q4_keep<KEEP>(0x3c003c00u),
+                 one3 = q4_keep<KEEP>(0x3c003c00u);
   int st = 0;                  // ring position of the next tile, running on across units
   uint32_t parity = 0;
+  // With three stages or more a tile's stage is refilled when the next tile is done (the others have left it by then); with
+  // two that would leave no time for the copy, so the warp whose turn it is waits for the others.
+  constexpr int LAG = NSTG >= 3 ? 1 : 0;
+  int turn = warp + LAG;       // tiles until this warp refills
   bool timed_out = false;
 
   // the segment being scanned: tiles [t_begin, t_begin + n_my) of unit (b, h), seg_tiles in all
@@ -286,7 +299,7 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
     // word w = 4 j + tq of a row: k-slots 2 tq, 2 tq + 1 and 2 tq + 8, 2 tq + 9 hold dims 8 w + (0, 4) and (2, 6) in one
     // step, (1, 5) and (3, 7) in the next; a code counts 2^-24, 2^-22 and 2^-20, 2^-18 there, which q makes up for. ----
     uint32_t qa[NGK][2], qb[NGK][2];
-    float off[2], f_q[GC], zq[GC], m_ref[GC], l_thr[GC], z_thr[GC];
+    float off[4], f_q[GC], zq[GC], m_ref[GC], l_thr[GC], z_thr[GC];
     {
       const int col_head = GC == 1 ? gid >> 1 : gid;
       const bool on = col_head < G && (GC == 2 || (gid & 1) == 0);
@@ -336,7 +349,10 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
       const float cs = p.qscale;   // log2(e) / sqrt(D)
       const float off_c = -7.5f * 0x1p-18f * seen, f_c = cs * q4_pow2(18 - e), z_c = cs * sum;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) off[i] = __shfl_sync(0xffffffffu, off_c, 4 * (2 * tq + i));
+      for (int i = 0; i < 2; ++i) {
+        off[i] = __shfl_sync(0xffffffffu, off_c, 4 * (2 * tq + i));
+        off[2 + i] = __uint_as_float(q4_keep<KEEP>(__float_as_uint(off[i])));
+      }
 #pragma unroll
       for (int i = 0; i < GC; ++i) {
         f_q[i] = __shfl_sync(0xffffffffu, f_c, 4 * (2 * tq + i));
@@ -349,7 +365,6 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
 #pragma unroll
     for (int t = 0; t < NT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
     dsum[0] = dsum[1] = dsum[2] = dsum[3] = 0.f;
-    float vn = 1.f;              // power of two the steps of V are scaled by
     bool have_main = false;      // the sums in shared memory hold something
     // the accumulators, less 7.5 per summed (signed) weight, plus what shared memory holds of them; channel rows gid (r = 0)
     // and gid + 8 (1) of tile t, in units of 2^-14 and 2^-20.  GC = 1: both columns belong to one head.
@@ -372,7 +387,7 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
           const uint32_t x0 = sw[k_at + 2 * mt * KSW + 4 * j], x1 = sw[k_at + (2 * mt + 1) * KSW + 4 * j];
           const uint32_t h0 = x0 >> 6, h1 = x1 >> 6;
           const uint32_t a0 = x0 & 0x000f000fu, a1 = x1 & 0x000f000fu, a2 = h0 & 0x003c003cu, a3 = h1 & 0x003c003cu;
-          if (j == 0) q4_mma_from(s[mt], off[0], off[1], a0, a1, a2, a3, qa[j][0], qa[j][1]);
+          if (j == 0) q4_mma_from(s[mt], off, a0, a1, a2, a3, qa[j][0], qa[j][1]);
           else q4_mma(s[mt], a0, a1, a2, a3, qa[j][0], qa[j][1]);
           q4_mma(s[mt], x0 & 0x00f000f0u, x1 & 0x00f000f0u, h0 & 0x03c003c0u, h1 & 0x03c003c0u, qb[j][0], qb[j][1]);
         }
@@ -386,25 +401,26 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         if (TAIL && 4 * gid + t >= nrows) ksz[t] = vsz[t] = 0u;
       }
       float e[4][GC], w[4][GC];
-      float big = 0.f;
+      for (bool raised = false;; raised = true) {
+        float big = 0.f;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float ks = q4_step(ksz[t]), kz = q4_middle(ksz[t]), vs = q4_step(vsz[t]) * (vn * row_sign);
+        for (int t = 0; t < 4; ++t) {
+          const float ks = q4_step(ksz[t]), kz = q4_middle(ksz[t]);
+          const float vs = __uint_as_float(vsz[t] * 65536u + row_sign);      // the step, negated on the second row of a pair
 #pragma unroll
-        for (int g = 0; g < GC; ++g) {
-          float x = fmaf(ks * f_q[g], s[t >> 1][2 * (t & 1) + g], fmaf(kz, zq[g], -m_ref[g]));
-          if (TAIL && 4 * gid + t >= nrows) x = -INFINITY;
-          e[t][g] = q4_ex2(x);
-          w[t][g] = e[t][g] * vs;
-          big = q4_max(big, fabsf(w[t][g]));
+          for (int g = 0; g < GC; ++g) {
+            float x = fmaf(ks * f_q[g], s[t >> 1][2 * (t & 1) + g], fmaf(kz, zq[g], -m_ref[g]));
+            if (TAIL && 4 * gid + t >= nrows) x = -INFINITY;
+            e[t][g] = q4_ex2(x);
+            w[t][g] = e[t][g] * vs;
+            big = q4_max(big, fabsf(w[t][g]));
+          }
         }
-      }
-      if (__any_sync(0xffffffffu, first || !(big <= Q4_WEIGHT_MAX))) {
-        // raise the reference maxima to the block's, and set the scale of the steps so that the largest weight is 4 .. 8
-        float a[2], most = 0.f, ratio = 1.f;
+        if (raised || !__any_sync(0xffffffffu, first || !(big <= Q4_WEIGHT_MAX))) break;
+        // raise the references so that the block's largest weight (its step included) becomes 4 .. 8
 #pragma unroll
         for (int g = 0; g < GC; ++g) {
-          float x[4], mx = -3e38f;
+          float x[4], mx = -3e38f, most = 0.f;
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             x[t] = fmaf(q4_step(ksz[t]) * f_q[g], s[t >> 1][2 * (t & 1) + g], q4_middle(ksz[t]) * zq[g]);
@@ -413,40 +429,31 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
           }
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-          const float m_new = fmaxf(m_ref[g], mx);
-          a[g] = a[1] = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
+#pragma unroll
+          for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(vsz[t]));
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+          const float m_new = fmaxf(m_ref[g], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 2, -80), 100) : 0.f));
+          const float alpha = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
           m_ref[g] = m_new;
-          l_thr[g] *= a[g];
-          z_thr[g] *= a[g];
+          l_thr[g] *= alpha;
+          z_thr[g] *= alpha;
+          constexpr int c = GC == 1 ? 2 : 1;                     // columns of this head
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            e[t][g] = q4_ex2(x[t] - m_new);
-            most = fmaxf(most, e[t][g] * q4_step(vsz[t]));
+          for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < c; ++i) {
+              o[t][g + i] *= alpha;
+              o[t][2 + g + i] *= alpha;
+            }
+            if (have_main) {
+              my_main[(t * 32 + lane) * MV + g] *= alpha;
+              my_main[(t * 32 + lane) * MV + GC + g] *= alpha;
+            }
           }
+#pragma unroll
+          for (int i = 0; i < c; ++i) dsum[g + i] *= alpha;
         }
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        if (first || most * vn > 8.f) {
-          const float to = q4_pow2(min(max(2 - q4_exponent(most), -120), 120));
-          if (!first) ratio = to / vn;
-          vn = to;
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int g = 0; g < GC; ++g) w[t][g] = e[t][g] * (q4_step(vsz[t]) * (vn * row_sign));
-        a[0] *= ratio;
-        a[1] *= ratio;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          o[t][0] *= a[0]; o[t][1] *= a[1];
-          o[t][2] *= a[0]; o[t][3] *= a[1];
-          if (have_main) {
-#pragma unroll
-            for (int r = 0; r < MV; ++r) my_main[(t * 32 + lane) * MV + r] *= a[r % GC];
-          }
-        }
-        dsum[0] *= a[0]; dsum[1] *= a[1];
       }
       // ---- row sums; the weights as fp16 pairs, turned into the B operand ----
       uint32_t pb[4], pl[4];
@@ -488,9 +495,8 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
           q4_mma(acc1, d0, d1, d2, d3, b0, b1);
           if constexpr (GC == 2) q4_mma(acc1, d0, d1, d2, d3, c0, c1);
         };
-        constexpr uint32_t ones = 0x3c003c00u;
-        q4_mma(dsum, ones, ones, ones, ones, b0, b1);
-        if constexpr (GC == 2) q4_mma(dsum, ones, ones, ones, ones, c0, c1);
+        q4_mma(dsum, one0, one1, one2, one3, b0, b1);
+        if constexpr (GC == 2) q4_mma(dsum, one0, one1, one2, one3, c0, c1);
         const uint32_t* v0 = sw + v_at + 2 * mt * VSW;
 #pragma unroll
         for (int u = 0; u < NGV / 2; ++u) {      // 64 channels: word 8 u + gid holds channels 64 u + 8 gid ..
@@ -540,15 +546,17 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         dsum[0] = dsum[1] = dsum[2] = dsum[3] = 0.f;
         have_main = true;
       }
-      // this warp is done with the stage (its loads have been used); the last one of the CTA refills it
+      // this warp is done with the stage (its loads have been used)
       __syncwarp();
-      if (lane == 0) {
-        __threadfence_block();
-        if (atomicAdd(&used[st], 1) == NW - 1) {
-          used[st] = 0;
-          __threadfence_block();
-          copy_ahead(i + NSTG, st);
+      if (lane == 0) mbar_arrive(bar0 + 8 * (Q4_MAX_STG + st));
+      if (turn-- == 0) {       // the warps take turns to refill
+        turn = NW - 1;
+        const int old = LAG == 0 ? st : st == 0 ? NSTG - 1 : st - 1;
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar0 + 8 * (Q4_MAX_STG + old), old > st ? parity ^ 1u : parity, p.wait_limit))) {
+          timed_out = true;
+          break;
         }
+        if (lane == 0) copy_ahead(i - LAG + NSTG, old);
       }
       if (++st == NSTG) { st = 0; parity ^= 1u; }
     }
@@ -589,7 +597,6 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
       __syncthreads();
       return;
     }
-    const float unscale = 1.f / vn;
 #pragma unroll
     for (int g = 0; g < GC; ++g) {
       const int head = GC * tq + g;
@@ -604,8 +611,8 @@ __global__ void __launch_bounds__(Q4_NW * 32, 2) attn_q4_kernel(const Q4ScanPara
         for (int t = 0; t < NT; ++t) {
           const bool wide = t < 4 * (NGV / 2);
           const int c = wide ? 64 * (t / 4) + 8 * gid + 2 * (t % 4) : 32 * (NGV - 1) + 4 * gid + 2 * (t % 2);
-          rr[c] = fmaf(o[t][g] * 0x1p14f, unscale, z_thr[g]) * f;
-          rr[c + 1] = fmaf(o[t][GC + g] * 0x1p20f, unscale, z_thr[g]) * f;
+          rr[c] = fmaf(o[t][g], 0x1p14f, z_thr[g]) * f;
+          rr[c + 1] = fmaf(o[t][GC + g], 0x1p20f, z_thr[g]) * f;
         }
       }
     }

@@ -163,7 +163,7 @@ struct rap_attn_args {
 rap_status rap_launch_attn(rap_ctx* ctx, const rap_attn_args& a, cudaStream_t st);
 rap_scan_params rap_fill_scan_params(rap_ctx* ctx, const rap_attn_args& a, int n_split_req);     // rap_attn_scan.cu
 // the 4-bit scan (rap_attn_q4_kernel.cuh) for words per K / V row and heads per lane, or nullptr (generated at build time)
-struct rap_q4_entry { int k_words, v_words, heads_per_lane, smem; const void* fn; };
+struct rap_q4_entry { int k_words, v_words, heads_per_lane, smem, threads; const void* fn; };
 const rap_q4_entry* rap_q4_find(int k_words, int v_words, int heads_per_lane);
 
 struct rap_proj_args {

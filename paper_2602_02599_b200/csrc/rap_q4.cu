@@ -20,66 +20,199 @@ __device__ __forceinline__ float warp_min_nan(float v) {
   return v;
 }
 
-// One warp per row, one lane per word of eight codes.
-template <typename T>
-__global__ void __launch_bounds__(256) quantize_rows_q4_kernel(const T* __restrict__ src, uint32_t* __restrict__ dst,
-                                                               long long n_rows, int W) {
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (row >= n_rows) return;
-  const T* x = src + row * W;
-  float v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = q4_ld(x + min(8 * lane + i, W - 1));      // past the end: the last element again
-  float hi = v[0], lo = v[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    hi = q4_max(hi, v[i]);
-    lo = q4_min(lo, v[i]);
+// ---- rows to 4 bits and back ----------------------------------------------------------------------------------------
+// Both directions are bound by the bytes they move (W e + row bytes per row each way).  A CTA takes R rows, whose bytes are
+// one contiguous range on either side: one bulk copy brings them into shared memory, four threads work on each row from
+// there (word k of a row belongs to thread k mod 4), one bulk copy takes the result out.  Row lengths of any parity are an
+// affair of the shared memory alone, and eight or more CTAs per SM keep enough bytes in flight.  The last rows' odd bytes
+// (a bulk copy moves multiples of 16) go by plain loads and stores.
+constexpr int Q4R_STAGE = 18 * 1024;     // target for a CTA's fp32 / bf16 rows; R is a multiple of 8, at most 64
+
+int q4_rows_per_cta(int W, int elem) {
+  int r = 64;
+  while (r > 8 && r * W * elem > Q4R_STAGE) r /= 2;
+  return r;
+}
+int q4_rows_smem(int W, int elem, int R) { return 16 + (R * W * elem + 31) / 16 * 16 + R * 4 * q4_row_words(W); }
+
+// bytes [0, n) of a 16-byte aligned global range into shared memory; every thread of the CTA calls it.  false: the wait ran out
+__device__ __forceinline__ bool q4_bring(unsigned char* dst, const unsigned char* src, int n, uint32_t bar, int32_t* status) {
+  const int bulk = n & ~15;
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_expect_tx(bar, bulk);
+    if (bulk) bulk_g2s(smem_u32(dst), src, bulk, bar);
   }
-  const Q4Row q = q4_decide(warp_max_nan(hi), warp_min_nan(lo));
-  uint32_t word = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (8 * lane + i < W) word |= q4_code(v[i], q) << (4 * i);
-  const int nw = q4_row_words(W);
-  uint32_t* d = dst + row * nw;
-  if (lane < nw - 1) d[lane] = word;
-  if (lane == 0) d[nw - 1] = q.sz;
+  for (int i = bulk + threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
+  __syncthreads();
+  if (mbar_wait_bounded(bar, 0)) return true;
+  if (threadIdx.x == 0) {
+    atomicCAS(&status[0], 0, (int)RAP_ETIMEOUT);
+    status[1] = (int)blockIdx.x;
+  }
+  return false;
+}
+// the way out: every thread has written its part of src (shared)
+__device__ __forceinline__ void q4_take(unsigned char* dst, const unsigned char* src, int n) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncthreads();
+  const int bulk = n & ~15;
+  if (threadIdx.x == 0 && bulk) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bulk) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+  for (int i = bulk + threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
+  if (threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // shared memory is free after this
 }
 
-template <typename T>
-__device__ __forceinline__ void dequantize_row(const uint32_t* __restrict__ src, T* __restrict__ dst, int W, int lane) {
+// eight numbers of a row in shared memory, from element `at` (a multiple of 8 past the row's start) on
+__device__ __forceinline__ void q4_eight(const float* base, int at, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = base[at + i];
+}
+__device__ __forceinline__ void q4_eight(const __nv_bfloat16* base, int at, float (&v)[8]) {
+  // rows of odd length start on half words: five words, shifted into place
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(base) + (at >> 1);
+  const uint32_t sh = (at & 1) * 16;
+  uint32_t x[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) x[i] = w[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t y = __funnelshift_r(x[i], x[i + 1], sh);
+    v[2 * i] = __uint_as_float(y << 16);
+    v[2 * i + 1] = __uint_as_float(y & 0xffff0000u);
+  }
+}
+
+// WPT: words of codes per thread, four threads a row
+template <typename T, int WPT>
+__global__ void __launch_bounds__(256) quantize_rows_q4_kernel(const T* __restrict__ src, uint32_t* __restrict__ dst,
+                                                               long long n_rows, int W, int R, int32_t* __restrict__ status) {
+  extern __shared__ __align__(128) unsigned char q4_rows_smem_buf[];
   const int nw = q4_row_words(W);
-  const uint32_t sz = src[nw - 1];
-  if (8 * lane >= W) return;
-  const uint32_t word = src[lane];
-  const float s = q4_step(sz), z = q4_middle(sz);
+  unsigned char* in = q4_rows_smem_buf + 16;
+  uint32_t* out = reinterpret_cast<uint32_t*>(in + (R * W * (int)sizeof(T) + 31) / 16 * 16);
+  const long long row0 = (long long)blockIdx.x * R;
+  const int rows = (int)min((long long)R, n_rows - row0);
+  if (!q4_bring(in, reinterpret_cast<const unsigned char*>(src + row0 * W), rows * W * (int)sizeof(T), smem_u32(q4_rows_smem_buf), status))
+    return;
+  const int row = threadIdx.x >> 2, q = threadIdx.x & 3;
+  // (threads past the last row work on the first one's numbers and store nothing: the shuffles below want whole warps)
+  const int at0 = (row < rows ? row : 0) * W;
+  const T* x = reinterpret_cast<const T*>(in);
+  float v[WPT][8];
+  float hi = q4_ld(x + at0), lo = hi;
+#pragma unroll
+  for (int k = 0; k < WPT; ++k) {
+    const int e0 = 8 * (q + 4 * k);
+    if (e0 + 8 <= W) {
+      q4_eight(x, at0 + e0, v[k]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        hi = q4_max(hi, v[k][i]);
+        lo = q4_min(lo, v[k][i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[k][i] = q4_ld(x + at0 + (e0 + i < W ? e0 + i : 0));      // past the end: a number of the row, masked below
+        if (e0 + i < W) {
+          hi = q4_max(hi, v[k][i]);
+          lo = q4_min(lo, v[k][i]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    hi = q4_max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    lo = q4_min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+  }
+  const Q4Row r = q4_decide(hi, lo);
+  if (row < rows) {
+#pragma unroll
+    for (int k = 0; k < WPT; ++k) {
+      const int w = q + 4 * k, left = W - 8 * w;       // codes this word holds, at most 8
+      if (w < nw - 1) {      // (nw - 1 <= 4 WPT: the padding word is among them)
+        uint32_t word = q4_word(v[k], r);
+        if (left < 8) word &= left > 0 ? (1u << (4 * left)) - 1u : 0u;
+        out[row * nw + w] = word;
+      }
+    }
+    if (q == 0) out[row * nw + nw - 1] = r.sz;
+  }
+  q4_take(reinterpret_cast<unsigned char*>(dst + row0 * nw), reinterpret_cast<const unsigned char*>(out), rows * nw * 4);
+}
+
+__device__ __forceinline__ void q4_put8(float* base, int at, const float (&v)[8], int n) {
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (8 * lane + i < W) q4_st(dst + 8 * lane + i, fmaf(s, (float)((word >> (4 * i)) & 15u) - 7.5f, z));
+    if (i < n) base[at + i] = v[i];
+}
+__device__ __forceinline__ void q4_put8(__nv_bfloat16* base, int at, const float (&v)[8], int n) {
+  if ((at & 1) == 0 && n >= 8) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(base + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 y = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) base[at + i] = __float2bfloat16_rn(v[i]);
+  }
+}
+// `rows` packed rows at src -> numbers at dst, by one CTA
+template <typename T>
+__device__ __forceinline__ void q4_rows_back(const uint32_t* src, T* dst, int rows, int W, int R, int32_t* status) {
+  extern __shared__ __align__(128) unsigned char q4_rows_smem_buf[];
+  const int nw = q4_row_words(W);
+  unsigned char* out = q4_rows_smem_buf + 16;
+  const uint32_t* in = reinterpret_cast<const uint32_t*>(out + (R * W * (int)sizeof(T) + 31) / 16 * 16);
+  if (!q4_bring(const_cast<unsigned char*>(reinterpret_cast<const unsigned char*>(in)), reinterpret_cast<const unsigned char*>(src),
+                rows * nw * 4, smem_u32(q4_rows_smem_buf), status))
+    return;
+  const int row = threadIdx.x >> 2, q = threadIdx.x & 3;
+  if (row < rows) {
+    const uint32_t sz = in[row * nw + nw - 1];
+    const float s = q4_step(sz), z = q4_middle(sz);
+    for (int e0 = 8 * q; e0 < W; e0 += 32) {
+      const uint32_t word = in[row * nw + (e0 >> 3)];
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // the code under the exponent of 2^22 (a last place of 1/2), less 2^22 + 7.5
+        const uint32_t bits = 0x4a800000u | ((i == 0 ? word << 1 : word >> (4 * i - 1)) & 0x1eu);
+        v[i] = fmaf(s, __uint_as_float(bits) - 4194311.5f, z);
+      }
+      q4_put8(reinterpret_cast<T*>(out), row * W + e0, v, W - e0);
+    }
+  }
+  q4_take(reinterpret_cast<unsigned char*>(dst), out, rows * W * (int)sizeof(T));
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256) dequantize_rows_q4_kernel(const uint32_t* __restrict__ src, T* __restrict__ dst,
-                                                                 long long n_rows, int W) {
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (row >= n_rows) return;
-  dequantize_row(src + row * q4_row_words(W), dst + row * W, W, threadIdx.x & 31);
+                                                                 long long n_rows, int W, int R, int32_t* __restrict__ status) {
+  const long long row0 = (long long)blockIdx.x * R;
+  q4_rows_back(src + row0 * q4_row_words(W), dst + row0 * W, (int)min((long long)R, n_rows - row0), W, R, status);
 }
 
-// A layer's K rows (blockIdx.z = 0) and V rows (1), up to every sequence's length: grid (rows of a unit / 8, units, 2)
+// A layer's K rows (blockIdx.z = 0) and V rows (1), up to every sequence's length: grid (rows of a unit / R, units, 2)
 template <typename T>
 __global__ void __launch_bounds__(256)
 read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict__ v4, T* __restrict__ k, T* __restrict__ v,
-                     const int32_t* __restrict__ seq_len, int Hkv, int S_cap, int P2, int dv) {
-  const int pos = blockIdx.x * 8 + (threadIdx.x >> 5);
+                     const int32_t* __restrict__ seq_len, int Hkv, int S_cap, int P2, int dv, int R, int32_t* __restrict__ status) {
+  const int pos = blockIdx.x * R;
   const int unit = blockIdx.y;
-  const int len = min(seq_len[unit / Hkv], S_cap);
-  if (pos >= len) return;
+  const int rows = min(min(seq_len[unit / Hkv], S_cap) - pos, R);
+  if (rows <= 0) return;
   const size_t row = (size_t)unit * S_cap + pos;
-  if (blockIdx.z == 0) dequantize_row(k4 + row * q4_row_words(P2), k + row * P2, P2, threadIdx.x & 31);
-  else dequantize_row(v4 + row * q4_row_words(dv), v + row * dv, dv, threadIdx.x & 31);
+  const int W = blockIdx.z ? dv : P2;
+  q4_rows_back((blockIdx.z ? v4 : k4) + row * q4_row_words(W), (blockIdx.z ? v : k) + row * W, rows, W, R, status);
 }
 
 // RoPE / append epilogue with quantisation.  One warp per (row t, item): items are the H_q query heads (rotated, rounded
@@ -320,25 +453,38 @@ __global__ void attn_q4_combine_kernel(const float* __restrict__ ws, int n_split
 
 }  // namespace
 
-rap_status rap_launch_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, long long n_rows, int W, const void* src, void* dst,
-                                       cudaStream_t st) {
-  const unsigned blocks = (unsigned)((n_rows + 7) / 8);
-  if (dtype_in == RAP_F32)
-    quantize_rows_q4_kernel<float><<<blocks, 256, 0, st>>>((const float*)src, (uint32_t*)dst, n_rows, W);
-  else
-    quantize_rows_q4_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>((const __nv_bfloat16*)src, (uint32_t*)dst, n_rows, W);
+template <typename T>
+static rap_status launch_quantize(rap_ctx* ctx, long long n_rows, int W, const void* src, void* dst, cudaStream_t st) {
+  const int R = q4_rows_per_cta(W, (int)sizeof(T)), smem = q4_rows_smem(W, (int)sizeof(T), R);
+  const unsigned blocks = (unsigned)((n_rows + R - 1) / R);
+  auto go = [&](auto kernel) { kernel<<<blocks, 4 * R, smem, st>>>((const T*)src, (uint32_t*)dst, n_rows, W, R, ctx->d_status); };
+  switch ((W + 31) / 32) {
+    case 1: go(quantize_rows_q4_kernel<T, 1>); break;
+    case 2: go(quantize_rows_q4_kernel<T, 2>); break;
+    case 3: go(quantize_rows_q4_kernel<T, 3>); break;
+    case 4: go(quantize_rows_q4_kernel<T, 4>); break;
+    default: go(quantize_rows_q4_kernel<T, 8>);
+  }
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
 }
 
+rap_status rap_launch_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, long long n_rows, int W, const void* src, void* dst,
+                                       cudaStream_t st) {
+  return dtype_in == RAP_F32 ? launch_quantize<float>(ctx, n_rows, W, src, dst, st)
+                             : launch_quantize<__nv_bfloat16>(ctx, n_rows, W, src, dst, st);
+}
+
 rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long long n_rows, int W, const void* src, void* dst,
                                          cudaStream_t st) {
-  const unsigned blocks = (unsigned)((n_rows + 7) / 8);
+  const int e = rap_elem_bytes(dtype_out), R = q4_rows_per_cta(W, e), smem = q4_rows_smem(W, e, R);
+  const unsigned blocks = (unsigned)((n_rows + R - 1) / R);
   if (dtype_out == RAP_F32)
-    dequantize_rows_q4_kernel<float><<<blocks, 256, 0, st>>>((const uint32_t*)src, (float*)dst, n_rows, W);
+    dequantize_rows_q4_kernel<float><<<blocks, 4 * R, smem, st>>>((const uint32_t*)src, (float*)dst, n_rows, W, R, ctx->d_status);
   else
-    dequantize_rows_q4_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>((const uint32_t*)src, (__nv_bfloat16*)dst, n_rows, W);
+    dequantize_rows_q4_kernel<__nv_bfloat16><<<blocks, 4 * R, smem, st>>>((const uint32_t*)src, (__nv_bfloat16*)dst, n_rows, W, R,
+                                                                          ctx->d_status);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
@@ -347,13 +493,14 @@ rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long l
 rap_status rap_launch_read_cache_q4(rap_ctx* ctx, int dtype, int B, int Hkv, int S_cap, int P2, int dv, const void* k4, const void* v4,
                                     const int32_t* seq_len, int len_max, void* k, void* v, cudaStream_t st) {
   if ((long long)B * Hkv > 65535) return RAP_ESHAPE;
-  const dim3 grid((len_max + 7) / 8, B * Hkv, 2);
+  const int W = P2 > dv ? P2 : dv, e = rap_elem_bytes(dtype), R = q4_rows_per_cta(W, e), smem = q4_rows_smem(W, e, R);
+  const dim3 grid((len_max + R - 1) / R, B * Hkv, 2);
   if (dtype == RAP_F32)
-    read_cache_q4_kernel<float><<<grid, 256, 0, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (float*)k, (float*)v, seq_len, Hkv,
-                                                      S_cap, P2, dv);
+    read_cache_q4_kernel<float><<<grid, 4 * R, smem, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (float*)k, (float*)v, seq_len, Hkv,
+                                                           S_cap, P2, dv, R, ctx->d_status);
   else
-    read_cache_q4_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (__nv_bfloat16*)k,
-                                                              (__nv_bfloat16*)v, seq_len, Hkv, S_cap, P2, dv);
+    read_cache_q4_kernel<__nv_bfloat16><<<grid, 4 * R, smem, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (__nv_bfloat16*)k,
+                                                                   (__nv_bfloat16*)v, seq_len, Hkv, S_cap, P2, dv, R, ctx->d_status);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
@@ -413,7 +560,7 @@ static rap_status launch_attn_q4_scan(rap_ctx* ctx, const rap_attn_args& a, cuda
   RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, e->fn, e->smem));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = p.s.balanced ? dim3(2 * ctx->sm_count) : dim3(p.s.n_split, a.Hkv, a.B);
-  cfg.blockDim = dim3(Q4_NW * 32);
+  cfg.blockDim = dim3(e->threads);
   cfg.dynamicSmemBytes = (size_t)e->smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
