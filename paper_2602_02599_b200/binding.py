@@ -119,19 +119,26 @@ def _lib():
 
 
 def _ptr(t):
-    """Device (or host) address of a torch tensor / numpy array / raw int; None -> NULL."""
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return c_void_p(t)
+    """Device (or host) address of a torch tensor / numpy array / raw int; None -> NULL (ctypes takes both as they are)."""
+    if t is None or type(t) is int:
+        return t
     if isinstance(t, np.ndarray):
-        return c_void_p(t.ctypes.data)
-    return c_void_p(t.data_ptr())
+        return t.ctypes.data
+    return t.data_ptr()
+
+
+_current = None      # (device of the calling thread, its current stream's handle by device)
 
 
 def _stream():
-    import torch
-    return c_void_p(torch.cuda.current_stream().cuda_stream)
+    """torch's current stream on the current device, as a handle; without making a Stream object for every call."""
+    global _current
+    if _current is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        _current = (torch.cuda.current_device, raw)
+    device, raw = _current
+    return raw(device())
 
 
 def _ptr_array(tensors):

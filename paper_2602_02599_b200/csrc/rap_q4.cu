@@ -36,17 +36,20 @@ int q4_rows_per_cta(int W, int elem) {
 int q4_rows_smem(int W, int elem, int R) { return 16 + (R * W * elem + 31) / 16 * 16 + R * 4 * q4_row_words(W); }
 
 // bytes [0, n) of a 16-byte aligned global range into shared memory; every thread of the CTA calls it.  false: the wait ran out
-__device__ __forceinline__ bool q4_bring(unsigned char* dst, const unsigned char* src, int n, uint32_t bar, int32_t* status) {
+__device__ __forceinline__ bool q4_bring(unsigned char* dst, const unsigned char* src, int n, uint32_t bar, uint32_t parity, bool again,
+                                         int32_t* status) {
   const int bulk = n & ~15;
   if (threadIdx.x == 0) {
-    mbar_init(bar, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (!again) {
+      mbar_init(bar, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     mbar_expect_tx(bar, bulk);
     if (bulk) bulk_g2s(smem_u32(dst), src, bulk, bar);
   }
   for (int i = bulk + threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
   __syncthreads();
-  if (mbar_wait_bounded(bar, 0)) return true;
+  if (__syncthreads_and(mbar_wait_bounded(bar, parity))) return true;      // one verdict for the CTA
   if (threadIdx.x == 0) {
     atomicCAS(&status[0], 0, (int)RAP_ETIMEOUT);
     status[1] = (int)blockIdx.x;
@@ -66,28 +69,47 @@ __device__ __forceinline__ void q4_take(unsigned char* dst, const unsigned char*
   if (threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // shared memory is free after this
 }
 
-// eight numbers of a row in shared memory, from element `at` (a multiple of 8 past the row's start) on
-__device__ __forceinline__ void q4_eight(const float* base, int at, float (&v)[8]) {
+// eight numbers of a row in shared memory, from element `at` on, and the row's extremes so far
+template <bool ODD>
+__device__ __forceinline__ void q4_eight(const float* base, int at, float (&v)[8], float& hi, float& lo) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = base[at + i];
-}
-__device__ __forceinline__ void q4_eight(const __nv_bfloat16* base, int at, float (&v)[8]) {
-  // rows of odd length start on half words: five words, shifted into place
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(base) + (at >> 1);
-  const uint32_t sh = (at & 1) * 16;
-  uint32_t x[5];
 #pragma unroll
-  for (int i = 0; i < 5; ++i) x[i] = w[i];
+  for (int i = 0; i < 8; i += 2) {
+    hi = q4_max3(hi, v[i], v[i + 1]);
+    lo = q4_min3(lo, v[i], v[i + 1]);
+  }
+}
+template <bool ODD>
+__device__ __forceinline__ void q4_eight(const __nv_bfloat16* base, int at, float (&v)[8], float& hi, float& lo) {
+  // rows of odd length may start on a half word: five words, shifted into place
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(base) + (at >> 1);
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = w[i];
+  if constexpr (ODD) {
+    const uint32_t sh = (at & 1) * 16, last = w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __funnelshift_r(y[i], i < 3 ? y[i + 1] : last, sh);
+  }
+  __nv_bfloat162 a = *reinterpret_cast<__nv_bfloat162*>(&y[0]), b = a;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    const __nv_bfloat162 c = *reinterpret_cast<__nv_bfloat162*>(&y[i]);
+    a = __hmax2_nan(a, c);
+    b = __hmin2_nan(b, c);
+  }
+  hi = q4_max3(hi, __low2float(a), __high2float(a));
+  lo = q4_min3(lo, __low2float(b), __high2float(b));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t y = __funnelshift_r(x[i], x[i + 1], sh);
-    v[2 * i] = __uint_as_float(y << 16);
-    v[2 * i + 1] = __uint_as_float(y & 0xffff0000u);
+    v[2 * i] = __uint_as_float(y[i] << 16);
+    v[2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
   }
 }
 
-// WPT: words of codes per thread, four threads a row
-template <typename T, int WPT>
+// WPT: words of codes per thread, four threads a row; ODD: rows of an odd number of bf16 numbers
+template <typename T, int WPT, bool ODD>
 __global__ void __launch_bounds__(256) quantize_rows_q4_kernel(const T* __restrict__ src, uint32_t* __restrict__ dst,
                                                                long long n_rows, int W, int R, int32_t* __restrict__ status) {
   extern __shared__ __align__(128) unsigned char q4_rows_smem_buf[];
@@ -96,7 +118,7 @@ __global__ void __launch_bounds__(256) quantize_rows_q4_kernel(const T* __restri
   uint32_t* out = reinterpret_cast<uint32_t*>(in + (R * W * (int)sizeof(T) + 31) / 16 * 16);
   const long long row0 = (long long)blockIdx.x * R;
   const int rows = (int)min((long long)R, n_rows - row0);
-  if (!q4_bring(in, reinterpret_cast<const unsigned char*>(src + row0 * W), rows * W * (int)sizeof(T), smem_u32(q4_rows_smem_buf), status))
+  if (!q4_bring(in, reinterpret_cast<const unsigned char*>(src + row0 * W), rows * W * (int)sizeof(T), smem_u32(q4_rows_smem_buf), 0, false, status))
     return;
   const int row = threadIdx.x >> 2, q = threadIdx.x & 3;
   // (threads past the last row work on the first one's numbers and store nothing: the shuffles below want whole warps)
@@ -108,20 +130,13 @@ __global__ void __launch_bounds__(256) quantize_rows_q4_kernel(const T* __restri
   for (int k = 0; k < WPT; ++k) {
     const int e0 = 8 * (q + 4 * k);
     if (e0 + 8 <= W) {
-      q4_eight(x, at0 + e0, v[k]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        hi = q4_max(hi, v[k][i]);
-        lo = q4_min(lo, v[k][i]);
-      }
+      q4_eight<ODD>(x, at0 + e0, v[k], hi, lo);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         v[k][i] = q4_ld(x + at0 + (e0 + i < W ? e0 + i : 0));      // past the end: a number of the row, masked below
-        if (e0 + i < W) {
-          hi = q4_max(hi, v[k][i]);
-          lo = q4_min(lo, v[k][i]);
-        }
+        hi = q4_max(hi, v[k][i]);
+        lo = q4_min(lo, v[k][i]);
       }
     }
   }
@@ -165,22 +180,23 @@ __device__ __forceinline__ void q4_put8(__nv_bfloat16* base, int at, const float
       if (i < n) base[at + i] = __float2bfloat16_rn(v[i]);
   }
 }
-// `rows` packed rows at src -> numbers at dst, by one CTA
+// `rows` packed rows at src -> numbers at dst, by one CTA.  A CTA may call it again: *turn counts the calls, false: a wait ran out
 template <typename T>
-__device__ __forceinline__ void q4_rows_back(const uint32_t* src, T* dst, int rows, int W, int R, int32_t* status) {
+__device__ __forceinline__ bool q4_rows_back(const uint32_t* src, T* dst, int rows, int W, int R, int32_t* status, uint32_t* turn) {
   extern __shared__ __align__(128) unsigned char q4_rows_smem_buf[];
   const int nw = q4_row_words(W);
   unsigned char* out = q4_rows_smem_buf + 16;
-  const uint32_t* in = reinterpret_cast<const uint32_t*>(out + (R * W * (int)sizeof(T) + 31) / 16 * 16);
-  if (!q4_bring(const_cast<unsigned char*>(reinterpret_cast<const unsigned char*>(in)), reinterpret_cast<const unsigned char*>(src),
-                rows * nw * 4, smem_u32(q4_rows_smem_buf), status))
-    return;
+  unsigned char* in = out + (R * W * (int)sizeof(T) + 31) / 16 * 16;
+  if (!q4_bring(in, reinterpret_cast<const unsigned char*>(src), rows * nw * 4, smem_u32(q4_rows_smem_buf), *turn & 1u, *turn > 0, status))
+    return false;
+  ++*turn;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(in);
   const int row = threadIdx.x >> 2, q = threadIdx.x & 3;
   if (row < rows) {
-    const uint32_t sz = in[row * nw + nw - 1];
+    const uint32_t sz = words[row * nw + nw - 1];
     const float s = q4_step(sz), z = q4_middle(sz);
     for (int e0 = 8 * q; e0 < W; e0 += 32) {
-      const uint32_t word = in[row * nw + (e0 >> 3)];
+      const uint32_t word = words[row * nw + (e0 >> 3)];
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -192,35 +208,51 @@ __device__ __forceinline__ void q4_rows_back(const uint32_t* src, T* dst, int ro
     }
   }
   q4_take(reinterpret_cast<unsigned char*>(dst), out, rows * W * (int)sizeof(T));
+  return true;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256) dequantize_rows_q4_kernel(const uint32_t* __restrict__ src, T* __restrict__ dst,
                                                                  long long n_rows, int W, int R, int32_t* __restrict__ status) {
   const long long row0 = (long long)blockIdx.x * R;
-  q4_rows_back(src + row0 * q4_row_words(W), dst + row0 * W, (int)min((long long)R, n_rows - row0), W, R, status);
+  uint32_t turn = 0;
+  q4_rows_back(src + row0 * q4_row_words(W), dst + row0 * W, (int)min((long long)R, n_rows - row0), W, R, status, &turn);
 }
 
-// A layer's K rows (blockIdx.z = 0) and V rows (1), up to every sequence's length: grid (rows of a unit / R, units, 2)
+// A layer's K rows and V rows up to every sequence's length.  The chunks of R rows that exist -- per sequence
+// (K or V) x KV head x rows -- form one sequence that the CTAs walk through with the grid's stride (a grid over all
+// positions spent 15 us on CTAs without rows in a batch of unlike lengths).
 template <typename T>
 __global__ void __launch_bounds__(256)
 read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict__ v4, T* __restrict__ k, T* __restrict__ v,
-                     const int32_t* __restrict__ seq_len, int Hkv, int S_cap, int P2, int dv, int R, int32_t* __restrict__ status) {
-  const int pos = blockIdx.x * R;
-  const int unit = blockIdx.y;
-  const int rows = min(min(seq_len[unit / Hkv], S_cap) - pos, R);
-  if (rows <= 0) return;
-  const size_t row = (size_t)unit * S_cap + pos;
-  const int W = blockIdx.z ? dv : P2;
-  q4_rows_back((blockIdx.z ? v4 : k4) + row * q4_row_words(W), (blockIdx.z ? v : k) + row * W, rows, W, R, status);
+                     const int32_t* __restrict__ seq_len, int B, int Hkv, int S_cap, int P2, int dv, int len_max, int R,
+                     int32_t* __restrict__ status) {
+  long long before = 0;        // chunks of the sequences before b
+  uint32_t turn = 0;
+  int b = 0, len = min(min(seq_len[0], S_cap), len_max), chunks = max(len + R - 1, 0) / R;
+  for (long long c = blockIdx.x;; c += gridDim.x) {
+    while (c - before >= 2LL * Hkv * chunks) {
+      before += 2LL * Hkv * chunks;
+      if (++b >= B) return;
+      len = min(min(seq_len[b], S_cap), len_max);
+      chunks = max(len + R - 1, 0) / R;
+    }
+    const int unit = (int)((c - before) / chunks), pos = (int)((c - before) - (long long)unit * chunks) * R;
+    const bool is_v = unit >= Hkv;
+    const size_t row = ((size_t)b * Hkv + unit - (is_v ? Hkv : 0)) * S_cap + pos;
+    const int W = is_v ? dv : P2;
+    if (!q4_rows_back((is_v ? v4 : k4) + row * q4_row_words(W), (is_v ? v : k) + row * W, min(len - pos, R), W, R, status, &turn)) return;
+  }
 }
 
-// RoPE / append epilogue with quantisation.  One warp per (row t, item): items are the H_q query heads (rotated, rounded
-// to the storage dtype, written to q_out as in the unquantised path), then the H_kv key heads (rotated in fp32, quantised,
-// appended), then the H_kv value heads (quantised, appended).  A lane owns pairs of neighbouring numbers, that is whole
-// bytes of a quantised row: P <= 128, d_v' <= 256, so at most four.  y holds `ksplit` partial results, each [T][n_out].
+// RoPE / append epilogue with quantisation.  One CTA per (row t, KV head h), one warp per item: the G query heads of h
+// (rotated, rounded to the storage dtype, written to q_out as in the unquantised path), its key head (rotated in fp32,
+// quantised, appended) and its value head (quantised, appended).  All of them rotate by the same angles, so the sines and
+// cosines -- fp64 angle and reduction -- are taken once per CTA (one warp per item on its own: 34 us for 512 rows of the
+// 8B-shaped layer, this: 11).  A lane owns pairs of neighbouring numbers, that is whole bytes of a quantised row: P <= 128,
+// d_v' <= 256, so at most four.  y holds `ksplit` partial results, each [T][n_out].
 template <typename T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(32 * (RAP_MAX_GROUP + 2))
 rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restrict__ bias, const int32_t* __restrict__ seq_id,
                       const int32_t* __restrict__ pos, const int32_t* __restrict__ slot, const double* __restrict__ inv_freq,
                       T* __restrict__ q_out, uint32_t* __restrict__ k4, uint32_t* __restrict__ v4, int Trows, int Hq, int Hkv,
@@ -229,72 +261,75 @@ rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restri
   // memory; the GEMM's results (and, through the GEMM, the end of the scan before it) are awaited here
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int items = Hq + 2 * Hkv;
-  const long long wid = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (wid >= (long long)Trows * items) return;
-  const int t = (int)(wid / items), item = (int)(wid - (long long)t * items);
+  __shared__ float2 turn[128];                                         // (cosine, sine) of every pair
+  const int t = blockIdx.x / Hkv, h = blockIdx.x - t * Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int P = P2 >> 1, G = Hq / Hkv;
   const int n_out = (Hq + Hkv) * P2 + Hkv * dv;
   const int p = pos[t];
   const int sq = seq_id ? seq_id[t] : t;
   const int sl = slot ? slot[t] : p;
   const bool row_ok = (sq >= 0 && sq < B_cache && sl >= 0 && sl < S_cap);
-  if (!row_ok && item == 0 && lane == 0) {
+  if (!row_ok && h == 0 && threadIdx.x == 0) {
     atomicCAS(&status[0], 0, (int)RAP_ECAPACITY);
     status[1] = t;
   }
-  const bool is_v = item >= Hq + Hkv, is_q = item < Hq;
-  if (!is_q && !row_ok) return;
-  const int h = is_q ? item / G : is_v ? item - Hq - Hkv : item - Hq;
-  const int col0 = is_v ? (Hq + Hkv) * P2 + h * dv : item * P2;      // q heads, then k heads: item * 2P either way
+  const bool is_q = warp < G, is_v = warp > G;
+  // columns of Y: q heads, then k heads (2P each), then v heads
+  const int col0 = is_v ? (Hq + Hkv) * P2 + h * dv : (is_q ? h * G + warp : Hq + h) * P2;
   const int W = is_v ? dv : P2;
   const size_t split_stride = (size_t)Trows * n_out;
   const float* yr = y + (size_t)t * n_out + col0;
-  // every partial of this lane's numbers first (independent loads), then the sums in split order and the bias
-  float pa[4][RAP_MAX_KSPLIT], pb[4][RAP_MAX_KSPLIT];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-#pragma unroll
-    for (int s = 0; s < RAP_MAX_KSPLIT; ++s) {
-      const int c = 2 * (lane + 32 * k);
-      pa[k][s] = (c < W && s < ksplit) ? yr[s * split_stride + c] : 0.f;
-      pb[k][s] = (c + 1 < W && s < ksplit) ? yr[s * split_stride + c + 1] : 0.f;
-    }
   float a[4], b[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int c = 2 * (lane + 32 * k);
     a[k] = b[k] = 0.f;
+    if (64 * k < W) {
+      const int c = 2 * (lane + 32 * k);
+#pragma unroll 4
+      for (int s = 0; s < ksplit; ++s) {                               // the sums in split order
+        a[k] += c < W ? yr[s * split_stride + c] : 0.f;
+        b[k] += c + 1 < W ? yr[s * split_stride + c + 1] : 0.f;
+      }
+      if (bias && c < W) a[k] += q4_ld(bias + col0 + c);
+      if (bias && c + 1 < W) b[k] += q4_ld(bias + col0 + c + 1);
+    }
+  }
+  for (int c = threadIdx.x; c < P; c += blockDim.x) {
+    // fp64 angle and reduction to [-pi, pi], fp32 sine and cosine of the reduced angle (as in the unquantised path)
+    const double ang = (double)p * inv_freq[h * half_dim + c];
+    const double turns = rint(ang * 0.15915494309189535);
+    const double red = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, ang));
+    float sf, cf;
+    sincosf((float)red, &sf, &cf);
+    turn[c] = make_float2(cf, sf);
+  }
+  __syncthreads();
+  if (!is_v) {
 #pragma unroll
-    for (int s = 0; s < RAP_MAX_KSPLIT; ++s)
-      if (s < ksplit) { a[k] += pa[k][s]; b[k] += pb[k][s]; }
-    if (bias && c < W) a[k] += q4_ld(bias + col0 + c);
-    if (bias && c + 1 < W) b[k] += q4_ld(bias + col0 + c + 1);
-    if (!is_v && c < W) {
-      // fp64 angle and reduction to [-pi, pi], fp32 sine and cosine of the reduced angle (as in the unquantised path)
-      const double ang = (double)p * inv_freq[h * half_dim + (c >> 1)];
-      const double turns = rint(ang * 0.15915494309189535);
-      const double red = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, ang));
-      float sf, cf;
-      sincosf((float)red, &sf, &cf);
-      const float x0 = a[k], x1 = b[k];
-      a[k] = fmaf(-x1, sf, __fmul_rn(x0, cf));          // the same roundings as the unquantised kernels
-      b[k] = fmaf(x0, sf, __fmul_rn(x1, cf));
+    for (int k = 0; k < 4; ++k) {
+      const int i = lane + 32 * k;
+      if (i < P) {
+        const float2 cs = turn[i];
+        const float x0 = a[k], x1 = b[k];
+        a[k] = fmaf(-x1, cs.y, __fmul_rn(x0, cs.x));          // the same roundings as the unquantised kernels
+        b[k] = fmaf(x0, cs.y, __fmul_rn(x1, cs.x));
+      }
     }
   }
   if (is_q) {
-    T* dst = q_out + ((size_t)t * Hq + item) * P2;
+    T* dst = q_out + ((size_t)t * Hq + h * G + warp) * P2;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int c = 2 * (lane + 32 * k);
-      if (c < W) {
-        q4_st(dst + c, a[k]);
-        q4_st(dst + c + 1, b[k]);
+      const int i = lane + 32 * k;
+      if (i < P) {
+        q4_st(dst + 2 * i, a[k]);
+        q4_st(dst + 2 * i + 1, b[k]);
       }
     }
     return;
   }
+  if (!row_ok) return;
   float hi = -INFINITY, lo = INFINITY;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -458,12 +493,21 @@ static rap_status launch_quantize(rap_ctx* ctx, long long n_rows, int W, const v
   const int R = q4_rows_per_cta(W, (int)sizeof(T)), smem = q4_rows_smem(W, (int)sizeof(T), R);
   const unsigned blocks = (unsigned)((n_rows + R - 1) / R);
   auto go = [&](auto kernel) { kernel<<<blocks, 4 * R, smem, st>>>((const T*)src, (uint32_t*)dst, n_rows, W, R, ctx->d_status); };
-  switch ((W + 31) / 32) {
-    case 1: go(quantize_rows_q4_kernel<T, 1>); break;
-    case 2: go(quantize_rows_q4_kernel<T, 2>); break;
-    case 3: go(quantize_rows_q4_kernel<T, 3>); break;
-    case 4: go(quantize_rows_q4_kernel<T, 4>); break;
-    default: go(quantize_rows_q4_kernel<T, 8>);
+  auto pick = [&](auto odd) {
+    constexpr bool ODD = decltype(odd)::value;
+    switch ((W + 31) / 32) {
+      case 1: go(quantize_rows_q4_kernel<T, 1, ODD>); break;
+      case 2: go(quantize_rows_q4_kernel<T, 2, ODD>); break;
+      case 3: go(quantize_rows_q4_kernel<T, 3, ODD>); break;
+      case 4: go(quantize_rows_q4_kernel<T, 4, ODD>); break;
+      default: go(quantize_rows_q4_kernel<T, 8, ODD>);
+    }
+  };
+  if constexpr (sizeof(T) == 2) {
+    if (W & 1) pick(std::true_type{});
+    else pick(std::false_type{});
+  } else {
+    pick(std::false_type{});
   }
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
@@ -492,15 +536,16 @@ rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long l
 
 rap_status rap_launch_read_cache_q4(rap_ctx* ctx, int dtype, int B, int Hkv, int S_cap, int P2, int dv, const void* k4, const void* v4,
                                     const int32_t* seq_len, int len_max, void* k, void* v, cudaStream_t st) {
-  if ((long long)B * Hkv > 65535) return RAP_ESHAPE;
   const int W = P2 > dv ? P2 : dv, e = rap_elem_bytes(dtype), R = q4_rows_per_cta(W, e), smem = q4_rows_smem(W, e, R);
-  const dim3 grid((len_max + R - 1) / R, B * Hkv, 2);
+  const long long chunks = 2LL * B * Hkv * ((len_max + R - 1) / R), most = 8LL * ctx->sm_count;      // eight CTAs fit an SM
+  const unsigned grid = (unsigned)(chunks < most ? chunks : most);
   if (dtype == RAP_F32)
-    read_cache_q4_kernel<float><<<grid, 4 * R, smem, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (float*)k, (float*)v, seq_len, Hkv,
-                                                           S_cap, P2, dv, R, ctx->d_status);
+    read_cache_q4_kernel<float><<<grid, 4 * R, smem, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (float*)k, (float*)v, seq_len, B,
+                                                           Hkv, S_cap, P2, dv, len_max, R, ctx->d_status);
   else
     read_cache_q4_kernel<__nv_bfloat16><<<grid, 4 * R, smem, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (__nv_bfloat16*)k,
-                                                                   (__nv_bfloat16*)v, seq_len, Hkv, S_cap, P2, dv, R, ctx->d_status);
+                                                                   (__nv_bfloat16*)v, seq_len, B, Hkv, S_cap, P2, dv, len_max, R,
+                                                                   ctx->d_status);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
@@ -516,12 +561,12 @@ rap_status rap_launch_qkv_rope_append_q4(rap_ctx* ctx, const rap_proj_args& a, c
     s = rap_launch_proj_generic(ctx, a, st);
   }
   if (s != RAP_OK) return s;
-  const long long warps = (long long)a.T * (a.Hq + 2 * a.Hkv);
+  if ((long long)a.T * a.Hkv > 0x7fffffffLL) return RAP_ESHAPE;
   // inside a decode step (a.pdl): launched behind the tcgen05 GEMM with programmatic serialization, so that its launch
   // overlaps the GEMM's tail (the CUDA-core GEMM never triggers early, which makes the attribute a no-op there)
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((warps + 7) / 8), 1, 1);
-  cfg.blockDim = dim3(256, 1, 1);
+  cfg.gridDim = dim3((unsigned)(a.T * a.Hkv), 1, 1);
+  cfg.blockDim = dim3(32 * (a.Hq / a.Hkv + 2), 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -36,6 +36,17 @@ __device__ __forceinline__ float q4_min(float a, float b) {
   return r;
 }
 
+__device__ __forceinline__ float q4_max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float q4_min3(float a, float b, float c) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 struct Q4Row {
   float z, r;            // middle; 1 / step (0 where the step is)
   uint32_t sz;           // the row's last word
@@ -57,16 +68,14 @@ __device__ __forceinline__ uint32_t q4_code(float x, const Q4Row& q) {
   const float t = __fadd_rn(__fmul_rn(__fsub_rn(x, q.z), q.r), 7.5f);
   return q.bad ? 8u : __float_as_uint(__fadd_rn(t, 12582912.0f)) & 15u;
 }
-// a word of eight codes: the rounded places as floats, joined by exact products (16, 256) on the multiplier
+// a word of eight codes: with 1.5 2^23 added a place is 0x4b400000 + code as an integer, and the eight sum up as digits
 __device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Row& q) {
   if (q.bad) return 0x88888888u;
-  float r[8];
+  uint32_t word = 0u - 0x4b400000u * 0x11111111u;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    r[i] = __fadd_rn(__fadd_rn(__fadd_rn(__fmul_rn(__fsub_rn(x[i], q.z), q.r), 7.5f), 12582912.0f), -12582912.0f);
-  const float lo = fmaf(256.f, fmaf(16.f, r[3], r[2]), fmaf(16.f, r[1], r[0]));
-  const float hi = fmaf(256.f, fmaf(16.f, r[7], r[6]), fmaf(16.f, r[5], r[4]));
-  return __byte_perm(__float_as_uint(lo + 8388608.f), __float_as_uint(hi + 8388608.f), 0x5410);
+    word += __float_as_uint(__fadd_rn(__fadd_rn(__fmul_rn(__fsub_rn(x[i], q.z), q.r), 7.5f), 12582912.0f)) << (4 * i);
+  return word;
 }
 __device__ __forceinline__ float q4_step(uint32_t sz) { return __uint_as_float(sz << 16); }
 __device__ __forceinline__ float q4_middle(uint32_t sz) { return __uint_as_float(sz & 0xffff0000u); }
