@@ -21,76 +21,147 @@ __device__ __forceinline__ float warp_min_nan(float v) {
 }
 
 // ---- rows to 4 bits and back ----------------------------------------------------------------------------------------
-// Both directions are bound by the bytes they move (W e + row bytes per row each way).  A CTA takes R rows, whose bytes are
-// one contiguous range on either side: one bulk copy brings them into shared memory, four threads work on each row from
-// there (word k of a row belongs to thread k mod 4), one bulk copy takes the result out.  Row lengths of any parity are an
-// affair of the shared memory alone, and eight or more CTAs per SM keep enough bytes in flight.  The last rows' odd bytes
-// (a bulk copy moves multiples of 16) go by plain loads and stores.
-constexpr int Q4R_STAGE = 18 * 1024;     // target for a CTA's fp32 / bf16 rows; R is a multiple of 8, at most 64
+// Both directions are bound by the bytes they move (W e + row bytes per row each way).  R rows are one contiguous range on
+// either side: a bulk copy brings them into shared memory, four threads work on each row from there (word k of a row belongs
+// to thread k mod 4), a bulk copy takes the result out.  Row lengths of any parity are an affair of the shared memory alone.
+// The CTAs walk over the chunks with the grid's stride, the next chunk's copy in flight under the current one's arithmetic
+// and the last one's way out under both.  Odd bytes at the end (a bulk copy moves multiples of 16) go by plain loads and
+// stores, so nothing behind the last row is touched.
+constexpr int Q4R_STAGE = 18 * 1024;     // most bytes of a chunk's fp32 / bf16 rows; R is a multiple of 8, at most 64
 
 int q4_rows_per_cta(int W, int elem) {
   int r = 64;
   while (r > 8 && r * W * elem > Q4R_STAGE) r /= 2;
   return r;
 }
-int q4_rows_smem(int W, int elem, int R) { return 16 + (R * W * elem + 31) / 16 * 16 + R * 4 * q4_row_words(W); }
+struct Q4Chunk {
+  const unsigned char* src;
+  unsigned char* dst;
+  int in_bytes, out_bytes, rows, W;
+};
+// bytes of an input / output buffer that holds n (the loads of a row's last word may reach 32 past it)
+__host__ __device__ constexpr int q4_buffer(int n) { return (n + 47) / 16 * 16; }
+constexpr int Q4R_HEAD = 128;            // the two barriers
+constexpr int Q4R_THREADS = 128;         // 32 rows at a time
 
-// bytes [0, n) of a 16-byte aligned global range into shared memory; every thread of the CTA calls it.  false: the wait ran out
-__device__ __forceinline__ bool q4_bring(unsigned char* dst, const unsigned char* src, int n, uint32_t bar, uint32_t parity, bool again,
-                                         int32_t* status) {
-  const int bulk = n & ~15;
+// `total` chunks over the grid: chunk(c) says where chunk c lies, body(chunk, in, out) works from one buffer into the other
+template <typename Chunk, typename Body>
+__device__ __forceinline__ void q4_rows_pipeline(unsigned char* smem, int in_cap, int out_cap, long long total, int32_t* status,
+                                                 Chunk chunk, Body body) {
+  long long c = blockIdx.x;
+  if (c >= total) return;
+  const uint32_t bars = smem_u32(smem);
+  unsigned char* const in0 = smem + Q4R_HEAD;
+  unsigned char* const out0 = in0 + 2 * in_cap;
   if (threadIdx.x == 0) {
-    if (!again) {
-      mbar_init(bar, 1);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_init(bars, 1);
+    mbar_init(bars + 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  auto bring = [&](const Q4Chunk& k, int buf) {
+    const int bulk = k.in_bytes & ~15;
+    unsigned char* to = in0 + buf * in_cap;
+    if (threadIdx.x == 0) {
+      mbar_expect_tx(bars + 8 * buf, bulk);
+      if (bulk) bulk_g2s(smem_u32(to), k.src, bulk, bars + 8 * buf);
     }
-    mbar_expect_tx(bar, bulk);
-    if (bulk) bulk_g2s(smem_u32(dst), src, bulk, bar);
+    for (int i = bulk + threadIdx.x; i < k.in_bytes; i += blockDim.x) to[i] = k.src[i];
+  };
+  Q4Chunk now = chunk(c);
+  bring(now, 0);
+  int buf = 0;
+  uint32_t parity = 0;
+  for (;;) {
+    const bool more = c + gridDim.x < total;
+    Q4Chunk next = now;
+    if (more) {
+      next = chunk(c + gridDim.x);
+      bring(next, buf ^ 1);            // (everyone left that buffer before the last barrier below)
+    }
+    // the copy has landed, and the store that read this output buffer two chunks ago is done with it
+    const bool here = mbar_wait_bounded(bars + 8 * buf, parity);
+    if (threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    if (!__syncthreads_and(here)) {    // one verdict for the CTA
+      if (threadIdx.x == 0) {
+        atomicCAS(&status[0], 0, (int)RAP_ETIMEOUT);
+        status[1] = (int)blockIdx.x;
+        if (more) mbar_wait_bounded(bars + 8 * (buf ^ 1), buf ? parity ^ 1u : parity);      // a copy in flight may still land
+      }
+      break;
+    }
+    unsigned char* out = out0 + buf * out_cap;
+    body(now, in0 + buf * in_cap, out);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    const int bulk = now.out_bytes & ~15;
+    if (threadIdx.x == 0) {
+      if (bulk)
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(now.dst), "r"(smem_u32(out)), "r"(bulk) : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    for (int i = bulk + threadIdx.x; i < now.out_bytes; i += blockDim.x) now.dst[i] = out[i];
+    if (!more) break;
+    c += gridDim.x;
+    now = next;
+    parity ^= (uint32_t)buf;           // both buffers have been used once more
+    buf ^= 1;
   }
-  for (int i = bulk + threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
-  __syncthreads();
-  if (__syncthreads_and(mbar_wait_bounded(bar, parity))) return true;      // one verdict for the CTA
-  if (threadIdx.x == 0) {
-    atomicCAS(&status[0], 0, (int)RAP_ETIMEOUT);
-    status[1] = (int)blockIdx.x;
-  }
-  return false;
-}
-// the way out: every thread has written its part of src (shared)
-__device__ __forceinline__ void q4_take(unsigned char* dst, const unsigned char* src, int n) {
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  __syncthreads();
-  const int bulk = n & ~15;
-  if (threadIdx.x == 0 && bulk) {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bulk) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-  }
-  for (int i = bulk + threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
-  if (threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // shared memory is free after this
+  if (threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");     // shared memory may go
 }
 
-// eight numbers of a row in shared memory, from element `at` on, and the row's extremes so far
-template <bool ODD>
-__device__ __forceinline__ void q4_eight(const float* base, int at, float (&v)[8], float& hi, float& lo) {
+// How rows lie in shared memory: on words, on half words (bf16 rows of odd length), or on 16 bytes (lengths that are multiples
+// of 8; those of 64 and 128, where all rows start on one bank, are eight times as slow word by word)
+enum Q4Rows { Q4_WORDS, Q4_HALVES, Q4_VECTORS };
+
+// eight numbers of a row in shared memory, from element `at` on, of which the first n count (the others become the first one),
+// and the row's extremes so far
+template <Q4Rows HOW, bool PART>
+__device__ __forceinline__ void q4_eight(const float* base, int at, int n, float (&v)[8], float& hi, float& lo) {
+  if constexpr (HOW == Q4_VECTORS) {
+    const float4 a = *reinterpret_cast<const float4*>(base + at), b = *reinterpret_cast<const float4*>(base + at + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = base[at + i];
+    for (int i = 0; i < 8; ++i) v[i] = base[at + i];
+  }
+  if constexpr (PART && HOW != Q4_VECTORS) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v[i] = i < n ? v[i] : v[0];
+  }
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     hi = q4_max3(hi, v[i], v[i + 1]);
     lo = q4_min3(lo, v[i], v[i + 1]);
   }
 }
-template <bool ODD>
-__device__ __forceinline__ void q4_eight(const __nv_bfloat16* base, int at, float (&v)[8], float& hi, float& lo) {
+template <Q4Rows HOW, bool PART>
+__device__ __forceinline__ void q4_eight(const __nv_bfloat16* base, int at, int n, float (&v)[8], float& hi, float& lo) {
   // rows of odd length may start on a half word: five words, shifted into place
+  constexpr bool ODD = HOW == Q4_HALVES;
   const uint32_t* w = reinterpret_cast<const uint32_t*>(base) + (at >> 1);
   uint32_t y[4];
+  if constexpr (HOW == Q4_VECTORS) {
+    const uint4 a = *reinterpret_cast<const uint4*>(w);
+    y[0] = a.x; y[1] = a.y; y[2] = a.z; y[3] = a.w;
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = w[i];
+    for (int i = 0; i < 4; ++i) y[i] = w[i];
+  }
   if constexpr (ODD) {
     const uint32_t sh = (at & 1) * 16, last = w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = __funnelshift_r(y[i], i < 3 ? y[i + 1] : last, sh);
+  }
+  if constexpr (PART && HOW != Q4_VECTORS) {
+    const uint32_t twice = __byte_perm(y[0], 0, 0x1010);
+    if constexpr (ODD) y[0] = n > 1 ? y[0] : twice;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      if constexpr (ODD) y[i] = 2 * i + 1 < n ? y[i] : 2 * i < n ? __byte_perm(y[i], y[0], 0x5410) : twice;
+      else y[i] = 2 * i < n ? y[i] : twice;
+    }
   }
   __nv_bfloat162 a = *reinterpret_cast<__nv_bfloat162*>(&y[0]), b = a;
 #pragma unroll
@@ -108,141 +179,169 @@ __device__ __forceinline__ void q4_eight(const __nv_bfloat16* base, int at, floa
   }
 }
 
-// WPT: words of codes per thread, four threads a row; ODD: rows of an odd number of bf16 numbers
-template <typename T, int WPT, bool ODD>
-__global__ void __launch_bounds__(256) quantize_rows_q4_kernel(const T* __restrict__ src, uint32_t* __restrict__ dst,
-                                                               long long n_rows, int W, int R, int32_t* __restrict__ status) {
-  extern __shared__ __align__(128) unsigned char q4_rows_smem_buf[];
-  const int nw = q4_row_words(W);
-  unsigned char* in = q4_rows_smem_buf + 16;
-  uint32_t* out = reinterpret_cast<uint32_t*>(in + (R * W * (int)sizeof(T) + 31) / 16 * 16);
-  const long long row0 = (long long)blockIdx.x * R;
-  const int rows = (int)min((long long)R, n_rows - row0);
-  if (!q4_bring(in, reinterpret_cast<const unsigned char*>(src + row0 * W), rows * W * (int)sizeof(T), smem_u32(q4_rows_smem_buf), 0, false, status))
-    return;
-  const int row = threadIdx.x >> 2, q = threadIdx.x & 3;
-  // (threads past the last row work on the first one's numbers and store nothing: the shuffles below want whole warps)
-  const int at0 = (row < rows ? row : 0) * W;
-  const T* x = reinterpret_cast<const T*>(in);
-  float v[WPT][8];
-  float hi = q4_ld(x + at0), lo = hi;
+// WPT = ceil(W / 32): words of codes per thread, four threads a row, so only a thread's last word can be short (or past the
+// end: it then works on the row's first numbers again and stores nothing).
+// What bounds the conversion is instruction issue next to the bytes: 513 instructions for 8 rows of 90 took 70 us for a
+// million rows, hence no branches, extremes of bf16 pairs, and digits summed by one multiply-add each.
+template <typename T, int WPT, Q4Rows HOW>
+__device__ __forceinline__ void quantize_chunk(const T* x, uint32_t* out, int rows, int W, int nw) {
+  const int q = threadIdx.x & 3;
+  const int last = 8 * (q + 4 * (WPT - 1)), left = W - last;           // this thread's last word: elements from `last` on
+  const uint32_t mask = left >= 8 ? 0xffffffffu : left > 0 ? (1u << (4 * left)) - 1u : 0u;
+  const bool store_last = q + 4 * (WPT - 1) < nw - 1;
+  for (int row = threadIdx.x >> 2; row < ((rows + 7) & ~7); row += Q4R_THREADS / 4) {      // (whole warps: the shuffles)
+    const int at0 = min(row, rows - 1) * W + 8 * q;
+    float v[WPT][8];
+    float hi = -INFINITY, lo = INFINITY;
 #pragma unroll
-  for (int k = 0; k < WPT; ++k) {
-    const int e0 = 8 * (q + 4 * k);
-    if (e0 + 8 <= W) {
-      q4_eight<ODD>(x, at0 + e0, v[k], hi, lo);
-    } else {
+    for (int k = 0; k < WPT - 1; ++k) q4_eight<HOW, false>(x, at0 + 32 * k, 8, v[k], hi, lo);
+    q4_eight<HOW, true>(x, left > 0 ? at0 + 32 * (WPT - 1) : at0 - 8 * q, left > 0 ? left : 1, v[WPT - 1], hi, lo);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[k][i] = q4_ld(x + at0 + (e0 + i < W ? e0 + i : 0));      // past the end: a number of the row, masked below
-        hi = q4_max(hi, v[k][i]);
-        lo = q4_min(lo, v[k][i]);
-      }
+    for (int o = 1; o < 4; o <<= 1) {
+      hi = q4_max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      lo = q4_min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    }
+    const Q4Row r = q4_decide(hi, lo);
+    if (row < rows) {
+      uint32_t* o = out + row * nw;
+#pragma unroll
+      for (int k = 0; k < WPT - 1; ++k) o[q + 4 * k] = q4_word(v[k], r);
+      const uint32_t word = q4_word(v[WPT - 1], r) & mask;
+      if (store_last) o[q + 4 * (WPT - 1)] = word;
+      if (q == 0) o[nw - 1] = r.sz;
     }
   }
-#pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
-    hi = q4_max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    lo = q4_min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-  }
-  const Q4Row r = q4_decide(hi, lo);
-  if (row < rows) {
-#pragma unroll
-    for (int k = 0; k < WPT; ++k) {
-      const int w = q + 4 * k, left = W - 8 * w;       // codes this word holds, at most 8
-      if (w < nw - 1) {      // (nw - 1 <= 4 WPT: the padding word is among them)
-        uint32_t word = q4_word(v[k], r);
-        if (left < 8) word &= left > 0 ? (1u << (4 * left)) - 1u : 0u;
-        out[row * nw + w] = word;
-      }
-    }
-    if (q == 0) out[row * nw + nw - 1] = r.sz;
-  }
-  q4_take(reinterpret_cast<unsigned char*>(dst + row0 * nw), reinterpret_cast<const unsigned char*>(out), rows * nw * 4);
 }
 
+template <typename T, int WPT, Q4Rows HOW>
+__global__ void __launch_bounds__(Q4R_THREADS) quantize_rows_q4_kernel(const T* __restrict__ src, uint32_t* __restrict__ dst,
+                                                               long long n_rows, int W, int R, int32_t* __restrict__ status) {
+  extern __shared__ __align__(128) unsigned char q4_rows_smem[];
+  const int nw = q4_row_words(W), row_bytes = W * (int)sizeof(T);
+  auto chunk = [&](long long c) {
+    const int rows = (int)min((long long)R, n_rows - c * R);
+    return Q4Chunk{reinterpret_cast<const unsigned char*>(src + c * R * W), reinterpret_cast<unsigned char*>(dst + c * R * nw),
+                   rows * row_bytes, rows * nw * 4, rows, W};
+  };
+  q4_rows_pipeline(q4_rows_smem, q4_buffer(R * row_bytes), q4_buffer(R * nw * 4), (n_rows + R - 1) / R, status, chunk,
+                   [&](const Q4Chunk& k, const unsigned char* in, unsigned char* to) {
+                     quantize_chunk<T, WPT, HOW>(reinterpret_cast<const T*>(in), reinterpret_cast<uint32_t*>(to), k.rows, W, nw);
+                   });
+}
+
+template <bool VECTORS>
 __device__ __forceinline__ void q4_put8(float* base, int at, const float (&v)[8], int n) {
+  if constexpr (VECTORS) {
+    *reinterpret_cast<float4*>(base + at) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(base + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (i < n) base[at + i] = v[i];
 }
+template <bool VECTORS>
 __device__ __forceinline__ void q4_put8(__nv_bfloat16* base, int at, const float (&v)[8], int n) {
-  if ((at & 1) == 0 && n >= 8) {
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    y[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  if constexpr (VECTORS) {
+    *reinterpret_cast<uint4*>(base + at) = make_uint4(y[0], y[1], y[2], y[3]);
+    return;
+  }
+  if ((at & 1) == 0) {
     uint32_t* w = reinterpret_cast<uint32_t*>(base + at);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 y = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&y);
-    }
-  } else {
+    for (int i = 0; i < 4; ++i)
+      if (2 * i + 1 < n) w[i] = y[i];
+    if (n < 8 && (n & 1)) base[at + n - 1] = __float2bfloat16_rn(n == 1 ? v[0] : n == 3 ? v[2] : n == 5 ? v[4] : v[6]);
+  } else {                       // (rows of odd length) from a half word on
+    unsigned short* u = reinterpret_cast<unsigned short*>(base) + at;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) base[at + i] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < 4; ++i) {
+      if (2 * i < n) u[2 * i] = (unsigned short)y[i];
+      if (2 * i + 1 < n) u[2 * i + 1] = (unsigned short)(y[i] >> 16);
+    }
   }
 }
-// `rows` packed rows at src -> numbers at dst, by one CTA.  A CTA may call it again: *turn counts the calls, false: a wait ran out
-template <typename T>
-__device__ __forceinline__ bool q4_rows_back(const uint32_t* src, T* dst, int rows, int W, int R, int32_t* status, uint32_t* turn) {
-  extern __shared__ __align__(128) unsigned char q4_rows_smem_buf[];
-  const int nw = q4_row_words(W);
-  unsigned char* out = q4_rows_smem_buf + 16;
-  unsigned char* in = out + (R * W * (int)sizeof(T) + 31) / 16 * 16;
-  if (!q4_bring(in, reinterpret_cast<const unsigned char*>(src), rows * nw * 4, smem_u32(q4_rows_smem_buf), *turn & 1u, *turn > 0, status))
-    return false;
-  ++*turn;
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(in);
-  const int row = threadIdx.x >> 2, q = threadIdx.x & 3;
-  if (row < rows) {
-    const uint32_t sz = words[row * nw + nw - 1];
-    const float s = q4_step(sz), z = q4_middle(sz);
-    for (int e0 = 8 * q; e0 < W; e0 += 32) {
-      const uint32_t word = words[row * nw + (e0 >> 3)];
-      float v[8];
+// The numbers of a word: a code in bits 4 i .. (i = 1 .. 4) under the exponent of 2^23 is 2^23 + c 16^i; less 2^23 + 7.5 16^i it
+// is (c - 7.5) 16^i exactly, and the step takes the 16^-i along (exactly too: 2^-126 - 7 - 16 is the last bit there is): one
+// mask, one addition, one fused multiply-add a number.  Codes 0 and 5 to 7 come into place by a shift.
+template <typename T, bool VECTORS>
+__device__ __forceinline__ void dequantize_chunk(const uint32_t* in, T* out, int rows, int W) {
+  const int nw = q4_row_words(W), q = threadIdx.x & 3;
+  uint32_t base;                 // 0x4b000000 in a register: mask and exponent in one instruction
+  asm volatile("mov.b32 %0, 0x4b000000;" : "=r"(base));
+  for (int row = threadIdx.x >> 2; row < rows; row += Q4R_THREADS / 4) {
+    const uint32_t sz = in[row * nw + nw - 1];
+    const float z = q4_middle(sz);
+    float s[5];
+    s[0] = q4_step(sz);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        // the code under the exponent of 2^22 (a last place of 1/2), less 2^22 + 7.5
-        const uint32_t bits = 0x4a800000u | ((i == 0 ? word << 1 : word >> (4 * i - 1)) & 0x1eu);
-        v[i] = fmaf(s, __uint_as_float(bits) - 4194311.5f, z);
-      }
-      q4_put8(reinterpret_cast<T*>(out), row * W + e0, v, W - e0);
+    for (int i = 1; i < 5; ++i) s[i] = s[i - 1] * 0.0625f;
+    auto number = [&](uint32_t w, int i) {       // the code in bits 4 i ..
+      uint32_t bits;
+      asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(bits) : "r"(w), "r"(15u << (4 * i)), "r"(base));
+      const float one = (float)(1u << (4 * i));
+      return fmaf(s[i], __uint_as_float(bits) - (8388608.f + 7.5f * one), z);
+    };
+#pragma unroll 4
+    for (int e0 = 8 * q; e0 < W; e0 += 32) {
+      const uint32_t word = in[row * nw + (e0 >> 3)], up = word << 4, down = word >> 8;
+      const float v[8] = {number(up, 1), number(word, 1), number(word, 2), number(word, 3), number(word, 4), number(down, 3),
+                          number(down, 4), number(word >> 12, 4)};
+      q4_put8<VECTORS>(out, row * W + e0, v, W - e0);
     }
   }
-  q4_take(reinterpret_cast<unsigned char*>(dst), out, rows * W * (int)sizeof(T));
-  return true;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) dequantize_rows_q4_kernel(const uint32_t* __restrict__ src, T* __restrict__ dst,
+template <typename T, bool VECTORS>
+__global__ void __launch_bounds__(Q4R_THREADS) dequantize_rows_q4_kernel(const uint32_t* __restrict__ src, T* __restrict__ dst,
                                                                  long long n_rows, int W, int R, int32_t* __restrict__ status) {
-  const long long row0 = (long long)blockIdx.x * R;
-  uint32_t turn = 0;
-  q4_rows_back(src + row0 * q4_row_words(W), dst + row0 * W, (int)min((long long)R, n_rows - row0), W, R, status, &turn);
+  extern __shared__ __align__(128) unsigned char q4_rows_smem[];
+  const int nw = q4_row_words(W), row_bytes = W * (int)sizeof(T);
+  auto chunk = [&](long long c) {
+    const int rows = (int)min((long long)R, n_rows - c * R);
+    return Q4Chunk{reinterpret_cast<const unsigned char*>(src + c * R * nw), reinterpret_cast<unsigned char*>(dst + c * R * W),
+                   rows * nw * 4, rows * row_bytes, rows, W};
+  };
+  q4_rows_pipeline(q4_rows_smem, q4_buffer(R * nw * 4), q4_buffer(R * row_bytes), (n_rows + R - 1) / R, status, chunk,
+                   [&](const Q4Chunk& k, const unsigned char* in, unsigned char* to) {
+                     dequantize_chunk<T, VECTORS>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), k.rows, W);
+                   });
 }
 
 // A layer's K rows and V rows up to every sequence's length.  The chunks of R rows that exist -- per sequence
-// (K or V) x KV head x rows -- form one sequence that the CTAs walk through with the grid's stride (a grid over all
-// positions spent 15 us on CTAs without rows in a batch of unlike lengths).
-template <typename T>
-__global__ void __launch_bounds__(256)
+// (K or V) x KV head x rows -- form one sequence (a grid over all positions spent 15 us on CTAs without rows in a batch of
+// unlike lengths); a CTA finds its chunks in the prefix of the sequences' chunk counts, which it makes first.
+constexpr int Q4R_SEQS = 1024;           // sequences per launch
+template <typename T, bool VECTORS>
+__global__ void __launch_bounds__(Q4R_THREADS)
 read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict__ v4, T* __restrict__ k, T* __restrict__ v,
                      const int32_t* __restrict__ seq_len, int B, int Hkv, int S_cap, int P2, int dv, int len_max, int R,
                      int32_t* __restrict__ status) {
-  long long before = 0;        // chunks of the sequences before b
-  uint32_t turn = 0;
-  int b = 0, len = min(min(seq_len[0], S_cap), len_max), chunks = max(len + R - 1, 0) / R;
-  for (long long c = blockIdx.x;; c += gridDim.x) {
-    while (c - before >= 2LL * Hkv * chunks) {
-      before += 2LL * Hkv * chunks;
-      if (++b >= B) return;
-      len = min(min(seq_len[b], S_cap), len_max);
-      chunks = max(len + R - 1, 0) / R;
-    }
-    const int unit = (int)((c - before) / chunks), pos = (int)((c - before) - (long long)unit * chunks) * R;
+  extern __shared__ __align__(128) unsigned char q4_rows_smem[];
+  __shared__ int pref[Q4R_SEQS + 2];
+  SkPlan plan;
+  sk_plan_shared(seq_len, B, 2 * Hkv, 0, len_max, R, (int)gridDim.x, pref, Q4R_SEQS + 2, &plan);
+  auto chunk = [&](long long c) {
+    const int b = sk_seq_of(pref, B, (int)c);
+    const int len = min(max(seq_len[b], 0), len_max), per = (len + R - 1) / R;
+    const int at = (int)c - (b ? pref[b - 1] : 0), unit = at / per, pos = (at - unit * per) * R, rows = min(len - pos, R);
     const bool is_v = unit >= Hkv;
     const size_t row = ((size_t)b * Hkv + unit - (is_v ? Hkv : 0)) * S_cap + pos;
-    const int W = is_v ? dv : P2;
-    if (!q4_rows_back((is_v ? v4 : k4) + row * q4_row_words(W), (is_v ? v : k) + row * W, min(len - pos, R), W, R, status, &turn)) return;
-  }
+    const int W = is_v ? dv : P2, nw = q4_row_words(W);
+    return Q4Chunk{reinterpret_cast<const unsigned char*>((is_v ? v4 : k4) + row * nw),
+                   reinterpret_cast<unsigned char*>((is_v ? v : k) + row * W), rows * nw * 4, rows * W * (int)sizeof(T), rows, W};
+  };
+  const int wide = max(P2, dv);
+  q4_rows_pipeline(q4_rows_smem, q4_buffer(R * q4_row_words(wide) * 4), q4_buffer(R * wide * (int)sizeof(T)), plan.T, status, chunk,
+                   [&](const Q4Chunk& c, const unsigned char* in, unsigned char* to) {
+                     dequantize_chunk<T, VECTORS>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), c.rows, c.W);
+                   });
 }
 
 // RoPE / append epilogue with quantisation.  One CTA per (row t, KV head h), one warp per item: the G query heads of h
@@ -488,27 +587,43 @@ __global__ void attn_q4_combine_kernel(const float* __restrict__ ws, int n_split
 
 }  // namespace
 
+namespace {
+// rows per chunk, dynamic shared memory and CTAs of a launch over `chunks(R)` chunks
+struct Q4RowsLaunch { int R, smem; unsigned grid; };
+template <typename Chunks>
+Q4RowsLaunch q4_rows_launch(rap_ctx* ctx, int W, int elem, Chunks chunks) {
+  Q4RowsLaunch l;
+  l.R = q4_rows_per_cta(W, elem);
+  while (l.R > 16 && chunks(l.R) < 2 * ctx->sm_count) l.R /= 2;      // small calls: shorter chunks on more SMs
+  l.smem = Q4R_HEAD + 2 * (q4_buffer(l.R * W * elem) + q4_buffer(l.R * 4 * q4_row_words(W)));      // under 48 KB by Q4R_STAGE
+  int fit = (220 * 1024) / (l.smem + 1024 + (Q4R_SEQS + 2) * 4);      // CTAs an SM holds, by shared memory and by threads
+  if (fit > 2048 / Q4R_THREADS) fit = 2048 / Q4R_THREADS;
+  const long long n = chunks(l.R), most = (long long)fit * ctx->sm_count;
+  l.grid = (unsigned)(n < most ? n : most);
+  return l;
+}
+}  // namespace
+
 template <typename T>
 static rap_status launch_quantize(rap_ctx* ctx, long long n_rows, int W, const void* src, void* dst, cudaStream_t st) {
-  const int R = q4_rows_per_cta(W, (int)sizeof(T)), smem = q4_rows_smem(W, (int)sizeof(T), R);
-  const unsigned blocks = (unsigned)((n_rows + R - 1) / R);
-  auto go = [&](auto kernel) { kernel<<<blocks, 4 * R, smem, st>>>((const T*)src, (uint32_t*)dst, n_rows, W, R, ctx->d_status); };
-  auto pick = [&](auto odd) {
-    constexpr bool ODD = decltype(odd)::value;
+  const Q4RowsLaunch l = q4_rows_launch(ctx, W, (int)sizeof(T), [&](int R) { return (n_rows + R - 1) / R; });
+  auto go = [&](auto kernel) { kernel<<<l.grid, Q4R_THREADS, l.smem, st>>>((const T*)src, (uint32_t*)dst, n_rows, W, l.R, ctx->d_status); };
+  auto pick = [&](auto how) {
+    constexpr Q4Rows HOW = decltype(how)::value;
     switch ((W + 31) / 32) {
-      case 1: go(quantize_rows_q4_kernel<T, 1, ODD>); break;
-      case 2: go(quantize_rows_q4_kernel<T, 2, ODD>); break;
-      case 3: go(quantize_rows_q4_kernel<T, 3, ODD>); break;
-      case 4: go(quantize_rows_q4_kernel<T, 4, ODD>); break;
-      default: go(quantize_rows_q4_kernel<T, 8, ODD>);
+      case 1: go(quantize_rows_q4_kernel<T, 1, HOW>); break;
+      case 2: go(quantize_rows_q4_kernel<T, 2, HOW>); break;
+      case 3: go(quantize_rows_q4_kernel<T, 3, HOW>); break;
+      case 4: go(quantize_rows_q4_kernel<T, 4, HOW>); break;
+      case 5: go(quantize_rows_q4_kernel<T, 5, HOW>); break;
+      case 6: go(quantize_rows_q4_kernel<T, 6, HOW>); break;
+      case 7: go(quantize_rows_q4_kernel<T, 7, HOW>); break;
+      default: go(quantize_rows_q4_kernel<T, 8, HOW>);
     }
   };
-  if constexpr (sizeof(T) == 2) {
-    if (W & 1) pick(std::true_type{});
-    else pick(std::false_type{});
-  } else {
-    pick(std::false_type{});
-  }
+  if (W % 8 == 0) pick(std::integral_constant<Q4Rows, Q4_VECTORS>{});
+  else if (sizeof(T) == 2 && W % 2) pick(std::integral_constant<Q4Rows, Q4_HALVES>{});
+  else pick(std::integral_constant<Q4Rows, Q4_WORDS>{});
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
@@ -520,15 +635,36 @@ rap_status rap_launch_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, long long
                              : launch_quantize<__nv_bfloat16>(ctx, n_rows, W, src, dst, st);
 }
 
+template <typename T>
+static rap_status launch_dequantize(rap_ctx* ctx, long long n_rows, int W, const void* src, void* dst, cudaStream_t st) {
+  const Q4RowsLaunch l = q4_rows_launch(ctx, W, (int)sizeof(T), [&](int R) { return (n_rows + R - 1) / R; });
+  auto go = [&](auto kernel) {
+    kernel<<<l.grid, Q4R_THREADS, l.smem, st>>>((const uint32_t*)src, (T*)dst, n_rows, W, l.R, ctx->d_status);
+  };
+  if (W % 8 == 0) go(dequantize_rows_q4_kernel<T, true>);
+  else go(dequantize_rows_q4_kernel<T, false>);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}
+
 rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long long n_rows, int W, const void* src, void* dst,
                                          cudaStream_t st) {
-  const int e = rap_elem_bytes(dtype_out), R = q4_rows_per_cta(W, e), smem = q4_rows_smem(W, e, R);
-  const unsigned blocks = (unsigned)((n_rows + R - 1) / R);
-  if (dtype_out == RAP_F32)
-    dequantize_rows_q4_kernel<float><<<blocks, 4 * R, smem, st>>>((const uint32_t*)src, (float*)dst, n_rows, W, R, ctx->d_status);
-  else
-    dequantize_rows_q4_kernel<__nv_bfloat16><<<blocks, 4 * R, smem, st>>>((const uint32_t*)src, (__nv_bfloat16*)dst, n_rows, W, R,
-                                                                          ctx->d_status);
+  return dtype_out == RAP_F32 ? launch_dequantize<float>(ctx, n_rows, W, src, dst, st)
+                              : launch_dequantize<__nv_bfloat16>(ctx, n_rows, W, src, dst, st);
+}
+
+template <typename T>
+static rap_status launch_read_cache(rap_ctx* ctx, int B, int Hkv, int S_cap, int P2, int dv, const uint32_t* k4, const uint32_t* v4,
+                                    const int32_t* seq_len, int len_max, T* k, T* v, cudaStream_t st) {
+  const Q4RowsLaunch l = q4_rows_launch(ctx, P2 > dv ? P2 : dv, (int)sizeof(T),
+                                        [&](int R) { return 2LL * B * Hkv * ((len_max + R - 1) / R); });
+  if (2LL * B * Hkv * ((len_max + l.R - 1) / l.R) > 0x7fffffffLL) return RAP_ESHAPE;
+  auto go = [&](auto kernel) {
+    kernel<<<l.grid, Q4R_THREADS, l.smem, st>>>(k4, v4, k, v, seq_len, B, Hkv, S_cap, P2, dv, len_max, l.R, ctx->d_status);
+  };
+  if (P2 % 8 == 0 && dv % 8 == 0) go(read_cache_q4_kernel<T, true>);
+  else go(read_cache_q4_kernel<T, false>);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
@@ -536,18 +672,18 @@ rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long l
 
 rap_status rap_launch_read_cache_q4(rap_ctx* ctx, int dtype, int B, int Hkv, int S_cap, int P2, int dv, const void* k4, const void* v4,
                                     const int32_t* seq_len, int len_max, void* k, void* v, cudaStream_t st) {
-  const int W = P2 > dv ? P2 : dv, e = rap_elem_bytes(dtype), R = q4_rows_per_cta(W, e), smem = q4_rows_smem(W, e, R);
-  const long long chunks = 2LL * B * Hkv * ((len_max + R - 1) / R), most = 8LL * ctx->sm_count;      // eight CTAs fit an SM
-  const unsigned grid = (unsigned)(chunks < most ? chunks : most);
-  if (dtype == RAP_F32)
-    read_cache_q4_kernel<float><<<grid, 4 * R, smem, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (float*)k, (float*)v, seq_len, B,
-                                                           Hkv, S_cap, P2, dv, len_max, R, ctx->d_status);
-  else
-    read_cache_q4_kernel<__nv_bfloat16><<<grid, 4 * R, smem, st>>>((const uint32_t*)k4, (const uint32_t*)v4, (__nv_bfloat16*)k,
-                                                                   (__nv_bfloat16*)v, seq_len, B, Hkv, S_cap, P2, dv, len_max, R,
-                                                                   ctx->d_status);
-  ctx->launches++;
-  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  for (int b = 0; b < B; b += Q4R_SEQS) {      // (one launch unless the batch is enormous)
+    const int n = B - b < Q4R_SEQS ? B - b : Q4R_SEQS;
+    const size_t row = (size_t)b * Hkv * S_cap;
+    const uint32_t* ks = (const uint32_t*)k4 + row * q4_row_words(P2);
+    const uint32_t* vs = (const uint32_t*)v4 + row * q4_row_words(dv);
+    const rap_status s =
+        dtype == RAP_F32 ? launch_read_cache(ctx, n, Hkv, S_cap, P2, dv, ks, vs, seq_len + b, len_max, (float*)k + row * P2,
+                                             (float*)v + row * dv, st)
+                         : launch_read_cache(ctx, n, Hkv, S_cap, P2, dv, ks, vs, seq_len + b, len_max, (__nv_bfloat16*)k + row * P2,
+                                             (__nv_bfloat16*)v + row * dv, st);
+    if (s != RAP_OK) return s;
+  }
   return RAP_OK;
 }
 

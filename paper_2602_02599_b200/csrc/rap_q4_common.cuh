@@ -56,10 +56,12 @@ __device__ __forceinline__ Q4Row q4_decide(float hi, float lo) {
   Q4Row q;
   q.z = __bfloat162float(__float2bfloat16_rn(__fadd_rn(__fmul_rn(hi, 0.5f), __fmul_rn(lo, 0.5f))));
   const float reach = q4_max(__fsub_rn(hi, q.z), __fsub_rn(q.z, lo));
-  float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(reach, 7.5f)));
+  // reach / 7.5, correctly rounded: the fp64 product is 2^-52 off the quotient, and 2 reach / 15 lies at least a thirtieth of
+  // an fp32 step from any rounding border (15 times a border is an odd multiple of its last place, which no fp32 number is)
+  float s = __bfloat162float(__float2bfloat16_rn((float)((double)reach * (1.0 / 7.5))));
   q.bad = !(s < INFINITY);
   if (s < 1.17549435e-38f) s = 0.f;
-  q.r = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
+  q.r = s > 0.f ? __frcp_rn(s) : 0.f;
   q.sz = q.bad ? 0x7fff7fffu : (__float_as_uint(q.z) & 0xffff0000u) | (__float_as_uint(s) >> 16);      // bf16 numbers: exact
   return q;
 }
@@ -70,12 +72,11 @@ __device__ __forceinline__ uint32_t q4_code(float x, const Q4Row& q) {
 }
 // a word of eight codes: with 1.5 2^23 added a place is 0x4b400000 + code as an integer, and the eight sum up as digits
 __device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Row& q) {
-  if (q.bad) return 0x88888888u;
   uint32_t word = 0u - 0x4b400000u * 0x11111111u;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     word += __float_as_uint(__fadd_rn(__fadd_rn(__fmul_rn(__fsub_rn(x[i], q.z), q.r), 7.5f), 12582912.0f)) << (4 * i);
-  return word;
+  return q.bad ? 0x88888888u : word;
 }
 __device__ __forceinline__ float q4_step(uint32_t sz) { return __uint_as_float(sz << 16); }
 __device__ __forceinline__ float q4_middle(uint32_t sz) { return __uint_as_float(sz & 0xffff0000u); }
