@@ -9,6 +9,10 @@ rap_status rap_launch_proj_generic(rap_ctx* ctx, const rap_proj_args& a, cudaStr
 
 namespace {
 
+__device__ __forceinline__ void q4_st2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+__device__ __forceinline__ void q4_st2(__nv_bfloat16* p, float a, float b) {
+  *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(a, b);
+}
 __device__ __forceinline__ float warp_max_nan(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = q4_max(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -348,20 +352,19 @@ read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict
 // (rotated, rounded to the storage dtype, written to q_out as in the unquantised path), its key head (rotated in fp32,
 // quantised, appended) and its value head (quantised, appended).  All of them rotate by the same angles, so the sines and
 // cosines -- fp64 angle and reduction -- are taken once per CTA (one warp per item on its own: 34 us for 512 rows of the
-// 8B-shaped layer, this: 11).  A lane owns pairs of neighbouring numbers, that is whole bytes of a quantised row: P <= 128,
-// d_v' <= 256, so at most four.  y holds `ksplit` partial results, each [T][n_out].
-template <typename T>
+// 8B-shaped layer, this: 10.6).  A lane owns KP pairs of neighbouring numbers, that is whole bytes of a quantised row; P <= 128
+// and d_v' <= 256, so KP <= 4.  y holds `ksplit` partial results, each [T][n_out].
+template <typename T, int KP, bool BIAS>
 __global__ void __launch_bounds__(32 * (RAP_MAX_GROUP + 2))
 rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restrict__ bias, const int32_t* __restrict__ seq_id,
                       const int32_t* __restrict__ pos, const int32_t* __restrict__ slot, const double* __restrict__ inv_freq,
                       T* __restrict__ q_out, uint32_t* __restrict__ k4, uint32_t* __restrict__ v4, int Trows, int Hq, int Hkv,
                       int P2, int dv, int half_dim, int B_cache, int S_cap, int32_t* __restrict__ status) {
-  // launched behind the GEMM with programmatic serialization inside a decode step: nothing above this line touches
-  // memory; the GEMM's results (and, through the GEMM, the end of the scan before it) are awaited here
+  // launched behind the GEMM with programmatic serialization: nothing above this line touches memory; the GEMM's results (and, through the GEMM, the end of the scan before it) are awaited here
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ float2 turn[128];                                         // (cosine, sine) of every pair
-  const int t = blockIdx.x / Hkv, h = blockIdx.x - t * Hkv;
+  const int t = blockIdx.x, h = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int P = P2 >> 1, G = Hq / Hkv;
   const int n_out = (Hq + Hkv) * P2 + Hkv * dv;
@@ -379,19 +382,28 @@ rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restri
   const int W = is_v ? dv : P2;
   const size_t split_stride = (size_t)Trows * n_out;
   const float* yr = y + (size_t)t * n_out + col0;
-  float a[4], b[4];
+  float a[KP], b[KP];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    a[k] = b[k] = 0.f;
-    if (64 * k < W) {
+  for (int k = 0; k < KP; ++k) {
+    const int c = 2 * (lane + 32 * k);
+    a[k] = c < W ? yr[c] : 0.f;
+    b[k] = c + 1 < W ? yr[c + 1] : 0.f;
+  }
+  for (int s = 1; s < ksplit; ++s) {                                   // the sums in split order
+    yr += split_stride;
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
       const int c = 2 * (lane + 32 * k);
-#pragma unroll 4
-      for (int s = 0; s < ksplit; ++s) {                               // the sums in split order
-        a[k] += c < W ? yr[s * split_stride + c] : 0.f;
-        b[k] += c + 1 < W ? yr[s * split_stride + c + 1] : 0.f;
-      }
-      if (bias && c < W) a[k] += q4_ld(bias + col0 + c);
-      if (bias && c + 1 < W) b[k] += q4_ld(bias + col0 + c + 1);
+      a[k] += c < W ? yr[c] : 0.f;
+      b[k] += c + 1 < W ? yr[c + 1] : 0.f;
+    }
+  }
+  if constexpr (BIAS) {
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+      const int c = 2 * (lane + 32 * k);
+      if (c < W) a[k] += q4_ld(bias + col0 + c);
+      if (c + 1 < W) b[k] += q4_ld(bias + col0 + c + 1);
     }
   }
   for (int c = threadIdx.x; c < P; c += blockDim.x) {
@@ -406,7 +418,7 @@ rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restri
   __syncthreads();
   if (!is_v) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < KP; ++k) {
       const int i = lane + 32 * k;
       if (i < P) {
         const float2 cs = turn[i];
@@ -419,11 +431,10 @@ rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restri
   if (is_q) {
     T* dst = q_out + ((size_t)t * Hq + h * G + warp) * P2;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < KP; ++k) {
       const int i = lane + 32 * k;
       if (i < P) {
-        q4_st(dst + 2 * i, a[k]);
-        q4_st(dst + 2 * i + 1, b[k]);
+        q4_st2(dst + 2 * i, a[k], b[k]);
       }
     }
     return;
@@ -431,7 +442,7 @@ rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restri
   if (!row_ok) return;
   float hi = -INFINITY, lo = INFINITY;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < KP; ++k) {
     const int c = 2 * (lane + 32 * k);
     if (c < W) { hi = q4_max(hi, a[k]); lo = q4_min(lo, a[k]); }
     if (c + 1 < W) { hi = q4_max(hi, b[k]); lo = q4_min(lo, b[k]); }
@@ -441,10 +452,10 @@ rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restri
   uint32_t* row = (is_v ? v4 : k4) + (((size_t)sq * Hkv + h) * S_cap + sl) * (size_t)nw;
   unsigned char* bytes = reinterpret_cast<unsigned char*>(row);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < KP; ++k) {
     const int i = lane + 32 * k, c = 2 * i;
     if (c < W) bytes[i] = (unsigned char)(q4_code(a[k], q) | (c + 1 < W ? q4_code(b[k], q) << 4 : 0u));
-    else if (i < 4 * (nw - 1)) bytes[i] = 0;
+    else if (i < 4 * (nw - 1)) bytes[i] = 0;      // (4 (nw - 1) <= 32 KP)
   }
   if (lane == 0) row[nw - 1] = q.sz;
 }
@@ -687,6 +698,22 @@ rap_status rap_launch_read_cache_q4(rap_ctx* ctx, int dtype, int B, int Hkv, int
   return RAP_OK;
 }
 
+template <typename T>
+static cudaError_t launch_rope_append(const cudaLaunchConfig_t& cfg, rap_ctx* ctx, const rap_proj_args& a, int ksplit) {
+  auto go = [&](auto kernel) {
+    return cudaLaunchKernelEx(&cfg, kernel, (const float*)ctx->d_proj_ws, ksplit, (const T*)a.bias, a.seq_id, a.pos, a.slot, a.inv_freq,
+                              (T*)a.q_out, (uint32_t*)a.k_cache, (uint32_t*)a.v_cache, a.T, a.Hq, a.Hkv, a.P2, a.dv, a.half_dim,
+                              a.B_cache, a.S_cap, ctx->d_status);
+  };
+  auto pick = [&](auto bias) {
+    constexpr bool BIAS = decltype(bias)::value;
+    const int kp = ((a.P2 > a.dv ? a.P2 : a.dv) + 63) / 64;
+    return kp == 1 ? go(rope_append_q4_kernel<T, 1, BIAS>) : kp == 2 ? go(rope_append_q4_kernel<T, 2, BIAS>)
+                                                                     : go(rope_append_q4_kernel<T, 4, BIAS>);
+  };
+  return a.bias ? pick(std::true_type{}) : pick(std::false_type{});
+}
+
 // a.k_cache / a.v_cache are the quantised caches of this layer
 rap_status rap_launch_qkv_rope_append_q4(rap_ctx* ctx, const rap_proj_args& a, cudaStream_t st) {
   int ksplit = 1;
@@ -697,29 +724,20 @@ rap_status rap_launch_qkv_rope_append_q4(rap_ctx* ctx, const rap_proj_args& a, c
     s = rap_launch_proj_generic(ctx, a, st);
   }
   if (s != RAP_OK) return s;
-  if ((long long)a.T * a.Hkv > 0x7fffffffLL) return RAP_ESHAPE;
-  // inside a decode step (a.pdl): launched behind the tcgen05 GEMM with programmatic serialization, so that its launch
-  // overlaps the GEMM's tail (the CUDA-core GEMM never triggers early, which makes the attribute a no-op there)
+  if (a.Hkv > 65535) return RAP_ESHAPE;
+  // launched behind the library's own GEMM with programmatic serialization, so that its launch overlaps the GEMM's tail (the
+  // CUDA-core GEMM never triggers early, which makes the attribute a no-op there)
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(a.T * a.Hkv), 1, 1);
+  cfg.gridDim = dim3((unsigned)a.T, (unsigned)a.Hkv, 1);
   cfg.blockDim = dim3(32 * (a.Hq / a.Hkv + 2), 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = a.pdl ? 1 : 0;
-  const float* y = ctx->d_proj_ws;
-  uint32_t* k4 = (uint32_t*)a.k_cache;
-  uint32_t* v4 = (uint32_t*)a.v_cache;
-  if (a.dtype == RAP_F32)
-    RAP_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, rope_append_q4_kernel<float>, y, ksplit, (const float*)a.bias, a.seq_id, a.pos,
-                                         a.slot, a.inv_freq, (float*)a.q_out, k4, v4, a.T, a.Hq, a.Hkv, a.P2, a.dv, a.half_dim,
-                                         a.B_cache, a.S_cap, ctx->d_status));
-  else
-    RAP_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, rope_append_q4_kernel<__nv_bfloat16>, y, ksplit, (const __nv_bfloat16*)a.bias,
-                                         a.seq_id, a.pos, a.slot, a.inv_freq, (__nv_bfloat16*)a.q_out, k4, v4, a.T, a.Hq, a.Hkv,
-                                         a.P2, a.dv, a.half_dim, a.B_cache, a.S_cap, ctx->d_status));
+  cfg.numAttrs = 1;
+  const cudaError_t err = a.dtype == RAP_F32 ? launch_rope_append<float>(cfg, ctx, a, ksplit) : launch_rope_append<__nv_bfloat16>(cfg, ctx, a, ksplit);
+  RAP_CUDA_TRY(ctx, err);
   ctx->launches++;
   return RAP_OK;
 }
