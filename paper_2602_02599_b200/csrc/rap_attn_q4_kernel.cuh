@@ -136,6 +136,64 @@ __device__ __forceinline__ uint32_t q4_mul2(uint32_t a, uint32_t b) {
   return r;
 }
 
+// The balanced split here: as in SkPlan, but a unit costs its tiles and Q4_UNIT more (its q, its merge), and where no unit has
+// more than Q4_WHOLE tiles units are not split at all (a merge through global memory costs three or four tiles' time).  A
+// unit's positions in the sequence that the CTAs share out evenly: Q4_UNIT empty ones, then its tiles; or one for all of them.
+constexpr int Q4_UNIT = 2, Q4_WHOLE = 4;
+struct Q4Plan : SkPlan {
+  bool whole;
+  __device__ __forceinline__ int positions(int tiles) const { return tiles == 0 ? 0 : whole ? 1 : tiles + Q4_UNIT; }
+  __device__ __forceinline__ int empty() const { return whole ? 0 : Q4_UNIT; }
+};
+// The inclusive prefix of the positions of sequences 0..b goes to pref[0..B) (shared memory, room for `cap` ints; every thread
+// of the CTA calls this); a batch too large for it is planned by every thread on its own (false).
+__device__ __forceinline__ bool q4_plan(const ScanParams& p, int tile_rows, int* pref, int cap, Q4Plan* out) {
+  const bool shared = p.B <= cap - 2;
+  const int tid = threadIdx.x, lane = tid & 31;
+  auto tiles = [&](int b) { return sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, tile_rows); };
+  long long T = 0;
+  int n_max = 0;
+  if (!shared) {
+    for (int b = 0; b < p.B; ++b) n_max = max(n_max, tiles(b));
+    out->whole = n_max <= Q4_WHOLE;
+    for (int b = 0; b < p.B; ++b) T += (long long)out->positions(tiles(b)) * p.Hkv;
+  } else {
+    if (tid < 32) {
+      for (int b = lane; b < p.B; b += 32) n_max = max(n_max, tiles(b));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) n_max = max(n_max, __shfl_xor_sync(0xffffffffu, n_max, o));
+      out->whole = n_max <= Q4_WHOLE;
+      int carry = 0;
+      for (int base = 0; base < p.B; base += 32) {
+        const int b = base + lane;
+        int x = b < p.B ? out->positions(tiles(b)) * p.Hkv : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += y;
+        }
+        if (b < p.B) pref[b] = carry + x;
+        carry += __shfl_sync(0xffffffffu, x, 31);
+      }
+      if (lane == 0) {
+        pref[cap - 2] = carry;
+        pref[cap - 1] = n_max;
+      }
+    }
+    __syncthreads();
+    T = pref[cap - 2];
+    n_max = pref[cap - 1];
+    out->whole = n_max <= Q4_WHOLE;
+  }
+  out->T = (int)T;
+  out->nc = 0;
+  if (T > 0) {
+    const long long lim = out->whole ? T : (long long)(RAP_MAX_SPLIT - 2) * T / (n_max + Q4_UNIT);      // segments per unit
+    out->nc = (int)max(1LL, min(min((long long)gridDim.x, lim), T));
+  }
+  return shared;
+}
+
 template <int KSW, int VSW, int GC>
 __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kernel(const Q4ScanParams pp) {
   using C = Q4Cfg<KSW, VSW, GC>;
@@ -156,15 +214,13 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
   const int gid = lane >> 2, tq = lane & 3;
   const int G = pp.G, DV = pp.dv;
   int b = 0, h = 0;
-  SkPlan plan;
-  plan.T = 0; plan.nc = 0;
-  int cur = 0, hi = 0, unit_start = 0;
+  Q4Plan plan;
+  plan.T = 0; plan.nc = 0; plan.whole = false;
+  int lo = 0, hi = 0, unit_start = 0;      // this CTA's positions, the current unit's first one
   if (p.balanced) {
     // the plan (reads the lengths only): computed by the first warp where the ring will be
     int* pref = reinterpret_cast<int*>(smem + C::OFF_RING);
-    const bool shared_plan = sk_plan_shared(p.seq_len, p.B, p.Hkv, p.len_add, p.S_cap, ST, (int)gridDim.x, pref,
-                                            NSTG * C::STAGE_W, &plan);
-    if (!shared_plan) plan = sk_plan(p.seq_len, p.B, p.Hkv, p.len_add, p.S_cap, ST, (int)gridDim.x);
+    const bool shared_plan = q4_plan(p, ST, pref, NSTG * C::STAGE_W, &plan);
     // everything below reads what the previous kernel in the stream wrote, and writes what the next one may depend on
     pdl_wait();
     pdl_launch_dependents();
@@ -179,23 +235,23 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
       }
     }
     if ((int)blockIdx.x >= plan.nc) return;
-    cur = (int)((long long)blockIdx.x * plan.T / plan.nc);
+    lo = (int)((long long)blockIdx.x * plan.T / plan.nc);
     hi = (int)((long long)(blockIdx.x + 1) * plan.T / plan.nc);
-    if (cur >= hi) return;
+    if (lo >= hi) return;
     int pb = 0;
-    if (shared_plan) {       // the unit that holds tile `cur`
-      b = sk_seq_of(pref, p.B, cur);
+    if (shared_plan) {       // the unit that holds position `lo`
+      b = sk_seq_of(pref, p.B, lo);
       pb = b > 0 ? pref[b - 1] : 0;
     } else {
       for (b = 0; b < p.B; ++b) {
-        const int nb = sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST) * p.Hkv;
-        if (cur < pb + nb) break;
+        const int nb = plan.positions(sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST)) * p.Hkv;
+        if (lo < pb + nb) break;
         pb += nb;
       }
     }
-    const int ntb = sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST);
-    h = (cur - pb) / ntb;
-    unit_start = pb + h * ntb;
+    const int per = plan.positions(sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST));
+    h = (lo - pb) / per;
+    unit_start = pb + h * per;
   } else {
     pdl_wait();
     pdl_launch_dependents();
@@ -240,19 +296,37 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
 
   // the segment being scanned: tiles [t_begin, t_begin + n_my) of unit (b, h), seg_tiles in all
   int len = 0, seg_tiles = 0, t_begin = 0, n_my = 0;
-  auto segment = [&]() {
-    len = min(max(p.seq_len[b] + p.len_add, 0), p.S_cap);
-    seg_tiles = (len + ST - 1) / ST;
-    if (p.balanced) {
-      t_begin = cur - unit_start;
-      n_my = min(seg_tiles - t_begin, hi - cur);
-    } else {
-      const int tps = (seg_tiles + p.n_split - 1) / p.n_split;
-      t_begin = min(seg_tiles, (int)blockIdx.x * tps);
-      n_my = min(seg_tiles, t_begin + tps) - t_begin;
+  auto length = [&](int seq) { return min(max(p.seq_len[seq] + p.len_add, 0), p.S_cap); };
+  auto part = [&](int start, int tiles, int& first, int& count) {      // of the unit at position `start`, this CTA's tiles
+    first = plan.whole ? 0 : max(0, lo - start - Q4_UNIT);
+    count = (plan.whole ? tiles : min(tiles, max(0, hi - start - Q4_UNIT))) - first;
+  };
+  auto next_unit = [&](int& seq, int& head, int& start, int tiles) {   // (a further one exists where start < hi)
+    start += plan.positions(tiles);
+    if (++head == p.Hkv) {
+      head = 0;
+      do { ++seq; } while (seq < p.B - 1 && sk_tiles_of(p.seq_len, seq, p.len_add, p.S_cap, ST) == 0);
     }
   };
-  segment();
+  auto find_segment = [&]() {          // the first unit from (b, h) on that has tiles for this CTA
+    while (unit_start < hi) {
+      len = length(b);
+      seg_tiles = (len + ST - 1) / ST;
+      part(unit_start, seg_tiles, t_begin, n_my);
+      if (n_my > 0) return true;
+      next_unit(b, h, unit_start, seg_tiles);
+    }
+    return false;
+  };
+  if (p.balanced) {
+    if (!find_segment()) return;
+  } else {
+    len = length(b);
+    seg_tiles = (len + ST - 1) / ST;
+    const int tps = (seg_tiles + p.n_split - 1) / p.n_split;
+    t_begin = min(seg_tiles, (int)blockIdx.x * tps);
+    n_my = min(seg_tiles, t_begin + tps) - t_begin;
+  }
   if (n_my <= 0) {             // (equal ranges only) nothing to scan: neutral partials
     float* base = p.ws + (((size_t)b * p.Hq + (size_t)h * G) * p.n_split + blockIdx.x) * (size_t)(DV + 2);
     for (int i = tid; i < G * (DV + 2); i += THREADS) {
@@ -263,19 +337,21 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
   }
   // Copies run ahead of the scan over the CTA's whole tile sequence, unit borders included: copy_ahead brings the tile that
   // lies k >= 0 places behind the current segment's first one (by one lane), if the CTA has it.
-  const int seq_tiles = p.balanced ? hi - cur : n_my;
-  int done = 0;                // tiles of the segments before this one
+  bool begun = false;          // (test hook: only the very first tile goes without its copy)
   auto copy_ahead = [&](int k, int stg) {
-    if (done + k >= seq_tiles) return;
     int ib = b, ih = h, ilen = len, it = t_begin + k;
-    for (int n = seg_tiles; it >= n;) {               // a later unit (only in balanced mode)
-      it -= n;
-      if (++ih == p.Hkv) {
-        ih = 0;
-        do { ++ib; } while (ib < p.B - 1 && sk_tiles_of(p.seq_len, ib, p.len_add, p.S_cap, ST) == 0);
-        ilen = min(max(p.seq_len[ib] + p.len_add, 0), p.S_cap);
-        n = (ilen + ST - 1) / ST;
-      }
+    if (k >= n_my) {           // in a later unit (only in balanced mode)
+      if (!p.balanced) return;
+      int start = unit_start, tiles = seg_tiles, first = t_begin, count = n_my;
+      do {
+        k -= count;
+        next_unit(ib, ih, start, tiles);
+        if (start >= hi) return;
+        ilen = length(ib);
+        tiles = (ilen + ST - 1) / ST;
+        part(start, tiles, first, count);
+      } while (k >= count);
+      it = first + k;
     }
     const int j0 = it * ST;
     const int rows = min(ST, ((ilen + 7) & ~7) - j0);        // rows a copy may touch: S_cap is a multiple of 8
@@ -285,7 +361,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
       const uint32_t bar = bar0 + 8 * stg, dst = ring_u + 4 * stg * C::STAGE_W;
       const size_t row0 = ((size_t)ib * p.Hkv + ih) * (size_t)p.S_cap + j0;
       mbar_expect_tx(bar, kb + vb);
-      if (!(p.dbg_skip_copy && blockIdx.x == 0 && done + k == 0)) {
+      if (!(p.dbg_skip_copy && blockIdx.x == 0 && !begun && stg == 0)) {
         bulk_g2s(dst, p.k + row0 * (4 * KSW), kb, bar);
         bulk_g2s(dst + 4 * ST * KSW, p.v + row0 * (4 * VSW), vb, bar);
       }
@@ -293,31 +369,35 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
   };
   if (tid == 0)
     for (int i = 0; i < NSTG; ++i) copy_ahead(i, i);
+  begun = true;
+  // q of a unit as it is stored: column gid is head gid / 2 on even columns (GC = 1) or head gid (GC = 2), else zeros
+  uint32_t w_q[NGK][4];
+  auto load_q = [&]() {
+    const int col_head = GC == 1 ? gid >> 1 : gid;
+    const bool on = col_head < G && (GC == 2 || (gid & 1) == 0);
+    const uint32_t* qrow = p.q + ((size_t)b * p.Hq + (size_t)h * G + (on ? col_head : 0)) * pp.P;
+#pragma unroll
+    for (int j = 0; j < NGK; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = 4 * (4 * j + tq) + i;
+        w_q[j][i] = (on && at < pp.P) ? qrow[at] : 0u;
+      }
+  };
+  load_q();
 
   for (;;) {   // one pass per segment (a single one unless the mode is balanced)
-    // ---- q as the B operand: column gid is head gid / 2 on even columns (GC = 1) or head gid (GC = 2), else zeros.  Of
-    // word w = 4 j + tq of a row: k-slots 2 tq, 2 tq + 1 and 2 tq + 8, 2 tq + 9 hold dims 8 w + (0, 4) and (2, 6) in one
+    // ---- q as the B operand.  Of word w = 4 j + tq of a row: k-slots 2 tq, 2 tq + 1 and 2 tq + 8, 2 tq + 9 hold dims 8 w + (0, 4) and (2, 6) in one
     // step, (1, 5) and (3, 7) in the next; a code counts 2^-24, 2^-22 and 2^-20, 2^-18 there, which q makes up for. ----
     uint32_t qa[NGK][2], qb[NGK][2];
     float off[4], f_q[GC], zq[GC], m_ref[GC], l_thr[GC], z_thr[GC];
     {
-      const int col_head = GC == 1 ? gid >> 1 : gid;
-      const bool on = col_head < G && (GC == 2 || (gid & 1) == 0);
-      const uint32_t* qrow = p.q + ((size_t)b * p.Hq + (size_t)h * G + (on ? col_head : 0)) * pp.P;
-      uint32_t w[NGK][4];
       float top = 0.f, sum = 0.f;
 #pragma unroll
       for (int j = 0; j < NGK; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int at = 4 * (4 * j + tq) + i;
-          w[j][i] = (on && at < pp.P) ? qrow[at] : 0u;
-        }
-#pragma unroll
-      for (int j = 0; j < NGK; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x0 = __uint_as_float(w[j][i] << 16), x1 = __uint_as_float(w[j][i] & 0xffff0000u);
+          const float x0 = __uint_as_float(w_q[j][i] << 16), x1 = __uint_as_float(w_q[j][i] & 0xffff0000u);
           top = fmaxf(top, fmaxf(fabsf(x0), fabsf(x1)));
           sum += x0 + x1;
         }
@@ -331,8 +411,8 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
         float x[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[2 * i] = __uint_as_float(w[j][i] << 16) * sc;
-          x[2 * i + 1] = __uint_as_float(w[j][i] & 0xffff0000u) * sc;
+          x[2 * i] = __uint_as_float(w_q[j][i] << 16) * sc;
+          x[2 * i + 1] = __uint_as_float(w_q[j][i] & 0xffff0000u) * sc;
         }
         qa[j][0] = q4_pack(64.f * x[0], 64.f * x[4]);
         qa[j][1] = q4_pack(16.f * x[2], 16.f * x[6]);
@@ -616,24 +696,16 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
         }
       }
     }
-    const int b0 = b, h0 = h, start0 = unit_start, tiles0 = seg_tiles;      // this segment's place
+    const int b0 = b, h0 = h, start0 = unit_start + plan.empty(), tiles0 = seg_tiles;      // this segment's place
     bool more = false;
-    if (p.balanced) {
-      cur += n_my;
-      done += n_my;
-      more = cur < hi;
-      if (more) {              // the following unit, from its first tile
-        unit_start += seg_tiles;
-        if (++h == p.Hkv) {
-          h = 0;
-          do { ++b; } while (b < p.B - 1 && sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST) == 0);
-        }
-        segment();
-      }
+    if (p.balanced) {          // the following unit; its q is on the way while this one is merged
+      next_unit(b, h, unit_start, seg_tiles);
+      more = find_segment();
+      if (more) load_q();
     }
     __syncthreads();
     const int first = p.balanced ? sk_cta_of(start0, plan) : 0;
-    const int nseg = p.balanced ? sk_cta_of(start0 + tiles0 - 1, plan) - first + 1 : 0;
+    const int nseg = !p.balanced ? 0 : plan.whole ? 1 : sk_cta_of(start0 + tiles0 - 1, plan) - first + 1;
     if (nseg == 1) {
       // the whole unit was scanned here: straight to the output
       const bool o_ok = RAP_BOUNDS(((size_t)b0 * p.Hq + (size_t)h0 * G + G) * DV - 1, (size_t)p.B * p.Hq * DV, p.status, 0x40c);
