@@ -142,6 +142,18 @@ __device__ __forceinline__ uint32_t q4_mul2(uint32_t a, uint32_t b) {
 constexpr int Q4_UNIT = 2, Q4_WHOLE = 4;
 struct Q4Plan : SkPlan {
   bool whole;
+  int per, extra;              // T = per nc + extra
+  // first position of CTA c, and the CTA that has position s (both as in SkPlan, floor(c T / nc), without 64-bit divisions: in
+  // line they were a sixth of the kernel's code, and a short call's time is largely the fetching of code)
+  __device__ __forceinline__ int first_of(int c) const { return c * per + (int)((unsigned)(c * extra) / (unsigned)nc); }
+  __device__ __forceinline__ int cta_of(int s) const {
+    const long long x = ((long long)s + 1) * nc - 1;
+    int c = (int)((float)x / (float)T);      // a guess, at most a few off
+    c = min(max(c, 0), nc - 1);
+    while (c > 0 && first_of(c) > s) --c;
+    while (c + 1 < nc && first_of(c + 1) <= s) ++c;
+    return c;
+  }
   __device__ __forceinline__ int positions(int tiles) const { return tiles == 0 ? 0 : whole ? 1 : tiles + Q4_UNIT; }
   __device__ __forceinline__ int empty() const { return whole ? 0 : Q4_UNIT; }
 };
@@ -154,16 +166,20 @@ __device__ __forceinline__ bool q4_plan(const ScanParams& p, int tile_rows, int*
   long long T = 0;
   int n_max = 0;
   if (!shared) {
+#pragma unroll 1
     for (int b = 0; b < p.B; ++b) n_max = max(n_max, tiles(b));
     out->whole = n_max <= Q4_WHOLE;
+#pragma unroll 1
     for (int b = 0; b < p.B; ++b) T += (long long)out->positions(tiles(b)) * p.Hkv;
   } else {
     if (tid < 32) {
+#pragma unroll 1
       for (int b = lane; b < p.B; b += 32) n_max = max(n_max, tiles(b));
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) n_max = max(n_max, __shfl_xor_sync(0xffffffffu, n_max, o));
       out->whole = n_max <= Q4_WHOLE;
       int carry = 0;
+#pragma unroll 1
       for (int base = 0; base < p.B; base += 32) {
         const int b = base + lane;
         int x = b < p.B ? out->positions(tiles(b)) * p.Hkv : 0;
@@ -186,10 +202,16 @@ __device__ __forceinline__ bool q4_plan(const ScanParams& p, int tile_rows, int*
     out->whole = n_max <= Q4_WHOLE;
   }
   out->T = (int)T;
-  out->nc = 0;
+  out->nc = out->per = out->extra = 0;
   if (T > 0) {
-    const long long lim = out->whole ? T : (long long)(RAP_MAX_SPLIT - 2) * T / (n_max + Q4_UNIT);      // segments per unit
-    out->nc = (int)max(1LL, min(min((long long)gridDim.x, lim), T));
+    int nc = min((int)gridDim.x, out->T);
+    if (!out->whole) {         // at most RAP_MAX_SPLIT segments a unit: nc <= (RAP_MAX_SPLIT - 2) T / longest
+      const unsigned longest = (unsigned)(n_max + Q4_UNIT), q = (unsigned)out->T / longest;
+      if (q < 1024u) nc = min(nc, (int)((RAP_MAX_SPLIT - 2) * q + (RAP_MAX_SPLIT - 2) * ((unsigned)out->T - q * longest) / longest));
+    }
+    out->nc = max(1, nc);
+    out->per = out->T / out->nc;
+    out->extra = out->T - out->per * out->nc;
   }
   return shared;
 }
@@ -225,24 +247,28 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
     pdl_wait();
     pdl_launch_dependents();
     if (blockIdx.x == 0) {   // sequences without any row are scanned by nobody: their output is zero
+#pragma unroll 1
       for (int i = tid; i < p.B * p.Hkv; i += THREADS) p.unit_cnt_other[i] = 0;   // counters a launch that gave up left behind
       if (tid == 0) *p.dyn_next_other = 0;          // and the piece counter a bf16 tensor-core launch before this one used
+#pragma unroll 1
       for (int bb = 0; bb < p.B; ++bb) {
         const bool empty = shared_plan ? pref[bb] == (bb > 0 ? pref[bb - 1] : 0)
                                        : sk_tiles_of(p.seq_len, bb, p.len_add, p.S_cap, ST) == 0;
         if (empty)
+#pragma unroll 1
           for (int i = tid; i < p.Hq * DV; i += THREADS) p.out[(size_t)bb * p.Hq * DV + i] = 0.f;
       }
     }
     if ((int)blockIdx.x >= plan.nc) return;
-    lo = (int)((long long)blockIdx.x * plan.T / plan.nc);
-    hi = (int)((long long)(blockIdx.x + 1) * plan.T / plan.nc);
+    lo = plan.first_of(blockIdx.x);
+    hi = plan.first_of(blockIdx.x + 1);
     if (lo >= hi) return;
     int pb = 0;
     if (shared_plan) {       // the unit that holds position `lo`
       b = sk_seq_of(pref, p.B, lo);
       pb = b > 0 ? pref[b - 1] : 0;
     } else {
+#pragma unroll 1
       for (b = 0; b < p.B; ++b) {
         const int nb = plan.positions(sk_tiles_of(p.seq_len, b, p.len_add, p.S_cap, ST)) * p.Hkv;
         if (lo < pb + nb) break;
@@ -305,10 +331,12 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
     start += plan.positions(tiles);
     if (++head == p.Hkv) {
       head = 0;
+#pragma unroll 1
       do { ++seq; } while (seq < p.B - 1 && sk_tiles_of(p.seq_len, seq, p.len_add, p.S_cap, ST) == 0);
     }
   };
   auto find_segment = [&]() {          // the first unit from (b, h) on that has tiles for this CTA
+#pragma unroll 1
     while (unit_start < hi) {
       len = length(b);
       seg_tiles = (len + ST - 1) / ST;
@@ -329,6 +357,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
   }
   if (n_my <= 0) {             // (equal ranges only) nothing to scan: neutral partials
     float* base = p.ws + (((size_t)b * p.Hq + (size_t)h * G) * p.n_split + blockIdx.x) * (size_t)(DV + 2);
+#pragma unroll 1
     for (int i = tid; i < G * (DV + 2); i += THREADS) {
       const int g = i / (DV + 2), c = i - g * (DV + 2);
       base[(size_t)g * p.n_split * (DV + 2) + c] = (c == DV) ? -INFINITY : 0.f;
@@ -343,6 +372,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
     if (k >= n_my) {           // in a later unit (only in balanced mode)
       if (!p.balanced) return;
       int start = unit_start, tiles = seg_tiles, first = t_begin, count = n_my;
+#pragma unroll 1
       do {
         k -= count;
         next_unit(ib, ih, start, tiles);
@@ -368,6 +398,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
     }
   };
   if (tid == 0)
+#pragma unroll 1
     for (int i = 0; i < NSTG; ++i) copy_ahead(i, i);
   begun = true;
   // q of a unit as it is stored: column gid is head gid / 2 on even columns (GC = 1) or head gid (GC = 2), else zeros
@@ -596,6 +627,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
 
     bool fresh = true;           // no row of this segment so far
     int nrows = len - t_begin * ST - Q4_BR * warp;      // valid rows from this warp's block on
+#pragma unroll 1
     for (int i = 0; i < n_my; ++i, nrows -= ST) {
       if (__any_sync(0xffffffffu, !mbar_test_wait(bar0 + 8 * st, parity)) &&
           !__all_sync(0xffffffffu, mbar_wait_slow(bar0 + 8 * st, parity, p.wait_limit))) {   // warp-uniform verdict
@@ -670,6 +702,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
       }
       // give copies still in flight a bounded chance to land before the shared memory is released
       if (tid == 0)
+#pragma unroll 1
         for (int sg = 0; sg < NSTG; ++sg) {
           mbar_wait_bounded(bar0 + 8 * sg, 0, p.wait_limit);
           mbar_wait_bounded(bar0 + 8 * sg, 1, p.wait_limit);
@@ -704,11 +737,16 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
       if (more) load_q();
     }
     __syncthreads();
-    const int first = p.balanced ? sk_cta_of(start0, plan) : 0;
-    const int nseg = !p.balanced ? 0 : plan.whole ? 1 : sk_cta_of(start0 + tiles0 - 1, plan) - first + 1;
+    // the CTAs that share the unit (most often none but this one)
+    int first = 0, nseg = p.balanced ? 1 : 0;
+    if (p.balanced && !plan.whole && (start0 < lo || start0 + tiles0 > hi)) {
+      first = plan.cta_of(start0);
+      nseg = plan.cta_of(start0 + tiles0 - 1) - first + 1;
+    }
     if (nseg == 1) {
       // the whole unit was scanned here: straight to the output
       const bool o_ok = RAP_BOUNDS(((size_t)b0 * p.Hq + (size_t)h0 * G + G) * DV - 1, (size_t)p.B * p.Hq * DV, p.status, 0x40c);
+#pragma unroll 1
       for (int i = tid; i < G * DV && o_ok; i += THREADS) {
         const int g = i / DV, c = i - g * DV;
         float sum = 0.f, l = 0.f;
@@ -724,6 +762,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
       float* unit_ws = p.ws + ((size_t)b0 * p.Hq + (size_t)h0 * G) * ws_head;
       float* ws_base = unit_ws + (size_t)((int)blockIdx.x - first) * (DV + 2);
       const bool ws_ok = RAP_BOUNDS((ws_base - p.ws) + (long long)(G - 1) * ws_head + DV + 1, p.ws_floats, p.status, 0x409);
+#pragma unroll 1
       for (int i = tid; i < G * DV && ws_ok; i += THREADS) {
         const int g = i / DV, c = i - g * DV;
         float sum = 0.f;
@@ -753,6 +792,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
         const bool m_ok = RAP_BOUNDS((unit_ws - p.ws) + (long long)(G - 1) * ws_head + (long long)(nseg - 1) * (DV + 2) + DV + 1,
                                      p.ws_floats, p.status, 0x40b);
         float* wgt = red;        // [G][RAP_MAX_SPLIT] segment weights, then G reciprocals of the denominators
+#pragma unroll 1
         for (int g = warp; g < G && m_ok; g += NW) {
           const float* gb = unit_ws + (size_t)g * ws_head;
           float mv[2], lv[2];
@@ -777,6 +817,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
           if (lane == 0) wgt[G * RAP_MAX_SPLIT + g] = den != 0.f ? 1.f / den : 0.f;
         }
         __syncthreads();
+#pragma unroll 1
         for (int i = tid; i < G * DV && m_ok; i += THREADS) {
           const int g = i / DV, c = i - g * DV;
           const float* gb = unit_ws + (size_t)g * ws_head + c;
