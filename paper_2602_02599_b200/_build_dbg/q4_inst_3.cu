@@ -1,0 +1,21 @@
+// generated by build.py: instantiations of the tensor-core scan over a 4-bit cache, part 3
+#include "rap_attn_q4_kernel.cuh"
+namespace {
+template <int K, int V, int C> rap_q4_entry entry() {
+  return rap_q4_entry{K, V, C, Q4Cfg<K, V, C>::SMEM, Q4Cfg<K, V, C>::NW * 32, (const void*)attn_q4_kernel<K, V, C>};
+}
+}  // namespace
+const rap_q4_entry* rap_q4_table_3(int* n) {
+  static const rap_q4_entry table[] = {
+    entry<3, 9, 1>(),
+    entry<7, 9, 1>(),
+    entry<11, 9, 1>(),
+    entry<15, 9, 1>(),
+    entry<3, 9, 2>(),
+    entry<7, 9, 2>(),
+    entry<11, 9, 2>(),
+    entry<15, 9, 2>(),
+  };
+  *n = (int)(sizeof(table) / sizeof(table[0]));
+  return table;
+}

@@ -148,6 +148,7 @@ struct Q4Whole {
   static constexpr int SUMS = 4 * NGV;                                // fp32 sums per lane: 4 channels of each of NGV tiles
   static constexpr int FLUSH = 512;                                   // blocks: 255 * 255 * 32 * 512 < 2^31
   static constexpr uint32_t LOW = 0x0f0f0f0fu;
+  static constexpr float LIMIT = 4294967040.f;                        // rounds to less than 2^32
   int gid, tq, lane;
   At at;
   uint32_t qd[NGK][4];         // B operands of word group j: digits (0 | 2) and (1 | 3) of the bytes' coefficient, then of the codes'
@@ -155,6 +156,7 @@ struct Q4Whole {
   int acc[NGV][2][2][4];       // [tile][bytes, codes][digits 0 and 2, 1 and 3][row gid: two columns, row gid + 8: two columns]
   uint32_t s_even, s_odd;      // sums of the weights' digits: column gid, this lane's rows
   float f_q, zq, m_ref[1], l_thr[1], z_thr[1];
+  float limit;                 // of a weight: above it the reference is raised; 0: flush at the next block
   bool have, dirty;            // shared memory / the accumulators hold something
 
   __device__ __forceinline__ static int q_head(int gid) { return gid >> 1; }
@@ -172,32 +174,34 @@ struct Q4Whole {
       }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = min(max(21 - q4_exponent(top), -100), 120);         // the largest |q| 2^e lies in [2^21, 2^22)
+    const int e = min(21 - q4_exponent(top), 120);                    // the largest |q| 2^e lies in [2^21, 2^22)
     const float sc = q4_pow2(e);
     int total = 0;
-    const int sh = (gid & 1) * 16;                                    // this column's two digits of four
+    const uint32_t mine = (gid & 1) ? 0x7362u : 0x5140u;              // this column's two digits of four, of two numbers
 #pragma unroll
     for (int j = 0; j < NGK; ++j) {
-      uint32_t d[4] = {0u, 0u, 0u, 0u};
+      uint32_t x[2][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int qe = __float2int_rn(__uint_as_float(w[j][i] << 16) * sc), qo = __float2int_rn(__uint_as_float(w[j][i] & 0xffff0000u) * sc);
         total += qe + qo;
         // balanced digits -128 .. 127 of a number: the bytes of (x + 0x80808080) less 128 each
-        const uint32_t b = (((uint32_t)qo + 0x80808080u) ^ 0x80808080u) >> sh, c = (((uint32_t)(16 * qe - qo) + 0x80808080u) ^ 0x80808080u) >> sh;
-        d[0] |= (b & 255u) << (8 * i);
-        d[1] |= (b >> 8 & 255u) << (8 * i);
-        d[2] |= (c & 255u) << (8 * i);
-        d[3] |= (c >> 8 & 255u) << (8 * i);
+        x[0][i] = (uint32_t)qo + 0x80808080u;
+        x[1][i] = (uint32_t)(16 * qe - qo) + 0x80808080u;
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) qd[j][i] = d[i];
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t y = __byte_perm(x[k][0], x[k][1], mine), z = __byte_perm(x[k][2], x[k][3], mine);
+        qd[j][2 * k] = __byte_perm(y, z, 0x5410) ^ 0x80808080u;
+        qd[j][2 * k + 1] = __byte_perm(y, z, 0x7632) ^ 0x80808080u;
+      }
     }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
       total += __shfl_xor_sync(0xffffffffu, total, o);
       sum += __shfl_xor_sync(0xffffffffu, sum, o);
     }
+    sum = fmaf(top, 0.f, sum);                                        // an infinity in q makes its head's outputs NaN
     const long long offset = -120LL * total;                          // |total| < 2^29
     const int high = (int)((offset + 32768) >> 16), low = (int)(offset - ((long long)high << 16));
     const int from = 8 * tq;                                          // a lane that holds this lane's head
@@ -210,6 +214,7 @@ struct Q4Whole {
     l_thr[0] = z_thr[0] = 0.f;
     clear();
     have = dirty = false;
+    limit = LIMIT;
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -246,19 +251,15 @@ struct Q4Whole {
       }
     }
   }
-  __device__ __forceinline__ void flush(float* sums) {
-    float v[NGV][4];
-    total(sums, v);
-#pragma unroll
-    for (int t = 0; t < NGV; ++t) reinterpret_cast<float4*>(sums)[t * 32 + lane] = make_float4(v[t][0], v[t][1], v[t][2], v[t][3]);
-    clear();
-    have = true;
-    dirty = false;
-  }
+  __device__ __forceinline__ void flush(float*) { limit = 0.f; }      // (done by the next block: one copy of the code)
+
+  struct Rows {                // of the lane's four rows
+    float s[4], e[4], w[4], big;                                      // 16 sum q (c - 7.5), weights, weights times V step, their maximum
+    uint32_t ksz[4], vsz[4];
+  };
   template <bool TAIL>
-  __device__ __forceinline__ void block(const uint32_t* __restrict__ sw, int nrows, float* sums) {
+  __device__ __forceinline__ void weigh(const uint32_t* __restrict__ sw, int nrows, Rows& r) {
     // ---- logits: two tiles of 16 rows, 64 dims a step ----
-    float s[4];
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
       const uint32_t* x = sw + at.k + 2 * mt * KSW;
@@ -285,64 +286,75 @@ struct Q4Whole {
         }
       }
 #pragma unroll
-      for (int r = 0; r < 2; ++r)      // 16 sum q (c - 7.5): digits 3 .. 0
-        s[2 * mt + r] = fmaf((float)(odd[2 * r + 1] * 256 + even[2 * r + 1]), 65536.f, (float)(odd[2 * r] * 256 + even[2 * r]));
+      for (int i = 0; i < 2; ++i)      // digits 3 .. 0
+        r.s[2 * mt + i] = fmaf((float)(odd[2 * i + 1] * 256 + even[2 * i + 1]), 65536.f, (float)(odd[2 * i] * 256 + even[2 * i]));
     }
     // ---- weights ----
-    uint32_t ksz[4], vsz[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      ksz[t] = sw[at.ksz + t * KSW];
-      vsz[t] = sw[at.vsz + t * VSW];
-      if (TAIL && 4 * gid + t >= nrows) ksz[t] = vsz[t] = 0u;
+      r.ksz[t] = sw[at.ksz + t * KSW];
+      r.vsz[t] = sw[at.vsz + t * VSW];
+      if (TAIL && 4 * gid + t >= nrows) r.ksz[t] = r.vsz[t] = 0u;
     }
-    float e[4], w[4];
-    for (bool raised = false;; raised = true) {
-      float big = 0.f;
+    weights(r, TAIL ? nrows : Q4_BR);
+  }
+  __device__ __forceinline__ void weights(Rows& r, int nrows) {
+    r.big = 0.f;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        float x = fmaf(q4_step(ksz[t]) * f_q, s[t], fmaf(q4_middle(ksz[t]), zq, -m_ref[0]));
-        if (TAIL && 4 * gid + t >= nrows) x = -INFINITY;
-        e[t] = q4_ex2(x);
-        w[t] = e[t] * q4_step(vsz[t]);
-        big = q4_max(big, w[t]);
-      }
-      if (raised || !__any_sync(0xffffffffu, !(big < 4294967040.f))) break;      // (a first block's reference is -inf)
-      // raise the reference so that the block's largest weight (its step included) becomes 2^27 .. 2^28
-      float x[4], mx = -3e38f, most = 0.f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        x[t] = fmaf(q4_step(ksz[t]) * f_q, s[t], q4_middle(ksz[t]) * zq);
-        if (TAIL && 4 * gid + t >= nrows) x[t] = -INFINITY;
-        mx = fmaxf(mx, x[t]);
-      }
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-#pragma unroll
-      for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(vsz[t]));
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-      const float m_new = fmaxf(m_ref[0], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 27, -100), 100) : 0.f));
-      const float alpha = q4_ex2(m_ref[0] - m_new);          // first block: 2^(-inf) = 0
-      m_ref[0] = m_new;
-      l_thr[0] *= alpha;
-      z_thr[0] *= alpha;
-      if (dirty) flush(sums);
-      if (have) {
-#pragma unroll
-        for (int t = 0; t < NGV; ++t) {
-          float4& v = reinterpret_cast<float4*>(sums)[t * 32 + lane];
-          v = make_float4(v.x * alpha, v.y * alpha, v.z * alpha, v.w * alpha);
-        }
-      }
+    for (int t = 0; t < 4; ++t) {
+      float x = fmaf(q4_step(r.ksz[t]) * f_q, r.s[t], fmaf(q4_middle(r.ksz[t]), zq, -m_ref[0]));
+      if (4 * gid + t >= nrows) x = -INFINITY;
+      r.e[t] = q4_ex2(x);
+      r.w[t] = r.e[t] * q4_step(r.vsz[t]);
+      r.big = q4_max(r.big, r.w[t]);
     }
+  }
+  // raise the reference so that the block's largest weight (its step included) becomes 2^27 .. 2^28; what is summed so far moves
+  // to shared memory, scaled
+  __device__ __forceinline__ void raise(Rows& r, int nrows, float* sums) {
+    float x[4], mx = -3e38f, most = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      x[t] = 4 * gid + t < nrows ? fmaf(q4_step(r.ksz[t]) * f_q, r.s[t], q4_middle(r.ksz[t]) * zq) : -INFINITY;
+      mx = fmaxf(mx, x[t]);
+    }
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+#pragma unroll
+    for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(r.vsz[t]));
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+    const float m_new = fmaxf(m_ref[0], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 27, -100), 100) : 0.f));
+    const float alpha = q4_ex2(m_ref[0] - m_new);          // first block: 2^(-inf) = 0
+    m_ref[0] = m_new;
+    l_thr[0] *= alpha;
+    z_thr[0] *= alpha;
+    if (dirty) {
+      float v[NGV][4];
+      total(sums, v);
+#pragma unroll
+      for (int t = 0; t < NGV; ++t)
+        reinterpret_cast<float4*>(sums)[t * 32 + lane] = make_float4(v[t][0] * alpha, v[t][1] * alpha, v[t][2] * alpha, v[t][3] * alpha);
+      clear();
+      have = true;
+      dirty = false;
+    }
+    limit = LIMIT;
+    weights(r, nrows);
+  }
+
+  __device__ __forceinline__ void block(const uint32_t* __restrict__ sw, int nrows, float* sums) {
+    Rows r;
+    if (nrows >= Q4_BR) weigh<false>(sw, nrows, r);
+    else weigh<true>(sw, nrows, r);
+    if (__any_sync(0xffffffffu, !(r.big < limit))) raise(r, nrows, sums);      // (a first block's reference is -inf)
     // ---- row sums; the weights' digits, turned into the B operand: k-slots 4 tq .. are rows 8 tq + t, 8 tq + 4 + t of t = 0, 1 (2, 3) ----
     uint32_t p[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      l_thr[0] += e[t];
-      z_thr[0] = fmaf(e[t], q4_middle(vsz[t]), z_thr[0]);
-      p[t] = q4_transpose(__float2uint_rn(w[t]));
+      l_thr[0] += r.e[t];
+      z_thr[0] = fmaf(r.e[t], q4_middle(r.vsz[t]), z_thr[0]);
+      p[t] = q4_transpose(__float2uint_rn(r.w[t]));
     }
     const uint32_t e0 = __byte_perm(p[0], p[1], 0x6420), e1 = __byte_perm(p[2], p[3], 0x6420);
     const uint32_t o0 = __byte_perm(p[0], p[1], 0x7531), o1 = __byte_perm(p[2], p[3], 0x7531);
@@ -437,7 +449,7 @@ struct Q4Half {
       }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = min(max(8 - q4_exponent(top), -100), 120);          // the largest |q| 2^e lies in [2^8, 2^9)
+    const int e = min(max(8 - q4_exponent(top), -109), 120);          // the largest |q| 2^e lies in [2^8, 2^9)
     const float sc = q4_pow2(e);
     float seen = 0.f;            // sum of q 2^e as the MMAs see it
 #pragma unroll
@@ -460,6 +472,7 @@ struct Q4Half {
       seen += __shfl_xor_sync(0xffffffffu, seen, d);
       sum += __shfl_xor_sync(0xffffffffu, sum, d);
     }
+    sum = fmaf(top, 0.f, sum);   // an infinity in q makes its head's outputs NaN
     // what the accumulator columns 2 tq, 2 tq + 1 need, from the lanes that hold those columns of q
     const float off_c = -7.5f * 0x1p-18f * seen, f_c = cs * q4_pow2(18 - e), z_c = cs * sum;
 #pragma unroll
@@ -502,10 +515,13 @@ struct Q4Half {
     have = true;
   }
 
+  struct Rows {                // of the lane's four rows, each for two heads
+    float s[2][4], e[4][2], w[4][2], big;
+    uint32_t ksz[4], vsz[4];
+  };
   template <bool TAIL>
-  __device__ __forceinline__ void block(const uint32_t* __restrict__ sw, int nrows, float* sums) {
+  __device__ __forceinline__ void weigh(const uint32_t* __restrict__ sw, int nrows, Rows& r) {
     // ---- S = K q: two tiles of 16 rows, two steps of 16 dims per group ----
-    float s[2][4];
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
@@ -513,81 +529,88 @@ struct Q4Half {
         const uint32_t x0 = sw[at.k + 2 * mt * KSW + 4 * j], x1 = sw[at.k + (2 * mt + 1) * KSW + 4 * j];
         const uint32_t h0 = x0 >> 6, h1 = x1 >> 6;
         const uint32_t a0 = x0 & 0x000f000fu, a1 = x1 & 0x000f000fu, a2 = h0 & 0x003c003cu, a3 = h1 & 0x003c003cu;
-        if (j == 0) q4_mma_from(s[mt], off, a0, a1, a2, a3, qa[j][0], qa[j][1]);
-        else q4_mma(s[mt], a0, a1, a2, a3, qa[j][0], qa[j][1]);
-        q4_mma(s[mt], x0 & 0x00f000f0u, x1 & 0x00f000f0u, h0 & 0x03c003c0u, h1 & 0x03c003c0u, qb[j][0], qb[j][1]);
+        if (j == 0) q4_mma_from(r.s[mt], off, a0, a1, a2, a3, qa[j][0], qa[j][1]);
+        else q4_mma(r.s[mt], a0, a1, a2, a3, qa[j][0], qa[j][1]);
+        q4_mma(r.s[mt], x0 & 0x00f000f0u, x1 & 0x00f000f0u, h0 & 0x03c003c0u, h1 & 0x03c003c0u, qb[j][0], qb[j][1]);
       }
     }
     // ---- weights ----
-    uint32_t ksz[4], vsz[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      ksz[t] = sw[at.ksz + t * KSW];
-      vsz[t] = sw[at.vsz + t * VSW];
-      if (TAIL && 4 * gid + t >= nrows) ksz[t] = vsz[t] = 0u;
+      r.ksz[t] = sw[at.ksz + t * KSW];
+      r.vsz[t] = sw[at.vsz + t * VSW];
+      if (TAIL && 4 * gid + t >= nrows) r.ksz[t] = r.vsz[t] = 0u;
     }
-    float e[4][2], w[4][2];
-    for (bool raised = false;; raised = true) {
-      float big = 0.f;
+    weights(r, TAIL ? nrows : Q4_BR);
+  }
+  __device__ __forceinline__ void weights(Rows& r, int nrows) {
+    r.big = 0.f;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float ks = q4_step(ksz[t]), kz = q4_middle(ksz[t]);
-        const float vs = __uint_as_float(vsz[t] * 65536u + row_sign);      // the step, negated on the second row of a pair
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          float x = fmaf(ks * f_q[g], s[t >> 1][2 * (t & 1) + g], fmaf(kz, zq[g], -m_ref[g]));
-          if (TAIL && 4 * gid + t >= nrows) x = -INFINITY;
-          e[t][g] = q4_ex2(x);
-          w[t][g] = e[t][g] * vs;
-          big = q4_max(big, fabsf(w[t][g]));
-        }
-      }
-      if (raised || !__any_sync(0xffffffffu, !(big <= WEIGHT_MAX))) break;       // (a first block's reference is -inf)
-      // raise the references so that the block's largest weight (its step included) becomes 4 .. 8
+    for (int t = 0; t < 4; ++t) {
+      const float ks = q4_step(r.ksz[t]), kz = q4_middle(r.ksz[t]);
+      const float vs = __uint_as_float(r.vsz[t] * 65536u + row_sign);      // the step, negated on the second row of a pair
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        float x[4], mx = -3e38f, most = 0.f;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          x[t] = fmaf(q4_step(ksz[t]) * f_q[g], s[t >> 1][2 * (t & 1) + g], q4_middle(ksz[t]) * zq[g]);
-          if (TAIL && 4 * gid + t >= nrows) x[t] = -INFINITY;
-          mx = fmaxf(mx, x[t]);
-        }
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-#pragma unroll
-        for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(vsz[t]));
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        const float m_new = fmaxf(m_ref[g], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 2, -80), 100) : 0.f));
-        const float alpha = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
-        m_ref[g] = m_new;
-        l_thr[g] *= alpha;
-        z_thr[g] *= alpha;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          o[t][g] *= alpha;
-          o[t][2 + g] *= alpha;
-          if (have) {
-            sums[(t * 32 + lane) * 4 + g] *= alpha;
-            sums[(t * 32 + lane) * 4 + 2 + g] *= alpha;
-          }
-        }
-        dsum[g] *= alpha;
+        float x = fmaf(ks * f_q[g], r.s[t >> 1][2 * (t & 1) + g], fmaf(kz, zq[g], -m_ref[g]));
+        if (4 * gid + t >= nrows) x = -INFINITY;
+        r.e[t][g] = q4_ex2(x);
+        r.w[t][g] = r.e[t][g] * vs;
+        r.big = q4_max(r.big, fabsf(r.w[t][g]));
       }
     }
+  }
+  // raise the references so that the block's largest weight (its step included) becomes 4 .. 8
+  __device__ __forceinline__ void raise(Rows& r, int nrows, float* sums) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float x[4], mx = -3e38f, most = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        x[t] = 4 * gid + t < nrows ? fmaf(q4_step(r.ksz[t]) * f_q[g], r.s[t >> 1][2 * (t & 1) + g], q4_middle(r.ksz[t]) * zq[g]) : -INFINITY;
+        mx = fmaxf(mx, x[t]);
+      }
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+#pragma unroll
+      for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(r.vsz[t]));
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+      const float m_new = fmaxf(m_ref[g], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 2, -80), 100) : 0.f));
+      const float alpha = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
+      m_ref[g] = m_new;
+      l_thr[g] *= alpha;
+      z_thr[g] *= alpha;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        o[t][g] *= alpha;
+        o[t][2 + g] *= alpha;
+        if (have) {
+          sums[(t * 32 + lane) * 4 + g] *= alpha;
+          sums[(t * 32 + lane) * 4 + 2 + g] *= alpha;
+        }
+      }
+      dsum[g] *= alpha;
+    }
+    weights(r, nrows);
+  }
+
+  __device__ __forceinline__ void block(const uint32_t* __restrict__ sw, int nrows, float* sums) {
+    Rows r;
+    if (nrows >= Q4_BR) weigh<false>(sw, nrows, r);
+    else weigh<true>(sw, nrows, r);
+    if (__any_sync(0xffffffffu, !(r.big <= WEIGHT_MAX))) raise(r, nrows, sums);      // (a first block's references are -inf)
     // ---- row sums; the weights as fp16 pairs, turned into the B operand ----
     uint32_t pb[4], pl[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const float vz = q4_middle(vsz[t]);
+      const float vz = q4_middle(r.vsz[t]);
       float top[2], rest[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        l_thr[g] += e[t][g];
-        z_thr[g] = fmaf(e[t][g], vz, z_thr[g]);
-        top[g] = __uint_as_float(__float_as_uint(w[t][g]) & 0xffff0000u);
-        rest[g] = w[t][g] - top[g];
+        l_thr[g] += r.e[t][g];
+        z_thr[g] = fmaf(r.e[t][g], vz, z_thr[g]);
+        top[g] = __uint_as_float(__float_as_uint(r.w[t][g]) & 0xffff0000u);
+        rest[g] = r.w[t][g] - top[g];
       }
       pb[t] = q4_transpose(q4_pack(top[0], top[1]));
       pl[t] = q4_transpose(q4_pack(rest[0], rest[1]));

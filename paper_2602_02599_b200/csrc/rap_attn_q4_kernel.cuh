@@ -55,7 +55,9 @@ struct Q4Plan : SkPlan {
     const long long x = ((long long)s + 1) * nc - 1;
     int c = (int)((float)x / (float)T);      // a guess, at most a few off
     c = min(max(c, 0), nc - 1);
+#pragma unroll 1
     while (c > 0 && first_of(c) > s) --c;
+#pragma unroll 1
     while (c + 1 < nc && first_of(c + 1) <= s) ++c;
     return c;
   }
@@ -328,10 +330,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
 #ifdef RAP_DEBUG_BOUNDS
       in_ok = __all_sync(0xffffffffu, RAP_BOUNDS((int)(sw - reinterpret_cast<const uint32_t*>(smem)) + eng.at.reach(), C::SMEM / 4, p.status, 0x405));
 #endif
-      if (in_ok) {
-        if (nrows >= Q4_BR) eng.template block<false>(sw, nrows, my_main);
-        else if (nrows > 0) eng.template block<true>(sw, nrows, my_main);
-      }
+      if (in_ok && nrows > 0) eng.block(sw, nrows, my_main);
       // this warp is done with the stage (its loads have been used)
       __syncwarp();
       if (lane == 0) mbar_arrive(bar0 + 8 * (Q4_MAX_STG + st));

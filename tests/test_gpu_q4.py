@@ -418,6 +418,134 @@ def test_attention_captured_and_replayed():
     st.close()
 
 
+@pytest.mark.parametrize("G", [3, 8])
+def test_attention_large_q_on_small_rows_and_an_infinity_in_q(G):
+    w = _small(batch=2, n_q_heads=2 * G, n_kv_heads=2)
+    lens = [400, 35]
+    st, q, k4, v4, dl = _attn_stack(w, lens, seed=10, gain=1e33)
+    g = torch.Generator(device=st.device).manual_seed(3)
+    x = torch.randn((2, w.n_kv_heads, st.s_cap, 2 * w.n_pairs), generator=g, device=st.device) * 1e-33
+    st.ctx.rap_quantize_rows_q4(binding.RAP_F32, x.numel() // x.shape[-1], x.shape[-1], x, k4)
+    held = [q4_util.unpack(c, W) for c, W in ((k4, 2 * w.n_pairs), (v4, w.n_vch))]
+    out = _run_attn(st, w, q, k4, v4, dl)
+    _ok(st)
+    q4_util.check_attn(util.to_np64(out), util.to_np64(q), held[0], held[1], lens, w.head_dim)
+    for value in (float("inf"), float("-inf"), float("nan")):
+        q2 = q.clone()
+        q2[0, G + 1, 5] = value
+        got = _run_attn(st, w, q2, k4, v4, dl)
+        _ok(st)
+        assert torch.isnan(got[0, G + 1]).all()
+        got[0, G + 1] = out[0, G + 1]
+        q4_util.check_attn(util.to_np64(got), util.to_np64(q), held[0], held[1], lens, w.head_dim)
+    st.close()
+
+
+@pytest.mark.parametrize("G", [1, 4, 5])
+def test_attention_one_cta_over_a_long_sequence_of_the_largest_codes(G):
+    """140,000 rows on one CTA: 547 blocks a warp, past what one filling of the accumulators may hold.  The first tiles' rows weigh
+    2^-3.9 of the others, so that the weights stay just below the size at which the reference is raised.  All rows have the same V, so
+    the outputs are its numbers."""
+    n, dv = 140000, 64
+    w = _small(n_pairs=16, n_vch=dv, n_q_heads=G, n_kv_heads=1)
+    st = DecodeStack(w, s_cap=n, alloc_cache=False)
+    st.build_tables(*synth.draw_scores(w))
+    codes = np.zeros((1, 1, n, 32), dtype=np.uint8)
+    codes[:, :, 2048:, 0] = 15
+    one = np.ones((1, 1, n))
+    v_codes = np.where(np.arange(dv) < 40, 15, np.arange(dv) % 16).astype(np.uint8) * np.ones((1, 1, n, 1), dtype=np.uint8)
+    k4, v4 = (torch.from_numpy(q4_util.pack(c, one, 0 * one)).to(st.device) for c in (codes, v_codes))
+    q = torch.zeros((1, G, 32), dtype=st.dt, device=st.device)
+    q[:, :, 0] = 3.9 * float(np.sqrt(w.head_dim) * np.log(2)) / 15
+    out = util.to_np64(_run_attn(st, w, q, k4, v4, torch.tensor([n], dtype=torch.int32, device=st.device), 1))
+    _ok(st)
+    # the codes' sums are exact (G <= 4) or rounded once per 16 blocks; the row sums, fp32, take 4 * 547 additions a lane
+    want = v_codes[0, 0, 0] - 7.5
+    assert np.all(np.abs(out[0] - want) <= 2.0 ** -24 * (4 * 547 + 600) * np.abs(want).max())
+    st.close()
+
+
+def test_attention_of_twenty_thousand_sequences():
+    """More than the plan in shared memory holds: sequences of every length 0 .. 49, the same fifty again and again."""
+    B, w = 20000, _small(n_q_heads=8, n_kv_heads=2)
+    lens = list(range(50))
+    st, q, k4, v4, dl = _attn_stack(replace(w, batch=50), lens, seed=12, s_cap=56)
+    small = _run_attn(st, w, q, k4, v4, dl)
+    _ok(st)
+    held = [q4_util.unpack(c, W) for c, W in ((k4, 2 * w.n_pairs), (v4, w.n_vch))]
+    q4_util.check_attn(util.to_np64(small), util.to_np64(q), held[0], held[1], lens, w.head_dim)
+    st.close()
+    big = DecodeStack(replace(w, batch=B), s_cap=56, alloc_cache=False)
+    big.build_tables(*synth.draw_scores(w))
+    out = _run_attn(big, w, q.repeat(B // 50, 1, 1), k4.repeat(B // 50, 1, 1, 1), v4.repeat(B // 50, 1, 1, 1), dl.repeat(B // 50), bound=49)
+    _ok(big)
+    assert torch.equal(out, small.repeat(B // 50, 1, 1))
+    big.close()
+
+
+def test_read_cache_of_many_sequences():
+    """More sequences than one plan of the read-back covers."""
+    B, S = 2500, 24
+    w = _small(batch=B, n_q_heads=2, n_kv_heads=1, n_pairs=3, n_vch=5)
+    st = DecodeStack(w, s_cap=S)
+    st.build_tables(*synth.draw_scores(w))
+    k4, v4 = q4_util.caches(st, 0)
+    g = torch.Generator(device=st.device).manual_seed(2)
+    dl = torch.randint(0, S + 1, (B,), generator=g, device=st.device, dtype=torch.int32)
+    dl[100:1400] = 0
+    used = (torch.arange(S, device=st.device)[None, :] < dl[:, None])[:, None, :, None]
+    want = []
+    for packed, W, cache in ((k4, 6, st.k_cache[0]), (v4, 5, st.v_cache[0])):
+        x = torch.randn(packed.shape[:3] + (W,), generator=g, device=st.device)
+        st.ctx.rap_quantize_rows_q4(binding.RAP_F32, B * S, W, x, packed)
+        back = torch.empty(x.shape, dtype=st.dt, device=st.device)
+        st.ctx.rap_dequantize_rows_q4(_kind(w.dtype), B * S, W, packed, back)
+        cache.fill_(7.0)
+        want.append(torch.where(used, back, torch.full_like(back, 7.0)))
+    st.ctx.rap_read_cache_q4(0, B, k4, v4, S, dl, S, st.k_cache[0], st.v_cache[0])
+    _ok(st)
+    assert torch.equal(st.k_cache[0], want[0]) and torch.equal(st.v_cache[0], want[1])
+    st.close()
+
+
+def test_two_contexts_on_two_streams():
+    cases = [_attn_stack(_small(batch=3), [3000, 911, 64], seed=s) for s in (20, 21)]
+    w = _small(batch=3)
+    alone = [_run_attn(st, w, q, k4, v4, dl) for st, q, k4, v4, dl in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [[], []]
+    for _ in range(6):
+        for i, (st, q, k4, v4, dl) in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(_run_attn(st, w, q, k4, v4, dl, bound=3000))
+    torch.cuda.synchronize()
+    for i, (st, *_rest) in enumerate(cases):
+        assert all(torch.equal(alone[i], o) for o in outs[i])
+        assert st.ctx.rap_get_last_device_status() == (0, 0)
+        st.close()
+
+
+def test_a_wait_that_runs_out_is_reported_and_the_next_launch_is_right():
+    w = _small(batch=5)
+    lens = [900, 5, 0, 411, 64]
+    st, q, k4, v4, dl = _attn_stack(w, lens, seed=13)
+    want = _run_attn(st, w, q, k4, v4, dl)
+    _ok(st)
+    st.ctx.rap_debug_arm_wait_timeout()
+    got = _run_attn(st, w, q, k4, v4, dl)                  # returns: the wait is bounded
+    torch.cuda.synchronize()
+    assert torch.isnan(got[0, : w.group]).all()            # the first unit was never finished
+    done = ~torch.isnan(got).any(-1)
+    assert int((~done).sum()) <= 2 * w.group and torch.equal(got[done], want[done])
+    for _ in range(2):
+        assert torch.equal(_run_attn(st, w, q, k4, v4, dl), want)
+    torch.cuda.synchronize()
+    code, _detail = st.ctx.rap_get_last_device_status()
+    assert code == binding.RAP_ETIMEOUT and st.ctx.rap_get_last_device_status() == (0, 0)
+    st.close()
+
+
 # ---- together ------------------------------------------------------------------------------------------------------------------
 
 
