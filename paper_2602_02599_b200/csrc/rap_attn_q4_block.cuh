@@ -17,9 +17,10 @@
 //     that the transpose wants.  The reference of the softmax makes the block's largest weight 2^27 .. 2^28 and is raised when
 //     one passes 2^32; what is lost of a weight is 2^-29 of the largest.  Sums are exact, 7.5 sum p comes off in whole numbers too.
 // A word of eight codes costs one mask on the K side and three byte permutes or masks on the V side, where fp16 operands cost
-// five and eight (measured on 32 heads, 8 KV heads, 32K rows, batch 32: 158 us against 167).
+// five and eight (measured on 32 heads, 8 KV heads, 32K rows, batch 32: 156 us against 167).
 //
-// Q4Half, five to eight heads: the digits of a weight would take two MMAs more per operand, and twice the accumulators.  fp16 in,
+// Q4Half, five to eight heads: the whole-number form would need twice the accumulators, 96 registers for rows of 90; on six warps of
+// 168 registers it took 117 us for five heads over 4 sequences of up to 100K rows, this form 82.  fp16 in,
 // fp32 accumulate (m16n8k16):
 //   * A nibble under no exponent bits is an fp16 subnormal, so an operand register of two codes is one mask of a shifted word.
 //     Which code sits on which k-slot is free as long as both operands agree; on the K side the factors between the positions go
