@@ -250,8 +250,13 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
  *                           nor written.  h_seq_len_max: the caller's bound on d_seq_len (<= S_cap).
  *   rap_qkv_rope_append_q4  rap_qkv_rope_append with the new K and V rows quantised straight from their fp32 values; q~
  *                           as in rap_qkv_rope_append.  The rows of one call name distinct (sequence, slot) pairs.
- *   rap_decode_attn_q4      rap_decode_attn over quantised caches (Eq. 2 on the values above; a row's weight stays fp32
- *                           to about 2^-22).  Rows past a sequence's length may hold anything.
+ *   rap_decode_attn_q4      rap_decode_attn over quantised caches (Eq. 2 on the values above).  bf16 stacks with rows of up
+ *                           to 128 numbers: q~ enters with 22 bits of its head's largest number (H_q / H_kv <= 4) or as fp16
+ *                           pairs of that range, a row's weight with 19 bits or more of its own and not below 2^-28 of the
+ *                           largest; sums are exact or fp32.  V steps below about 2^-70 lose digits (an absolute 2^-98 a
+ *                           row).  A NaN row makes the outputs of its KV head's query heads NaN, a NaN or an infinity in q~
+ *                           those of its own head (H_q / H_kv > 4: a q~ from 2^117 on as well).  Rows past a sequence's
+ *                           length may hold anything.
  *   rap_decode_step_q4      rap_decode_step over quantised caches (h_k4 / h_v4: HOST arrays of L device pointers).
  * Arguments, errors and stream behaviour as for the unquantised calls; RAP_EINVAL when the current device is not the
  * one the context was created on. */
