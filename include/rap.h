@@ -252,14 +252,14 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
  *                           as in rap_qkv_rope_append.  The rows of one call name distinct (sequence, slot) pairs.
  *   rap_decode_attn_q4      rap_decode_attn over quantised caches (Eq. 2 on the values above).  bf16 stacks with rows of up
  *                           to 128 numbers: q~ enters with 22 bits of its head's largest number (H_q / H_kv <= 4) or as fp16
- *                           pairs of that range, a row's weight with 19 bits or more of its own and not below 2^-28 of the
- *                           largest; sums are exact or fp32.  V steps below about 2^-70 lose digits (an absolute 2^-98 a
- *                           row).  A NaN row makes the outputs of its KV head's query heads NaN, a NaN or an infinity in q~
- *                           those of its own head (H_q / H_kv > 4: a q~ from 2^117 on as well).  Rows past a sequence's
- *                           length may hold anything.
+ *                           pairs of that range, a row's weight with 19 bits or more of its own down to 2^-27 of the largest
+ *                           (below, the mean over rows is kept); sums are exact or fp32.  V steps below about 2^-70 lose
+ *                           digits (an absolute 2^-98 a row).  A NaN row makes the outputs of its KV head's query heads NaN,
+ *                           a NaN or an infinity in q~ those of its own head (H_q / H_kv > 4: a q~ from 2^117 on as well).
+ *                           Rows past a sequence's length may hold anything.
  *   rap_decode_step_q4      rap_decode_step over quantised caches (h_k4 / h_v4: HOST arrays of L device pointers).
  * Arguments, errors and stream behaviour as for the unquantised calls; RAP_EINVAL when the current device is not the
- * one the context was created on. */
+ * one the context was created on, and from the conversions when what they read and what they write overlap. */
 size_t rap_q4_row_bytes(int32_t W);
 rap_status rap_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, int64_t n_rows, int32_t W, const void* d_rows, void* d_q4,
                                 void* stream);

@@ -590,12 +590,18 @@ static rap_status on_own_device(rap_ctx* ctx) {
 
 size_t rap_q4_row_bytes(int32_t W) { return W < 1 ? 0 : 4 * (((((size_t)W + 1) / 2 + 4 + 3) / 4) | 1); }
 
-// shared by the two directions; an empty call is not checked further by the callers
-static rap_status rows_q4_check(rap_ctx* ctx, int32_t dtype, int64_t n_rows, int32_t W, const void* from, const void* to) {
-  if (!ctx || !from || !to) return RAP_EINVAL;
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y ? y - x < na : x - y < nb;
+}
+
+// shared by the two directions (q4: the quantised side); an empty call is not checked further by the callers
+static rap_status rows_q4_check(rap_ctx* ctx, int32_t dtype, int64_t n_rows, int32_t W, const void* rows, const void* q4) {
+  if (!ctx || !rows || !q4) return RAP_EINVAL;
   if ((dtype != RAP_F32 && dtype != RAP_BF16) || n_rows < 0 || W < 1) return RAP_EINVAL;
-  if (!rap_aligned16(from) || !rap_aligned16(to)) return RAP_EALIGN;
+  if (!rap_aligned16(rows) || !rap_aligned16(q4)) return RAP_EALIGN;
   if (W > 256 || (n_rows + 7) / 8 > 0x7fffffffLL) return RAP_ESHAPE;
+  if (overlap(rows, (size_t)n_rows * W * rap_elem_bytes(dtype), q4, (size_t)n_rows * rap_q4_row_bytes(W))) return RAP_EINVAL;
   return on_own_device(ctx);
 }
 
@@ -608,7 +614,7 @@ rap_status rap_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, int64_t n_rows, 
 
 rap_status rap_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, int64_t n_rows, int32_t W, const void* d_q4, void* d_rows,
                                   void* stream) {
-  const rap_status s = rows_q4_check(ctx, dtype_out, n_rows, W, d_q4, d_rows);
+  const rap_status s = rows_q4_check(ctx, dtype_out, n_rows, W, d_rows, d_q4);
   if (s != RAP_OK || n_rows == 0) return s;
   return rap_launch_dequantize_rows_q4(ctx, dtype_out, n_rows, W, d_q4, d_rows, (cudaStream_t)stream);
 }
@@ -625,6 +631,14 @@ rap_status rap_read_cache_q4(rap_ctx* ctx, int32_t layer, int32_t B, const void*
   if (!rap_aligned16(d_k4) || !rap_aligned16(d_v4) || !rap_aligned16(d_seq_len) || !rap_aligned16(d_k_cache) ||
       !rap_aligned16(d_v_cache))
     return RAP_EALIGN;
+  const size_t rows = (size_t)B * d.n_kv_heads * S_cap, e = rap_elem_bytes(d.dtype);
+  const void* const from[2] = {d_k4, d_v4};
+  const void* const to[2] = {d_k_cache, d_v_cache};
+  const size_t from_bytes[2] = {rows * rap_q4_row_bytes(2 * ctx->n_pairs[layer]), rows * rap_q4_row_bytes(ctx->n_vch[layer])};
+  const size_t to_bytes[2] = {rows * 2 * ctx->n_pairs[layer] * e, rows * ctx->n_vch[layer] * e};
+  for (int i = 0; i < 4; ++i)
+    if (overlap(from[i & 1], from_bytes[i & 1], to[i >> 1], to_bytes[i >> 1])) return RAP_EINVAL;
+  if (overlap(to[0], to_bytes[0], to[1], to_bytes[1])) return RAP_EINVAL;
   const rap_status s = on_own_device(ctx);
   if (s != RAP_OK || B == 0 || h_seq_len_max == 0) return s;
   return rap_launch_read_cache_q4(ctx, d.dtype, B, d.n_kv_heads, S_cap, 2 * ctx->n_pairs[layer], ctx->n_vch[layer], d_k4, d_v4,

@@ -15,7 +15,9 @@
 //   * outputs: sum p c from the masked bytes, sum p c' = (sum p b - sum p c) / 16.  A row's weight, its V step included, is a whole
 //     number of 32 bits whose four bytes are the digits: the register of a lane's weight is already the pair of 16-bit columns
 //     that the transpose wants.  The reference of the softmax makes the block's largest weight 2^27 .. 2^28 and is raised when
-//     one passes 2^32; what is lost of a weight is 2^-29 of the largest.  Sums are exact, 7.5 sum p comes off in whole numbers too.
+//     one passes 2^32.  Sums are exact, 7.5 sum p comes off in whole numbers too.  A weight's fraction (2^-27 of the largest, or
+//     less) is cut at a point that moves by the golden section from block to block, so that equal weights far below the largest --
+//     100,000 of 2^-26 beside one of 1 -- are right in the sum (rounded to nearest they were off together, by a quarter).
 // A word of eight codes costs one mask on the K side and three byte permutes or masks on the V side, where fp16 operands cost
 // five and eight (measured on 32 heads, 8 KV heads, 32K rows, batch 32: 156 us against 167).
 //
@@ -32,7 +34,7 @@
 //     every two rows that share an operand register the second enters with its codes complemented (15 - c, the same mask
 //     operation) and its weight negated (off by 3e-4 at 32K rows without it).  What is left is 7.5 times the sum of the signed
 //     weights, which one MMA against ones keeps along.  Every FLUSH blocks the accumulators move into fp32 sums in shared memory.
-//   * The reference makes the largest weight 4 .. 8, raised when one passes 2^15.
+//   * The reference makes the largest weight 2^9 .. 2^10 (fp16 ends 33 places below that), raised when one passes 2^15.
 // The middles are summed apart in fp32; a power of two in every weight drops out of the quotient.  Rows past the end get weight,
 // step and middle zero by selection (TAIL); their bytes may be anything.
 #pragma once
@@ -156,8 +158,9 @@ struct Q4Whole {
   int off[4], zero[4];         // -120 sum q as 2^16 off[1] + off[0], on both tile halves
   int acc[NGV][2][2][4];       // [tile][bytes, codes][digits 0 and 2, 1 and 3][row gid: two columns, row gid + 8: two columns]
   uint32_t s_even, s_odd;      // sums of the weights' digits: column gid, this lane's rows
-  float f_q, zq, m_ref[1], l_thr[1], z_thr[1];
+  float f_q, zq, m_ref[1], l_thr[1], z_thr[1], l_part, z_part;      // l, z: sums of the weights, and with the middles; see settle
   float limit;                 // of a weight: above it the reference is raised; 0: flush at the next block
+  float point;                 // where a weight's fraction is cut: up from 1 - point on
   bool have, dirty;            // shared memory / the accumulators hold something
 
   __device__ __forceinline__ static int q_head(int gid) { return gid >> 1; }
@@ -212,10 +215,11 @@ struct Q4Whole {
     zq = __shfl_sync(0xffffffffu, cs * sum, from);
     zero[0] = zero[1] = zero[2] = zero[3] = 0;
     m_ref[0] = -INFINITY;
-    l_thr[0] = z_thr[0] = 0.f;
+    l_thr[0] = z_thr[0] = l_part = z_part = 0.f;
     clear();
     have = dirty = false;
     limit = LIMIT;
+    point = 0.125f * gid;
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -251,6 +255,13 @@ struct Q4Whole {
         v[t][2 * r + 1] = fmaf(y, 0.0625f, r ? was.w : was.y);
       }
     }
+  }
+  // the sums of the last blocks to those of all (called every few blocks: fewer additions to a number that one large weight has
+  // made large)
+  __device__ __forceinline__ void settle() {
+    l_thr[0] += l_part;
+    z_thr[0] += z_part;
+    l_part = z_part = 0.f;
   }
   __device__ __forceinline__ void flush(float*) { limit = 0.f; }      // (done by the next block: one copy of the code)
 
@@ -328,6 +339,7 @@ struct Q4Whole {
     const float m_new = fmaxf(m_ref[0], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 27, -100), 100) : 0.f));
     const float alpha = q4_ex2(m_ref[0] - m_new);          // first block: 2^(-inf) = 0
     m_ref[0] = m_new;
+    settle();
     l_thr[0] *= alpha;
     z_thr[0] *= alpha;
     if (dirty) {
@@ -353,10 +365,12 @@ struct Q4Whole {
     uint32_t p[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      l_thr[0] += r.e[t];
-      z_thr[0] = fmaf(r.e[t], q4_middle(r.vsz[t]), z_thr[0]);
-      p[t] = q4_transpose(__float2uint_rn(r.w[t]));
+      l_part += r.e[t];
+      z_part = fmaf(r.e[t], q4_middle(r.vsz[t]), z_part);
+      p[t] = q4_transpose(__float2uint_rz(r.w[t] + point));
     }
+    point += 0.618034f;
+    if (point >= 1.f) point -= 1.f;
     const uint32_t e0 = __byte_perm(p[0], p[1], 0x6420), e1 = __byte_perm(p[2], p[3], 0x6420);
     const uint32_t o0 = __byte_perm(p[0], p[1], 0x7531), o1 = __byte_perm(p[2], p[3], 0x7531);
     s_even = __dp4a(e0, 0x01010101u, __dp4a(e1, 0x01010101u, s_even));
@@ -404,7 +418,10 @@ struct Q4Whole {
 
   // scaled sums of head g of this lane to the merge buffer (which may lie where `sums` does)
   float out[NGV][4];
-  __device__ __forceinline__ void finish(float* sums) { total(sums, out); }
+  __device__ __forceinline__ void finish(float* sums) {
+    settle();
+    total(sums, out);
+  }
   __device__ __forceinline__ void put(float* rr, int, float f) const {
 #pragma unroll
     for (int t = 0; t < NGV; ++t) {
@@ -428,7 +445,7 @@ struct Q4Half {
   int gid, tq, lane;
   At at;
   uint32_t qa[NGK][2], qb[NGK][2];
-  float off[4], f_q[2], zq[2], m_ref[2], l_thr[2], z_thr[2];
+  float off[4], f_q[2], zq[2], m_ref[2], l_thr[2], z_thr[2], l_part[2], z_part[2];
   float o[NT][4], dsum[4];     // columns 2 tq, 2 tq + 1 are this lane's heads
   uint32_t flip0, flip4, row_sign;
   bool have;
@@ -482,7 +499,7 @@ struct Q4Half {
       f_q[i] = __shfl_sync(0xffffffffu, f_c, 4 * (2 * tq + i));
       zq[i] = __shfl_sync(0xffffffffu, z_c, 4 * (2 * tq + i));
       m_ref[i] = -INFINITY;
-      l_thr[i] = z_thr[i] = 0.f;
+      l_thr[i] = z_thr[i] = l_part[i] = z_part[i] = 0.f;
     }
     flip0 = q4_keep(0x000f0000u);
     flip4 = q4_keep(0x00f00000u);
@@ -506,6 +523,14 @@ struct Q4Half {
       o[t][1] = fmaf(-7.5f * 0x1p-14f, dsum[1], o[t][1]) + was.y;
       o[t][2] = fmaf(-7.5f * 0x1p-20f, dsum[0], o[t][2]) + was.z;
       o[t][3] = fmaf(-7.5f * 0x1p-20f, dsum[1], o[t][3]) + was.w;
+    }
+  }
+  __device__ __forceinline__ void settle() {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      l_thr[g] += l_part[g];
+      z_thr[g] += z_part[g];
+      l_part[g] = z_part[g] = 0.f;
     }
   }
   __device__ __forceinline__ void flush(float* sums) {
@@ -560,8 +585,9 @@ struct Q4Half {
       }
     }
   }
-  // raise the references so that the block's largest weight (its step included) becomes 4 .. 8
+  // raise the references so that the block's largest weight (its step included) becomes 2^9 .. 2^10
   __device__ __forceinline__ void raise(Rows& r, int nrows, float* sums) {
+    settle();
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       float x[4], mx = -3e38f, most = 0.f;
@@ -576,7 +602,7 @@ struct Q4Half {
       for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(r.vsz[t]));
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-      const float m_new = fmaxf(m_ref[g], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 2, -80), 100) : 0.f));
+      const float m_new = fmaxf(m_ref[g], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 9, -80), 100) : 0.f));
       const float alpha = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
       m_ref[g] = m_new;
       l_thr[g] *= alpha;
@@ -608,8 +634,8 @@ struct Q4Half {
       float top[2], rest[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        l_thr[g] += r.e[t][g];
-        z_thr[g] = fmaf(r.e[t][g], vz, z_thr[g]);
+        l_part[g] += r.e[t][g];
+        z_part[g] = fmaf(r.e[t][g], vz, z_part[g]);
         top[g] = __uint_as_float(__float_as_uint(r.w[t][g]) & 0xffff0000u);
         rest[g] = r.w[t][g] - top[g];
       }
@@ -650,7 +676,10 @@ struct Q4Half {
     }
   }
 
-  __device__ __forceinline__ void finish(float* sums) { total(sums); }
+  __device__ __forceinline__ void finish(float* sums) {
+    settle();
+    total(sums);
+  }
   __device__ __forceinline__ void put(float* rr, int g, float f) const {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {

@@ -336,6 +336,7 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
       if (lane == 0) mbar_arrive(bar0 + 8 * (Q4_MAX_STG + st));
       if (turn-- == 0) {       // the warps take turns to refill
         turn = NW - 1;
+        eng.settle();
         if ((held += NW) >= C::Engine::FLUSH) {
           eng.flush(my_main);
           held = 0;

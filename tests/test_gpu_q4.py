@@ -465,6 +465,40 @@ def test_attention_one_cta_over_a_long_sequence_of_the_largest_codes(G):
     st.close()
 
 
+@pytest.mark.parametrize("G", [1, 4, 5])
+def test_attention_one_large_weight_over_a_long_flat_tail(G):
+    """One row outweighs each of 60,000 equal ones by 2^25.5 or so: what a narrow weight loses of each must not add up."""
+    n = 60000
+    w = _small(n_pairs=16, n_vch=48, n_q_heads=G, n_kv_heads=1)
+    st = DecodeStack(w, s_cap=n, alloc_cache=False)
+    st.build_tables(*synth.draw_scores(w))
+    k_codes, v_codes = np.zeros((1, 1, n, 32), dtype=np.uint8), np.full((1, 1, n, 48), 15, dtype=np.uint8)
+    k_codes[:, :, 5] = 15
+    v_codes[:, :, 5] = 0
+    one = np.ones((1, 1, n))
+    held = [(c, one, 0 * one) for c in (k_codes, v_codes)]
+    k4, v4 = (torch.from_numpy(q4_util.pack(*h)).to(st.device) for h in held)
+    q = torch.zeros((1, G, 32), dtype=st.dt, device=st.device)
+    q[:, :, 0] = torch.tensor([25.3 + 0.1 * g for g in range(G)]) * float(np.sqrt(w.head_dim) * np.log(2)) / 15
+    want = O.decode_attn_q4(util.to_np64(q), held[0], held[1], [n], w.head_dim)
+    for n_split in (0, 1):
+        out = util.to_np64(_run_attn(st, w, q, k4, v4, torch.tensor([n], dtype=torch.int32, device=st.device), n_split))
+        _ok(st)
+        # The logits, up to 26 / log2(e), may be off by 2^-22 of that.  The row sums, fp32, take 30 or so additions of eight blocks each
+        # and one per row among eight blocks: 40 times 2^-24.
+        # G <= 4: a weight's fraction counts up to 2^-27 of the largest weight and is cut at points that follow the golden section: of a
+        # lane's N equal weights per row of a block at most 2 + log2 N too many or too few are cut up; 8 lanes x 4 rows x 8 warps hold
+        # N <= 235 each.  (Cut alike, the tail would be off by up to 60000 2^-28 = 2.2e-4.)
+        # G > 4: fp16 ends 2^-33 below the largest weight, 60000 times half of that; the splitting's 2^-19 of the tail; and the MMAs
+        # cut their running sums off: those of 16 blocks, 64 MMAs, by 2^-23 of at most 15 (the large row, complemented), and 7.5 times
+        # the sum of the weights by as much of 7.5.  (Later ones start from nothing.)
+        tail = (n - 1) * 2.0 ** -25.2
+        tol = 7.5 * (2 * tail * (26 * 2.0 ** -22 + 2.0 ** -19) + 40 * 2.0 ** -24 + 2.0 ** -20)
+        tol += 7.5 * 256 * 10 * 2.0 ** -27 if G <= 4 else 7.5 * n * 2.0 ** -34 + 64 * 2.0 ** -23 * (15 + 7.5)
+        assert np.all(np.abs(out - want) <= tol), (np.abs(out - want).max(), tol)
+    st.close()
+
+
 def test_attention_of_twenty_thousand_sequences():
     """More than the plan in shared memory holds: sequences of every length 0 .. 49, the same fifty again and again."""
     B, w = 20000, _small(n_q_heads=8, n_kv_heads=2)
@@ -678,4 +712,27 @@ def test_refusals():
     refused(binding.RAP_ESHAPE, st.ctx.rap_quantize_rows_q4, binding.RAP_F32, 1, 257, x, k4)
     _ok(st)
     assert not k4.any() and not v4.any()
+    st.close()
+
+
+def test_conversions_refuse_buffers_that_overlap():
+    w = synth.scaled_down(synth.LLAMA_8B, n_layers=1, batch=2, seq=16, hidden=256)
+    st = DecodeStack(w, s_cap=16)
+    st.build_tables(*synth.draw_scores(w))
+    k4, v4 = q4_util.caches(st, 0)
+    dl = torch.tensor([3, 4], dtype=torch.int32, device=st.device)
+    K, V = st.k_cache[0], st.v_cache[0]
+    rows = torch.randn((64, 90), device=st.device)
+    for call in (lambda: st.ctx.rap_quantize_rows_q4(binding.RAP_F32, 64, 90, rows, rows),
+                 lambda: st.ctx.rap_dequantize_rows_q4(binding.RAP_F32, 8, 90, rows.data_ptr() + 64, rows),
+                 lambda: st.ctx.rap_read_cache_q4(0, 2, K, v4, 16, dl, 4, K, V),
+                 lambda: st.ctx.rap_read_cache_q4(0, 2, k4, V, 16, dl, 4, K, V),
+                 lambda: st.ctx.rap_read_cache_q4(0, 2, k4, v4, 16, dl, 4, K, K.data_ptr() + 16)):
+        with pytest.raises(binding.RapError) as e:
+            call()
+        assert e.value.status == binding.RAP_EINVAL
+    before = rows.clone()
+    st.ctx.rap_read_cache_q4(0, 2, k4, k4, 16, dl, 4, K, V)          # the same source twice is no overlap
+    _ok(st)
+    assert torch.equal(rows, before)
     st.close()

@@ -132,3 +132,24 @@ def test_host_refusals_before_any_device_call(lib):
         assert lib.rap_decode_attn_q4(ctx, 0, 1, None, a, a, 8, a, 8, 0, a, None) == binding.RAP_EINVAL
     finally:
         lib.rap_destroy(ctx)
+
+
+def test_conversions_refuse_buffers_that_overlap(lib):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present: the GPU tests make these calls on a whole context")
+    desc = binding.rap_model_desc(1, 256, 4, 2, 64, 10000.0, 0, binding.RAP_BF16, 4, 4)
+    ctx = ctypes.c_void_p()
+    assert lib.rap_create(ctypes.byref(desc), ctypes.byref(ctx)) == binding.RAP_ECUDA
+    try:
+        rows, a = 100, 1 << 20
+        wide, narrow = rows * 90 * 2, rows * 52
+        for f in (lib.rap_quantize_rows_q4, lib.rap_dequantize_rows_q4):
+            first, second = (wide, narrow) if f is lib.rap_quantize_rows_q4 else (narrow, wide)
+            # (no device: a call that passes the checks ends at the question for the current device)
+            for b, clear in ((a, False), (a + first - first % 16 - 16, False), (a + first + 16 - first % 16, True),
+                             (a - second + second % 16 + 16, False), (a - second - 16 + second % 16, True)):
+                s = f(ctx, binding.RAP_BF16, rows, 90, a, b // 16 * 16, None)
+                assert s == (binding.RAP_ECUDA if clear else binding.RAP_EINVAL), (b - a, s)
+    finally:
+        lib.rap_destroy(ctx)
