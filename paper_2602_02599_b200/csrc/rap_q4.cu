@@ -42,6 +42,7 @@ struct Q4Chunk {
   const unsigned char* src;
   unsigned char* dst;
   int in_bytes, out_bytes, rows, W;
+  bool is_v;
 };
 // bytes of an input / output buffer that holds n (the loads of a row's last word may reach 32 past it)
 __host__ __device__ constexpr int q4_buffer(int n) { return (n + 47) / 16 * 16; }
@@ -225,7 +226,7 @@ __global__ void __launch_bounds__(Q4R_THREADS) quantize_rows_q4_kernel(const T* 
   auto chunk = [&](long long c) {
     const int rows = (int)min((long long)R, n_rows - c * R);
     return Q4Chunk{reinterpret_cast<const unsigned char*>(src + c * R * W), reinterpret_cast<unsigned char*>(dst + c * R * nw),
-                   rows * row_bytes, rows * nw * 4, rows, W};
+                   rows * row_bytes, rows * nw * 4, rows, W, false};
   };
   q4_rows_pipeline(q4_rows_smem, q4_buffer(R * row_bytes), q4_buffer(R * nw * 4), (n_rows + R - 1) / R, status, chunk,
                    [&](const Q4Chunk& k, const unsigned char* in, unsigned char* to) {
@@ -233,18 +234,19 @@ __global__ void __launch_bounds__(Q4R_THREADS) quantize_rows_q4_kernel(const T* 
                    });
 }
 
-template <bool VECTORS>
+// eight numbers to a row in shared memory, from element `at` on; PART: the first n of them (a row's last word)
+template <Q4Rows HOW, bool PART>
 __device__ __forceinline__ void q4_put8(float* base, int at, const float (&v)[8], int n) {
-  if constexpr (VECTORS) {
+  if constexpr (HOW == Q4_VECTORS) {
     *reinterpret_cast<float4*>(base + at) = make_float4(v[0], v[1], v[2], v[3]);
     *reinterpret_cast<float4*>(base + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < n) base[at + i] = v[i];
+    for (int i = 0; i < 8; ++i)
+      if (!PART || i < n) base[at + i] = v[i];
+  }
 }
-template <bool VECTORS>
+template <Q4Rows HOW, bool PART>
 __device__ __forceinline__ void q4_put8(__nv_bfloat16* base, int at, const float (&v)[8], int n) {
   uint32_t y[4];
 #pragma unroll
@@ -252,29 +254,32 @@ __device__ __forceinline__ void q4_put8(__nv_bfloat16* base, int at, const float
     const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
     y[i] = *reinterpret_cast<const uint32_t*>(&h);
   }
-  if constexpr (VECTORS) {
+  if constexpr (HOW == Q4_VECTORS) {
     *reinterpret_cast<uint4*>(base + at) = make_uint4(y[0], y[1], y[2], y[3]);
-    return;
-  }
-  if ((at & 1) == 0) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(base + at);
+  } else if constexpr (HOW == Q4_WORDS) {      // (rows of even length: n is even)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (2 * i + 1 < n) w[i] = y[i];
-    if (n < 8 && (n & 1)) base[at + n - 1] = __float2bfloat16_rn(n == 1 ? v[0] : n == 3 ? v[2] : n == 5 ? v[4] : v[6]);
-  } else {                       // (rows of odd length) from a half word on
+      if (!PART || 2 * i < n) *reinterpret_cast<uint32_t*>(base + at + 2 * i) = y[i];
+  } else if constexpr (PART) {
     unsigned short* u = reinterpret_cast<unsigned short*>(base) + at;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (2 * i < n) u[2 * i] = (unsigned short)y[i];
-      if (2 * i + 1 < n) u[2 * i + 1] = (unsigned short)(y[i] >> 16);
-    }
+    for (int i = 0; i < 8; ++i)
+      if (i < n) u[i] = (unsigned short)(y[i >> 1] >> (16 * (i & 1)));
+  } else {      // rows of odd length may start on a half word: three whole words and two halves, the same stores for either start
+    const bool odd = at & 1;
+    uint32_t* w = reinterpret_cast<uint32_t*>(base + at + odd);
+    unsigned short* u = reinterpret_cast<unsigned short*>(base) + at;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) w[i] = odd ? __funnelshift_r(y[i], y[i + 1], 16) : y[i];
+    u[odd ? 0 : 6] = (unsigned short)(odd ? y[0] : y[3]);
+    u[7] = (unsigned short)(y[3] >> 16);
   }
 }
 // The numbers of a word: a code in bits 4 i .. (i = 1 .. 4) under the exponent of 2^23 is 2^23 + c 16^i; less 2^23 + 7.5 16^i it
 // is (c - 7.5) 16^i exactly, and the step takes the 16^-i along (exactly too: 2^-126 - 7 - 16 is the last bit there is): one
 // mask, one addition, one fused multiply-add a number.  Codes 0 and 5 to 7 come into place by a shift.
-template <typename T, bool VECTORS>
+// All words of a row but the last go without tests (with them the odd rows of 115 took 643 instructions for 8, 74 us for 700,000).
+template <typename T, Q4Rows HOW>
 __device__ __forceinline__ void dequantize_chunk(const uint32_t* in, T* out, int rows, int W) {
   const int nw = q4_row_words(W), q = threadIdx.x & 3;
   uint32_t base;                 // 0x4b000000 in a register: mask and exponent in one instruction
@@ -292,17 +297,20 @@ __device__ __forceinline__ void dequantize_chunk(const uint32_t* in, T* out, int
       const float one = (float)(1u << (4 * i));
       return fmaf(s[i], __uint_as_float(bits) - (8388608.f + 7.5f * one), z);
     };
-#pragma unroll 4
-    for (int e0 = 8 * q; e0 < W; e0 += 32) {
+    auto eight = [&](int e0, auto part) {
       const uint32_t word = in[row * nw + (e0 >> 3)], up = word << 4, down = word >> 8;
       const float v[8] = {number(up, 1), number(word, 1), number(word, 2), number(word, 3), number(word, 4), number(down, 3),
                           number(down, 4), number(word >> 12, 4)};
-      q4_put8<VECTORS>(out, row * W + e0, v, W - e0);
-    }
+      q4_put8<HOW, decltype(part)::value>(out, row * W + e0, v, W - e0);
+    };
+    int e0 = 8 * q;
+#pragma unroll 4
+    for (; e0 + 8 <= W; e0 += 32) eight(e0, std::false_type{});
+    if (HOW != Q4_VECTORS && e0 < W) eight(e0, std::true_type{});
   }
 }
 
-template <typename T, bool VECTORS>
+template <typename T, Q4Rows HOW>
 __global__ void __launch_bounds__(Q4R_THREADS) dequantize_rows_q4_kernel(const uint32_t* __restrict__ src, T* __restrict__ dst,
                                                                  long long n_rows, int W, int R, int32_t* __restrict__ status) {
   extern __shared__ __align__(128) unsigned char q4_rows_smem[];
@@ -310,11 +318,11 @@ __global__ void __launch_bounds__(Q4R_THREADS) dequantize_rows_q4_kernel(const u
   auto chunk = [&](long long c) {
     const int rows = (int)min((long long)R, n_rows - c * R);
     return Q4Chunk{reinterpret_cast<const unsigned char*>(src + c * R * nw), reinterpret_cast<unsigned char*>(dst + c * R * W),
-                   rows * nw * 4, rows * row_bytes, rows, W};
+                   rows * nw * 4, rows * row_bytes, rows, W, false};
   };
   q4_rows_pipeline(q4_rows_smem, q4_buffer(R * nw * 4), q4_buffer(R * row_bytes), (n_rows + R - 1) / R, status, chunk,
                    [&](const Q4Chunk& k, const unsigned char* in, unsigned char* to) {
-                     dequantize_chunk<T, VECTORS>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), k.rows, W);
+                     dequantize_chunk<T, HOW>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), k.rows, W);
                    });
 }
 
@@ -322,7 +330,7 @@ __global__ void __launch_bounds__(Q4R_THREADS) dequantize_rows_q4_kernel(const u
 // (K or V) x KV head x rows -- form one sequence (a grid over all positions spent 15 us on CTAs without rows in a batch of
 // unlike lengths); a CTA finds its chunks in the prefix of the sequences' chunk counts, which it makes first.
 constexpr int Q4R_SEQS = 1024;           // sequences per launch
-template <typename T, bool VECTORS>
+template <typename T, Q4Rows HOW_K, Q4Rows HOW_V>
 __global__ void __launch_bounds__(Q4R_THREADS)
 read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict__ v4, T* __restrict__ k, T* __restrict__ v,
                      const int32_t* __restrict__ seq_len, int B, int Hkv, int S_cap, int P2, int dv, int len_max, int R,
@@ -339,12 +347,13 @@ read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict
     const size_t row = ((size_t)b * Hkv + unit - (is_v ? Hkv : 0)) * S_cap + pos;
     const int W = is_v ? dv : P2, nw = q4_row_words(W);
     return Q4Chunk{reinterpret_cast<const unsigned char*>((is_v ? v4 : k4) + row * nw),
-                   reinterpret_cast<unsigned char*>((is_v ? v : k) + row * W), rows * nw * 4, rows * W * (int)sizeof(T), rows, W};
+                   reinterpret_cast<unsigned char*>((is_v ? v : k) + row * W), rows * nw * 4, rows * W * (int)sizeof(T), rows, W, is_v};
   };
   const int wide = max(P2, dv);
   q4_rows_pipeline(q4_rows_smem, q4_buffer(R * q4_row_words(wide) * 4), q4_buffer(R * wide * (int)sizeof(T)), plan.T, status, chunk,
                    [&](const Q4Chunk& c, const unsigned char* in, unsigned char* to) {
-                     dequantize_chunk<T, VECTORS>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), c.rows, c.W);
+                     if (c.is_v) dequantize_chunk<T, HOW_V>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), c.rows, c.W);
+                     else dequantize_chunk<T, HOW_K>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), c.rows, c.W);
                    });
 }
 
@@ -652,8 +661,9 @@ static rap_status launch_dequantize(rap_ctx* ctx, long long n_rows, int W, const
   auto go = [&](auto kernel) {
     kernel<<<l.grid, Q4R_THREADS, l.smem, st>>>((const uint32_t*)src, (T*)dst, n_rows, W, l.R, ctx->d_status);
   };
-  if (W % 8 == 0) go(dequantize_rows_q4_kernel<T, true>);
-  else go(dequantize_rows_q4_kernel<T, false>);
+  if (W % 8 == 0) go(dequantize_rows_q4_kernel<T, Q4_VECTORS>);
+  else if (sizeof(T) == 2 && W % 2) go(dequantize_rows_q4_kernel<T, Q4_HALVES>);
+  else go(dequantize_rows_q4_kernel<T, Q4_WORDS>);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
@@ -674,8 +684,14 @@ static rap_status launch_read_cache(rap_ctx* ctx, int B, int Hkv, int S_cap, int
   auto go = [&](auto kernel) {
     kernel<<<l.grid, Q4R_THREADS, l.smem, st>>>(k4, v4, k, v, seq_len, B, Hkv, S_cap, P2, dv, len_max, l.R, ctx->d_status);
   };
-  if (P2 % 8 == 0 && dv % 8 == 0) go(read_cache_q4_kernel<T, true>);
-  else go(read_cache_q4_kernel<T, false>);
+  auto pick = [&](auto k_how) {      // (K rows are of even length)
+    constexpr Q4Rows HOW_K = decltype(k_how)::value;
+    if (dv % 8 == 0) go(read_cache_q4_kernel<T, HOW_K, Q4_VECTORS>);
+    else if (sizeof(T) == 2 && dv % 2) go(read_cache_q4_kernel<T, HOW_K, Q4_HALVES>);
+    else go(read_cache_q4_kernel<T, HOW_K, Q4_WORDS>);
+  };
+  if (P2 % 8 == 0) pick(std::integral_constant<Q4Rows, Q4_VECTORS>{});
+  else pick(std::integral_constant<Q4Rows, Q4_WORDS>{});
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;

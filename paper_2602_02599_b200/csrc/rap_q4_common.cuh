@@ -70,12 +70,41 @@ __device__ __forceinline__ uint32_t q4_code(float x, const Q4Row& q) {
   const float t = __fadd_rn(__fmul_rn(__fsub_rn(x, q.z), q.r), 7.5f);
   return q.bad ? 8u : __float_as_uint(__fadd_rn(t, 12582912.0f)) & 15u;
 }
+// two fp32 numbers in one instruction (each rounded as by itself): half the issue slots
+typedef unsigned long long q4_f2;
+__device__ __forceinline__ q4_f2 q4_two(float a, float b) {
+  q4_f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void q4_apart(q4_f2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ q4_f2 q4_add(q4_f2 a, q4_f2 b) {
+  q4_f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ q4_f2 q4_mul(q4_f2 a, q4_f2 b) {
+  q4_f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ q4_f2 q4_fma(q4_f2 a, q4_f2 b, q4_f2 c) {
+  q4_f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 // a word of eight codes: with 1.5 2^23 added a place is 0x4b400000 + code as an integer, and the eight sum up as digits
 __device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Row& q) {
   uint32_t word = 0u - 0x4b400000u * 0x11111111u;
+  const q4_f2 z = q4_two(-q.z, -q.z), r = q4_two(q.r, q.r), half = q4_two(7.5f, 7.5f), magic = q4_two(12582912.0f, 12582912.0f);
+  const q4_f2 one = q4_two(1.f, 1.f);      // (a sum behind a product of this width is contracted into one rounding; a fused one is not)
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    word += __float_as_uint(__fadd_rn(__fadd_rn(__fmul_rn(__fsub_rn(x[i], q.z), q.r), 7.5f), 12582912.0f)) << (4 * i);
+  for (int i = 0; i < 8; i += 2) {
+    float a, b;
+    q4_apart(q4_add(q4_fma(q4_mul(q4_add(q4_two(x[i], x[i + 1]), z), r), one, half), magic), a, b);
+    word += __float_as_uint(a) << (4 * i);
+    word += __float_as_uint(b) << (4 * i + 4);
+  }
   return q.bad ? 0x88888888u : word;
 }
 __device__ __forceinline__ float q4_step(uint32_t sz) { return __uint_as_float(sz << 16); }
