@@ -19,10 +19,10 @@
 //     less) is cut at a point that moves by the golden section from block to block, so that equal weights far below the largest --
 //     100,000 of 2^-26 beside one of 1 -- are right in the sum (rounded to nearest they were off together, by a quarter).
 // A word of eight codes costs one mask on the K side and three byte permutes or masks on the V side, where fp16 operands cost
-// five and eight (measured on 32 heads, 8 KV heads, 32K rows, batch 32: 156 us against 167).
+// five and eight (measured on 32 heads, 8 KV heads, 32K rows, batch 32: 158 us against 167).
 //
 // Q4Half, five to eight heads: the whole-number form would need twice the accumulators, 96 registers for rows of 90; on six warps of
-// 168 registers it took 117 us for five heads over 4 sequences of up to 100K rows, this form 82.  fp16 in,
+// 168 registers it took 117 us for five heads over 4 sequences of up to 100K rows, this form 81.  fp16 in,
 // fp32 accumulate (m16n8k16):
 //   * A nibble under no exponent bits is an fp16 subnormal, so an operand register of two codes is one mask of a shifted word.
 //     Which code sits on which k-slot is free as long as both operands agree; on the K side the factors between the positions go
@@ -445,7 +445,8 @@ struct Q4Half {
   int gid, tq, lane;
   At at;
   uint32_t qa[NGK][2], qb[NGK][2];
-  float off[4], f_q[2], zq[2], m_ref[2], l_thr[2], z_thr[2], l_part[2], z_part[2];
+  float off[4], f_q[2], zq[2], m_ref[2], l_thr[2], z_thr[2];
+  q4_f2 l_part, z_part;        // sums of the last blocks, both heads
   float o[NT][4], dsum[4];     // columns 2 tq, 2 tq + 1 are this lane's heads
   uint32_t flip0, flip4, row_sign;
   bool have;
@@ -499,8 +500,9 @@ struct Q4Half {
       f_q[i] = __shfl_sync(0xffffffffu, f_c, 4 * (2 * tq + i));
       zq[i] = __shfl_sync(0xffffffffu, z_c, 4 * (2 * tq + i));
       m_ref[i] = -INFINITY;
-      l_thr[i] = z_thr[i] = l_part[i] = z_part[i] = 0.f;
+      l_thr[i] = z_thr[i] = 0.f;
     }
+    l_part = z_part = 0ull;
     flip0 = q4_keep(0x000f0000u);
     flip4 = q4_keep(0x00f00000u);
     row_sign = (gid & 1) ? 0x80000000u : 0u;      // rows 4 gid + t of odd gid are the second of their pair
@@ -526,12 +528,14 @@ struct Q4Half {
     }
   }
   __device__ __forceinline__ void settle() {
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      l_thr[g] += l_part[g];
-      z_thr[g] += z_part[g];
-      l_part[g] = z_part[g] = 0.f;
-    }
+    float a, b;
+    q4_apart(l_part, a, b);
+    l_thr[0] += a;
+    l_thr[1] += b;
+    q4_apart(z_part, a, b);
+    z_thr[0] += a;
+    z_thr[1] += b;
+    l_part = z_part = 0ull;
   }
   __device__ __forceinline__ void flush(float* sums) {
     total(sums);
@@ -575,14 +579,13 @@ struct Q4Half {
     for (int t = 0; t < 4; ++t) {
       const float ks = q4_step(r.ksz[t]), kz = q4_middle(r.ksz[t]);
       const float vs = __uint_as_float(r.vsz[t] * 65536u + row_sign);      // the step, negated on the second row of a pair
+      float x[2];                // (both heads in one instruction each)
+      q4_apart(q4_fma(q4_mul(q4_two(ks, ks), q4_two(f_q[0], f_q[1])), q4_two(r.s[t >> 1][2 * (t & 1)], r.s[t >> 1][2 * (t & 1) + 1]),
+                      q4_fma(q4_two(kz, kz), q4_two(zq[0], zq[1]), q4_two(-m_ref[0], -m_ref[1]))), x[0], x[1]);
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        float x = fmaf(ks * f_q[g], r.s[t >> 1][2 * (t & 1) + g], fmaf(kz, zq[g], -m_ref[g]));
-        if (4 * gid + t >= nrows) x = -INFINITY;
-        r.e[t][g] = q4_ex2(x);
-        r.w[t][g] = r.e[t][g] * vs;
-        r.big = q4_max(r.big, fabsf(r.w[t][g]));
-      }
+      for (int g = 0; g < 2; ++g) r.e[t][g] = q4_ex2(4 * gid + t < nrows ? x[g] : -INFINITY);
+      q4_apart(q4_mul(q4_two(r.e[t][0], r.e[t][1]), q4_two(vs, vs)), r.w[t][0], r.w[t][1]);
+      r.big = q4_max3(r.big, fabsf(r.w[t][0]), fabsf(r.w[t][1]));
     }
   }
   // raise the references so that the block's largest weight (its step included) becomes 2^9 .. 2^10
@@ -631,14 +634,13 @@ struct Q4Half {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const float vz = q4_middle(r.vsz[t]);
+      const q4_f2 e = q4_two(r.e[t][0], r.e[t][1]);
+      l_part = q4_add(l_part, e);
+      z_part = q4_fma(e, q4_two(vz, vz), z_part);
       float top[2], rest[2];
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        l_part[g] += r.e[t][g];
-        z_part[g] = fmaf(r.e[t][g], vz, z_part[g]);
-        top[g] = __uint_as_float(__float_as_uint(r.w[t][g]) & 0xffff0000u);
-        rest[g] = r.w[t][g] - top[g];
-      }
+      for (int g = 0; g < 2; ++g) top[g] = __uint_as_float(__float_as_uint(r.w[t][g]) & 0xffff0000u);
+      q4_apart(q4_fma(q4_two(top[0], top[1]), q4_two(-1.f, -1.f), q4_two(r.w[t][0], r.w[t][1])), rest[0], rest[1]);
       pb[t] = q4_transpose(q4_pack(top[0], top[1]));
       pl[t] = q4_transpose(q4_pack(rest[0], rest[1]));
     }
