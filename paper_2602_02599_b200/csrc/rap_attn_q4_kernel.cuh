@@ -21,7 +21,7 @@ struct Q4Cfg {
   static_assert(KSW % 2 == 1 && VSW % 2 == 1 && KSW <= 17 && VSW <= 17, "rows of up to 128 codes");
   using Engine = std::conditional_t<GC == 1, Q4Whole<KSW, VSW>, Q4Half<KSW, VSW>>;
   // Warps per CTA, two CTAs to an SM: eight of 128 registers, or six of 168 where the whole-number form has four groups of sums to
-  // hold (with eight it spilled: 77 us for a batch of 16 with 16K rows of 128, with six 61).
+  // hold (with eight it spilled: 77 us for a batch of 16 with 16K rows of 128, with six 62).
   static constexpr int NW = GC == 1 && Engine::NGV == 4 ? 6 : 8;
   static constexpr int TILE = NW * Q4_BR;                             // rows per CTA tile
   static constexpr int CW = 32 * Engine::NGV;                         // channel slots of the reduction buffer

@@ -278,7 +278,9 @@ __device__ __forceinline__ void q4_put8(__nv_bfloat16* base, int at, const float
 // The numbers of a word: a code in bits 4 i .. (i = 1 .. 4) under the exponent of 2^23 is 2^23 + c 16^i; less 2^23 + 7.5 16^i it
 // is (c - 7.5) 16^i exactly, and the step takes the 16^-i along (exactly too: 2^-126 - 7 - 16 is the last bit there is): one
 // mask, one addition, one fused multiply-add a number.  Codes 0 and 5 to 7 come into place by a shift.
-// All words of a row but the last go without tests (with them the odd rows of 115 took 643 instructions for 8, 74 us for 700,000).
+// Rows that may start on a half word: all words but the last go without tests (with them 8 rows of 115 took 643 instructions, 700,000
+// 74 us; without 41).  Rows on words: the tests are few, and a separate last word would be a pass
+// more (read-back of 16 sequences of up to 8K rows of 90: 12.3 us against 14.2).
 template <typename T, Q4Rows HOW>
 __device__ __forceinline__ void dequantize_chunk(const uint32_t* in, T* out, int rows, int W) {
   const int nw = q4_row_words(W), q = threadIdx.x & 3;
@@ -304,9 +306,14 @@ __device__ __forceinline__ void dequantize_chunk(const uint32_t* in, T* out, int
       q4_put8<HOW, decltype(part)::value>(out, row * W + e0, v, W - e0);
     };
     int e0 = 8 * q;
+    if constexpr (HOW == Q4_WORDS) {
 #pragma unroll 4
-    for (; e0 + 8 <= W; e0 += 32) eight(e0, std::false_type{});
-    if (HOW != Q4_VECTORS && e0 < W) eight(e0, std::true_type{});
+      for (; e0 < W; e0 += 32) eight(e0, std::true_type{});
+    } else {
+#pragma unroll 4
+      for (; e0 + 8 <= W; e0 += 32) eight(e0, std::false_type{});
+      if (HOW == Q4_HALVES && e0 < W) eight(e0, std::true_type{});
+    }
   }
 }
 
