@@ -249,7 +249,11 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
  *                           those (rap_prefill_attn over a quantised prefix).  Rows from d_seq_len[b] on are neither read
  *                           nor written.  h_seq_len_max: the caller's bound on d_seq_len (<= S_cap).
  *   rap_qkv_rope_append_q4  rap_qkv_rope_append with the new K and V rows quantised straight from their fp32 values; q~
- *                           as in rap_qkv_rope_append.  The rows of one call name distinct (sequence, slot) pairs.
+ *                           as in rap_qkv_rope_append.  So that a K row's codes are defined to the bit by the projection's
+ *                           fp32 sums a, b of a pair, its rotation is a c - b s, a s + b c with c, s the cosine and sine
+ *                           of the fp64 angle rounded to fp32, and every product and sum rounded to fp32 by itself
+ *                           (rap_qkv_rope_append's own K may be an fp32 place away before it is rounded to the storage
+ *                           dtype).  The rows of one call name distinct (sequence, slot) pairs.
  *   rap_decode_attn_q4      rap_decode_attn over quantised caches (Eq. 2 on the values above).  bf16 stacks with rows of up
  *                           to 128 numbers: q~ enters with 22 bits of its head's largest number (H_q / H_kv <= 4) or as fp16
  *                           pairs of that range, a row's weight with 19 bits or more of its own down to 2^-27 of the largest

@@ -686,6 +686,18 @@ def quantize_rows_q4(x):
     return c.astype(np.uint8), s.astype(np.float64) + nan, z.astype(np.float64) + nan
 
 
+def rotate_k_q4(y, pos, inv_freq):
+    """The K rows that the quantising append hands to quantize_rows_q4, defined to the bit: cosine and sine of the fp64 angle
+    rounded to fp32, then a c - b s and a s + b c with every product and sum rounded to fp32.
+    y fp32 [T, H_kv, 2P] (projected, pairs interleaved), pos [T], inv_freq fp64 [H_kv, P] -> fp32 [T, H_kv, 2P]."""
+    f = np.float32
+    y = np.asarray(y, dtype=f)
+    ang = np.asarray(pos, dtype=np.float64)[:, None, None] * np.asarray(inv_freq, dtype=np.float64)
+    c, s = np.cos(ang).astype(f), np.sin(ang).astype(f)
+    a, b = y[..., 0::2], y[..., 1::2]
+    return np.stack([a * c - b * s, a * s + b * c], axis=-1).reshape(y.shape)
+
+
 def dequantize_rows_q4(codes, steps, middles):
     """x_i = z + s (c_i - 7.5), fp64."""
     c = np.asarray(codes, dtype=np.float64) - 7.5

@@ -365,26 +365,48 @@ read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict
 }
 
 // RoPE / append epilogue with quantisation.  One CTA per (row t, KV head h), one warp per item: the G query heads of h
-// (rotated, rounded to the storage dtype, written to q_out as in the unquantised path), its key head (rotated in fp32,
-// quantised, appended) and its value head (quantised, appended).  All of them rotate by the same angles, so the sines and
-// cosines -- fp64 angle and reduction -- are taken once per CTA (one warp per item on its own: 34 us for 512 rows of the
-// 8B-shaped layer, this: 10.6).  A lane owns KP pairs of neighbouring numbers, that is whole bytes of a quantised row; P <= 128
-// and d_v' <= 256, so KP <= 4.  y holds `ksplit` partial results, each [T][n_out].
+// (rotated, rounded to the storage dtype, written to q_out as in the unquantised path), its key head (rotated, quantised,
+// appended) and its value head (quantised, appended).  All of them rotate by the same angles, so the sines and cosines are
+// taken once per CTA (one warp per item on its own: 34 us for 512 rows of the 8B-shaped layer, this: 10.6).
+// A code is a step function of the rotated number, so an error of an fp32 place moves one now and then by a whole step, and the
+// rotation of the key head is fixed to the bit: sines and cosines of the fp64 angle in fp64, rounded to fp32, then products and
+// sums rounded one by one.  (With the query heads' fp32 sines two or three codes of 370,000 were another one.)  The fp64 pair costs
+// nothing where it is taken before the GEMM is awaited (512 rows, GEMM and read-backs included: 39.4 us with either sine, 43.4
+// with the fp64 pair behind the wait).
+// A lane owns KP pairs of neighbouring numbers, that is whole bytes of a quantised row; P <= 128 and d_v' <= 256, so KP <= 4.
+// y holds `ksplit` partial results, each [T][n_out].
 template <typename T, int KP, bool BIAS>
 __global__ void __launch_bounds__(32 * (RAP_MAX_GROUP + 2))
 rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restrict__ bias, const int32_t* __restrict__ seq_id,
                       const int32_t* __restrict__ pos, const int32_t* __restrict__ slot, const double* __restrict__ inv_freq,
                       T* __restrict__ q_out, uint32_t* __restrict__ k4, uint32_t* __restrict__ v4, int Trows, int Hq, int Hkv,
                       int P2, int dv, int half_dim, int B_cache, int S_cap, int32_t* __restrict__ status) {
-  // launched behind the GEMM with programmatic serialization: nothing above this line touches memory; the GEMM's results (and, through the GEMM, the end of the scan before it) are awaited here
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  __shared__ float2 turn[128];                                         // (cosine, sine) of every pair
+  __shared__ float2 turn[256];                   // (cosine, sine) of every pair: P for the query heads, P for the key head
   const int t = blockIdx.x, h = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int P = P2 >> 1, G = Hq / Hkv;
   const int n_out = (Hq + Hkv) * P2 + Hkv * dv;
   const int p = pos[t];
+  for (int c = threadIdx.x; c < 2 * P; c += blockDim.x) {
+    // fp64 angle and reduction to [-pi, pi] (off by 2^-50 at most); for the query heads fp32 sine and cosine of the reduced
+    // angle (as in the unquantised path)
+    const double ang = (double)p * inv_freq[h * half_dim + (c < P ? c : c - P)];
+    const double turns = rint(ang * 0.15915494309189535);
+    const double red = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, ang));
+    if (c < P) {
+      float sf, cf;
+      sincosf((float)red, &sf, &cf);
+      turn[c] = make_float2(cf, sf);
+    } else {
+      double sd, cd;
+      sincospi(red * 0.3183098861837907, &sd, &cd);      // (sincos itself has a branch for far angles: 72 bytes of stack)
+      turn[c] = make_float2((float)cd, (float)sd);
+    }
+  }
+  // launched behind the GEMM with programmatic serialization: the GEMM's results (and, through the GEMM, the end of the scan before
+  // it) are awaited here.  What is read above, positions and frequencies, no kernel of such a chain writes.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int sq = seq_id ? seq_id[t] : t;
   const int sl = slot ? slot[t] : p;
   const bool row_ok = (sq >= 0 && sq < B_cache && sl >= 0 && sl < S_cap);
@@ -422,25 +444,17 @@ rope_append_q4_kernel(const float* __restrict__ y, int ksplit, const T* __restri
       if (c + 1 < W) b[k] += q4_ld(bias + col0 + c + 1);
     }
   }
-  for (int c = threadIdx.x; c < P; c += blockDim.x) {
-    // fp64 angle and reduction to [-pi, pi], fp32 sine and cosine of the reduced angle (as in the unquantised path)
-    const double ang = (double)p * inv_freq[h * half_dim + c];
-    const double turns = rint(ang * 0.15915494309189535);
-    const double red = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, ang));
-    float sf, cf;
-    sincosf((float)red, &sf, &cf);
-    turn[c] = make_float2(cf, sf);
-  }
   __syncthreads();
   if (!is_v) {
 #pragma unroll
     for (int k = 0; k < KP; ++k) {
       const int i = lane + 32 * k;
       if (i < P) {
-        const float2 cs = turn[i];
+        const float2 cs = turn[is_q ? i : P + i];
         const float x0 = a[k], x1 = b[k];
-        a[k] = fmaf(-x1, cs.y, __fmul_rn(x0, cs.x));          // the same roundings as the unquantised kernels
-        b[k] = fmaf(x0, cs.y, __fmul_rn(x1, cs.x));
+        const float c0 = __fmul_rn(x0, cs.x), c1 = __fmul_rn(x1, cs.x);
+        a[k] = is_q ? fmaf(-x1, cs.y, c0) : __fsub_rn(c0, __fmul_rn(x1, cs.y));      // q~: the same roundings as the unquantised kernels
+        b[k] = is_q ? fmaf(x0, cs.y, c1) : __fadd_rn(__fmul_rn(x0, cs.y), c1);
       }
     }
   }

@@ -208,6 +208,39 @@ def test_append_bf16_holds_the_oracle_rows(name, T):
     st.close()
 
 
+@pytest.mark.parametrize("name,T,seed", [("8b", 4000, 1), ("8b", 4000, 2), ("sweep1.0", 2500, 3), ("8b", 30, 4), ("tiny", 600, 5)])
+def test_append_writes_the_codes_of_the_rotation_as_it_is_defined(name, T, seed):
+    """Every byte of the appended rows is the row quantiser's on O.rotate_k_q4 of the projection (V: on the projection).
+    Activations and weights lie on a coarse grid, so that the projection's sums -- multiples of 2^-12 below 2^8 -- are exact in
+    fp32 in any order, and far positions.  (The two sides' fp64 sines differ by an ulp or two, which moves an fp32 rounding
+    once in 2^26 numbers, and then a code once in a million: nothing in 6 million numbers.)"""
+    w = replace(synth.scaled_down(synth.CONFIGS[name], n_layers=1, batch=2, seq=16, hidden=256), seq=16)
+    S = (T // 2 + 24) // 8 * 8
+    st, tabs, _ = util.build_small_stack(w, *synth.draw_scores(w), s_cap=S, max_rows=T)
+    rng = np.random.default_rng(seed)
+    X = (np.round(rng.normal(0, 8, (T, w.hidden))) / 8).astype(np.float32)
+    Wq = (np.round(rng.normal(0, 0.02 * 512, (st.n_out(0), w.hidden))) / 512).astype(np.float32)
+    up = lambda a: torch.from_numpy(a).to(st.device)
+    seq_id = np.repeat(np.arange(2), (T + 1) // 2)[:T].astype(np.int32)
+    slot = (np.arange(T) - np.where(seq_id, (T + 1) // 2, 0)).astype(np.int32)
+    pos = (slot + np.where(seq_id, 91234, 3)).astype(np.int32)
+    k4, v4 = q4_util.caches(st, 0)
+    q = torch.empty((T, w.n_q_heads, 2 * w.n_pairs), dtype=st.dt, device=st.device)
+    st.ctx.rap_qkv_rope_append_q4(0, T, up(X).to(st.dt), up(Wq).to(st.dt), None, up(seq_id), up(pos), up(slot), int(slot.max()), st.inv_freq, q,
+                                  k4, v4, 2, S)
+    _ok(st)
+    H, P2, dv = w.n_kv_heads, 2 * w.n_pairs, w.n_vch
+    Y = X.astype(np.float64) @ Wq[w.n_q_heads * P2:].astype(np.float64).T
+    assert np.array_equal(Y, Y.astype(np.float32))
+    freq = st.inv_freq[0, :, : w.n_pairs].cpu().numpy()
+    K = O.rotate_k_q4(Y[:, : H * P2].reshape(T, H, P2), pos, freq)
+    V = Y[:, H * P2:].reshape(T, H, dv).astype(np.float32)
+    for packed, rows in ((k4, K), (v4, V)):
+        got = packed.cpu().numpy()[seq_id, :, slot]
+        assert np.array_equal(got, q4_util.pack(*O.quantize_rows_q4(rows)))
+    st.close()
+
+
 def test_append_skips_rows_out_of_range_and_reports_them():
     w = synth.scaled_down(synth.LLAMA_8B, n_layers=1, batch=2, seq=16, hidden=256)
     ks, vs = synth.draw_scores(w)

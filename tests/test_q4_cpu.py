@@ -93,6 +93,20 @@ def test_quantiser_round_trip_and_special_rows():
     assert np.isnan(O.quantize_rows_q4(np.array([[3.4e38, 3.4e38]]))[1])      # the middle is not a bf16 number
 
 
+def test_k_rotation_as_the_append_defines_it():
+    """Against complex arithmetic in fp64: three roundings to fp32 and that of the sine, each half a step of at most the pair's
+    length; positions far out; and a quarter turn is exact up to the cosine of the fp64 angle."""
+    rng = np.random.default_rng(3)
+    y = rng.normal(0, 2, (50, 2, 18)).astype(np.float32)
+    pos, freq = rng.integers(0, 10 ** 6, 50), 500000.0 ** (-rng.random((2, 9)))
+    z = (y[..., 0::2] + 1j * y[..., 1::2].astype(np.complex128)) * np.exp(1j * (pos[:, None, None] * freq))
+    got = O.rotate_k_q4(y, pos, freq)
+    off = np.abs(got[..., 0::2] + 1j * got[..., 1::2].astype(np.complex128) - z)
+    assert got.dtype == np.float32 and np.all(off <= 4 * 2.0 ** -24 * 2 * np.abs(z))
+    got = O.rotate_k_q4(np.array([[[3.0, -5.0]]]), [1], [[np.pi / 2]])
+    assert np.allclose(got, [5.0, 3.0], rtol=2.0 ** -22, atol=0)
+
+
 def test_attention_closed_forms():
     rng = np.random.default_rng(4)
     B, Hkv, G, cap, P2, dv, D = 2, 2, 2, 8, 6, 5, 8
