@@ -337,13 +337,14 @@ __global__ void __launch_bounds__(Q4R_THREADS) dequantize_rows_q4_kernel(const u
 // (K or V) x KV head x rows -- form one sequence (a grid over all positions spent 15 us on CTAs without rows in a batch of
 // unlike lengths); a CTA finds its chunks in the prefix of the sequences' chunk counts, which it makes first.
 constexpr int Q4R_SEQS = 1024;           // sequences per launch
+constexpr int Q4R_PLAN = ((Q4R_SEQS + 2) * 4 + 127) / 128 * 128;      // bytes of the prefix, in front of the barriers
 template <typename T, Q4Rows HOW_K, Q4Rows HOW_V>
 __global__ void __launch_bounds__(Q4R_THREADS)
 read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict__ v4, T* __restrict__ k, T* __restrict__ v,
                      const int32_t* __restrict__ seq_len, int B, int Hkv, int S_cap, int P2, int dv, int len_max, int R,
                      int32_t* __restrict__ status) {
   extern __shared__ __align__(128) unsigned char q4_rows_smem[];
-  __shared__ int pref[Q4R_SEQS + 2];
+  int* const pref = reinterpret_cast<int*>(q4_rows_smem);
   SkPlan plan;
   sk_plan_shared(seq_len, B, 2 * Hkv, 0, len_max, R, (int)gridDim.x, pref, Q4R_SEQS + 2, &plan);
   auto chunk = [&](long long c) {
@@ -357,7 +358,7 @@ read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict
                    reinterpret_cast<unsigned char*>((is_v ? v : k) + row * W), rows * nw * 4, rows * W * (int)sizeof(T), rows, W, is_v};
   };
   const int wide = max(P2, dv);
-  q4_rows_pipeline(q4_rows_smem, q4_buffer(R * q4_row_words(wide) * 4), q4_buffer(R * wide * (int)sizeof(T)), plan.T, status, chunk,
+  q4_rows_pipeline(q4_rows_smem + Q4R_PLAN, q4_buffer(R * q4_row_words(wide) * 4), q4_buffer(R * wide * (int)sizeof(T)), plan.T, status, chunk,
                    [&](const Q4Chunk& c, const unsigned char* in, unsigned char* to) {
                      if (c.is_v) dequantize_chunk<T, HOW_V>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), c.rows, c.W);
                      else dequantize_chunk<T, HOW_K>(reinterpret_cast<const uint32_t*>(in), reinterpret_cast<T*>(to), c.rows, c.W);
@@ -629,15 +630,19 @@ __global__ void attn_q4_combine_kernel(const float* __restrict__ ws, int n_split
 }  // namespace
 
 namespace {
-// rows per chunk, dynamic shared memory and CTAs of a launch over `chunks(R)` chunks
+// rows per chunk, shared memory (all of it dynamic; `plan` bytes beside barriers and buffers) and CTAs of a launch over
+// `chunks(R)` chunks
 struct Q4RowsLaunch { int R, smem; unsigned grid; };
 template <typename Chunks>
-Q4RowsLaunch q4_rows_launch(rap_ctx* ctx, int W, int elem, Chunks chunks) {
+Q4RowsLaunch q4_rows_launch(rap_ctx* ctx, int W, int elem, int plan, Chunks chunks) {
   Q4RowsLaunch l;
+  auto bytes = [&](int R) { return plan + Q4R_HEAD + 2 * (q4_buffer(R * W * elem) + q4_buffer(R * 4 * q4_row_words(W))); };
   l.R = q4_rows_per_cta(W, elem);
+  // what a launch may take without asking for more (the plan beside 64 bf16 rows of 138 to 144 numbers is over it)
+  while (l.R > 8 && bytes(l.R) > 48 * 1024) l.R /= 2;
   while (l.R > 16 && chunks(l.R) < 2 * ctx->sm_count) l.R /= 2;      // small calls: shorter chunks on more SMs
-  l.smem = Q4R_HEAD + 2 * (q4_buffer(l.R * W * elem) + q4_buffer(l.R * 4 * q4_row_words(W)));      // under 48 KB by Q4R_STAGE
-  int fit = (220 * 1024) / (l.smem + 1024 + (Q4R_SEQS + 2) * 4);      // CTAs an SM holds, by shared memory and by threads
+  l.smem = bytes(l.R);
+  int fit = (220 * 1024) / (l.smem + 1024);      // CTAs an SM holds, by shared memory and by threads
   if (fit > 2048 / Q4R_THREADS) fit = 2048 / Q4R_THREADS;
   const long long n = chunks(l.R), most = (long long)fit * ctx->sm_count;
   l.grid = (unsigned)(n < most ? n : most);
@@ -647,7 +652,7 @@ Q4RowsLaunch q4_rows_launch(rap_ctx* ctx, int W, int elem, Chunks chunks) {
 
 template <typename T>
 static rap_status launch_quantize(rap_ctx* ctx, long long n_rows, int W, const void* src, void* dst, cudaStream_t st) {
-  const Q4RowsLaunch l = q4_rows_launch(ctx, W, (int)sizeof(T), [&](int R) { return (n_rows + R - 1) / R; });
+  const Q4RowsLaunch l = q4_rows_launch(ctx, W, (int)sizeof(T), 0, [&](int R) { return (n_rows + R - 1) / R; });
   auto go = [&](auto kernel) { kernel<<<l.grid, Q4R_THREADS, l.smem, st>>>((const T*)src, (uint32_t*)dst, n_rows, W, l.R, ctx->d_status); };
   auto pick = [&](auto how) {
     constexpr Q4Rows HOW = decltype(how)::value;
@@ -678,7 +683,7 @@ rap_status rap_launch_quantize_rows_q4(rap_ctx* ctx, int32_t dtype_in, long long
 
 template <typename T>
 static rap_status launch_dequantize(rap_ctx* ctx, long long n_rows, int W, const void* src, void* dst, cudaStream_t st) {
-  const Q4RowsLaunch l = q4_rows_launch(ctx, W, (int)sizeof(T), [&](int R) { return (n_rows + R - 1) / R; });
+  const Q4RowsLaunch l = q4_rows_launch(ctx, W, (int)sizeof(T), 0, [&](int R) { return (n_rows + R - 1) / R; });
   auto go = [&](auto kernel) {
     kernel<<<l.grid, Q4R_THREADS, l.smem, st>>>((const uint32_t*)src, (T*)dst, n_rows, W, l.R, ctx->d_status);
   };
@@ -699,7 +704,7 @@ rap_status rap_launch_dequantize_rows_q4(rap_ctx* ctx, int32_t dtype_out, long l
 template <typename T>
 static rap_status launch_read_cache(rap_ctx* ctx, int B, int Hkv, int S_cap, int P2, int dv, const uint32_t* k4, const uint32_t* v4,
                                     const int32_t* seq_len, int len_max, T* k, T* v, cudaStream_t st) {
-  const Q4RowsLaunch l = q4_rows_launch(ctx, P2 > dv ? P2 : dv, (int)sizeof(T),
+  const Q4RowsLaunch l = q4_rows_launch(ctx, P2 > dv ? P2 : dv, (int)sizeof(T), Q4R_PLAN,
                                         [&](int R) { return 2LL * B * Hkv * ((len_max + R - 1) / R); });
   if (2LL * B * Hkv * ((len_max + l.R - 1) / l.R) > 0x7fffffffLL) return RAP_ESHAPE;
   auto go = [&](auto kernel) {

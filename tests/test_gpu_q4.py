@@ -575,6 +575,32 @@ def test_read_cache_of_many_sequences():
     st.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_read_cache_at_every_width_of_long_calls(dtype):
+    """Rows of every width up to 256, K as wide as V or narrower, with enough rows for the longest chunks: whatever the width,
+    what a chunk takes of shared memory has to fit beside the plan."""
+    lens, S = [640, 639, 0, 300], 640
+    for W in list(range(57, 81)) + list(range(113, 257)) if dtype == "bf16" else list(range(33, 90)) + list(range(90, 257, 9)):
+        w = replace(_small(batch=4), head_dim=256, dtype=dtype, n_q_heads=8, n_kv_heads=8, n_pairs=W // 2 if W % 3 else 5, n_vch=W)
+        st = DecodeStack(w, s_cap=S)
+        st.build_tables(*synth.draw_scores(w))
+        g = torch.Generator(device=st.device).manual_seed(W)
+        used = (torch.arange(S, device=st.device)[None, :] < torch.tensor(lens, device=st.device)[:, None])[:, None, :, None]
+        held, want = q4_util.caches(st, 0), []
+        for packed, width, cache in zip(held, (2 * w.n_pairs, W), (st.k_cache[0], st.v_cache[0])):
+            x = torch.randn(packed.shape[:3] + (width,), generator=g, device=st.device)
+            st.ctx.rap_quantize_rows_q4(binding.RAP_F32, 4 * 8 * S, width, x, packed)
+            back = torch.empty(x.shape, dtype=st.dt, device=st.device)
+            st.ctx.rap_dequantize_rows_q4(_kind(dtype), 4 * 8 * S, width, packed, back)
+            cache.fill_(7.0)
+            want.append(torch.where(used, back, torch.full_like(back, 7.0)))
+        dl = torch.tensor(lens, dtype=torch.int32, device=st.device)
+        st.ctx.rap_read_cache_q4(0, 4, held[0], held[1], S, dl, S, st.k_cache[0], st.v_cache[0])
+        _ok(st)
+        assert torch.equal(st.k_cache[0], want[0]) and torch.equal(st.v_cache[0], want[1]), W
+        st.close()
+
+
 def test_two_contexts_on_two_streams():
     cases = [_attn_stack(_small(batch=3), [3000, 911, 64], seed=s) for s in (20, 21)]
     w = _small(batch=3)
