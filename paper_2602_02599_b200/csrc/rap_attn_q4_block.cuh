@@ -37,6 +37,10 @@
 //   * The reference makes the largest weight 2^9 .. 2^10 (fp16 ends 33 places below that), raised when one passes 2^15.
 // The middles are summed apart in fp32; a power of two in every weight drops out of the quotient.  Rows past the end get weight,
 // step and middle zero by selection (TAIL); their bytes may be anything.
+//
+// In both the reference is bounded by the sums of exponentials and of exponentials times middle too, not by the weights alone: rows
+// without a step (constant rows) weigh nothing, however far their logits lie above the reference.  A block in which a lane's sums pass
+// 2^104 raises it so that they fall below 2^102, which leaves 2^26 rows room in fp32.  (Costs 0.3% up to four heads, 2% from five on.)
 #pragma once
 #include <type_traits>
 
@@ -46,6 +50,8 @@
 namespace {
 
 constexpr int Q4_BR = 32;                // rows per warp block
+constexpr float Q4_SUM_MAX = 0x1p104f;   // of a lane's exponentials and of their products with the middles, in a block
+constexpr int Q4_SUM_TOP = 97;           // exponent that a raise leaves the largest of either
 
 __device__ __forceinline__ void q4_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -266,7 +272,8 @@ struct Q4Whole {
   __device__ __forceinline__ void flush(float*) { limit = 0.f; }      // (done by the next block: one copy of the code)
 
   struct Rows {                // of the lane's four rows
-    float s[4], e[4], w[4], big;                                      // 16 sum q (c - 7.5), weights, weights times V step, their maximum
+    float s[4], w[4], big;                                            // 16 sum q (c - 7.5), weights times V step, their maximum
+    float l, z;                                                       // sums of the weights, and with the middles
     uint32_t ksz[4], vsz[4];
   };
   template <bool TAIL>
@@ -316,15 +323,17 @@ struct Q4Whole {
     for (int t = 0; t < 4; ++t) {
       float x = fmaf(q4_step(r.ksz[t]) * f_q, r.s[t], fmaf(q4_middle(r.ksz[t]), zq, -m_ref[0]));
       if (4 * gid + t >= nrows) x = -INFINITY;
-      r.e[t] = q4_ex2(x);
-      r.w[t] = r.e[t] * q4_step(r.vsz[t]);
+      const float e = q4_ex2(x);
+      r.w[t] = e * q4_step(r.vsz[t]);
       r.big = q4_max(r.big, r.w[t]);
+      r.l = t ? r.l + e : e;
+      r.z = t ? fmaf(e, q4_middle(r.vsz[t]), r.z) : e * q4_middle(r.vsz[t]);
     }
   }
-  // raise the reference so that the block's largest weight (its step included) becomes 2^27 .. 2^28; what is summed so far moves
-  // to shared memory, scaled
+  // raise the reference so that the block's largest weight (its step included) becomes 2^27 .. 2^28, or as far as the sums ask
+  // for; what is summed so far moves to shared memory, scaled
   __device__ __forceinline__ void raise(Rows& r, int nrows, float* sums) {
-    float x[4], mx = -3e38f, most = 0.f;
+    float x[4], mx = -3e38f, most = 0.f, far = 0.f;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       x[t] = 4 * gid + t < nrows ? fmaf(q4_step(r.ksz[t]) * f_q, r.s[t], q4_middle(r.ksz[t]) * zq) : -INFINITY;
@@ -333,10 +342,18 @@ struct Q4Whole {
 #pragma unroll
     for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
 #pragma unroll
-    for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(r.vsz[t]));
+    for (int t = 0; t < 4; ++t) {
+      const float e = q4_ex2(x[t] - mx);
+      most = fmaxf(most, e * q4_step(r.vsz[t]));
+      far = fmaxf(far, e * fabsf(q4_middle(r.vsz[t])));
+    }
 #pragma unroll
-    for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-    const float m_new = fmaxf(m_ref[0], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 27, -100), 100) : 0.f));
+    for (int d = 4; d < 32; d <<= 1) {
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+      far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, d));
+    }
+    const int up = max(most > 0.f ? min(q4_exponent(most) - 27, 100) : 0, max(far > 0.f ? q4_exponent(far) : 0, 0) - Q4_SUM_TOP);
+    const float m_new = fmaxf(m_ref[0], mx + (float)up);
     const float alpha = q4_ex2(m_ref[0] - m_new);          // first block: 2^(-inf) = 0
     m_ref[0] = m_new;
     settle();
@@ -360,15 +377,14 @@ struct Q4Whole {
     Rows r;
     if (nrows >= Q4_BR) weigh<false>(sw, nrows, r);
     else weigh<true>(sw, nrows, r);
-    if (__any_sync(0xffffffffu, !(r.big < limit))) raise(r, nrows, sums);      // (a first block's reference is -inf)
+    // (a first block's reference is -inf)
+    if (__any_sync(0xffffffffu, !(r.big < limit) || !(r.l + fabsf(r.z) < Q4_SUM_MAX))) raise(r, nrows, sums);
     // ---- row sums; the weights' digits, turned into the B operand: k-slots 4 tq .. are rows 8 tq + t, 8 tq + 4 + t of t = 0, 1 (2, 3) ----
+    l_part += r.l;
+    z_part += r.z;
     uint32_t p[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      l_part += r.e[t];
-      z_part = fmaf(r.e[t], q4_middle(r.vsz[t]), z_part);
-      p[t] = q4_transpose(__float2uint_rz(r.w[t] + point));
-    }
+    for (int t = 0; t < 4; ++t) p[t] = q4_transpose(__float2uint_rz(r.w[t] + point));
     point += 0.618034f;
     if (point >= 1.f) point -= 1.f;
     const uint32_t e0 = __byte_perm(p[0], p[1], 0x6420), e1 = __byte_perm(p[2], p[3], 0x6420);
@@ -546,7 +562,8 @@ struct Q4Half {
   }
 
   struct Rows {                // of the lane's four rows, each for two heads
-    float s[2][4], e[4][2], w[4][2], big;
+    float s[2][4], w[4][2], big;
+    q4_f2 l, z;                // sums of the weights, and with the middles
     uint32_t ksz[4], vsz[4];
   };
   template <bool TAIL>
@@ -583,17 +600,28 @@ struct Q4Half {
       q4_apart(q4_fma(q4_mul(q4_two(ks, ks), q4_two(f_q[0], f_q[1])), q4_two(r.s[t >> 1][2 * (t & 1)], r.s[t >> 1][2 * (t & 1) + 1]),
                       q4_fma(q4_two(kz, kz), q4_two(zq[0], zq[1]), q4_two(-m_ref[0], -m_ref[1]))), x[0], x[1]);
 #pragma unroll
-      for (int g = 0; g < 2; ++g) r.e[t][g] = q4_ex2(4 * gid + t < nrows ? x[g] : -INFINITY);
-      q4_apart(q4_mul(q4_two(r.e[t][0], r.e[t][1]), q4_two(vs, vs)), r.w[t][0], r.w[t][1]);
+      for (int g = 0; g < 2; ++g) x[g] = q4_ex2(4 * gid + t < nrows ? x[g] : -INFINITY);
+      const q4_f2 e = q4_two(x[0], x[1]);
+      const float vz = q4_middle(r.vsz[t]);
+      q4_apart(q4_mul(e, q4_two(vs, vs)), r.w[t][0], r.w[t][1]);
       r.big = q4_max3(r.big, fabsf(r.w[t][0]), fabsf(r.w[t][1]));
+      r.l = t ? q4_add(r.l, e) : e;
+      r.z = t ? q4_fma(e, q4_two(vz, vz), r.z) : q4_mul(e, q4_two(vz, vz));
     }
   }
-  // raise the references so that the block's largest weight (its step included) becomes 2^9 .. 2^10
+  // of a lane's sums
+  __device__ __forceinline__ static float sum_size(const Rows& r) {
+    float a, b, c, d;
+    q4_apart(r.l, a, b);
+    q4_apart(r.z, c, d);
+    return (a + b) + (fabsf(c) + fabsf(d));
+  }
+  // raise the references so that the block's largest weight (its step included) becomes 2^9 .. 2^10, or as far as the sums ask for
   __device__ __forceinline__ void raise(Rows& r, int nrows, float* sums) {
     settle();
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      float x[4], mx = -3e38f, most = 0.f;
+      float x[4], mx = -3e38f, most = 0.f, far = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         x[t] = 4 * gid + t < nrows ? fmaf(q4_step(r.ksz[t]) * f_q[g], r.s[t >> 1][2 * (t & 1) + g], q4_middle(r.ksz[t]) * zq[g]) : -INFINITY;
@@ -602,10 +630,18 @@ struct Q4Half {
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
 #pragma unroll
-      for (int t = 0; t < 4; ++t) most = fmaxf(most, q4_ex2(x[t] - mx) * q4_step(r.vsz[t]));
+      for (int t = 0; t < 4; ++t) {
+        const float e = q4_ex2(x[t] - mx);
+        most = fmaxf(most, e * q4_step(r.vsz[t]));
+        far = fmaxf(far, e * fabsf(q4_middle(r.vsz[t])));
+      }
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-      const float m_new = fmaxf(m_ref[g], mx + (most > 0.f ? (float)min(max(q4_exponent(most) - 9, -80), 100) : 0.f));
+      for (int d = 4; d < 32; d <<= 1) {
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, d));
+      }
+      const int up = max(most > 0.f ? min(max(q4_exponent(most) - 9, -80), 100) : 0, max(far > 0.f ? q4_exponent(far) : 0, 0) - Q4_SUM_TOP);
+      const float m_new = fmaxf(m_ref[g], mx + (float)up);
       const float alpha = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
       m_ref[g] = m_new;
       l_thr[g] *= alpha;
@@ -628,15 +664,14 @@ struct Q4Half {
     Rows r;
     if (nrows >= Q4_BR) weigh<false>(sw, nrows, r);
     else weigh<true>(sw, nrows, r);
-    if (__any_sync(0xffffffffu, !(r.big <= WEIGHT_MAX))) raise(r, nrows, sums);      // (a first block's references are -inf)
+    // (a first block's references are -inf)
+    if (__any_sync(0xffffffffu, !(r.big <= WEIGHT_MAX) || !(sum_size(r) < Q4_SUM_MAX))) raise(r, nrows, sums);
     // ---- row sums; the weights as fp16 pairs, turned into the B operand ----
+    l_part = q4_add(l_part, r.l);
+    z_part = q4_add(z_part, r.z);
     uint32_t pb[4], pl[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const float vz = q4_middle(r.vsz[t]);
-      const q4_f2 e = q4_two(r.e[t][0], r.e[t][1]);
-      l_part = q4_add(l_part, e);
-      z_part = q4_fma(e, q4_two(vz, vz), z_part);
       float top[2], rest[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) top[g] = __uint_as_float(__float_as_uint(r.w[t][g]) & 0xffff0000u);

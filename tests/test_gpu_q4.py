@@ -359,6 +359,40 @@ def test_attention_v_of_any_magnitude(scale):
     st.close()
 
 
+@pytest.mark.parametrize("G", [1, 4, 5, 8])
+@pytest.mark.parametrize("middle", [0.0, 0.75, -3e30])
+def test_attention_logits_that_rise_over_v_rows_without_a_step(G, middle):
+    """Constant V rows have no step, so their weights never come near a limit of weight times step: a logit far above those of the
+    blocks before must still raise the reference, or the row sums leave fp32.  40 of 1000 rows lie `bits` binary places above the
+    others; with d_v' = 1 all rows are constant.  (Where the 40 are zero rows the others, 2^-60 of them and less, make the output:
+    a weight is right to 2^-27 of the largest.)"""
+    n = 1000
+    for dv, bits in ((48, 60), (48, 100), (48, 124), (48, 127.9), (48, 300), (1, 60), (1, 124), (1, 400)):
+        w = _small(n_pairs=16, n_vch=dv, n_q_heads=G, n_kv_heads=1)
+        st = DecodeStack(w, s_cap=n, alloc_cache=False)
+        st.build_tables(*synth.draw_scores(w))
+        rng = np.random.default_rng(dv)
+        k_codes, v_codes = np.zeros((1, 1, n, 32), dtype=np.uint8), rng.integers(0, 16, (1, 1, n, dv)).astype(np.uint8)
+        k_codes[:, :, 600:640, 0] = 15
+        one = np.ones((1, 1, n))
+        v_step, v_mid = 0.25 * one, O.round_bf16(rng.normal(0, 1, (1, 1, n)))
+        if dv == 1:
+            v_step[:] = 0.0
+        v_step[:, :, 600:640], v_mid[:, :, 600:640] = 0.0, O.round_bf16(middle * (1 + 0.5 * rng.random(40)))
+        held = [(k_codes, one, 0 * one), (v_codes, v_step, v_mid)]
+        k4, v4 = (torch.from_numpy(q4_util.pack(*h)).to(st.device) for h in held)
+        q = torch.zeros((1, G, 32), dtype=st.dt, device=st.device)
+        q[:, :, 0] = bits * float(np.sqrt(w.head_dim) * np.log(2)) / 15
+        for n_split in (0, 1, 3):
+            out = _run_attn(st, w, q, k4, v4, torch.tensor([n], dtype=torch.int32, device=st.device), n_split)
+            _ok(st)
+            assert torch.isfinite(out).all(), (dv, bits, n_split)
+            want = O.decode_attn_q4(util.to_np64(q), held[0], held[1], [n], w.head_dim)
+            tol = q4_util.attn_bound(util.to_np64(q), held[0], held[1], [n], w.head_dim) + n * 2.0 ** -27 * 7.5 * 0.25
+            assert np.all(np.abs(util.to_np64(out) - want) <= tol), (dv, bits, n_split)
+        st.close()
+
+
 def test_attention_fp32_and_wide_heads():
     _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], seed=2)
     _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], 3, seed=3)
