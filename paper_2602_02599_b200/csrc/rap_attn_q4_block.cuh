@@ -41,6 +41,10 @@
 // In both the reference is bounded by the sums of exponentials and of exponentials times middle too, not by the weights alone: rows
 // without a step (constant rows) weigh nothing, however far their logits lie above the reference.  A block in which a lane's sums pass
 // 2^104 raises it so that they fall below 2^102, which leaves 2^26 rows room in fp32.  (Costs 0.3% up to four heads, 2% from five on.)
+// It only ever rises, so a block without a step sets it as low as those sums allow, 97 places below its largest logit: any block with
+// steps that counts beside it then finds its weights too large, not too small.  References are whole numbers, and scaling from one to
+// another is exact: two may lie 200 places apart where their rows count alike (zero rows beside V of 1e20).  For the same reason every
+// warp's sums are scaled before the merge so that its row sum lies in [1, 2).
 #pragma once
 #include <type_traits>
 
@@ -98,6 +102,30 @@ __device__ __forceinline__ uint32_t q4_transpose(uint32_t x) {      // an 8x8 ti
 }
 __device__ __forceinline__ float q4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
 __device__ __forceinline__ int q4_exponent(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
+// 2^d of a whole number d <= 0; 0 below 2^-149, for -inf and for a NaN
+__device__ __forceinline__ float q4_down(float d) {
+  return d >= -149.f ? __uint_as_float(d >= -126.f ? (uint32_t)((int)d + 127) << 23 : 1u << ((int)d + 149)) : 0.f;
+}
+// Scales a row sum and a middles' sum by 2^d; returns the factor for the sums of weights.  (Where 2^d is no fp32 number no sum of
+// weights counts any longer beside the new block's, but sums of exponentials may: in two factors.)
+__device__ __forceinline__ float q4_lower(float d, float& l, float& z) {
+  const float f = q4_down(d);
+  if (f == 0.f && d >= -252.f) {
+    const float rest = q4_down(d + 126.f);
+    l = l * 0x1p-126f * rest;
+    z = z * 0x1p-126f * rest;
+  } else {
+    l *= f;
+    z *= f;
+  }
+  return f;
+}
+// The reference that a raise asks for: mx the largest logit, most the largest 2^(x - floor(mx)) V step, far the same with |middle|;
+// the weight with the largest step becomes 2^want .. 2^(want + 1), if the sums leave room
+__device__ __forceinline__ float q4_reference(float mx, float most, float far, int want) {
+  const int room = (far > 0.f ? max(q4_exponent(far), 0) : 0) - Q4_SUM_TOP;
+  return floorf(mx) + (float)(most > 0.f ? max(min(q4_exponent(most) - want, 100), room) : room);
+}
 // two codes with the second row's complemented, (y ^ flip) & MASK with flip in a register: one instruction, where two
 // immediates would make two
 template <uint32_t MASK>
@@ -343,7 +371,7 @@ struct Q4Whole {
     for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const float e = q4_ex2(x[t] - mx);
+      const float e = q4_ex2(x[t] - floorf(mx));
       most = fmaxf(most, e * q4_step(r.vsz[t]));
       far = fmaxf(far, e * fabsf(q4_middle(r.vsz[t])));
     }
@@ -352,13 +380,10 @@ struct Q4Whole {
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
       far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, d));
     }
-    const int up = max(most > 0.f ? min(q4_exponent(most) - 27, 100) : 0, max(far > 0.f ? q4_exponent(far) : 0, 0) - Q4_SUM_TOP);
-    const float m_new = fmaxf(m_ref[0], mx + (float)up);
-    const float alpha = q4_ex2(m_ref[0] - m_new);          // first block: 2^(-inf) = 0
+    const float m_old = m_ref[0], m_new = fmaxf(m_old, q4_reference(mx, most, far, 27));
     m_ref[0] = m_new;
     settle();
-    l_thr[0] *= alpha;
-    z_thr[0] *= alpha;
+    const float alpha = q4_lower(m_old - m_new, l_thr[0], z_thr[0]);      // first block: 2^(-inf) = 0
     if (dirty) {
       float v[NGV][4];
       total(sums, v);
@@ -631,7 +656,7 @@ struct Q4Half {
       for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const float e = q4_ex2(x[t] - mx);
+        const float e = q4_ex2(x[t] - floorf(mx));
         most = fmaxf(most, e * q4_step(r.vsz[t]));
         far = fmaxf(far, e * fabsf(q4_middle(r.vsz[t])));
       }
@@ -640,12 +665,9 @@ struct Q4Half {
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
         far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, d));
       }
-      const int up = max(most > 0.f ? min(max(q4_exponent(most) - 9, -80), 100) : 0, max(far > 0.f ? q4_exponent(far) : 0, 0) - Q4_SUM_TOP);
-      const float m_new = fmaxf(m_ref[g], mx + (float)up);
-      const float alpha = q4_ex2(m_ref[g] - m_new);          // first block: 2^(-inf) = 0
+      const float m_old = m_ref[g], m_new = fmaxf(m_old, q4_reference(mx, most, far, 9));
       m_ref[g] = m_new;
-      l_thr[g] *= alpha;
-      z_thr[g] *= alpha;
+      const float alpha = q4_lower(m_old - m_new, l_thr[g], z_thr[g]);      // first block: 2^(-inf) = 0
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         o[t][g] *= alpha;

@@ -360,6 +360,15 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
         eng.l_thr[g] += __shfl_xor_sync(0xffffffffu, eng.l_thr[g], d);
         eng.z_thr[g] += __shfl_xor_sync(0xffffffffu, eng.z_thr[g], d);
       }
+    // row sums to [1, 2), and the references with them (whole numbers below 2^23: exact; logits beyond that are not right to a
+    // place anyway and keep their reference): what a warp weighs in the merge is then in its reference alone
+    float norm[GC];
+#pragma unroll
+    for (int g = 0; g < GC; ++g) {
+      const int k = fabsf(eng.m_ref[g]) < 0x1p22f ? min(max(q4_exponent(eng.l_thr[g]), -126), 126) : 0;
+      norm[g] = q4_pow2(-k);
+      eng.m_ref[g] += (float)k;
+    }
     if (timed_out && lane == 0) *s_flag = 1;
     if (gid == 0) {
 #pragma unroll
@@ -387,7 +396,8 @@ __global__ void __launch_bounds__(Q4Cfg<KSW, VSW, GC>::NW * 32, 2) attn_q4_kerne
       float m_all = -INFINITY;
 #pragma unroll
       for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, m_s[w * 8 + head]);
-      const float f = eng.m_ref[g] == -INFINITY ? 0.f : q4_ex2(eng.m_ref[g] - m_all);   // a warp without a block contributes nothing
+      const float d = eng.m_ref[g] - m_all;      // -inf or NaN: a warp without a block contributes nothing
+      const float f = d >= -126.f ? norm[g] * q4_pow2((int)d) : 0.f;
       if (gid == 0) l_s[warp * 8 + head] = eng.l_thr[g] * f;
       if (head < G) eng.put(my_main + head * CW, g, f);
     }

@@ -393,6 +393,37 @@ def test_attention_logits_that_rise_over_v_rows_without_a_step(G, middle):
         st.close()
 
 
+@pytest.mark.parametrize("G", [1, 4, 5, 8])
+@pytest.mark.parametrize("scale", [1.0, 1e-6, 1e20, 1e30])
+@pytest.mark.parametrize("gain", [0.0, 1.0])
+def test_attention_over_blocks_of_constant_v_rows(G, scale, gain):
+    """Rows without a V step, or with next to none, at the front or in the middle -- zeroed slots, zero rows, constant rows, noise --
+    say nothing about the weights that the rows behind them need; and they count in the row sums however far apart the steps lie."""
+    lens = [2000, 700]
+    w = _small(batch=2, n_q_heads=2 * G, n_kv_heads=2)
+    st, q, k4, v4, dl = _attn_stack(w, lens, seed=14, gain=gain)
+    g = torch.Generator(device=st.device).manual_seed(G)
+    x = torch.randn((2, 2, st.s_cap, w.n_vch), generator=g, device=st.device) * scale
+    st.ctx.rap_quantize_rows_q4(binding.RAP_F32, x.numel() // w.n_vch, w.n_vch, x, v4)
+    kept = v4.clone()
+    one = lambda step, middle: torch.from_numpy(q4_util.pack(np.arange(w.n_vch, dtype=np.uint8)[None] % 16, np.array([step]), O.round_bf16(np.array([middle])))).to(st.device)
+    constant, noise = one(0.0, 0.75 * scale), one(2.0 ** -90, 0.0)
+    for first, last in ((0, 32), (0, 256), (0, 512), (32, 64), (512, 768), (64, 1900), (0, 1999), (0, 2000)):
+        for row in (torch.zeros_like(constant), constant, noise):
+            v4.copy_(kept)
+            v4[:, :, first:last] = row
+            held = [q4_util.unpack(c, W) for c, W in ((k4, 2 * w.n_pairs), (v4, w.n_vch))]
+            for n_split in (0, 1):
+                out = _run_attn(st, w, q, k4, v4, dl, n_split)
+                _ok(st)
+                want = np.concatenate([O.decode_attn_q4(util.to_np64(q)[b:b + 1], *(tuple(a[b:b + 1] for a in h) for h in held), [n], w.head_dim)
+                                       for b, n in enumerate(lens)])
+                # (steps as small as the noise's: a row's weight is cut at 2^-97 of the largest exponential)
+                tol = q4_util.attn_bound(util.to_np64(q), held[0], held[1], lens, w.head_dim) + max(lens) * 7.5 * 2.0 ** -97
+                assert np.all(np.abs(util.to_np64(out) - want) <= tol), (first, last, n_split)
+    st.close()
+
+
 def test_attention_fp32_and_wide_heads():
     _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], seed=2)
     _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], 3, seed=3)
