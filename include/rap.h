@@ -380,7 +380,9 @@ rap_status rap_lowrank_decode_attn(rap_ctx* ctx, int32_t B, int32_t r, int32_t d
 
 /* Reads (and clears) the device status word after synchronizing `stream`.  code is a
  * rap_status (RAP_OK, RAP_ECAPACITY for a skipped out-of-range row, RAP_ETIMEOUT for a bounded
- * wait that gave up); detail identifies the row / stage. */
+ * wait that gave up); detail identifies the row / stage.  After RAP_ETIMEOUT the units (sequence, KV head) that the launch
+ * was at have no result; later calls are right again.  Replays of a captured graph that holds the launch are so only after
+ * this call, which also clears the counters that the launch left behind. */
 rap_status rap_get_last_device_status(rap_ctx* ctx, int32_t* code, int32_t* detail, void* stream);
 
 #ifdef __cplusplus

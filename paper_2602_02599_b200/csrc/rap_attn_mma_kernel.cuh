@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(MmaCfg<G, WK, DV>::THREADS, 2) attn_mma_kernel
     pdl_wait();
     pdl_launch_dependents();
     if (blockIdx.x == 0) {   // sequences without any row are scanned by nobody: their output is zero
-      for (int i = tid; i < p.B * p.Hkv; i += THREADS) p.unit_cnt_other[i] = 0;   // counters a launch that gave up left behind
+      for (int i = tid; i < p.other_units; i += THREADS) p.unit_cnt_other[i] = 0;   // counters a launch that gave up left behind
       if (tid == 0) *p.dyn_next_other = 0;                                        // and the piece counter of the previous launch
       for (int bb = 0; bb < p.B; ++bb) {
         const bool empty = shared_plan ? pref[bb] == (bb > 0 ? pref[bb - 1] : 0)

@@ -84,6 +84,8 @@ rap_scan_params rap_fill_scan_params(rap_ctx* ctx, const rap_attn_args& a, int n
   {   // two counter sets take turns; each launch clears the one its predecessor used
     const size_t n_units = (size_t)ctx->desc.max_batch * ctx->desc.n_kv_heads;
     const uint32_t set = balanced ? (ctx->scan_epoch++ & 1u) : 0u;
+    if (balanced && a.B * a.Hkv > ctx->scan_units) ctx->scan_units = a.B * a.Hkv;
+    p.other_units = ctx->scan_units;
     p.unit_cnt = ctx->d_unit_cnt + set * n_units;
     p.unit_cnt_other = ctx->d_unit_cnt + (set ^ 1u) * n_units;
     p.dyn_next = ctx->d_unit_cnt + 2 * n_units + set;

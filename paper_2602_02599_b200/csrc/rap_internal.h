@@ -29,6 +29,7 @@ struct rap_ctx {
   size_t attn_ws_bytes = 0;
   int32_t* d_unit_cnt = nullptr;  // [2][max_batch][H_kv] partial-arrival counters of the balanced scan (zero between calls)
   uint32_t scan_epoch = 0;        // balanced scans launched so far: picks the counter set
+  int scan_units = 0;             // most units (sequences x KV heads) a balanced scan has had so far: counters that may not be zero
   float* d_proj_ws = nullptr;     // fp32 projection results / split-K partials
   size_t proj_ws_bytes = 0;
   int32_t* d_proj_cnt = nullptr;  // fused projection: two sets of [row tiles][4] split-arrival counters (zero between calls)
@@ -121,6 +122,7 @@ struct rap_scan_params {
   float qscale;
   int32_t* unit_cnt;   // balanced mode: arrivals per (sequence, KV head) unit, zero between calls
   int32_t* unit_cnt_other;   // the set the previous launch used; cleared by this launch (two sets take turns)
+  int other_units;     // counters of it to clear: of the largest batch so far, not of this call's
   float* out;          // balanced mode: [B][Hq][DV], written by the CTA that completes a unit
   uint32_t wait_limit; // probes of a stage barrier before a warp gives up (RAP_ETIMEOUT)
   int dbg_skip_copy;   // test hook: the first warp of the first CTA arms its first stage and issues no copy for it

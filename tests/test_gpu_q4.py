@@ -704,6 +704,44 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_launch_is_right():
     st.close()
 
 
+@pytest.mark.parametrize("scan", ["q4", "bf16"])
+def test_a_wait_that_runs_out_at_a_large_batch_then_a_small_one_then_the_large_one(scan):
+    """What a launch that gave up leaves in the arrival counters of units beyond a following smaller batch must not reach the next
+    large one.  CTA 0, which gives up, has a part of the second sequence (the first is empty); others finish theirs.  The calls' q
+    differ, so that a unit merged from an older call's partials shows.  The status is read at the end (that clears the counters)."""
+    w = _small(batch=40, n_kv_heads=1, n_q_heads=4)
+    lens = [0] + [9000] * 39
+    if scan == "q4":
+        st, q, k, v, dl = _attn_stack(w, lens, seed=15)
+        call = st.ctx.rap_decode_attn_q4
+    else:
+        st, q, _k4, _v4, dl = _attn_stack(w, lens, seed=15)
+        g = torch.Generator(device=st.device).manual_seed(15)
+        k, v = (torch.randn((40, 1, st.s_cap, W), generator=g, device=st.device).to(st.dt) for W in (2 * w.n_pairs, w.n_vch))
+        call = st.ctx.rap_decode_attn
+
+    def run(x, B=40):
+        out = torch.full((B, w.n_q_heads, w.n_vch), float("nan"), dtype=torch.float32, device=st.device)
+        call(0, B, x, k, v, st.s_cap, dl, 9000, 0, out)
+        return out
+
+    qs = [q, q.flip(0).contiguous(), (q * 0.5).contiguous()]
+    want = [run(x) for x in qs]
+    _ok(st)
+    for first in (0, 1):                         # from either of the two sets of counters
+        if first:
+            run(q)
+        st.ctx.rap_debug_arm_wait_timeout()
+        gave_up = run(qs[0])
+        assert not run(q, 1).any()
+        for i in (1, 2, 0, 1, 2):
+            got = run(qs[i])
+            assert torch.equal(got, want[i]), i
+        assert torch.isnan(gave_up[1]).all() and torch.equal(gave_up[0], want[0][0])
+        assert st.ctx.rap_get_last_device_status()[0] == binding.RAP_ETIMEOUT
+    st.close()
+
+
 # ---- together ------------------------------------------------------------------------------------------------------------------
 
 
