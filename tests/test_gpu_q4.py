@@ -338,6 +338,35 @@ def test_attention_flat_and_peaked(gain):
     _attn_case(_small(batch=2), [1500, 40], seed=7, gain=gain)
 
 
+@pytest.mark.parametrize("G", [1, 4, 5, 8])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 20, 2.0 ** 100])
+def test_attention_one_row_left_of_many(G, size):
+    """A q far out of fp16's range (the K steps make up for it), and one row 40 binary places above the rest, another one for every
+    query head: the outputs are that row's V numbers, which a tolerance made of sum |q| could not tell.  The rest, 2000 rows of
+    2^-40, counts 2^-29; the row's own weight 2^-19 of its size for five heads and more (two fp16 numbers of it, the second rounded),
+    2^-27 for up to four; V numbers are off by that and three fp32 roundings."""
+    n, P = 2000, 16
+    w = _small(n_pairs=P, n_vch=90, n_q_heads=G, n_kv_heads=1)
+    st = DecodeStack(w, s_cap=n, alloc_cache=False)
+    st.build_tables(*synth.draw_scores(w))
+    rng = np.random.default_rng(G)
+    one = np.ones((1, 1, n))
+    rows = rng.permutation(n)[:G]
+    k_codes, v_codes = np.zeros((1, 1, n, 2 * P), dtype=np.uint8), rng.integers(0, 16, (1, 1, n, 90)).astype(np.uint8)
+    k_codes[0, 0, rows, np.arange(G)] = 15          # head g asks dimension g
+    held = [(k_codes, one / size, 0 * one), (v_codes, one, 0 * one)]
+    k4, v4 = (torch.from_numpy(q4_util.pack(*h)).to(st.device) for h in held)
+    q = torch.zeros((1, G, 2 * P), dtype=st.dt, device=st.device)
+    for g in range(G):
+        q[0, g, g] = 41 * float(np.sqrt(w.head_dim) * np.log(2)) / 15 * size
+    want = v_codes[0, 0, rows] - 7.5
+    for n_split in (0, 1, 5):
+        out = util.to_np64(_run_attn(st, w, q, k4, v4, torch.tensor([n], dtype=torch.int32, device=st.device), n_split))[0]
+        _ok(st)
+        assert np.all(np.abs(out - want) <= 7.5 * (2 * 2.0 ** -29 + (2.0 ** -19 if G > 4 else 2.0 ** -26) + 4 * 2.0 ** -24)), np.abs(out - want).max()
+    st.close()
+
+
 @pytest.mark.parametrize("shift", [50.0, -3.0])
 def test_attention_rows_off_centre(shift):
     _attn_case(_small(batch=2), [1100, 200], seed=8, shift=shift)
