@@ -243,7 +243,7 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
  * dense; q~ is not quantised.
  *   rap_quantize_rows_q4    d_rows [n_rows][W] (dtype_in = RAP_F32 or RAP_BF16) -> d_q4 [n_rows][row bytes]; also the way
  *                           to convert a layer's cache (n_rows = B * H_kv * S_cap).  RAP_ESHAPE if W > 256.
- *   rap_dequantize_rows_q4  the way back: d_q4 -> d_rows [n_rows][W], rounded once to dtype_out.
+ *   rap_dequantize_rows_q4  the way back: d_q4 -> d_rows [n_rows][W], the values above in fp32, then rounded to dtype_out.
  *   rap_read_cache_q4       rows [0, d_seq_len[b]) of every sequence of a layer's K and V cache -> compact caches in the
  *                           storage dtype (d_k_cache, d_v_cache as in rap_decode_attn, same S_cap), for calls that take
  *                           those (rap_prefill_attn over a quantised prefix).  Rows from d_seq_len[b] on are neither read
@@ -255,12 +255,18 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
  *                           (rap_qkv_rope_append's own K may be an fp32 place away before it is rounded to the storage
  *                           dtype).  The rows of one call name distinct (sequence, slot) pairs.
  *   rap_decode_attn_q4      rap_decode_attn over quantised caches (Eq. 2 on the values above).  bf16 stacks with rows of up
- *                           to 128 numbers: q~ enters with 22 bits of its head's largest number (H_q / H_kv <= 4) or as fp16
- *                           pairs of that range, a row's weight with 19 bits or more of its own down to 2^-27 of the largest
- *                           (below, the mean over rows is kept); sums are exact or fp32.  V steps below about 2^-70 lose
- *                           digits (an absolute 2^-98 a row).  A NaN row makes the outputs of its KV head's query heads NaN,
- *                           a NaN or an infinity in q~ those of its own head (H_q / H_kv > 4: a q~ from 2^117 on as well).
- *                           Rows past a sequence's length may hold anything.
+ *                           to 128 numbers round q~ and the products of a row's weight and its V step, relative to the
+ *                           largest number of the head's q~ and to the largest such product among the rows that a warp has
+ *                           scanned so far; sums of both are exact (H_q / H_kv <= 4) or fp32, those of the weights and of
+ *                           weight times middle fp32.
+ *                             H_q / H_kv <= 4: q~ to multiples of 2^-21; products to multiples of 2^-27 or finer, cut at a
+ *                             point that moves from block to block, so that many small ones are right in their sum.
+ *                             H_q / H_kv > 4: q~ is exact down to 2^-25 and a multiple of 2^-32 below; products keep 19 bits
+ *                             down to 2^-15 and are rounded to a multiple of 2^-33 or finer below, equal ones alike.
+ *                           V steps below about 2^-70, and rows that weigh 2^-70 of one without a step or less, lose digits
+ *                           (products are cut at 2^-97 of the largest weight).  A NaN row makes the outputs of its KV head's
+ *                           query heads NaN, a NaN or an infinity in q~ those of its own head (H_q / H_kv > 4: a q~ from 2^117
+ *                           on as well).  Rows past a sequence's length may hold anything.
  *   rap_decode_step_q4      rap_decode_step over quantised caches (h_k4 / h_v4: HOST arrays of L device pointers).
  * Arguments, errors and stream behaviour as for the unquantised calls; RAP_EINVAL when the current device is not the
  * one the context was created on, and from the conversions when what they read and what they write overlap. */

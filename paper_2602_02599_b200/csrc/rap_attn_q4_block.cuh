@@ -22,7 +22,7 @@
 // five and eight (measured on 32 heads, 8 KV heads, 32K rows, batch 32: 158 us against 167).
 //
 // Q4Half, five to eight heads: the whole-number form would need twice the accumulators, 96 registers for rows of 90; on six warps of
-// 168 registers it took 117 us for five heads over 4 sequences of up to 100K rows, this form 81.  fp16 in,
+// 168 registers it took 117 us for five heads over 4 sequences of up to 100K rows, this form 84.  fp16 in,
 // fp32 accumulate (m16n8k16):
 //   * A nibble under no exponent bits is an fp16 subnormal, so an operand register of two codes is one mask of a shifted word.
 //     Which code sits on which k-slot is free as long as both operands agree; on the K side the factors between the positions go

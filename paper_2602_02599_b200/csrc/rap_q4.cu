@@ -368,12 +368,12 @@ read_cache_q4_kernel(const uint32_t* __restrict__ k4, const uint32_t* __restrict
 // RoPE / append epilogue with quantisation.  One CTA per (row t, KV head h), one warp per item: the G query heads of h
 // (rotated, rounded to the storage dtype, written to q_out as in the unquantised path), its key head (rotated, quantised,
 // appended) and its value head (quantised, appended).  All of them rotate by the same angles, so the sines and cosines are
-// taken once per CTA (one warp per item on its own: 34 us for 512 rows of the 8B-shaped layer, this: 10.6).
+// taken once per CTA (one warp per item on its own: 34 us for 512 rows of the 8B-shaped layer, this: 12.2).
 // A code is a step function of the rotated number, so an error of an fp32 place moves one now and then by a whole step, and the
 // rotation of the key head is fixed to the bit: sines and cosines of the fp64 angle in fp64, rounded to fp32, then products and
-// sums rounded one by one.  (With the query heads' fp32 sines two or three codes of 370,000 were another one.)  The fp64 pair costs
-// nothing where it is taken before the GEMM is awaited (512 rows, GEMM and read-backs included: 39.4 us with either sine, 43.4
-// with the fp64 pair behind the wait).
+// sums rounded one by one.  (With the query heads' fp32 sines two or three codes of 370,000 were another one.)  The fp64 pair is
+// taken before the GEMM is awaited: by itself the kernel takes 12.2 us for 512 rows where it took 10.6, behind the GEMM and with
+// the read-backs 39.4 either way (43.4 with the pair behind the wait).
 // A lane owns KP pairs of neighbouring numbers, that is whole bytes of a quantised row; P <= 128 and d_v' <= 256, so KP <= 4.
 // y holds `ksplit` partial results, each [T][n_out].
 template <typename T, int KP, bool BIAS>
