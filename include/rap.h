@@ -264,7 +264,9 @@ rap_status rap_decode_step_q8(rap_ctx* ctx, int32_t B, const void* d_x, const vo
  *                             H_q / H_kv > 4: q~ is exact down to 2^-25 and a multiple of 2^-32 below; products keep 19 bits
  *                             down to 2^-15 and are rounded to a multiple of 2^-33 or finer below, equal ones alike.
  *                           V steps below about 2^-70, and rows that weigh 2^-70 of one without a step or less, lose digits
- *                           (products are cut at 2^-97 of the largest weight).  A NaN row makes the outputs of its KV head's
+ *                           (products are cut at 2^-97 of the largest weight).  A row's exponential is taken in fp32 of its
+ *                           logit plus up to 29 - log2(V step), so it is off by up to 2^-19 of itself for steps of 2^-4 and
+ *                           more, 2^-17 for steps below 2^-36 or none (H_q / H_kv > 4: 2^-20, 2^-17).  A NaN row makes the outputs of its KV head's
  *                           query heads NaN, a NaN or an infinity in q~ those of its own head (H_q / H_kv > 4: a q~ from 2^117
  *                           on as well).  Rows past a sequence's length may hold anything.
  *   rap_decode_step_q4      rap_decode_step over quantised caches (h_k4 / h_v4: HOST arrays of L device pointers).

@@ -14,7 +14,7 @@
 //     The offset -7.5 sum q is the accumulators' initial value.  Every product and sum is exact.
 //   * outputs: sum p c from the masked bytes, sum p c' = (sum p b - sum p c) / 16.  A row's weight, its V step included, is a whole
 //     number of 32 bits whose four bytes are the digits: the register of a lane's weight is already the pair of 16-bit columns
-//     that the transpose wants.  The reference of the softmax makes the block's largest weight 2^27 .. 2^28 and is raised when
+//     that the transpose wants.  The reference of the softmax makes the block's largest weight 2^27 .. 2^29 and is raised when
 //     one passes 2^32.  Sums are exact, 7.5 sum p comes off in whole numbers too.  A weight's fraction (2^-27 of the largest, or
 //     less) is cut at a point that moves by the golden section from block to block, so that equal weights far below the largest --
 //     100,000 of 2^-26 beside one of 1 -- are right in the sum (rounded to nearest they were off together, by a quarter).
@@ -34,7 +34,7 @@
 //     every two rows that share an operand register the second enters with its codes complemented (15 - c, the same mask
 //     operation) and its weight negated (off by 3e-4 at 32K rows without it).  What is left is 7.5 times the sum of the signed
 //     weights, which one MMA against ones keeps along.  Every FLUSH blocks the accumulators move into fp32 sums in shared memory.
-//   * The reference makes the largest weight 2^9 .. 2^10 (fp16 ends 33 places below that), raised when one passes 2^15.
+//   * The reference makes the largest weight 2^9 .. 2^11 (fp16 ends 33 places below that), raised when one passes 2^15.
 // The middles are summed apart in fp32; a power of two in every weight drops out of the quotient.  Rows past the end get weight,
 // step and middle zero by selection (TAIL); their bytes may be anything.
 //
@@ -120,11 +120,12 @@ __device__ __forceinline__ float q4_lower(float d, float& l, float& z) {
   }
   return f;
 }
-// The reference that a raise asks for: mx the largest logit, most the largest 2^(x - floor(mx)) V step, far the same with |middle|;
-// the weight with the largest step becomes 2^want .. 2^(want + 1), if the sums leave room
-__device__ __forceinline__ float q4_reference(float mx, float most, float far, int want) {
-  const int room = (far > 0.f ? max(q4_exponent(far), 0) : 0) - Q4_SUM_TOP;
-  return floorf(mx) + (float)(most > 0.f ? max(min(q4_exponent(most) - want, 100), room) : room);
+// How far above a row's logit the reference has to lie, given the row's last word: so that the weight times the step stays below
+// 2^(want + 2), and the sums below Q4_SUM_TOP.  From the exponents alone, since the row may weigh nothing beside another one (its 2^x
+// relative to the largest underflows) and yet be the one whose step matters.  (A step or a middle of 0 counts as 2^-127.)
+__device__ __forceinline__ float q4_lift(uint32_t sz, int want) {
+  const int step = (int)((sz >> 7) & 255u) - 127, middle = (int)((sz >> 23) & 255u) - 127;
+  return (float)max(step - want, max(middle, 0) - Q4_SUM_TOP);
 }
 // two codes with the second row's complemented, (y ^ flip) & MASK with flip in a register: one instruction, where two
 // immediates would make two
@@ -358,29 +359,17 @@ struct Q4Whole {
       r.z = t ? fmaf(e, q4_middle(r.vsz[t]), r.z) : e * q4_middle(r.vsz[t]);
     }
   }
-  // raise the reference so that the block's largest weight (its step included) becomes 2^27 .. 2^28, or as far as the sums ask
+  // raise the reference so that the block's largest weight (its step included) becomes 2^27 .. 2^29, or as far as the sums ask
   // for; what is summed so far moves to shared memory, scaled
   __device__ __forceinline__ void raise(Rows& r, int nrows, float* sums) {
-    float x[4], mx = -3e38f, most = 0.f, far = 0.f;
+    float top = -3e38f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      x[t] = 4 * gid + t < nrows ? fmaf(q4_step(r.ksz[t]) * f_q, r.s[t], q4_middle(r.ksz[t]) * zq) : -INFINITY;
-      mx = fmaxf(mx, x[t]);
-    }
+    for (int t = 0; t < 4; ++t)
+      if (4 * gid + t < nrows)
+        top = fmaxf(top, fmaf(q4_step(r.ksz[t]) * f_q, r.s[t], q4_middle(r.ksz[t]) * zq) + q4_lift(r.vsz[t], 27));
 #pragma unroll
-    for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const float e = q4_ex2(x[t] - floorf(mx));
-      most = fmaxf(most, e * q4_step(r.vsz[t]));
-      far = fmaxf(far, e * fabsf(q4_middle(r.vsz[t])));
-    }
-#pragma unroll
-    for (int d = 4; d < 32; d <<= 1) {
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-      far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, d));
-    }
-    const float m_old = m_ref[0], m_new = fmaxf(m_old, q4_reference(mx, most, far, 27));
+    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    const float m_old = m_ref[0], m_new = fmaxf(m_old, floorf(top));
     m_ref[0] = m_new;
     settle();
     const float alpha = q4_lower(m_old - m_new, l_thr[0], z_thr[0]);      // first block: 2^(-inf) = 0
@@ -641,31 +630,19 @@ struct Q4Half {
     q4_apart(r.z, c, d);
     return (a + b) + (fabsf(c) + fabsf(d));
   }
-  // raise the references so that the block's largest weight (its step included) becomes 2^9 .. 2^10, or as far as the sums ask for
+  // raise the references so that the block's largest weight (its step included) becomes 2^9 .. 2^11, or as far as the sums ask for
   __device__ __forceinline__ void raise(Rows& r, int nrows, float* sums) {
     settle();
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      float x[4], mx = -3e38f, most = 0.f, far = 0.f;
+      float top = -3e38f;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        x[t] = 4 * gid + t < nrows ? fmaf(q4_step(r.ksz[t]) * f_q[g], r.s[t >> 1][2 * (t & 1) + g], q4_middle(r.ksz[t]) * zq[g]) : -INFINITY;
-        mx = fmaxf(mx, x[t]);
-      }
+      for (int t = 0; t < 4; ++t)
+        if (4 * gid + t < nrows)
+          top = fmaxf(top, fmaf(q4_step(r.ksz[t]) * f_q[g], r.s[t >> 1][2 * (t & 1) + g], q4_middle(r.ksz[t]) * zq[g]) + q4_lift(r.vsz[t], 9));
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float e = q4_ex2(x[t] - floorf(mx));
-        most = fmaxf(most, e * q4_step(r.vsz[t]));
-        far = fmaxf(far, e * fabsf(q4_middle(r.vsz[t])));
-      }
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) {
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, d));
-      }
-      const float m_old = m_ref[g], m_new = fmaxf(m_old, q4_reference(mx, most, far, 9));
+      for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const float m_old = m_ref[g], m_new = fmaxf(m_old, floorf(top));
       m_ref[g] = m_new;
       const float alpha = q4_lower(m_old - m_new, l_thr[g], z_thr[g]);      // first block: 2^(-inf) = 0
 #pragma unroll

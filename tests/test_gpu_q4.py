@@ -453,6 +453,35 @@ def test_attention_over_blocks_of_constant_v_rows(G, scale, gain):
     st.close()
 
 
+@pytest.mark.parametrize("G", [1, 4, 5, 8])
+@pytest.mark.parametrize("bits,step", [(130, 2.0 ** 66), (130, 2.0 ** 120), (40, 2.0 ** 66), (180, 2.0 ** 100)])
+def test_attention_steps_that_count_far_below_the_largest_logit(G, bits, step):
+    """Zero rows with the largest logits and, in their block, rows `bits` binary places below with steps so large that their weight
+    times step counts (2^-130 relative to the largest is no fp32 number): they make the output, or nearly nothing of it."""
+    n = 96
+    w = _small(n_pairs=16, n_vch=48, n_q_heads=G, n_kv_heads=1)
+    st = DecodeStack(w, s_cap=n, alloc_cache=False)
+    st.build_tables(*synth.draw_scores(w))
+    rng = np.random.default_rng(7)
+    k_codes, v_codes = np.zeros((1, 1, n, 32), dtype=np.uint8), rng.integers(0, 16, (1, 1, n, 48)).astype(np.uint8)
+    k_codes[..., 0] = 15
+    low = np.arange(n) % 7 == 3
+    k_codes[:, :, low, 0] = 0
+    one = np.ones((1, 1, n))
+    held = [(k_codes, one, 0 * one), (v_codes, np.where(low, step, 0.0) * one, 0 * one)]
+    k4, v4 = (torch.from_numpy(q4_util.pack(*h)).to(st.device) for h in held)
+    q = torch.zeros((1, G, 32), dtype=st.dt, device=st.device)
+    q[:, :, 0] = bits * float(np.sqrt(w.head_dim) * np.log(2)) / 15
+    want = O.decode_attn_q4(util.to_np64(q), held[0], held[1], [n], w.head_dim)
+    # (a product of weight and step is cut at 2^-97 of the largest weight, a sum of weights at 2^-149)
+    tol = q4_util.attn_bound(util.to_np64(q), held[0], held[1], [n], w.head_dim) + n * 7.5 * 2.0 ** -97
+    for n_split in (0, 1):
+        out = util.to_np64(_run_attn(st, w, q, k4, v4, torch.tensor([n], dtype=torch.int32, device=st.device), n_split))
+        _ok(st)
+        assert np.all(np.abs(out - want) <= tol), (np.abs(out - want).max(), np.abs(want).max())
+    st.close()
+
+
 def test_attention_fp32_and_wide_heads():
     _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], seed=2)
     _attn_case(replace(synth.TINY, batch=2, seq=200), [200, 77], 3, seed=3)
