@@ -851,6 +851,57 @@ def test_decode_step_equals_the_separate_calls(name):
     st.close()
 
 
+@pytest.mark.parametrize("name", ["8b", "tiny"])
+def test_decode_steps_back_to_back_and_replayed(name):
+    """Six steps that advance the lengths, each waited for; the same six enqueued back to back; and one captured step replayed six
+    times: caches, lengths and the last outputs are equal bit for bit (a position read too early would be the step before's)."""
+    base = synth.CONFIGS[name]
+    w = replace(base, batch=3, seq=120) if name == "tiny" else synth.scaled_down(base, n_layers=3, batch=3, seq=120, hidden=512)
+    st, _, _ = util.build_small_stack(w, *synth.draw_scores(w), full_weights=False, max_rows=64)
+    L = w.n_layers
+    g = torch.Generator(device=st.device).manual_seed(5)
+    start = []
+    for l in range(L):
+        pair = q4_util.caches(st, l)
+        for packed, W in zip(pair, (2 * st.n_pairs[l], st.n_vch[l])):
+            x = torch.empty(packed.shape[:3] + (W,), device=st.device).normal_(0, 1, generator=g)
+            st.ctx.rap_quantize_rows_q4(binding.RAP_F32, x.numel() // W, W, x, packed)
+        start.append(pair)
+    lens = torch.tensor([120, 0, 57], dtype=torch.int32, device=st.device)
+    x = torch.empty((L, w.batch, w.hidden), device=st.device).normal_(0, 1, generator=g).to(st.dt)
+
+    def case():
+        return [p[0].clone() for p in start], [p[1].clone() for p in start], lens.clone(), torch.zeros_like(st.out)
+
+    def step(k4, v4, dl, out):
+        st.ctx.rap_decode_step_q4(w.batch, x, st.w_qkv, None, st.inv_freq, k4, v4, st.s_cap, dl, 126, 0, st.q_scratch, out, st.out_stride, 1)
+
+    ran = []
+    for wait in (True, False):
+        c = case()
+        torch.cuda.synchronize()
+        for _ in range(6):
+            step(*c)
+            if wait:
+                torch.cuda.synchronize()
+        _ok(st)
+        ran.append(c)
+    c = case()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*c)
+    for _ in range(6):
+        graph.replay()
+    _ok(st)
+    ran.append(c)
+    assert torch.equal(ran[0][2], lens + 6)
+    for other in ran[1:]:
+        assert torch.equal(other[2], ran[0][2]) and torch.equal(other[3], ran[0][3])
+        assert all(torch.equal(a, b) for i in (0, 1) for a, b in zip(other[i], ran[0][i]))
+    del graph
+    st.close()
+
+
 def test_prompt_chunk_behind_a_quantised_prefix_then_decode():
     """As a server uses them: a prompt's first part appended in 4 bits, the rows read back, the second part attended over
     them by rap_prefill_attn, appended in 4 bits too, then a decode step of the attention over everything."""
