@@ -40,7 +40,8 @@
 //
 // In both the reference is bounded by the sums of exponentials and of exponentials times middle too, not by the weights alone: rows
 // without a step (constant rows) weigh nothing, however far their logits lie above the reference.  A block in which a lane's sums pass
-// 2^104 raises it so that they fall below 2^102, which leaves 2^26 rows room in fp32.  (Costs 0.3% up to four heads, 2% from five on.)
+// 2^104 raises it so that they fall below 2^103, which leaves 2^25 rows room in fp32.  (Up to four heads the bound costs nothing
+// that can be measured, from five on 3%: 82 us became 84.)
 // It only ever rises, so a block without a step sets it as low as those sums allow, 97 places below its largest logit: any block with
 // steps that counts beside it then finds its weights too large, not too small.  References are whole numbers, and scaling from one to
 // another is exact: two may lie 200 places apart where their rows count alike (zero rows beside V of 1e20).  For the same reason every
