@@ -335,6 +335,73 @@ rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, c
                             const void* d_v_cache, int32_t S_cap, const int32_t* d_start, int32_t h_start_max,
                             float* d_out, void* stream);
 
+/* ---- attention with a sliding window and sinks, over whole or rolling caches (the paper's layers attend to everything; models
+ * that alternate such layers with windowed ones keep the same compact rows) ------------------------------------------
+ * A query at position i sees the positions j <= i with j < n_sink (the first tokens stay visible) or j > i - window; the
+ * window counts the query's own position.  n_sink >= 0, window >= 1; a window of at least the longest length is plain causal
+ * attention.  Logits, scale and outputs as in rap_decode_attn; a query that sees nothing gives zeros.
+ * Caches are [B][H_kv][S_cap][W] as everywhere, and position p of a sequence lies in row
+ *     slot(p) = p                                              if p < n_sink
+ *               n_sink + (p - n_sink) mod (S_cap - n_sink)     otherwise,
+ * so a cache with S_cap >= the longest length holds position p in row p, and a shorter one is a rolling cache: the rows
+ * behind the sinks are used again and again, and lengths are not bounded by S_cap.  A rolling cache needs S_cap - n_sink
+ * >= window + new - 1, new being the most tokens that are appended before they attend (RAP_ECAPACITY where h_seq_len_max >
+ * S_cap and it is smaller).  n_sink < S_cap.
+ *
+ *   rap_build_slots          the rows of a ragged batch, from the request lengths, on the GPU: sequence b has d_seq_len[b]
+ *                            tokens cached and d_new_len[b] >= 0 new ones.  Rows are numbered sequence by sequence:
+ *                            d_row_start[b] (B + 1 of them, d_row_start[0] = 0) is b's first row, and row r of sequence b is
+ *                            its token p = d_seq_len[b] + (r - d_row_start[b]):
+ *                              d_seq_id[r] = b,  d_slot[r] = slot(p),  d_pos[r] = p + (d_pos_base ? d_pos_base[b] : 0),
+ *                              d_len_out[b] = d_seq_len[b] + d_new_len[b] (NULL: not wanted; d_seq_len itself: advanced in
+ *                            place) -- what rap_qkv_rope_append and rap_prefill_attn_window take.  d_pos_base (NULL: none):
+ *                            tokens ahead of the cache's first row, such as a shared prefix.  T: rows the outputs hold (NULL
+ *                            where there are none); rows from the sum of d_new_len on are left as they were.  The device status word reports, and the
+ *                            kernel survives: a negative length or a position beyond 2^31 - 1 (RAP_EINVAL; taken as 0, or the
+ *                            row is not written), a sum beyond T (RAP_ECAPACITY; the rows beyond T are not written), and a
+ *                            sequence with more new tokens than a rolling cache has rows (RAP_ECAPACITY; of the tokens that
+ *                            share a row all but the last get slot -1, which rap_qkv_rope_append skips).  Outputs must not
+ *                            overlap inputs or each other, but for d_len_out = d_seq_len.
+ *   rap_decode_attn_window   one new token of every sequence: d_q [B][H_q][2P], d_seq_len[b] counts the row just appended,
+ *                            d_out [B][H_q][d_v'] fp32.
+ *   rap_prefill_attn_window  a ragged block: d_q [T][H_q][2P] and d_out [T][H_q][d_v'] (fp32) hold the sequences' new tokens one
+ *                            after the other, sequence b's in rows d_row_start[b] .. d_row_start[b + 1] - 1 (any number, 0 and 1
+ *                            among them; d_row_start is not decreasing, 0 .. T).  d_seq_len[b] counts them: they are its last
+ *                            positions and their K / V rows are in the cache already.  Rows of d_out from d_row_start[B] on are
+ *                            left as they were.  h_new_max bounds the new tokens of a sequence, h_seq_len_max d_seq_len.  For
+ *                            bf16 stacks with 2P, d_v' <= 128 the softmax weights enter the product with V as two bf16 numbers
+ *                            each, so they carry 16 bits or more, and a V row that one query of a sequence's block sees and
+ *                            another does not must be finite; what no query sees may hold anything.
+ *
+ * ---- attention of a batch whose sequences share long prefixes -------------------------------------------------------
+ *   rap_decode_attn_shared   one new token of every sequence.  Sequences d_group_start[n] .. d_group_start[n + 1] - 1 form group
+ *                            n (n_groups of them; d_group_start[0] = 0 .. B, not decreasing) and share the d_prefix_len[n]
+ *                            (0 .. h_prefix_len_max <= S_cap_prefix) first rows of d_k_prefix / d_v_prefix
+ *                            [n_groups][H_kv][S_cap_prefix][W], caches like any other; sequence b's own rows follow them and lie
+ *                            in rows 0 .. d_seq_len[b] - 1 of d_k_cache / d_v_cache (0 is allowed; d_seq_len counts the row just
+ *                            appended).  The result is that of rap_decode_attn over both, one behind the other; a prefix is
+ *                            read once for all its sequences (for up to 256 / G of them at a time).  The own rows' positions
+ *                            begin at d_prefix_len[n]: append them with d_pos_base.  bf16 stacks with 2P, d_v' <= 128 take the
+ *                            prefix's softmax weights as two bf16 numbers each, as above.
+ * Partial results and arrival counters live in the context, so calls on one context must not overlap on the GPU (captured
+ * graphs of one context neither).  No call allocates or synchronizes; all may be captured.  All types and head shapes of the
+ * library are accepted.  RAP_EINVAL when the current device is not the context's. */
+rap_status rap_build_slots(rap_ctx* ctx, int32_t B, const int32_t* d_seq_len, const int32_t* d_new_len, const int32_t* d_pos_base,
+                           int32_t T, int32_t n_sink, int32_t S_cap, int32_t* d_row_start, int32_t* d_seq_id, int32_t* d_pos,
+                           int32_t* d_slot, int32_t* d_len_out, void* stream);
+rap_status rap_decode_attn_window(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_q, const void* d_k_cache,
+                                  const void* d_v_cache, int32_t S_cap, const int32_t* d_seq_len, int32_t h_seq_len_max,
+                                  int32_t n_sink, int32_t window, float* d_out, void* stream);
+rap_status rap_prefill_attn_window(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, const void* d_q, const void* d_k_cache,
+                                   const void* d_v_cache, int32_t S_cap, const int32_t* d_row_start, const int32_t* d_seq_len,
+                                   int32_t h_new_max, int32_t h_seq_len_max, int32_t n_sink, int32_t window, float* d_out,
+                                   void* stream);
+rap_status rap_decode_attn_shared(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_q, int32_t n_groups,
+                                  const void* d_k_prefix, const void* d_v_prefix, int32_t S_cap_prefix,
+                                  const int32_t* d_group_start, const int32_t* d_prefix_len, int32_t h_prefix_len_max,
+                                  const void* d_k_cache, const void* d_v_cache, int32_t S_cap, const int32_t* d_seq_len,
+                                  int32_t h_seq_len_max, float* d_out, void* stream);
+
 /* ---- output projection on the retained V channels (Algorithm 1: W~_o = E_v W_o) ------------
  * rap_pack_wo: offline column gather.  d_wo [hidden][H_q*D] is the dense W_o of `layer` (stored
  * [out][in]); d_wo_tilde [hidden][H_q*d_v'] receives, for query head g and retained channel c, the

@@ -31,6 +31,7 @@ EXPORTS = [
     "rap_q8_row_bytes", "rap_quantize_rows", "rap_qkv_rope_append_q8", "rap_decode_attn_q8", "rap_decode_step_q8",
     "rap_q4_row_bytes", "rap_quantize_rows_q4", "rap_dequantize_rows_q4", "rap_read_cache_q4", "rap_qkv_rope_append_q4",
     "rap_decode_attn_q4", "rap_decode_step_q4",
+    "rap_build_slots", "rap_decode_attn_window", "rap_prefill_attn_window", "rap_decode_attn_shared",
 ]
 
 
@@ -103,6 +104,10 @@ def _lib():
     lib.rap_qkv_rope_append_q4.argtypes = lib.rap_qkv_rope_append.argtypes
     lib.rap_decode_attn_q4.argtypes = lib.rap_decode_attn.argtypes
     lib.rap_decode_step_q4.argtypes = lib.rap_decode_step.argtypes
+    lib.rap_build_slots.argtypes = [P, c_int32, P, P, P, c_int32, c_int32, c_int32, P, P, P, P, P, P]
+    lib.rap_decode_attn_window.argtypes = [P, c_int32, c_int32, P, P, P, c_int32, P, c_int32, c_int32, c_int32, P, P]
+    lib.rap_prefill_attn_window.argtypes = [P, c_int32, c_int32, c_int32, P, P, P, c_int32, P, P, c_int32, c_int32, c_int32, c_int32, P, P]
+    lib.rap_decode_attn_shared.argtypes = [P, c_int32, c_int32, P, c_int32, P, P, c_int32, P, P, c_int32, P, P, c_int32, P, c_int32, P, P]
     lib.rap_budget_alloc.argtypes = [c_int32, c_int32, c_int32, P, c_double, P, P]
     lib.rap_prefill_attn.argtypes = [P, c_int32, c_int32, c_int32, P, P, P, c_int32, P, c_int32, P, P]
     lib.rap_pack_wo.argtypes = [P, c_int32, P, P, P, P]
@@ -379,6 +384,29 @@ class RapContext:
     def rap_prefill_attn(self, layer, B, T, d_q, d_k_cache, d_v_cache, S_cap, d_start, h_start_max, d_out):
         self._check(_lib().rap_prefill_attn(self._ctx, layer, B, T, _ptr(d_q), _ptr(d_k_cache), _ptr(d_v_cache), S_cap,
                                             _ptr(d_start), h_start_max, _ptr(d_out), _stream()), "rap_prefill_attn")
+
+    def rap_build_slots(self, B, d_seq_len, d_new_len, d_pos_base, T, n_sink, S_cap, d_row_start, d_seq_id, d_pos, d_slot, d_len_out):
+        self._check(_lib().rap_build_slots(self._ctx, B, _ptr(d_seq_len), _ptr(d_new_len), _ptr(d_pos_base), T, n_sink, S_cap,
+                                           _ptr(d_row_start), _ptr(d_seq_id), _ptr(d_pos), _ptr(d_slot), _ptr(d_len_out), _stream()),
+                    "rap_build_slots")
+
+    def rap_decode_attn_window(self, layer, B, d_q, d_k_cache, d_v_cache, S_cap, d_seq_len, h_seq_len_max, n_sink, window, d_out):
+        self._check(_lib().rap_decode_attn_window(self._ctx, layer, B, _ptr(d_q), _ptr(d_k_cache), _ptr(d_v_cache), S_cap,
+                                                  _ptr(d_seq_len), h_seq_len_max, n_sink, window, _ptr(d_out), _stream()),
+                    "rap_decode_attn_window")
+
+    def rap_prefill_attn_window(self, layer, B, T, d_q, d_k_cache, d_v_cache, S_cap, d_row_start, d_seq_len, h_new_max,
+                                h_seq_len_max, n_sink, window, d_out):
+        self._check(_lib().rap_prefill_attn_window(self._ctx, layer, B, T, _ptr(d_q), _ptr(d_k_cache), _ptr(d_v_cache), S_cap,
+                                                   _ptr(d_row_start), _ptr(d_seq_len), h_new_max, h_seq_len_max, n_sink, window,
+                                                   _ptr(d_out), _stream()), "rap_prefill_attn_window")
+
+    def rap_decode_attn_shared(self, layer, B, d_q, n_groups, d_k_prefix, d_v_prefix, S_cap_prefix, d_group_start, d_prefix_len,
+                               h_prefix_len_max, d_k_cache, d_v_cache, S_cap, d_seq_len, h_seq_len_max, d_out):
+        self._check(_lib().rap_decode_attn_shared(self._ctx, layer, B, _ptr(d_q), n_groups, _ptr(d_k_prefix), _ptr(d_v_prefix),
+                                                  S_cap_prefix, _ptr(d_group_start), _ptr(d_prefix_len), h_prefix_len_max,
+                                                  _ptr(d_k_cache), _ptr(d_v_cache), S_cap, _ptr(d_seq_len), h_seq_len_max,
+                                                  _ptr(d_out), _stream()), "rap_decode_attn_shared")
 
     def rap_pack_wo(self, layer, d_wo, d_v_idx, d_wo_tilde):
         self._check(_lib().rap_pack_wo(self._ctx, layer, _ptr(d_wo), _ptr(d_v_idx), _ptr(d_wo_tilde), _stream()),

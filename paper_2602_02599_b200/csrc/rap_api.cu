@@ -29,6 +29,7 @@ void free_all(rap_ctx* c) {
   if (c->d_unit_cnt) cudaFree(c->d_unit_cnt);
   if (c->d_proj_ws) cudaFree(c->d_proj_ws);
   if (c->d_proj_cnt) cudaFree(c->d_proj_cnt);
+  if (c->d_win_cnt) cudaFree(c->d_win_cnt);
   if (c->d_stage_x) cudaFree(c->d_stage_x);
   if (c->d_stage_out) cudaFree(c->d_stage_out);
   if (c->d_stage_q) cudaFree(c->d_stage_q);
@@ -220,6 +221,8 @@ rap_status rap_create(const rap_model_desc* desc, rap_ctx** out) {
   c->proj_cnt_n = 4 * (int)((n_out_max + 127) / 128);
   RAP_CUDA_TRY(c, cudaMalloc(&c->d_proj_cnt, 2 * (size_t)c->proj_cnt_n * sizeof(int32_t)));
   RAP_CUDA_TRY(c, cudaMemset(c->d_proj_cnt, 0, 2 * (size_t)c->proj_cnt_n * sizeof(int32_t)));
+  RAP_CUDA_TRY(c, cudaMalloc(&c->d_win_cnt, (2 * (size_t)d.max_batch * d.n_kv_heads + 1) * sizeof(int32_t)));
+  RAP_CUDA_TRY(c, cudaMemset(c->d_win_cnt, 0, (2 * (size_t)d.max_batch * d.n_kv_heads + 1) * sizeof(int32_t)));
   RAP_CUDA_TRY(c, cudaMalloc(&c->d_stage_x, c->stage_x_bytes));
   RAP_CUDA_TRY(c, cudaMalloc(&c->d_stage_out, c->stage_out_bytes));
   RAP_CUDA_TRY(c, cudaMalloc(&c->d_stage_q, (size_t)d.max_batch * d.n_q_heads * d.head_dim * e));
@@ -754,6 +757,115 @@ rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, c
                                  d_start, d_out, (cudaStream_t)stream);
 }
 
+// ---- windows with sinks, shared prefixes, slot maps ---------------------------------------------------------------------------
+static rap_win_args win_args(const rap_ctx* ctx, int32_t layer) {
+  const rap_model_desc& d = ctx->desc;
+  rap_win_args a = {};
+  a.Hq = d.n_q_heads; a.Hkv = d.n_kv_heads; a.P2 = 2 * ctx->n_pairs[layer]; a.dv = ctx->n_vch[layer];
+  a.head_dim = d.head_dim; a.dtype = d.dtype;
+  return a;
+}
+
+rap_status rap_build_slots(rap_ctx* ctx, int32_t B, const int32_t* d_seq_len, const int32_t* d_new_len, const int32_t* d_pos_base,
+                           int32_t T, int32_t n_sink, int32_t S_cap, int32_t* d_row_start, int32_t* d_seq_id, int32_t* d_pos,
+                           int32_t* d_slot, int32_t* d_len_out, void* stream) {
+  if (!ctx || !d_row_start || (B != 0 && (!d_seq_len || !d_new_len)) || (T != 0 && (!d_seq_id || !d_pos || !d_slot))) return RAP_EINVAL;
+  if (B < 0 || T < 0 || n_sink < 0 || S_cap < 1 || n_sink >= S_cap) return RAP_EINVAL;
+  if (B > ctx->desc.max_batch) return RAP_ESHAPE;
+  if (S_cap % 8) return RAP_EALIGN;
+  const void* const in[3] = {d_seq_len, d_new_len, d_pos_base};
+  const void* const out[5] = {d_row_start, d_seq_id, d_pos, d_slot, d_len_out};
+  const size_t out_bytes[5] = {((size_t)B + 1) * 4, (size_t)T * 4, (size_t)T * 4, (size_t)T * 4, (size_t)B * 4};
+  for (int i = 0; i < 3; ++i)
+    if (in[i] && !rap_aligned16(in[i])) return RAP_EALIGN;
+  for (int i = 0; i < 5; ++i) {
+    if (!out[i]) continue;
+    if (!rap_aligned16(out[i])) return RAP_EALIGN;
+    for (int j = 0; j < 3; ++j)
+      if (in[j] && overlap(in[j], (size_t)B * 4, out[i], out_bytes[i]) && !(i == 4 && j == 0 && in[j] == out[i])) return RAP_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[j], out_bytes[j], out[i], out_bytes[i])) return RAP_EINVAL;
+  }
+  const rap_status s = on_own_device(ctx);
+  if (s != RAP_OK) return s;
+  return rap_launch_build_slots(ctx, B, d_seq_len, d_new_len, d_pos_base, T, n_sink, S_cap, d_row_start, d_seq_id, d_pos, d_slot,
+                                d_len_out, (cudaStream_t)stream);
+}
+
+rap_status rap_decode_attn_window(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_q, const void* d_k_cache,
+                                  const void* d_v_cache, int32_t S_cap, const int32_t* d_seq_len, int32_t h_seq_len_max,
+                                  int32_t n_sink, int32_t window, float* d_out, void* stream) {
+  if (!ctx || !d_q || !d_k_cache || !d_v_cache || !d_seq_len || !d_out) return RAP_EINVAL;
+  if (!ctx->tables_built) return RAP_ESTATE;
+  const rap_model_desc& d = ctx->desc;
+  if (layer < 0 || layer >= d.n_layers || B < 0 || S_cap < 1 || h_seq_len_max < 0 || n_sink < 0 || window < 1 || n_sink >= S_cap)
+    return RAP_EINVAL;
+  if (B > d.max_batch) return RAP_ESHAPE;
+  if (S_cap % 8) return RAP_EALIGN;
+  if (h_seq_len_max > S_cap && window > S_cap - n_sink) return RAP_ECAPACITY;
+  if (!rap_aligned16(d_q) || !rap_aligned16(d_k_cache) || !rap_aligned16(d_v_cache) || !rap_aligned16(d_out) ||
+      !rap_aligned16(d_seq_len))
+    return RAP_EALIGN;
+  const rap_status s = on_own_device(ctx);
+  if (s != RAP_OK || B == 0) return s;
+  rap_win_args a = win_args(ctx, layer);
+  a.q = d_q; a.k = d_k_cache; a.v = d_v_cache; a.seq_len = d_seq_len; a.B = B; a.T = B; a.S_cap = S_cap;
+  a.n_sink = n_sink; a.window = window; a.h_len_max = h_seq_len_max; a.h_new_max = 1; a.out = d_out;
+  return rap_launch_decode_window(ctx, a, (cudaStream_t)stream);
+}
+
+rap_status rap_prefill_attn_window(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, const void* d_q, const void* d_k_cache,
+                                   const void* d_v_cache, int32_t S_cap, const int32_t* d_row_start, const int32_t* d_seq_len,
+                                   int32_t h_new_max, int32_t h_seq_len_max, int32_t n_sink, int32_t window, float* d_out,
+                                   void* stream) {
+  if (!ctx || !d_q || !d_k_cache || !d_v_cache || !d_row_start || !d_seq_len || !d_out) return RAP_EINVAL;
+  if (!ctx->tables_built) return RAP_ESTATE;
+  const rap_model_desc& d = ctx->desc;
+  if (layer < 0 || layer >= d.n_layers || B < 0 || T < 0 || S_cap < 1 || h_new_max < 0 || h_seq_len_max < h_new_max || n_sink < 0 ||
+      window < 1 || n_sink >= S_cap)
+    return RAP_EINVAL;
+  if (B > d.max_batch) return RAP_ESHAPE;
+  if (S_cap % 8) return RAP_EALIGN;
+  if (h_seq_len_max > S_cap && (long long)window + h_new_max - 1 > S_cap - n_sink) return RAP_ECAPACITY;
+  if (!rap_aligned16(d_q) || !rap_aligned16(d_k_cache) || !rap_aligned16(d_v_cache) || !rap_aligned16(d_out) ||
+      !rap_aligned16(d_row_start) || !rap_aligned16(d_seq_len))
+    return RAP_EALIGN;
+  const rap_status s = on_own_device(ctx);
+  if (s != RAP_OK || B == 0 || T == 0) return s;
+  rap_win_args a = win_args(ctx, layer);
+  a.q = d_q; a.k = d_k_cache; a.v = d_v_cache; a.row_start = d_row_start; a.seq_len = d_seq_len; a.B = B; a.T = T; a.S_cap = S_cap;
+  a.n_sink = n_sink; a.window = window; a.h_len_max = h_seq_len_max; a.h_new_max = h_new_max; a.out = d_out;
+  return rap_launch_prefill_window(ctx, a, (cudaStream_t)stream);
+}
+
+rap_status rap_decode_attn_shared(rap_ctx* ctx, int32_t layer, int32_t B, const void* d_q, int32_t n_groups,
+                                  const void* d_k_prefix, const void* d_v_prefix, int32_t S_cap_prefix,
+                                  const int32_t* d_group_start, const int32_t* d_prefix_len, int32_t h_prefix_len_max,
+                                  const void* d_k_cache, const void* d_v_cache, int32_t S_cap, const int32_t* d_seq_len,
+                                  int32_t h_seq_len_max, float* d_out, void* stream) {
+  if (!ctx || !d_q || !d_k_prefix || !d_v_prefix || !d_group_start || !d_prefix_len || !d_k_cache || !d_v_cache || !d_seq_len || !d_out)
+    return RAP_EINVAL;
+  if (!ctx->tables_built) return RAP_ESTATE;
+  const rap_model_desc& d = ctx->desc;
+  if (layer < 0 || layer >= d.n_layers || B < 0 || n_groups < 1 || S_cap_prefix < 1 || h_prefix_len_max < 0 || S_cap < 1 || h_seq_len_max < 0)
+    return RAP_EINVAL;
+  if (B > d.max_batch) return RAP_ESHAPE;
+  if (S_cap % 8 || S_cap_prefix % 8) return RAP_EALIGN;
+  if (h_seq_len_max > S_cap || h_prefix_len_max > S_cap_prefix) return RAP_ECAPACITY;
+  if (!rap_aligned16(d_q) || !rap_aligned16(d_k_prefix) || !rap_aligned16(d_v_prefix) || !rap_aligned16(d_group_start) ||
+      !rap_aligned16(d_prefix_len) || !rap_aligned16(d_k_cache) || !rap_aligned16(d_v_cache) || !rap_aligned16(d_seq_len) ||
+      !rap_aligned16(d_out))
+    return RAP_EALIGN;
+  const rap_status s = on_own_device(ctx);
+  if (s != RAP_OK || B == 0) return s;
+  rap_win_args a = win_args(ctx, layer);
+  a.q = d_q; a.k = d_k_cache; a.v = d_v_cache; a.seq_len = d_seq_len; a.B = B; a.T = B; a.S_cap = S_cap;
+  a.n_sink = 0; a.window = 0x7fffffff; a.h_len_max = h_seq_len_max; a.h_new_max = 1;
+  a.kp = d_k_prefix; a.vp = d_v_prefix; a.group_start = d_group_start; a.prefix_len = d_prefix_len; a.n_groups = n_groups;
+  a.S_pre = S_cap_prefix; a.h_prefix_max = h_prefix_len_max; a.out = d_out;
+  return rap_launch_decode_shared(ctx, a, (cudaStream_t)stream);
+}
+
 // argument checks of a decode step (everything but launching it)
 static rap_status decode_step_check(rap_ctx* ctx, int32_t B, const void* d_x, const void* const* h_w_qkv,
                                     const void* const* h_bias, const double* d_inv_freq, void* const* h_k_cache,
@@ -960,6 +1072,7 @@ rap_status rap_get_last_device_status(rap_ctx* ctx, int32_t* code, int32_t* deta
     const rap_model_desc& d = ctx->desc;
     RAP_CUDA_TRY(ctx, cudaMemsetAsync(ctx->d_unit_cnt, 0, (2 * (size_t)d.max_batch * d.n_kv_heads + 2) * sizeof(int32_t), st));
     RAP_CUDA_TRY(ctx, cudaMemsetAsync(ctx->d_proj_cnt, 0, 2 * (size_t)ctx->proj_cnt_n * sizeof(int32_t), st));
+    RAP_CUDA_TRY(ctx, cudaMemsetAsync(ctx->d_win_cnt, 0, (2 * (size_t)d.max_batch * d.n_kv_heads + 1) * sizeof(int32_t), st));
     RAP_CUDA_TRY(ctx, cudaStreamSynchronize(st));
   }
   *code = h[0];

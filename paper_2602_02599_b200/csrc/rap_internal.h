@@ -35,6 +35,9 @@ struct rap_ctx {
   int32_t* d_proj_cnt = nullptr;  // fused projection: two sets of [row tiles][4] split-arrival counters (zero between calls)
   int proj_cnt_n = 0;             // counters per set
   uint32_t proj_epoch = 0;        // launches of the fused projection so far: picks the set
+  int32_t* d_win_cnt = nullptr;   // windowed / shared-prefix decode: two sets of [max_batch][H_kv] arrival counters, then rap_build_slots' (zero between calls)
+  uint32_t win_epoch = 0;         // such launches so far: picks the set
+  int win_units = 0;              // most units such a launch has had so far: counters that may not be zero
   void* d_stage_x = nullptr;      // staging for rap_decode_step_host
   float* d_stage_out = nullptr;
   void* d_stage_q = nullptr;
@@ -210,3 +213,24 @@ rap_status rap_launch_read_cache_q4(rap_ctx* ctx, int dtype, int B, int Hkv, int
                                     const int32_t* seq_len, int len_max, void* k, void* v, cudaStream_t st);
 rap_status rap_launch_qkv_rope_append_q4(rap_ctx* ctx, const rap_proj_args& a, cudaStream_t st);
 rap_status rap_launch_attn_q4(rap_ctx* ctx, const rap_attn_args& a, cudaStream_t st);
+
+// attention with a window and sinks, over a shared prefix, and their slot maps (rap_window.cu, rap_window_scan.cu, rap_window_tc.cu)
+struct rap_win_args {
+  const void* q; const void* k; const void* v;      // q rows: [T][Hq][P2]
+  const int32_t* seq_len;
+  const int32_t* row_start;                          // NULL: one row per sequence (T == B)
+  int32_t B, T, Hq, Hkv, P2, dv, S_cap, head_dim, dtype;
+  int32_t n_sink, window;
+  int32_t h_len_max, h_new_max;
+  // shared prefix (n_groups == 0: none; then S_cap bounds the lengths only through the rolling rows)
+  const void* kp; const void* vp;
+  const int32_t* group_start; const int32_t* prefix_len;
+  int32_t n_groups, S_pre, h_prefix_max;
+  float* out;
+};
+rap_status rap_launch_build_slots(rap_ctx* ctx, int B, const int32_t* seq_len, const int32_t* new_len, const int32_t* pos_base, int T,
+                                  int n_sink, int S_cap, int32_t* row_start, int32_t* seq_id, int32_t* pos, int32_t* slot,
+                                  int32_t* len_out, cudaStream_t st);
+rap_status rap_launch_decode_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st);
+rap_status rap_launch_prefill_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st);
+rap_status rap_launch_decode_shared(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st);
