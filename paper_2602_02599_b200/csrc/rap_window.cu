@@ -309,6 +309,8 @@ rap_status rap_launch_build_slots(rap_ctx* ctx, int B, const int32_t* seq_len, c
   return RAP_OK;
 }
 
-rap_status rap_launch_decode_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) { return launch_generic(ctx, a, st); }
+rap_status rap_launch_decode_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) {
+  return rap_win_scan_takes(a) ? rap_launch_win_scan(ctx, a, 0, st) : launch_generic(ctx, a, st);
+}
 rap_status rap_launch_prefill_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) { return launch_generic(ctx, a, st); }
 rap_status rap_launch_decode_shared(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) { return launch_generic(ctx, a, st); }

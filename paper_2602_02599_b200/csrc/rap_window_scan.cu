@@ -1,0 +1,90 @@
+// Launch side of win_scan_kernel (rap_window_scan_kernel.cuh).
+#include "rap_window_scan_kernel.cuh"
+
+namespace {
+
+template <bool FOUR, bool VODD>
+const void* scan_fn(int n) {
+  switch (n) {
+    case 1: return (const void*)win_scan_kernel<1, FOUR, VODD>;
+    case 2: return (const void*)win_scan_kernel<2, FOUR, VODD>;
+    case 3: return (const void*)win_scan_kernel<3, FOUR, VODD>;
+    case 4: return (const void*)win_scan_kernel<4, FOUR, VODD>;
+    case 5: return (const void*)win_scan_kernel<5, FOUR, VODD>;
+    case 6: return (const void*)win_scan_kernel<6, FOUR, VODD>;
+    case 7: return (const void*)win_scan_kernel<7, FOUR, VODD>;
+    case 8: return (const void*)win_scan_kernel<8, FOUR, VODD>;
+  }
+  return nullptr;
+}
+
+}  // namespace
+
+bool rap_win_scan_takes(const rap_win_args& a) {
+  return a.dtype == RAP_BF16 && a.P2 >= 16 && a.P2 <= 128 && a.dv >= 16 && a.dv <= 128;
+}
+
+// n_pre: partials of a shared prefix that the launch before leaves in the first places of the workspace (0: none)
+rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, cudaStream_t st) {
+  WsParams p = {};
+  p.q = (const uint32_t*)a.q; p.k = (const unsigned char*)a.k; p.v = (const unsigned char*)a.v; p.seq_len = a.seq_len;
+  p.out = a.out; p.ws = ctx->d_attn_ws; p.ws_floats = (long long)(ctx->attn_ws_bytes / sizeof(float)); p.status = ctx->d_status;
+  p.B = a.B; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv; p.P = a.P2 / 2; p.dv = a.dv; p.S_cap = a.S_cap;
+  p.n_sink = a.n_sink; p.window = a.window; p.len_cap = a.n_groups ? a.S_cap : 0x7fffffff;
+  p.qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
+  p.n_pre = n_pre; p.n_groups = a.n_groups; p.group_start = a.group_start;
+  p.wait_limit = WAIT_LIMIT;
+  {   // two sets of counters take turns; each launch clears the one its predecessor used
+    const size_t n_units = (size_t)ctx->desc.max_batch * ctx->desc.n_kv_heads;
+    const uint32_t set = ctx->win_epoch++ & 1u;
+    if (a.B * a.Hkv > ctx->win_units) ctx->win_units = a.B * a.Hkv;
+    p.other_units = ctx->win_units;
+    p.unit_cnt = ctx->d_win_cnt + set * n_units;
+    p.unit_cnt_other = ctx->d_win_cnt + (set ^ 1u) * n_units;
+  }
+  const int k_row = 2 * a.P2, v_row = 2 * a.dv;
+  const bool vodd = (a.dv & 1) != 0;
+  p.pad16 = (k_row % 16 == 0 && v_row % 16 == 0) ? 1 : 0;
+  if (p.pad16) {
+    // 16 bytes more where a row is an even number of 16-byte units: then eight rows start on different banks
+    p.k_stride = k_row + (k_row % 32 == 0 ? 16 : 0);
+    p.v_stride = v_row + (v_row % 32 == 0 ? 16 : 0);
+    p.rs_log = 0;
+  } else {
+    p.k_stride = k_row;
+    p.v_stride = v_row;
+    // the eight rows of a fragment 4, 2 or 1 apart: P words a row times the step = 4 * odd puts them on different banks; odd
+    // d_v' wants the two rows of a register to be of one parity
+    p.rs_log = (p.P & 1) ? 2 : (p.P & 2) ? 1 : vodd ? 1 : 0;
+  }
+  p.stage_bytes = (32 * (p.k_stride + p.v_stride) + 16 + 127) / 128 * 128;
+  const int cw = (vodd ? a.dv + 1 : a.dv);
+  // two CTAs an SM; four warps with two stages each where they fit (up to 14 KB a stage), else three
+  p.n_stages = 2;
+  int smem = 0;
+  for (p.n_warps = 4; p.n_warps > 1; --p.n_warps) {
+    const int red = p.n_warps * p.G * cw * 4, join = (p.G * RAP_MAX_SPLIT + 8) * 4;
+    p.off_stage = (512 + (red > join ? red : join) + 127) / 128 * 128;
+    smem = p.off_stage + p.n_warps * p.n_stages * p.stage_bytes;
+    if (smem <= SMEM_BUDGET) break;
+  }
+  const int nk = (p.P + 7) / 8, nv = (a.dv + 15) / 16, n = nk > nv ? nk : nv;
+  const void* fn = p.G <= 4 ? (vodd ? scan_fn<true, true>(n) : scan_fn<true, false>(n)) : (vodd ? scan_fn<false, true>(n) : scan_fn<false, false>(n));
+  if (!fn || smem > SMEM_BUDGET) return RAP_EUNSUPPORTED;
+  RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, fn, SMEM_BUDGET));
+  void* args[] = {&p};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * ctx->sm_count);
+  cfg.blockDim = dim3(32 * p.n_warps);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = n_pre ? 1 : 0;      // behind the prefix's launch: it scans the sequences' own rows meanwhile and waits for it before joining
+  RAP_CUDA_TRY(ctx, cudaLaunchKernelExC(&cfg, fn, args));
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}

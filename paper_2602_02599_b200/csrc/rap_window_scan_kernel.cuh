@@ -1,0 +1,518 @@
+// One new token of every sequence over the rows that it sees: rap_decode_attn_window, and the sequences' own rows of
+// rap_decode_attn_shared, for bf16 heads of 16 to 128 dims (2P) and 16 to 128 channels (d_v').
+//
+// Bound by HBM: a row of 2 (2P + d_v') bytes takes 2 G (2P + d_v') flops, so what matters is that copies never pause and that
+// a launch ends soon.  The rows a unit (sequence, KV head) sees are at most three runs of consecutive cache rows (win_runs);
+// each run is cut into blocks of 32 rows from a multiple of 8 on (8 rows start on a 16-byte boundary for every width), and
+// all units' blocks form one sequence that the CTAs share evenly, whatever units they belong to.  Inside a CTA every warp is
+// its own pipeline over every NW-th block: a ring of stages that it fills itself, no barrier until the unit ends.
+//   * Rows of a multiple of 16 bytes are copied 16 bytes a lane into rows padded so that fragment loads meet 32 banks; all
+//     others as contiguous bulk copies, with the eight rows of a fragment spread so that they do.
+//   * S^T = q K^T and O += P V are mma.sync m16n8k16 (M would be G <= 8 query heads: far below a tcgen05 tile, and no
+//     descriptor describes rows of 180 bytes).  The 16 rows of A carry the softmax weights as three bf16 numbers, their
+//     rounding and two remainders (24 bits together), instead of padding: up to four heads rows 0-3, 4-7 and 8-11 in ONE
+//     instruction (q stands in rows 0-3 and again in 4-7, so every lane that needs a weight has computed it), up to eight
+//     heads two of the three in the first instruction and the last in a second one.
+//   * The running maximum is raised only when a logit exceeds it by more than 8 (in log2 units).
+//   * A unit that several CTAs share leaves one partial (sums, maximum, weight) each; who delivers the last one joins them in
+//     order, so a result does not depend on who that is.  The prefix of rap_decode_attn_shared comes as partials too.
+#pragma once
+#include "rap_attn_common.cuh"
+#include "rap_window_common.cuh"
+
+namespace {
+
+struct WsParams {
+  const uint32_t* q;          // [B][Hq][P] bf16 pairs
+  const unsigned char* k;     // [B][Hkv][S_cap][4 P bytes]
+  const unsigned char* v;     // [B][Hkv][S_cap][2 dv bytes]
+  const int32_t* seq_len;
+  float* out;                 // [B][Hq][dv]
+  float* ws;                  // [B][Hq][RAP_MAX_SPLIT][dv + 2]
+  long long ws_floats;
+  int32_t* unit_cnt;          // arrivals per unit, zero between calls
+  int32_t* unit_cnt_other;    // the set of the launch before; cleared by this one
+  int other_units;
+  int32_t* status;
+  int B, Hq, Hkv, G, P, dv, S_cap, n_sink, window, len_cap;
+  float qscale;               // log2(e) / sqrt(D)
+  int pad16;                  // 1: rows of a multiple of 16 bytes, copied into padded rows; 0: bulk copies
+  int k_stride, v_stride;     // bytes between rows in shared memory
+  int rs_log;                 // log2 of the row step between the columns of a fragment
+  int stage_bytes, n_stages, n_warps, off_stage;
+  uint32_t wait_limit;
+  // partials of a shared prefix: the first n_pre of a head's RAP_MAX_SPLIT, for sequences that are in a group
+  int n_pre, n_groups;
+  const int32_t* group_start;
+};
+
+__device__ __forceinline__ void ws_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ws_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t ws_pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t ws_prmt(uint32_t a, uint32_t b, uint32_t sel) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
+  return r;
+}
+__device__ __forceinline__ float ws_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float ws_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// The runs of a unit and their blocks of 32 rows; a unit without rows counts as one block, so that somebody writes its output.
+struct WsUnit {
+  WinRuns r;
+  int a[3], nb[3], n;       // first row and number of blocks by run; blocks together (>= 1)
+};
+__device__ __forceinline__ WsUnit ws_unit(const WsParams& p, int b) {
+  WsUnit u;
+  u.r = win_runs(min(p.seq_len[b], p.len_cap), p.n_sink, p.window, p.S_cap);
+  u.n = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    u.a[i] = u.r.lo[i] & ~7;
+    u.nb[i] = u.r.n[i] > 0 ? (u.r.lo[i] + u.r.n[i] - u.a[i] + 31) >> 5 : 0;
+    u.n += u.nb[i];
+  }
+  u.n = max(u.n, 1);
+  return u;
+}
+__device__ __forceinline__ int ws_scan_add(int x, int lane) {      // inclusive prefix over the warp
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// N: steps of 16 dims and blocks of 16 channels (the larger of the two); FOUR: up to four query heads a KV head; VODD: d_v' odd
+template <int N, bool FOUR, bool VODD>
+__global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                         // [NW][stages], 128 bytes
+  float* m_s = reinterpret_cast<float*>(smem + 128);                          // [4][8]
+  float* l_s = m_s + 32;                                                      // [4][8]
+  int* s_flag = reinterpret_cast<int*>(smem + 384);
+  int* s_last = s_flag + 1;
+  float* red = reinterpret_cast<float*>(smem + 512);                          // [NW][G][CW]; later the join's weights
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int gid = lane >> 2, tq = lane & 3;
+  const int NW = p.n_warps, NSTG = p.n_stages, THREADS = NW * 32;
+  const int G = p.G, P = p.P, dv = p.dv;
+
+  // ---- the plan: every warp works it out from the lengths ----
+  int T = 0, n_max = 1;
+  for (int b0 = 0; b0 < p.B; b0 += 32) {
+    const int n = b0 + lane < p.B ? ws_unit(p, b0 + lane).n : 0;
+    n_max = max(n_max, __reduce_max_sync(0xffffffffu, n));
+    T += __reduce_add_sync(0xffffffffu, n);
+  }
+  T *= p.Hkv;
+  // no unit is touched by more CTAs than there is room for partials behind the prefix's, and every CTA has a block for each warp
+  const long long room = (long long)(RAP_MAX_SPLIT - 2 - p.n_pre) * T / n_max;
+  const int nc = (int)max(1LL, min(min((long long)gridDim.x, room), (long long)(T + NW - 1) / NW));
+  if (blockIdx.x == 0)
+    for (int i = tid; i < p.other_units; i += THREADS) p.unit_cnt_other[i] = 0;      // what a launch that gave up left behind
+  if ((int)blockIdx.x >= nc) {
+    if (p.n_pre) pdl_wait();     // a launch is not over before the one that it overlaps
+    return;
+  }
+  int cur = (int)((long long)blockIdx.x * T / nc);
+  const int hi = (int)((long long)(blockIdx.x + 1) * T / nc);
+  auto cta_of = [&](int tile) { return (int)((((long long)tile + 1) * nc - 1) / T); };   // whose share holds this block
+  int b = 0, h, unit_start = 0;
+  for (int b0 = 0, carry = 0;; b0 += 32) {
+    const int n = b0 + lane < p.B ? ws_unit(p, b0 + lane).n * p.Hkv : 0;
+    const int x = ws_scan_add(n, lane) + carry;
+    const unsigned past = __ballot_sync(0xffffffffu, x > cur);
+    if (past) {
+      const int l = __ffs(past) - 1;
+      b = b0 + l;
+      unit_start = __shfl_sync(0xffffffffu, x - n, l);
+      break;
+    }
+    carry = __shfl_sync(0xffffffffu, x, 31);
+  }
+  WsUnit u = ws_unit(p, b);
+  h = (cur - unit_start) / u.n;
+  unit_start += h * u.n;
+
+  const uint32_t bar0 = smem_u32(bars) + warp * NSTG * 8;
+  unsigned char* wstage = smem + p.off_stage + (size_t)warp * NSTG * p.stage_bytes;
+  const uint32_t wstage_u = smem_u32(wstage);
+  if (tid == 0) {
+    *s_flag = 0;
+    for (int i = 0; i < NW * NSTG; ++i) mbar_init(smem_u32(bars) + 8 * i, p.pad16 ? 32 : 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+
+  // ---- fragment addresses inside a stage, in 32-bit words ----
+  auto frag_row = [&](int t, int n) { return (n << p.rs_log) + (t & ((1 << p.rs_log) - 1)) + ((t >> p.rs_log) << (3 + p.rs_log)); };
+  const int v_base = (32 * p.k_stride) >> 2;
+  const int vpair = (p.v_stride << p.rs_log) >> 2;           // words between the two rows of a V register (an even row step where dv is odd)
+  int koff[4], vofs[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    koff[t] = ((frag_row(t, gid) * p.k_stride) >> 2) + tq;
+    vofs[t] = v_base + ((frag_row(t, 2 * tq) * p.v_stride) >> 2) + gid;     // odd dv: rounded down for odd rows
+  }
+  const int k_last = P - 8;                                   // the last steps are shifted back into the row
+  const int c_last = VODD ? dv - 15 : dv - 16;                // so are the last blocks of channels (odd dv: one phantom channel)
+  const int CW = c_last + 16;
+  const int head = FOUR ? gid & 3 : gid;                      // the query head whose logits this lane holds
+  const float cs = p.qscale;
+  const int k_row = 4 * P, v_row = 2 * dv;                    // bytes in the cache
+
+  int st = 0;                  // ring position and phase of this warp, across units
+  uint32_t parity = 0;
+  bool timed_out = false, joined = false;
+
+  for (;;) {   // one pass per unit that this CTA touches
+    const int t0 = cur - unit_start;
+    const int n_my = min(u.n - t0, hi - cur);
+    const size_t unit = (size_t)b * p.Hkv + h;
+    const unsigned char* kg = p.k + unit * (size_t)p.S_cap * (size_t)k_row;
+    const unsigned char* vg = p.v + unit * (size_t)p.S_cap * (size_t)v_row;
+    const bool empty = u.nb[0] + u.nb[1] + u.nb[2] == 0;
+    const int n_blk = !empty && n_my > warp ? (n_my - warp + NW - 1) / NW : 0;
+
+    // first row of block i of this warp, and which of its 32 rows are seen
+    auto block_at = [&](int i, int& row0, int& lo, int& hi_row) {
+      int j = t0 + warp + i * NW, run = 0;
+      if (j >= u.nb[0]) { j -= u.nb[0]; run = 1; }
+      if (run == 1 && j >= u.nb[1]) { j -= u.nb[1]; run = 2; }
+      const int a = run == 0 ? u.a[0] : run == 1 ? u.a[1] : u.a[2];
+      const int l = run == 0 ? u.r.lo[0] : run == 1 ? u.r.lo[1] : u.r.lo[2];
+      const int e = l + (run == 0 ? u.r.n[0] : run == 1 ? u.r.n[1] : u.r.n[2]);
+      row0 = a + 32 * j;
+      lo = max(0, l - row0);
+      hi_row = min(32, e - row0);
+    };
+    auto issue_block = [&](int i, int stg) {
+      int row0, lo, hi_row;
+      block_at(i, row0, lo, hi_row);
+      const int rows = (hi_row + 7) & ~7;                     // inside the cache: S_cap is a multiple of 8
+      const uint32_t bar = bar0 + 8 * stg, dst = wstage_u + stg * p.stage_bytes;
+      const bool ok = RAP_BOUNDS(row0, p.S_cap, p.status, 0x201) && RAP_BOUNDS(row0 + rows - 1, p.S_cap, p.status, 0x202) &&
+                      RAP_BOUNDS(rows - 1, 32, p.status, 0x203) && RAP_BOUNDS(unit, (size_t)p.B * p.Hkv, p.status, 0x204);
+      const unsigned char* ks = kg + (size_t)row0 * k_row;
+      const unsigned char* vs = vg + (size_t)row0 * v_row;
+      if (p.pad16) {
+        const int c = lane & 15, kc = k_row >> 4, vc = v_row >> 4;
+        for (int r = lane >> 4; r < rows && ok; r += 2) {
+          if (c < kc)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + r * p.k_stride + 16 * c), "l"(ks + (size_t)r * k_row + 16 * c) : "memory");
+          if (c < vc)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 32 * p.k_stride + r * p.v_stride + 16 * c),
+                         "l"(vs + (size_t)r * v_row + 16 * c) : "memory");
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+      } else if (lane == 0) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // earlier reads and zeros come first
+        mbar_expect_tx(bar, ok ? (uint32_t)(rows * (k_row + v_row)) : 0u);
+        if (ok) {
+          bulk_g2s(dst, ks, (uint32_t)(rows * k_row), bar);
+          bulk_g2s(dst + 32 * p.k_stride, vs, (uint32_t)(rows * v_row), bar);
+        }
+      }
+    };
+    for (int i = 0; i < min(n_blk, NSTG - 1); ++i) issue_block(i, (st + i) % NSTG);
+
+    // ---- q as the A operand: words (8 ks + tq) and (8 ks + 4 + tq) of the lane's head; zero where a step overlaps the one before ----
+    uint32_t qa[N][2];
+    {
+      const uint32_t* qrow = p.q + ((size_t)b * p.Hq + (size_t)h * G + (head < G ? head : 0)) * P;
+#pragma unroll
+      for (int ks = 0; ks < N; ++ks) {
+        const int wb = min(8 * ks, k_last);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int w = wb + 4 * e + tq;
+          qa[ks][e] = (head < G && w >= 8 * ks && RAP_BOUNDS(w, P, p.status, 0x205)) ? qrow[w] : 0u;
+        }
+      }
+    }
+    float o[N][2][4];
+#pragma unroll
+    for (int cb = 0; cb < N; ++cb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[cb][e][r] = 0.f;
+    float m_ref = -INFINITY, l_thr = 0.f;
+
+    for (int i = 0; i < n_blk; ++i) {
+      if (i + NSTG - 1 < n_blk) issue_block(i + NSTG - 1, (st + NSTG - 1) % NSTG);
+      if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar0 + 8 * st, parity, p.wait_limit))) {
+        timed_out = true;
+        break;
+      }
+      int row0, lo, hi_row;
+      block_at(i, row0, lo, hi_row);
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(wstage + (size_t)st * p.stage_bytes);
+      const bool ragged = lo > 0 || hi_row < 32;
+      if (ragged) {
+        // rows that are not seen: their V is zero, so that the second product meets 0 * 0 there
+        uint16_t* vz = reinterpret_cast<uint16_t*>(wstage + (size_t)st * p.stage_bytes + 32 * p.k_stride);
+        const int vsr = p.v_stride >> 1;
+        for (int r = 0; r < 32; ++r)
+          if (r < lo || r >= hi_row)
+            for (int c = lane; c < dv; c += 32) vz[r * vsr + c] = 0;
+        if (VODD && lane < 8) vz[32 * vsr + lane] = 0;          // the phantom channel of the last row
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
+
+      // ---- S^T = q K^T: four fragments of 8 rows ----
+      float s[4][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < N; ++ks) {
+        const int wb = min(8 * ks, k_last);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t b0 = w[koff[t] + wb], b1 = w[koff[t] + wb + 4];
+          ws_mma(s[t], qa[ks][0], 0u, qa[ks][1], 0u, b0, b1);
+        }
+      }
+
+      // ---- softmax: lane (gid, tq) holds its head's logits of rows frag_row(t, 2 tq + e) ----
+      float x[4][2];
+      bool raise = false;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = frag_row(t, 2 * tq + e);
+          if (ragged && (row < lo || row >= hi_row)) s[t][e] = -INFINITY;
+          x[t][e] = fmaf(s[t][e], cs, -m_ref);
+          raise |= x[t][e] > 8.f;
+        }
+      if (__any_sync(0xffffffffu, raise || m_ref == -INFINITY)) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) mx = fmaxf(mx, s[t][e] * cs);
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float m_new = fmaxf(m_ref, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = ws_ex2(m_ref - ref);               // first block: 2^(-inf) = 0
+        m_ref = m_new;
+        l_thr *= alpha;
+#pragma unroll
+        for (int cb = 0; cb < N; ++cb)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[cb][e][r] *= alpha;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) x[t][e] = fmaf(s[t][e], cs, -ref);
+      }
+      uint32_t p0[4], p1[4], p2[4];      // the weights of rows frag_row(t, 2 tq) and frag_row(t, 2 tq + 1): bf16 roundings, remainders, theirs
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        float a = ws_ex2(x[t][0]), c = ws_ex2(x[t][1]);
+        l_thr += a + c;
+        p0[t] = ws_pack(a, c);
+        a -= ws_lo(p0[t]);
+        c -= ws_hi(p0[t]);
+        p1[t] = ws_pack(a, c);
+        p2[t] = ws_pack(a - ws_lo(p1[t]), c - ws_hi(p1[t]));
+        if (FOUR) {
+          p0[t] = gid < 4 ? p0[t] : p1[t];
+          p2[t] = gid < 4 ? p2[t] : 0u;
+        }
+      }
+
+      // ---- O += P V: two steps of 16 rows (fragments 2 kb and 2 kb + 1), blocks of 16 channels ----
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint32_t* v0 = w + vofs[2 * kb];
+        const uint32_t* v1 = w + vofs[2 * kb + 1];
+#pragma unroll
+        for (int cb = 0; cb < N; ++cb) {
+          const int cw = min(16 * cb, c_last) >> 1;
+          const uint32_t xa0 = v0[cw], xb0 = v0[cw + vpair], xa1 = v1[cw], xb1 = v1[cw + vpair];
+          const uint32_t be0 = ws_prmt(xa0, xb0, 0x5410u), bo0 = ws_prmt(xa0, xb0, 0x7632u);
+          uint32_t be1, bo1;
+          if constexpr (!VODD) {
+            be1 = ws_prmt(xa1, xb1, 0x5410u);
+            bo1 = ws_prmt(xa1, xb1, 0x7632u);
+          } else {
+            // odd rows of an odd dv: the aligned word holds channels (c - 1, c), the next one (c + 1, c + 2)
+            const uint32_t ya1 = v1[cw + 1], yb1 = v1[cw + vpair + 1];
+            be1 = ws_prmt(xa1, xb1, 0x7632u);
+            bo1 = ws_prmt(ya1, yb1, 0x5410u);
+          }
+          if constexpr (FOUR) {
+            ws_mma(o[cb][0], p0[2 * kb], p2[2 * kb], p0[2 * kb + 1], p2[2 * kb + 1], be0, be1);
+            ws_mma(o[cb][1], p0[2 * kb], p2[2 * kb], p0[2 * kb + 1], p2[2 * kb + 1], bo0, bo1);
+          } else {
+            ws_mma(o[cb][0], p0[2 * kb], p1[2 * kb], p0[2 * kb + 1], p1[2 * kb + 1], be0, be1);
+            ws_mma(o[cb][1], p0[2 * kb], p1[2 * kb], p0[2 * kb + 1], p1[2 * kb + 1], bo0, bo1);
+            ws_mma(o[cb][0], 0u, p2[2 * kb], 0u, p2[2 * kb + 1], be0, be1);
+            ws_mma(o[cb][1], 0u, p2[2 * kb], 0u, p2[2 * kb + 1], bo0, bo1);
+          }
+        }
+      }
+      __syncwarp();            // every lane is done with this stage before it is filled again
+      if (++st == NSTG) { st = 0; parity ^= 1u; }
+    }
+
+    // ---- the warps' sums together: common maximum per head ----
+    l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 1);
+    l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 2);
+    if (timed_out && lane == 0) *s_flag = 1;
+    if (tq == 0) m_s[warp * 8 + gid] = m_ref;
+    __syncthreads();
+    if (*s_flag) {
+      if (tid == 0) win_report(p.status, RAP_ETIMEOUT, (int)unit);
+      // copies still in flight get a bounded chance to land before the shared memory is released
+      if (lane == 0)
+        for (int sg = 0; sg < NSTG; ++sg) {
+          mbar_wait_bounded(bar0 + 8 * sg, 0, p.wait_limit);
+          mbar_wait_bounded(bar0 + 8 * sg, 1, p.wait_limit);
+        }
+      __syncthreads();
+      return;
+    }
+    float m_all = -INFINITY;
+    for (int i = 0; i < NW; ++i) m_all = fmaxf(m_all, m_s[i * 8 + gid]);
+    const float f = m_ref == -INFINITY ? 0.f : ws_ex2(m_ref - m_all);
+    if (tq == 0) l_s[warp * 8 + gid] = l_thr * f;
+    float* rr = red + ((size_t)warp * G + (head < G ? head : 0)) * CW;
+#pragma unroll
+    for (int cb = 0; cb < N; ++cb) {
+      const int c0 = min(16 * cb, c_last) + 4 * tq;
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float rest = o[cb][e][r + 2];
+          if (FOUR) rest += __shfl_down_sync(0xffffffffu, o[cb][e][r], 16);
+          // remainders of either sign times an infinity of V would be NaN: the roundings' sum says what it is
+          const float t = fabsf(o[cb][e][r]) == INFINITY ? o[cb][e][r] : o[cb][e][r] + rest;
+          if ((FOUR ? gid < 4 : true) && head < G) rr[c0 + 2 * r + e] = t * f;
+        }
+    }
+    __syncthreads();
+    int n_pre = 0;             // partials of the prefix, if the sequence has one
+    if (p.n_pre) {
+      const int g = win_owner(p.group_start, p.n_groups, b);
+      n_pre = g < p.n_groups && p.group_start[g] <= b ? p.n_pre : 0;
+    }
+    const int first = cta_of(unit_start), n_seg = cta_of(unit_start + u.n - 1) - first + 1;
+    const bool alone = n_seg == 1 && n_pre == 0;
+    const size_t ws_head = (size_t)RAP_MAX_SPLIT * (dv + 2);
+    float* ub = p.ws + ((size_t)b * p.Hq + (size_t)h * G) * ws_head;           // the unit's partials
+    float* mine = ub + (size_t)(p.n_pre + (int)blockIdx.x - first) * (dv + 2);
+    float* out = p.out + ((size_t)b * p.Hq + (size_t)h * G) * dv;
+    const bool ws_ok = RAP_BOUNDS(p.n_pre + (int)blockIdx.x - first, RAP_MAX_SPLIT, p.status, 0x206) &&
+                       RAP_BOUNDS((mine - p.ws) + (long long)(G - 1) * ws_head + dv + 1, p.ws_floats, p.status, 0x207);
+    for (int g = warp; g < G && ws_ok; g += NW) {
+      float l = 0.f, mm = -INFINITY;
+      for (int i = 0; i < NW; ++i) {
+        l += l_s[i * 8 + g];
+        mm = fmaxf(mm, m_s[i * 8 + g]);
+      }
+      const float inv = l != 0.f ? 1.f / l : 0.f;
+      for (int c = lane; c < dv; c += 32) {
+        float sum = 0.f;
+        for (int i = 0; i < NW; ++i) sum += red[((size_t)i * G + g) * CW + c];
+        if (alone) out[(size_t)g * dv + c] = sum * inv;
+        else mine[g * ws_head + c] = sum;
+      }
+      if (!alone && lane == 0) {
+        mine[g * ws_head + dv] = mm;
+        mine[g * ws_head + dv + 1] = l;
+      }
+    }
+    if (!alone) {
+      // ---- who delivers a unit's last partial joins them, in order ----
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) *s_last = n_seg == 1 || (RAP_BOUNDS(unit, (size_t)p.B * p.Hkv, p.status, 0x208) && atomicAdd(&p.unit_cnt[unit], 1) == n_seg - 1);
+      __syncthreads();
+      if (*s_last) {
+        if (p.n_pre && !joined) pdl_wait();        // the prefix's partials come from the launch before
+        joined = true;
+        __threadfence();
+        const float* from = ub + (size_t)(p.n_pre - n_pre) * (dv + 2);
+        const int n = n_pre + n_seg;               // <= RAP_MAX_SPLIT
+        float* wgt = red;                          // [G][RAP_MAX_SPLIT] weights, then the heads' reciprocals
+        for (int g = warp; g < G; g += NW) {
+          const float* gb = from + (size_t)g * ws_head;
+          float mv[2], lv[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int sg = lane + 32 * k;
+            lv[k] = sg < n ? __ldcg(gb + (size_t)sg * (dv + 2) + dv + 1) : 0.f;
+            mv[k] = sg < n ? __ldcg(gb + (size_t)sg * (dv + 2) + dv) : -INFINITY;
+            if (lv[k] == 0.f) mv[k] = -INFINITY;
+          }
+          float M = fmaxf(mv[0], mv[1]);
+#pragma unroll
+          for (int s2 = 16; s2 > 0; s2 >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, s2));
+          float den = 0.f;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float wk = lv[k] != 0.f ? exp2f(mv[k] - M) : 0.f;
+            wgt[g * RAP_MAX_SPLIT + lane + 32 * k] = wk;
+            den += wk * lv[k];
+          }
+#pragma unroll
+          for (int s2 = 16; s2 > 0; s2 >>= 1) den += __shfl_xor_sync(0xffffffffu, den, s2);
+          if (lane == 0) wgt[G * RAP_MAX_SPLIT + g] = den != 0.f ? 1.f / den : 0.f;
+        }
+        __syncthreads();
+        for (int i = tid; i < G * dv; i += THREADS) {
+          const int g = i / dv, c = i - g * dv;
+          const float* gb = from + (size_t)g * ws_head + c;
+          float num = 0.f;
+          for (int s0 = 0; s0 < n; s0 += 16) {     // sixteen loads in flight
+            float av[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) av[k] = s0 + k < n ? __ldcg(gb + (size_t)(s0 + k) * (dv + 2)) : 0.f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float wk = s0 + k < n ? wgt[g * RAP_MAX_SPLIT + s0 + k] : 0.f;
+              if (wk != 0.f) num += wk * av[k];
+            }
+          }
+          out[i] = num * wgt[G * RAP_MAX_SPLIT + g];
+        }
+        if (tid == 0) p.unit_cnt[unit] = 0;        // ready for the next call
+      }
+    }
+    // ---- the next unit, from its first block ----
+    cur += n_my;
+    if (cur >= hi) break;
+    unit_start += u.n;
+    if (++h == p.Hkv) {
+      h = 0;
+      if (++b >= p.B) break;
+      u = ws_unit(p, b);
+    }
+    __syncthreads();           // the sums and weights in shared memory have been read
+  }
+  if (p.n_pre) pdl_wait();
+}
+
+}  // namespace
