@@ -20,7 +20,7 @@ __device__ __forceinline__ WinRuns win_runs(int len, int n_sink, int window, int
   w.lo[1] = n_sink;
   w.n[1] = w.lo[2] = w.n[2] = 0;
   if (n > 0) {
-    const int a = n_sink + (len - n - n_sink) % R;
+    const int a = len <= S_cap ? len - n : n_sink + (len - n - n_sink) % R;
     w.lo[1] = a;
     w.n[1] = min(n, S_cap - a);
     w.lo[2] = n_sink;
@@ -44,6 +44,10 @@ __device__ __forceinline__ int win_owner(const int32_t* start, int n, int r) {
   }
   return lo;
 }
+
+// Partials of a query head in the context's workspace: RAP_MAX_SPLIT rows of d_v' sums (a multiple of four), then as many
+// (maximum, weight) pairs
+__host__ __device__ __forceinline__ size_t win_partial_floats(int dv) { return (size_t)RAP_MAX_SPLIT * (((dv + 3) & ~3) + 2); }
 
 __device__ __forceinline__ void win_report(int32_t* status, int code, int detail) {
   if (atomicCAS(&status[0], 0, code) == 0) status[1] = detail;

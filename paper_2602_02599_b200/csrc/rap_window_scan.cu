@@ -57,6 +57,7 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
     // d_v' wants the two rows of a register to be of one parity
     p.rs_log = (p.P & 1) ? 2 : (p.P & 2) ? 1 : vodd ? 1 : 0;
   }
+  p.per_cta = 4;
   p.stage_bytes = (32 * (p.k_stride + p.v_stride) + 16 + 127) / 128 * 128;
   const int cw = (vodd ? a.dv + 1 : a.dv);
   // two CTAs an SM; four warps with two stages each where they fit (up to 14 KB a stage), else three

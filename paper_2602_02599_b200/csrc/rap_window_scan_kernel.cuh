@@ -22,13 +22,16 @@
 
 namespace {
 
+// blocks that a unit's end takes as long as: joining the warps, its partial, the arrival (3 us against 0.5 us a block)
+constexpr int WS_OWN = 6;
+
 struct WsParams {
   const uint32_t* q;          // [B][Hq][P] bf16 pairs
   const unsigned char* k;     // [B][Hkv][S_cap][4 P bytes]
   const unsigned char* v;     // [B][Hkv][S_cap][2 dv bytes]
   const int32_t* seq_len;
   float* out;                 // [B][Hq][dv]
-  float* ws;                  // [B][Hq][RAP_MAX_SPLIT][dv + 2]
+  float* ws;                  // [B][Hq] partials (win_partial_floats)
   long long ws_floats;
   int32_t* unit_cnt;          // arrivals per unit, zero between calls
   int32_t* unit_cnt_other;    // the set of the launch before; cleared by this one
@@ -40,6 +43,7 @@ struct WsParams {
   int k_stride, v_stride;     // bytes between rows in shared memory
   int rs_log;                 // log2 of the row step between the columns of a fragment
   int stage_bytes, n_stages, n_warps, off_stage;
+  int per_cta;                // least blocks of a CTA
   uint32_t wait_limit;
   // partials of a shared prefix: the first n_pre of a head's RAP_MAX_SPLIT, for sequences that are in a group
   int n_pre, n_groups;
@@ -112,29 +116,32 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   const int NW = p.n_warps, NSTG = p.n_stages, THREADS = NW * 32;
   const int G = p.G, P = p.P, dv = p.dv;
 
-  // ---- the plan: every warp works it out from the lengths ----
-  int T = 0, n_max = 1;
+  // ---- the plan: every warp works it out from the lengths.  A unit counts WS_OWN blocks more than it has: what its end costs ----
+  int T = 0, n_max = 1, n_first = 0;
   for (int b0 = 0; b0 < p.B; b0 += 32) {
-    const int n = b0 + lane < p.B ? ws_unit(p, b0 + lane).n : 0;
+    const int n = b0 + lane < p.B ? ws_unit(p, b0 + lane).n + WS_OWN : 0;
+    if (b0 == 0) n_first = n;
     n_max = max(n_max, __reduce_max_sync(0xffffffffu, n));
     T += __reduce_add_sync(0xffffffffu, n);
   }
   T *= p.Hkv;
   // no unit is touched by more CTAs than there is room for partials behind the prefix's, and every CTA has a block for each warp
   const long long room = (long long)(RAP_MAX_SPLIT - 2 - p.n_pre) * T / n_max;
-  const int nc = (int)max(1LL, min(min((long long)gridDim.x, room), (long long)(T + NW - 1) / NW));
+  const int nc = (int)max(1LL, min(min((long long)gridDim.x, room), (long long)(T + p.per_cta - 1) / p.per_cta));
   if (blockIdx.x == 0)
     for (int i = tid; i < p.other_units; i += THREADS) p.unit_cnt_other[i] = 0;      // what a launch that gave up left behind
   if ((int)blockIdx.x >= nc) {
     if (p.n_pre) pdl_wait();     // a launch is not over before the one that it overlaps
     return;
   }
-  int cur = (int)((long long)blockIdx.x * T / nc);
-  const int hi = (int)((long long)(blockIdx.x + 1) * T / nc);
-  auto cta_of = [&](int tile) { return (int)((((long long)tile + 1) * nc - 1) / T); };   // whose share holds this block
+  // the first T % nc CTAs take one block more than the others
+  const int share = T / nc, extra = T - share * nc, mark = extra * (share + 1);
+  auto cta_of = [&](int tile) { return tile < mark ? tile / (share + 1) : extra + (tile - mark) / share; };   // whose share holds this block
+  int cur = (int)blockIdx.x * share + min((int)blockIdx.x, extra);
+  const int hi = cur + share + ((int)blockIdx.x < extra ? 1 : 0);
   int b = 0, h, unit_start = 0;
   for (int b0 = 0, carry = 0;; b0 += 32) {
-    const int n = b0 + lane < p.B ? ws_unit(p, b0 + lane).n * p.Hkv : 0;
+    const int n = (b0 == 0 ? n_first : b0 + lane < p.B ? ws_unit(p, b0 + lane).n + WS_OWN : 0) * p.Hkv;
     const int x = ws_scan_add(n, lane) + carry;
     const unsigned past = __ballot_sync(0xffffffffu, x > cur);
     if (past) {
@@ -146,8 +153,8 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
     carry = __shfl_sync(0xffffffffu, x, 31);
   }
   WsUnit u = ws_unit(p, b);
-  h = (cur - unit_start) / u.n;
-  unit_start += h * u.n;
+  h = (cur - unit_start) / (u.n + WS_OWN);
+  unit_start += h * (u.n + WS_OWN);
 
   const uint32_t bar0 = smem_u32(bars) + warp * NSTG * 8;
   unsigned char* wstage = smem + p.off_stage + (size_t)warp * NSTG * p.stage_bytes;
@@ -181,13 +188,23 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   bool timed_out = false, joined = false;
 
   for (;;) {   // one pass per unit that this CTA touches
-    const int t0 = cur - unit_start;
-    const int n_my = min(u.n - t0, hi - cur);
+    const int t0 = max(cur - unit_start - WS_OWN, 0);               // this CTA's blocks of the unit: [t0, t0 + n_my)
+    const int n_my = min(u.n, hi - unit_start - WS_OWN) - t0;
+    if (n_my <= 0) break;                                           // its share ends in what the unit counts beyond its blocks
     const size_t unit = (size_t)b * p.Hkv + h;
     const unsigned char* kg = p.k + unit * (size_t)p.S_cap * (size_t)k_row;
     const unsigned char* vg = p.v + unit * (size_t)p.S_cap * (size_t)v_row;
     const bool empty = u.nb[0] + u.nb[1] + u.nb[2] == 0;
     const int n_blk = !empty && n_my > warp ? (n_my - warp + NW - 1) / NW : 0;
+    int n_pre = 0;             // partials of the prefix, if the sequence has one
+    if (p.n_pre) {
+      const int g = win_owner(p.group_start, p.n_groups, b);
+      n_pre = g < p.n_groups && p.group_start[g] <= b ? p.n_pre : 0;
+    }
+    float* out = p.out + ((size_t)b * p.Hq + (size_t)h * G) * dv;
+    if (empty && n_pre == 0) {
+      for (int i = tid; i < G * dv; i += THREADS) out[i] = 0.f;
+    } else {
 
     // first row of block i of this warp, and which of its 32 rows are seen
     auto block_at = [&](int i, int& row0, int& lo, int& hi_row) {
@@ -266,12 +283,15 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
       const bool ragged = lo > 0 || hi_row < 32;
       if (ragged) {
         // rows that are not seen: their V is zero, so that the second product meets 0 * 0 there
-        uint16_t* vz = reinterpret_cast<uint16_t*>(wstage + (size_t)st * p.stage_bytes + 32 * p.k_stride);
-        const int vsr = p.v_stride >> 1;
-        for (int r = 0; r < 32; ++r)
-          if (r < lo || r >= hi_row)
-            for (int c = lane; c < dv; c += 32) vz[r * vsr + c] = 0;
-        if (VODD && lane < 8) vz[32 * vsr + lane] = 0;          // the phantom channel of the last row
+        unsigned char* vz = wstage + (size_t)st * p.stage_bytes + 32 * p.k_stride;
+        const int z0 = lo * p.v_stride, z1 = hi_row * p.v_stride, z2 = 32 * p.v_stride;     // bytes [0, z0) and [z1, z2)
+        if constexpr (VODD) {
+          for (int i = 2 * lane; i < z0; i += 64) *reinterpret_cast<uint16_t*>(vz + i) = 0;
+          for (int i = z1 + 2 * lane; i < z2; i += 64) *reinterpret_cast<uint16_t*>(vz + i) = 0;
+        } else {
+          for (int i = 4 * lane; i < z0; i += 128) *reinterpret_cast<uint32_t*>(vz + i) = 0u;
+          for (int i = z1 + 4 * lane; i < z2; i += 128) *reinterpret_cast<uint32_t*>(vz + i) = 0u;
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       }
@@ -408,24 +428,19 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
           float rest = o[cb][e][r + 2];
           if (FOUR) rest += __shfl_down_sync(0xffffffffu, o[cb][e][r], 16);
           // remainders of either sign times an infinity of V would be NaN: the roundings' sum says what it is
-          const float t = fabsf(o[cb][e][r]) == INFINITY ? o[cb][e][r] : o[cb][e][r] + rest;
+          float t = o[cb][e][r] + rest;
+          if (t != t && fabsf(o[cb][e][r]) == INFINITY) t = o[cb][e][r];
           if ((FOUR ? gid < 4 : true) && head < G) rr[c0 + 2 * r + e] = t * f;
         }
     }
     __syncthreads();
-    int n_pre = 0;             // partials of the prefix, if the sequence has one
-    if (p.n_pre) {
-      const int g = win_owner(p.group_start, p.n_groups, b);
-      n_pre = g < p.n_groups && p.group_start[g] <= b ? p.n_pre : 0;
-    }
-    const int first = cta_of(unit_start), n_seg = cta_of(unit_start + u.n - 1) - first + 1;
+    const int first = cta_of(unit_start + WS_OWN), n_seg = cta_of(unit_start + WS_OWN + u.n - 1) - first + 1;
     const bool alone = n_seg == 1 && n_pre == 0;
-    const size_t ws_head = (size_t)RAP_MAX_SPLIT * (dv + 2);
+    const int dv4 = (dv + 3) & ~3, my_seg = p.n_pre + (int)blockIdx.x - first;
+    const size_t ws_head = win_partial_floats(dv);
     float* ub = p.ws + ((size_t)b * p.Hq + (size_t)h * G) * ws_head;           // the unit's partials
-    float* mine = ub + (size_t)(p.n_pre + (int)blockIdx.x - first) * (dv + 2);
-    float* out = p.out + ((size_t)b * p.Hq + (size_t)h * G) * dv;
-    const bool ws_ok = RAP_BOUNDS(p.n_pre + (int)blockIdx.x - first, RAP_MAX_SPLIT, p.status, 0x206) &&
-                       RAP_BOUNDS((mine - p.ws) + (long long)(G - 1) * ws_head + dv + 1, p.ws_floats, p.status, 0x207);
+    const bool ws_ok = RAP_BOUNDS(my_seg, RAP_MAX_SPLIT, p.status, 0x206) &&
+                       RAP_BOUNDS((ub - p.ws) + (long long)G * ws_head - 1, p.ws_floats, p.status, 0x207);
     for (int g = warp; g < G && ws_ok; g += NW) {
       float l = 0.f, mm = -INFINITY;
       for (int i = 0; i < NW; ++i) {
@@ -437,12 +452,9 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         float sum = 0.f;
         for (int i = 0; i < NW; ++i) sum += red[((size_t)i * G + g) * CW + c];
         if (alone) out[(size_t)g * dv + c] = sum * inv;
-        else mine[g * ws_head + c] = sum;
+        else ub[g * ws_head + my_seg * dv4 + c] = sum;
       }
-      if (!alone && lane == 0) {
-        mine[g * ws_head + dv] = mm;
-        mine[g * ws_head + dv + 1] = l;
-      }
+      if (!alone && lane == 0) *reinterpret_cast<float2*>(ub + g * ws_head + RAP_MAX_SPLIT * dv4 + 2 * my_seg) = make_float2(mm, l);
     }
     if (!alone) {
       // ---- who delivers a unit's last partial joins them, in order ----
@@ -454,18 +466,16 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         if (p.n_pre && !joined) pdl_wait();        // the prefix's partials come from the launch before
         joined = true;
         __threadfence();
-        const float* from = ub + (size_t)(p.n_pre - n_pre) * (dv + 2);
-        const int n = n_pre + n_seg;               // <= RAP_MAX_SPLIT
-        float* wgt = red;                          // [G][RAP_MAX_SPLIT] weights, then the heads' reciprocals
+        const int s_first = p.n_pre - n_pre, n = n_pre + n_seg;      // <= RAP_MAX_SPLIT
+        float* wgt = red;                          // [G][RAP_MAX_SPLIT] weights over their sum
         for (int g = warp; g < G; g += NW) {
-          const float* gb = from + (size_t)g * ws_head;
+          const float2* ml = reinterpret_cast<const float2*>(ub + g * ws_head + RAP_MAX_SPLIT * dv4) + s_first;
           float mv[2], lv[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const int sg = lane + 32 * k;
-            lv[k] = sg < n ? __ldcg(gb + (size_t)sg * (dv + 2) + dv + 1) : 0.f;
-            mv[k] = sg < n ? __ldcg(gb + (size_t)sg * (dv + 2) + dv) : -INFINITY;
-            if (lv[k] == 0.f) mv[k] = -INFINITY;
+            const float2 x = lane + 32 * k < n ? __ldcg(ml + lane + 32 * k) : make_float2(-INFINITY, 0.f);
+            lv[k] = x.y;
+            mv[k] = x.y != 0.f ? x.x : -INFINITY;
           }
           float M = fmaxf(mv[0], mv[1]);
 #pragma unroll
@@ -473,38 +483,49 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
           float den = 0.f;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const float wk = lv[k] != 0.f ? exp2f(mv[k] - M) : 0.f;
-            wgt[g * RAP_MAX_SPLIT + lane + 32 * k] = wk;
-            den += wk * lv[k];
+            mv[k] = lv[k] != 0.f ? exp2f(mv[k] - M) : 0.f;
+            den += mv[k] * lv[k];
           }
 #pragma unroll
           for (int s2 = 16; s2 > 0; s2 >>= 1) den += __shfl_xor_sync(0xffffffffu, den, s2);
-          if (lane == 0) wgt[G * RAP_MAX_SPLIT + g] = den != 0.f ? 1.f / den : 0.f;
+          const float inv = den != 0.f ? 1.f / den : 0.f;
+          wgt[g * RAP_MAX_SPLIT + lane] = mv[0] * inv;
+          wgt[g * RAP_MAX_SPLIT + lane + 32] = mv[1] * inv;
         }
         __syncthreads();
-        for (int i = tid; i < G * dv; i += THREADS) {
-          const int g = i / dv, c = i - g * dv;
-          const float* gb = from + (size_t)g * ws_head + c;
-          float num = 0.f;
-          for (int s0 = 0; s0 < n; s0 += 16) {     // sixteen loads in flight
-            float av[16];
+        const int c4 = dv4 >> 2;
+        for (int i = tid; i < G * c4; i += THREADS) {     // four channels of a head
+          const int g = i / c4, c = 4 * (i - g * c4);
+          const float* gb = ub + g * ws_head + s_first * dv4 + c;
+          const float* wg = wgt + g * RAP_MAX_SPLIT;
+          float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int s0 = 0; s0 < n; s0 += 8) {      // eight loads in flight
+            float4 av[8];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) av[k] = s0 + k < n ? __ldcg(gb + (size_t)(s0 + k) * (dv + 2)) : 0.f;
+            for (int k = 0; k < 8; ++k) av[k] = __ldcg(reinterpret_cast<const float4*>(gb + min(s0 + k, n - 1) * dv4));
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float wk = s0 + k < n ? wgt[g * RAP_MAX_SPLIT + s0 + k] : 0.f;
-              if (wk != 0.f) num += wk * av[k];
+            for (int k = 0; k < 8; ++k) {
+              const float wk = s0 + k < n ? wg[s0 + k] : 0.f;
+              num.x = fmaf(wk, av[k].x, num.x);
+              num.y = fmaf(wk, av[k].y, num.y);
+              num.z = fmaf(wk, av[k].z, num.z);
+              num.w = fmaf(wk, av[k].w, num.w);
             }
           }
-          out[i] = num * wgt[G * RAP_MAX_SPLIT + g];
+          float* og = out + (size_t)g * dv + c;
+          og[0] = num.x;
+          if (c + 1 < dv) og[1] = num.y;
+          if (c + 2 < dv) og[2] = num.z;
+          if (c + 3 < dv) og[3] = num.w;
         }
         if (tid == 0) p.unit_cnt[unit] = 0;        // ready for the next call
       }
     }
+    }
     // ---- the next unit, from its first block ----
-    cur += n_my;
+    unit_start += u.n + WS_OWN;
+    cur = unit_start;
     if (cur >= hi) break;
-    unit_start += u.n;
     if (++h == p.Hkv) {
       h = 0;
       if (++b >= p.B) break;
