@@ -236,3 +236,6 @@ rap_status rap_launch_prefill_window(rap_ctx* ctx, const rap_win_args& a, cudaSt
 rap_status rap_launch_decode_shared(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st);
 bool rap_win_scan_takes(const rap_win_args& a);                                                            // rap_window_scan.cu
 rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, cudaStream_t st);
+bool rap_win_tc_takes(const rap_win_args& a);                                                              // rap_window_tc.cu
+rap_status rap_launch_win_tc(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st);
+rap_status rap_launch_win_prefix(rap_ctx* ctx, const rap_win_args& a, int* n_pre, cudaStream_t st);

@@ -312,5 +312,12 @@ rap_status rap_launch_build_slots(rap_ctx* ctx, int B, const int32_t* seq_len, c
 rap_status rap_launch_decode_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) {
   return rap_win_scan_takes(a) ? rap_launch_win_scan(ctx, a, 0, st) : launch_generic(ctx, a, st);
 }
-rap_status rap_launch_prefill_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) { return launch_generic(ctx, a, st); }
-rap_status rap_launch_decode_shared(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) { return launch_generic(ctx, a, st); }
+rap_status rap_launch_prefill_window(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) {
+  return rap_win_tc_takes(a) ? rap_launch_win_tc(ctx, a, st) : launch_generic(ctx, a, st);
+}
+rap_status rap_launch_decode_shared(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) {
+  if (!rap_win_tc_takes(a) || !rap_win_scan_takes(a)) return launch_generic(ctx, a, st);
+  int n_pre = 0;
+  const rap_status s = rap_launch_win_prefix(ctx, a, &n_pre, st);
+  return s == RAP_OK ? rap_launch_win_scan(ctx, a, n_pre, st) : s;
+}

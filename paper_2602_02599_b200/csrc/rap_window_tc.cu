@@ -1,0 +1,604 @@
+// Attention of many queries over the same cache rows on tcgen05: rap_prefill_attn_window (the rows are a ragged block's new
+// tokens) and the shared prefixes of rap_decode_attn_shared (the rows are the sequences of a group), for bf16 heads of up to
+// 128 dims and channels.
+//
+// A CTA takes 256 rows of one (sequence or group, KV head) as two query tiles of 128, a row being a (token, query head) pair:
+// the G query heads of a KV head sit side by side, so a block of 64 tokens with G = 4 fills both tiles, its rows see nearly the
+// same window, and a staged K / V tile serves all of them.  It walks the 64-row key tiles that any of its rows sees: the sinks,
+// then the window from the oldest visible position on (or one run from 0 where they meet).
+//   S_X  = Q_X K^T   tcgen05.mma (M = 128, N = 64, K = 2P in steps of 16), accumulator in tensor memory, double buffered
+//   P_X  = 2^(S - m) one thread per row: 64 logits in registers, masked only in tiles that reach an edge, lazy running maximum;
+//                    every weight leaves as two bf16 numbers, its rounding and the remainder (17 bits: outputs are fp32 and one
+//                    bf16 would put 1e-3 of error on them), which fill the 64 columns that the logits came from
+//   O_X += P_X V     A = P from tensor memory: eight steps of 16, the roundings' four and the remainders' four over the same V
+// Cache rows are not multiples of 16 bytes, so no tensor map describes them: four warps stage K and V with 4-byte cp.async
+// into rings of five 128-byte-swizzled tiles (K as stored is the K-major operand, V as stored the N-major one).  Odd d_v': rows
+// start on a half word, V goes through registers, two words and a byte permute each.  A rolling cache maps a position to its
+// row; a tile that does not cross the seam is one run of rows.
+// A K / V tile of 23 KB takes (4 P + 8 d_v') 64 cycles of the tensor pipe per 128 rows and 64 x 128 / 16 of the exponential
+// units, 576 and 512 cycles at P = 45: both, and the issue slots around them, bound it; HBM only below 128 rows.
+// Roles meet on mbarriers only; every wait is bounded and gives up early once another role has given up.
+#include <math.h>
+
+#include "rap_tc_common.cuh"
+#include "rap_window_common.cuh"
+
+namespace {
+
+constexpr int WT_KT = 64;                              // keys per tile
+constexpr int WT_THREADS = 448;                        // 8 softmax warps, 2 that issue MMAs, 2 that stage K, 2 that stage V
+constexpr int WT_STAGES = 5;
+constexpr int WT_Q_BYTES = 2 * 128 * 128;              // [128 rows][<= 128 dims]: two 64-element atom columns
+constexpr int WT_KV_BYTES = 2 * WT_KT * 128;           // [64 keys][<= 128 dims or channels]
+constexpr int WT_TAIL = 320;                           // mbarriers, TMEM address, give-up flag
+constexpr int WT_SMEM = 2 * WT_Q_BYTES + 2 * WT_STAGES * WT_KV_BYTES + WT_TAIL;
+
+struct WtParams {
+  const __nv_bfloat16* q;      // [rows][Hq][P2]
+  const __nv_bfloat16* k;      // [units][Hkv][S_cap][P2]
+  const __nv_bfloat16* v;      // [units][Hkv][S_cap][dv]
+  const int32_t* start;        // [units + 1]: first token (or sequence) of a unit in q
+  const int32_t* len;          // [units]: length with the new tokens, or prefix length
+  float* out;                  // [rows][Hq][dv]
+  float* ws;                   // partials (win_partial_floats) when split
+  int32_t* status;
+  int units, rows, Hq, Hkv, G, P2, dv, S_cap, n_sink, window, n_split;
+  float qscale;                // log2(e) / sqrt(D)
+};
+
+__device__ __forceinline__ void wt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
+// DK = k-steps of Q K^T (ceil(2P / 16)); NVP = d_v' rounded up to a multiple of 32 (N of the second MMA).
+// PREFIX: the rows are the sequences of group `unit`, all of which see all `len` rows of its cache, and the partials go to the
+// workspace; otherwise the rows are new tokens of sequence `unit`.
+template <int DK, int NVP, bool PREFIX>
+__global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p) {
+  extern __shared__ unsigned char wt_raw[];
+  unsigned char* smem = wt_raw + ((1024u - (pt_smem(wt_raw) & 1023u)) & 1023u);
+  unsigned char* q_s = smem;                                   // Q_A, Q_B
+  unsigned char* k_s = q_s + 2 * WT_Q_BYTES;                   // ring of K tiles
+  unsigned char* v_s = k_s + WT_STAGES * WT_KV_BYTES;          // ring of V tiles (N-major)
+  unsigned char* tail = v_s + WT_STAGES * WT_KV_BYTES;
+  const uint32_t bar_fk = pt_smem(tail), bar_ek = bar_fk + 8 * WT_STAGES, bar_fv = bar_ek + 8 * WT_STAGES,
+                 bar_ev = bar_fv + 8 * WT_STAGES, bar_s = bar_ev + 8 * WT_STAGES /* [X][2] */, bar_p = bar_s + 32 /* [X][2] */,
+                 bar_o = bar_p + 32 /* [X] */, bar_end = bar_o + 16 /* [X] */;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 32 * WT_STAGES + 96);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 32 * WT_STAGES + 100);
+  static_assert(32 * WT_STAGES + 104 <= WT_TAIL, "barriers and flags fit the tail");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = p.G, h = blockIdx.y;
+  if constexpr (PREFIX) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the own rows' scan may start where SMs come free
+
+  // ---- which unit, which of its rows: every warp walks the units' row counts, 256 rows a block ----
+  int unit = -1, q0 = 0;
+  for (int u0 = 0, carry = 0; u0 < p.units; u0 += 32) {
+    const int u = u0 + lane;
+    int n = 0;
+    if (u < p.units) {
+      const int s0 = min(max(p.start[u], 0), p.rows), s1 = min(max(p.start[u + 1], s0), p.rows);
+      n = ((s1 - s0) * G + 255) >> 8;
+    }
+    int x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, carry + x > (int)blockIdx.x);
+    if (past) {
+      const int l = __ffs(past) - 1;
+      unit = u0 + l;
+      q0 = ((int)blockIdx.x - carry - __shfl_sync(0xffffffffu, x - n, l)) * 256;
+      break;
+    }
+    carry += __shfl_sync(0xffffffffu, x, 31);
+  }
+  if (unit < 0) return;                                        // fewer row blocks than CTAs
+  const int first = min(max(p.start[unit], 0), p.rows);
+  const int n_tok = min(max(p.start[unit + 1], first), p.rows) - first, n_rows = n_tok * G;
+
+  // ---- the key tiles: n_st of sinks, then 64 rows each from position `base` on; nt[X] of them for query tile X ----
+  const int len = PREFIX ? min(max(p.len[unit], 0), p.S_cap) : max(p.len[unit], 0);
+  const int pos0 = len - n_tok;                                // position of the block's first token
+  int n_st = 0, base = 0, jend, nt[2], pmin[2], pmax[2], t_first = 0;
+#pragma unroll
+  for (int X = 0; X < 2; ++X) {
+    const int r0 = q0 + 128 * X, r1 = min(n_rows, r0 + 128) - 1;
+    pmin[X] = pos0 + r0 / G;
+    pmax[X] = r0 < n_rows ? pos0 + r1 / G : -1;
+  }
+  if constexpr (PREFIX) {
+    const int all = (len + WT_KT - 1) / WT_KT, per = (all + p.n_split - 1) / p.n_split;
+    t_first = min(all, (int)blockIdx.z * per);
+    jend = len;
+#pragma unroll
+    for (int X = 0; X < 2; ++X) nt[X] = q0 + 128 * X < n_rows ? min(all, t_first + per) - t_first : 0;
+  } else {
+    const int old = (int)max(0LL, (long long)pmin[0] - p.window + 1);            // the oldest position in a window
+    if (old > p.n_sink) {
+      n_st = (p.n_sink + WT_KT - 1) / WT_KT;
+      base = old;
+    }
+    jend = max(pmax[0], pmax[1]) + 1;
+#pragma unroll
+    for (int X = 0; X < 2; ++X) nt[X] = pmax[X] >= 0 ? n_st + (pmax[X] - base) / WT_KT + 1 : 0;
+  }
+  const int n_max = max(nt[0], nt[1]);
+  const __nv_bfloat16* kg = p.k + ((size_t)unit * p.Hkv + h) * (size_t)p.S_cap * p.P2;
+  const __nv_bfloat16* vg = p.v + ((size_t)unit * p.Hkv + h) * (size_t)p.S_cap * p.dv;
+  // first position of a tile, and the position behind its last one
+  auto tile_at = [&](int tile, int& j0, int& j1) {
+    if (PREFIX) {
+      j0 = (t_first + tile) * WT_KT;
+      j1 = jend;
+    } else {
+      j0 = tile < n_st ? tile * WT_KT : base + (tile - n_st) * WT_KT;
+      j1 = tile < n_st ? p.n_sink : jend;
+    }
+  };
+
+  if (tid == 0) {
+    for (int i = 0; i < WT_STAGES; ++i) {
+      pt_mbar_init(bar_fk + 8 * i, 64);
+      pt_mbar_init(bar_ek + 8 * i, 2);               // both MMA-issuing lanes release a buffer
+      pt_mbar_init(bar_fv + 8 * i, 64);
+      pt_mbar_init(bar_ev + 8 * i, 2);
+    }
+    for (int i = 0; i < 4; ++i) {
+      pt_mbar_init(bar_s + 8 * i, 1);
+      pt_mbar_init(bar_p + 8 * i, 128);              // one barrier per S buffer: the softmax may be a tile ahead of who waits for it
+    }
+    for (int X = 0; X < 2; ++X) pt_mbar_init(bar_o + 8 * X, 1);
+    pt_mbar_init(bar_end, 1);
+    pt_mbar_init(bar_end + 8, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pt_smem(tmem_slot)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // Q and K pad dims are zero in both (V's pad channels only reach accumulator columns that nothing reads)
+  for (int i = tid; i < (2 * WT_Q_BYTES + WT_STAGES * WT_KV_BYTES) / 16; i += WT_THREADS)
+    reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+  const int kw = p.P2 >> 1;                          // 4-byte words per q / K row
+  {
+    // a warp takes rows warp, warp + 14, ...; the loads of ten rows are in flight before the first store
+    constexpr int NWARP = WT_THREADS / 32, QB = 10;
+    const uint32_t* qsrc = reinterpret_cast<const uint32_t*>(p.q) + ((size_t)first * p.Hq + (size_t)h * G) * kw;
+#pragma unroll 1
+    for (int r0 = warp; r0 < 256; r0 += NWARP * QB) {
+      uint32_t qv[QB][2];
+#pragma unroll
+      for (int u = 0; u < QB; ++u) {
+        const int r = r0 + NWARP * u, n = q0 + r;
+        const bool ok = r < 256 && n < n_rows;
+        const int t = n / G;
+#pragma unroll
+        for (int sl = 0; sl < 2; ++sl) {
+          const int w = lane + 32 * sl;
+          qv[u][sl] = (ok && w < kw) ? __ldg(qsrc + ((size_t)t * p.Hq + (n - t * G)) * kw + w) : 0u;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < QB; ++u) {
+        const int r = r0 + NWARP * u;
+        if (r < 256 && q0 + r < n_rows) {
+          unsigned char* qd = q_s + (r >> 7) * WT_Q_BYTES;
+#pragma unroll
+          for (int sl = 0; sl < 2; ++sl) {
+            const int w = lane + 32 * sl;
+            if (w < kw) *reinterpret_cast<uint32_t*>(qd + pt_off(r & 127, 2 * w, 128)) = qv[u][sl];
+          }
+        }
+      }
+    }
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = *tmem_slot;             // S_X(t): columns 128 X + 64 (t & 1); O_X: columns 256 + 128 X
+  constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(WT_KT >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+  constexpr uint32_t IDESC_O = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(NVP >> 3) << 17) |
+                               ((uint32_t)(128 >> 4) << 24);
+  auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+    if (pt_test_wait(bar, parity)) return true;
+    for (uint32_t i = 0; i < PT_WAIT_LIMIT; ++i) {
+      if (pt_try_wait(bar, parity)) return true;
+      if ((i & 15u) == 15u && *abort_flag) return false;
+    }
+    *abort_flag = 1;
+    return false;
+  };
+
+  float l_run = 0.f, m_ref = -INFINITY;
+  const int X = (warp >> 2) & 1;                     // softmax group = query tile
+  const int row = (warp & 3) * 32 + lane;
+  const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+  const uint32_t tmem_o = tmem_base + 256 + 128 * X;
+  if (warp >= 10) {
+    // ================= producers: warps 10-11 stage K, warps 12-13 stage V, a row of every two each =================
+    const bool is_v = warp >= 12;
+    const int pw = (warp - 10) & 1;
+    const int rowlen = is_v ? p.dv : p.P2;
+    const unsigned char* src0 = reinterpret_cast<const unsigned char*>(is_v ? vg : kg);
+    unsigned char* ring = is_v ? v_s : k_s;
+    const uint32_t bar_f = is_v ? bar_fv : bar_fk, bar_e = is_v ? bar_ev : bar_ek;
+    const bool half = (rowlen & 1) != 0;             // rows start on a half word: through registers
+    uint32_t swz[4][2];
+    const int words = (rowlen + 1) >> 1;
+#pragma unroll
+    for (int sl = 0; sl < 2; ++sl)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) swz[c][sl] = pt_swz2(4 * (lane + 32 * sl), (pw + 2 * c) & 7);
+    const bool one = lane < words, two = lane + 32 < words;
+    const int R = p.S_cap - p.n_sink;
+    int stg = 0, use = 0;
+    for (int tile = 0; tile < n_max; ++tile) {
+      int j0, j1;
+      tile_at(tile, j0, j1);
+      if (use > 0 && !wait(bar_e + 8 * stg, (use - 1) & 1)) break;
+      const uint32_t du = pt_smem(ring + stg * WT_KV_BYTES);
+      const int rows_ok = min(WT_KT, j1 - j0);
+      // the tile's rows are one run from row s0 on unless it crosses the seam of a rolling cache
+      int s0 = j0;
+      bool run = j0 + rows_ok <= p.S_cap;
+      if (!run && j0 >= p.n_sink) {
+        s0 = p.n_sink + (j0 - p.n_sink) % R;
+        run = s0 + rows_ok <= p.S_cap;
+      }
+      auto slot_of = [&](int r) { return run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap); };
+      if (half) {
+        // eight rows a batch: all their words (and the ones behind, for rows that start in the middle of a word) in flight
+#pragma unroll 1
+        for (int i0 = 0; i0 < WT_KT / 2; i0 += 8) {
+          uint32_t a[8][2], b[8][2];
+          int odd = 0;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const int r = pw + 2 * (i0 + u);
+            const bool ok = r < rows_ok;
+            const int s = ok ? slot_of(r) : 0;
+            const uint32_t* src = reinterpret_cast<const uint32_t*>(src0 + (((size_t)s * (size_t)(2 * rowlen)) & ~(size_t)3));
+            odd |= (s & 1) << u;
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
+              const int w = lane + 32 * sl;
+              a[u][sl] = ok && w < words ? __ldg(src + w) : 0u;
+              b[u][sl] = ok && (s & 1) && w + 1 < words ? __ldg(src + w + 1) : 0u;
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const int r = pw + 2 * (i0 + u);
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
+              const uint32_t v = (odd >> u) & 1 ? __funnelshift_r(a[u][sl], b[u][sl], 16) : a[u][sl];
+              if (sl == 0 ? one : two)
+                *reinterpret_cast<uint32_t*>(ring + stg * WT_KV_BYTES + r * 128 + swz[u & 3][sl]) = v;
+            }
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_f + 8 * stg) : "memory");
+      } else {
+        if (run && rows_ok == WT_KT) {
+          // a full tile in one run: no predicates, running pointers
+          const unsigned char* sp = src0 + (size_t)(s0 + pw) * (size_t)(2 * rowlen) + 4 * lane;
+          uint32_t db = du + (uint32_t)pw * 128u;
+#pragma unroll 4
+          for (int i = 0; i < WT_KT / 2; ++i) {
+            if (one) pt_cp4(db + swz[i & 3][0], sp, 4);
+            if (two) pt_cp4(db + swz[i & 3][1], sp + 128, 4);
+            sp += 4 * rowlen;                          // two rows on
+            db += 256;
+          }
+        } else {
+#pragma unroll 4
+          for (int i = 0; i < WT_KT / 2; ++i) {
+            const int r = pw + 2 * i;
+            const bool ok = r < rows_ok;               // rows behind the end: zeros, nothing is read
+            const uint32_t* src = reinterpret_cast<const uint32_t*>(src0 + (size_t)(ok ? slot_of(r) : 0) * (size_t)(2 * rowlen));
+            const uint32_t rb = du + (uint32_t)r * 128u;
+            if (one) pt_cp4(rb + swz[i & 3][0], src + lane, ok ? 4 : 0);
+            if (two) pt_cp4(rb + swz[i & 3][1], src + lane + 32, ok ? 4 : 0);
+          }
+        }
+        // the arrival is triggered by the completion of this thread's copies: go on to the next tile
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_f + 8 * stg) : "memory");
+      }
+      if (++stg == WT_STAGES) { stg = 0; ++use; }
+    }
+    // copies that nobody waited for (a role gave up) have landed before the shared memory is used for the output
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp >= 8) {
+    // ================= MMA issue: lane 0 of warp 8 for query tile A, of warp 9 for query tile B =================
+    // A buffer of the rings is free when both lanes have committed past it; a lane whose tile needs no more keys keeps
+    // arriving in step (after the buffer was filled), so the phases stay aligned.
+    if (lane == 0 && n_max > 0) {
+      const int Y = warp - 8, n_y = Y ? nt[1] : nt[0];
+      const uint32_t tmem_sy = tmem_base + 128u * (uint32_t)Y, tmem_oy = tmem_base + 256u + 128u * (uint32_t)Y;
+      constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+      constexpr uint32_t BUF16 = (uint32_t)WT_KV_BYTES >> 4;
+      uint32_t q_lo[DK];
+#pragma unroll
+      for (int ks = 0; ks < DK; ++ks)
+        q_lo[ks] = (((pt_smem(q_s + Y * WT_Q_BYTES) + (uint32_t)((ks >> 2) * 16384 + (ks & 3) * 32)) & 0x3FFFFu) >> 4) | (1u << 16);
+      const uint32_t k_lo0 = ((pt_smem(k_s) & 0x3FFFFu) >> 4) | (1u << 16);
+      const uint32_t v_lo0 = ((pt_smem(v_s) & 0x3FFFFu) >> 4) | ((8192u >> 4) << 16);
+      auto issue_s = [&](uint32_t kbuf, uint32_t sbuf) {     // S into buffer sbuf from K buffer kbuf
+        const uint32_t kb = k_lo0 + kbuf * BUF16, td = tmem_sy + 64u * sbuf;
+#pragma unroll
+        for (int ks = 0; ks < DK; ++ks)
+          pt_mma2(td, q_lo[ks], kb + (uint32_t)(((ks >> 2) * 8192 + (ks & 3) * 32) >> 4), DESC_HI, IDESC_S, ks > 0 ? 1u : 0u);
+        pt_commit(bar_s + 8 * (2 * Y + sbuf));
+      };
+      auto release = [&](uint32_t bar, bool issued) {   // after MMAs: when they complete; otherwise at once
+        if (issued) pt_commit(bar);
+        else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+      };
+      bool ok = wait(bar_fk, 0);
+      if (ok) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (n_y > 0) issue_s(0, 0);
+        release(bar_ek, n_y > 0);
+      }
+      uint32_t kbuf = 1, kpar = 0;       // ring position and phase of K tile + 1
+      uint32_t vbuf = 0, vpar = 0;       // of V tile
+      for (int tile = 0; ok && tile < n_max; ++tile) {
+        const uint32_t sb = (uint32_t)tile & 1u;
+        if (tile + 1 < n_max) {
+          if (!wait(bar_fk + 8 * kbuf, kpar)) { ok = false; break; }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          if (tile + 1 < n_y) issue_s(kbuf, sb ^ 1u);
+          release(bar_ek + 8 * kbuf, tile + 1 < n_y);
+          if (++kbuf == WT_STAGES) { kbuf = 0; kpar ^= 1u; }
+        }
+        if (!wait(bar_fv + 8 * vbuf, vpar)) { ok = false; break; }
+        if (tile < n_y) {
+          if (!wait(bar_p + 8 * (2 * Y + sb), (uint32_t)(tile >> 1) & 1u)) { ok = false; break; }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t vb = v_lo0 + vbuf * BUF16, ta = tmem_sy + 64u * sb;
+#pragma unroll
+          for (int ks = 0; ks < WT_KT / 8; ++ks)    // the roundings (32 columns of two keys), then the remainders, over the same V
+            pt_mma_ts2(tmem_oy, ta + 8u * (uint32_t)ks, vb + (uint32_t)((ks & 3) * 2048 >> 4), DESC_HI, IDESC_O,
+                       (tile > 0 || ks > 0) ? 1u : 0u);
+          pt_commit(bar_o + 8 * Y);
+        }
+        release(bar_ev + 8 * vbuf, tile < n_y);
+        if (++vbuf == WT_STAGES) { vbuf = 0; vpar ^= 1u; }
+      }
+      // every MMA issued above has completed before tensor memory is released
+      pt_commit(bar_end + 8 * Y);
+      wait(bar_end + 8 * Y, 0);
+    }
+    __syncwarp();
+  } else {
+    // ================= softmax group X: one thread per row of query tile X =================
+    const int n = q0 + 128 * X + row;
+    const int pos = n < n_rows ? pos0 + n / G : -1;
+    const bool active = q0 + 128 * X + (warp & 3) * 32 < n_rows;       // some row of this warp is one
+    const int n_my = X ? nt[1] : nt[0], p_min = X ? pmin[1] : pmin[0], p_max = X ? pmax[1] : pmax[0];
+    bool rows_ok = true;
+    for (int tile = 0; tile < n_my; ++tile) {
+      int j0, j1;
+      tile_at(tile, j0, j1);
+      const uint32_t trow = tmem_base + 128u * (uint32_t)X + 64u * (uint32_t)(tile & 1) + lane_off;
+      if (!__all_sync(0xffffffffu, wait(bar_s + 8 * (2 * X + (tile & 1)), (tile >> 1) & 1))) { rows_ok = false; break; }
+      if (active) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        uint32_t r[64];
+        pt_ld32_nowait(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
+        pt_ld32_nowait(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        // nothing of the tile is hidden from any row of this query tile
+        const bool whole = PREFIX ? j0 + WT_KT <= j1
+                                  : tile >= n_st && j0 + WT_KT - 1 <= p_min && j0 > p_max - p.window && j0 + WT_KT <= j1;
+        if (!whole) {
+          // columns [0, c1) of the tile, without those behind the sinks and before the window
+          const int c1 = PREFIX ? j1 - j0 : min(j1, pos + 1) - j0;
+          const int c_win = PREFIX ? 0 : (int)max(0LL, (long long)pos - p.window + 1 - j0), c_sink = PREFIX ? 0 : p.n_sink - j0;
+          auto below = [](int c) { return c <= 0 ? 0ull : c >= 64 ? ~0ull : (1ull << c) - 1; };
+          const uint64_t seen = below(c1) & (~below(c_win) | below(c_sink));
+          const uint32_t s_lo = (uint32_t)seen, s_hi = (uint32_t)(seen >> 32);
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (!((j < 32 ? s_lo : s_hi) & (1u << (j & 31)))) r[j] = 0xff800000u;      // -infinity: weight 0
+        }
+        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 64; ++j) mx4[j & 3] = fmaxf(mx4[j & 3], __uint_as_float(r[j]));
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.qscale;
+        float alpha = 1.f;
+        if (mx > m_ref + 8.f) {          // lazy reference maximum: weights stay <= 2^8
+          alpha = pt_ex2(m_ref - mx);
+          m_ref = mx;
+          l_run *= alpha;
+        }
+        const float nm = m_ref == -INFINITY ? 0.f : -m_ref;
+        if (tile > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+          // rare: rescale this warp's accumulator rows in tensor memory, once the previous tile's update is in
+          if (!__all_sync(0xffffffffu, wait(bar_o + 8 * X, (tile - 1) & 1))) { rows_ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+          for (int c0 = 0; c0 < NVP; c0 += 32) {
+            uint32_t oc[32];
+            pt_ld32(tmem_o + lane_off + c0, oc);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) oc[j] = __float_as_uint(__uint_as_float(oc[j]) * alpha);
+            pt_st32(tmem_o + lane_off + c0, oc);
+          }
+        }
+        // weights, two a packed instruction: p = rounding + remainder, each half of a tile column; the row sum takes p itself
+        uint64_t qs2, nm2, neg1, l2[2] = {0ull, 0ull};
+        asm("mov.b64 %0, {%1, %1};" : "=l"(qs2) : "f"(p.qscale));
+        asm("mov.b64 %0, {%1, %1};" : "=l"(nm2) : "f"(nm));
+        asm("mov.b64 %0, {%1, %1};" : "=l"(neg1) : "f"(-1.f));
+#pragma unroll
+        for (int g8 = 0; g8 < 4; ++g8) {
+          uint32_t hi[8], lo[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int j = 16 * g8 + 2 * k;
+            uint64_t s2, x2, p2, h2;
+            asm("mov.b64 %0, {%1, %2};" : "=l"(s2) : "r"(r[j]), "r"(r[j + 1]));
+            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x2) : "l"(s2), "l"(qs2), "l"(nm2));
+            float x0, x1;
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
+            const float p0 = pt_ex2(x0), p1 = pt_ex2(x1);
+            asm("mov.b64 %0, {%1, %2};" : "=l"(p2) : "f"(p0), "f"(p1));
+            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(l2[k & 1]) : "l"(l2[k & 1]), "l"(p2));
+            const __nv_bfloat162 v2 = __floats2bfloat162_rn(p0, p1);
+            hi[k] = *reinterpret_cast<const uint32_t*>(&v2);
+            asm("mov.b64 %0, {%1, %2};" : "=l"(h2) : "r"(hi[k] << 16), "r"(hi[k] & 0xffff0000u));
+            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x2) : "l"(h2), "l"(neg1), "l"(p2));
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
+            const __nv_bfloat162 w2 = __floats2bfloat162_rn(x0, x1);
+            lo[k] = *reinterpret_cast<const uint32_t*>(&w2);
+          }
+          // over the columns that the logits came from; the next S into this buffer is issued after the MMA that reads these
+          wt_st8(trow + 8 * g8, hi);
+          wt_st8(trow + 32 + 8 * g8, lo);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float a0, a1;
+          asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(l2[k]));
+          l_run += a0 + a1;
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      }
+      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_p + 8 * (2 * X + (tile & 1))) : "memory");
+    }
+    if (rows_ok && n_my > 0) __all_sync(0xffffffffu, wait(bar_o + 8 * X, (n_my - 1) & 1));
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  const bool timed_out = *abort_flag != 0;
+  if (timed_out && tid == 0) win_report(p.status, RAP_ETIMEOUT, 0x60000000 | ((int)blockIdx.x & 0xffffff));
+  // The tiles are free now (every MMA has completed, every copy has landed).  A thread owns a row in tensor memory, but a row
+  // of the output is contiguous in global memory: the rows go through shared memory (rows of NVP + 1 floats: the
+  // row-per-thread stores hit 32 banks) and leave as whole rows, one warp per row.
+  float* o_s = reinterpret_cast<float*>(smem);
+  constexpr int OS = NVP + 1;
+  static_assert(256 * OS * 4 <= WT_SMEM - WT_TAIL, "the output tile fits the freed tiles");
+  const int dv4 = (p.dv + 3) & ~3;
+  const size_t ws_head = win_partial_floats(p.dv);
+  if (warp < 8 && !timed_out) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const int n = q0 + 128 * X + row;
+    const float f = PREFIX ? 1.f : l_run != 0.f ? 1.f / l_run : 0.f;
+    float* orow = o_s + (size_t)(128 * X + row) * OS;
+    if ((X ? nt[1] : nt[0]) > 0) {
+#pragma unroll 1
+      for (int c0 = 0; c0 < NVP; c0 += 32) {
+        uint32_t oc[32];
+        pt_ld32(tmem_o + lane_off + c0, oc);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) orow[c0 + j] = l_run != 0.f ? __uint_as_float(oc[j]) * f : 0.f;
+      }
+    } else {
+      for (int c = 0; c < p.dv; ++c) orow[c] = 0.f;            // nothing to see
+    }
+    if (PREFIX && n < n_rows) {
+      const int t = n / G;
+      float* ml = p.ws + ((size_t)(first + t) * p.Hq + (size_t)h * G + (n - t * G)) * ws_head + RAP_MAX_SPLIT * dv4 + 2 * blockIdx.z;
+      *reinterpret_cast<float2*>(ml) = make_float2(m_ref, l_run);
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  }
+  __syncthreads();
+  if (!timed_out) {
+    for (int r = warp; r < 256 && q0 + r < n_rows; r += WT_THREADS / 32) {
+      const int n = q0 + r, t = n / G;
+      const size_t head = (size_t)(first + t) * p.Hq + (size_t)h * G + (n - t * G);
+      float* dst = PREFIX ? p.ws + head * ws_head + (size_t)blockIdx.z * dv4 : p.out + head * p.dv;
+      const float* src = o_s + (size_t)r * OS;
+      for (int c = lane; c < p.dv; c += 32) dst[c] = src[c];
+    }
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+  }
+}
+
+template <int DK, int NVP, bool PREFIX>
+rap_status launch_wt(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
+  const int smem = WT_SMEM + 1024;
+  RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, win_tc_kernel<DK, NVP, PREFIX>, smem));
+  const dim3 grid(blocks, p.Hkv, p.n_split);
+  win_tc_kernel<DK, NVP, PREFIX><<<grid, WT_THREADS, smem, st>>>(p);
+  ctx->launches++;
+  RAP_CUDA_TRY(ctx, cudaGetLastError());
+  return RAP_OK;
+}
+template <bool PREFIX>
+rap_status launch_any(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
+  // steps and accumulator columns as the head needs them, in four sizes (a step more costs 3% at 90 dims)
+  const int dk = (p.P2 + 15) / 16, nvp = (p.dv + 31) / 32 * 32;
+  if (dk <= 4 && nvp <= 64) return launch_wt<4, 64, PREFIX>(ctx, p, blocks, st);
+  if (dk <= 6 && nvp <= 96) return launch_wt<6, 96, PREFIX>(ctx, p, blocks, st);
+  if (dk <= 7) return launch_wt<7, 128, PREFIX>(ctx, p, blocks, st);
+  return launch_wt<8, 128, PREFIX>(ctx, p, blocks, st);
+}
+
+WtParams base_params(rap_ctx* ctx, const rap_win_args& a) {
+  WtParams p = {};
+  p.q = (const __nv_bfloat16*)a.q; p.out = a.out; p.ws = ctx->d_attn_ws; p.status = ctx->d_status;
+  p.rows = a.T; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv; p.P2 = a.P2; p.dv = a.dv;
+  p.qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
+  p.n_split = 1;
+  return p;
+}
+
+}  // namespace
+
+bool rap_win_tc_takes(const rap_win_args& a) {
+  return a.dtype == RAP_BF16 && a.P2 <= 128 && a.dv <= 128 && a.Hkv <= 65535 && (long long)a.T * (a.Hq / a.Hkv) < (1LL << 31) - 256;
+}
+
+rap_status rap_launch_win_tc(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) {
+  WtParams p = base_params(ctx, a);
+  p.k = (const __nv_bfloat16*)a.k; p.v = (const __nv_bfloat16*)a.v; p.start = a.row_start; p.len = a.seq_len; p.units = a.B;
+  p.S_cap = a.S_cap; p.n_sink = a.n_sink; p.window = a.window;
+  // row blocks of 256: as many as T rows can make, one more for each sequence that may begin a block
+  const int seqs = a.B < a.T ? a.B : a.T;
+  const int blocks = (int)((long long)a.T * p.G / 256) + seqs;
+  return launch_any<false>(ctx, p, blocks, st);
+}
+
+// The prefixes' partials of rap_decode_attn_shared, *n_pre of them for each query head (0: the prefixes are empty)
+rap_status rap_launch_win_prefix(rap_ctx* ctx, const rap_win_args& a, int* n_pre, cudaStream_t st) {
+  *n_pre = 0;
+  if (a.h_prefix_max == 0) return RAP_OK;
+  WtParams p = base_params(ctx, a);
+  p.k = (const __nv_bfloat16*)a.kp; p.v = (const __nv_bfloat16*)a.vp; p.start = a.group_start; p.len = a.prefix_len; p.units = a.n_groups;
+  p.S_cap = a.S_pre; p.n_sink = 0; p.window = 0x7fffffff;
+  const int groups = a.n_groups < a.B ? a.n_groups : a.B;
+  const int blocks = (int)((long long)a.B * p.G / 256) + groups;
+  // the split that ends soonest: waves of one CTA an SM, each its tiles and about six tiles' worth of beginning and end
+  const long long tiles = (a.h_prefix_max + WT_KT - 1) / WT_KT, units = (long long)a.Hkv * ((long long)a.B * p.G / 256 + (groups > 1 ? groups : 1));
+  long long best = -1;
+  for (int s = 1; s <= 40 && s <= tiles; ++s) {
+    const long long cost = (units * s + ctx->sm_count - 1) / ctx->sm_count * ((tiles + s - 1) / s + 6);
+    if (best < 0 || cost < best) {
+      best = cost;
+      p.n_split = s;
+    }
+  }
+  *n_pre = p.n_split;
+  return launch_any<true>(ctx, p, blocks, st);
+}
