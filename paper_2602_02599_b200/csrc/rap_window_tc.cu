@@ -52,10 +52,30 @@ __device__ __forceinline__ void wt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
                : "memory");
 }
 
-// DK = k-steps of Q K^T (ceil(2P / 16)); NVP = d_v' rounded up to a multiple of 32 (N of the second MMA).
+__device__ __forceinline__ void wt_cp4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ float wt_max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ void wt_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// DK = k-steps of Q K^T (ceil(2P / 16)); NVP = columns of the second MMA, a multiple of 16 from d_v' on.  LSUM: NVP > d_v', and
+// column d_v' of every V tile holds the constant one, so that the row sums of the very weights that it multiplies come out of
+// the second MMA (a fifth of the softmax threads' instructions otherwise).
 // PREFIX: the rows are the sequences of group `unit`, all of which see all `len` rows of its cache, and the partials go to the
 // workspace; otherwise the rows are new tokens of sequence `unit`.
-template <int DK, int NVP, bool PREFIX>
+template <int DK, int NVP, bool LSUM, bool PREFIX>
 __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p) {
   extern __shared__ unsigned char wt_raw[];
   unsigned char* smem = wt_raw + ((1024u - (pt_smem(wt_raw) & 1023u)) & 1023u);
@@ -101,15 +121,18 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   const int first = min(max(p.start[unit], 0), p.rows);
   const int n_tok = min(max(p.start[unit + 1], first), p.rows) - first, n_rows = n_tok * G;
 
+  // row r of the block is query head row_g of token row_t: rows in [0, 264) over G <= 8 by a 16-bit reciprocal, exact there
+  const int t_base = q0 / G, t_rest = q0 - t_base * G, g_recip = (65536 + G - 1) / G;
+  auto row_t = [&](int r) { return t_base + (((t_rest + r) * g_recip) >> 16); };
+
   // ---- the key tiles: n_st of sinks, then 64 rows each from position `base` on; nt[X] of them for query tile X ----
   const int len = PREFIX ? min(max(p.len[unit], 0), p.S_cap) : max(p.len[unit], 0);
   const int pos0 = len - n_tok;                                // position of the block's first token
   int n_st = 0, base = 0, jend, nt[2], pmin[2], pmax[2], t_first = 0;
 #pragma unroll
   for (int X = 0; X < 2; ++X) {
-    const int r0 = q0 + 128 * X, r1 = min(n_rows, r0 + 128) - 1;
-    pmin[X] = pos0 + r0 / G;
-    pmax[X] = r0 < n_rows ? pos0 + r1 / G : -1;
+    pmin[X] = pos0 + row_t(128 * X);
+    pmax[X] = q0 + 128 * X < n_rows ? pos0 + row_t(min(n_rows - q0, 128 * X + 128) - 1) : -1;
   }
   if constexpr (PREFIX) {
     const int all = (len + WT_KT - 1) / WT_KT, per = (all + p.n_split - 1) / p.n_split;
@@ -163,39 +186,41 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // Q and K pad dims are zero in both (V's pad channels only reach accumulator columns that nothing reads)
-  for (int i = tid; i < (2 * WT_Q_BYTES + WT_STAGES * WT_KV_BYTES) / 16; i += WT_THREADS)
-    reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
-  __syncthreads();
   const int kw = p.P2 >> 1;                          // 4-byte words per q / K row
+  // pad dims are zero in Q and in K (V's pad channels only reach accumulator columns that nothing reads)
+  for (int i = tid; i < WT_STAGES * WT_KT * (8 * DK - kw); i += WT_THREADS) {
+    const int br = i / (8 * DK - kw), w = kw + i - br * (8 * DK - kw);
+    *reinterpret_cast<uint32_t*>(k_s + (br >> 6) * WT_KV_BYTES + (br & 63) * 128 + pt_swz2(4 * w, br & 7)) = 0u;
+  }
+  if constexpr (LSUM) {
+    // the ones: channel dv of all 64 rows of every V buffer (odd dv: the producers write it with the row's last word)
+    for (int i = tid; i < WT_STAGES * WT_KT; i += WT_THREADS) {
+      const int buf = i / WT_KT, r = i - buf * WT_KT;
+      *reinterpret_cast<uint32_t*>(v_s + buf * WT_KV_BYTES + r * 128 + pt_swz2(4 * (p.dv >> 1), r & 7)) = p.dv & 1 ? 0x3f800000u : 0x3f80u;
+    }
+  }
   {
     // a warp takes rows warp, warp + 14, ...; the loads of ten rows are in flight before the first store
     constexpr int NWARP = WT_THREADS / 32, QB = 10;
-    const uint32_t* qsrc = reinterpret_cast<const uint32_t*>(p.q) + ((size_t)first * p.Hq + (size_t)h * G) * kw;
+    const uint32_t* qsrc = reinterpret_cast<const uint32_t*>(p.q) + ((size_t)(first + t_base) * p.Hq + (size_t)h * G) * kw + lane;
 #pragma unroll 1
     for (int r0 = warp; r0 < 256; r0 += NWARP * QB) {
       uint32_t qv[QB][2];
 #pragma unroll
       for (int u = 0; u < QB; ++u) {
-        const int r = r0 + NWARP * u, n = q0 + r;
-        const bool ok = r < 256 && n < n_rows;
-        const int t = n / G;
-#pragma unroll
-        for (int sl = 0; sl < 2; ++sl) {
-          const int w = lane + 32 * sl;
-          qv[u][sl] = (ok && w < kw) ? __ldg(qsrc + ((size_t)t * p.Hq + (n - t * G)) * kw + w) : 0u;
-        }
+        const int r = r0 + NWARP * u, t = row_t(r) - t_base;
+        const bool ok = r < 256 && q0 + r < n_rows;
+        const uint32_t* src = qsrc + ((size_t)t * p.Hq + (t_rest + r - t * G)) * kw;
+        qv[u][0] = ok && lane < kw ? __ldg(src) : 0u;
+        qv[u][1] = ok && lane + 32 < kw ? __ldg(src + 32) : 0u;
       }
 #pragma unroll
       for (int u = 0; u < QB; ++u) {
         const int r = r0 + NWARP * u;
-        if (r < 256 && q0 + r < n_rows) {
-          unsigned char* qd = q_s + (r >> 7) * WT_Q_BYTES;
-#pragma unroll
-          for (int sl = 0; sl < 2; ++sl) {
-            const int w = lane + 32 * sl;
-            if (w < kw) *reinterpret_cast<uint32_t*>(qd + pt_off(r & 127, 2 * w, 128)) = qv[u][sl];
-          }
+        if (r < 256) {
+          unsigned char* qd = q_s + r * 128 + ((r >> 7) << 14) + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2);
+          if (lane < 8 * DK) *reinterpret_cast<uint32_t*>(qd) = qv[u][0];
+          if (lane + 32 < 8 * DK) *reinterpret_cast<uint32_t*>(qd + 128 * 128) = qv[u][1];
         }
       }
     }
@@ -280,7 +305,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
             const int r = pw + 2 * (i0 + u);
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl) {
-              const uint32_t v = (odd >> u) & 1 ? __funnelshift_r(a[u][sl], b[u][sl], 16) : a[u][sl];
+              uint32_t v = (odd >> u) & 1 ? __funnelshift_r(a[u][sl], b[u][sl], 16) : a[u][sl];
+              if (LSUM && lane + 32 * sl == words - 1) v = (v & 0xffffu) | 0x3f800000u;
               if (sl == 0 ? one : two)
                 *reinterpret_cast<uint32_t*>(ring + stg * WT_KV_BYTES + r * 128 + swz[u & 3][sl]) = v;
             }
@@ -292,13 +318,22 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         if (run && rows_ok == WT_KT) {
           // a full tile in one run: no predicates, running pointers
           const unsigned char* sp = src0 + (size_t)(s0 + pw) * (size_t)(2 * rowlen) + 4 * lane;
-          uint32_t db = du + (uint32_t)pw * 128u;
-#pragma unroll 4
-          for (int i = 0; i < WT_KT / 2; ++i) {
-            if (one) pt_cp4(db + swz[i & 3][0], sp, 4);
-            if (two) pt_cp4(db + swz[i & 3][1], sp + 128, 4);
-            sp += 4 * rowlen;                          // two rows on
-            db += 256;
+          const uint32_t db = du + (uint32_t)pw * 128u;
+          uint32_t d0[4], d1[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            d0[c] = db + swz[c][0] + 256u * c;
+            d1[c] = db + swz[c][1] + 256u * c;
+          }
+          if (one) {
+            const unsigned char* a = sp;
+#pragma unroll
+            for (int i = 0; i < WT_KT / 2; ++i, a += 4 * rowlen) wt_cp4(d0[i & 3] + (i >> 2) * 1024, a);
+          }
+          if (two) {
+            const unsigned char* a = sp;
+#pragma unroll
+            for (int i = 0; i < WT_KT / 2; ++i, a += 4 * rowlen) wt_cp4(d1[i & 3] + (i >> 2) * 1024, a + 128);
           }
         } else {
 #pragma unroll 4
@@ -386,7 +421,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   } else {
     // ================= softmax group X: one thread per row of query tile X =================
     const int n = q0 + 128 * X + row;
-    const int pos = n < n_rows ? pos0 + n / G : -1;
+    const int pos = n < n_rows ? pos0 + row_t(128 * X + row) : -1;
     const bool active = q0 + 128 * X + (warp & 3) * 32 < n_rows;       // some row of this warp is one
     const int n_my = X ? nt[1] : nt[0], p_min = X ? pmin[1] : pmin[0], p_max = X ? pmax[1] : pmax[0];
     bool rows_ok = true;
@@ -397,28 +432,42 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       if (!__all_sync(0xffffffffu, wait(bar_s + 8 * (2 * X + (tile & 1)), (tile >> 1) & 1))) { rows_ok = false; break; }
       if (active) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        uint32_t r[64];
-        pt_ld32_nowait(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
-        pt_ld32_nowait(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
         // nothing of the tile is hidden from any row of this query tile
         const bool whole = PREFIX ? j0 + WT_KT <= j1
                                   : tile >= n_st && j0 + WT_KT - 1 <= p_min && j0 > p_max - p.window && j0 + WT_KT <= j1;
         if (!whole) {
-          // columns [0, c1) of the tile, without those behind the sinks and before the window
+          // the few tiles at an edge: hidden logits become -infinity (weight 0) where they are, so that the tiles' common path
+          // knows no mask.  Seen are columns [0, c1), without those behind the sinks and before the window
           const int c1 = PREFIX ? j1 - j0 : min(j1, pos + 1) - j0;
           const int c_win = PREFIX ? 0 : (int)max(0LL, (long long)pos - p.window + 1 - j0), c_sink = PREFIX ? 0 : p.n_sink - j0;
           auto below = [](int c) { return c <= 0 ? 0ull : c >= 64 ? ~0ull : (1ull << c) - 1; };
           const uint64_t seen = below(c1) & (~below(c_win) | below(c_sink));
-          const uint32_t s_lo = (uint32_t)seen, s_hi = (uint32_t)(seen >> 32);
+#pragma unroll 1
+          for (int c = 0; c < 64; c += 16) {
+            uint32_t e[16];
+            wt_ld16(trow + c, e);
+            const uint32_t bits = (uint32_t)(seen >> c);
 #pragma unroll
-          for (int j = 0; j < 64; ++j)
-            if (!((j < 32 ? s_lo : s_hi) & (1u << (j & 31)))) r[j] = 0xff800000u;      // -infinity: weight 0
+            for (int j = 0; j < 16; ++j)
+              if (!(bits & (1u << j))) e[j] = 0xff800000u;
+            wt_st8(trow + c, *reinterpret_cast<uint32_t(*)[8]>(e));
+            wt_st8(trow + c + 8, *reinterpret_cast<uint32_t(*)[8]>(e + 8));
+          }
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         }
-        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        uint32_t r[64];
+        pt_ld32_nowait(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
+        pt_ld32_nowait(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        float mx4[4];
 #pragma unroll
-        for (int j = 0; j < 64; ++j) mx4[j & 3] = fmaxf(mx4[j & 3], __uint_as_float(r[j]));
-        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.qscale;
+        for (int c = 0; c < 4; ++c) {
+          mx4[c] = __uint_as_float(r[16 * c]);
+#pragma unroll
+          for (int j = 1; j < 15; j += 2) mx4[c] = wt_max3(mx4[c], __uint_as_float(r[16 * c + j]), __uint_as_float(r[16 * c + j + 1]));
+          mx4[c] = fmaxf(mx4[c], __uint_as_float(r[16 * c + 15]));
+        }
+        const float mx = fmaxf(wt_max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * p.qscale;
         float alpha = 1.f;
         if (mx > m_ref + 8.f) {          // lazy reference maximum: weights stay <= 2^8
           alpha = pt_ex2(m_ref - mx);
@@ -431,37 +480,42 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           if (!__all_sync(0xffffffffu, wait(bar_o + 8 * X, (tile - 1) & 1))) { rows_ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-          for (int c0 = 0; c0 < NVP; c0 += 32) {
-            uint32_t oc[32];
-            pt_ld32(tmem_o + lane_off + c0, oc);
+          for (int c0 = 0; c0 < NVP; c0 += 16) {
+            uint32_t oc[16];
+            wt_ld16(tmem_o + lane_off + c0, oc);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) oc[j] = __float_as_uint(__uint_as_float(oc[j]) * alpha);
-            pt_st32(tmem_o + lane_off + c0, oc);
+            for (int j = 0; j < 16; ++j) oc[j] = __float_as_uint(__uint_as_float(oc[j]) * alpha);
+            wt_st8(tmem_o + lane_off + c0, *reinterpret_cast<uint32_t(*)[8]>(oc));
+            wt_st8(tmem_o + lane_off + c0 + 8, *reinterpret_cast<uint32_t(*)[8]>(oc + 8));
           }
         }
-        // weights, two a packed instruction: p = rounding + remainder, each half of a tile column; the row sum takes p itself
-        uint64_t qs2, nm2, neg1, l2[2] = {0ull, 0ull};
+        // p = rounding + remainder, two weights a column and packed instruction
+        uint64_t qs2, nm2;
+        float ls[2] = {0.f, 0.f};
         asm("mov.b64 %0, {%1, %1};" : "=l"(qs2) : "f"(p.qscale));
         asm("mov.b64 %0, {%1, %1};" : "=l"(nm2) : "f"(nm));
-        asm("mov.b64 %0, {%1, %1};" : "=l"(neg1) : "f"(-1.f));
 #pragma unroll
         for (int g8 = 0; g8 < 4; ++g8) {
           uint32_t hi[8], lo[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const int j = 16 * g8 + 2 * k;
-            uint64_t s2, x2, p2, h2;
+            uint64_t s2, x2;
             asm("mov.b64 %0, {%1, %2};" : "=l"(s2) : "r"(r[j]), "r"(r[j + 1]));
             asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x2) : "l"(s2), "l"(qs2), "l"(nm2));
             float x0, x1;
             asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
             const float p0 = pt_ex2(x0), p1 = pt_ex2(x1);
-            asm("mov.b64 %0, {%1, %2};" : "=l"(p2) : "f"(p0), "f"(p1));
-            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(l2[k & 1]) : "l"(l2[k & 1]), "l"(p2));
+            if constexpr (!LSUM) {
+              ls[0] += p0;
+              ls[1] += p1;
+            }
             const __nv_bfloat162 v2 = __floats2bfloat162_rn(p0, p1);
             hi[k] = *reinterpret_cast<const uint32_t*>(&v2);
+            uint64_t p2, h2;
+            asm("mov.b64 %0, {%1, %2};" : "=l"(p2) : "f"(p0), "f"(p1));
             asm("mov.b64 %0, {%1, %2};" : "=l"(h2) : "r"(hi[k] << 16), "r"(hi[k] & 0xffff0000u));
-            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x2) : "l"(h2), "l"(neg1), "l"(p2));
+            asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(x2) : "l"(p2), "l"(h2));
             asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
             const __nv_bfloat162 w2 = __floats2bfloat162_rn(x0, x1);
             lo[k] = *reinterpret_cast<const uint32_t*>(&w2);
@@ -470,12 +524,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           wt_st8(trow + 8 * g8, hi);
           wt_st8(trow + 32 + 8 * g8, lo);
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float a0, a1;
-          asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(l2[k]));
-          l_run += a0 + a1;
-        }
+        if constexpr (!LSUM) l_run += ls[0] + ls[1];
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       }
@@ -499,21 +548,23 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   if (warp < 8 && !timed_out) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const int n = q0 + 128 * X + row;
+    const int n_my = X ? nt[1] : nt[0];
+    if (LSUM && n_my > 0) l_run = __uint_as_float(pt_ld1(tmem_o + lane_off + (uint32_t)p.dv));
     const float f = PREFIX ? 1.f : l_run != 0.f ? 1.f / l_run : 0.f;
     float* orow = o_s + (size_t)(128 * X + row) * OS;
-    if ((X ? nt[1] : nt[0]) > 0) {
+    if (n_my > 0) {
 #pragma unroll 1
-      for (int c0 = 0; c0 < NVP; c0 += 32) {
-        uint32_t oc[32];
-        pt_ld32(tmem_o + lane_off + c0, oc);
+      for (int c0 = 0; c0 < NVP; c0 += 16) {
+        uint32_t oc[16];
+        wt_ld16(tmem_o + lane_off + c0, oc);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) orow[c0 + j] = l_run != 0.f ? __uint_as_float(oc[j]) * f : 0.f;
+        for (int j = 0; j < 16; ++j) orow[c0 + j] = l_run != 0.f ? __uint_as_float(oc[j]) * f : 0.f;
       }
     } else {
       for (int c = 0; c < p.dv; ++c) orow[c] = 0.f;            // nothing to see
     }
     if (PREFIX && n < n_rows) {
-      const int t = n / G;
+      const int t = row_t(128 * X + row);
       float* ml = p.ws + ((size_t)(first + t) * p.Hq + (size_t)h * G + (n - t * G)) * ws_head + RAP_MAX_SPLIT * dv4 + 2 * blockIdx.z;
       *reinterpret_cast<float2*>(ml) = make_float2(m_ref, l_run);
     }
@@ -522,8 +573,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   __syncthreads();
   if (!timed_out) {
     for (int r = warp; r < 256 && q0 + r < n_rows; r += WT_THREADS / 32) {
-      const int n = q0 + r, t = n / G;
-      const size_t head = (size_t)(first + t) * p.Hq + (size_t)h * G + (n - t * G);
+      const int t = row_t(r);
+      const size_t head = (size_t)(first + t) * p.Hq + (size_t)h * G + (q0 + r - t * G);
       float* dst = PREFIX ? p.ws + head * ws_head + (size_t)blockIdx.z * dv4 : p.out + head * p.dv;
       const float* src = o_s + (size_t)r * OS;
       for (int c = lane; c < p.dv; c += 32) dst[c] = src[c];
@@ -535,24 +586,25 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   }
 }
 
-template <int DK, int NVP, bool PREFIX>
+template <int DK, int NVP, bool LSUM, bool PREFIX>
 rap_status launch_wt(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
   const int smem = WT_SMEM + 1024;
-  RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, win_tc_kernel<DK, NVP, PREFIX>, smem));
+  RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, win_tc_kernel<DK, NVP, LSUM, PREFIX>, smem));
   const dim3 grid(blocks, p.Hkv, p.n_split);
-  win_tc_kernel<DK, NVP, PREFIX><<<grid, WT_THREADS, smem, st>>>(p);
+  win_tc_kernel<DK, NVP, LSUM, PREFIX><<<grid, WT_THREADS, smem, st>>>(p);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
 }
 template <bool PREFIX>
 rap_status launch_any(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
-  // steps and accumulator columns as the head needs them, in four sizes (a step more costs 3% at 90 dims)
-  const int dk = (p.P2 + 15) / 16, nvp = (p.dv + 31) / 32 * 32;
-  if (dk <= 4 && nvp <= 64) return launch_wt<4, 64, PREFIX>(ctx, p, blocks, st);
-  if (dk <= 6 && nvp <= 96) return launch_wt<6, 96, PREFIX>(ctx, p, blocks, st);
-  if (dk <= 7) return launch_wt<7, 128, PREFIX>(ctx, p, blocks, st);
-  return launch_wt<8, 128, PREFIX>(ctx, p, blocks, st);
+  // the steps and columns that the head needs, in four sizes; 128 channels leave no column for the row sums
+  const int dk = (p.P2 + 15) / 16, nv = p.dv + 1;
+  if (dk <= 4 && nv <= 80) return launch_wt<4, 80, true, PREFIX>(ctx, p, blocks, st);
+  if (dk <= 6 && nv <= 96) return launch_wt<6, 96, true, PREFIX>(ctx, p, blocks, st);
+  if (dk <= 7 && nv <= 112) return launch_wt<7, 112, true, PREFIX>(ctx, p, blocks, st);
+  if (nv <= 128) return launch_wt<8, 128, true, PREFIX>(ctx, p, blocks, st);
+  return launch_wt<8, 128, false, PREFIX>(ctx, p, blocks, st);
 }
 
 WtParams base_params(rap_ctx* ctx, const rap_win_args& a) {
