@@ -12,9 +12,8 @@
 //                    bf16 would put 1e-3 of error on them), which fill the 64 columns that the logits came from
 //   O_X += P_X V     A = P from tensor memory: eight steps of 16, the roundings' four and the remainders' four over the same V
 // Cache rows are not multiples of 16 bytes, so no tensor map describes them: four warps stage K and V with 4-byte cp.async
-// into rings of five 128-byte-swizzled tiles (K as stored is the K-major operand, V as stored the N-major one).  Odd d_v': rows
-// start on a half word, V goes through registers, two words and a byte permute each.  A rolling cache maps a position to its
-// row; a tile that does not cross the seam is one run of rows.
+// into rings of five 128-byte-swizzled tiles (K as stored is the K-major operand, V as stored the N-major one).  Odd d_v' (HALF):
+// every other row starts in the middle of a word, so V's words are copied as they lie and put in place when they have landed.  A rolling cache maps a position to its row; a tile that does not cross the seam is one run.
 // A K / V tile of 23 KB takes (4 P + 8 d_v') 64 cycles of the tensor pipe per 128 rows and 64 x 128 / 16 of the exponential
 // units, 576 and 512 cycles at P = 45: both, and the issue slots around them, bound it; HBM only below 128 rows.
 // Roles meet on mbarriers only; every wait is bounded and gives up early once another role has given up.
@@ -27,10 +26,10 @@ namespace {
 
 constexpr int WT_KT = 64;                              // keys per tile
 constexpr int WT_THREADS = 448;                        // 8 softmax warps, 2 that issue MMAs, 2 that stage K, 2 that stage V
-constexpr int WT_STAGES = 5;
 constexpr int WT_Q_BYTES = 2 * 128 * 128;              // [128 rows][<= 128 dims]: two 64-element atom columns
 constexpr int WT_KV_BYTES = 2 * WT_KT * 128;           // [64 keys][<= 128 dims or channels]
 constexpr int WT_TAIL = 320;                           // mbarriers, TMEM address, give-up flag
+constexpr int WT_STAGES = 5;                           // K buffers and V buffers
 constexpr int WT_SMEM = 2 * WT_Q_BYTES + 2 * WT_STAGES * WT_KV_BYTES + WT_TAIL;
 
 struct WtParams {
@@ -52,6 +51,41 @@ __device__ __forceinline__ void wt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
                : "memory");
 }
 
+// The MMA-issuing warps run as whole warps and predicate each instruction on one elected lane: the descriptors then live in
+// uniform registers.  A single lane's branch had every operand moved there one by one (a hundred cycles an MMA).
+__device__ __forceinline__ uint32_t wt_elect() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e;
+}
+__device__ __forceinline__ void wt_mma_ss(uint32_t e, uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %3};\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(tmem_d),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc), "r"(e)
+      : "memory");
+}
+__device__ __forceinline__ void wt_mma_ts(uint32_t e, uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc), "r"(e)
+      : "memory");
+}
+// when the elected lane's MMAs complete (mma), or at once
+__device__ __forceinline__ void wt_release(uint32_t e, uint32_t bar, bool mma) {
+  if (mma)
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(e) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+                 "@q mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(e) : "memory");
+}
 __device__ __forceinline__ void wt_cp4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -75,7 +109,7 @@ __device__ __forceinline__ void wt_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 // the second MMA (a fifth of the softmax threads' instructions otherwise).
 // PREFIX: the rows are the sequences of group `unit`, all of which see all `len` rows of its cache, and the partials go to the
 // workspace; otherwise the rows are new tokens of sequence `unit`.
-template <int DK, int NVP, bool LSUM, bool PREFIX>
+template <int DK, int NVP, bool LSUM, bool HALF, bool PREFIX>
 __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p) {
   extern __shared__ unsigned char wt_raw[];
   unsigned char* smem = wt_raw + ((1024u - (pt_smem(wt_raw) & 1023u)) & 1023u);
@@ -89,7 +123,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 32 * WT_STAGES + 96);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 32 * WT_STAGES + 100);
   static_assert(32 * WT_STAGES + 104 <= WT_TAIL, "barriers and flags fit the tail");
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = p.G, h = blockIdx.y;
   if constexpr (PREFIX) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the own rows' scan may start where SMs come free
 
@@ -209,7 +243,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
 #pragma unroll
       for (int u = 0; u < QB; ++u) {
         const int r = r0 + NWARP * u, t = row_t(r) - t_base;
-        const bool ok = r < 256 && q0 + r < n_rows;
+        const bool ok = r < 256 && q0 + r < n_rows && RAP_BOUNDS(first + t_base + t, p.rows, p.status, 0x307);
         const uint32_t* src = qsrc + ((size_t)t * p.Hq + (t_rest + r - t * G)) * kw;
         qv[u][0] = ok && lane < kw ? __ldg(src) : 0u;
         qv[u][1] = ok && lane + 32 < kw ? __ldg(src + 32) : 0u;
@@ -239,7 +273,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       if (pt_try_wait(bar, parity)) return true;
       if ((i & 15u) == 15u && *abort_flag) return false;
     }
-    *abort_flag = 1;
+    *abort_flag = (warp << 16) | (int)(bar - bar_fk) | 0x60000000;      // given up: which warp, on which barrier
     return false;
   };
 
@@ -256,7 +290,6 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     const unsigned char* src0 = reinterpret_cast<const unsigned char*>(is_v ? vg : kg);
     unsigned char* ring = is_v ? v_s : k_s;
     const uint32_t bar_f = is_v ? bar_fv : bar_fk, bar_e = is_v ? bar_ev : bar_ek;
-    const bool half = (rowlen & 1) != 0;             // rows start on a half word: through registers
     uint32_t swz[4][2];
     const int words = (rowlen + 1) >> 1;
 #pragma unroll
@@ -265,59 +298,84 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       for (int c = 0; c < 4; ++c) swz[c][sl] = pt_swz2(4 * (lane + 32 * sl), (pw + 2 * c) & 7);
     const bool one = lane < words, two = lane + 32 < words;
     const int R = p.S_cap - p.n_sink;
-    int stg = 0, use = 0;
-    for (int tile = 0; tile < n_max; ++tile) {
-      int j0, j1;
-      tile_at(tile, j0, j1);
-      if (use > 0 && !wait(bar_e + 8 * stg, (use - 1) & 1)) break;
-      const uint32_t du = pt_smem(ring + stg * WT_KV_BYTES);
-      const int rows_ok = min(WT_KT, j1 - j0);
-      // the tile's rows are one run from row s0 on unless it crosses the seam of a rolling cache
-      int s0 = j0;
-      bool run = j0 + rows_ok <= p.S_cap;
-      if (!run && j0 >= p.n_sink) {
-        s0 = p.n_sink + (j0 - p.n_sink) % R;
-        run = s0 + rows_ok <= p.S_cap;
-      }
-      auto slot_of = [&](int r) { return run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap); };
-      if (half) {
-        // eight rows a batch: all their words (and the ones behind, for rows that start in the middle of a word) in flight
-#pragma unroll 1
-        for (int i0 = 0; i0 < WT_KT / 2; i0 += 8) {
-          uint32_t a[8][2], b[8][2];
-          int odd = 0;
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int r = pw + 2 * (i0 + u);
-            const bool ok = r < rows_ok;
-            const int s = ok ? slot_of(r) : 0;
-            const uint32_t* src = reinterpret_cast<const uint32_t*>(src0 + (((size_t)s * (size_t)(2 * rowlen)) & ~(size_t)3));
-            odd |= (s & 1) << u;
-#pragma unroll
-            for (int sl = 0; sl < 2; ++sl) {
-              const int w = lane + 32 * sl;
-              a[u][sl] = ok && w < words ? __ldg(src + w) : 0u;
-              b[u][sl] = ok && (s & 1) && w + 1 < words ? __ldg(src + w + 1) : 0u;
-            }
+    // the warp's i-th tile row is pw + 2 i; K: the key of that number, V: keys k and k + 8 of sixteen lie side by side
+    auto key_of = [&](int i) { return is_v ? 16 * (i >> 3) + (i & 7) + 8 * pw : pw + 2 * i; };
+    // the rows of a tile are one run from row s0 on unless the tile crosses the seam of a rolling cache
+    auto run_of = [&](int j0, int n, int& s0) {
+      s0 = j0;
+      if (j0 + n <= p.S_cap) return true;
+      s0 = j0 >= p.n_sink ? p.n_sink + (j0 - p.n_sink) % R : j0;
+      return s0 + n <= p.S_cap;
+    };
+    if (HALF && is_v) {
+      // Rows of an odd number of half words: every other one starts in the middle of a word.  The words that hold a row are
+      // copied as they lie, AHEAD tiles ahead; once they have landed, a lane that copied a word of such a row puts its half and
+      // the half from the lane behind in its place (no lane reads what another one copied).
+      constexpr int AHEAD = 3;                         // below WT_STAGES - 1: the tile before the oldest unfinished one is never waited for
+      int stg = 0, use = 0, fix = 0;
+      for (int step = 0; step < n_max + AHEAD; ++step) {
+        if (step < n_max) {
+          int j0, j1, s0;
+          tile_at(step, j0, j1);
+          if (use > 0 && !__all_sync(0xffffffffu, wait(bar_e + 8 * stg, (use - 1) & 1))) break;
+          const int n = min(WT_KT, j1 - j0);
+          const bool run = run_of(j0, n, s0);
+          const uint32_t du = pt_smem(ring + stg * WT_KV_BYTES) + (uint32_t)pw * 128u;
+#pragma unroll 4
+          for (int i = 0; i < WT_KT / 2; ++i) {
+            const int r = key_of(i), sl = r < n ? (run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap)) : 0;
+            const unsigned char* src = src0 + (((size_t)sl * (size_t)(2 * rowlen)) & ~(size_t)3) + 4 * lane;
+            const int bytes = r < n && RAP_BOUNDS(sl, p.S_cap, p.status, 0x302) ? 4 : 0;
+            if (one) pt_cp4(du + i * 256 + swz[i & 3][0], src, bytes);
+            if (two) pt_cp4(du + i * 256 + swz[i & 3][1], src + 128, bytes);
           }
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int r = pw + 2 * (i0 + u);
-#pragma unroll
-            for (int sl = 0; sl < 2; ++sl) {
-              uint32_t v = (odd >> u) & 1 ? __funnelshift_r(a[u][sl], b[u][sl], 16) : a[u][sl];
-              if (LSUM && lane + 32 * sl == words - 1) v = (v & 0xffffu) | 0x3f800000u;
-              if (sl == 0 ? one : two)
-                *reinterpret_cast<uint32_t*>(ring + stg * WT_KV_BYTES + r * 128 + swz[u & 3][sl]) = v;
-            }
+          if (++stg == WT_STAGES) { stg = 0; ++use; }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (step < AHEAD) continue;
+        asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+        int j0, j1, s0;
+        tile_at(step - AHEAD, j0, j1);
+        const bool run = run_of(j0, min(WT_KT, j1 - j0), s0);
+        unsigned char* vt = ring + fix * WT_KV_BYTES + pw * 128;
+#pragma unroll 4
+        for (int i = 0; i < WT_KT / 2; ++i) {
+          const int r = key_of(i), sl = run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap);
+          uint32_t* w0 = reinterpret_cast<uint32_t*>(vt + i * 256 + swz[i & 3][0]);
+          uint32_t* w1 = reinterpret_cast<uint32_t*>(vt + i * 256 + swz[i & 3][1]);
+          uint32_t v0 = *w0, v1 = *w1;
+          if (sl & 1) {                                // the same for the whole warp
+            const uint32_t n0 = __shfl_sync(0xffffffffu, v0, (lane + 1) & 31), n1 = __shfl_sync(0xffffffffu, v1, (lane + 1) & 31);
+            v0 = __funnelshift_r(v0, lane == 31 ? n1 : n0, 16);
+            v1 = __funnelshift_r(v1, n1, 16);
           }
+          if (LSUM && lane == words - 1) v0 = (v0 & 0xffffu) | 0x3f800000u;
+          if (LSUM && lane + 32 == words - 1) v1 = (v1 & 0xffffu) | 0x3f800000u;
+          if (one) *w0 = v0;
+          if (two) *w1 = v1;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_f + 8 * stg) : "memory");
-      } else {
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_f + 8 * fix) : "memory");
+        if (++fix == WT_STAGES) fix = 0;
+      }
+    } else {
+      int stg = 0, use = 0;
+      for (int tile = 0; tile < n_max; ++tile) {
+        int j0, j1;
+        tile_at(tile, j0, j1);
+        if (use > 0 && !wait(bar_e + 8 * stg, (use - 1) & 1)) break;
+        const uint32_t du = pt_smem(ring + stg * WT_KV_BYTES);
+        const int rows_ok = min(WT_KT, j1 - j0);
+        int s0;
+        const bool run = run_of(j0, rows_ok, s0);
+        if (!RAP_BOUNDS(rows_ok - 1, WT_KT, p.status, 0x304) || !RAP_BOUNDS(run ? s0 : 0, p.S_cap, p.status, 0x305) ||
+            !RAP_BOUNDS(run ? s0 + rows_ok - 1 : 0, p.S_cap, p.status, 0x306))
+          break;
+        auto slot_of = [&](int r) { return run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap); };
         if (run && rows_ok == WT_KT) {
           // a full tile in one run: no predicates, running pointers
-          const unsigned char* sp = src0 + (size_t)(s0 + pw) * (size_t)(2 * rowlen) + 4 * lane;
+          const unsigned char* sp = src0 + (size_t)(s0 + key_of(0)) * (size_t)(2 * rowlen) + 4 * lane;
+          const size_t step = (size_t)(is_v ? 2 : 4) * rowlen, skip = is_v ? (size_t)16 * rowlen : 0;   // V: eight keys further after eight
           const uint32_t db = du + (uint32_t)pw * 128u;
           uint32_t d0[4], d1[4];
 #pragma unroll
@@ -328,94 +386,96 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           if (one) {
             const unsigned char* a = sp;
 #pragma unroll
-            for (int i = 0; i < WT_KT / 2; ++i, a += 4 * rowlen) wt_cp4(d0[i & 3] + (i >> 2) * 1024, a);
+            for (int i = 0; i < WT_KT / 2; ++i, a += step) {
+              if (i && !(i & 7)) a += skip;
+              wt_cp4(d0[i & 3] + (i >> 2) * 1024, a);
+            }
           }
           if (two) {
-            const unsigned char* a = sp;
+            const unsigned char* a = sp + 128;
 #pragma unroll
-            for (int i = 0; i < WT_KT / 2; ++i, a += 4 * rowlen) wt_cp4(d1[i & 3] + (i >> 2) * 1024, a + 128);
+            for (int i = 0; i < WT_KT / 2; ++i, a += step) {
+              if (i && !(i & 7)) a += skip;
+              wt_cp4(d1[i & 3] + (i >> 2) * 1024, a);
+            }
           }
         } else {
 #pragma unroll 4
           for (int i = 0; i < WT_KT / 2; ++i) {
-            const int r = pw + 2 * i;
+            const int r = key_of(i);
             const bool ok = r < rows_ok;               // rows behind the end: zeros, nothing is read
             const uint32_t* src = reinterpret_cast<const uint32_t*>(src0 + (size_t)(ok ? slot_of(r) : 0) * (size_t)(2 * rowlen));
-            const uint32_t rb = du + (uint32_t)r * 128u;
+            const uint32_t rb = du + (uint32_t)(pw + 2 * i) * 128u;
             if (one) pt_cp4(rb + swz[i & 3][0], src + lane, ok ? 4 : 0);
             if (two) pt_cp4(rb + swz[i & 3][1], src + lane + 32, ok ? 4 : 0);
           }
         }
         // the arrival is triggered by the completion of this thread's copies: go on to the next tile
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_f + 8 * stg) : "memory");
+        if (++stg == WT_STAGES) { stg = 0; ++use; }
       }
-      if (++stg == WT_STAGES) { stg = 0; ++use; }
     }
     // copies that nobody waited for (a role gave up) have landed before the shared memory is used for the output
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= 8) {
-    // ================= MMA issue: lane 0 of warp 8 for query tile A, of warp 9 for query tile B =================
-    // A buffer of the rings is free when both lanes have committed past it; a lane whose tile needs no more keys keeps
+    // ================= MMA issue: warp 8 for query tile A, warp 9 for query tile B =================
+    // A buffer of the rings is free when both warps have committed past it; a warp whose tile needs no more keys keeps
     // arriving in step (after the buffer was filled), so the phases stay aligned.
-    if (lane == 0 && n_max > 0) {
+    if (n_max > 0) {
       const int Y = warp - 8, n_y = Y ? nt[1] : nt[0];
+      const uint32_t e = wt_elect();
       const uint32_t tmem_sy = tmem_base + 128u * (uint32_t)Y, tmem_oy = tmem_base + 256u + 128u * (uint32_t)Y;
       constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
       constexpr uint32_t BUF16 = (uint32_t)WT_KV_BYTES >> 4;
-      uint32_t q_lo[DK];
-#pragma unroll
-      for (int ks = 0; ks < DK; ++ks)
-        q_lo[ks] = (((pt_smem(q_s + Y * WT_Q_BYTES) + (uint32_t)((ks >> 2) * 16384 + (ks & 3) * 32)) & 0x3FFFFu) >> 4) | (1u << 16);
+      const uint32_t q_lo = (((pt_smem(q_s) + (uint32_t)Y * WT_Q_BYTES) & 0x3FFFFu) >> 4) | (1u << 16);
       const uint32_t k_lo0 = ((pt_smem(k_s) & 0x3FFFFu) >> 4) | (1u << 16);
       const uint32_t v_lo0 = ((pt_smem(v_s) & 0x3FFFFu) >> 4) | ((8192u >> 4) << 16);
+      auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
       auto issue_s = [&](uint32_t kbuf, uint32_t sbuf) {     // S into buffer sbuf from K buffer kbuf
         const uint32_t kb = k_lo0 + kbuf * BUF16, td = tmem_sy + 64u * sbuf;
 #pragma unroll
         for (int ks = 0; ks < DK; ++ks)
-          pt_mma2(td, q_lo[ks], kb + (uint32_t)(((ks >> 2) * 8192 + (ks & 3) * 32) >> 4), DESC_HI, IDESC_S, ks > 0 ? 1u : 0u);
-        pt_commit(bar_s + 8 * (2 * Y + sbuf));
+          wt_mma_ss(e, td, q_lo + (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4),
+                    kb + (uint32_t)(((ks >> 2) * 8192 + (ks & 3) * 32) >> 4), DESC_HI, IDESC_S, ks > 0 ? 1u : 0u);
+        wt_release(e, bar_s + 8 * (2 * Y + sbuf), true);
       };
-      auto release = [&](uint32_t bar, bool issued) {   // after MMAs: when they complete; otherwise at once
-        if (issued) pt_commit(bar);
-        else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-      };
-      bool ok = wait(bar_fk, 0);
+      bool ok = wait_all(bar_fk, 0);
       if (ok) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (n_y > 0) issue_s(0, 0);
-        release(bar_ek, n_y > 0);
+        wt_release(e, bar_ek, n_y > 0);
       }
       uint32_t kbuf = 1, kpar = 0;       // ring position and phase of K tile + 1
       uint32_t vbuf = 0, vpar = 0;       // of V tile
       for (int tile = 0; ok && tile < n_max; ++tile) {
         const uint32_t sb = (uint32_t)tile & 1u;
         if (tile + 1 < n_max) {
-          if (!wait(bar_fk + 8 * kbuf, kpar)) { ok = false; break; }
+          if (!wait_all(bar_fk + 8 * kbuf, kpar)) { ok = false; break; }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           if (tile + 1 < n_y) issue_s(kbuf, sb ^ 1u);
-          release(bar_ek + 8 * kbuf, tile + 1 < n_y);
+          wt_release(e, bar_ek + 8 * kbuf, tile + 1 < n_y);
           if (++kbuf == WT_STAGES) { kbuf = 0; kpar ^= 1u; }
         }
-        if (!wait(bar_fv + 8 * vbuf, vpar)) { ok = false; break; }
+        if (!wait_all(bar_fv + 8 * vbuf, vpar)) { ok = false; break; }
         if (tile < n_y) {
-          if (!wait(bar_p + 8 * (2 * Y + sb), (uint32_t)(tile >> 1) & 1u)) { ok = false; break; }
+          if (!wait_all(bar_p + 8 * (2 * Y + sb), (uint32_t)(tile >> 1) & 1u)) { ok = false; break; }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t vb = v_lo0 + vbuf * BUF16, ta = tmem_sy + 64u * sb;
 #pragma unroll
-          for (int ks = 0; ks < WT_KT / 8; ++ks)    // the roundings (32 columns of two keys), then the remainders, over the same V
-            pt_mma_ts2(tmem_oy, ta + 8u * (uint32_t)ks, vb + (uint32_t)((ks & 3) * 2048 >> 4), DESC_HI, IDESC_O,
-                       (tile > 0 || ks > 0) ? 1u : 0u);
-          pt_commit(bar_o + 8 * Y);
+          for (int ks = 0; ks < WT_KT / 8; ++ks)    // sixteen keys' roundings (eight columns), then their remainders, over the same V
+            wt_mma_ts(e, tmem_oy, ta + 8u * (uint32_t)ks, vb + (uint32_t)((ks >> 1) * 2048 >> 4), DESC_HI, IDESC_O,
+                      (tile > 0 || ks > 0) ? 1u : 0u);
+          wt_release(e, bar_o + 8 * Y, true);
         }
-        release(bar_ev + 8 * vbuf, tile < n_y);
+        wt_release(e, bar_ev + 8 * vbuf, tile < n_y);
         if (++vbuf == WT_STAGES) { vbuf = 0; vpar ^= 1u; }
       }
-      // every MMA issued above has completed before tensor memory is released
-      pt_commit(bar_end + 8 * Y);
-      wait(bar_end + 8 * Y, 0);
+      // every MMA issued above has completed before tensor memory is released, also when a role has given up
+      wt_release(e, bar_end + 8 * Y, true);
+      for (uint32_t i = 0; i < PT_WAIT_LIMIT && !__all_sync(0xffffffffu, pt_try_wait(bar_end + 8 * Y, 0)); ++i) {}
     }
     __syncwarp();
   } else {
@@ -489,41 +549,34 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
             wt_st8(tmem_o + lane_off + c0 + 8, *reinterpret_cast<uint32_t(*)[8]>(oc + 8));
           }
         }
-        // p = rounding + remainder, two weights a column and packed instruction
-        uint64_t qs2, nm2;
+        // p = rounding + remainder.  Columns k and k + 8 of sixteen make a pair: its roundings replace column k, its remainders
+        // column k + 8, so the registers that the logits came in leave again as whole blocks (a store of eight columns each cost
+        // a third of the kernel's time), and the V rows of sixteen keys are staged in that order
         float ls[2] = {0.f, 0.f};
-        asm("mov.b64 %0, {%1, %1};" : "=l"(qs2) : "f"(p.qscale));
-        asm("mov.b64 %0, {%1, %1};" : "=l"(nm2) : "f"(nm));
 #pragma unroll
-        for (int g8 = 0; g8 < 4; ++g8) {
-          uint32_t hi[8], lo[8];
+        for (int g16 = 0; g16 < 64; g16 += 16)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int j = 16 * g8 + 2 * k;
-            uint64_t s2, x2;
-            asm("mov.b64 %0, {%1, %2};" : "=l"(s2) : "r"(r[j]), "r"(r[j + 1]));
-            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x2) : "l"(s2), "l"(qs2), "l"(nm2));
-            float x0, x1;
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
-            const float p0 = pt_ex2(x0), p1 = pt_ex2(x1);
+          for (int k = g16; k < g16 + 8; ++k) {
+            const float p0 = pt_ex2(fmaf(__uint_as_float(r[k]), p.qscale, nm)), p1 = pt_ex2(fmaf(__uint_as_float(r[k + 8]), p.qscale, nm));
             if constexpr (!LSUM) {
               ls[0] += p0;
               ls[1] += p1;
             }
             const __nv_bfloat162 v2 = __floats2bfloat162_rn(p0, p1);
-            hi[k] = *reinterpret_cast<const uint32_t*>(&v2);
-            uint64_t p2, h2;
+            const uint32_t hi = *reinterpret_cast<const uint32_t*>(&v2);
+            uint64_t p2, h2, x2;
+            float x0, x1;
             asm("mov.b64 %0, {%1, %2};" : "=l"(p2) : "f"(p0), "f"(p1));
-            asm("mov.b64 %0, {%1, %2};" : "=l"(h2) : "r"(hi[k] << 16), "r"(hi[k] & 0xffff0000u));
+            asm("mov.b64 %0, {%1, %2};" : "=l"(h2) : "r"(hi << 16), "r"(hi & 0xffff0000u));
             asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(x2) : "l"(p2), "l"(h2));
             asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
             const __nv_bfloat162 w2 = __floats2bfloat162_rn(x0, x1);
-            lo[k] = *reinterpret_cast<const uint32_t*>(&w2);
+            r[k] = hi;
+            r[k + 8] = *reinterpret_cast<const uint32_t*>(&w2);
           }
-          // over the columns that the logits came from; the next S into this buffer is issued after the MMA that reads these
-          wt_st8(trow + 8 * g8, hi);
-          wt_st8(trow + 32 + 8 * g8, lo);
-        }
+        // over the columns that the logits came from; the next S into this buffer is issued after the MMA that reads these
+        pt_st32(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
+        pt_st32(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
         if constexpr (!LSUM) l_run += ls[0] + ls[1];
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -536,7 +589,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   const bool timed_out = *abort_flag != 0;
-  if (timed_out && tid == 0) win_report(p.status, RAP_ETIMEOUT, 0x60000000 | ((int)blockIdx.x & 0xffffff));
+  if (timed_out && tid == 0) win_report(p.status, RAP_ETIMEOUT, *abort_flag);
   // The tiles are free now (every MMA has completed, every copy has landed).  A thread owns a row in tensor memory, but a row
   // of the output is contiguous in global memory: the rows go through shared memory (rows of NVP + 1 floats: the
   // row-per-thread stores hit 32 banks) and leave as whole rows, one warp per row.
@@ -577,6 +630,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       const size_t head = (size_t)(first + t) * p.Hq + (size_t)h * G + (q0 + r - t * G);
       float* dst = PREFIX ? p.ws + head * ws_head + (size_t)blockIdx.z * dv4 : p.out + head * p.dv;
       const float* src = o_s + (size_t)r * OS;
+      if (!RAP_BOUNDS(first + t, p.rows, p.status, 0x308)) break;
       for (int c = lane; c < p.dv; c += 32) dst[c] = src[c];
     }
   }
@@ -586,15 +640,21 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   }
 }
 
-template <int DK, int NVP, bool LSUM, bool PREFIX>
-rap_status launch_wt(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
+template <int DK, int NVP, bool LSUM, bool HALF, bool PREFIX>
+rap_status launch_as(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
   const int smem = WT_SMEM + 1024;
-  RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, win_tc_kernel<DK, NVP, LSUM, PREFIX>, smem));
+  RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, win_tc_kernel<DK, NVP, LSUM, HALF, PREFIX>, smem));
   const dim3 grid(blocks, p.Hkv, p.n_split);
-  win_tc_kernel<DK, NVP, LSUM, PREFIX><<<grid, WT_THREADS, smem, st>>>(p);
+  win_tc_kernel<DK, NVP, LSUM, HALF, PREFIX><<<grid, WT_THREADS, smem, st>>>(p);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   return RAP_OK;
+}
+template <int DK, int NVP, bool LSUM, bool PREFIX>
+rap_status launch_wt(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
+  if constexpr (LSUM)
+    if (p.dv & 1) return launch_as<DK, NVP, LSUM, true, PREFIX>(ctx, p, blocks, st);
+  return launch_as<DK, NVP, LSUM, false, PREFIX>(ctx, p, blocks, st);     // 128 channels, the one width without LSUM, is even
 }
 template <bool PREFIX>
 rap_status launch_any(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
