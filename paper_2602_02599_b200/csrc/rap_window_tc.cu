@@ -25,7 +25,8 @@
 namespace {
 
 constexpr int WT_KT = 64;                              // keys per tile
-constexpr int WT_THREADS = 448;                        // 8 softmax warps, 2 that issue MMAs, 2 that stage K, 2 that stage V
+constexpr int WT_NP = 3;                               // warps that stage K, and as many that stage V
+constexpr int WT_THREADS = 32 * (8 + 2 + 2 * WT_NP);   // 8 softmax warps, 2 that issue MMAs
 constexpr int WT_Q_BYTES = 2 * 128 * 128;              // [128 rows][<= 128 dims]: two 64-element atom columns
 constexpr int WT_KV_BYTES = 2 * WT_KT * 128;           // [64 keys][<= 128 dims or channels]
 constexpr int WT_TAIL = 320;                           // mbarriers, TMEM address, give-up flag
@@ -200,9 +201,9 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
 
   if (tid == 0) {
     for (int i = 0; i < WT_STAGES; ++i) {
-      pt_mbar_init(bar_fk + 8 * i, 64);
+      pt_mbar_init(bar_fk + 8 * i, 32 * WT_NP);
       pt_mbar_init(bar_ek + 8 * i, 2);               // both MMA-issuing lanes release a buffer
-      pt_mbar_init(bar_fv + 8 * i, 64);
+      pt_mbar_init(bar_fv + 8 * i, 32 * WT_NP);
       pt_mbar_init(bar_ev + 8 * i, 2);
     }
     for (int i = 0; i < 4; ++i) {
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     }
   }
   {
-    // a warp takes rows warp, warp + 14, ...; the loads of ten rows are in flight before the first store
+    // a warp takes rows warp, warp + 16, ...; the loads of ten rows are in flight before the first store
     constexpr int NWARP = WT_THREADS / 32, QB = 10;
     const uint32_t* qsrc = reinterpret_cast<const uint32_t*>(p.q) + ((size_t)(first + t_base) * p.Hq + (size_t)h * G) * kw + lane;
 #pragma unroll 1
@@ -282,30 +283,47 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   const int row = (warp & 3) * 32 + lane;
   const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
   const uint32_t tmem_o = tmem_base + 256 + 128 * X;
+  // registers: 256 threads of 168 and 256 of 88 are the 512 x 128 that the block has
+  static_assert(WT_THREADS == 512, "the split below is of 512 threads");
+  if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp >= 10) {
-    // ================= producers: warps 10-11 stage K, warps 12-13 stage V, a row of every two each =================
-    const bool is_v = warp >= 12;
-    const int pw = (warp - 10) & 1;
-    const int rowlen = is_v ? p.dv : p.P2;
-    const unsigned char* src0 = reinterpret_cast<const unsigned char*>(is_v ? vg : kg);
+    // ================= producers: WT_NP warps each stage K and V, eight tile rows at a time =================
+    const bool is_v = warp >= 10 + WT_NP;
+    const int pw = warp - 10 - (is_v ? WT_NP : 0);
+    const int rowlen = is_v ? p.dv : p.P2, rb = 2 * rowlen;
+    const unsigned char* src0 = reinterpret_cast<const unsigned char*>(is_v ? vg : kg) + 4 * lane;
     unsigned char* ring = is_v ? v_s : k_s;
     const uint32_t bar_f = is_v ? bar_fv : bar_fk, bar_e = is_v ? bar_ev : bar_ek;
-    uint32_t swz[4][2];
     const int words = (rowlen + 1) >> 1;
-#pragma unroll
-    for (int sl = 0; sl < 2; ++sl)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) swz[c][sl] = pt_swz2(4 * (lane + 32 * sl), (pw + 2 * c) & 7);
     const bool one = lane < words, two = lane + 32 < words;
+    uint32_t swz[8];                                   // of the lane's first word in a tile row, by row % 8; its second one is 8 KB on
+#pragma unroll
+    for (int c = 0; c < 8; ++c) swz[c] = pt_swz2(4 * lane, c) + 128u * c;
     const int R = p.S_cap - p.n_sink;
-    // the warp's i-th tile row is pw + 2 i; K: the key of that number, V: keys k and k + 8 of sixteen lie side by side
-    auto key_of = [&](int i) { return is_v ? 16 * (i >> 3) + (i & 7) + 8 * pw : pw + 2 * i; };
+    // the key of tile row i; V: keys k and k + 8 of sixteen lie side by side
+    auto key_of = [&](int i) { return is_v ? (i & 48) + ((i & 15) >> 1) + 8 * (i & 1) : i; };
     // the rows of a tile are one run from row s0 on unless the tile crosses the seam of a rolling cache
     auto run_of = [&](int j0, int n, int& s0) {
       s0 = j0;
       if (j0 + n <= p.S_cap) return true;
       s0 = j0 >= p.n_sink ? p.n_sink + (j0 - p.n_sink) % R : j0;
       return s0 + n <= p.S_cap;
+    };
+    // the first of this warp's groups of eight rows; they take turns, so that the odd group falls to each of them
+    auto first_group = [&](int tile) { return (pw + tile) % WT_NP; };
+    // words as they lie in the cache, row by row; rows behind the tile's last are zeros and nothing is read for them
+    auto copy_rows = [&](uint32_t du, int tile, int j0, int n, bool run, int s0) {
+#pragma unroll 1
+      for (int g = first_group(tile); g < WT_KT / 8; g += WT_NP)
+#pragma unroll
+       for (int c = 0; c < 8; ++c) {
+        const int i = 8 * g + c, r = key_of(i), sl = r < n ? (run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap)) : 0;
+        const unsigned char* src = src0 + (((size_t)sl * (size_t)rb) & ~(size_t)3);
+        const int bytes = r < n && RAP_BOUNDS(sl, p.S_cap, p.status, 0x302) ? 4 : 0;
+        if (one) pt_cp4(du + g * 1024 + swz[c], src, bytes);
+        if (two) pt_cp4(du + g * 1024 + swz[c] + 8192, src + 128, bytes);
+      }
     };
     if (HALF && is_v) {
       // Rows of an odd number of half words: every other one starts in the middle of a word.  The words that hold a row are
@@ -320,15 +338,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           if (use > 0 && !__all_sync(0xffffffffu, wait(bar_e + 8 * stg, (use - 1) & 1))) break;
           const int n = min(WT_KT, j1 - j0);
           const bool run = run_of(j0, n, s0);
-          const uint32_t du = pt_smem(ring + stg * WT_KV_BYTES) + (uint32_t)pw * 128u;
-#pragma unroll 4
-          for (int i = 0; i < WT_KT / 2; ++i) {
-            const int r = key_of(i), sl = r < n ? (run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap)) : 0;
-            const unsigned char* src = src0 + (((size_t)sl * (size_t)(2 * rowlen)) & ~(size_t)3) + 4 * lane;
-            const int bytes = r < n && RAP_BOUNDS(sl, p.S_cap, p.status, 0x302) ? 4 : 0;
-            if (one) pt_cp4(du + i * 256 + swz[i & 3][0], src, bytes);
-            if (two) pt_cp4(du + i * 256 + swz[i & 3][1], src + 128, bytes);
-          }
+          copy_rows(pt_smem(ring + stg * WT_KV_BYTES), step, j0, n, run, s0);
           if (++stg == WT_STAGES) { stg = 0; ++use; }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -337,13 +347,14 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         int j0, j1, s0;
         tile_at(step - AHEAD, j0, j1);
         const bool run = run_of(j0, min(WT_KT, j1 - j0), s0);
-        unsigned char* vt = ring + fix * WT_KV_BYTES + pw * 128;
-#pragma unroll 4
-        for (int i = 0; i < WT_KT / 2; ++i) {
-          const int r = key_of(i), sl = run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap);
-          uint32_t* w0 = reinterpret_cast<uint32_t*>(vt + i * 256 + swz[i & 3][0]);
-          uint32_t* w1 = reinterpret_cast<uint32_t*>(vt + i * 256 + swz[i & 3][1]);
-          uint32_t v0 = *w0, v1 = *w1;
+        unsigned char* vt = ring + fix * WT_KV_BYTES;
+#pragma unroll 1
+        for (int g = first_group(step - AHEAD); g < WT_KT / 8; g += WT_NP)
+#pragma unroll
+         for (int c = 0; c < 8; ++c) {
+          const int r = key_of(8 * g + c), sl = run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap);
+          uint32_t* w0 = reinterpret_cast<uint32_t*>(vt + g * 1024 + swz[c]);
+          uint32_t v0 = w0[0], v1 = w0[2048];
           if (sl & 1) {                                // the same for the whole warp
             const uint32_t n0 = __shfl_sync(0xffffffffu, v0, (lane + 1) & 31), n1 = __shfl_sync(0xffffffffu, v1, (lane + 1) & 31);
             v0 = __funnelshift_r(v0, lane == 31 ? n1 : n0, 16);
@@ -351,8 +362,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           }
           if (LSUM && lane == words - 1) v0 = (v0 & 0xffffu) | 0x3f800000u;
           if (LSUM && lane + 32 == words - 1) v1 = (v1 & 0xffffu) | 0x3f800000u;
-          if (one) *w0 = v0;
-          if (two) *w1 = v1;
+          if (one) w0[0] = v0;
+          if (two) w0[2048] = v1;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_f + 8 * fix) : "memory");
@@ -361,54 +372,31 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     } else {
       int stg = 0, use = 0;
       for (int tile = 0; tile < n_max; ++tile) {
-        int j0, j1;
+        int j0, j1, s0;
         tile_at(tile, j0, j1);
         if (use > 0 && !wait(bar_e + 8 * stg, (use - 1) & 1)) break;
         const uint32_t du = pt_smem(ring + stg * WT_KV_BYTES);
-        const int rows_ok = min(WT_KT, j1 - j0);
-        int s0;
-        const bool run = run_of(j0, rows_ok, s0);
-        if (!RAP_BOUNDS(rows_ok - 1, WT_KT, p.status, 0x304) || !RAP_BOUNDS(run ? s0 : 0, p.S_cap, p.status, 0x305) ||
-            !RAP_BOUNDS(run ? s0 + rows_ok - 1 : 0, p.S_cap, p.status, 0x306))
+        const int n = min(WT_KT, j1 - j0);
+        const bool run = run_of(j0, n, s0);
+        if (!RAP_BOUNDS(n - 1, WT_KT, p.status, 0x304) || !RAP_BOUNDS(run ? s0 : 0, p.S_cap, p.status, 0x305) ||
+            !RAP_BOUNDS(run ? s0 + n - 1 : 0, p.S_cap, p.status, 0x306))
           break;
-        auto slot_of = [&](int r) { return run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap); };
-        if (run && rows_ok == WT_KT) {
-          // a full tile in one run: no predicates, running pointers
-          const unsigned char* sp = src0 + (size_t)(s0 + key_of(0)) * (size_t)(2 * rowlen) + 4 * lane;
-          const size_t step = (size_t)(is_v ? 2 : 4) * rowlen, skip = is_v ? (size_t)16 * rowlen : 0;   // V: eight keys further after eight
-          const uint32_t db = du + (uint32_t)pw * 128u;
-          uint32_t d0[4], d1[4];
+        if (run && n == WT_KT) {
+          // a full tile in one run: no predicates, running pointers (V: from key k to k + 8 and back to k + 1)
+          const long long even = is_v ? 8LL * rb : rb, odd = is_v ? -7LL * rb : rb;
+#pragma unroll 1
+          for (int g = first_group(tile); g < WT_KT / 8; g += WT_NP) {
+            const unsigned char* a = src0 + (size_t)(s0 + key_of(8 * g)) * (size_t)rb;
+            const uint32_t dg = du + g * 1024;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            d0[c] = db + swz[c][0] + 256u * c;
-            d1[c] = db + swz[c][1] + 256u * c;
-          }
-          if (one) {
-            const unsigned char* a = sp;
-#pragma unroll
-            for (int i = 0; i < WT_KT / 2; ++i, a += step) {
-              if (i && !(i & 7)) a += skip;
-              wt_cp4(d0[i & 3] + (i >> 2) * 1024, a);
-            }
-          }
-          if (two) {
-            const unsigned char* a = sp + 128;
-#pragma unroll
-            for (int i = 0; i < WT_KT / 2; ++i, a += step) {
-              if (i && !(i & 7)) a += skip;
-              wt_cp4(d1[i & 3] + (i >> 2) * 1024, a);
+            for (int c = 0; c < 8; ++c) {
+              if (one) wt_cp4(dg + swz[c], a);
+              if (two) wt_cp4(dg + swz[c] + 8192, a + 128);
+              a += (c & 1) ? odd : even;
             }
           }
         } else {
-#pragma unroll 4
-          for (int i = 0; i < WT_KT / 2; ++i) {
-            const int r = key_of(i);
-            const bool ok = r < rows_ok;               // rows behind the end: zeros, nothing is read
-            const uint32_t* src = reinterpret_cast<const uint32_t*>(src0 + (size_t)(ok ? slot_of(r) : 0) * (size_t)(2 * rowlen));
-            const uint32_t rb = du + (uint32_t)(pw + 2 * i) * 128u;
-            if (one) pt_cp4(rb + swz[i & 3][0], src + lane, ok ? 4 : 0);
-            if (two) pt_cp4(rb + swz[i & 3][1], src + lane + 32, ok ? 4 : 0);
-          }
+          copy_rows(du, tile, j0, n, run, s0);
         }
         // the arrival is triggered by the completion of this thread's copies: go on to the next tile
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_f + 8 * stg) : "memory");
