@@ -201,7 +201,7 @@ rap_status rap_create(const rap_model_desc* desc, rap_ctx** out) {
   const size_t e = rap_elem_bytes(d.dtype);
   size_t n_out_max = (size_t)(d.n_q_heads + 2 * d.n_kv_heads) * d.head_dim;
   if ((size_t)d.hidden > n_out_max) n_out_max = d.hidden;       // the workspace also serves rap_out_proj
-  c->attn_ws_bytes = (size_t)d.max_batch * d.n_q_heads * RAP_MAX_SPLIT * (size_t)((d.head_dim + 3) / 4 * 4 + 2) * sizeof(float);
+  c->attn_ws_bytes = (size_t)d.max_batch * d.n_q_heads * RAP_MAX_SPLIT * (size_t)((d.head_dim + 3) / 4 * 4 + 2) * sizeof(float) + 16;
   // full-size fp32 results for any row count, plus room for reduction splits on decode-sized calls
   {
     const size_t small_rows = d.max_rows < 256 ? d.max_rows : 256;

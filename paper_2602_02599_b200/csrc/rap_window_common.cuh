@@ -45,9 +45,66 @@ __device__ __forceinline__ int win_owner(const int32_t* start, int n, int r) {
   return lo;
 }
 
-// Partials of a query head in the context's workspace: RAP_MAX_SPLIT rows of d_v' sums (a multiple of four), then as many
-// (maximum, weight) pairs
-__host__ __device__ __forceinline__ size_t win_partial_floats(int dv) { return (size_t)RAP_MAX_SPLIT * (((dv + 3) & ~3) + 2); }
+// Partials in the context's workspace: d_v' sums (a multiple of four), and (maximum, weight) pairs apart from them.  The own
+// rows' lie head by head, RAP_MAX_SPLIT - n_pre of them for each; a shared prefix's lie split by split over all heads, n_pre
+// times, ahead of them (a CTA writes one split of 256 neighbouring rows).
+struct WinPartials {
+  float* pre;          // [n_pre][heads][dv4], then [n_pre][heads][2]
+  float* own;          // [heads][slots][dv4], then [heads][slots][2]
+  long long heads;     // B * H_q
+  int dv4, n_pre, slots;
+  __device__ __forceinline__ float* pre_sums(long long head, int s) const { return pre + (s * heads + head) * dv4; }
+  __device__ __forceinline__ float2* pre_pair(long long head, int s) const { return reinterpret_cast<float2*>(pre + n_pre * heads * dv4) + s * heads + head; }
+  __device__ __forceinline__ float* own_sums(long long head, int s) const { return own + (head * slots + s) * dv4; }
+  __device__ __forceinline__ float2* own_pair(long long head, int s) const { return reinterpret_cast<float2*>(own + heads * slots * dv4) + head * slots + s; }
+};
+static inline WinPartials win_partials(float* ws, long long heads, int dv, int n_pre) {
+  WinPartials w;
+  w.heads = heads; w.dv4 = (dv + 3) & ~3; w.n_pre = n_pre; w.slots = RAP_MAX_SPLIT - n_pre;
+  w.pre = ws;
+  w.own = ws + ((n_pre * heads * (w.dv4 + 2) + 3) & ~3LL);      // 16-byte aligned
+  return w;
+}
+
+// How the prefixes' tiles of 64 rows are shared by the SMs: a (group, 256 rows, KV head) of n tiles takes ceil(n / per) CTAs,
+// `per` tiles each.  With fewer such pieces than half the SMs one wave of CTAs holds everything (sum of ceil(n / per) <= all
+// tiles / per + pieces); with more, four waves' worth of at least 16 tiles even out what the pieces differ by.  Every warp
+// that calls it gets the same answer.
+constexpr int WIN_MAX_PRE = 40;      // most splits of a prefix: the own rows keep RAP_MAX_SPLIT - 40 places
+struct WinPrefixPlan {
+  int per;             // tiles of a split
+};
+__device__ __forceinline__ int win_group_rows(const int32_t* start, int g, int B, int G) {
+  const int s0 = min(max(start[g], 0), B), s1 = min(max(start[g + 1], s0), B);
+  return (s1 - s0) * G;
+}
+__device__ __forceinline__ int win_group_tiles(const int32_t* len, int g, int S_cap) { return (min(max(len[g], 0), S_cap) + 63) >> 6; }
+__device__ __forceinline__ WinPrefixPlan win_prefix_plan(const int32_t* start, const int32_t* len, int n_groups, int B, int G, int Hkv, int S_cap,
+                                                         int sms, int n_pre) {
+  const int lane = threadIdx.x & 31;
+  int pieces = 0, most = 0;
+  long long all = 0;
+  for (int g0 = 0; g0 < n_groups; g0 += 32) {
+    const int g = g0 + lane;
+    int blocks = 0, tiles = 0;
+    if (g < n_groups) {
+      tiles = win_group_tiles(len, g, S_cap);
+      blocks = tiles ? (win_group_rows(start, g, B, G) + 255) >> 8 : 0;
+    }
+    pieces += __reduce_add_sync(0xffffffffu, blocks);
+    most = max(most, __reduce_max_sync(0xffffffffu, blocks ? tiles : 0));
+    // tiles * blocks < 2^31 in a lane: a cache's rows and a batch's rows fit a GPU together
+    const int lo = (tiles * blocks) & 0xffff, hi = (tiles * blocks) >> 16;
+    all += __reduce_add_sync(0xffffffffu, lo) + ((long long)__reduce_add_sync(0xffffffffu, hi) << 16);
+  }
+  pieces *= Hkv;
+  all *= Hkv;
+  WinPrefixPlan pl;
+  long long per = 2 * pieces <= sms ? (all + sms - pieces - 1) / (sms - pieces) : max(16LL, (all + 4 * sms - 1) / (4 * sms));
+  per = max(per, (long long)(most + n_pre - 1) / n_pre);
+  pl.per = (int)max(1LL, min(per, 0x7fffffffLL));
+  return pl;
+}
 
 __device__ __forceinline__ void win_report(int32_t* status, int code, int detail) {
   if (atomicCAS(&status[0], 0, code) == 0) status[1] = detail;

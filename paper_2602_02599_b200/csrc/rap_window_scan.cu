@@ -24,15 +24,15 @@ bool rap_win_scan_takes(const rap_win_args& a) {
   return a.dtype == RAP_BF16 && a.P2 >= 16 && a.P2 <= 128 && a.dv >= 16 && a.dv <= 128;
 }
 
-// n_pre: partials of a shared prefix that the launch before leaves in the first places of the workspace (0: none)
+// n_pre: the most partials of a shared prefix that the launch before leaves for a head (0: none)
 rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, cudaStream_t st) {
   WsParams p = {};
   p.q = (const uint32_t*)a.q; p.k = (const unsigned char*)a.k; p.v = (const unsigned char*)a.v; p.seq_len = a.seq_len;
-  p.out = a.out; p.ws = ctx->d_attn_ws; p.ws_floats = (long long)(ctx->attn_ws_bytes / sizeof(float)); p.status = ctx->d_status;
+  p.out = a.out; p.ws = win_partials(ctx->d_attn_ws, (long long)a.B * a.Hq, a.dv, n_pre); p.ws_floats = (long long)(ctx->attn_ws_bytes / sizeof(float)); p.status = ctx->d_status;
   p.B = a.B; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv; p.P = a.P2 / 2; p.dv = a.dv; p.S_cap = a.S_cap;
   p.n_sink = a.n_sink; p.window = a.window; p.len_cap = a.n_groups ? a.S_cap : 0x7fffffff;
   p.qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
-  p.n_pre = n_pre; p.n_groups = a.n_groups; p.group_start = a.group_start;
+  p.n_groups = a.n_groups; p.group_start = a.group_start; p.prefix_len = a.prefix_len; p.S_pre = a.S_pre; p.sms = ctx->sm_count;
   p.wait_limit = WAIT_LIMIT;
   {   // two sets of counters take turns; each launch clears the one its predecessor used
     const size_t n_units = (size_t)ctx->desc.max_batch * ctx->desc.n_kv_heads;

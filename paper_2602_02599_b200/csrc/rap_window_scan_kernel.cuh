@@ -31,8 +31,8 @@ struct WsParams {
   const unsigned char* v;     // [B][Hkv][S_cap][2 dv bytes]
   const int32_t* seq_len;
   float* out;                 // [B][Hq][dv]
-  float* ws;                  // [B][Hq] partials (win_partial_floats)
-  long long ws_floats;
+  WinPartials ws;
+  long long ws_floats;        // size of the workspace from ws.pre on
   int32_t* unit_cnt;          // arrivals per unit, zero between calls
   int32_t* unit_cnt_other;    // the set of the launch before; cleared by this one
   int other_units;
@@ -45,9 +45,10 @@ struct WsParams {
   int stage_bytes, n_stages, n_warps, off_stage;
   int per_cta;                // least blocks of a CTA
   uint32_t wait_limit;
-  // partials of a shared prefix: the first n_pre of a head's RAP_MAX_SPLIT, for sequences that are in a group
-  int n_pre, n_groups;
+  // shared prefixes (ws.n_pre > 0): what the plan of their splits is made of
+  int n_groups, S_pre, sms;
   const int32_t* group_start;
+  const int32_t* prefix_len;
 };
 
 __device__ __forceinline__ void ws_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -126,12 +127,12 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   }
   T *= p.Hkv;
   // no unit is touched by more CTAs than there is room for partials behind the prefix's, and every CTA has a block for each warp
-  const long long room = (long long)(RAP_MAX_SPLIT - 2 - p.n_pre) * T / n_max;
+  const long long room = (long long)(RAP_MAX_SPLIT - 2 - p.ws.n_pre) * T / n_max;
   const int nc = (int)max(1LL, min(min((long long)gridDim.x, room), (long long)(T + p.per_cta - 1) / p.per_cta));
   if (blockIdx.x == 0)
     for (int i = tid; i < p.other_units; i += THREADS) p.unit_cnt_other[i] = 0;      // what a launch that gave up left behind
   if ((int)blockIdx.x >= nc) {
-    if (p.n_pre) pdl_wait();     // a launch is not over before the one that it overlaps
+    if (p.ws.n_pre) pdl_wait();     // a launch is not over before the one that it overlaps
     return;
   }
   // the first T % nc CTAs take one block more than the others
@@ -156,6 +157,9 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   h = (cur - unit_start) / (u.n + WS_OWN);
   unit_start += h * (u.n + WS_OWN);
 
+  int pre_per = 1;
+  if (p.ws.n_pre)
+    pre_per = win_prefix_plan(p.group_start, p.prefix_len, p.n_groups, p.B, G, p.Hkv, p.S_pre, p.sms, p.ws.n_pre).per;
   const uint32_t bar0 = smem_u32(bars) + warp * NSTG * 8;
   unsigned char* wstage = smem + p.off_stage + (size_t)warp * NSTG * p.stage_bytes;
   const uint32_t wstage_u = smem_u32(wstage);
@@ -197,9 +201,9 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
     const bool empty = u.nb[0] + u.nb[1] + u.nb[2] == 0;
     const int n_blk = !empty && n_my > warp ? (n_my - warp + NW - 1) / NW : 0;
     int n_pre = 0;             // partials of the prefix, if the sequence has one
-    if (p.n_pre) {
+    if (p.ws.n_pre) {
       const int g = win_owner(p.group_start, p.n_groups, b);
-      n_pre = g < p.n_groups && p.group_start[g] <= b ? p.n_pre : 0;
+      if (g < p.n_groups && p.group_start[g] <= b) n_pre = (win_group_tiles(p.prefix_len, g, p.S_pre) + pre_per - 1) / pre_per;
     }
     float* out = p.out + ((size_t)b * p.Hq + (size_t)h * G) * dv;
     if (empty && n_pre == 0) {
@@ -436,11 +440,10 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
     __syncthreads();
     const int first = cta_of(unit_start + WS_OWN), n_seg = cta_of(unit_start + WS_OWN + u.n - 1) - first + 1;
     const bool alone = n_seg == 1 && n_pre == 0;
-    const int dv4 = (dv + 3) & ~3, my_seg = p.n_pre + (int)blockIdx.x - first;
-    const size_t ws_head = win_partial_floats(dv);
-    float* ub = p.ws + ((size_t)b * p.Hq + (size_t)h * G) * ws_head;           // the unit's partials
-    const bool ws_ok = RAP_BOUNDS(my_seg, RAP_MAX_SPLIT, p.status, 0x206) &&
-                       RAP_BOUNDS((ub - p.ws) + (long long)G * ws_head - 1, p.ws_floats, p.status, 0x207);
+    const int dv4 = p.ws.dv4, my_seg = (int)blockIdx.x - first;
+    const long long head0 = (long long)b * p.Hq + (long long)h * G;            // the unit's first query head
+    const bool ws_ok = RAP_BOUNDS(my_seg, p.ws.slots, p.status, 0x206) &&
+                       RAP_BOUNDS(reinterpret_cast<float*>(p.ws.own_pair(head0 + G - 1, my_seg)) + 1 - p.ws.pre, p.ws_floats, p.status, 0x207);
     for (int g = warp; g < G && ws_ok; g += NW) {
       float l = 0.f, mm = -INFINITY;
       for (int i = 0; i < NW; ++i) {
@@ -452,9 +455,9 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         float sum = 0.f;
         for (int i = 0; i < NW; ++i) sum += red[((size_t)i * G + g) * CW + c];
         if (alone) out[(size_t)g * dv + c] = sum * inv;
-        else ub[g * ws_head + my_seg * dv4 + c] = sum;
+        else p.ws.own_sums(head0 + g, my_seg)[c] = sum;
       }
-      if (!alone && lane == 0) *reinterpret_cast<float2*>(ub + g * ws_head + RAP_MAX_SPLIT * dv4 + 2 * my_seg) = make_float2(mm, l);
+      if (!alone && lane == 0) *p.ws.own_pair(head0 + g, my_seg) = make_float2(mm, l);
     }
     if (!alone) {
       // ---- who delivers a unit's last partial joins them, in order ----
@@ -463,17 +466,17 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
       if (tid == 0) *s_last = n_seg == 1 || (RAP_BOUNDS(unit, (size_t)p.B * p.Hkv, p.status, 0x208) && atomicAdd(&p.unit_cnt[unit], 1) == n_seg - 1);
       __syncthreads();
       if (*s_last) {
-        if (p.n_pre && !joined) pdl_wait();        // the prefix's partials come from the launch before
+        if (p.ws.n_pre && !joined) pdl_wait();        // the prefix's partials come from the launch before
         joined = true;
         __threadfence();
-        const int s_first = p.n_pre - n_pre, n = n_pre + n_seg;      // <= RAP_MAX_SPLIT
+        const int n = n_pre + n_seg;               // <= RAP_MAX_SPLIT
         float* wgt = red;                          // [G][RAP_MAX_SPLIT] weights over their sum
         for (int g = warp; g < G; g += NW) {
-          const float2* ml = reinterpret_cast<const float2*>(ub + g * ws_head + RAP_MAX_SPLIT * dv4) + s_first;
           float mv[2], lv[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const float2 x = lane + 32 * k < n ? __ldcg(ml + lane + 32 * k) : make_float2(-INFINITY, 0.f);
+            const int sg = lane + 32 * k;
+            const float2 x = sg < n_pre ? __ldcg(p.ws.pre_pair(head0 + g, sg)) : sg < n ? __ldcg(p.ws.own_pair(head0 + g, sg - n_pre)) : make_float2(-INFINITY, 0.f);
             lv[k] = x.y;
             mv[k] = x.y != 0.f ? x.x : -INFINITY;
           }
@@ -496,13 +499,18 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         const int c4 = dv4 >> 2;
         for (int i = tid; i < G * c4; i += THREADS) {     // four channels of a head
           const int g = i / c4, c = 4 * (i - g * c4);
-          const float* gb = ub + g * ws_head + s_first * dv4 + c;
+          const float* pb = p.ws.pre_sums(head0 + g, 0) + c;
+          const float* ob = p.ws.own_sums(head0 + g, 0) + c;
+          const long long pre_step = p.ws.heads * dv4;
           const float* wg = wgt + g * RAP_MAX_SPLIT;
           float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
           for (int s0 = 0; s0 < n; s0 += 8) {      // eight loads in flight
             float4 av[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) av[k] = __ldcg(reinterpret_cast<const float4*>(gb + min(s0 + k, n - 1) * dv4));
+            for (int k = 0; k < 8; ++k) {
+              const int sg = min(s0 + k, n - 1);
+              av[k] = __ldcg(reinterpret_cast<const float4*>(sg < n_pre ? pb + sg * pre_step : ob + (sg - n_pre) * dv4));
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               const float wk = s0 + k < n ? wg[s0 + k] : 0.f;
@@ -533,7 +541,7 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
     }
     __syncthreads();           // the sums and weights in shared memory have been read
   }
-  if (p.n_pre) pdl_wait();
+  if (p.ws.n_pre) pdl_wait();
 }
 
 }  // namespace

@@ -40,9 +40,9 @@ struct WtParams {
   const int32_t* start;        // [units + 1]: first token (or sequence) of a unit in q
   const int32_t* len;          // [units]: length with the new tokens, or prefix length
   float* out;                  // [rows][Hq][dv]
-  float* ws;                   // partials (win_partial_floats) when split
+  WinPartials ws;              // where a prefix's partials go
   int32_t* status;
-  int units, rows, Hq, Hkv, G, P2, dv, S_cap, n_sink, window, n_split;
+  int units, rows, Hq, Hkv, G, P2, dv, S_cap, n_sink, window, sms;
   float qscale;                // log2(e) / sqrt(D)
 };
 
@@ -95,6 +95,18 @@ __device__ __forceinline__ float wt_max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// after the wait for loads: no arithmetic on what they return is moved ahead of it
+template <int N>
+__device__ __forceinline__ void wt_loaded(uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i])::"memory");
+}
+__device__ __forceinline__ void wt_ld8(uint32_t taddr, uint32_t* r) {      // to be waited for
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
 __device__ __forceinline__ void wt_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -103,6 +115,7 @@ __device__ __forceinline__ void wt_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "r"(taddr)
       : "memory");
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+  wt_loaded<16>(r);
 }
 
 // DK = k-steps of Q K^T (ceil(2P / 16)); NVP = columns of the second MMA, a multiple of 16 from d_v' on.  LSUM: NVP > d_v', and
@@ -120,24 +133,26 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   unsigned char* tail = v_s + WT_STAGES * WT_KV_BYTES;
   const uint32_t bar_fk = pt_smem(tail), bar_ek = bar_fk + 8 * WT_STAGES, bar_fv = bar_ek + 8 * WT_STAGES,
                  bar_ev = bar_fv + 8 * WT_STAGES, bar_s = bar_ev + 8 * WT_STAGES /* [X][2] */, bar_p = bar_s + 32 /* [X][2] */,
-                 bar_o = bar_p + 32 /* [X] */, bar_end = bar_o + 16 /* [X] */;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 32 * WT_STAGES + 96);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 32 * WT_STAGES + 100);
-  static_assert(32 * WT_STAGES + 104 <= WT_TAIL, "barriers and flags fit the tail");
+                 bar_o = bar_p + 32 /* [X] */, bar_end = bar_o + 16 /* [X] */, bar_q = bar_end + 16 /* [X] */;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 32 * WT_STAGES + 112);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 32 * WT_STAGES + 116);
+  static_assert(32 * WT_STAGES + 120 <= WT_TAIL, "barriers and flags fit the tail");
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int G = p.G, h = blockIdx.y;
+  const int G = p.G;
   if constexpr (PREFIX) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the own rows' scan may start where SMs come free
 
-  // ---- which unit, which of its rows: every warp walks the units' row counts, 256 rows a block ----
-  int unit = -1, q0 = 0;
+  // ---- which unit, which of its rows, which KV head (and which split of a prefix): every warp walks the units, 256 rows a block ----
+  int unit = -1, q0 = 0, h = blockIdx.y, split = 0, per = 0;
+  if constexpr (PREFIX) per = win_prefix_plan(p.start, p.len, p.units, p.rows, G, p.Hkv, p.S_cap, p.sms, p.ws.n_pre).per;
   for (int u0 = 0, carry = 0; u0 < p.units; u0 += 32) {
     const int u = u0 + lane;
-    int n = 0;
+    int n = 0, n_split = 1;
     if (u < p.units) {
-      const int s0 = min(max(p.start[u], 0), p.rows), s1 = min(max(p.start[u + 1], s0), p.rows);
-      n = ((s1 - s0) * G + 255) >> 8;
+      n = (win_group_rows(p.start, u, p.rows, G) + 255) >> 8;
+      if constexpr (PREFIX) n_split = (win_group_tiles(p.len, u, p.S_cap) + per - 1) / per * p.Hkv;
     }
-    int x = n;
+    int x = n * n_split;
+    const int mine = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, x, o);
@@ -147,7 +162,16 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     if (past) {
       const int l = __ffs(past) - 1;
       unit = u0 + l;
-      q0 = ((int)blockIdx.x - carry - __shfl_sync(0xffffffffu, x - n, l)) * 256;
+      int at = (int)blockIdx.x - carry - __shfl_sync(0xffffffffu, x - mine, l);
+      if constexpr (PREFIX) {        // KV heads of a split side by side, then splits, then blocks of rows
+        const int ns = __shfl_sync(0xffffffffu, n_split, l);
+        q0 = at / ns * 256;
+        at -= at / ns * ns;
+        split = at / p.Hkv;
+        h = at - split * p.Hkv;
+      } else {
+        q0 = at * 256;
+      }
       break;
     }
     carry += __shfl_sync(0xffffffffu, x, 31);
@@ -170,8 +194,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     pmax[X] = q0 + 128 * X < n_rows ? pos0 + row_t(min(n_rows - q0, 128 * X + 128) - 1) : -1;
   }
   if constexpr (PREFIX) {
-    const int all = (len + WT_KT - 1) / WT_KT, per = (all + p.n_split - 1) / p.n_split;
-    t_first = min(all, (int)blockIdx.z * per);
+    const int all = (len + WT_KT - 1) / WT_KT;
+    t_first = split * per;
     jend = len;
 #pragma unroll
     for (int X = 0; X < 2; ++X) nt[X] = q0 + 128 * X < n_rows ? min(all, t_first + per) - t_first : 0;
@@ -213,6 +237,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     for (int X = 0; X < 2; ++X) pt_mbar_init(bar_o + 8 * X, 1);
     pt_mbar_init(bar_end, 1);
     pt_mbar_init(bar_end + 8, 1);
+    pt_mbar_init(bar_q, 128);
+    pt_mbar_init(bar_q + 8, 128);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -222,7 +248,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const int kw = p.P2 >> 1;                          // 4-byte words per q / K row
-  // pad dims are zero in Q and in K (V's pad channels only reach accumulator columns that nothing reads)
+  // K's pad dims are zero (Q's too, below; V's pad channels only reach accumulator columns that nothing reads)
   for (int i = tid; i < WT_STAGES * WT_KT * (8 * DK - kw); i += WT_THREADS) {
     const int br = i / (8 * DK - kw), w = kw + i - br * (8 * DK - kw);
     *reinterpret_cast<uint32_t*>(k_s + (br >> 6) * WT_KV_BYTES + (br & 63) * 128 + pt_swz2(4 * w, br & 7)) = 0u;
@@ -232,32 +258,6 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     for (int i = tid; i < WT_STAGES * WT_KT; i += WT_THREADS) {
       const int buf = i / WT_KT, r = i - buf * WT_KT;
       *reinterpret_cast<uint32_t*>(v_s + buf * WT_KV_BYTES + r * 128 + pt_swz2(4 * (p.dv >> 1), r & 7)) = p.dv & 1 ? 0x3f800000u : 0x3f80u;
-    }
-  }
-  {
-    // a warp takes rows warp, warp + 16, ...; the loads of ten rows are in flight before the first store
-    constexpr int NWARP = WT_THREADS / 32, QB = 10;
-    const uint32_t* qsrc = reinterpret_cast<const uint32_t*>(p.q) + ((size_t)(first + t_base) * p.Hq + (size_t)h * G) * kw + lane;
-#pragma unroll 1
-    for (int r0 = warp; r0 < 256; r0 += NWARP * QB) {
-      uint32_t qv[QB][2];
-#pragma unroll
-      for (int u = 0; u < QB; ++u) {
-        const int r = r0 + NWARP * u, t = row_t(r) - t_base;
-        const bool ok = r < 256 && q0 + r < n_rows && RAP_BOUNDS(first + t_base + t, p.rows, p.status, 0x307);
-        const uint32_t* src = qsrc + ((size_t)t * p.Hq + (t_rest + r - t * G)) * kw;
-        qv[u][0] = ok && lane < kw ? __ldg(src) : 0u;
-        qv[u][1] = ok && lane + 32 < kw ? __ldg(src + 32) : 0u;
-      }
-#pragma unroll
-      for (int u = 0; u < QB; ++u) {
-        const int r = r0 + NWARP * u;
-        if (r < 256) {
-          unsigned char* qd = q_s + r * 128 + ((r >> 7) << 14) + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2);
-          if (lane < 8 * DK) *reinterpret_cast<uint32_t*>(qd) = qv[u][0];
-          if (lane + 32 < 8 * DK) *reinterpret_cast<uint32_t*>(qd + 128 * 128) = qv[u][1];
-        }
-      }
     }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
                     kb + (uint32_t)(((ks >> 2) * 8192 + (ks & 3) * 32) >> 4), DESC_HI, IDESC_S, ks > 0 ? 1u : 0u);
         wt_release(e, bar_s + 8 * (2 * Y + sbuf), true);
       };
-      bool ok = wait_all(bar_fk, 0);
+      bool ok = (n_y == 0 || wait_all(bar_q + 8 * Y, 0)) && wait_all(bar_fk, 0);
       if (ok) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -473,6 +473,28 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     const bool active = q0 + 128 * X + (warp & 3) * 32 < n_rows;       // some row of this warp is one
     const int n_my = X ? nt[1] : nt[0], p_min = X ? pmin[1] : pmin[0], p_max = X ? pmax[1] : pmax[0];
     bool rows_ok = true;
+    if (n_my > 0) {
+      // Q_X: a warp stages its 32 rows, all in flight at once; rows behind the block's last and pad dims are zeros
+      const uint32_t* qsrc = reinterpret_cast<const uint32_t*>(p.q) + ((size_t)(first + t_base) * p.Hq + (size_t)h * G) * kw + lane;
+      unsigned char* qd = q_s + X * WT_Q_BYTES + (warp & 3) * 32 * 128 + ((lane & 3) << 2);
+      uint32_t qv[32][2];
+#pragma unroll
+      for (int u = 0; u < 32; ++u) {
+        const int rr = 128 * X + (warp & 3) * 32 + u, t = row_t(rr) - t_base;
+        const bool ok = q0 + rr < n_rows && RAP_BOUNDS(first + t_base + t, p.rows, p.status, 0x307);
+        const uint32_t* src = qsrc + ((size_t)t * p.Hq + (t_rest + rr - t * G)) * kw;
+        qv[u][0] = ok && lane < kw ? __ldg(src) : 0u;
+        qv[u][1] = ok && lane + 32 < kw ? __ldg(src + 32) : 0u;
+      }
+#pragma unroll
+      for (int u = 0; u < 32; ++u) {
+        unsigned char* d = qd + u * 128 + (((lane >> 2) ^ (u & 7)) << 4);
+        if (lane < 8 * DK) *reinterpret_cast<uint32_t*>(d) = qv[u][0];
+        if (lane + 32 < 8 * DK) *reinterpret_cast<uint32_t*>(d + 128 * 128) = qv[u][1];
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_q + 8 * X) : "memory");
+    }
     for (int tile = 0; tile < n_my; ++tile) {
       int j0, j1;
       tile_at(tile, j0, j1);
@@ -507,6 +529,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         pt_ld32_nowait(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
         pt_ld32_nowait(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        wt_loaded<64>(r);
         float mx4[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -571,57 +594,55 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       }
       asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_p + 8 * (2 * X + (tile & 1))) : "memory");
     }
-    if (rows_ok && n_my > 0) __all_sync(0xffffffffu, wait(bar_o + 8 * X, (n_my - 1) & 1));
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    // ---- the output.  A thread owns a row in tensor memory, but a row of the output is contiguous in global memory: a warp
+    // passes its 32 rows through its part of Q_X's tiles, CC columns at a time (rows of CC + 1 floats hit 32 banks), and they
+    // leave as pieces of whole rows.  Every MMA of the query tile is done when bar_end says so.
+    if (rows_ok && n_my > 0) rows_ok = __all_sync(0xffffffffu, wait(bar_end + 8 * X, 0));
+    if (rows_ok && active) {
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      constexpr int CC = NVP == 128 ? 32 : NVP / 2;
+      static_assert(CC % 8 == 0 && 4 * 32 * (CC + 1) * 4 <= WT_Q_BYTES, "four warps' rows fit the tile");
+      float* o_s = reinterpret_cast<float*>(q_s + X * WT_Q_BYTES) + (warp & 3) * 32 * (CC + 1);
+      if (LSUM && n_my > 0) l_run = __uint_as_float(pt_ld1(tmem_o + lane_off + (uint32_t)p.dv));
+      const float f = PREFIX ? 1.f : l_run != 0.f ? 1.f / l_run : 0.f;
+      const int r_first = 128 * X + (warp & 3) * 32, r_n = min(32, n_rows - q0 - r_first);
+      const long long unit_head = (long long)first * p.Hq + (long long)h * G;
+      if (PREFIX && lane < r_n) {
+        const int t = row_t(r_first + lane);
+        const long long head = unit_head + (long long)t * p.Hq + (q0 + r_first + lane - t * G);
+        *p.ws.pre_pair(head, split) = make_float2(m_ref, l_run);
+      }
+#pragma unroll 1
+      for (int c0 = 0; c0 < p.dv; c0 += CC) {
+        uint32_t oc[CC];
+        if (n_my > 0) {
+#pragma unroll
+          for (int c = 0; c < CC; c += 8) wt_ld8(tmem_o + lane_off + c0 + c, oc + c);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          wt_loaded<CC>(oc);
+        }
+        const bool some = n_my > 0 && l_run != 0.f;              // nothing seen: zeros
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < CC; ++c) o_s[lane * (CC + 1) + c] = some ? __uint_as_float(oc[c]) * f : 0.f;
+        __syncwarp();
+        const int n_c = min(CC, p.dv - c0);
+#pragma unroll 4
+        for (int r = 0; r < r_n; ++r) {
+          const int t = row_t(r_first + r);
+          const long long head = unit_head + (long long)t * p.Hq + (q0 + r_first + r - t * G);
+          if (!RAP_BOUNDS(first + t, p.rows, p.status, 0x308) || !RAP_BOUNDS(split, PREFIX ? p.ws.n_pre : 1, p.status, 0x309)) break;
+          float* dst = (PREFIX ? p.ws.pre_sums(head, split) : p.out + head * p.dv) + c0;
+          if (lane < n_c) dst[lane] = o_s[r * (CC + 1) + lane];
+          if (lane + 32 < n_c) dst[lane + 32] = o_s[r * (CC + 1) + lane + 32];
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  const bool timed_out = *abort_flag != 0;
-  if (timed_out && tid == 0) win_report(p.status, RAP_ETIMEOUT, *abort_flag);
-  // The tiles are free now (every MMA has completed, every copy has landed).  A thread owns a row in tensor memory, but a row
-  // of the output is contiguous in global memory: the rows go through shared memory (rows of NVP + 1 floats: the
-  // row-per-thread stores hit 32 banks) and leave as whole rows, one warp per row.
-  float* o_s = reinterpret_cast<float*>(smem);
-  constexpr int OS = NVP + 1;
-  static_assert(256 * OS * 4 <= WT_SMEM - WT_TAIL, "the output tile fits the freed tiles");
-  const int dv4 = (p.dv + 3) & ~3;
-  const size_t ws_head = win_partial_floats(p.dv);
-  if (warp < 8 && !timed_out) {
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const int n = q0 + 128 * X + row;
-    const int n_my = X ? nt[1] : nt[0];
-    if (LSUM && n_my > 0) l_run = __uint_as_float(pt_ld1(tmem_o + lane_off + (uint32_t)p.dv));
-    const float f = PREFIX ? 1.f : l_run != 0.f ? 1.f / l_run : 0.f;
-    float* orow = o_s + (size_t)(128 * X + row) * OS;
-    if (n_my > 0) {
-#pragma unroll 1
-      for (int c0 = 0; c0 < NVP; c0 += 16) {
-        uint32_t oc[16];
-        wt_ld16(tmem_o + lane_off + c0, oc);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) orow[c0 + j] = l_run != 0.f ? __uint_as_float(oc[j]) * f : 0.f;
-      }
-    } else {
-      for (int c = 0; c < p.dv; ++c) orow[c] = 0.f;            // nothing to see
-    }
-    if (PREFIX && n < n_rows) {
-      const int t = row_t(128 * X + row);
-      float* ml = p.ws + ((size_t)(first + t) * p.Hq + (size_t)h * G + (n - t * G)) * ws_head + RAP_MAX_SPLIT * dv4 + 2 * blockIdx.z;
-      *reinterpret_cast<float2*>(ml) = make_float2(m_ref, l_run);
-    }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  }
-  __syncthreads();
-  if (!timed_out) {
-    for (int r = warp; r < 256 && q0 + r < n_rows; r += WT_THREADS / 32) {
-      const int t = row_t(r);
-      const size_t head = (size_t)(first + t) * p.Hq + (size_t)h * G + (q0 + r - t * G);
-      float* dst = PREFIX ? p.ws + head * ws_head + (size_t)blockIdx.z * dv4 : p.out + head * p.dv;
-      const float* src = o_s + (size_t)r * OS;
-      if (!RAP_BOUNDS(first + t, p.rows, p.status, 0x308)) break;
-      for (int c = lane; c < p.dv; c += 32) dst[c] = src[c];
-    }
-  }
+  if (*abort_flag != 0 && tid == 0) win_report(p.status, RAP_ETIMEOUT, *abort_flag);
   if (warp == 8) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
@@ -632,7 +653,7 @@ template <int DK, int NVP, bool LSUM, bool HALF, bool PREFIX>
 rap_status launch_as(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t st) {
   const int smem = WT_SMEM + 1024;
   RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, win_tc_kernel<DK, NVP, LSUM, HALF, PREFIX>, smem));
-  const dim3 grid(blocks, p.Hkv, p.n_split);
+  const dim3 grid(blocks, PREFIX ? 1 : p.Hkv);
   win_tc_kernel<DK, NVP, LSUM, HALF, PREFIX><<<grid, WT_THREADS, smem, st>>>(p);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
@@ -657,10 +678,10 @@ rap_status launch_any(rap_ctx* ctx, const WtParams& p, int blocks, cudaStream_t 
 
 WtParams base_params(rap_ctx* ctx, const rap_win_args& a) {
   WtParams p = {};
-  p.q = (const __nv_bfloat16*)a.q; p.out = a.out; p.ws = ctx->d_attn_ws; p.status = ctx->d_status;
+  p.q = (const __nv_bfloat16*)a.q; p.out = a.out; p.status = ctx->d_status;
   p.rows = a.T; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv; p.P2 = a.P2; p.dv = a.dv;
   p.qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
-  p.n_split = 1;
+  p.sms = ctx->sm_count;
   return p;
 }
 
@@ -687,18 +708,12 @@ rap_status rap_launch_win_prefix(rap_ctx* ctx, const rap_win_args& a, int* n_pre
   WtParams p = base_params(ctx, a);
   p.k = (const __nv_bfloat16*)a.kp; p.v = (const __nv_bfloat16*)a.vp; p.start = a.group_start; p.len = a.prefix_len; p.units = a.n_groups;
   p.S_cap = a.S_pre; p.n_sink = 0; p.window = 0x7fffffff;
-  const int groups = a.n_groups < a.B ? a.n_groups : a.B;
-  const int blocks = (int)((long long)a.B * p.G / 256) + groups;
-  // the split that ends soonest: waves of one CTA an SM, each its tiles and about six tiles' worth of beginning and end
-  const long long tiles = (a.h_prefix_max + WT_KT - 1) / WT_KT, units = (long long)a.Hkv * ((long long)a.B * p.G / 256 + (groups > 1 ? groups : 1));
-  long long best = -1;
-  for (int s = 1; s <= 40 && s <= tiles; ++s) {
-    const long long cost = (units * s + ctx->sm_count - 1) / ctx->sm_count * ((tiles + s - 1) / s + 6);
-    if (best < 0 || cost < best) {
-      best = cost;
-      p.n_split = s;
-    }
-  }
-  *n_pre = p.n_split;
-  return launch_any<true>(ctx, p, blocks, st);
+  // the device makes the plan (win_prefix_plan); here only how many CTAs it can come to
+  const long long tiles = (a.h_prefix_max + WT_KT - 1) / WT_KT, groups = a.n_groups < a.B ? a.n_groups : a.B;
+  const long long pieces = (long long)a.Hkv * (groups > 1 ? (long long)a.B * p.G / 256 + groups : ((long long)a.B * p.G + 255) / 256);
+  const long long blocks = 2 * pieces <= ctx->sm_count ? ctx->sm_count : 4LL * ctx->sm_count + pieces;
+  if (blocks > 0x7fffffffLL) return RAP_ESHAPE;
+  *n_pre = (int)(tiles < WIN_MAX_PRE ? tiles : WIN_MAX_PRE);
+  p.ws = win_partials(ctx->d_attn_ws, (long long)a.B * a.Hq, a.dv, *n_pre);
+  return launch_any<true>(ctx, p, (int)blocks, st);
 }
