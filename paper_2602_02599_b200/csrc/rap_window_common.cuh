@@ -45,22 +45,23 @@ __device__ __forceinline__ int win_owner(const int32_t* start, int n, int r) {
   return lo;
 }
 
-// Partials in the context's workspace: d_v' sums (a multiple of four), and (maximum, weight) pairs apart from them.  The own
-// rows' lie head by head, RAP_MAX_SPLIT - n_pre of them for each; a shared prefix's lie split by split over all heads, n_pre
-// times, ahead of them (a CTA writes one split of 256 neighbouring rows).
+// Partials in the context's workspace: d_v' sums (dv4: a multiple of four), and (maximum, weight) pairs apart from them.  The
+// own rows' lie by unit (sequence, KV head): RAP_MAX_SPLIT - n_pre places, each of the unit's G query heads.  A shared prefix's
+// lie ahead of them split by split over all heads, n_pre times (a CTA writes one split of 256 neighbouring rows).  The sums of
+// one place or split of a unit are one run of G * dv4 floats.
 struct WinPartials {
   float* pre;          // [n_pre][heads][dv4], then [n_pre][heads][2]
-  float* own;          // [heads][slots][dv4], then [heads][slots][2]
+  float* own;          // [units][slots][G][dv4], then [units][slots][G][2]
   long long heads;     // B * H_q
-  int dv4, n_pre, slots;
+  int dv4, n_pre, slots, G;
   __device__ __forceinline__ float* pre_sums(long long head, int s) const { return pre + (s * heads + head) * dv4; }
   __device__ __forceinline__ float2* pre_pair(long long head, int s) const { return reinterpret_cast<float2*>(pre + n_pre * heads * dv4) + s * heads + head; }
-  __device__ __forceinline__ float* own_sums(long long head, int s) const { return own + (head * slots + s) * dv4; }
-  __device__ __forceinline__ float2* own_pair(long long head, int s) const { return reinterpret_cast<float2*>(own + heads * slots * dv4) + head * slots + s; }
+  __device__ __forceinline__ float* own_sums(long long unit, int s) const { return own + (unit * slots + s) * (long long)(G * dv4); }
+  __device__ __forceinline__ float2* own_pair(long long unit, int s) const { return reinterpret_cast<float2*>(own + heads * slots * dv4) + (unit * slots + s) * G; }
 };
-static inline WinPartials win_partials(float* ws, long long heads, int dv, int n_pre) {
+static inline WinPartials win_partials(float* ws, long long heads, int G, int dv, int n_pre) {
   WinPartials w;
-  w.heads = heads; w.dv4 = (dv + 3) & ~3; w.n_pre = n_pre; w.slots = RAP_MAX_SPLIT - n_pre;
+  w.heads = heads; w.G = G; w.dv4 = (dv + 3) & ~3; w.n_pre = n_pre; w.slots = RAP_MAX_SPLIT - n_pre;
   w.pre = ws;
   w.own = ws + ((n_pre * heads * (w.dv4 + 2) + 3) & ~3LL);      // 16-byte aligned
   return w;

@@ -4,16 +4,19 @@
 namespace {
 
 template <bool FOUR, bool VODD>
-const void* scan_fn(int n) {
-  switch (n) {
-    case 1: return (const void*)win_scan_kernel<1, FOUR, VODD>;
-    case 2: return (const void*)win_scan_kernel<2, FOUR, VODD>;
-    case 3: return (const void*)win_scan_kernel<3, FOUR, VODD>;
-    case 4: return (const void*)win_scan_kernel<4, FOUR, VODD>;
-    case 5: return (const void*)win_scan_kernel<5, FOUR, VODD>;
-    case 6: return (const void*)win_scan_kernel<6, FOUR, VODD>;
-    case 7: return (const void*)win_scan_kernel<7, FOUR, VODD>;
-    case 8: return (const void*)win_scan_kernel<8, FOUR, VODD>;
+const void* scan_fn(int n, int nw) {
+  switch (n * 8 + nw) {
+    case 1 * 8 + 4: return (const void*)win_scan_kernel<1, FOUR, VODD, 4>;
+    case 2 * 8 + 4: return (const void*)win_scan_kernel<2, FOUR, VODD, 4>;
+    case 3 * 8 + 4: return (const void*)win_scan_kernel<3, FOUR, VODD, 4>;
+    case 4 * 8 + 4: return (const void*)win_scan_kernel<4, FOUR, VODD, 4>;
+    case 5 * 8 + 4: return (const void*)win_scan_kernel<5, FOUR, VODD, 4>;
+    case 6 * 8 + 4: return (const void*)win_scan_kernel<6, FOUR, VODD, 4>;
+    case 6 * 8 + 3: return (const void*)win_scan_kernel<6, FOUR, VODD, 3>;
+    case 7 * 8 + 4: return (const void*)win_scan_kernel<7, FOUR, VODD, 4>;
+    case 7 * 8 + 3: return (const void*)win_scan_kernel<7, FOUR, VODD, 3>;
+    case 8 * 8 + 2: return (const void*)win_scan_kernel<8, FOUR, VODD, 2>;      // unpruned heads, seven or eight to a KV head
+    case 8 * 8 + 3: return (const void*)win_scan_kernel<8, FOUR, VODD, 3>;
   }
   return nullptr;
 }
@@ -28,12 +31,14 @@ bool rap_win_scan_takes(const rap_win_args& a) {
 rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, cudaStream_t st) {
   WsParams p = {};
   p.q = (const uint32_t*)a.q; p.k = (const unsigned char*)a.k; p.v = (const unsigned char*)a.v; p.seq_len = a.seq_len;
-  p.out = a.out; p.ws = win_partials(ctx->d_attn_ws, (long long)a.B * a.Hq, a.dv, n_pre); p.ws_floats = (long long)(ctx->attn_ws_bytes / sizeof(float)); p.status = ctx->d_status;
+  p.out = a.out; p.ws = win_partials(ctx->d_attn_ws, (long long)a.B * a.Hq, a.Hq / a.Hkv, a.dv, n_pre); p.ws_floats = (long long)(ctx->attn_ws_bytes / sizeof(float)); p.status = ctx->d_status;
   p.B = a.B; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.Hq / a.Hkv; p.P = a.P2 / 2; p.dv = a.dv; p.S_cap = a.S_cap;
   p.n_sink = a.n_sink; p.window = a.window; p.len_cap = a.n_groups ? a.S_cap : 0x7fffffff;
   p.qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
   p.n_groups = a.n_groups; p.group_start = a.group_start; p.prefix_len = a.prefix_len; p.S_pre = a.S_pre; p.sms = ctx->sm_count;
   p.wait_limit = WAIT_LIMIT;
+  // what a unit's end takes, in blocks of half a microsecond: 3 us, or 10 with a prefix's splits to join
+  p.own = n_pre ? 20 : 6;
   {   // two sets of counters take turns; each launch clears the one its predecessor used
     const size_t n_units = (size_t)ctx->desc.max_batch * ctx->desc.n_kv_heads;
     const uint32_t set = ctx->win_epoch++ & 1u;
@@ -57,26 +62,25 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
     // d_v' wants the two rows of a register to be of one parity
     p.rs_log = (p.P & 1) ? 2 : (p.P & 2) ? 1 : vodd ? 1 : 0;
   }
-  p.per_cta = 4;
   p.stage_bytes = (32 * (p.k_stride + p.v_stride) + 16 + 127) / 128 * 128;
   const int cw = (vodd ? a.dv + 1 : a.dv);
-  // two CTAs an SM; four warps with two stages each where they fit (up to 14 KB a stage), else three
-  p.n_stages = 2;
-  int smem = 0;
-  for (p.n_warps = 4; p.n_warps > 1; --p.n_warps) {
-    const int red = p.n_warps * p.G * cw * 4, join = (p.G * RAP_MAX_SPLIT + 8) * 4;
-    p.off_stage = (512 + (red > join ? red : join) + 127) / 128 * 128;
-    smem = p.off_stage + p.n_warps * p.n_stages * p.stage_bytes;
-    if (smem <= SMEM_BUDGET) break;
-  }
+  // two CTAs an SM; four warps with two stages each where they fit (up to 13 KB a stage), else three
   const int nk = (p.P + 7) / 8, nv = (a.dv + 15) / 16, n = nk > nv ? nk : nv;
-  const void* fn = p.G <= 4 ? (vodd ? scan_fn<true, true>(n) : scan_fn<true, false>(n)) : (vodd ? scan_fn<false, true>(n) : scan_fn<false, false>(n));
+  int nw = n == 8 ? 3 : 4, smem = 0;
+  for (;; --nw) {
+    const int red = nw * p.G * cw * 4, join = p.G * RAP_MAX_SPLIT * 4;
+    p.off_stage = (512 + (red > join ? red : join) + 127) / 128 * 128;
+    smem = p.off_stage + nw * WS_STAGES * p.stage_bytes;
+    p.join_places = nw * WS_STAGES * p.stage_bytes / (4 * p.G * p.ws.dv4);      // partials that fit the stages
+    if (smem <= SMEM_BUDGET || nw == 2) break;
+  }
+  const void* fn = p.G <= 4 ? (vodd ? scan_fn<true, true>(n, nw) : scan_fn<true, false>(n, nw)) : (vodd ? scan_fn<false, true>(n, nw) : scan_fn<false, false>(n, nw));
   if (!fn || smem > SMEM_BUDGET) return RAP_EUNSUPPORTED;
   RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, fn, SMEM_BUDGET));
   void* args[] = {&p};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * ctx->sm_count);
-  cfg.blockDim = dim3(32 * p.n_warps);
+  cfg.blockDim = dim3(32 * nw);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

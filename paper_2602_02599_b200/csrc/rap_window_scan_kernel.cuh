@@ -22,9 +22,6 @@
 
 namespace {
 
-// blocks that a unit's end takes as long as: joining the warps, its partial, the arrival (3 us against 0.5 us a block)
-constexpr int WS_OWN = 6;
-
 struct WsParams {
   const uint32_t* q;          // [B][Hq][P] bf16 pairs
   const unsigned char* k;     // [B][Hkv][S_cap][4 P bytes]
@@ -42,8 +39,9 @@ struct WsParams {
   int pad16;                  // 1: rows of a multiple of 16 bytes, copied into padded rows; 0: bulk copies
   int k_stride, v_stride;     // bytes between rows in shared memory
   int rs_log;                 // log2 of the row step between the columns of a fragment
-  int stage_bytes, n_stages, n_warps, off_stage;
-  int per_cta;                // least blocks of a CTA
+  int stage_bytes, off_stage;
+  int own;                    // blocks that a unit's end takes as long as
+  int join_places;            // partials that the stages hold together
   uint32_t wait_limit;
   // shared prefixes (ws.n_pre > 0): what the plan of their splits is made of
   int n_groups, S_pre, sms;
@@ -102,11 +100,15 @@ __device__ __forceinline__ int ws_scan_add(int x, int lane) {      // inclusive 
   return x;
 }
 
-// N: steps of 16 dims and blocks of 16 channels (the larger of the two); FOUR: up to four query heads a KV head; VODD: d_v' odd
-template <int N, bool FOUR, bool VODD>
-__global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
+// N: steps of 16 dims and blocks of 16 channels (the larger of the two); FOUR: up to four query heads a KV head; VODD: d_v' odd;
+// NW: warps.  A short launch executes most of this once a CTA, so what it costs is fetching it: divisions by run-time numbers
+// and 64-bit ones are kept out of the usual path.
+constexpr int WS_STAGES = 2;
+template <int N, bool FOUR, bool VODD, int NW>
+__global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                         // [NW][stages], 128 bytes
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                         // [NW][stages], at most 64 bytes; then the join's
+  const uint32_t bar_join = smem_u32(smem) + 64;
   float* m_s = reinterpret_cast<float*>(smem + 128);                          // [4][8]
   float* l_s = m_s + 32;                                                      // [4][8]
   int* s_flag = reinterpret_cast<int*>(smem + 384);
@@ -114,21 +116,29 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   float* red = reinterpret_cast<float*>(smem + 512);                          // [NW][G][CW]; later the join's weights
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gid = lane >> 2, tq = lane & 3;
-  const int NW = p.n_warps, NSTG = p.n_stages, THREADS = NW * 32;
+  constexpr int NSTG = WS_STAGES, THREADS = NW * 32;
   const int G = p.G, P = p.P, dv = p.dv;
 
-  // ---- the plan: every warp works it out from the lengths.  A unit counts WS_OWN blocks more than it has: what its end costs ----
+  if (tid == 0) {
+    *s_flag = 0;
+    for (int i = 0; i < NW * NSTG; ++i) mbar_init(smem_u32(bars) + 8 * i, p.pad16 ? 32 : 1);
+    mbar_init(bar_join, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // ---- the plan: every warp works it out from the lengths.  A unit counts p.own blocks more than it has ----
   int T = 0, n_max = 1, n_first = 0;
   for (int b0 = 0; b0 < p.B; b0 += 32) {
-    const int n = b0 + lane < p.B ? ws_unit(p, b0 + lane).n + WS_OWN : 0;
+    const int n = b0 + lane < p.B ? ws_unit(p, b0 + lane).n + p.own : 0;
     if (b0 == 0) n_first = n;
     n_max = max(n_max, __reduce_max_sync(0xffffffffu, n));
     T += __reduce_add_sync(0xffffffffu, n);
   }
   T *= p.Hkv;
   // no unit is touched by more CTAs than there is room for partials behind the prefix's, and every CTA has a block for each warp
-  const long long room = (long long)(RAP_MAX_SPLIT - 2 - p.ws.n_pre) * T / n_max;
-  const int nc = (int)max(1LL, min(min((long long)gridDim.x, room), (long long)(T + p.per_cta - 1) / p.per_cta));
+  const int places = RAP_MAX_SPLIT - 2 - p.ws.n_pre;
+  int nc = min((int)gridDim.x, (T + 3) >> 2);
+  // ... (a unit of n_max blocks falls to at most n_max nc / T + 2 CTAs)
+  if (n_max > T / (int)gridDim.x * places) nc = (int)max(1LL, min((long long)nc, (long long)places * T / n_max));
   if (blockIdx.x == 0)
     for (int i = tid; i < p.other_units; i += THREADS) p.unit_cnt_other[i] = 0;      // what a launch that gave up left behind
   if ((int)blockIdx.x >= nc) {
@@ -142,7 +152,7 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   const int hi = cur + share + ((int)blockIdx.x < extra ? 1 : 0);
   int b = 0, h, unit_start = 0;
   for (int b0 = 0, carry = 0;; b0 += 32) {
-    const int n = (b0 == 0 ? n_first : b0 + lane < p.B ? ws_unit(p, b0 + lane).n + WS_OWN : 0) * p.Hkv;
+    const int n = (b0 == 0 ? n_first : b0 + lane < p.B ? ws_unit(p, b0 + lane).n + p.own : 0) * p.Hkv;
     const int x = ws_scan_add(n, lane) + carry;
     const unsigned past = __ballot_sync(0xffffffffu, x > cur);
     if (past) {
@@ -154,8 +164,8 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
     carry = __shfl_sync(0xffffffffu, x, 31);
   }
   WsUnit u = ws_unit(p, b);
-  h = (cur - unit_start) / (u.n + WS_OWN);
-  unit_start += h * (u.n + WS_OWN);
+  h = (cur - unit_start) / (u.n + p.own);
+  unit_start += h * (u.n + p.own);
 
   int pre_per = 1;
   if (p.ws.n_pre)
@@ -163,13 +173,6 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   const uint32_t bar0 = smem_u32(bars) + warp * NSTG * 8;
   unsigned char* wstage = smem + p.off_stage + (size_t)warp * NSTG * p.stage_bytes;
   const uint32_t wstage_u = smem_u32(wstage);
-  if (tid == 0) {
-    *s_flag = 0;
-    for (int i = 0; i < NW * NSTG; ++i) mbar_init(smem_u32(bars) + 8 * i, p.pad16 ? 32 : 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  __syncthreads();
-
   // ---- fragment addresses inside a stage, in 32-bit words ----
   auto frag_row = [&](int t, int n) { return (n << p.rs_log) + (t & ((1 << p.rs_log) - 1)) + ((t >> p.rs_log) << (3 + p.rs_log)); };
   const int v_base = (32 * p.k_stride) >> 2;
@@ -187,19 +190,22 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
   const float cs = p.qscale;
   const int k_row = 4 * P, v_row = 2 * dv;                    // bytes in the cache
 
+  __syncthreads();             // the barriers are initialised
+  bool used = false;           // the ring has been read: copies into it come after those reads
   int st = 0;                  // ring position and phase of this warp, across units
   uint32_t parity = 0;
   bool timed_out = false, joined = false;
+  uint32_t join_parity = 0;
 
   for (;;) {   // one pass per unit that this CTA touches
-    const int t0 = max(cur - unit_start - WS_OWN, 0);               // this CTA's blocks of the unit: [t0, t0 + n_my)
-    const int n_my = min(u.n, hi - unit_start - WS_OWN) - t0;
+    const int t0 = max(cur - unit_start - p.own, 0);               // this CTA's blocks of the unit: [t0, t0 + n_my)
+    const int n_my = min(u.n, hi - unit_start - p.own) - t0;
     if (n_my <= 0) break;                                           // its share ends in what the unit counts beyond its blocks
     const size_t unit = (size_t)b * p.Hkv + h;
     const unsigned char* kg = p.k + unit * (size_t)p.S_cap * (size_t)k_row;
     const unsigned char* vg = p.v + unit * (size_t)p.S_cap * (size_t)v_row;
     const bool empty = u.nb[0] + u.nb[1] + u.nb[2] == 0;
-    const int n_blk = !empty && n_my > warp ? (n_my - warp + NW - 1) / NW : 0;
+    const int n_blk = !empty && n_my > warp ? (int)((unsigned)(n_my - warp + NW - 1) / NW) : 0;
     int n_pre = 0;             // partials of the prefix, if the sequence has one
     if (p.ws.n_pre) {
       const int g = win_owner(p.group_start, p.n_groups, b);
@@ -242,7 +248,7 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
       } else if (lane == 0) {
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // earlier reads and zeros come first
+        if (used) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // earlier reads and zeros come first
         mbar_expect_tx(bar, ok ? (uint32_t)(rows * (k_row + v_row)) : 0u);
         if (ok) {
           bulk_g2s(dst, ks, (uint32_t)(rows * k_row), bar);
@@ -250,7 +256,8 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         }
       }
     };
-    for (int i = 0; i < min(n_blk, NSTG - 1); ++i) issue_block(i, (st + i) % NSTG);
+    static_assert(NSTG == 2, "one block ahead");
+    if (n_blk > 0) issue_block(0, st);
 
     // ---- q as the A operand: words (8 ks + tq) and (8 ks + 4 + tq) of the lane's head; zero where a step overlaps the one before ----
     uint32_t qa[N][2];
@@ -276,7 +283,7 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
     float m_ref = -INFINITY, l_thr = 0.f;
 
     for (int i = 0; i < n_blk; ++i) {
-      if (i + NSTG - 1 < n_blk) issue_block(i + NSTG - 1, (st + NSTG - 1) % NSTG);
+      if (i + 1 < n_blk) issue_block(i + 1, st ^ 1);
       if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar0 + 8 * st, parity, p.wait_limit))) {
         timed_out = true;
         break;
@@ -397,6 +404,7 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         }
       }
       __syncwarp();            // every lane is done with this stage before it is filled again
+      used = true;
       if (++st == NSTG) { st = 0; parity ^= 1u; }
     }
 
@@ -408,6 +416,7 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
     __syncthreads();
     if (*s_flag) {
       if (tid == 0) win_report(p.status, RAP_ETIMEOUT, (int)unit);
+      if (p.ws.n_pre) pdl_wait();
       // copies still in flight get a bounded chance to land before the shared memory is released
       if (lane == 0)
         for (int sg = 0; sg < NSTG; ++sg) {
@@ -438,12 +447,12 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         }
     }
     __syncthreads();
-    const int first = cta_of(unit_start + WS_OWN), n_seg = cta_of(unit_start + WS_OWN + u.n - 1) - first + 1;
+    const int first = cta_of(unit_start + p.own), n_seg = cta_of(unit_start + p.own + u.n - 1) - first + 1;
     const bool alone = n_seg == 1 && n_pre == 0;
     const int dv4 = p.ws.dv4, my_seg = (int)blockIdx.x - first;
     const long long head0 = (long long)b * p.Hq + (long long)h * G;            // the unit's first query head
     const bool ws_ok = RAP_BOUNDS(my_seg, p.ws.slots, p.status, 0x206) &&
-                       RAP_BOUNDS(reinterpret_cast<float*>(p.ws.own_pair(head0 + G - 1, my_seg)) + 1 - p.ws.pre, p.ws_floats, p.status, 0x207);
+                       RAP_BOUNDS(reinterpret_cast<float*>(p.ws.own_pair(unit, my_seg) + G) - 1 - p.ws.pre, p.ws_floats, p.status, 0x207);
     for (int g = warp; g < G && ws_ok; g += NW) {
       float l = 0.f, mm = -INFINITY;
       for (int i = 0; i < NW; ++i) {
@@ -455,28 +464,48 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
         float sum = 0.f;
         for (int i = 0; i < NW; ++i) sum += red[((size_t)i * G + g) * CW + c];
         if (alone) out[(size_t)g * dv + c] = sum * inv;
-        else p.ws.own_sums(head0 + g, my_seg)[c] = sum;
+        else p.ws.own_sums(unit, my_seg)[g * dv4 + c] = sum;
       }
-      if (!alone && lane == 0) *p.ws.own_pair(head0 + g, my_seg) = make_float2(mm, l);
+      if (!alone && lane == 0) p.ws.own_pair(unit, my_seg)[g] = make_float2(mm, l);
     }
     if (!alone) {
       // ---- who delivers a unit's last partial joins them, in order ----
-      __threadfence();
       __syncthreads();
-      if (tid == 0) *s_last = n_seg == 1 || (RAP_BOUNDS(unit, (size_t)p.B * p.Hkv, p.status, 0x208) && atomicAdd(&p.unit_cnt[unit], 1) == n_seg - 1);
+      if (tid == 0) {          // what the CTA has written is released with its arrival, what others have written acquired
+        int before = n_seg - 1;
+        if (n_seg > 1 && RAP_BOUNDS(unit, (size_t)p.B * p.Hkv, p.status, 0x208))
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(&p.unit_cnt[unit]) : "memory");
+        *s_last = before == n_seg - 1;
+      }
       __syncthreads();
       if (*s_last) {
         if (p.ws.n_pre && !joined) pdl_wait();        // the prefix's partials come from the launch before
         joined = true;
-        __threadfence();
-        const int n = n_pre + n_seg;               // <= RAP_MAX_SPLIT
+        // The partials' sums come in as bulk copies, one round trip for all that fit the stages (all units' partials but the
+        // largest): the prefix's split by split, the own ones in one run.  Their weights are worked out meanwhile.
+        const int n = n_pre + n_seg, part = G * dv4;                 // n <= RAP_MAX_SPLIT
+        float* sums = reinterpret_cast<float*>(smem + p.off_stage);
         float* wgt = red;                          // [G][RAP_MAX_SPLIT] weights over their sum
+        auto fetch = [&](int s0, int m) {          // warp 0: partials [s0, s0 + m)
+          if (lane == 0) {
+            asm volatile("fence.proxy.async;" ::: "memory");        // the stages have been read; other CTAs' partials are acquired
+            mbar_expect_tx(bar_join, (uint32_t)(m * part * 4));
+          }
+          __syncwarp();
+          for (int s = s0 + lane; s < min(s0 + m, n_pre); s += 32)
+            bulk_g2s(smem_u32(sums + (s - s0) * part), p.ws.pre_sums(head0, s), (uint32_t)(part * 4), bar_join);
+          const int o0 = max(s0, n_pre), o1 = s0 + m;
+          if (lane == 0 && o1 > o0)
+            bulk_g2s(smem_u32(sums + (o0 - s0) * part), p.ws.own_sums(unit, o0 - n_pre), (uint32_t)((o1 - o0) * part * 4), bar_join);
+        };
+        int m = min(n, p.join_places);
+        if (warp == 0) fetch(0, m);
         for (int g = warp; g < G; g += NW) {
           float mv[2], lv[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int sg = lane + 32 * k;
-            const float2 x = sg < n_pre ? __ldcg(p.ws.pre_pair(head0 + g, sg)) : sg < n ? __ldcg(p.ws.own_pair(head0 + g, sg - n_pre)) : make_float2(-INFINITY, 0.f);
+            const float2 x = sg < n_pre ? __ldcg(p.ws.pre_pair(head0 + g, sg)) : sg < n ? __ldcg(p.ws.own_pair(unit, sg - n_pre) + g) : make_float2(-INFINITY, 0.f);
             lv[k] = x.y;
             mv[k] = x.y != 0.f ? x.x : -INFINITY;
           }
@@ -495,43 +524,61 @@ __global__ void __launch_bounds__(128, 2) win_scan_kernel(const WsParams p) {
           wgt[g * RAP_MAX_SPLIT + lane] = mv[0] * inv;
           wgt[g * RAP_MAX_SPLIT + lane + 32] = mv[1] * inv;
         }
-        __syncthreads();
-        const int c4 = dv4 >> 2;
-        for (int i = tid; i < G * c4; i += THREADS) {     // four channels of a head
-          const int g = i / c4, c = 4 * (i - g * c4);
-          const float* pb = p.ws.pre_sums(head0 + g, 0) + c;
-          const float* ob = p.ws.own_sums(head0 + g, 0) + c;
-          const long long pre_step = p.ws.heads * dv4;
-          const float* wg = wgt + g * RAP_MAX_SPLIT;
-          float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int s0 = 0; s0 < n; s0 += 8) {      // eight loads in flight
-            float4 av[8];
+        constexpr int COLS = (8 * 32 + THREADS - 1) / THREADS;      // groups of four channels a thread has, at most
+        float4 num[COLS];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int sg = min(s0 + k, n - 1);
-              av[k] = __ldcg(reinterpret_cast<const float4*>(sg < n_pre ? pb + sg * pre_step : ob + (sg - n_pre) * dv4));
-            }
+        for (int k = 0; k < COLS; ++k) num[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        bool got = true;
+        for (int s0 = 0;;) {
+          __syncthreads();
+          got = __syncthreads_and(mbar_wait_bounded(bar_join, join_parity, p.wait_limit));
+          join_parity ^= 1u;
+          if (!got) break;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float wk = s0 + k < n ? wg[s0 + k] : 0.f;
-              num.x = fmaf(wk, av[k].x, num.x);
-              num.y = fmaf(wk, av[k].y, num.y);
-              num.z = fmaf(wk, av[k].z, num.z);
-              num.w = fmaf(wk, av[k].w, num.w);
+          for (int k = 0; k < COLS; ++k) {
+            const int i = 4 * (tid + k * THREADS);
+            if (i < part) {
+              const float* wg = wgt + i / dv4 * RAP_MAX_SPLIT + s0;
+              for (int s = 0; s < m; ++s) {
+                const float4 v = *reinterpret_cast<const float4*>(sums + s * part + i);
+                const float wk = wg[s];
+                num[k].x = fmaf(wk, v.x, num[k].x);
+                num[k].y = fmaf(wk, v.y, num[k].y);
+                num[k].z = fmaf(wk, v.z, num[k].z);
+                num[k].w = fmaf(wk, v.w, num[k].w);
+              }
             }
           }
-          float* og = out + (size_t)g * dv + c;
-          og[0] = num.x;
-          if (c + 1 < dv) og[1] = num.y;
-          if (c + 2 < dv) og[2] = num.z;
-          if (c + 3 < dv) og[3] = num.w;
+          s0 += m;
+          if (s0 >= n) break;
+          m = min(n - s0, p.join_places);
+          __syncthreads();
+          if (warp == 0) fetch(s0, m);
         }
+        if (!got) {
+          if (tid == 0) win_report(p.status, RAP_ETIMEOUT, (int)unit);
+          if (p.ws.n_pre) pdl_wait();
+          return;
+        }
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) {
+          const int i = 4 * (tid + k * THREADS);
+          if (i < part) {
+            const int g = i / dv4, c = i - g * dv4;
+            float* og = out + (size_t)g * dv + c;
+            og[0] = num[k].x;
+            if (c + 1 < dv) og[1] = num[k].y;
+            if (c + 2 < dv) og[2] = num[k].z;
+            if (c + 3 < dv) og[3] = num[k].w;
+          }
+        }
+        used = true;
         if (tid == 0) p.unit_cnt[unit] = 0;        // ready for the next call
       }
     }
     }
     // ---- the next unit, from its first block ----
-    unit_start += u.n + WS_OWN;
+    unit_start += u.n + p.own;
     cur = unit_start;
     if (cur >= hi) break;
     if (++h == p.Hkv) {

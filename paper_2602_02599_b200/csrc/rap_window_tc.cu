@@ -714,6 +714,6 @@ rap_status rap_launch_win_prefix(rap_ctx* ctx, const rap_win_args& a, int* n_pre
   const long long blocks = 2 * pieces <= ctx->sm_count ? ctx->sm_count : 4LL * ctx->sm_count + pieces;
   if (blocks > 0x7fffffffLL) return RAP_ESHAPE;
   *n_pre = (int)(tiles < WIN_MAX_PRE ? tiles : WIN_MAX_PRE);
-  p.ws = win_partials(ctx->d_attn_ws, (long long)a.B * a.Hq, a.dv, *n_pre);
+  p.ws = win_partials(ctx->d_attn_ws, (long long)a.B * a.Hq, p.G, a.dv, *n_pre);
   return launch_any<true>(ctx, p, (int)blocks, st);
 }
