@@ -283,10 +283,15 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   const int row = (warp & 3) * 32 + lane;
   const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
   const uint32_t tmem_o = tmem_base + 256 + 128 * X;
-  // registers: 256 threads of 168 and 256 of 88 are the 512 x 128 that the block has
+  // registers: two times 256 threads share the 512 x 128 that the block has (the prefix's staging holds more addresses)
   static_assert(WT_THREADS == 512, "the split below is of 512 threads");
-  if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-  else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  if constexpr (PREFIX) {
+    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+  } else {
+    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  }
   if (warp >= 10) {
     // ================= producers: WT_NP warps each stage K and V, eight tile rows at a time =================
     const bool is_v = warp >= 10 + WT_NP;
@@ -306,7 +311,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     // the rows of a tile are one run from row s0 on unless the tile crosses the seam of a rolling cache
     auto run_of = [&](int j0, int n, int& s0) {
       s0 = j0;
-      if (j0 + n <= p.S_cap) return true;
+      if (PREFIX || j0 + n <= p.S_cap) return true;
       s0 = j0 >= p.n_sink ? p.n_sink + (j0 - p.n_sink) % R : j0;
       return s0 + n <= p.S_cap;
     };
@@ -325,6 +330,20 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         if (two) pt_cp4(du + g * 1024 + swz[c] + 8192, src + 128, bytes);
       }
     };
+    // A prefix's rows come from HBM, once: what a launch keeps on its way with 4-byte copies alone is a third of what HBM takes
+    // (2200 cycles a tile), so their lines are asked into L2 some tiles ahead, a tile's as one bulk request of whole 16-byte
+    // units (a cache's end is one: S_cap is a multiple of 8).
+    constexpr int L2_AHEAD = 12;
+    auto prefetch = [&](int tile) {
+      if (!PREFIX || pw != 0 || lane != 0 || tile >= n_max) return;
+      int j0, j1;
+      tile_at(tile, j0, j1);
+      const size_t b0 = (size_t)j0 * (size_t)rb & ~(size_t)15, b1 = ((size_t)min(j0 + WT_KT, j1) * (size_t)rb + 15) & ~(size_t)15;
+      if (!RAP_BOUNDS(b1 - 1, (size_t)p.S_cap * (size_t)rb, p.status, 0x30a)) return;
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src0 + b0), "r"((uint32_t)(b1 - b0)) : "memory");
+    };
+#pragma unroll 1
+    for (int t = 0; t < L2_AHEAD; ++t) prefetch(t);
     if (HALF && is_v) {
       // Rows of an odd number of half words: every other one starts in the middle of a word.  The words that hold a row are
       // copied as they lie, AHEAD tiles ahead; once they have landed, a lane that copied a word of such a row puts its half and
@@ -338,6 +357,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           if (use > 0 && !__all_sync(0xffffffffu, wait(bar_e + 8 * stg, (use - 1) & 1))) break;
           const int n = min(WT_KT, j1 - j0);
           const bool run = run_of(j0, n, s0);
+          prefetch(step + L2_AHEAD);
           copy_rows(pt_smem(ring + stg * WT_KV_BYTES), step, j0, n, run, s0);
           if (++stg == WT_STAGES) { stg = 0; ++use; }
         }
@@ -378,6 +398,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         const uint32_t du = pt_smem(ring + stg * WT_KV_BYTES);
         const int n = min(WT_KT, j1 - j0);
         const bool run = run_of(j0, n, s0);
+        prefetch(tile + L2_AHEAD);
         if (!RAP_BOUNDS(n - 1, WT_KT, p.status, 0x304) || !RAP_BOUNDS(run ? s0 : 0, p.S_cap, p.status, 0x305) ||
             !RAP_BOUNDS(run ? s0 + n - 1 : 0, p.S_cap, p.status, 0x306))
           break;
