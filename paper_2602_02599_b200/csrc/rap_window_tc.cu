@@ -25,8 +25,7 @@
 namespace {
 
 constexpr int WT_KT = 64;                              // keys per tile
-constexpr int WT_NP = 3;                               // warps that stage K, and as many that stage V
-constexpr int WT_THREADS = 32 * (8 + 2 + 2 * WT_NP);   // 8 softmax warps, 2 that issue MMAs
+constexpr int WT_THREADS = 512;                        // 8 softmax warps, 2 that issue MMAs, 6 that stage K and V
 constexpr int WT_Q_BYTES = 2 * 128 * 128;              // [128 rows][<= 128 dims]: two 64-element atom columns
 constexpr int WT_KV_BYTES = 2 * WT_KT * 128;           // [64 keys][<= 128 dims or channels]
 constexpr int WT_TAIL = 320;                           // mbarriers, TMEM address, give-up flag
@@ -125,6 +124,7 @@ __device__ __forceinline__ void wt_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 // workspace; otherwise the rows are new tokens of sequence `unit`.
 template <int DK, int NVP, bool LSUM, bool HALF, bool PREFIX>
 __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p) {
+  constexpr int NK = HALF ? 2 : 3, NV = 6 - NK;        // warps that stage K, and V (of odd width: twice the work)
   extern __shared__ unsigned char wt_raw[];
   unsigned char* smem = wt_raw + ((1024u - (pt_smem(wt_raw) & 1023u)) & 1023u);
   unsigned char* q_s = smem;                                   // Q_A, Q_B
@@ -225,9 +225,9 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
 
   if (tid == 0) {
     for (int i = 0; i < WT_STAGES; ++i) {
-      pt_mbar_init(bar_fk + 8 * i, 32 * WT_NP);
+      pt_mbar_init(bar_fk + 8 * i, 32 * NK);
       pt_mbar_init(bar_ek + 8 * i, 2);               // both MMA-issuing lanes release a buffer
-      pt_mbar_init(bar_fv + 8 * i, 32 * WT_NP);
+      pt_mbar_init(bar_fv + 8 * i, 32 * NV);
       pt_mbar_init(bar_ev + 8 * i, 2);
     }
     for (int i = 0; i < 4; ++i) {
@@ -283,9 +283,10 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   const int row = (warp & 3) * 32 + lane;
   const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
   const uint32_t tmem_o = tmem_base + 256 + 128 * X;
-  // registers: two times 256 threads share the 512 x 128 that the block has (the prefix's staging holds more addresses)
+  // registers: two times 256 threads share the 512 x 128 that the block has (staging a prefix or
+  // odd rows holds more addresses)
   static_assert(WT_THREADS == 512, "the split below is of 512 threads");
-  if constexpr (PREFIX) {
+  if constexpr (PREFIX || HALF) {
     if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
   } else {
@@ -293,9 +294,9 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   }
   if (warp >= 10) {
-    // ================= producers: WT_NP warps each stage K and V, eight tile rows at a time =================
-    const bool is_v = warp >= 10 + WT_NP;
-    const int pw = warp - 10 - (is_v ? WT_NP : 0);
+    // ================= producers: NK warps stage K, NV warps V, eight tile rows at a time =================
+    const bool is_v = warp >= 10 + NK;
+    const int pw = warp - 10 - (is_v ? NK : 0), np = is_v ? NV : NK;
     const int rowlen = is_v ? p.dv : p.P2, rb = 2 * rowlen;
     const unsigned char* src0 = reinterpret_cast<const unsigned char*>(is_v ? vg : kg) + 4 * lane;
     unsigned char* ring = is_v ? v_s : k_s;
@@ -316,18 +317,34 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       return s0 + n <= p.S_cap;
     };
     // the first of this warp's groups of eight rows; they take turns, so that the odd group falls to each of them
-    auto first_group = [&](int tile) { return (pw + tile) % WT_NP; };
+    auto first_group = [&](int tile) { return is_v ? (pw + tile) % NV : (pw + tile) % NK; };
     // words as they lie in the cache, row by row; rows behind the tile's last are zeros and nothing is read for them
     auto copy_rows = [&](uint32_t du, int tile, int j0, int n, bool run, int s0) {
+      const size_t first_byte = (size_t)s0 * (size_t)rb;
+      const unsigned char* run0 = src0 + (first_byte & ~(size_t)3);
+      const int head = (int)(first_byte & 3);
 #pragma unroll 1
-      for (int g = first_group(tile); g < WT_KT / 8; g += WT_NP)
+      for (int g = first_group(tile); g < WT_KT / 8; g += np) {
+        const uint32_t dg = du + g * 1024;
+        if (run) {
 #pragma unroll
-       for (int c = 0; c < 8; ++c) {
-        const int i = 8 * g + c, r = key_of(i), sl = r < n ? (run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap)) : 0;
-        const unsigned char* src = src0 + (((size_t)sl * (size_t)rb) & ~(size_t)3);
-        const int bytes = r < n && RAP_BOUNDS(sl, p.S_cap, p.status, 0x302) ? 4 : 0;
-        if (one) pt_cp4(du + g * 1024 + swz[c], src, bytes);
-        if (two) pt_cp4(du + g * 1024 + swz[c] + 8192, src + 128, bytes);
+          for (int c = 0; c < 8; ++c) {
+            const int r = key_of(8 * g + c), bytes = r < n && RAP_BOUNDS(s0 + r, p.S_cap, p.status, 0x302) ? 4 : 0;
+            const unsigned char* src = run0 + (bytes ? (head + r * rb) & ~3 : 0);
+            if (one) pt_cp4(dg + swz[c], src, bytes);
+            if (two) pt_cp4(dg + swz[c] + 8192, src + 128, bytes);
+          }
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < 8; ++c) {
+            const int r = key_of(8 * g + c), sl = r < n ? win_slot(j0 + r, p.n_sink, p.S_cap) : 0;
+            const unsigned char* src = src0 + (((size_t)sl * (size_t)rb) & ~(size_t)3);
+            const int bytes = r < n && RAP_BOUNDS(sl, p.S_cap, p.status, 0x303) ? 4 : 0;
+            const uint32_t d = dg + 128u * c + pt_swz2(4 * lane, c);
+            if (one) pt_cp4(d, src, bytes);
+            if (two) pt_cp4(d + 8192, src + 128, bytes);
+          }
+        }
       }
     };
     // A prefix's rows come from HBM, once: what a launch keeps on its way with 4-byte copies alone is a third of what HBM takes
@@ -368,22 +385,27 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         tile_at(step - AHEAD, j0, j1);
         const bool run = run_of(j0, min(WT_KT, j1 - j0), s0);
         unsigned char* vt = ring + fix * WT_KV_BYTES;
-#pragma unroll 1
-        for (int g = first_group(step - AHEAD); g < WT_KT / 8; g += WT_NP)
-#pragma unroll
-         for (int c = 0; c < 8; ++c) {
-          const int r = key_of(8 * g + c), sl = run ? s0 + r : win_slot(j0 + r, p.n_sink, p.S_cap);
-          uint32_t* w0 = reinterpret_cast<uint32_t*>(vt + g * 1024 + swz[c]);
+        // (without a branch on the row's parity: eight rows' loads, shuffles and stores then overlap)
+        auto place = [&](uint32_t* w0, int odd) {
           uint32_t v0 = w0[0], v1 = w0[2048];
-          if (sl & 1) {                                // the same for the whole warp
-            const uint32_t n0 = __shfl_sync(0xffffffffu, v0, (lane + 1) & 31), n1 = __shfl_sync(0xffffffffu, v1, (lane + 1) & 31);
-            v0 = __funnelshift_r(v0, lane == 31 ? n1 : n0, 16);
-            v1 = __funnelshift_r(v1, n1, 16);
-          }
+          const uint32_t n0 = __shfl_sync(0xffffffffu, v0, (lane + 1) & 31), n1 = __shfl_sync(0xffffffffu, v1, (lane + 1) & 31);
+          v0 = __funnelshift_r(v0, lane == 31 ? n1 : n0, odd * 16);
+          v1 = __funnelshift_r(v1, n1, odd * 16);
           if (LSUM && lane == words - 1) v0 = (v0 & 0xffffu) | 0x3f800000u;
           if (LSUM && lane + 32 == words - 1) v1 = (v1 & 0xffffu) | 0x3f800000u;
           if (one) w0[0] = v0;
           if (two) w0[2048] = v1;
+        };
+#pragma unroll 1
+        for (int g = first_group(step - AHEAD); g < WT_KT / 8; g += np) {
+          if (run) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) place(reinterpret_cast<uint32_t*>(vt + g * 1024 + swz[c]), (s0 + key_of(8 * g + c)) & 1);
+          } else {
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c)
+              place(reinterpret_cast<uint32_t*>(vt + g * 1024 + 128 * c + pt_swz2(4 * lane, c)), win_slot(j0 + key_of(8 * g + c), p.n_sink, p.S_cap) & 1);
+          }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_f + 8 * fix) : "memory");
@@ -406,7 +428,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           // a full tile in one run: no predicates, running pointers (V: from key k to k + 8 and back to k + 1)
           const long long even = is_v ? 8LL * rb : rb, odd = is_v ? -7LL * rb : rb;
 #pragma unroll 1
-          for (int g = first_group(tile); g < WT_KT / 8; g += WT_NP) {
+          for (int g = first_group(tile); g < WT_KT / 8; g += np) {
             const unsigned char* a = src0 + (size_t)(s0 + key_of(8 * g)) * (size_t)rb;
             const uint32_t dg = du + g * 1024;
 #pragma unroll
