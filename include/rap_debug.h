@@ -43,7 +43,8 @@ rap_status rap_set_proj_variant(rap_ctx* ctx, int32_t variant);
  * millions.  That warp gives up, its CTA records RAP_ETIMEOUT in the device status word, waits (bounded) for its
  * other copies and returns; every other CTA finishes normally.  The units that CTA touched stay unfinished (their
  * outputs are not written).  Later launches run normally: each launch clears the arrival counters its predecessor
- * used, so nothing has to be reset by hand.  The hook disarms itself when it is used. */
+ * used, so nothing has to be reset by hand.  The hook disarms itself when it is used.  The scan of
+ * rap_decode_attn_window and rap_decode_attn_shared takes it the same way, whichever is launched next. */
 rap_status rap_debug_arm_wait_timeout(rap_ctx* ctx);
 
 /* The tensor-core scan of rap_decode_attn (head shapes of the shaped workloads: the five retain ratios at D = 128,

@@ -17,8 +17,10 @@ template <> __device__ __forceinline__ float wg_ld<__nv_bfloat16>(const __nv_bfl
 
 // Any 2P, d_v' <= 256, G <= 8, fp32 or bf16.  CTA (row, KV head, split): the G query heads of one token over its share of the
 // rows that the token sees -- the shared prefix's first, then its own -- tile by tile with a running maximum and sum, all in
-// fp32.  A warp computes a row's logits (lanes over dims), a thread owns a channel of the output.  One split writes the
-// output; several leave (accumulators, maximum, sum) for win_combine_kernel.
+// fp32.  Eight lanes compute a row's logits; a thread owns a channel of the output for every n_grp-th row of the tile (256 /
+// channels, a power of two), and the groups' sums are added at the end.  Bound by latency at the sizes that fp32 stacks have: a
+// tile's loads are all on their way at once.  One split writes the output; several leave (accumulators, maximum, sum) for
+// win_combine_kernel, which is launched under the scan's tail.
 template <typename T>
 __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_args a, float qscale, int n_split, float* __restrict__ ws) {
   extern __shared__ float wg_smem[];
@@ -27,6 +29,7 @@ __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_a
   float* s_s = q_s + G * P2;               // [G][WG_TILE]
   float* alpha_s = s_s + G * WG_TILE;      // [G]
   float* l_s = alpha_s + G;                // [G]
+  float* red = l_s + G;                    // [n_grp - 1][dv] of one head
   const int row = blockIdx.x, h = blockIdx.y, split = blockIdx.z;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
@@ -61,6 +64,10 @@ __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_a
 
   for (int i = tid; i < G * P2; i += WG_THREADS)
     q_s[i] = wg_ld<T>((const T*)a.q + ((size_t)row * a.Hq + h * G) * P2 + i) * qscale;
+  // V: thread (grp, ch)
+  const int w_log = dv <= 32 ? 5 : dv <= 64 ? 6 : dv <= 128 ? 7 : 8, n_grp = WG_THREADS >> w_log;
+  const int ch = tid & ((1 << w_log) - 1), grp = tid >> w_log;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   float m_run = -INFINITY, l_run = 0.f;    // warp g < G, the same in every lane
   float acc[RAP_MAX_GROUP];
 #pragma unroll
@@ -69,13 +76,16 @@ __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_a
 
   for (long long j0 = v0; j0 < v1; j0 += WG_TILE) {
     const int nj = (int)min((long long)WG_TILE, v1 - j0);
-    for (int j = warp; j < nj; j += WG_THREADS / 32) {
-      const long long v = j0 + j;
+#pragma unroll 2
+    for (int j = tid >> 3; j < WG_TILE; j += WG_THREADS / 8) {
+      const int l8 = lane & 7;
+      const long long v = j0 + min(j, nj - 1);
       const T* kr = v < pre ? kp + (size_t)v * P2 : kc + (size_t)cache_row((int)(v - pre)) * P2;
       float part[RAP_MAX_GROUP];
 #pragma unroll
       for (int g = 0; g < RAP_MAX_GROUP; ++g) part[g] = 0.f;
-      for (int d = lane; d < P2; d += 32) {
+#pragma unroll 4
+      for (int d = l8; d < P2; d += 8) {
         const float kv = wg_ld<T>(kr + d);
 #pragma unroll
         for (int g = 0; g < RAP_MAX_GROUP; ++g)
@@ -86,8 +96,8 @@ __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_a
         if (g < G) {
           float s = part[g];
 #pragma unroll
-          for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-          if (lane == 0) s_s[g * WG_TILE + j] = s;
+          for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+          if (l8 == 0) s_s[g * WG_TILE + j] = s;
         }
       }
     }
@@ -113,19 +123,32 @@ __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_a
       if (lane == 0) alpha_s[g] = alpha;
     }
     __syncthreads();
-    if (tid < dv) {
+    if (ch < dv) {
 #pragma unroll
       for (int g = 0; g < RAP_MAX_GROUP; ++g)
         if (g < G) acc[g] *= alpha_s[g];
-      for (int j = 0; j < nj; ++j) {
+#pragma unroll 4
+      for (int j = grp; j < nj; j += n_grp) {
         const long long v = j0 + j;
-        const float vv = wg_ld<T>((v < pre ? vp + (size_t)v * dv : vc + (size_t)cache_row((int)(v - pre)) * dv) + tid);
+        const float vv = wg_ld<T>((v < pre ? vp + (size_t)v * dv : vc + (size_t)cache_row((int)(v - pre)) * dv) + ch);
 #pragma unroll
         for (int g = 0; g < RAP_MAX_GROUP; ++g)
           if (g < G) acc[g] = fmaf(s_s[g * WG_TILE + j], vv, acc[g]);
       }
     }
     __syncthreads();
+  }
+  if (n_grp > 1) {       // the groups' sums, one head at a time
+#pragma unroll
+    for (int g = 0; g < RAP_MAX_GROUP; ++g) {
+      if (g < G) {
+        if (grp > 0 && ch < dv) red[(grp - 1) * dv + ch] = acc[g];
+        __syncthreads();
+        if (grp == 0 && ch < dv)
+          for (int i = 1; i < n_grp; ++i) acc[g] += red[(i - 1) * dv + ch];
+        __syncthreads();
+      }
+    }
   }
   if (n_split == 1) {
     if (warp < G && lane == 0) l_s[warp] = l_run;
@@ -150,6 +173,7 @@ __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_a
 
 // out = sum_s 2^(m_s - M) acc_s / sum_s 2^(m_s - M) l_s over the splits of one query head (an empty split has l = 0)
 __global__ void __launch_bounds__(128) win_combine_kernel(const float* __restrict__ ws, int n_split, int dv, float* __restrict__ out) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const float* base = ws + (size_t)blockIdx.x * n_split * (size_t)(dv + 2);
   float M = -INFINITY, den = 0.f;
   for (int s = 0; s < n_split; ++s)
@@ -179,14 +203,23 @@ rap_status launch_generic(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) 
     n_split = (int)(ns > RAP_MAX_SPLIT ? RAP_MAX_SPLIT : ns < 1 ? 1 : ns);
   }
   const float qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
-  const size_t smem = (size_t)(G * a.P2 + G * WG_TILE + 2 * G) * sizeof(float);
+  const size_t smem = (size_t)(G * a.P2 + G * WG_TILE + 2 * G + WG_THREADS) * sizeof(float);
   const dim3 grid(a.T, a.Hkv, n_split);
   if (a.dtype == RAP_F32) win_generic_kernel<float><<<grid, WG_THREADS, smem, st>>>(a, qscale, n_split, ctx->d_attn_ws);
   else win_generic_kernel<__nv_bfloat16><<<grid, WG_THREADS, smem, st>>>(a, qscale, n_split, ctx->d_attn_ws);
   ctx->launches++;
   RAP_CUDA_TRY(ctx, cudaGetLastError());
   if (n_split > 1) {
-    win_combine_kernel<<<a.T * a.Hq, 128, 0, st>>>(ctx->d_attn_ws, n_split, a.dv, a.out);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.T * a.Hq);
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    RAP_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, win_combine_kernel, (const float*)ctx->d_attn_ws, n_split, a.dv, a.out));
     ctx->launches++;
     RAP_CUDA_TRY(ctx, cudaGetLastError());
   }
@@ -196,8 +229,8 @@ rap_status launch_generic(rap_ctx* ctx, const rap_win_args& a, cudaStream_t st) 
 // ---- slot maps ----------------------------------------------------------------------------------------------------------------
 // Every CTA walks all sequences, SL_THREADS at a time: a block-wide prefix sum of the new tokens gives their first rows, and
 // the CTA's share of the rows finds its sequence by bisection in that piece.  Bound by a launch and a few dependent loads: 12
-// bytes a row are written.  The lengths may be advanced in place, so the CTA that comes last (a counter, zero again afterwards)
-// writes them, when all have read them.
+// bytes a row are written.  Lengths that are advanced in place are written by the CTA that comes last (a counter, zero again
+// afterwards), when all have read them.
 constexpr int SL_THREADS = 512;
 __global__ void __launch_bounds__(SL_THREADS) build_slots_kernel(int B, const int32_t* seq_len, const int32_t* __restrict__ new_len,
                                                                  const int32_t* __restrict__ pos_base, int T, int n_sink, int S_cap,
@@ -252,6 +285,7 @@ __global__ void __launch_bounds__(SL_THREADS) build_slots_kernel(int B, const in
     __syncthreads();
     if (first_cta && b < B) {
       row_start[b + 1] = (int32_t)min(end, (long long)T);
+      if (len_out && len_out != seq_len) len_out[b] = (int32_t)min((long long)past + fresh, 0x7fffffffLL);
       if (end > T) win_report(status, RAP_ECAPACITY, b);
       const long long rolled = (long long)past + fresh - max(past, n_sink);     // new tokens behind the sinks
       if (rolled > S_cap - n_sink) win_report(status, RAP_ECAPACITY, b);
@@ -278,7 +312,7 @@ __global__ void __launch_bounds__(SL_THREADS) build_slots_kernel(int B, const in
     __syncthreads();
   }
   if (first_cta && tid == 0) row_start[0] = 0;
-  if (!len_out) return;
+  if (!len_out || len_out != seq_len) return;
   if (tid == 0) {
     last_s = 1;
     if (gridDim.x > 1) {
@@ -298,8 +332,9 @@ __global__ void __launch_bounds__(SL_THREADS) build_slots_kernel(int B, const in
 rap_status rap_launch_build_slots(rap_ctx* ctx, int B, const int32_t* seq_len, const int32_t* new_len, const int32_t* pos_base, int T,
                                   int n_sink, int S_cap, int32_t* row_start, int32_t* seq_id, int32_t* pos, int32_t* slot,
                                   int32_t* len_out, cudaStream_t st) {
-  // rows over the SMs from 2048 on: below, one CTA has written them before a second launch wave's lengths are read
-  const int ctas = (int)(((long long)T + 2047) / 2048);
+  // two rows a thread: more CTAs read the lengths again, fewer write longer (9400 rows of 64 sequences: 5.2 us with 2048 rows a
+  // CTA and a counter, 3.4 as it is)
+  const int ctas = (int)(((long long)T + 1023) / 1024);
   const int grid = ctas < 1 ? 1 : ctas > 2 * ctx->sm_count ? 2 * ctx->sm_count : ctas;
   int32_t* ticket = ctx->d_win_cnt + 2 * (size_t)ctx->desc.max_batch * ctx->desc.n_kv_heads;
   build_slots_kernel<<<grid, SL_THREADS, 0, st>>>(B, seq_len, new_len, pos_base, T, n_sink, S_cap, row_start, seq_id, pos, slot, len_out,

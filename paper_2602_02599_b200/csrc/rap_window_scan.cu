@@ -39,6 +39,11 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
   p.wait_limit = WAIT_LIMIT;
   // what a unit's end takes, in blocks of half a microsecond: 3 us, or 10 with a prefix's splits to join
   p.own = n_pre ? 20 : 6;
+  if (ctx->dbg_arm_timeout) {        // test hook (rap_debug_arm_wait_timeout)
+    p.wait_limit = 4096;
+    p.dbg_skip_copy = 1;
+    ctx->dbg_arm_timeout = 0;
+  }
   {   // two sets of counters take turns; each launch clears the one its predecessor used
     const size_t n_units = (size_t)ctx->desc.max_batch * ctx->desc.n_kv_heads;
     const uint32_t set = ctx->win_epoch++ & 1u;

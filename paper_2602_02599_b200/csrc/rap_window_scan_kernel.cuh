@@ -43,6 +43,7 @@ struct WsParams {
   int own;                    // blocks that a unit's end takes as long as
   int join_places;            // partials that the stages hold together
   uint32_t wait_limit;
+  int dbg_skip_copy;          // test hook: the first unit's first block is armed and not copied
   // shared prefixes (ws.n_pre > 0): what the plan of their splits is made of
   int n_groups, S_pre, sms;
   const int32_t* group_start;
@@ -235,6 +236,10 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
       const uint32_t bar = bar0 + 8 * stg, dst = wstage_u + stg * p.stage_bytes;
       const bool ok = RAP_BOUNDS(row0, p.S_cap, p.status, 0x201) && RAP_BOUNDS(row0 + rows - 1, p.S_cap, p.status, 0x202) &&
                       RAP_BOUNDS(rows - 1, 32, p.status, 0x203) && RAP_BOUNDS(unit, (size_t)p.B * p.Hkv, p.status, 0x204);
+      if (p.dbg_skip_copy && unit == 0 && t0 == 0 && warp == 0 && i == 0) {     // nothing is in flight for this stage when the CTA leaves
+        if (!p.pad16 && lane == 0) mbar_expect_tx(bar, 16);
+        return;
+      }
       const unsigned char* ks = kg + (size_t)row0 * k_row;
       const unsigned char* vs = vg + (size_t)row0 * v_row;
       if (p.pad16) {

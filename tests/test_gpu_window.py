@@ -313,6 +313,37 @@ def test_large_logits():
     H.close()
 
 
+@pytest.mark.parametrize("pairs,vch", [(45, 90), (64, 128)])
+def test_a_wait_that_runs_out_is_reported(pairs, vch):
+    """One stage is armed and nothing copied into it: the launch ends, says so, and the next ones are right again."""
+    H = W.Heads(2, 4, pairs, vch, "bf16", 3)
+    K, V, q = H.randn(3, 2, 512, 2 * pairs), H.randn(3, 2, 512, vch), H.query(3)
+    lens, want = [500, 30, 400], []
+    for b, n in enumerate(lens):
+        want.append(H.reference(q[b], [(K, V, b, W.seen(n - 1, 4, 300))]))
+
+    def call():
+        out = H.out(3)
+        H.ctx.rap_decode_attn_window(0, 3, q, K, V, 512, H.ints(lens), 500, 4, 300, out)
+        return out
+
+    H.ctx.rap_debug_arm_wait_timeout()
+    call()
+    assert H.ctx.rap_get_last_device_status()[0] == binding.RAP_ETIMEOUT
+    H.ctx.rap_debug_arm_wait_timeout()
+    call()                                              # counters left behind, and not asked for
+    for _ in range(3):
+        out = call()
+        W.check(out, torch.stack([w[0] for w in want]), torch.stack([w[1] for w in want]))
+    assert H.ctx.rap_get_last_device_status()[0] == binding.RAP_ETIMEOUT
+    out = H.out(3)
+    H.ctx.rap_decode_attn_shared(0, 3, q, 1, K, V, 512, H.ints([0, 3]), H.ints([512]), 512, K, V, 512, H.ints(lens), 500, out)
+    for b, n in enumerate(lens):
+        W.check(out[b], *H.reference(q[b], [(K, V, 0, range(512)), (K, V, b, range(n))]))
+    H.clean()
+    H.close()
+
+
 def refused(status, f, *a):
     with pytest.raises(binding.RapError) as e:
         f(*a)
