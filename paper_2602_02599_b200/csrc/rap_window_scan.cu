@@ -6,20 +6,23 @@ namespace {
 template <bool FOUR, bool VODD>
 const void* scan_fn(int n, int nw) {
   switch (n * 8 + nw) {
-    case 1 * 8 + 4: return (const void*)win_scan_kernel<1, FOUR, VODD, 4>;
-    case 2 * 8 + 4: return (const void*)win_scan_kernel<2, FOUR, VODD, 4>;
-    case 3 * 8 + 4: return (const void*)win_scan_kernel<3, FOUR, VODD, 4>;
-    case 4 * 8 + 4: return (const void*)win_scan_kernel<4, FOUR, VODD, 4>;
-    case 5 * 8 + 4: return (const void*)win_scan_kernel<5, FOUR, VODD, 4>;
-    case 6 * 8 + 4: return (const void*)win_scan_kernel<6, FOUR, VODD, 4>;
-    case 6 * 8 + 3: return (const void*)win_scan_kernel<6, FOUR, VODD, 3>;
-    case 7 * 8 + 4: return (const void*)win_scan_kernel<7, FOUR, VODD, 4>;
-    case 7 * 8 + 3: return (const void*)win_scan_kernel<7, FOUR, VODD, 3>;
-    case 8 * 8 + 2: return (const void*)win_scan_kernel<8, FOUR, VODD, 2>;      // unpruned heads, seven or eight to a KV head
-    case 8 * 8 + 3: return (const void*)win_scan_kernel<8, FOUR, VODD, 3>;
+    case 1 * 8 + 4: return (const void*)win_scan_kernel<1, FOUR, VODD, 4, false>;
+    case 2 * 8 + 4: return (const void*)win_scan_kernel<2, FOUR, VODD, 4, false>;
+    case 3 * 8 + 4: return (const void*)win_scan_kernel<3, FOUR, VODD, 4, false>;
+    case 4 * 8 + 4: return (const void*)win_scan_kernel<4, FOUR, VODD, 4, false>;
+    case 5 * 8 + 4: return (const void*)win_scan_kernel<5, FOUR, VODD, 4, false>;
+    case 6 * 8 + 4: return (const void*)win_scan_kernel<6, FOUR, VODD, 4, false>;
+    case 6 * 8 + 3: return (const void*)win_scan_kernel<6, FOUR, VODD, 3, false>;
+    case 7 * 8 + 4: return (const void*)win_scan_kernel<7, FOUR, VODD, 4, false>;
+    case 7 * 8 + 3: return (const void*)win_scan_kernel<7, FOUR, VODD, 3, false>;
+    case 8 * 8 + 2: return (const void*)win_scan_kernel<8, FOUR, VODD, 2, false>;      // unpruned heads, seven or eight to a KV head
+    case 8 * 8 + 3: return (const void*)win_scan_kernel<8, FOUR, VODD, 3, false>;
   }
   return nullptr;
 }
+
+template <bool FOUR>
+const void* scan_tma_fn(int n) { return n == 4 ? (const void*)win_scan_kernel<4, FOUR, false, 4, true> : (const void*)win_scan_kernel<8, FOUR, false, 3, true>; }
 
 }  // namespace
 
@@ -54,7 +57,9 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
   }
   const int k_row = 2 * a.P2, v_row = 2 * a.dv;
   const bool vodd = (a.dv & 1) != 0;
-  p.pad16 = (k_row % 16 == 0 && v_row % 16 == 0) ? 1 : 0;
+  const long long cache_rows = (long long)a.B * a.Hkv * a.S_cap;
+  const bool tma = k_row == v_row && (k_row == 128 || k_row == 256) && cache_rows < (1LL << 31);       // rows are the maps' y
+  p.pad16 = (!tma && k_row % 16 == 0 && v_row % 16 == 0) ? 1 : 0;
   if (p.pad16) {
     // 16 bytes more where a row is an even number of 16-byte units: then eight rows start on different banks
     p.k_stride = k_row + (k_row % 32 == 0 ? 16 : 0);
@@ -65,24 +70,32 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
     p.v_stride = v_row;
     // the eight rows of a fragment 4, 2 or 1 apart: P words a row times the step = 4 * odd puts them on different banks; odd
     // d_v' wants the two rows of a register to be of one parity
-    p.rs_log = (p.P & 1) ? 2 : (p.P & 2) ? 1 : vodd ? 1 : 0;
+    p.rs_log = (p.P & 1) ? 2 : (p.P & 2) ? 1 : vodd ? 1 : 0;      // (tensor maps: rows 0-7 of a fragment in order)
   }
-  p.stage_bytes = (32 * (p.k_stride + p.v_stride) + 16 + 127) / 128 * 128;
+  p.stage_bytes = tma ? 32 * (p.k_stride + p.v_stride) : (32 * (p.k_stride + p.v_stride) + 16 + 127) / 128 * 128;
   const int cw = (vodd ? a.dv + 1 : a.dv);
   // two CTAs an SM; four warps with two stages each where they fit (up to 13 KB a stage), else three
   const int nk = (p.P + 7) / 8, nv = (a.dv + 15) / 16, n = nk > nv ? nk : nv;
   int nw = n == 8 ? 3 : 4, smem = 0;
   for (;; --nw) {
     const int red = nw * p.G * cw * 4, join = p.G * RAP_MAX_SPLIT * 4;
-    p.off_stage = (512 + (red > join ? red : join) + 127) / 128 * 128;
-    smem = p.off_stage + nw * WS_STAGES * p.stage_bytes;
+    const int unit = tma ? 1024 : 128;
+    p.off_stage = (512 + (red > join ? red : join) + unit - 1) / unit * unit;
+    smem = p.off_stage + nw * WS_STAGES * p.stage_bytes + (tma ? 1024 : 0);
     p.join_places = nw * WS_STAGES * p.stage_bytes / (4 * p.G * p.ws.dv4);      // partials that fit the stages
     if (smem <= SMEM_BUDGET || nw == 2) break;
   }
   const void* fn = p.G <= 4 ? (vodd ? scan_fn<true, true>(n, nw) : scan_fn<true, false>(n, nw)) : (vodd ? scan_fn<false, true>(n, nw) : scan_fn<false, false>(n, nw));
+  alignas(64) unsigned char map_k[128] = {0}, map_v[128] = {0};      // CUtensorMap images (the other forms ignore them)
+  if (tma) {
+    fn = p.G <= 4 ? scan_tma_fn<true>(n) : scan_tma_fn<false>(n);
+    if (!rap_tensor_map_bf16(ctx, map_k, a.k, (uint64_t)cache_rows, (uint64_t)a.P2, 32) ||
+        !rap_tensor_map_bf16(ctx, map_v, a.v, (uint64_t)cache_rows, (uint64_t)a.dv, 32))
+      return RAP_EUNSUPPORTED;
+  }
   if (!fn || smem > SMEM_BUDGET) return RAP_EUNSUPPORTED;
   RAP_CUDA_TRY(ctx, rap_raise_smem(ctx, fn, SMEM_BUDGET));
-  void* args[] = {&p};
+  void* args[] = {&p, map_k, map_v};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * ctx->sm_count);
   cfg.blockDim = dim3(32 * nw);

@@ -6,8 +6,9 @@
 // each run is cut into blocks of 32 rows from a multiple of 8 on (8 rows start on a 16-byte boundary for every width), and
 // all units' blocks form one sequence that the CTAs share evenly, whatever units they belong to.  Inside a CTA every warp is
 // its own pipeline over every NW-th block: a ring of stages that it fills itself, no barrier until the unit ends.
-//   * Rows of a multiple of 16 bytes are copied 16 bytes a lane into rows padded so that fragment loads meet 32 banks; all
-//     others as contiguous bulk copies, with the eight rows of a fragment spread so that they do.
+//   * Rows of a multiple of 128 bytes come through tensor maps with the 128-byte swizzle, rows of another multiple of 16 are
+//     copied 16 bytes a lane into rows padded so that fragment loads meet 32 banks; all others are contiguous bulk copies,
+//     with the eight rows of a fragment spread so that they do.
 //   * S^T = q K^T and O += P V are mma.sync m16n8k16 (M would be G <= 8 query heads: far below a tcgen05 tile, and no
 //     descriptor describes rows of 180 bytes).  The 16 rows of A carry the softmax weights as three bf16 numbers, their
 //     rounding and two remainders (24 bits together), instead of padding: up to four heads rows 0-3, 4-7 and 8-11 in ONE
@@ -17,6 +18,8 @@
 //   * A unit that several CTAs share leaves one partial (sums, maximum, weight) each; who delivers the last one joins them in
 //     order, so a result does not depend on who that is.  The prefix of rap_decode_attn_shared comes as partials too.
 #pragma once
+#include <cuda.h>
+
 #include "rap_attn_common.cuh"
 #include "rap_window_common.cuh"
 
@@ -55,6 +58,13 @@ __device__ __forceinline__ void ws_mma(float (&c)[4], uint32_t a0, uint32_t a1, 
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// one box of a 2-D tensor map (x = element column, y = row) into this CTA's shared memory; no multicast
+__device__ __forceinline__ void ws_tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
 }
 __device__ __forceinline__ float ws_ex2(float x) {
   float y;
@@ -105,9 +115,14 @@ __device__ __forceinline__ int ws_scan_add(int x, int lane) {      // inclusive 
 // NW: warps.  A short launch executes most of this once a CTA, so what it costs is fetching it: divisions by run-time numbers
 // and 64-bit ones are kept out of the usual path.
 constexpr int WS_STAGES = 2;
-template <int N, bool FOUR, bool VODD, int NW>
-__global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) {
-  extern __shared__ __align__(128) unsigned char smem[];
+// TMA: rows of exactly 32 N bytes (K and V) through tensor maps, N = 4 or 8: panels of 32 rows x 128 bytes, the 16-byte chunk c
+// of row r at chunk c ^ (r % 8)
+template <int N, bool FOUR, bool VODD, int NW, bool TMA>
+__global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, const __grid_constant__ CUtensorMap map_k,
+                                                              const __grid_constant__ CUtensorMap map_v) {
+  static_assert(!TMA || N % 4 == 0, "whole panels");
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  unsigned char* smem = TMA ? smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u) : smem_raw;     // panels start on 1024 bytes
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem);                         // [NW][stages], at most 64 bytes; then the join's
   const uint32_t bar_join = smem_u32(smem) + 64;
   float* m_s = reinterpret_cast<float*>(smem + 128);                          // [4][8]
@@ -140,6 +155,14 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
   int nc = min((int)gridDim.x, (T + 3) >> 2);
   // ... (a unit of n_max blocks falls to at most n_max nc / T + 2 CTAs)
   if (n_max > T / (int)gridDim.x * places) nc = (int)max(1LL, min((long long)nc, (long long)places * T / n_max));
+  // Units of about the same size (within a fifth of the largest): the same number of CTAs for each, so that no CTA ends two of
+  // them, if that leaves at most a quarter of the CTA slots empty -- HBM is as busy with those missing (32 sequences of 4096
+  // rows 65.9 -> 61.8 us; not with padded rows, which keep the SMs busier: 66 -> 71 us there).  Four blocks a CTA, as above.
+  const int units = p.B * p.Hkv, most_parts = min(places, max(1, (n_max - p.own) >> 2));
+  int parts = (int)gridDim.x / units;
+  const bool even = parts >= 1 && !p.pad16 && (long long)n_max * units <= (long long)T + T / 5 && (parts > most_parts || units * parts * 4 >= (int)gridDim.x * 3);
+  parts = min(parts, most_parts);
+  if (even) nc = units * parts;
   if (blockIdx.x == 0)
     for (int i = tid; i < p.other_units; i += THREADS) p.unit_cnt_other[i] = 0;      // what a launch that gave up left behind
   if ((int)blockIdx.x >= nc) {
@@ -150,23 +173,35 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
   const int share = T / nc, extra = T - share * nc, mark = extra * (share + 1);
   auto cta_of = [&](int tile) { return tile < mark ? tile / (share + 1) : extra + (tile - mark) / share; };   // whose share holds this block
   int cur = (int)blockIdx.x * share + min((int)blockIdx.x, extra);
-  const int hi = cur + share + ((int)blockIdx.x < extra ? 1 : 0);
+  int hi = cur + share + ((int)blockIdx.x < extra ? 1 : 0);
   int b = 0, h, unit_start = 0;
-  for (int b0 = 0, carry = 0;; b0 += 32) {
-    const int n = (b0 == 0 ? n_first : b0 + lane < p.B ? ws_unit(p, b0 + lane).n + p.own : 0) * p.Hkv;
-    const int x = ws_scan_add(n, lane) + carry;
-    const unsigned past = __ballot_sync(0xffffffffu, x > cur);
-    if (past) {
-      const int l = __ffs(past) - 1;
-      b = b0 + l;
-      unit_start = __shfl_sync(0xffffffffu, x - n, l);
-      break;
+  const int my_unit = even ? (int)blockIdx.x / parts : 0;
+  if (even) {
+    b = my_unit / p.Hkv;
+  } else {
+    for (int b0 = 0, carry = 0;; b0 += 32) {
+      const int n = (b0 == 0 ? n_first : b0 + lane < p.B ? ws_unit(p, b0 + lane).n + p.own : 0) * p.Hkv;
+      const int x = ws_scan_add(n, lane) + carry;
+      const unsigned past = __ballot_sync(0xffffffffu, x > cur);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        b = b0 + l;
+        unit_start = __shfl_sync(0xffffffffu, x - n, l);
+        break;
+      }
+      carry = __shfl_sync(0xffffffffu, x, 31);
     }
-    carry = __shfl_sync(0xffffffffu, x, 31);
   }
   WsUnit u = ws_unit(p, b);
-  h = (cur - unit_start) / (u.n + p.own);
-  unit_start += h * (u.n + p.own);
+  if (even) {
+    const int part = (int)blockIdx.x - my_unit * parts;
+    h = my_unit - b * p.Hkv;
+    cur = p.own + (int)((long long)u.n * part / parts);
+    hi = p.own + (int)((long long)u.n * (part + 1) / parts);
+  } else {
+    h = (cur - unit_start) / (u.n + p.own);
+    unit_start += h * (u.n + p.own);
+  }
 
   int pre_per = 1;
   if (p.ws.n_pre)
@@ -184,6 +219,13 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
     koff[t] = ((frag_row(t, gid) * p.k_stride) >> 2) + tq;
     vofs[t] = v_base + ((frag_row(t, 2 * tq) * p.v_stride) >> 2) + gid;     // odd dv: rounded down for odd rows
   }
+  int kx[8], vx[4][2];           // TMA: word of the lane in its row's chunk c; words of rows 2 tq + e in chunks of 16 channels
+#pragma unroll
+  for (int c = 0; c < 8; ++c) kx[c] = gid * 32 + ((c ^ gid) << 2) + tq;
+#pragma unroll
+  for (int cm = 0; cm < 4; ++cm)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) vx[cm][e] = v_base + (2 * tq + e) * 32 + (((2 * cm + (gid >> 2)) ^ (2 * tq + e)) << 2) + (gid & 3);
   const int k_last = P - 8;                                   // the last steps are shifted back into the row
   const int c_last = VODD ? dv - 15 : dv - 16;                // so are the last blocks of channels (odd dv: one phantom channel)
   const int CW = c_last + 16;
@@ -237,12 +279,24 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
       const bool ok = RAP_BOUNDS(row0, p.S_cap, p.status, 0x201) && RAP_BOUNDS(row0 + rows - 1, p.S_cap, p.status, 0x202) &&
                       RAP_BOUNDS(rows - 1, 32, p.status, 0x203) && RAP_BOUNDS(unit, (size_t)p.B * p.Hkv, p.status, 0x204);
       if (p.dbg_skip_copy && unit == 0 && t0 == 0 && warp == 0 && i == 0) {     // nothing is in flight for this stage when the CTA leaves
-        if (!p.pad16 && lane == 0) mbar_expect_tx(bar, 16);
+        if ((TMA || !p.pad16) && lane == 0) mbar_expect_tx(bar, 16);
         return;
       }
       const unsigned char* ks = kg + (size_t)row0 * k_row;
       const unsigned char* vs = vg + (size_t)row0 * v_row;
-      if (p.pad16) {
+      if constexpr (TMA) {
+        if (lane == 0) {         // whole boxes: rows of a neighbouring unit are masked, rows behind the tensor's end come as zeros
+          if (used) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_expect_tx(bar, ok ? (uint32_t)(N * 1024 * 2) : 0u);
+          const int y = (int)unit * p.S_cap + row0;
+          if (ok) {
+#pragma unroll
+            for (int pn = 0; pn < N / 4; ++pn) ws_tma_2d(dst + pn * 4096, &map_k, 64 * pn, y, bar);
+#pragma unroll
+            for (int pn = 0; pn < N / 4; ++pn) ws_tma_2d(dst + N * 1024 + pn * 4096, &map_v, 64 * pn, y, bar);
+          }
+        }
+      } else if (p.pad16) {
         const int c = lane & 15, kc = k_row >> 4, vc = v_row >> 4;
         for (int r = lane >> 4; r < rows && ok; r += 2) {
           if (c < kc)
@@ -301,7 +355,12 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
         // rows that are not seen: their V is zero, so that the second product meets 0 * 0 there
         unsigned char* vz = wstage + (size_t)st * p.stage_bytes + 32 * p.k_stride;
         const int z0 = lo * p.v_stride, z1 = hi_row * p.v_stride, z2 = 32 * p.v_stride;     // bytes [0, z0) and [z1, z2)
-        if constexpr (VODD) {
+        if constexpr (TMA) {     // a row is 128 bytes of every panel, whatever the swizzle
+          for (int pn = 0; pn < N / 4; ++pn) {
+            for (int i = 4 * lane; i < 128 * lo; i += 128) *reinterpret_cast<uint32_t*>(vz + pn * 4096 + i) = 0u;
+            for (int i = 128 * hi_row + 4 * lane; i < 4096; i += 128) *reinterpret_cast<uint32_t*>(vz + pn * 4096 + i) = 0u;
+          }
+        } else if constexpr (VODD) {
           for (int i = 2 * lane; i < z0; i += 64) *reinterpret_cast<uint16_t*>(vz + i) = 0;
           for (int i = z1 + 2 * lane; i < z2; i += 64) *reinterpret_cast<uint16_t*>(vz + i) = 0;
         } else {
@@ -321,7 +380,14 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
         const int wb = min(8 * ks, k_last);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const uint32_t b0 = w[koff[t] + wb], b1 = w[koff[t] + wb + 4];
+          uint32_t b0, b1;
+          if constexpr (TMA) {
+            b0 = w[kx[(2 * ks) % 8] + (ks / 4) * 1024 + 256 * t];
+            b1 = w[kx[(2 * ks + 1) % 8] + (ks / 4) * 1024 + 256 * t];
+          } else {
+            b0 = w[koff[t] + wb];
+            b1 = w[koff[t] + wb + 4];
+          }
           ws_mma(s[t], qa[ks][0], 0u, qa[ks][1], 0u, b0, b1);
         }
       }
@@ -385,7 +451,18 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
 #pragma unroll
         for (int cb = 0; cb < N; ++cb) {
           const int cw = min(16 * cb, c_last) >> 1;
-          const uint32_t xa0 = v0[cw], xb0 = v0[cw + vpair], xa1 = v1[cw], xb1 = v1[cw + vpair];
+          uint32_t xa0, xb0, xa1, xb1;
+          if constexpr (TMA) {
+            xa0 = w[vx[cb % 4][0] + (cb / 4) * 1024 + 512 * kb];
+            xb0 = w[vx[cb % 4][1] + (cb / 4) * 1024 + 512 * kb];
+            xa1 = w[vx[cb % 4][0] + (cb / 4) * 1024 + 512 * kb + 256];
+            xb1 = w[vx[cb % 4][1] + (cb / 4) * 1024 + 512 * kb + 256];
+          } else {
+            xa0 = v0[cw];
+            xb0 = v0[cw + vpair];
+            xa1 = v1[cw];
+            xb1 = v1[cw + vpair];
+          }
           const uint32_t be0 = ws_prmt(xa0, xb0, 0x5410u), bo0 = ws_prmt(xa0, xb0, 0x7632u);
           uint32_t be1, bo1;
           if constexpr (!VODD) {
@@ -452,9 +529,17 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p) 
         }
     }
     __syncthreads();
-    const int first = cta_of(unit_start + p.own), n_seg = cta_of(unit_start + p.own + u.n - 1) - first + 1;
+    int my_seg, n_seg;             // this CTA's place among those that hold blocks of the unit, and how many they are
+    if (even) {
+      my_seg = u.n < parts ? t0 : (int)blockIdx.x - my_unit * parts;      // fewer blocks than CTAs: one each, the others none
+      n_seg = min(u.n, parts);
+    } else {
+      const int first = cta_of(unit_start + p.own);
+      my_seg = (int)blockIdx.x - first;
+      n_seg = cta_of(unit_start + p.own + u.n - 1) - first + 1;
+    }
     const bool alone = n_seg == 1 && n_pre == 0;
-    const int dv4 = p.ws.dv4, my_seg = (int)blockIdx.x - first;
+    const int dv4 = p.ws.dv4;
     const long long head0 = (long long)b * p.Hq + (long long)h * G;            // the unit's first query head
     const bool ws_ok = RAP_BOUNDS(my_seg, p.ws.slots, p.status, 0x206) &&
                        RAP_BOUNDS(reinterpret_cast<float*>(p.ws.own_pair(unit, my_seg) + G) - 1 - p.ws.pre, p.ws_floats, p.status, 0x207);
