@@ -184,6 +184,16 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   const int t_base = q0 / G, t_rest = q0 - t_base * G, g_recip = (65536 + G - 1) / G;
   auto row_t = [&](int r) { return t_base + (((t_rest + r) * g_recip) >> 16); };
 
+  const int kw = p.P2 >> 1;                          // 4-byte words per q / K row
+  // (while the unit's numbers are on their way) K's pad dims are zero (Q's too, below; V's pad channels only reach accumulator
+  // columns that nothing reads); LSUM: channel dv of all rows of every V buffer is one (odd dv: the producers write it with the
+  // row's last word)
+  for (int i = tid; i < WT_STAGES * WT_KT; i += WT_THREADS) {
+    const int at = (i >> 6) * WT_KV_BYTES + (i & 63) * 128;
+    for (int w = kw; w < 8 * DK; ++w) *reinterpret_cast<uint32_t*>(k_s + at + pt_swz2(4 * w, i & 7)) = 0u;
+    if constexpr (LSUM) *reinterpret_cast<uint32_t*>(v_s + at + pt_swz2(4 * (p.dv >> 1), i & 7)) = p.dv & 1 ? 0x3f800000u : 0x3f80u;
+  }
+
   // ---- the key tiles: n_st of sinks, then 64 rows each from position `base` on; nt[X] of them for query tile X ----
   const int len = PREFIX ? min(max(p.len[unit], 0), p.S_cap) : max(p.len[unit], 0);
   const int pos0 = len - n_tok;                                // position of the block's first token
@@ -246,19 +256,6 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pt_smem(tmem_slot)), "r"(512)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  const int kw = p.P2 >> 1;                          // 4-byte words per q / K row
-  // K's pad dims are zero (Q's too, below; V's pad channels only reach accumulator columns that nothing reads)
-  for (int i = tid; i < WT_STAGES * WT_KT * (8 * DK - kw); i += WT_THREADS) {
-    const int br = i / (8 * DK - kw), w = kw + i - br * (8 * DK - kw);
-    *reinterpret_cast<uint32_t*>(k_s + (br >> 6) * WT_KV_BYTES + (br & 63) * 128 + pt_swz2(4 * w, br & 7)) = 0u;
-  }
-  if constexpr (LSUM) {
-    // the ones: channel dv of all 64 rows of every V buffer (odd dv: the producers write it with the row's last word)
-    for (int i = tid; i < WT_STAGES * WT_KT; i += WT_THREADS) {
-      const int buf = i / WT_KT, r = i - buf * WT_KT;
-      *reinterpret_cast<uint32_t*>(v_s + buf * WT_KV_BYTES + r * 128 + pt_swz2(4 * (p.dv >> 1), r & 7)) = p.dv & 1 ? 0x3f800000u : 0x3f80u;
-    }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
