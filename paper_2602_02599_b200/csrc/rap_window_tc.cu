@@ -306,28 +306,32 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     const int R = p.S_cap - p.n_sink;
     // the key of tile row i; V: keys k and k + 8 of sixteen lie side by side
     auto key_of = [&](int i) { return is_v ? (i & 48) + ((i & 15) >> 1) + 8 * (i & 1) : i; };
-    // the rows of a tile are one run from row s0 on unless the tile crosses the seam of a rolling cache
+    // the rows of a tile are one run from row s0 on, or two if it crosses the seam of a rolling cache (false: more, the cache is
+    // shorter than the tile)
     auto run_of = [&](int j0, int n, int& s0) {
       s0 = j0;
       if (PREFIX || j0 + n <= p.S_cap) return true;
       s0 = j0 >= p.n_sink ? p.n_sink + (j0 - p.n_sink) % R : j0;
-      return s0 + n <= p.S_cap;
+      return s0 + n <= p.S_cap || n <= R;
     };
+    // row of the tile's key r, then
+    auto row_of = [&](int s0, int r) { return s0 + r - (!PREFIX && s0 + r >= p.S_cap ? R : 0); };
     // the first of this warp's groups of eight rows; they take turns, so that the odd group falls to each of them
     auto first_group = [&](int tile) { return is_v ? (pw + tile) % NV : (pw + tile) % NK; };
     // words as they lie in the cache, row by row; rows behind the tile's last are zeros and nothing is read for them
     auto copy_rows = [&](uint32_t du, int tile, int j0, int n, bool run, int s0) {
-      const size_t first_byte = (size_t)s0 * (size_t)rb;
-      const unsigned char* run0 = src0 + (first_byte & ~(size_t)3);
-      const int head = (int)(first_byte & 3);
+      const long long b0 = (long long)s0 * rb, b1 = (long long)(s0 - R) * rb;      // where the tile's first row lies, and would lie for those behind the seam
+      const unsigned char *run0 = src0 + (b0 & ~3LL), *run1 = src0 + (b1 & ~3LL);
+      const int head0 = (int)(b0 & 3), head1 = (int)(b1 & 3);
 #pragma unroll 1
       for (int g = first_group(tile); g < WT_KT / 8; g += np) {
         const uint32_t dg = du + g * 1024;
         if (run) {
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
-            const int r = key_of(8 * g + c), bytes = r < n && RAP_BOUNDS(s0 + r, p.S_cap, p.status, 0x302) ? 4 : 0;
-            const unsigned char* src = run0 + (bytes ? (head + r * rb) & ~3 : 0);
+            const int r = key_of(8 * g + c), bytes = r < n && RAP_BOUNDS(row_of(s0, r), p.S_cap, p.status, 0x302) ? 4 : 0;
+            const bool seam = !PREFIX && bytes && s0 + r >= p.S_cap;
+            const unsigned char* src = (seam ? run1 : run0) + (bytes ? ((seam ? head1 : head0) + r * rb) & ~3 : 0);
             if (one) pt_cp4(dg + swz[c], src, bytes);
             if (two) pt_cp4(dg + swz[c] + 8192, src + 128, bytes);
           }
@@ -397,7 +401,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         for (int g = first_group(step - AHEAD); g < WT_KT / 8; g += np) {
           if (run) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) place(reinterpret_cast<uint32_t*>(vt + g * 1024 + swz[c]), (s0 + key_of(8 * g + c)) & 1);
+            for (int c = 0; c < 8; ++c) place(reinterpret_cast<uint32_t*>(vt + g * 1024 + swz[c]), row_of(s0, key_of(8 * g + c)) & 1);
           } else {
 #pragma unroll 1
             for (int c = 0; c < 8; ++c)
@@ -419,9 +423,9 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         const bool run = run_of(j0, n, s0);
         prefetch(tile + L2_AHEAD);
         if (!RAP_BOUNDS(n - 1, WT_KT, p.status, 0x304) || !RAP_BOUNDS(run ? s0 : 0, p.S_cap, p.status, 0x305) ||
-            !RAP_BOUNDS(run ? s0 + n - 1 : 0, p.S_cap, p.status, 0x306))
+            !RAP_BOUNDS(run ? row_of(s0, n - 1) : 0, p.S_cap, p.status, 0x306))
           break;
-        if (run && n == WT_KT) {
+        if (n == WT_KT && s0 + n <= p.S_cap) {
           // a full tile in one run: no predicates, running pointers (V: from key k to k + 8 and back to k + 1)
           const long long even = is_v ? 8LL * rb : rb, odd = is_v ? -7LL * rb : rb;
 #pragma unroll 1
@@ -646,11 +650,11 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       if (LSUM && n_my > 0) l_run = __uint_as_float(pt_ld1(tmem_o + lane_off + (uint32_t)p.dv));
       const float f = PREFIX ? 1.f : l_run != 0.f ? 1.f / l_run : 0.f;
       const int r_first = 128 * X + (warp & 3) * 32, r_n = min(32, n_rows - q0 - r_first);
-      const long long unit_head = (long long)first * p.Hq + (long long)h * G;
+      // this lane's row: its head's place behind that of the block's first token
+      const int my_t = row_t(r_first + lane), my_head = (my_t - t_base) * p.Hq + (q0 + r_first + lane - my_t * G);
+      const long long head0 = (long long)(first + t_base) * p.Hq + (long long)h * G;
       if (PREFIX && lane < r_n) {
-        const int t = row_t(r_first + lane);
-        const long long head = unit_head + (long long)t * p.Hq + (q0 + r_first + lane - t * G);
-        *p.ws.pre_pair(head, split) = make_float2(m_ref, l_run);
+        *p.ws.pre_pair(head0 + my_head, split) = make_float2(m_ref, l_run);
       }
 #pragma unroll 1
       for (int c0 = 0; c0 < p.dv; c0 += CC) {
@@ -667,14 +671,14 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         for (int c = 0; c < CC; ++c) o_s[lane * (CC + 1) + c] = some ? __uint_as_float(oc[c]) * f : 0.f;
         __syncwarp();
         const int n_c = min(CC, p.dv - c0);
+        float* dst0 = (PREFIX ? p.ws.pre_sums(head0, split) : p.out + head0 * p.dv) + c0 + lane;
+        const int dst_row = PREFIX ? p.ws.dv4 : p.dv;
 #pragma unroll 4
         for (int r = 0; r < r_n; ++r) {
-          const int t = row_t(r_first + r);
-          const long long head = unit_head + (long long)t * p.Hq + (q0 + r_first + r - t * G);
-          if (!RAP_BOUNDS(first + t, p.rows, p.status, 0x308) || !RAP_BOUNDS(split, PREFIX ? p.ws.n_pre : 1, p.status, 0x309)) break;
-          float* dst = (PREFIX ? p.ws.pre_sums(head, split) : p.out + head * p.dv) + c0;
-          if (lane < n_c) dst[lane] = o_s[r * (CC + 1) + lane];
-          if (lane + 32 < n_c) dst[lane + 32] = o_s[r * (CC + 1) + lane + 32];
+          if (!RAP_BOUNDS(first + row_t(r_first + r), p.rows, p.status, 0x308) || !RAP_BOUNDS(split, PREFIX ? p.ws.n_pre : 1, p.status, 0x309)) break;
+          float* dst = dst0 + (long long)__shfl_sync(0xffffffffu, my_head, r) * dst_row;
+          if (lane < n_c) dst[0] = o_s[r * (CC + 1) + lane];
+          if (lane + 32 < n_c) dst[32] = o_s[r * (CC + 1) + lane + 32];
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
