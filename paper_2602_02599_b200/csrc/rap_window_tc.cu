@@ -326,7 +326,14 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
 #pragma unroll 1
       for (int g = first_group(tile); g < WT_KT / 8; g += np) {
         const uint32_t dg = du + g * 1024;
-        if (run) {
+        if (HALF && n == WT_KT && s0 + n <= p.S_cap && RAP_BOUNDS(s0 + n - 1, p.S_cap, p.status, 0x302)) {      // no predicates
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const unsigned char* src = run0 + ((head0 + key_of(8 * g + c) * rb) & ~3);
+            if (one) wt_cp4(dg + swz[c], src);
+            if (two) wt_cp4(dg + swz[c] + 8192, src + 128);
+          }
+        } else if (run) {
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
             const int r = key_of(8 * g + c), bytes = r < n && RAP_BOUNDS(row_of(s0, r), p.S_cap, p.status, 0x302) ? 4 : 0;
@@ -368,6 +375,13 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       // the half from the lane behind in its place (no lane reads what another one copied).
       constexpr int AHEAD = 3;                         // below WT_STAGES - 1: the tile before the oldest unfinished one is never waited for
       int stg = 0, use = 0, fix = 0;
+      uint32_t keep[2], ones[2];                       // LSUM: the high half of a row's last word is the constant one
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bool last = LSUM && lane + 32 * i == words - 1;
+        keep[i] = last ? 0xffffu : ~0u;
+        ones[i] = last ? 0x3f800000u : 0u;
+      }
       for (int step = 0; step < n_max + AHEAD; ++step) {
         if (step < n_max) {
           int j0, j1, s0;
@@ -392,8 +406,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           const uint32_t n0 = __shfl_sync(0xffffffffu, v0, (lane + 1) & 31), n1 = __shfl_sync(0xffffffffu, v1, (lane + 1) & 31);
           v0 = __funnelshift_r(v0, lane == 31 ? n1 : n0, odd * 16);
           v1 = __funnelshift_r(v1, n1, odd * 16);
-          if (LSUM && lane == words - 1) v0 = (v0 & 0xffffu) | 0x3f800000u;
-          if (LSUM && lane + 32 == words - 1) v1 = (v1 & 0xffffu) | 0x3f800000u;
+          v0 = (v0 & keep[0]) | ones[0];
+          v1 = (v1 & keep[1]) | ones[1];
           if (one) w0[0] = v0;
           if (two) w0[2048] = v1;
         };
