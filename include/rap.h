@@ -370,7 +370,7 @@ rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, c
  *                            positions and their K / V rows are in the cache already.  Rows of d_out from d_row_start[B] on are
  *                            left as they were.  h_new_max bounds the new tokens of a sequence, h_seq_len_max d_seq_len.  For
  *                            bf16 stacks with 2P, d_v' <= 128 the softmax weights enter the product with V as two bf16 numbers
- *                            each, so they carry 16 bits or more (outputs are within 1e-5 of their size), and a V row that one query of a sequence's block sees and
+ *                            each, so they carry 16 bits or more, and a V row that one query of a sequence's block sees and
  *                            another does not must be finite; what no query sees may hold anything.
  *
  * ---- attention of a batch whose sequences share long prefixes -------------------------------------------------------
