@@ -10,8 +10,9 @@
 //   P_X  = 2^(S - m) one thread per row: 64 logits in registers, masked only in tiles that reach an edge, lazy running maximum;
 //                    every weight leaves as two bf16 numbers, its rounding and the remainder (17 bits: outputs are fp32 and one
 //                    bf16 would put 1e-3 of error on them), which fill the 64 columns that the logits came from.  Measured
-//                    against 64 bits 1.4e-6 ... 4.4e-6 of an output's size (7e-6 at 128 channels); a third bf16 number gave 2.4e-6 ... 4.3e-6 (the sums
-//                    in tensor memory are cut, not rounded, at every step, and it adds steps) and took 8 to 25% longer
+//                    against 64 bits 0.7e-6 ... 4.4e-6 of an output's size (7e-6 at 128 channels); a third bf16 number
+//                    left 2.4e-6 ... 4.3e-6 on long rows (the sums in tensor memory are cut, not rounded, at every step, and it
+//                    adds steps) and took 8 to 25% longer
 //   O_X += P_X V     A = P from tensor memory: eight steps of 16, the roundings' four and the remainders' four over the same V
 // Cache rows are not multiples of 16 bytes, so no tensor map describes them: six warps stage K and V with 4-byte cp.async
 // into rings of four and five 128-byte-swizzled tiles (K as stored is the K-major operand, V as stored the N-major one).  Odd d_v'
@@ -19,7 +20,7 @@
 // landed.  A rolling cache maps a position to its row; a tile is one run of rows, or two if it crosses the seam.
 // A K / V tile of 23 KB takes (4 P + 8 d_v') 64 cycles of the tensor pipe per 128 rows and 64 x 128 / 16 of the exponential
 // units: twice 576 and 512 cycles at P = 45.  Measured 2250 a tile: 8192 tokens at window 2048, 32 query heads, in 330 us (512
-// TFLOP/s of 2 (2P + d_v') a visible pair), the tensor pipe busy 44% of the time, the exponential units 40%, an issue slot 62%.
+// TFLOP/s of 2 (2P + d_v') a visible pair), the tensor pipe busy 43% of the time, the exponential units 39%, an issue slot 61%.
 // What bounds it is the softmax warps' stream of instructions (exponential, two conversions, two stores a logit) with the
 // 4-byte copies beside it; four warps instead of two on a scheduler (half a row a thread) took 17% longer, remainders through
 // shared memory 10%.  Few rows (prefixes of small groups, odd widths): the copies, 1300 to 2000 cycles a tile.
@@ -330,7 +331,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
     auto first_group = [&](int tile) { return is_v ? (pw + tile) % NV : (pw + tile) % NK; };
     // words as they lie in the cache, row by row; rows behind the tile's last are zeros and nothing is read for them
     auto copy_rows = [&](uint32_t du, int tile, int j0, int n, bool run, int s0) {
-      const long long b0 = (long long)s0 * rb, b1 = (long long)(s0 - R) * rb;      // where the tile's first row lies, and would lie for those behind the seam
+      // where the tile's first row lies, and where it would lie for the rows behind the seam
+      const long long b0 = (long long)s0 * rb, b1 = (long long)(s0 - R) * rb;
       const unsigned char *run0 = src0 + (b0 & ~3LL), *run1 = src0 + (b1 & ~3LL);
       const int head0 = (int)(b0 & 3), head1 = (int)(b1 & 3);
 #pragma unroll 1
