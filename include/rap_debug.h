@@ -56,6 +56,14 @@ rap_status rap_debug_arm_wait_timeout(rap_ctx* ctx);
  * which CTA ends up with which piece (a piece is a fixed range of tiles, and partials are merged in tile order). */
 rap_status rap_debug_set_scan_pieces(rap_ctx* ctx, int32_t piece_tiles, int32_t frac_x256);
 
+/* How the one-token scan of rap_decode_attn_window and rap_decode_attn_shared would share a batch among the CTAs of a GPU with
+ * sm_count SMs; a host-side calculation, the very code that the kernel runs.  h_blocks[b] >= 1: blocks of 32 rows that sequence b's
+ * new token sees; n_pre: partials of a shared prefix (0 .. 40); padded: rows of K and V are copied into padded rows (both of a
+ * multiple of 16 bytes, unless both of 128 or both of 256).  *most: CTAs that the most widely shared (sequence, KV head) falls
+ * to, each of which leaves a partial result; *places: how many there is room for. */
+rap_status rap_debug_window_plan(int32_t sm_count, int32_t B, int32_t n_kv_heads, const int32_t* h_blocks, int32_t n_pre, int32_t padded,
+                                 int32_t* most, int32_t* places);
+
 /* Shows that the index checks of the bounds-checking build (librap_b200_dbg.so, compiled with -DRAP_DEBUG_BOUNDS) are
  * live, without any access leaving a buffer: the next shape-specialised scan launch is told that the split-KV
  * workspace holds only n_floats floats (it is as large as ever).  In the bounds-checking build the writes of partials

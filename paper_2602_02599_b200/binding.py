@@ -27,7 +27,7 @@ EXPORTS = [
     "rap_get_last_device_status", "rap_kernel_launch_count", "rap_set_attn_variant",
     "rap_decode_attn_noalloc", "rap_profile_attn", "rap_profile_attn_read",
     "rap_pack_wo", "rap_out_proj", "rap_budget_alloc", "rap_prefill_attn", "rap_build_tables_hybrid",
-    "rap_build_tables_partial", "rap_build_tables_freq", "rap_set_proj_variant", "rap_debug_arm_wait_timeout", "rap_debug_claim_scan_workspace", "rap_debug_set_scan_pieces",
+    "rap_build_tables_partial", "rap_build_tables_freq", "rap_set_proj_variant", "rap_debug_arm_wait_timeout", "rap_debug_claim_scan_workspace", "rap_debug_set_scan_pieces", "rap_debug_window_plan",
     "rap_q8_row_bytes", "rap_quantize_rows", "rap_qkv_rope_append_q8", "rap_decode_attn_q8", "rap_decode_step_q8",
     "rap_q4_row_bytes", "rap_quantize_rows_q4", "rap_dequantize_rows_q4", "rap_read_cache_q4", "rap_qkv_rope_append_q4",
     "rap_decode_attn_q4", "rap_decode_step_q4",
@@ -90,6 +90,7 @@ def _lib():
     lib.rap_debug_arm_wait_timeout.argtypes = [P]
     lib.rap_debug_set_scan_pieces.argtypes = [P, c_int32, c_int32]
     lib.rap_debug_claim_scan_workspace.argtypes = [P, c_int64]
+    lib.rap_debug_window_plan.argtypes = [c_int32, c_int32, c_int32, P, c_int32, c_int32, P, P]
     lib.rap_q8_row_bytes.argtypes = [c_int32]
     lib.rap_q8_row_bytes.restype = c_size_t
     lib.rap_quantize_rows.argtypes = [P, c_int32, c_int64, c_int32, P, P, P]
@@ -170,6 +171,16 @@ def rap_budget_alloc(k_pair_scores, rho, head_dim):
     if s:
         raise RapError(s, "rap_budget_alloc")
     return n_pairs, n_vch
+
+
+def rap_debug_window_plan(sm_count, n_kv_heads, blocks, n_pre=0, padded=False):
+    """(most partials of a unit, places for them) of the one-token scan for sequences of so many blocks of 32 visible rows."""
+    n = np.ascontiguousarray(blocks, dtype=np.int32)
+    most, places = c_int32(), c_int32()
+    s = _lib().rap_debug_window_plan(sm_count, len(n), n_kv_heads, _ptr(n), n_pre, int(padded), byref(most), byref(places))
+    if s:
+        raise RapError(s, "rap_debug_window_plan")
+    return most.value, places.value
 
 
 def rap_q8_row_bytes(W):

@@ -107,6 +107,43 @@ __device__ __forceinline__ WinPrefixPlan win_prefix_plan(const int32_t* start, c
   return pl;
 }
 
+// How the one-token scan shares its blocks of 32 rows among the CTAs.  A unit (sequence, KV head) counts `own` blocks more than
+// the n that it has, ahead of them; T is the sum over all units, n_max the largest unit's count.  CTAs that hold blocks of a unit
+// leave a partial each, and there are RAP_MAX_SPLIT - n_pre places for them behind a shared prefix's, so the plan keeps every
+// unit on at most that many CTAs: with `share` blocks or more in each, n consecutive blocks touch at most (n - 2) / share + 2.
+// The host runs the same code (rap_debug_window_plan).
+struct WinScanPlan {
+  int nc;                // CTAs that have work
+  int parts;             // even: CTAs of each unit
+  int share, extra;      // otherwise: blocks of a CTA; the first `extra` CTAs have one more
+  bool even;
+  __host__ __device__ __forceinline__ int cta_of(int tile) const {      // whose share holds this block
+    const int mark = extra * (share + 1);
+    return tile < mark ? tile / (share + 1) : extra + (tile - mark) / share;
+  }
+};
+__host__ __device__ __forceinline__ WinScanPlan win_scan_plan(int T, int n_max, int units, int grid, int own, int n_pre, bool padded) {
+  WinScanPlan pl;
+  const int places = RAP_MAX_SPLIT - n_pre;
+  // every CTA has a block for each of its warps, and enough for the longest unit's partials to have a place
+  const int least = n_max - own > 2 ? (n_max - own - 2) / (places - 1) + 1 : 1;      // (n - 2) / least <= places - 2
+  int nc = (T + 3) >> 2;
+  nc = nc < grid ? nc : grid;
+  if (T / nc < least) nc = T / least;
+  // Units of about the same size (within a fifth of the largest): the same number of CTAs for each, so that no CTA ends two of
+  // them, if that leaves at most a quarter of the CTA slots empty -- HBM is as busy with those missing (32 sequences of 4096
+  // rows 65.9 -> 61.8 us; not with padded rows, which keep the SMs busier: 66 -> 71 us there).  Four blocks a CTA, as above.
+  int most_parts = (n_max - own) >> 2;
+  most_parts = most_parts < 1 ? 1 : most_parts < places - 2 ? most_parts : places - 2;
+  int parts = grid / units;
+  pl.even = parts >= 1 && !padded && (long long)n_max * units <= (long long)T + T / 5 && (parts > most_parts || units * parts * 4 >= grid * 3);
+  pl.parts = parts < most_parts ? parts : most_parts;
+  pl.nc = pl.even ? units * pl.parts : nc;
+  pl.share = T / pl.nc;
+  pl.extra = T - pl.share * pl.nc;
+  return pl;
+}
+
 __device__ __forceinline__ void win_report(int32_t* status, int code, int detail) {
   if (atomicCAS(&status[0], 0, code) == 0) status[1] = detail;
 }

@@ -24,7 +24,34 @@ const void* scan_fn(int n, int nw) {
 template <bool FOUR>
 const void* scan_tma_fn(int n) { return n == 4 ? (const void*)win_scan_kernel<4, FOUR, false, 4, true> : (const void*)win_scan_kernel<8, FOUR, false, 3, true>; }
 
+// what a unit's end takes, in blocks of half a microsecond: 3 us, or 10 with a prefix's splits to join
+int unit_end(int n_pre) { return n_pre ? 20 : 6; }
+
 }  // namespace
+
+rap_status rap_debug_window_plan(int32_t sm_count, int32_t B, int32_t n_kv_heads, const int32_t* h_blocks, int32_t n_pre, int32_t padded,
+                                 int32_t* most, int32_t* places) {
+  if (!h_blocks || !most || !places || sm_count < 1 || B < 1 || n_kv_heads < 1 || n_pre < 0 || n_pre > WIN_MAX_PRE) return RAP_EINVAL;
+  const int own = unit_end(n_pre);
+  long long T = 0;
+  int n_max = 1;
+  for (int b = 0; b < B; ++b) {
+    if (h_blocks[b] < 1 || h_blocks[b] > (1 << 26)) return RAP_EINVAL;      // 2^31 rows
+    T += (long long)(h_blocks[b] + own) * n_kv_heads;
+    if (h_blocks[b] + own > n_max) n_max = h_blocks[b] + own;
+  }
+  if (T > 0x7fffffffLL) return RAP_EINVAL;
+  const WinScanPlan plan = win_scan_plan((int)T, n_max, B * n_kv_heads, 2 * sm_count, own, n_pre, padded != 0);
+  *most = 0;
+  *places = RAP_MAX_SPLIT - n_pre;
+  for (int b = 0, start = 0; b < B; ++b)
+    for (int h = 0; h < n_kv_heads; ++h, start += h_blocks[b] + own) {
+      const int first = plan.cta_of(start + own), last = plan.cta_of(start + own + h_blocks[b] - 1);
+      const int n = plan.even ? (h_blocks[b] < plan.parts ? h_blocks[b] : plan.parts) : last - first + 1;
+      if (n > *most) *most = n;
+    }
+  return RAP_OK;
+}
 
 bool rap_win_scan_takes(const rap_win_args& a) {
   return a.dtype == RAP_BF16 && a.P2 >= 16 && a.P2 <= 128 && a.dv >= 16 && a.dv <= 128;
@@ -40,8 +67,7 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
   p.qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
   p.n_groups = a.n_groups; p.group_start = a.group_start; p.prefix_len = a.prefix_len; p.S_pre = a.S_pre; p.sms = ctx->sm_count;
   p.wait_limit = WAIT_LIMIT;
-  // what a unit's end takes, in blocks of half a microsecond: 3 us, or 10 with a prefix's splits to join
-  p.own = n_pre ? 20 : 6;
+  p.own = unit_end(n_pre);
   if (ctx->dbg_arm_timeout) {        // test hook (rap_debug_arm_wait_timeout)
     p.wait_limit = 4096;
     p.dbg_skip_copy = 1;

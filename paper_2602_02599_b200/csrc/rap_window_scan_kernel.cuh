@@ -152,28 +152,15 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
     T += __reduce_add_sync(0xffffffffu, n);
   }
   T *= p.Hkv;
-  // no unit is touched by more CTAs than there is room for partials behind the prefix's, and every CTA has a block for each warp
-  const int places = RAP_MAX_SPLIT - 2 - p.ws.n_pre;
-  int nc = min((int)gridDim.x, (T + 3) >> 2);
-  // ... (a unit of n_max blocks falls to at most n_max nc / T + 2 CTAs)
-  if (n_max > T / (int)gridDim.x * places) nc = (int)max(1LL, min((long long)nc, (long long)places * T / n_max));
-  // Units of about the same size (within a fifth of the largest): the same number of CTAs for each, so that no CTA ends two of
-  // them, if that leaves at most a quarter of the CTA slots empty -- HBM is as busy with those missing (32 sequences of 4096
-  // rows 65.9 -> 61.8 us; not with padded rows, which keep the SMs busier: 66 -> 71 us there).  Four blocks a CTA, as above.
-  const int units = p.B * p.Hkv, most_parts = min(places, max(1, (n_max - p.own) >> 2));
-  int parts = (int)gridDim.x / units;
-  const bool even = parts >= 1 && !p.pad16 && (long long)n_max * units <= (long long)T + T / 5 && (parts > most_parts || units * parts * 4 >= (int)gridDim.x * 3);
-  parts = min(parts, most_parts);
-  if (even) nc = units * parts;
+  const WinScanPlan plan = win_scan_plan(T, n_max, p.B * p.Hkv, (int)gridDim.x, p.own, p.ws.n_pre, p.pad16 != 0);
+  const bool even = plan.even;
+  const int nc = plan.nc, parts = plan.parts, share = plan.share, extra = plan.extra;
   if (blockIdx.x == 0)
     for (int i = tid; i < p.other_units; i += THREADS) p.unit_cnt_other[i] = 0;      // what a launch that gave up left behind
   if ((int)blockIdx.x >= nc) {
     if (p.ws.n_pre) pdl_wait();     // a launch is not over before the one that it overlaps
     return;
   }
-  // the first T % nc CTAs take one block more than the others
-  const int share = T / nc, extra = T - share * nc, mark = extra * (share + 1);
-  auto cta_of = [&](int tile) { return tile < mark ? tile / (share + 1) : extra + (tile - mark) / share; };   // whose share holds this block
   int cur = (int)blockIdx.x * share + min((int)blockIdx.x, extra);
   int hi = cur + share + ((int)blockIdx.x < extra ? 1 : 0);
   int b = 0, h, unit_start = 0;
@@ -536,9 +523,9 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
       my_seg = u.n < parts ? t0 : (int)blockIdx.x - my_unit * parts;      // fewer blocks than CTAs: one each, the others none
       n_seg = min(u.n, parts);
     } else {
-      const int first = cta_of(unit_start + p.own);
+      const int first = plan.cta_of(unit_start + p.own);
       my_seg = (int)blockIdx.x - first;
-      n_seg = cta_of(unit_start + p.own + u.n - 1) - first + 1;
+      n_seg = plan.cta_of(unit_start + p.own + u.n - 1) - first + 1;
     }
     const bool alone = n_seg == 1 && n_pre == 0;
     const int dv4 = p.ws.dv4;
@@ -575,7 +562,7 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
         joined = true;
         // The partials' sums come in as bulk copies, one round trip for all that fit the stages (all units' partials but the
         // largest): the prefix's split by split, the own ones in one run.  Their weights are worked out meanwhile.
-        const int n = n_pre + n_seg, part = G * dv4;                 // n <= RAP_MAX_SPLIT
+        const int n = n_pre + n_seg, part = G * dv4;                 // n <= RAP_MAX_SPLIT by the plan
         float* sums = reinterpret_cast<float*>(smem + p.off_stage);
         float* wgt = red;                          // [G][RAP_MAX_SPLIT] weights over their sum
         auto fetch = [&](int s0, int m) {          // warp 0: partials [s0, s0 + m)

@@ -653,3 +653,28 @@ def test_shared_prefixes_of_many_rows_a_split(pairs, vch, group):
     shared(H, [6400, 6399, 6337, 6400, 4097, 4096, 6400, 6400], [1] * 8, [0, 3, 1, 40, 7, 0, 64, 9], 6400, 64)
     H.clean()
     H.close()
+
+
+@pytest.mark.parametrize("kv,lens,shape", [
+    (2, [16384, 4096], (45, 90, 4)), (2, [16384, 4096], (48, 96, 4)), (4, [16860, 999, 364], (45, 90, 4)), (4, [3230, 14656], (58, 115, 3)),
+    (2, [8224], (48, 96, 4)), (4, [8224], (48, 96, 4)), (2, [8704], (48, 96, 5)), (4, [9120], (48, 96, 2)),
+    (2, [128, 6976, 96, 448, 3264, 9152], (64, 128, 4)), (4, [1696, 9504], (32, 64, 8))])
+def test_decode_long_units(kv, lens, shape):
+    """Few units, one far longer than the others: as many CTAs share it as there are places for partials."""
+    pairs, vch, group = shape
+    H = W.Heads(kv, group, pairs, vch, "bf16", len(lens))
+    s_cap = (max(lens) + 7) // 8 * 8
+    for order in (lens, lens[::-1]):
+        W.check(*decode(H, order, 0, s_cap, s_cap))
+    H.clean()
+    H.close()
+
+
+@pytest.mark.parametrize("kv,prefix,lens,shape", [(4, 1280, [248, 5744], (45, 90, 4)), (2, 640, [96, 160, 7328, 3904, 96, 7360], (45, 90, 4)),
+                                                  (4, 1280, [248, 5744], (48, 96, 4)), (2, 4000, [9000], (48, 96, 3))])
+def test_shared_long_units(kv, prefix, lens, shape):
+    pairs, vch, group = shape
+    H = W.Heads(kv, group, pairs, vch, "bf16", len(lens))
+    shared(H, [prefix], [len(lens)], lens, prefix, (max(lens) + 7) // 8 * 8)
+    H.clean()
+    H.close()

@@ -76,3 +76,38 @@ def test_refusals_before_any_device_call(lib):
         assert lib.rap_decode_attn_shared(ctx, 0, 1, a[0], 1, a[1], a[2], 16, a[3], None, 8, a[5], a[6], 16, a[7], 8, a[8], None) == E
     finally:
         lib.rap_destroy(ctx)
+
+
+def blocks(rows):
+    return [max(1, (n + 31) // 32) for n in rows]
+
+
+# (KV heads, visible rows, partials of a prefix, rows of K and V both of a multiple of 16 bytes)
+LONG_UNITS = [(2, [16384, 4096], 0, False), (2, [16384, 4096], 0, True), (4, [16860, 999, 364], 0, False), (4, [3230, 14656], 0, False),
+              (2, [8224], 0, True), (4, [8224], 0, True), (2, [8704], 0, True), (4, [9120], 0, True), (4, [248, 5744], 20, False),
+              (2, [128, 6976, 96, 448, 3264, 9152], 0, False), (2, [96, 160, 7328, 3904, 96, 7360], 10, False), (4, [1696, 9504], 0, False)]
+
+
+@pytest.mark.parametrize("kv,rows,n_pre,padded", LONG_UNITS)
+def test_every_partial_has_a_place(lib, kv, rows, n_pre, padded):
+    most, places = binding.rap_debug_window_plan(148, kv, blocks(rows), n_pre, padded)
+    assert 1 <= most <= places == 64 - n_pre
+
+
+def test_every_partial_has_a_place_in_random_batches(lib):
+    """Batches of every kind: alike, spread over the logarithm, a long sequence among short ones at either end."""
+    r = np.random.RandomState(11)
+    for i in range(30000):
+        kv, B = r.randint(1, 17), int(np.exp(r.uniform(0, np.log(60))))
+        most_rows = np.exp(r.uniform(0, np.log(65536)))
+        rows = np.exp(r.uniform(0, np.log(most_rows + 1), B)).astype(int) if i % 3 else np.full(B, int(most_rows)) - r.randint(0, 40, B)
+        if i % 3 == 2:
+            rows[r.choice([0, B - 1])] = int(np.exp(r.uniform(np.log(2000), np.log(65536))))
+        n_pre = r.choice([0, 0, r.randint(1, 41)])
+        most, places = binding.rap_debug_window_plan(r.choice([148, 148, 132, 7]), kv, blocks(np.maximum(rows, 0)), n_pre, i % 2)
+        assert 1 <= most <= places, (kv, rows.tolist(), n_pre, i % 2)
+    for bad in ([], [0], [2 ** 27]):
+        with pytest.raises(binding.RapError):
+            binding.rap_debug_window_plan(148, 8, bad)
+    with pytest.raises(binding.RapError):
+        binding.rap_debug_window_plan(148, 8, [4], n_pre=41)
