@@ -346,7 +346,7 @@ rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, c
  * so a cache with S_cap >= the longest length holds position p in row p, and a shorter one is a rolling cache: the rows
  * behind the sinks are used again and again, and lengths are not bounded by S_cap.  A rolling cache needs S_cap - n_sink
  * >= window + new - 1, new being the most tokens that are appended before they attend (RAP_ECAPACITY where h_seq_len_max >
- * S_cap and it is smaller).  n_sink < S_cap.
+ * S_cap and it is smaller).  n_sink < S_cap; the attention calls take caches of up to 2^31 - 72 rows (RAP_ESHAPE beyond).
  *
  *   rap_build_slots          the rows of a ragged batch, from the request lengths, on the GPU: sequence b has d_seq_len[b]
  *                            tokens cached and d_new_len[b] >= 0 new ones.  Rows are numbered sequence by sequence:

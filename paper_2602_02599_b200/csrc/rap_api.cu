@@ -758,6 +758,8 @@ rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, c
 }
 
 // ---- windows with sinks, shared prefixes, slot maps ---------------------------------------------------------------------------
+constexpr int32_t WIN_MAX_ROWS = 0x7fffffff - 71;      // rows of a cache: the kernels count up to 64 beyond the last one in 32 bits
+
 static rap_win_args win_args(const rap_ctx* ctx, int32_t layer) {
   const rap_model_desc& d = ctx->desc;
   rap_win_args a = {};
@@ -800,7 +802,7 @@ rap_status rap_decode_attn_window(rap_ctx* ctx, int32_t layer, int32_t B, const 
   const rap_model_desc& d = ctx->desc;
   if (layer < 0 || layer >= d.n_layers || B < 0 || S_cap < 1 || h_seq_len_max < 0 || n_sink < 0 || window < 1 || n_sink >= S_cap)
     return RAP_EINVAL;
-  if (B > d.max_batch) return RAP_ESHAPE;
+  if (B > d.max_batch || S_cap > WIN_MAX_ROWS) return RAP_ESHAPE;
   if (S_cap % 8) return RAP_EALIGN;
   if (h_seq_len_max > S_cap && window > S_cap - n_sink) return RAP_ECAPACITY;
   if (!rap_aligned16(d_q) || !rap_aligned16(d_k_cache) || !rap_aligned16(d_v_cache) || !rap_aligned16(d_out) ||
@@ -824,7 +826,7 @@ rap_status rap_prefill_attn_window(rap_ctx* ctx, int32_t layer, int32_t B, int32
   if (layer < 0 || layer >= d.n_layers || B < 0 || T < 0 || S_cap < 1 || h_new_max < 0 || h_seq_len_max < h_new_max || n_sink < 0 ||
       window < 1 || n_sink >= S_cap)
     return RAP_EINVAL;
-  if (B > d.max_batch) return RAP_ESHAPE;
+  if (B > d.max_batch || S_cap > WIN_MAX_ROWS) return RAP_ESHAPE;
   if (S_cap % 8) return RAP_EALIGN;
   if (h_seq_len_max > S_cap && (long long)window + h_new_max - 1 > S_cap - n_sink) return RAP_ECAPACITY;
   if (!rap_aligned16(d_q) || !rap_aligned16(d_k_cache) || !rap_aligned16(d_v_cache) || !rap_aligned16(d_out) ||
@@ -849,7 +851,7 @@ rap_status rap_decode_attn_shared(rap_ctx* ctx, int32_t layer, int32_t B, const 
   const rap_model_desc& d = ctx->desc;
   if (layer < 0 || layer >= d.n_layers || B < 0 || n_groups < 1 || S_cap_prefix < 1 || h_prefix_len_max < 0 || S_cap < 1 || h_seq_len_max < 0)
     return RAP_EINVAL;
-  if (B > d.max_batch) return RAP_ESHAPE;
+  if (B > d.max_batch || S_cap > WIN_MAX_ROWS || S_cap_prefix > WIN_MAX_ROWS) return RAP_ESHAPE;
   if (S_cap % 8 || S_cap_prefix % 8) return RAP_EALIGN;
   if (h_seq_len_max > S_cap || h_prefix_len_max > S_cap_prefix) return RAP_ECAPACITY;
   if (!rap_aligned16(d_q) || !rap_aligned16(d_k_prefix) || !rap_aligned16(d_v_prefix) || !rap_aligned16(d_group_start) ||

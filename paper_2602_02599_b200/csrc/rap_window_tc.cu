@@ -410,7 +410,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
         int j0, j1, s0;
         tile_at(step - AHEAD, j0, j1);
-        const bool run = run_of(j0, min(WT_KT, j1 - j0), s0);
+        const int n = min(WT_KT, j1 - j0);
+        const bool run = run_of(j0, n, s0);
         unsigned char* vt = ring + fix * WT_KV_BYTES;
         // (without a branch on the row's parity: eight rows' loads, shuffles and stores then overlap)
         auto place = [&](uint32_t* w0, int odd) {
@@ -431,7 +432,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
           } else {
 #pragma unroll 1
             for (int c = 0; c < 8; ++c)
-              place(reinterpret_cast<uint32_t*>(vt + g * 1024 + 128 * c + pt_swz2(4 * lane, c)), win_slot(j0 + key_of(8 * g + c), p.n_sink, p.S_cap) & 1);
+              place(reinterpret_cast<uint32_t*>(vt + g * 1024 + 128 * c + pt_swz2(4 * lane, c)), win_slot(j0 + min(key_of(8 * g + c), n - 1), p.n_sink, p.S_cap) & 1);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -588,8 +589,9 @@ __global__ void __launch_bounds__(WT_THREADS, 1) win_tc_kernel(const WtParams p)
         if (active) {
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           // nothing of the tile is hidden from any row of this query tile
-          const bool whole = PREFIX ? j0 + WT_KT <= j1
-                                    : tile >= n_st && j0 + WT_KT - 1 <= p_min && j0 > p_max - p.window && j0 + WT_KT <= j1;
+          // (differences: positions end at 2^31 - 2)
+          const bool whole = PREFIX ? j1 - j0 >= WT_KT
+                                    : tile >= n_st && p_min - j0 >= WT_KT - 1 && p_max - j0 < p.window && j1 - j0 >= WT_KT;
           if (!whole) {
             // the few tiles at an edge: hidden logits become -infinity (weight 0) where they are, so that the tiles' common path
             // knows no mask.  Seen are columns [0, c1), without those behind the sinks and before the window

@@ -678,3 +678,33 @@ def test_shared_long_units(kv, prefix, lens, shape):
     shared(H, [prefix], [len(lens)], lens, prefix, (max(lens) + 7) // 8 * 8)
     H.clean()
     H.close()
+
+
+@pytest.mark.parametrize("pairs,vch,group,dtype", [(45, 90, 4, "bf16"), (58, 115, 3, "bf16"), (64, 128, 5, "bf16"), (45, 90, 4, "f32")])
+@pytest.mark.parametrize("end", [2 ** 31 - 1, 2 ** 31 - 40, 2 ** 31 - 64])
+def test_prefill_at_the_last_positions(end, pairs, vch, group, dtype):
+    """Rolling caches bound no length: blocks that end right below 2^31."""
+    H = W.Heads(2, group, pairs, vch, dtype, 4)
+    new = [130, 1, 0, 70]
+    prefill(H, [end - n for n in new], new, 4, 100, 240, pad=2)
+    prefill(H, [end - n for n in new], new, 0, 33, 168)
+    H.clean()
+    H.close()
+
+
+def test_caches_of_too_many_rows_are_refused():
+    """Rows and the blocks that reach beyond the last one are counted in 32 bits."""
+    H = W.Heads(2, 4, 45, 90, "bf16", 2)
+    K, V = H.caches(2, 64)
+    q, out, n, s = H.query(2), H.out(2, fill=1.0), H.ints([0, 0]), H.ints([0, 1, 2])
+    most, S = 2 ** 31 - 72, binding.RAP_ESHAPE
+    for rows in (most + 8, 2 ** 31 - 8):
+        refused(S, H.ctx.rap_decode_attn_window, 0, 2, q, K, V, rows, n, 0, 0, 8, out)
+        refused(S, H.ctx.rap_prefill_attn_window, 0, 2, 2, q, K, V, rows, s, n, 1, 1, 0, 8, out)
+        refused(S, H.ctx.rap_decode_attn_shared, 0, 2, q, 1, K, V, rows, s, n, 0, K, V, 64, n, 0, out)
+        refused(S, H.ctx.rap_decode_attn_shared, 0, 2, q, 1, K, V, 64, s, n, 0, K, V, rows, n, 0, out)
+    assert (out == 1.0).all()
+    H.ctx.rap_decode_attn_window(0, 2, q, K, V, most, n, 0, 0, 8, out)      # nothing is seen, nothing is read
+    assert (out == 0.0).all()
+    H.clean()
+    H.close()
