@@ -14,7 +14,7 @@ LIB_DBG = os.path.join(HERE, "librap_b200_dbg.so")      # the same sources with 
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["rap_api.cu", "rap_proj.cu", "rap_proj_tc.cu", "rap_attn.cu", "rap_attn_fast.cu", "rap_attn_scan.cu",
            "rap_lowrank.cu", "rap_lowrank_tc.cu", "rap_prefill.cu", "rap_prefill_tc.cu", "rap_q8.cu", "rap_q4.cu", "rap_window.cu",
-           "rap_window_scan.cu", "rap_window_tc.cu"]
+           "rap_window_scan.cu", "rap_window_scan_long.cu", "rap_window_tc.cu"]
 SCAN_PARTS = 8      # translation units the scan kernel's instantiations are spread over
 
 

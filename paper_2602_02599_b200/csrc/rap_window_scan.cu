@@ -1,28 +1,19 @@
 // Launch side of win_scan_kernel (rap_window_scan_kernel.cuh).
 #include "rap_window_scan_kernel.cuh"
 
+const void* rap_win_scan_long_fn(int G, bool vodd, bool tma, int n, int nw);      // rap_window_scan_long.cu
+
 namespace {
 
-template <bool FOUR, bool VODD>
-const void* scan_fn(int n, int nw) {
-  switch (n * 8 + nw) {
-    case 1 * 8 + 4: return (const void*)win_scan_kernel<1, FOUR, VODD, 4, false>;
-    case 2 * 8 + 4: return (const void*)win_scan_kernel<2, FOUR, VODD, 4, false>;
-    case 3 * 8 + 4: return (const void*)win_scan_kernel<3, FOUR, VODD, 4, false>;
-    case 4 * 8 + 4: return (const void*)win_scan_kernel<4, FOUR, VODD, 4, false>;
-    case 5 * 8 + 4: return (const void*)win_scan_kernel<5, FOUR, VODD, 4, false>;
-    case 6 * 8 + 4: return (const void*)win_scan_kernel<6, FOUR, VODD, 4, false>;
-    case 6 * 8 + 3: return (const void*)win_scan_kernel<6, FOUR, VODD, 3, false>;
-    case 7 * 8 + 4: return (const void*)win_scan_kernel<7, FOUR, VODD, 4, false>;
-    case 7 * 8 + 3: return (const void*)win_scan_kernel<7, FOUR, VODD, 3, false>;
-    case 8 * 8 + 2: return (const void*)win_scan_kernel<8, FOUR, VODD, 2, false>;      // unpruned heads, seven or eight to a KV head
-    case 8 * 8 + 3: return (const void*)win_scan_kernel<8, FOUR, VODD, 3, false>;
-  }
-  return nullptr;
+// About how many blocks of a unit one warp can get, from what the host knows: every unit as long as the bounds allow
+long long most_blocks(const WsParams& p, const rap_win_args& a, int n_pre, int grid, int nw) {
+  const long long rows = a.n_groups ? a.h_len_max : (long long)(a.h_len_max < a.window ? a.h_len_max : a.window) + a.n_sink;
+  const long long n = (rows + 31) / 32 + 3, units = (long long)a.B * a.Hkv;      // a run begins and ends inside a block
+  const long long share = units < grid ? n / (grid / units) : n;                  // by units of a size ...
+  const long long least = n / (RAP_MAX_SPLIT - n_pre - 3);                        // ... and for all partials to have places
+  const long long cta = (share > least ? share : least) + 2;
+  return ((cta < n ? cta : n) + nw - 1) / nw;
 }
-
-template <bool FOUR>
-const void* scan_tma_fn(int n) { return n == 4 ? (const void*)win_scan_kernel<4, FOUR, false, 4, true> : (const void*)win_scan_kernel<8, FOUR, false, 3, true>; }
 
 // what a unit's end takes, in blocks of half a microsecond: 3 us, or 10 with a prefix's splits to join
 int unit_end(int n_pre) { return n_pre ? 20 : 6; }
@@ -111,10 +102,10 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
     p.join_places = nw * WS_STAGES * p.stage_bytes / (4 * p.G * p.ws.dv4);      // partials that fit the stages
     if (smem <= SMEM_BUDGET || nw == 2) break;
   }
-  const void* fn = p.G <= 4 ? (vodd ? scan_fn<true, true>(n, nw) : scan_fn<true, false>(n, nw)) : (vodd ? scan_fn<false, true>(n, nw) : scan_fn<false, false>(n, nw));
+  const bool sums_long = most_blocks(p, a, n_pre, 2 * ctx->sm_count, nw) > WS_LONG;
+  const void* fn = sums_long ? rap_win_scan_long_fn(p.G, vodd, tma, n, nw) : scan_any<false>(p.G, vodd, tma, n, nw);
   alignas(64) unsigned char map_k[128] = {0}, map_v[128] = {0};      // CUtensorMap images (the other forms ignore them)
   if (tma) {
-    fn = p.G <= 4 ? scan_tma_fn<true>(n) : scan_tma_fn<false>(n);
     if (!rap_tensor_map_bf16(ctx, map_k, a.k, (uint64_t)cache_rows, (uint64_t)a.P2, 32) ||
         !rap_tensor_map_bf16(ctx, map_v, a.v, (uint64_t)cache_rows, (uint64_t)a.dv, 32))
       return RAP_EUNSUPPORTED;

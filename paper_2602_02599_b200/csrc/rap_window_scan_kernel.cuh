@@ -117,9 +117,13 @@ __device__ __forceinline__ int ws_scan_add(int x, int lane) {      // inclusive 
 // NW: warps.  A short launch executes most of this once a CTA, so what it costs is fetching it: divisions by run-time numbers
 // and 64-bit ones are kept out of the usual path.
 constexpr int WS_STAGES = 2;
+// LONG: for launches in which a warp may add up more than WS_LONG blocks of a unit.  The MMA cuts its sums where it adds them, it
+// does not round them, which takes 1e-6 of a sum for every thousand rows (2.3e-6 where V has one sign), so here they leave the
+// accumulators every WS_DRAIN blocks for the warp's part of the buffer that the warps' sums meet in, added there in fp32.
+constexpr int WS_LONG = 64, WS_DRAIN = 32;
 // TMA: rows of exactly 32 N bytes (K and V) through tensor maps, N = 4 or 8: panels of 32 rows x 128 bytes, the 16-byte chunk c
 // of row r at chunk c ^ (r % 8)
-template <int N, bool FOUR, bool VODD, int NW, bool TMA>
+template <int N, bool FOUR, bool VODD, int NW, bool TMA, bool LONG>
 __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, const __grid_constant__ CUtensorMap map_k,
                                                               const __grid_constant__ CUtensorMap map_v) {
   static_assert(!TMA || N % 4 == 0, "whole panels");
@@ -329,6 +333,17 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[cb][e][r] = 0.f;
     float m_ref = -INFINITY, l_thr = 0.f;
+    float* red_w = red + (size_t)warp * G * CW;                  // this warp's sums [G][CW]
+    float* rr = red_w + (size_t)(head < G ? head : 0) * CW;
+    const bool holds = (FOUR ? gid < 4 : true) && head < G;     // this lane holds sums of its head
+    // sum r (of two) of a block of channels over the three bf16 numbers of the weights.  Remainders of either sign times an
+    // infinity of V would be NaN: the roundings' sum says what it is
+    auto whole_sum = [&](const float (&oc)[4], int r) {
+      float rest = oc[r + 2];
+      if (FOUR) rest += __shfl_down_sync(0xffffffffu, oc[r], 16);
+      const float t = oc[r] + rest;
+      return t != t && fabsf(oc[r]) == INFINITY ? oc[r] : t;
+    };
 
     for (int i = 0; i < n_blk; ++i) {
       if (i + 1 < n_blk) issue_block(i + 1, st ^ 1);
@@ -477,11 +492,45 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
       __syncwarp();            // every lane is done with this stage before it is filled again
       used = true;
       if (++st == NSTG) { st = 0; parity ^= 1u; }
+
+      if (LONG && (i % WS_DRAIN == WS_DRAIN - 1 || i + 1 == n_blk)) {      // rr and l_s, relative to m_s
+        const bool more = i >= WS_DRAIN;
+        const float m_old = more ? m_s[warp * 8 + gid] : m_ref, wt = m_old == m_ref ? 1.f : ws_ex2(m_old - m_ref);
+        l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 1);
+        l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 2);
+        if (more) l_thr = fmaf(l_s[warp * 8 + gid], wt, l_thr);
+        __syncwarp();
+        if (tq == 0) {
+          l_s[warp * 8 + gid] = l_thr;
+          m_s[warp * 8 + gid] = m_ref;
+        }
+        l_thr = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < N; ++cb) {
+          const int c0 = min(16 * cb, c_last) + 4 * tq;        // four channels; those before 16 cb are the last block's too
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const bool mine = holds && c0 + 2 * r >= 16 * cb;
+            float2* at = reinterpret_cast<float2*>(rr + c0 + 2 * r);
+            float2 x = make_float2(0.f, 0.f);
+            if (mine && more) x = *at;
+            x = make_float2(fmaf(x.x, wt, whole_sum(o[cb][0], r)), fmaf(x.y, wt, whole_sum(o[cb][1], r)));
+            if (mine) *at = x;
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[cb][0][r] = o[cb][1][r] = 0.f;
+        }
+        __syncwarp();
+      }
     }
 
     // ---- the warps' sums together: common maximum per head ----
-    l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 1);
-    l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 2);
+    if constexpr (LONG) {
+      l_thr = n_blk > 0 ? l_s[warp * 8 + gid] : 0.f;
+    } else {
+      l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 1);
+      l_thr += __shfl_xor_sync(0xffffffffu, l_thr, 2);
+    }
     if (timed_out && lane == 0) *s_flag = 1;
     if (tq == 0) m_s[warp * 8 + gid] = m_ref;
     __syncthreads();
@@ -501,21 +550,23 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
     for (int i = 0; i < NW; ++i) m_all = fmaxf(m_all, m_s[i * 8 + gid]);
     const float f = m_ref == -INFINITY ? 0.f : ws_ex2(m_ref - m_all);
     if (tq == 0) l_s[warp * 8 + gid] = l_thr * f;
-    float* rr = red + ((size_t)warp * G + (head < G ? head : 0)) * CW;
+    if constexpr (LONG) {
+      for (int g = 0; g < G; ++g) {
+        const float fg = __shfl_sync(0xffffffffu, f, 4 * g);
+        for (int c = lane; c < CW; c += 32) red_w[g * CW + c] = n_blk > 0 ? red_w[g * CW + c] * fg : 0.f;
+      }
+    } else {
 #pragma unroll
-    for (int cb = 0; cb < N; ++cb) {
-      const int c0 = min(16 * cb, c_last) + 4 * tq;
+      for (int cb = 0; cb < N; ++cb) {
+        const int c0 = min(16 * cb, c_last) + 4 * tq;
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float rest = o[cb][e][r + 2];
-          if (FOUR) rest += __shfl_down_sync(0xffffffffu, o[cb][e][r], 16);
-          // remainders of either sign times an infinity of V would be NaN: the roundings' sum says what it is
-          float t = o[cb][e][r] + rest;
-          if (t != t && fabsf(o[cb][e][r]) == INFINITY) t = o[cb][e][r];
-          if ((FOUR ? gid < 4 : true) && head < G) rr[c0 + 2 * r + e] = t * f;
-        }
+          for (int e = 0; e < 2; ++e) {
+            const float t = whole_sum(o[cb][e], r);
+            if (holds) rr[c0 + 2 * r + e] = t * f;
+          }
+      }
     }
     __syncthreads();
     int my_seg, n_seg;             // this CTA's place among those that hold blocks of the unit, and how many they are
@@ -668,6 +719,35 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
     __syncthreads();           // the sums and weights in shared memory have been read
   }
   if (p.ws.n_pre) pdl_wait();
+}
+
+// The form for G query heads a KV head, odd d_v' or not, rows through tensor maps or not, n steps of 16, nw warps
+template <bool FOUR, bool VODD, bool LONG>
+const void* scan_fn(int n, int nw) {
+  switch (n * 8 + nw) {
+    case 1 * 8 + 4: return (const void*)win_scan_kernel<1, FOUR, VODD, 4, false, LONG>;
+    case 2 * 8 + 4: return (const void*)win_scan_kernel<2, FOUR, VODD, 4, false, LONG>;
+    case 3 * 8 + 4: return (const void*)win_scan_kernel<3, FOUR, VODD, 4, false, LONG>;
+    case 4 * 8 + 4: return (const void*)win_scan_kernel<4, FOUR, VODD, 4, false, LONG>;
+    case 5 * 8 + 4: return (const void*)win_scan_kernel<5, FOUR, VODD, 4, false, LONG>;
+    case 6 * 8 + 4: return (const void*)win_scan_kernel<6, FOUR, VODD, 4, false, LONG>;
+    case 6 * 8 + 3: return (const void*)win_scan_kernel<6, FOUR, VODD, 3, false, LONG>;
+    case 7 * 8 + 4: return (const void*)win_scan_kernel<7, FOUR, VODD, 4, false, LONG>;
+    case 7 * 8 + 3: return (const void*)win_scan_kernel<7, FOUR, VODD, 3, false, LONG>;
+    case 8 * 8 + 2: return (const void*)win_scan_kernel<8, FOUR, VODD, 2, false, LONG>;      // unpruned heads, seven or eight to a KV head
+    case 8 * 8 + 3: return (const void*)win_scan_kernel<8, FOUR, VODD, 3, false, LONG>;
+  }
+  return nullptr;
+}
+
+template <bool FOUR, bool LONG>
+const void* scan_tma_fn(int n) { return n == 4 ? (const void*)win_scan_kernel<4, FOUR, false, 4, true, LONG> : (const void*)win_scan_kernel<8, FOUR, false, 3, true, LONG>; }
+
+template <bool LONG>
+const void* scan_any(int G, bool vodd, bool tma, int n, int nw) {
+  if (tma) return G <= 4 ? scan_tma_fn<true, LONG>(n) : scan_tma_fn<false, LONG>(n);
+  if (G <= 4) return vodd ? scan_fn<true, true, LONG>(n, nw) : scan_fn<true, false, LONG>(n, nw);
+  return vodd ? scan_fn<false, true, LONG>(n, nw) : scan_fn<false, false, LONG>(n, nw);
 }
 
 }  // namespace

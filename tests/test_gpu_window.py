@@ -708,3 +708,83 @@ def test_caches_of_too_many_rows_are_refused():
     assert (out == 0.0).all()
     H.clean()
     H.close()
+
+
+@pytest.mark.parametrize("offset", [0.0, 1.0])
+@pytest.mark.parametrize("pairs,vch,group,n", [(45, 90, 4, 65536), (64, 128, 5, 40000), (58, 115, 3, 40000), (48, 96, 8, 50000)])
+def test_decode_many_rows_a_warp(pairs, vch, group, n, offset):
+    """More units than there are CTAs, so that a warp sums a quarter of a unit's rows (of 40,000 to 65,536) alone; V of zero mean
+    and around one."""
+    B = 40
+    H = W.Heads(8, group, pairs, vch, "bf16", B)
+    K, V = H.randn(B, 8, n, 2 * pairs), H.randn(B, 8, n, vch)
+    V += offset
+    q, out = H.query(B), H.out(B)
+    lens = [n - 37 * b for b in range(B)]
+    H.ctx.rap_decode_attn_window(0, B, q, K, V, n, H.ints(lens), n, 0, 2 ** 31 - 1, out)
+    for b in (0, 1, B // 2, B - 1):
+        W.check(out[b], *H.reference(q[b], [(K, V, b, range(lens[b]))]))
+    H.clean()
+    H.close()
+
+
+@pytest.mark.parametrize("pairs,vch,group", [(45, 90, 4), (58, 115, 3), (64, 128, 4), (32, 64, 8), (48, 96, 5), (9, 17, 6), (16, 33, 2), (64, 127, 6), (64, 128, 7), (8, 128, 1)])
+def test_decode_long_sums_at_every_border(pairs, vch, group):
+    """A launch whose bounds allow many rows a warp, with units of every length: none, one row, and around the blocks after which
+    sums leave the accumulators."""
+    lens = [9000, 0, 1, 31, 33, 100, 3073, 4063, 4064, 4065, 4095, 4096, 4097, 4127, 4129, 4191, 4193, 4223, 4225, 6144, 6145, 8190, 8192, 8193,
+            8225, 8256, 8257, 8289, 8321, 8449, 8999, 700, 2048, 5000, 0, 12, 7777, 128, 129, 64]
+    H = W.Heads(8, group, pairs, vch, "bf16", len(lens))
+    W.check(*decode(H, lens, 3, 10 ** 6, 9000))
+    H.clean()
+    H.close()
+
+
+def test_decode_long_sums_of_special_values():
+    B, n = 40, 9000
+    H = W.Heads(8, 4, 45, 90, "bf16", B)
+    K, V, q = H.randn(B, 8, n, 90), H.randn(B, 8, n, 90), H.query(B)
+    K[0, 1, 5000, 3] = math.nan
+    V[1, 0, 41, 5] = math.inf                          # before sums have left the accumulators, and behind
+    V[2, 0, 8900, 76] = -math.inf
+    V[3, 7, 8950, 89] = math.inf
+    K[4, :, n - 40:] = math.inf                        # not seen
+    V[4, :, n - 40:] = math.nan
+    out, lens = H.out(B), [n] * 4 + [n - 40] * 36
+    H.ctx.rap_decode_attn_window(0, B, q, K, V, n, H.ints(lens), n, 0, n, out)
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[0, 4:8] = True
+    bad[1, :4, 5] = bad[2, :4, 76] = bad[3, 28:, 89] = True
+    assert torch.equal(~torch.isfinite(out), bad)
+    assert torch.isnan(out[0, 4:8]).all() and (out[1, :4, 5] == math.inf).all() and (out[2, :4, 76] == -math.inf).all() and (out[3, 28:, 89] == math.inf).all()
+    W.check(out[4], *H.reference(q[4], [(K, V, 4, range(n - 40))]))
+    H.clean()
+    H.close()
+
+
+@pytest.mark.parametrize("rising", [False, True])
+def test_decode_maxima_that_move_over_many_rows(rising):
+    """The largest logits in the last rows, or in the first."""
+    B, n = 40, 20000
+    for pairs, vch, group in ((45, 90, 4), (64, 128, 8)):
+        H = W.Heads(8, group, pairs, vch, "bf16", B)
+        slope = torch.linspace(0.2, 8.0, n, device=H.device)[:, None]
+        K = torch.empty((B, 8, n, 2 * pairs), dtype=H.dt, device=H.device)
+        for b in range(B):
+            K[b] = (H.randn(8, n, 2 * pairs).float() * (slope if rising else slope.flip(0))).to(H.dt)
+        V, q, out = H.randn(B, 8, n, vch), H.query(B), H.out(B)
+        H.ctx.rap_decode_attn_window(0, B, q, K, V, n, H.ints([n] * B), n, 0, n, out)
+        for b in (0, 17, B - 1):
+            want, bound = H.reference(q[b], [(K, V, b, range(n))])
+            assert ((out[b] - want).abs() <= bound).all()
+        H.clean()
+        H.close()
+
+
+def test_shared_long_sums():
+    """Many own rows behind a prefix."""
+    for pairs, vch, group in ((45, 90, 4), (48, 96, 3)):
+        H = W.Heads(8, group, pairs, vch, "bf16", 40)
+        shared(H, [500, 0, 1300], [20, 1, 19], [9000 - 300 * (b % 30) for b in range(40)], 1304, 9000)
+        H.clean()
+        H.close()

@@ -22,10 +22,10 @@ def test_edge_cases_pass_with_every_index_checked():
     assert " passed" in r.stdout and "failed" not in r.stdout
 
 
-def test_long_units_pass_with_every_index_checked():
+def test_long_sequences_pass_with_every_index_checked():
     from paper_2602_02599_b200 import build
     env = dict(os.environ, RAP_LIBRARY=build.build_debug())
-    r = subprocess.run([sys.executable, "-m", "pytest", os.path.join(ROOT, "tests", "test_gpu_window.py"), "-m", "gpu", "-x", "-q", "-k", "long_units"],
+    r = subprocess.run([sys.executable, "-m", "pytest", os.path.join(ROOT, "tests", "test_gpu_window.py"), "-m", "gpu", "-x", "-q", "-k", "long_units or long_sums or last_positions"],
                        cwd=ROOT, env=env, capture_output=True, text=True, timeout=1500)
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
     assert " passed" in r.stdout and "failed" not in r.stdout
