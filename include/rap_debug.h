@@ -47,6 +47,11 @@ rap_status rap_set_proj_variant(rap_ctx* ctx, int32_t variant);
  * rap_decode_attn_window and rap_decode_attn_shared takes it the same way, whichever is launched next. */
 rap_status rap_debug_arm_wait_timeout(rap_ctx* ctx);
 
+/* The same for the waits in which the scan of rap_decode_attn_window and rap_decode_attn_shared joins a unit's partial results:
+ * in the next launch of it every join waits for 16 bytes more than it copies and gives up.  The CTA records RAP_ETIMEOUT, waits
+ * (bounded) once more, for the copies that are on their way, and returns; units that are split stay unfinished. */
+rap_status rap_debug_arm_join_timeout(rap_ctx* ctx);
+
 /* The tensor-core scan of rap_decode_attn (head shapes of the shaped workloads: the five retain ratios at D = 128,
  * 3 to 5 query heads per KV head) normally decides by the size of a launch whether its last tiles are handed
  * out at run time (pieces of some tiles, claimed from a counter by the CTAs as they finish) or assigned up front like

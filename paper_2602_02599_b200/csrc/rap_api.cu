@@ -87,6 +87,12 @@ rap_status rap_debug_arm_wait_timeout(rap_ctx* ctx) {
   return RAP_OK;
 }
 
+rap_status rap_debug_arm_join_timeout(rap_ctx* ctx) {
+  if (!ctx) return RAP_EINVAL;
+  ctx->dbg_arm_join = 1;
+  return RAP_OK;
+}
+
 rap_status rap_debug_set_scan_pieces(rap_ctx* ctx, int32_t piece_tiles, int32_t frac_x256) {
   if (!ctx || piece_tiles < -1 || frac_x256 < 0 || frac_x256 > 256) return RAP_EINVAL;
   ctx->dbg_dyn_piece = piece_tiles;

@@ -69,6 +69,7 @@ struct rap_ctx {
   int32_t attn_variant = 0;
   long long dbg_ws_floats = 0;    // > 0: the next scan launch is told its workspace holds only this many floats (rap_debug.h)
   int32_t dbg_dyn_piece = -1, dbg_dyn_frac = 0;   // test hook: pieces claimed at run time, forced (-1: the launcher decides; rap_debug.h)
+  int32_t dbg_arm_join = 0;       // the next windowed / shared-prefix scan's joins run into bounded waits on purpose (rap_debug.h)
   int32_t dbg_arm_timeout = 0;    // the next tensor-core scan launch runs into a bounded wait on purpose (rap_debug.h)
   int32_t proj_variant = 0;       // 1: rap_qkv_rope_append always takes the two-stage path (GEMM, then the epilogue kernel)
   int64_t launches = 0;

@@ -64,6 +64,11 @@ rap_status rap_launch_win_scan(rap_ctx* ctx, const rap_win_args& a, int n_pre, c
     p.dbg_skip_copy = 1;
     ctx->dbg_arm_timeout = 0;
   }
+  if (ctx->dbg_arm_join) {           // test hook (rap_debug_arm_join_timeout)
+    p.wait_limit = 4096;
+    p.dbg_lost_bytes = 16;
+    ctx->dbg_arm_join = 0;
+  }
   {   // two sets of counters take turns; each launch clears the one its predecessor used
     const size_t n_units = (size_t)ctx->desc.max_batch * ctx->desc.n_kv_heads;
     const uint32_t set = ctx->win_epoch++ & 1u;

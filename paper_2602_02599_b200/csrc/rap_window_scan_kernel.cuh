@@ -49,6 +49,7 @@ struct WsParams {
   int join_places;            // partials that the stages hold together
   uint32_t wait_limit;
   int dbg_skip_copy;          // test hook: the first unit's first block is armed and not copied
+  int dbg_lost_bytes;         // test hook: a join waits for so many bytes more than it copies
   // shared prefixes (ws.n_pre > 0): what the plan of their splits is made of
   int n_groups, S_pre, sms;
   const int32_t* group_start;
@@ -619,7 +620,7 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
         auto fetch = [&](int s0, int m) {          // warp 0: partials [s0, s0 + m)
           if (lane == 0) {
             asm volatile("fence.proxy.async;" ::: "memory");        // the stages have been read; other CTAs' partials are acquired
-            mbar_expect_tx(bar_join, (uint32_t)(m * part * 4));
+            mbar_expect_tx(bar_join, (uint32_t)(m * part * 4 + p.dbg_lost_bytes));
           }
           __syncwarp();
           for (int s = s0 + lane; s < min(s0 + m, n_pre); s += 32)
@@ -662,8 +663,8 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
         for (int s0 = 0;;) {
           __syncthreads();
           got = __syncthreads_and(mbar_wait_bounded(bar_join, join_parity, p.wait_limit));
-          join_parity ^= 1u;
           if (!got) break;
+          join_parity ^= 1u;
 #pragma unroll
           for (int k = 0; k < COLS; ++k) {
             const int i = 4 * (tid + k * THREADS);
@@ -686,8 +687,12 @@ __global__ void __launch_bounds__(32 * NW, 2) win_scan_kernel(const WsParams p, 
           if (warp == 0) fetch(s0, m);
         }
         if (!got) {
-          if (tid == 0) win_report(p.status, RAP_ETIMEOUT, (int)unit);
+          if (tid == 0) {
+            win_report(p.status, RAP_ETIMEOUT, (int)unit);
+            mbar_wait_bounded(bar_join, join_parity, p.wait_limit);      // copies still in flight: as above
+          }
           if (p.ws.n_pre) pdl_wait();
+          __syncthreads();
           return;
         }
 #pragma unroll

@@ -788,3 +788,34 @@ def test_shared_long_sums():
         shared(H, [500, 0, 1300], [20, 1, 19], [9000 - 300 * (b % 30) for b in range(40)], 1304, 9000)
         H.clean()
         H.close()
+
+
+@pytest.mark.parametrize("pairs,vch", [(45, 90), (64, 128), (48, 96)])
+def test_a_join_that_runs_out_is_reported(pairs, vch):
+    """Joins that wait for more than is copied: the launch ends, says so, and the next ones are right again."""
+    H = W.Heads(2, 4, pairs, vch, "bf16", 3)
+    K, V, q = H.randn(3, 2, 2048, 2 * pairs), H.randn(3, 2, 2048, vch), H.query(3)
+    lens, start, plen = H.ints([2000, 30, 1900]), H.ints([0, 3]), H.ints([700])
+    window = [H.reference(q[b], [(K, V, b, W.seen(n - 1, 4, 1500))]) for b, n in enumerate(lens.tolist())]
+    behind = [H.reference(q[b], [(K, V, 0, range(700)), (K, V, b, range(n))]) for b, n in enumerate(lens.tolist())]
+
+    def call(prefix):
+        out = H.out(3)
+        if prefix:
+            H.ctx.rap_decode_attn_shared(0, 3, q, 1, K, V, 2048, start, plen, 700, K, V, 2048, lens, 2000, out)
+        else:
+            H.ctx.rap_decode_attn_window(0, 3, q, K, V, 2048, lens, 2000, 4, 1500, out)
+        return out
+
+    for prefix in (False, True):
+        H.ctx.rap_debug_arm_join_timeout()
+        call(prefix)
+        assert H.ctx.rap_get_last_device_status()[0] == binding.RAP_ETIMEOUT
+        H.ctx.rap_debug_arm_join_timeout()
+        call(prefix)                                     # counters left behind, and not asked for
+        for again in (True, False, True):
+            want = behind if again else window
+            W.check(call(again), torch.stack([w[0] for w in want]), torch.stack([w[1] for w in want]))
+        assert H.ctx.rap_get_last_device_status()[0] == binding.RAP_ETIMEOUT
+    H.clean()
+    H.close()
