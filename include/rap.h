@@ -370,8 +370,11 @@ rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, c
  *                            positions and their K / V rows are in the cache already.  Rows of d_out from d_row_start[B] on are
  *                            left as they were.  h_new_max bounds the new tokens of a sequence, h_seq_len_max d_seq_len.  For
  *                            bf16 stacks with 2P, d_v' <= 128 the softmax weights enter the product with V as two bf16 numbers
- *                            each, so they carry 16 bits or more, and a V row that one query of a sequence's block sees and
- *                            another does not must be finite; what no query sees may hold anything.
+ *                            each, so they carry 16 bits or more, and up to 2560 rows at a time are summed in tensor memory, which
+ *                            cuts a sum at every step (together 4e-6 to 7e-6 of an output's size; 1.1e-5 at 128 channels where V
+ *                            is of one sign).  In these stacks a V row that a query of a sequence's block sees must be finite: an
+ *                            infinity comes out as an infinity or NaN, in its channel of the block's queries of that KV head,
+ *                            whether they see the row or not.  What no query sees may hold anything.
  *
  * ---- attention of a batch whose sequences share long prefixes -------------------------------------------------------
  *   rap_decode_attn_shared   one new token of every sequence.  Sequences d_group_start[n] .. d_group_start[n + 1] - 1 form group
@@ -379,10 +382,11 @@ rap_status rap_prefill_attn(rap_ctx* ctx, int32_t layer, int32_t B, int32_t T, c
  *                            (0 .. h_prefix_len_max <= S_cap_prefix) first rows of d_k_prefix / d_v_prefix
  *                            [n_groups][H_kv][S_cap_prefix][W], caches like any other; sequence b's own rows follow them and lie
  *                            in rows 0 .. d_seq_len[b] - 1 of d_k_cache / d_v_cache (0 is allowed; d_seq_len counts the row just
- *                            appended).  The result is that of rap_decode_attn over both, one behind the other; a prefix is
- *                            read once for all its sequences (for up to 256 / G of them at a time).  The own rows' positions
- *                            begin at d_prefix_len[n]: append them with d_pos_base.  bf16 stacks with 2P, d_v' <= 128 take the
- *                            prefix's softmax weights as two bf16 numbers each, as above.
+ *                            appended).  The result is that of rap_decode_attn over both, one behind the other.  The own rows'
+ *                            positions begin at d_prefix_len[n]: append them with d_pos_base.  bf16 stacks with 16 <= 2P, d_v' <=
+ *                            128 read a prefix once for all its sequences (for up to 256 / G of them at a time) and take its
+ *                            softmax weights as two bf16 numbers each; a prefix's V rows must be finite there, as above (an
+ *                            infinity in an own row gives an infinity).  All other stacks read a prefix once for every sequence.
  * Partial results and arrival counters live in the context, so calls on one context must not overlap on the GPU (captured
  * graphs of one context neither).  No call allocates or synchronizes; all may be captured.  All types and head shapes of the
  * library are accepted.  RAP_EINVAL when the current device is not the context's. */

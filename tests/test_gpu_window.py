@@ -819,3 +819,87 @@ def test_a_join_that_runs_out_is_reported(pairs, vch):
         assert H.ctx.rap_get_last_device_status()[0] == binding.RAP_ETIMEOUT
     H.clean()
     H.close()
+
+
+@pytest.mark.parametrize("pairs,vch,group,dtype", [(45, 90, 4, "bf16"), (58, 115, 3, "bf16"), (64, 128, 4, "bf16"), (45, 90, 4, "f32")])
+def test_special_values_in_blocks(pairs, vch, group, dtype):
+    """A NaN in a K row reaches the queries that see it, an infinity in a V row its channel: as an infinity in fp32; in bf16, where
+    a weight is a rounding and a remainder, as an infinity if the remainder is positive and as NaN (inf - inf, or 0 inf) if not, and
+    for queries of the block that do not see the row too.  What no query sees may hold anything."""
+    H = W.Heads(2, group, pairs, vch, dtype, 3)
+    n_sink, window, s_cap = 4, 60, 400
+    new, past = [70, 40, 5], [100, 60, 300]
+    K, V = H.randn(3, 2, s_cap, 2 * pairs), H.randn(3, 2, s_cap, vch)
+    K[0, 1, 120, 3] = math.nan
+    V[1, 0, 80, 5] = math.inf
+    K[2, :, 5:240], V[2, :, 5:240] = math.nan, -math.inf
+    K[:, :, 305:], V[:, :, 305:] = math.inf, math.nan
+    T, start, lens = sum(new), [0, 70, 110, 115], [p + n for p, n in zip(past, new)]
+    q, out = H.query(T), H.out(T)
+    H.ctx.rap_prefill_attn_window(0, 3, T, q, K, V, s_cap, H.ints(start), H.ints(lens), max(new), max(lens), n_sink, window, out)
+    for b in range(3):
+        for i in range(new[b]):
+            pos, o = past[b] + i, out[start[b] + i]
+            rows = W.seen(pos, n_sink, window)
+            want, bound = H.reference(q[start[b] + i], [(K, V, b, rows)])
+            good = torch.ones_like(o, dtype=torch.bool)
+            if b == 0 and 120 in rows:
+                assert torch.isnan(o[group:]).all()
+                good[group:] = False
+            if b == 1 and (80 in rows or dtype == "bf16"):
+                assert 80 not in rows or ((o[:group, 5] == math.inf) if dtype == "f32" else ~torch.isfinite(o[:group, 5])).all()
+                good[:group, 5] = False
+            assert torch.isfinite(o[good]).all() and ((o - want).abs() <= bound + 1e-30)[good].all()
+    H.clean()
+    H.close()
+
+
+@pytest.mark.parametrize("pairs,vch,group,dtype", [(45, 90, 4, "bf16"), (58, 115, 3, "bf16"), (64, 128, 4, "bf16"), (45, 90, 4, "f32")])
+def test_special_values_behind_prefixes(pairs, vch, group, dtype):
+    """The same of a prefix: a NaN in K reaches its group's outputs of that KV head, an infinity in V its channel, as an infinity
+    (fp32) or that or NaN (bf16); in a sequence's own rows it gives an infinity, in rows that are not seen nothing."""
+    H = W.Heads(2, group, pairs, vch, dtype, 5)
+    prefix, groups, lens = [200, 333], [3, 2], [9, 0, 40, 33, 5]
+    KP, VP = H.randn(2, 2, 400, 2 * pairs), H.randn(2, 2, 400, vch)
+    K, V, q, out = H.randn(5, 2, 64, 2 * pairs), H.randn(5, 2, 64, vch), H.query(5), H.out(5)
+    VP[0, 1, 70, 7] = math.inf
+    KP[1, 0, 332, 1] = math.nan
+    V[2, 0, 39, 9] = -math.inf
+    for n, p in enumerate(prefix):
+        KP[n, :, p:], VP[n, :, p:] = math.nan, math.inf
+    for b, n in enumerate(lens):
+        K[b, :, n:], V[b, :, n:] = math.inf, math.nan
+    H.ctx.rap_decode_attn_shared(0, 5, q, 2, KP, VP, 400, H.ints([0, 3, 5]), H.ints(prefix), 333, K, V, 64, H.ints(lens), 40, out)
+    for b in range(5):
+        n = 0 if b < 3 else 1
+        want, bound = H.reference(q[b], [(KP, VP, n, range(prefix[n])), (K, V, b, range(lens[b]))])
+        good = torch.ones_like(out[b], dtype=torch.bool)
+        if n == 0:
+            hit = out[b][group:, 7]
+            assert ((hit == math.inf) if dtype == "f32" else ~torch.isfinite(hit)).all()
+            good[group:, 7] = False
+        else:
+            assert torch.isnan(out[b][:group]).all()
+            good[:group] = False
+        if b == 2:
+            assert (out[b][:group, 9] == -math.inf).all()
+            good[:group, 9] = False
+        assert torch.isfinite(out[b][good]).all() and ((out[b] - want).abs() <= bound + 1e-30)[good].all()
+    H.clean()
+    H.close()
+
+
+def test_far_rows_behind_a_prefix():
+    """A prefix whose group lies behind 2^31 numbers and 2^32 bytes of its cache, and own rows as far."""
+    H = W.Heads(2, 2, 64, 128, "bf16", 2)
+    cap = 9 * 2 ** 20
+    K, V = [torch.empty((2, 2, cap, 128), dtype=torch.bfloat16, device=H.device) for _ in range(2)]
+    for c in (K, V):
+        H.fill(c, 1, range(700))
+        H.fill(c, 0, range(40))
+    q, out = H.query(2), H.out(2)
+    H.ctx.rap_decode_attn_shared(0, 2, q, 2, K, V, cap, H.ints([0, 1, 2]), H.ints([3, 700]), 700, K, V, cap, H.ints([40, 500]), 500, out)
+    for b, p in enumerate((3, 700)):
+        W.check(out[b], *H.reference(q[b], [(K, V, b, range(p)), (K, V, b, range((40, 500)[b]))]))
+    H.clean()
+    H.close()
