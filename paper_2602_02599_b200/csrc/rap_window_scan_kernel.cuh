@@ -17,8 +17,9 @@
 //   * The running maximum is raised only when a logit exceeds it by more than 8 (in log2 units).
 //   * A unit that several CTAs share leaves one partial (sums, maximum, weight) each; who delivers the last one joins them in
 //     order, so a result does not depend on who that is.  The prefix of rap_decode_attn_shared comes as partials too.
-// Measured: 32 sequences of up to 4100 rows, 8 KV heads, P = 45, d_v' = 90 (332 MB) in 56 us, 5.9 TB/s; one sequence in 10.5 us,
-// which is latency: plan 2, first copy 2, three blocks a warp 2, arrival and join 3.
+// Measured (replayed from a graph; 1 to 3 us more a call made by itself): 32 sequences of up to 4100 rows, 8 KV heads, P = 45,
+// d_v' = 90 (332 MB) in 56.5 us, 5.8 TB/s; one sequence in 11.4 us, which is latency: plan 2, first copy 2, three blocks a warp 2,
+// arrival and join 3.
 #pragma once
 #include <cuda.h>
 
@@ -120,7 +121,9 @@ __device__ __forceinline__ int ws_scan_add(int x, int lane) {      // inclusive 
 constexpr int WS_STAGES = 2;
 // LONG: for launches in which a warp may add up more than WS_LONG blocks of a unit.  The MMA cuts its sums where it adds them, it
 // does not round them, which takes 1e-6 of a sum for every thousand rows (2.3e-6 where V has one sign), so here they leave the
-// accumulators every WS_DRAIN blocks for the warp's part of the buffer that the warps' sums meet in, added there in fp32.
+// accumulators every WS_DRAIN blocks for the warp's part of the buffer that the warps' sums meet in, added there in fp32.  40
+// sequences of 65,536 rows: 1.4e-5 -> 1.3e-6 of the output (3.7e-5 -> 1.6e-6).  Times within 4% of the other form's there;
+// short launches would take 1 to 3 us more in it.
 constexpr int WS_LONG = 64, WS_DRAIN = 32;
 // TMA: rows of exactly 32 N bytes (K and V) through tensor maps, N = 4 or 8: panels of 32 rows x 128 bytes, the 16-byte chunk c
 // of row r at chunk c ^ (r % 8)

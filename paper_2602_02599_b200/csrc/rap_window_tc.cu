@@ -10,7 +10,8 @@
 //   P_X  = 2^(S - m) one thread per row: 64 logits in registers, masked only in tiles that reach an edge, lazy running maximum;
 //                    every weight leaves as two bf16 numbers, its rounding and the remainder (17 bits: outputs are fp32 and one
 //                    bf16 would put 1e-3 of error on them), which fill the 64 columns that the logits came from.  Measured
-//                    against 64 bits 0.7e-6 ... 4.4e-6 of an output's size (7e-6 at 128 channels); a third bf16 number
+//                    against 64 bits 0.7e-6 ... 5.9e-6 of an output's size (7e-6 at 128 channels; 7.5e-6 and 1.1e-5
+//                    where V is of one sign); a third bf16 number
 //                    left 2.4e-6 ... 4.3e-6 on long rows (the sums in tensor memory are cut, not rounded, at every step, and it
 //                    adds steps) and took 8 to 25% longer
 //   O_X += P_X V     A = P from tensor memory: eight steps of 16, the roundings' four and the remainders' four over the same V
@@ -19,9 +20,9 @@
 // (HALF): every other row starts in the middle of a word, so V's words are copied as they lie and put in place when they have
 // landed.  A rolling cache maps a position to its row; a tile is one run of rows, or two if it crosses the seam.
 // A K / V tile of 23 KB takes (4 P + 8 d_v') 64 cycles of the tensor pipe per 128 rows and 64 x 128 / 16 of the exponential
-// units: twice 576 and 512 cycles at P = 45.  Measured 2250 a tile: 8192 tokens at window 2048, 32 query heads, in 330 us (512
-// TFLOP/s of 2 (2P + d_v') a visible pair), the tensor pipe busy 43% of the time, the exponential units 39%, an issue slot 61%.
-// What bounds it is the softmax warps' stream of instructions (exponential, two conversions, two stores a logit) with the
+// units: twice 576 and 512 cycles at P = 45.  Measured 2250 a tile: 8192 tokens at window 2048, 32 query heads, in 330 us replayed
+// from a graph and 358 a call by itself (512 and 473 TFLOP/s of 2 (2P + d_v') a visible pair), the tensor pipe busy 43% of the
+// time, the exponential units 39%, an issue slot 61%.  What bounds it is the softmax warps' stream of instructions (exponential, two conversions, two stores a logit) with the
 // 4-byte copies beside it; four warps instead of two on a scheduler (half a row a thread) took 17% longer, remainders through
 // shared memory 10%.  Few rows (prefixes of small groups, odd widths): the copies, 1300 to 2000 cycles a tile.
 // Roles meet on mbarriers only; every wait is bounded and gives up early once another role has given up.
